@@ -380,6 +380,89 @@ int ubp_block_scores(const float *W, int M, int C, int R, int Nb, void *workspac
 int ubp_bed_select(const float *W, int M, int C, int R, int Nb, int64_t m, void *workspace, size_t workspace_bytes,
                    uint8_t *mask, int64_t *n_selected, void *stream);
 
+/* ---------------------------------------------- token-major operators
+ * A block-pruned linear layer of a language model: the same blob (R == 1, blocks of Nb consecutive output features at
+ * one input feature), activations with one token per row, in 16 or 8 bits, one token to many. The feed-forward block
+ *     h = x + r, q = norm(h)     ubp_rmsnorm (8-bit rows with a scale each)
+ *     a = act(G q) * (U q)       ubp_linear, gated plan
+ *     p = a in 8 bits            ubp_quant_rows
+ *     y = D p + h                ubp_linear with a residual
+ * is four calls. Strides (ld*) are in elements between the rows of consecutive tokens; rows are contiguous. T == 0 is a
+ * no-op. Pointers need the alignment of their element type only; 16-byte aligned rows are faster. Infinities and NaNs in
+ * a row stay in that row's outputs. */
+typedef enum {
+    UBP_F32 = 0,
+    UBP_F16 = 1,
+    UBP_BF16 = 2,
+    UBP_E4M3 = 3          /* 8-bit float, 4 exponent and 3 mantissa bits, largest value 448, with a scale beside it */
+} ubp_dtype;
+
+typedef enum {
+    UBP_ACT_NONE = 0,
+    UBP_ACT_RELU = 1,
+    UBP_ACT_GELU = 2,         /* 0.5 v (1 + erf(v / sqrt 2)) */
+    UBP_ACT_GELU_TANH = 3,    /* 0.5 v (1 + tanh(sqrt(2 / pi) (v + 0.044715 v^3))) */
+    UBP_ACT_SILU = 4          /* v / (1 + e^-v) */
+} ubp_act;
+
+/* ubp_rmsnorm: for each of T rows of C values
+ *     h = x + residual  (residual may be NULL: h = x)
+ *     y = h * gamma / sqrt(mean(h^2) + eps)
+ * x, residual, h have type `dtype` (UBP_F32, UBP_F16, UBP_BF16); gamma [C] has that type or UBP_F32. h (nullable) receives
+ * the sum rounded to `dtype` (the norm itself uses the unrounded sum); it may be x's or residual's own buffer with the same
+ * stride. y_dtype is `dtype`, or UBP_E4M3: then scales[t] = max(max |y| / 448, 2^-126) and the row holds
+ * e4m3(y / scales[t]), rounded to nearest even; a row of zeros has scale 2^-126 and codes 0. Arithmetic and statistics are
+ * fp32. scales is ignored for other output types.
+ * Errors: UBP_E_ARG (null, types, sizes, a stride below C, a misaligned pointer), UBP_E_UNSUPPORTED (more than 2^31 row
+ * groups), UBP_E_CUDA. */
+int ubp_rmsnorm(const void *x, int64_t ldx, const void *residual, int64_t ldr, const void *gamma, int gamma_dtype, int dtype,
+                int64_t T, int C, float eps, void *h, int64_t ldh, void *y, int64_t ldy, int y_dtype, float *scales,
+                void *stream);
+
+/* ubp_quant_rows: each of T rows of C values of type `dtype` -> UBP_E4M3 codes q and scales[t], as above with y = x. */
+int ubp_quant_rows(const void *x, int64_t ldx, int dtype, int64_t T, int C, void *q, int64_t ldq, float *scales, void *stream);
+
+/* Plan of a token-major product. `dtype` is the type of weights and activations: UBP_BF16, UBP_F16 (the blob's fp32 weights
+ * are rounded to nearest even) or UBP_E4M3 (each weight row is divided by its own scale max(max |w| / 448, 2^-126) and
+ * rounded; the scales are part of the plan). gated != 0: the layer is [gate; up] with M / 2 rows each (M even) and the
+ * product returns act(gate) * up. The device image holds the layer twice: the kept blocks (few tokens, bound by reading the
+ * weights) and a densified matrix (many tokens, tensor cores).
+ * Same division of labour as ubp_plan_*: size and image are host only, the caller owns dev_buf (256-byte aligned), the
+ * upload is one cudaMemcpyAsync on `stream`. Errors as there; UBP_E_UNSUPPORTED for R != 1, more than 65536 input
+ * features or 2^31 entries. */
+typedef struct ubp_linear_plan ubp_linear_plan_t;
+int ubp_linear_plan_size(const void *blob, size_t len, int dtype, int gated, size_t *dev_bytes);
+/* geom receives {nbk, nslab, Mp, Kp, bytes per value}; offs the byte offsets of {row scales, entry offsets, channel
+ * indices, weights, dense matrix} in the image. */
+int ubp_linear_plan_image(const void *blob, size_t len, int dtype, int gated, void *host_buf, size_t cap, int32_t geom[5],
+                          int64_t offs[5]);
+int ubp_linear_plan_build(const void *blob, size_t len, int dtype, int gated, void *dev_buf, size_t dev_bytes, void *stream,
+                          ubp_linear_plan_t **plan);
+void ubp_linear_plan_free(ubp_linear_plan_t *plan);
+/* as ubp_plan_check / ubp_plan_clear_status */
+int ubp_linear_plan_check(const ubp_linear_plan_t *plan, void *stream);
+int ubp_linear_plan_clear_status(const ubp_linear_plan_t *plan, void *stream);
+
+/* ubp_linear: for T tokens
+ *     z[t][o] = sum_k W[o][k] x[t][k]  (* x_scales[t] * row scale[o] under an 8-bit plan)  + bias[o]
+ *     y[t][o] = act(z[t][o]) + residual[t][o]                             plain plan, F = M features
+ *     y[t][f] = act(z[t][f]) * z[t][F + f] + residual[t][f]               gated plan, F = M / 2 features
+ *   x         device, the plan's type, [T][C];  x_scales device fp32 [T], required under an 8-bit plan, else NULL
+ *   bias      device fp32 [M] or NULL;  act a ubp_act
+ *   residual  device [T][F] in y's type or NULL; may be y itself (same pointer and stride)
+ *   y         device [T][F], y_dtype: the plan's type or UBP_F32 under a 16-bit plan; UBP_BF16, UBP_F16 or UBP_F32 under
+ *             an 8-bit one
+ *   workspace device, 16-byte aligned, at least ubp_linear_workspace_size(...) bytes of it (0: may be NULL)
+ * Products and sums are fp32 (8-bit products are exact in fp32), everything after the sum is fp32, y is rounded once. Sums
+ * run in a fixed order: results are bitwise reproducible. Up to a few tokens the kept blocks are multiplied on the CUDA
+ * cores; from there on the densified weight on the tensor cores. y must not overlap x; with residual == y each element is
+ * read before it is written.
+ * Errors: UBP_E_ARG, UBP_E_SPACE (workspace), UBP_E_UNSUPPORTED, UBP_E_CUDA. */
+size_t ubp_linear_workspace_size(const ubp_linear_plan_t *plan, const void *x, int64_t ldx, int64_t T);
+int ubp_linear(const ubp_linear_plan_t *plan, const void *x, int64_t ldx, const float *x_scales, int64_t T, const float *bias,
+               int act, const void *residual, int64_t ldr, void *y, int64_t ldy, int y_dtype, void *workspace,
+               size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -85,6 +85,18 @@ def load():
     L.ubp_bed_workspace_size.argtypes = [i32, i32, i32, C.POINTER(sz)]
     L.ubp_block_scores.argtypes = [vp, i32, i32, i32, i32, vp, sz, vp, vp]
     L.ubp_bed_select.argtypes = [vp, i32, i32, i32, i32, i64, vp, sz, vp, vp, vp]
+    L.ubp_rmsnorm.argtypes = [vp, i64, vp, i64, vp, i32, i32, i64, i32, C.c_float, vp, i64, vp, i64, i32, vp, vp]
+    L.ubp_quant_rows.argtypes = [vp, i64, i32, i64, i32, vp, i64, vp, vp]
+    L.ubp_linear_plan_size.argtypes = [vp, sz, i32, i32, C.POINTER(sz)]
+    L.ubp_linear_plan_image.argtypes = [vp, sz, i32, i32, vp, sz, C.POINTER(C.c_int32), C.POINTER(i64)]
+    L.ubp_linear_plan_build.argtypes = [vp, sz, i32, i32, vp, sz, vp, C.POINTER(vp)]
+    L.ubp_linear_plan_free.argtypes = [vp]
+    L.ubp_linear_plan_free.restype = None
+    L.ubp_linear_plan_check.argtypes = [vp, vp]
+    L.ubp_linear_plan_clear_status.argtypes = [vp, vp]
+    L.ubp_linear_workspace_size.argtypes = [vp, vp, i64, i64]
+    L.ubp_linear_workspace_size.restype = sz
+    L.ubp_linear.argtypes = [vp, vp, i64, vp, i64, vp, i32, vp, i64, vp, i64, i32, vp, sz, vp]
     _lib = L
     return L
 
@@ -500,4 +512,238 @@ def ubp_bed_select(W, Nb: int, m: int, stream=None):
     sel = _selector_for(W, Nb)
     out = sel.select(W, m, stream=stream)
     torch.cuda.synchronize(W.device)
+    return out
+
+
+# ------------------------------------------------------------------ token-major operators (language-model layers)
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+_DTYPES = None
+
+
+def _dtypes():
+    """torch dtype -> ubp_dtype (built on first use: importing the package does not import torch)."""
+    global _DTYPES
+    if _DTYPES is None:
+        import torch
+        _DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.float8_e4m3fn: 3}
+    return _DTYPES
+
+
+def _rows(t, name, T, C, dtype, device):
+    """Check a [T][C] CUDA tensor with contiguous rows of one type; returns its row stride."""
+    if t.dim() != 2 or t.shape[0] != T or t.shape[1] != C or t.dtype != dtype or t.device != device:
+        raise ValueError(f"{name} must be a [{T}][{C}] tensor of {dtype} on {device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
+    st = t.stride()
+    if C > 1 and st[1] != 1:
+        raise ValueError(f"{name} must have contiguous rows")
+    if T > 1 and st[0] < C:
+        raise ValueError(f"{name}: rows must not overlap")
+    return st[0]
+
+
+class _on:
+    """Current device set to `device` for the call (a no-op, without torch's context manager, where it already is)."""
+
+    def __init__(self, device):
+        import torch
+        self.ctx = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+    def __enter__(self):
+        if self.ctx is not None:
+            self.ctx.__enter__()
+
+    def __exit__(self, *a):
+        if self.ctx is not None:
+            self.ctx.__exit__(*a)
+
+
+def ubp_rmsnorm(x, gamma, eps: float = 1e-6, residual=None, out_dtype=None, out=None, scales=None, residual_out=None,
+                stream=None):
+    """Root mean square norm of the rows of x [T][C] (float32, float16 or bfloat16), with the residual's addition:
+    h = x + residual; y = h * gamma / sqrt(mean(h^2) + eps). Returns (y, scales, h): y in x's type with scales None, or
+    (out_dtype=torch.float8_e4m3fn) in 8 bits with one float32 scale a row; h is x + residual in x's type, or None without
+    a residual. residual_out may be the residual or x itself."""
+    import torch
+    L = load()
+    if not (isinstance(x, torch.Tensor) and x.is_cuda and x.dim() == 2 and x.dtype in _dtypes()) or x.dtype == torch.float8_e4m3fn:
+        raise ValueError("x must be a [T][C] float32, float16 or bfloat16 CUDA tensor")
+    T, Cc = x.shape
+    dev, dt = x.device, x.dtype
+    ldx = _rows(x, "x", T, Cc, dt, dev)
+    if gamma.dim() != 1 or gamma.shape[0] != Cc or gamma.stride(0) != 1 and Cc > 1 or gamma.device != dev or gamma.dtype not in (dt, torch.float32):
+        raise ValueError("gamma must be a contiguous [C] tensor of x's type or float32 on x's device")
+    if out_dtype is None:
+        out_dtype = out.dtype if out is not None else dt
+    q = out_dtype == torch.float8_e4m3fn
+    if not q and out_dtype != dt:
+        raise ValueError("out_dtype must be x's type or torch.float8_e4m3fn")
+    if out is None:
+        out = torch.empty((T, Cc), dtype=out_dtype, device=dev)
+    ldy = _rows(out, "out", T, Cc, out_dtype, dev)
+    if q and scales is None:
+        scales = torch.empty(T, dtype=torch.float32, device=dev)
+    if q and not (scales.dtype == torch.float32 and scales.device == dev and tuple(scales.shape) == (T,) and scales.is_contiguous()):
+        raise ValueError("scales must be a contiguous float32 [T] tensor on x's device")
+    ldr = ldh = 0
+    if residual is not None:
+        ldr = _rows(residual, "residual", T, Cc, dt, dev)
+        if residual_out is None:
+            residual_out = torch.empty((T, Cc), dtype=dt, device=dev)
+    if residual_out is not None:
+        ldh = _rows(residual_out, "residual_out", T, Cc, dt, dev)
+    with _on(dev):
+        _chk(L.ubp_rmsnorm(x.data_ptr(), ldx, None if residual is None else residual.data_ptr(), ldr, gamma.data_ptr(),
+                           _dtypes()[gamma.dtype], _dtypes()[dt], T, Cc, eps,
+                           None if residual_out is None else residual_out.data_ptr(), ldh, out.data_ptr(), ldy,
+                           _dtypes()[out_dtype], scales.data_ptr() if q else None, _stream_ptr(stream)), "ubp_rmsnorm")
+    return out, (scales if q else None), residual_out
+
+
+def ubp_quant_rows(x, out=None, scales=None, stream=None):
+    """Rows of x [T][C] (float32, float16 or bfloat16) in 8 bits: (q float8_e4m3fn [T][C], scales float32 [T]) with
+    x ~= q * scales[:, None]."""
+    import torch
+    L = load()
+    if not (isinstance(x, torch.Tensor) and x.is_cuda and x.dim() == 2 and x.dtype in _dtypes()) or x.dtype == torch.float8_e4m3fn:
+        raise ValueError("x must be a [T][C] float32, float16 or bfloat16 CUDA tensor")
+    T, Cc = x.shape
+    dev = x.device
+    ldx = _rows(x, "x", T, Cc, x.dtype, dev)
+    if out is None:
+        out = torch.empty((T, Cc), dtype=torch.float8_e4m3fn, device=dev)
+    ldq = _rows(out, "out", T, Cc, torch.float8_e4m3fn, dev)
+    if scales is None:
+        scales = torch.empty(T, dtype=torch.float32, device=dev)
+    if not (scales.dtype == torch.float32 and scales.device == dev and tuple(scales.shape) == (T,) and scales.is_contiguous()):
+        raise ValueError("scales must be a contiguous float32 [T] tensor on x's device")
+    with _on(dev):
+        _chk(L.ubp_quant_rows(x.data_ptr(), ldx, _dtypes()[x.dtype], T, Cc, out.data_ptr(), ldq, scales.data_ptr(),
+                              _stream_ptr(stream)), "ubp_quant_rows")
+    return out, scales
+
+
+def linear_plan_image(blob: bytes, dtype, gated: bool = False):
+    """Host copy of a LinearPlan's device image with its geometry and section offsets (no GPU needed)."""
+    L = load()
+    b = np.frombuffer(blob, np.uint8)
+    n = C.c_size_t(0)
+    dt = _dtypes()[dtype]
+    _chk(L.ubp_linear_plan_size(_np_ptr(b), b.size, dt, int(gated), C.byref(n)), "ubp_linear_plan_size")
+    buf = np.zeros(n.value, np.uint8)
+    geom, offs = (C.c_int32 * 5)(), (C.c_int64 * 5)()
+    _chk(L.ubp_linear_plan_image(_np_ptr(b), b.size, dt, int(gated), _np_ptr(buf), n.value, geom, offs), "ubp_linear_plan_image")
+    return (buf, dict(zip(["nbk", "nslab", "Mp", "Kp", "bytes"], [int(g) for g in geom])),
+            dict(zip(["scale", "off", "idx", "val", "dense"], [int(o) for o in offs])))
+
+
+class LinearPlan:
+    """Device plan of one block-pruned linear layer for ubp_linear. `blob` comes from ubp_pack (R = 1); dtype is the type
+    of weights and activations: torch.bfloat16, torch.float16, or torch.float8_e4m3fn (weights are quantised here with one
+    scale a row, `row_scales`). gated: the layer's rows are [gate; up] and the product returns act(gate) * up."""
+
+    def __init__(self, blob: bytes, dtype, gated: bool = False, device="cuda", stream=None):
+        import torch
+        L = load()
+        self._lib = L
+        self._handle = None
+        if dtype not in _dtypes() or dtype == torch.float32:
+            raise ValueError("dtype must be torch.bfloat16, torch.float16 or torch.float8_e4m3fn")
+        d = np.frombuffer(blob, np.uint8)
+        v = _View()
+        _chk(L.ubp_blob_view(_np_ptr(d), d.size, C.byref(v)), "ubp_blob_view")
+        self.M, self.C, self.Nb, self.m = v.M, v.C, v.Nb, v.m
+        self.dtype, self.gated = dtype, bool(gated)
+        n = C.c_size_t(0)
+        _chk(L.ubp_linear_plan_size(_np_ptr(d), d.size, _dtypes()[dtype], int(gated), C.byref(n)), "ubp_linear_plan_size")
+        self.dev_bytes = n.value
+        self.out_features = v.M // 2 if gated else v.M
+        self.buffer = torch.empty(n.value + 256, dtype=torch.uint8, device=device)
+        self.device = self.buffer.device
+        self._dev = (self.buffer.data_ptr() + 255) // 256 * 256
+        h = C.c_void_p()
+        with torch.cuda.device(self.device):
+            _chk(L.ubp_linear_plan_build(_np_ptr(d), d.size, _dtypes()[dtype], int(gated), C.c_void_p(self._dev), n.value,
+                                         _stream_ptr(stream), C.byref(h)), "ubp_linear_plan_build")
+        self._handle = h
+
+    @property
+    def handle(self):
+        if self._handle is None:
+            raise RuntimeError("plan was freed")
+        return self._handle
+
+    @property
+    def row_scales(self):
+        """float32 [M] view of the plan's weight scales (8-bit plans), else None."""
+        import torch
+        if self.dtype != torch.float8_e4m3fn:
+            return None
+        at = self._dev - self.buffer.data_ptr() + 256
+        return self.buffer[at:at + 4 * self.M].view(torch.float32)
+
+    def check(self, stream=None):
+        """Synchronise the stream and raise if a kernel reported a failed bounded wait."""
+        with _on(self.device):
+            _chk(self._lib.ubp_linear_plan_check(self.handle, _stream_ptr(stream)), "ubp_linear_plan_check")
+
+    def clear_status(self, stream=None):
+        with _on(self.device):
+            _chk(self._lib.ubp_linear_plan_clear_status(self.handle, _stream_ptr(stream)), "ubp_linear_plan_clear_status")
+
+    def free(self):
+        if self._handle is not None:
+            self._lib.ubp_linear_plan_free(self._handle)
+            self._handle = None
+
+    def __del__(self):
+        try:
+            self.free()
+        except Exception:
+            pass
+
+
+def ubp_linear(plan: LinearPlan, x, bias=None, activation: str = "none", residual=None, x_scales=None, out=None,
+               out_dtype=None, stream=None, workspace=None):
+    """y[T][F] = act(x @ W.T + bias) + residual with the plan's block-pruned W (gated plan: act(gate) * up + residual).
+    x: [T][C] in the plan's type, rows contiguous; 8-bit plans need x_scales (float32 [T]). bias: float32 [M]. residual:
+    [T][F] in the output's type, may be `out` itself. out_dtype: the plan's type (8-bit plans: bfloat16) unless given.
+    workspace: a CUDA tensor for inputs whose rows are not 16-byte aligned (allocated here when needed and not given)."""
+    import torch
+    L = plan._lib
+    dev, F = plan.device, plan.out_features
+    if not (isinstance(x, torch.Tensor) and x.dim() == 2):
+        raise ValueError("x must be a [T][C] CUDA tensor")
+    T = x.shape[0]
+    ldx = _rows(x, "x", T, plan.C, plan.dtype, dev)
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}")
+    if (plan.dtype == torch.float8_e4m3fn) != (x_scales is not None):
+        raise ValueError("x_scales goes with an 8-bit plan")
+    for t, n, k in ((x_scales, "x_scales", T), (bias, "bias", plan.M)):
+        if t is not None and not (t.dtype == torch.float32 and t.device == dev and tuple(t.shape) == (k,) and t.is_contiguous()):
+            raise ValueError(f"{n} must be a contiguous float32 [{k}] tensor on the plan's device")
+    if out_dtype is None:
+        out_dtype = out.dtype if out is not None else torch.bfloat16 if plan.dtype == torch.float8_e4m3fn else plan.dtype
+    if out_dtype not in _dtypes():
+        raise ValueError("out_dtype must be float32, float16 or bfloat16")
+    if out is None:
+        out = torch.empty((T, F), dtype=out_dtype, device=dev)
+    ldy = _rows(out, "out", T, F, out_dtype, dev)
+    ldr = 0 if residual is None else _rows(residual, "residual", T, F, out_dtype, dev)
+    with _on(dev):
+        px = x.data_ptr()
+        need = L.ubp_linear_workspace_size(plan.handle, px, ldx, T)
+        own_ws = need and workspace is None
+        if own_ws:
+            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
+        if workspace is not None and workspace.device != dev:
+            raise ValueError("workspace is on another device than the plan")
+        _chk(L.ubp_linear(plan.handle, px, ldx, None if x_scales is None else x_scales.data_ptr(), T,
+                          None if bias is None else bias.data_ptr(), ACTIVATIONS[activation],
+                          None if residual is None else residual.data_ptr(), ldr, out.data_ptr(), ldy, _dtypes()[out_dtype],
+                          None if workspace is None else workspace.data_ptr(),
+                          0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
+             "ubp_linear")
+        if own_ws and stream is not None:
+            workspace.record_stream(stream)
     return out

@@ -1,0 +1,70 @@
+// Token-major products with a block-pruned weight: plan of one layer and what its two kernels share.
+#ifndef UBP_LINEAR_H_
+#define UBP_LINEAR_H_
+
+#include <cuda.h>
+
+#include <cstddef>
+#include <cstdint>
+#include <vector>
+
+#include "ubp.h"
+
+namespace ubp {
+
+// Input channels per slab: the sparse form's entries of a start row are in channel order with an offset kept at every slab
+// boundary, so that a launch may cut the reduction at any of them.
+constexpr int LIN_SLAB = 512;
+
+// Device image (all offsets from its base, which is 256-byte aligned):
+//   [0, 256)      header; int32 status word at byte 0
+//   scale_off     float[M]: scale of each weight row (8-bit plans only)
+//   off_off       uint32[(M * nslab) + 1]: first entry of (start row i, slab s) at i * nslab + s
+//   idx_off       uint16[entries]: input channel of an entry
+//   val_off       weights of an entry: nbk consecutive output rows from its start row (plan's type)
+//   dense_off     the densified weight [Mp][Kp] (plan's type), K contiguous. Gated plans interleave the two halves in
+//                 groups of 16 rows: dense row 32 g + i is gate row 16 g + i, dense row 32 g + 16 + i is up row 16 g + i.
+//                 Kp = C rounded up to 128 bytes, Mp = rows rounded up to 128; the padding is zero.
+struct LinearImage {
+    std::vector<uint8_t> bytes;
+    size_t scale_off = 0, off_off = 0, idx_off = 0, val_off = 0, dense_off = 0, total = 0;
+    int nbk = 1, nslab = 1, Mp = 0, Kp = 0;
+    int64_t entries = 0;
+};
+int build_linear_image(const ubp_view_t &v, int dtype, bool gated, bool count_only, LinearImage &img);
+
+constexpr uint32_t kLinearMagic = 0x4c504255u;   // "UBPL": first word of a live handle
+
+}  // namespace ubp
+
+struct ubp_linear_plan {
+    uint32_t magic;
+    int M, C, Nb, m;
+    int dtype, gated;
+    int F;                          // output features: M, or M / 2 of a gated plan
+    ubp::LinearImage img;           // host copy (kept until free)
+    uint8_t *dev;                   // caller's device buffer
+};
+
+namespace ubp {
+
+// One product, as the kernels get it (device pointers; strides in elements).
+struct LinearArgs {
+    const void *x;
+    int64_t ldx;
+    const float *xs;                // scale of each token, 8-bit plans only
+    int64_t T;
+    const float *bias;              // [M] or null
+    int act;
+    const void *res;                // null or [T][F] in y's type
+    int64_t ldr;
+    void *y;
+    int64_t ldy;
+    int *status;
+    int M, C, F, gated;
+};
+
+int launch_linear_sparse(const ubp_linear_plan *p, const LinearArgs &a, int y_dtype, void *stream);
+
+}  // namespace ubp
+#endif

@@ -1,0 +1,123 @@
+// extern "C" surface of the token-major products: plan life cycle, argument checks, choice of the kernel.
+#include <cuda_runtime.h>
+
+#include <cstring>
+#include <new>
+
+#include "ubp_internal.h"
+#include "ubp_linear.h"
+#include "ubp_types.cuh"
+
+static bool live(const ubp_linear_plan *p) { return p && p->magic == ubp::kLinearMagic; }
+
+extern "C" {
+
+int ubp_linear_plan_size(const void *blob, size_t len, int dtype, int gated, size_t *dev_bytes)
+{
+    if (!dev_bytes) return UBP_E_ARG;
+    ubp_view_t v;
+    if (int rc = ubp::blob_view(blob, len, &v)) return rc;
+    ubp::LinearImage img;
+    if (int rc = ubp::build_linear_image(v, dtype, gated != 0, true, img)) return rc;
+    *dev_bytes = img.total;
+    return UBP_OK;
+}
+
+int ubp_linear_plan_image(const void *blob, size_t len, int dtype, int gated, void *host_buf, size_t cap, int32_t geom[5],
+                          int64_t offs[5])
+{
+    if (!host_buf || !geom || !offs) return UBP_E_ARG;
+    ubp_view_t v;
+    if (int rc = ubp::blob_view(blob, len, &v)) return rc;
+    try {
+        ubp::LinearImage img;
+        if (int rc = ubp::build_linear_image(v, dtype, gated != 0, false, img)) return rc;
+        if (cap < img.total) return UBP_E_SPACE;
+        std::memcpy(host_buf, img.bytes.data(), img.total);
+        geom[0] = img.nbk; geom[1] = img.nslab; geom[2] = img.Mp; geom[3] = img.Kp; geom[4] = ubp::dtype_size(dtype);
+        offs[0] = (int64_t)img.scale_off; offs[1] = (int64_t)img.off_off; offs[2] = (int64_t)img.idx_off;
+        offs[3] = (int64_t)img.val_off; offs[4] = (int64_t)img.dense_off;
+    } catch (const std::bad_alloc &) { return UBP_E_SPACE; }
+    return UBP_OK;
+}
+
+int ubp_linear_plan_build(const void *blob, size_t len, int dtype, int gated, void *dev_buf, size_t dev_bytes, void *stream,
+                          ubp_linear_plan_t **plan)
+{
+    if (!plan || !dev_buf || (reinterpret_cast<uintptr_t>(dev_buf) & 255)) return UBP_E_ARG;
+    *plan = nullptr;
+    ubp_view_t v;
+    if (int rc = ubp::blob_view(blob, len, &v)) return rc;
+    ubp_linear_plan *p = nullptr;
+    try {
+        p = new ubp_linear_plan();
+        int rc = ubp::build_linear_image(v, dtype, gated != 0, true, p->img);
+        if (!rc && dev_bytes < p->img.total) rc = UBP_E_SPACE;
+        if (!rc) rc = ubp::build_linear_image(v, dtype, gated != 0, false, p->img);
+        if (rc) { delete p; return rc; }
+    } catch (const std::bad_alloc &) { delete p; return UBP_E_SPACE; }
+    p->magic = ubp::kLinearMagic;
+    p->M = v.M; p->C = v.C; p->Nb = v.Nb; p->m = v.m;
+    p->dtype = dtype; p->gated = gated != 0;
+    p->F = p->gated ? v.M / 2 : v.M;
+    p->dev = static_cast<uint8_t *>(dev_buf);
+    const cudaError_t e = cudaMemcpyAsync(dev_buf, p->img.bytes.data(), p->img.total, cudaMemcpyHostToDevice,
+                                          static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) { ubp::set_last_cuda_error((int)e); delete p; return UBP_E_CUDA; }
+    *plan = p;
+    return UBP_OK;
+}
+
+void ubp_linear_plan_free(ubp_linear_plan_t *plan)
+{
+    if (live(plan)) { plan->magic = 0; delete plan; }
+}
+
+int ubp_linear_plan_check(const ubp_linear_plan_t *plan, void *stream)
+{
+    if (!live(plan)) return UBP_E_ARG;
+    int word = 0;
+    cudaError_t e = cudaMemcpyAsync(&word, plan->dev, sizeof word, cudaMemcpyDeviceToHost, static_cast<cudaStream_t>(stream));
+    if (e == cudaSuccess) e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) { ubp::set_last_cuda_error((int)e); return UBP_E_CUDA; }
+    return word == 0 ? UBP_OK : UBP_E_DEVICE;
+}
+
+int ubp_linear_plan_clear_status(const ubp_linear_plan_t *plan, void *stream)
+{
+    if (!live(plan)) return UBP_E_ARG;
+    const cudaError_t e = cudaMemsetAsync(plan->dev, 0, sizeof(int), static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) { ubp::set_last_cuda_error((int)e); return UBP_E_CUDA; }
+    return UBP_OK;
+}
+
+size_t ubp_linear_workspace_size(const ubp_linear_plan_t *plan, const void *x, int64_t ldx, int64_t T)
+{
+    (void)x; (void)ldx; (void)T;
+    return live(plan) ? 0 : 0;
+}
+
+int ubp_linear(const ubp_linear_plan_t *plan, const void *x, int64_t ldx, const float *x_scales, int64_t T, const float *bias,
+               int act, const void *residual, int64_t ldr, void *y, int64_t ldy, int y_dtype, void *workspace,
+               size_t workspace_bytes, void *stream)
+{
+    if (!live(plan) || T < 0 || act < UBP_ACT_NONE || act > UBP_ACT_SILU) return UBP_E_ARG;
+    const bool q = plan->dtype == UBP_E4M3;
+    if (y_dtype != UBP_F32 && y_dtype != plan->dtype && !(q && (y_dtype == UBP_BF16 || y_dtype == UBP_F16))) return UBP_E_ARG;
+    if (y_dtype == UBP_E4M3) return UBP_E_ARG;
+    if (q ? (!x_scales && T > 0) : x_scales != nullptr) return UBP_E_ARG;
+    if (T == 0) return UBP_OK;
+    const uintptr_t b = (uintptr_t)ubp::dtype_size(plan->dtype), o = (uintptr_t)ubp::dtype_size(y_dtype);
+    if (!x || !y || (T > 1 && (ldx < plan->C || ldy < plan->F || (residual && ldr < plan->F)))) return UBP_E_ARG;
+    auto off = [](const void *p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) != 0; };
+    if (off(x, b) || off(y, o) || off(residual, o) || off(bias, 4) || off(x_scales, 4) || off(workspace, 16)) return UBP_E_ARG;
+    if (workspace_bytes < ubp_linear_workspace_size(plan, x, ldx, T)) return UBP_E_SPACE;
+    ubp::LinearArgs a;
+    a.x = x; a.ldx = ldx; a.xs = x_scales; a.T = T; a.bias = bias; a.act = act;
+    a.res = residual; a.ldr = ldr; a.y = y; a.ldy = ldy;
+    a.status = reinterpret_cast<int *>(plan->dev);
+    a.M = plan->M; a.C = plan->C; a.F = plan->F; a.gated = plan->gated;
+    return ubp::launch_linear_sparse(plan, a, y_dtype, stream);
+}
+
+}  // extern "C"

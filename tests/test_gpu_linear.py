@@ -1,0 +1,201 @@
+"""Token-major products with a block-pruned weight against the formula in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from linear_ref import F8, TINY, UNIT, make_weight, product64, quantise, typed_weight
+
+pytestmark = pytest.mark.gpu
+
+BF16, F16, F32 = torch.bfloat16, torch.float16, torch.float32
+IDS = {BF16: "bf16", F16: "f16", F8: "e4m3", F32: "f32"}
+
+
+@pytest.fixture(scope="module")
+def ubp():
+    import paper_2407_19644_b200 as m
+    m.load()
+    return m
+
+
+def inputs(T, C, dtype, pad, lead, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    v = torch.randn(T, C, device="cuda", generator=g)
+    xs = None
+    if dtype == F8:
+        v, xs = quantise(v) if T else (v.to(F8), torch.empty(0, device="cuda"))
+    buf = torch.full((T * (C + pad) + lead,), 1.0e4 if dtype != F8 else 448.0, device="cuda").to(dtype)
+    x = buf[lead:].view(T, C + pad)[:, :C]
+    x.copy_(v.to(dtype))
+    return x, xs
+
+
+def check(ubp, W, mask, Nb, T, dtype, out_dtype, act="none", gated=False, bias=True, residual=True, pad=0, lead=0, seed=0, ypad=0):
+    M, C = W.shape
+    F = M // 2 if gated else M
+    plan = ubp.LinearPlan(ubp.ubp_pack(W, mask, Nb), dtype, gated=gated)
+    x, xs = inputs(T, C, dtype, pad, lead, seed)
+    g = torch.Generator(device="cuda").manual_seed(seed + 1)
+    b = torch.randn(M, device="cuda", generator=g) if bias else None
+    ybuf = torch.full((T * (F + ypad) + lead,), 7.0, device="cuda", dtype=out_dtype)
+    y = ybuf[lead:].view(T, F + ypad)[:, :F]
+    r = None
+    if residual:
+        rbuf = torch.full((T, F + pad), float("nan"), device="cuda", dtype=out_dtype)
+        r = rbuf[:, :F]
+        r.copy_(torch.randn(T, F, device="cuda", generator=g))
+    ubp.ubp_linear(plan, x, bias=b, activation=act, residual=r, x_scales=xs, out=y)
+    plan.check()
+    x64 = x.double() * (xs.double()[:, None] if xs is not None else 1.0)
+    W64 = typed_weight(W, dtype).cuda()
+    want, d = product64(x64, W64, None if b is None else b.double(), act, gated, None if r is None else r.double())
+    err = (y.double() - want).abs()
+    bound = d + UNIT[out_dtype] * (want.abs() + d) + TINY[out_dtype]
+    assert torch.isfinite(y.float()).all()
+    assert (err <= bound).all(), float((err / bound).max())
+    if ypad:
+        assert (ybuf[lead:].view(T, F + ypad)[:, F:] == 7.0).all()
+    return plan, x, xs, b, r, y
+
+
+#: (tokens, rows, input features, block rows, sparsity)
+SHAPES = [(1, 1, 1, 1, 0), (1, 64, 64, 4, 50), (3, 66, 37, 5, 40), (2, 130, 1003, 2, 70), (4, 258, 515, 8, 80), (8, 300, 2050, 16, 60),
+          (9, 96, 129, 3, 50), (5, 1000, 4100, 4, 90), (7, 40, 9000, 4, 50), (23, 260, 512, 4, 70), (64, 128, 64, 2, 50),
+          (127, 256, 65, 4, 60), (128, 254, 128, 4, 60), (129, 514, 200, 8, 70), (300, 770, 1000, 4, 80), (513, 32, 1030, 4, 50)]
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F8], ids=IDS.get)
+@pytest.mark.parametrize("T,M,C,Nb,p", SHAPES)
+def test_product(ubp, dtype, T, M, C, Nb, p):
+    W, mask = make_weight(M, C, Nb, p, 100 + M)
+    out = BF16 if dtype == F8 else dtype
+    check(ubp, W, mask, Nb, T, dtype, out)
+    check(ubp, W, mask, Nb, T, dtype, out, act="gelu", residual=False, pad=3, ypad=5, seed=5)
+    check(ubp, W, mask, Nb, T, dtype, F32, bias=False, residual=False, pad=8, seed=9)
+    if M % 2 == 0:
+        check(ubp, W, mask, Nb, T, dtype, out, act="silu", gated=True, bias=False, residual=False, seed=13)
+        check(ubp, W, mask, Nb, T, dtype, F32, act="gelu_tanh", gated=True, pad=1, lead=1, ypad=3, seed=17)
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("T", [1, 6, 150])
+def test_activations(ubp, act, T):
+    W, mask = make_weight(96, 80, 4, 50, 3)
+    for gated in (False, True):
+        for dtype, out in ((BF16, BF16), (F16, F16), (F8, F16), (F8, F32)):
+            check(ubp, W, mask, 4, T, dtype, out, act=act, gated=gated, seed=21)
+
+
+@pytest.mark.parametrize("T", [1, 4, 70, 300])
+def test_rows_without_blocks(ubp, T):
+    W, mask = make_weight(64, 48, 4, 95, 3)
+    W, mask = W.copy(), mask.copy()
+    W[:40], mask[:40] = 0, 0                       # whole output rows empty
+    mask[40:] = 0
+    mask[44:48, :] = 1                             # and one full stripe
+    W = np.where(mask, np.random.default_rng(0).standard_normal(W.shape), 0).astype(np.float32)
+    for dtype in (BF16, F8):
+        check(ubp, W, mask, 4, T, dtype, BF16, seed=2)
+        check(ubp, W, mask, 4, T, dtype, BF16, act="silu", gated=True, seed=3)
+    empty = np.zeros_like(mask)
+    check(ubp, W * 0, empty, 4, T, F16, F16, act="relu", seed=4)
+
+
+@pytest.mark.parametrize("T", [1, 3, 40, 260])
+def test_same_result_twice_and_in_place_residual(ubp, T):
+    W, mask = make_weight(512, 1500, 4, 70, 8)
+    plan, x, xs, b, r, y = check(ubp, W, mask, 4, T, BF16, BF16, seed=30)
+    again = ubp.ubp_linear(plan, x, bias=b, residual=r, x_scales=xs)
+    assert torch.equal(again, y)
+    z = r.contiguous().clone()
+    assert ubp.ubp_linear(plan, x, bias=b, residual=z, x_scales=xs, out=z) is z
+    assert torch.equal(z, y)
+
+
+@pytest.mark.parametrize("T", [3, 200])
+def test_bad_token_stays_alone(ubp, T):
+    """A NaN or an infinity in one token's row leaves the other tokens' outputs as they are."""
+    W, mask = make_weight(256, 300, 4, 60, 8)
+    plan, x, xs, b, r, y = check(ubp, W, mask, 4, T, BF16, BF16, seed=31)
+    x = x.clone()
+    x[1, 7] = float("nan")
+    got = ubp.ubp_linear(plan, x, bias=b, residual=r)
+    keep = [t for t in range(T) if t != 1]
+    assert torch.equal(got[keep], y[keep])
+    touched = torch.from_numpy(mask[:, 7] != 0).cuda()
+    assert got[1][touched].isnan().all()
+
+
+@pytest.mark.parametrize("T", [2, 100])
+def test_other_stream_and_no_tokens(ubp, T):
+    W, mask = make_weight(256, 320, 4, 60, 8)
+    plan, x, xs, b, r, y = check(ubp, W, mask, 4, T, F16, F16, pad=1, seed=32)
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        z = x
+        for _ in range(20):
+            z = z * 1.0
+        got = ubp.ubp_linear(plan, z, bias=b, residual=r)
+    st.synchronize()
+    assert torch.equal(got, y)
+    got = ubp.ubp_linear(plan, x, bias=b, residual=r, stream=st)
+    st.synchronize()
+    assert torch.equal(got, y)
+    assert ubp.ubp_linear(plan, x[:0]).shape == (0, 256)
+
+
+def test_row_scales(ubp):
+    W, mask = make_weight(70, 90, 2, 60, 4)
+    W[3], mask[3] = W[3], mask[3]
+    plan = ubp.LinearPlan(ubp.ubp_pack(W, mask, 2), F8)
+    assert torch.equal(plan.row_scales.cpu(), quantise(torch.from_numpy(W))[1])
+    assert ubp.LinearPlan(ubp.ubp_pack(W, mask, 2), BF16).row_scales is None
+
+
+def test_block_of_a_feed_forward_layer(ubp):
+    """Norm -> gated product -> rows to 8 bits -> product with the residual, each step against 64 bits from the step's
+    own inputs."""
+    C, F, T = 256, 640, 37
+    Wg, mg = make_weight(2 * F, C, 4, 70, 1)
+    Wd, md = make_weight(C, F, 4, 70, 2)
+    up, down = ubp.LinearPlan(ubp.ubp_pack(Wg, mg, 4), F8, gated=True), ubp.LinearPlan(ubp.ubp_pack(Wd, md, 4), F8)
+    g = torch.Generator(device="cuda").manual_seed(0)
+    x, r = (torch.randn(T, C, device="cuda", generator=g).to(BF16) for _ in range(2))
+    q, s, h = ubp.ubp_rmsnorm(x, torch.ones(C, device="cuda", dtype=BF16), 1e-5, residual=r, out_dtype=F8)
+    a = ubp.ubp_linear(up, q, activation="silu", x_scales=s)
+    want, d = product64(q.double() * s.double()[:, None], typed_weight(Wg, F8).cuda(), None, "silu", True, None)
+    assert ((a.double() - want).abs() <= d + UNIT[BF16] * (want.abs() + d)).all()
+    p, ps = ubp.ubp_quant_rows(a)
+    y = ubp.ubp_linear(down, p, residual=h, x_scales=ps, out=h.clone())
+    want, d = product64(p.double() * ps.double()[:, None], typed_weight(Wd, F8).cuda(), None, "none", False, h.double())
+    assert ((y.double() - want).abs() <= d + UNIT[BF16] * (want.abs() + d)).all()
+
+
+def test_refusals(ubp):
+    W, mask = make_weight(64, 32, 4, 50, 1)
+    blob = ubp.ubp_pack(W, mask, 4)
+    plan, p8 = ubp.LinearPlan(blob, BF16), ubp.LinearPlan(blob, F8)
+    x = torch.randn(4, 32, device="cuda").to(BF16)
+    s = torch.ones(4, device="cuda")
+    bad = [lambda: ubp.ubp_linear(plan, x.half()), lambda: ubp.ubp_linear(plan, x[:, :31]), lambda: ubp.ubp_linear(plan, x, x_scales=s),
+           lambda: ubp.ubp_linear(p8, x.to(F8)), lambda: ubp.ubp_linear(plan, x, activation="swish"),
+           lambda: ubp.ubp_linear(plan, x, bias=torch.zeros(63, device="cuda")), lambda: ubp.ubp_linear(plan, x, bias=torch.zeros(64, device="cuda").half()),
+           lambda: ubp.ubp_linear(plan, x, residual=torch.zeros(4, 64, device="cuda")), lambda: ubp.ubp_linear(plan, x.cpu()),
+           lambda: ubp.ubp_linear(plan, x, out=torch.zeros(4, 63, device="cuda", dtype=BF16)),
+           lambda: ubp.ubp_linear(plan, x[:1].expand(4, 32)), lambda: ubp.LinearPlan(blob, F32)]
+    for f in bad:
+        with pytest.raises(ValueError):
+            f()
+    for f, code in ((lambda: ubp.ubp_linear(plan, x, out_dtype=F16), -1),
+                    (lambda: ubp.ubp_linear(p8, x.to(F8), x_scales=s, out_dtype=F8), -1),
+                    (lambda: ubp.LinearPlan(blob[:-1], BF16), -4)):
+        with pytest.raises(ubp.UbpError) as e:
+            f()
+        assert e.value.code == code
+    W1, m1 = make_weight(33, 32, 1, 50, 1)
+    with pytest.raises(ubp.UbpError):
+        ubp.LinearPlan(ubp.ubp_pack(W1, m1, 1), BF16, gated=True)          # an odd number of rows has no halves
+    plan.free()
+    with pytest.raises(RuntimeError):
+        ubp.ubp_linear(plan, x)
