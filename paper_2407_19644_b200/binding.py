@@ -94,6 +94,7 @@ def load():
     L.ubp_linear_plan_free.restype = None
     L.ubp_linear_plan_check.argtypes = [vp, vp]
     L.ubp_linear_plan_clear_status.argtypes = [vp, vp]
+    L.ubp_linear_choice.argtypes = [vp, i64, C.POINTER(i32), C.POINTER(i32), C.POINTER(i32)]
     L.ubp_linear_workspace_size.argtypes = [vp, vp, i64, i64]
     L.ubp_linear_workspace_size.restype = sz
     L.ubp_linear.argtypes = [vp, vp, i64, vp, i64, vp, i32, vp, i64, vp, i64, i32, vp, sz, vp]
@@ -680,6 +681,14 @@ class LinearPlan:
             return None
         at = self._dev - self.buffer.data_ptr() + 256
         return self.buffer[at:at + 4 * self.M].view(torch.float32)
+
+    def choice(self, T: int):
+        """(kernel, tile, split) a call with T tokens takes: kernel 0 = kept blocks on the CUDA cores, 1 = tensor cores with
+        `tile` tokens a block and `split` blocks to a reduction, 2 = tensor cores, CTA pairs on 256 tokens x `tile` rows."""
+        k, t, s = C.c_int32(), C.c_int32(), C.c_int32()
+        with _on(self.device):
+            _chk(self._lib.ubp_linear_choice(self.handle, int(T), C.byref(k), C.byref(t), C.byref(s)), "ubp_linear_choice")
+        return k.value, t.value, s.value
 
     def check(self, stream=None):
         """Synchronise the stream and raise if a kernel reported a failed bounded wait."""

@@ -64,7 +64,20 @@ struct LinearArgs {
     int M, C, F, gated;
 };
 
+// Which kernel a launch takes and its tile.
+enum { LIN_SPARSE = 0, LIN_FEW = 1, LIN_MANY = 2 };
+struct LinearChoice {
+    int kernel;                     // LIN_*
+    int cols;                       // LIN_FEW: tokens per tile; LIN_MANY: dense weight rows per tile
+    int split;                      // LIN_FEW: blocks of a cluster that share a reduction
+};
+LinearChoice linear_choose(const ubp_linear_plan *p, int64_t T, int sms);
+
 int launch_linear_sparse(const ubp_linear_plan *p, const LinearArgs &a, int y_dtype, void *stream);
+// whether the tensor-core kernels can copy x's rows as they are (else they go through the workspace, [T][Kp])
+bool linear_x_direct(const ubp_linear_plan *p, const void *x, int64_t ldx, int64_t T);
+int launch_linear_tc(const ubp_linear_plan *p, const LinearArgs &a, int y_dtype, const LinearChoice &ch, void *workspace, int sms,
+                     void *stream);
 
 }  // namespace ubp
 #endif

@@ -8,6 +8,32 @@
 #include "ubp_linear.h"
 #include "ubp_types.cuh"
 
+namespace ubp {
+
+LinearChoice linear_choose(const ubp_linear_plan *p, int64_t T, int sms)
+{
+    if (T <= 16) return {LIN_SPARSE, 0, 0};
+    const int rows = p->gated ? (p->F + 15) / 16 * 32 : p->M, rt = (rows + 127) / 128;
+    const int nk = p->img.Kp * (p->dtype == UBP_E4M3 ? 1 : 2) / 128;
+    if (T <= 256) {
+        const int cols = (int)((T + 15) / 16 * 16);
+        int S = 1;
+        while (S < 8 && rt * S * 2 <= sms && nk / (S * 2) >= 4) S *= 2;
+        return {LIN_FEW, cols, S};
+    }
+    const int64_t t256 = ((T + 255) / 256) * ((rows + 255) / 256);
+    return {LIN_MANY, t256 >= sms / 2 ? 256 : 128, 0};
+}
+
+static int device_sms()
+{
+    int sms = 148, dev = 0;
+    if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    return sms;
+}
+
+}  // namespace ubp
+
 static bool live(const ubp_linear_plan *p) { return p && p->magic == ubp::kLinearMagic; }
 
 extern "C" {
@@ -93,8 +119,17 @@ int ubp_linear_plan_clear_status(const ubp_linear_plan_t *plan, void *stream)
 
 size_t ubp_linear_workspace_size(const ubp_linear_plan_t *plan, const void *x, int64_t ldx, int64_t T)
 {
-    (void)x; (void)ldx; (void)T;
-    return live(plan) ? 0 : 0;
+    if (!live(plan) || T <= 0) return 0;
+    if (ubp::linear_choose(plan, T, ubp::device_sms()).kernel == ubp::LIN_SPARSE || ubp::linear_x_direct(plan, x, ldx, T)) return 0;
+    return (size_t)T * (size_t)plan->img.Kp * (size_t)ubp::dtype_size(plan->dtype);
+}
+
+int ubp_linear_choice(const ubp_linear_plan_t *plan, int64_t T, int *kernel, int *tile, int *split)
+{
+    if (!live(plan) || T < 0 || !kernel || !tile || !split) return UBP_E_ARG;
+    const ubp::LinearChoice ch = ubp::linear_choose(plan, T, ubp::device_sms());
+    *kernel = ch.kernel; *tile = ch.cols; *split = ch.split;
+    return UBP_OK;
 }
 
 int ubp_linear(const ubp_linear_plan_t *plan, const void *x, int64_t ldx, const float *x_scales, int64_t T, const float *bias,
@@ -117,7 +152,10 @@ int ubp_linear(const ubp_linear_plan_t *plan, const void *x, int64_t ldx, const 
     a.res = residual; a.ldr = ldr; a.y = y; a.ldy = ldy;
     a.status = reinterpret_cast<int *>(plan->dev);
     a.M = plan->M; a.C = plan->C; a.F = plan->F; a.gated = plan->gated;
-    return ubp::launch_linear_sparse(plan, a, y_dtype, stream);
+    const int sms = ubp::device_sms();
+    const ubp::LinearChoice ch = ubp::linear_choose(plan, T, sms);
+    if (ch.kernel == ubp::LIN_SPARSE) return ubp::launch_linear_sparse(plan, a, y_dtype, stream);
+    return ubp::launch_linear_tc(plan, a, y_dtype, ch, workspace, sms, stream);
 }
 
 }  // extern "C"
