@@ -518,44 +518,76 @@ def ubp_bed_select(W, Nb: int, m: int, stream=None):
 
 # ------------------------------------------------------------------ token-major operators (language-model layers)
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
-_DTYPES = None
+
+
+class _Torch:
+    """What the token-major calls need of torch, looked up once (importing the package does not import torch). A call on a
+    token or two is bound by the host, so these calls check what they are given without context managers or stream objects
+    (a torch.cuda.current_stream() is 3 us, the raw handle 0.1 us)."""
+
+    def __init__(self):
+        import torch
+        self.torch = torch
+        self.Tensor, self.empty, self.empty_like = torch.Tensor, torch.empty, torch.empty_like
+        self.f32, self.bf16, self.f8 = torch.float32, torch.bfloat16, torch.float8_e4m3fn
+        self.codes = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.float8_e4m3fn: 3}
+        self.row_types = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
+        self.current_device = torch.cuda.current_device
+        self.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+            (lambda index: torch.cuda.current_stream(index).cuda_stream)
+
+
+_torch = None
+
+
+def _tk() -> _Torch:
+    global _torch
+    if _torch is None:
+        _torch = _Torch()
+    return _torch
 
 
 def _dtypes():
-    """torch dtype -> ubp_dtype (built on first use: importing the package does not import torch)."""
-    global _DTYPES
-    if _DTYPES is None:
-        import torch
-        _DTYPES = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.float8_e4m3fn: 3}
-    return _DTYPES
+    return _tk().codes
 
 
-def _rows(t, name, T, C, dtype, device):
-    """Check a [T][C] CUDA tensor with contiguous rows of one type; returns its row stride."""
-    if t.dim() != 2 or t.shape[0] != T or t.shape[1] != C or t.dtype != dtype or t.device != device:
-        raise ValueError(f"{name} must be a [{T}][{C}] tensor of {dtype} on {device}, got {tuple(t.shape)} {t.dtype} on {t.device}")
-    st = t.stride()
-    if C > 1 and st[1] != 1:
-        raise ValueError(f"{name} must have contiguous rows")
-    if T > 1 and st[0] < C:
-        raise ValueError(f"{name}: rows must not overlap")
-    return st[0]
+def _ld(t, name, T, Cc, dtype, dev):
+    """Check a [T][Cc] CUDA tensor with contiguous, disjoint rows of one type on device `dev`; returns its row stride."""
+    sh = t.shape
+    if len(sh) != 2 or sh[0] != T or sh[1] != Cc or t.dtype != dtype or t.get_device() != dev:
+        raise ValueError(f"{name} must be a [{T}][{Cc}] tensor of {dtype} on cuda:{dev}, got {tuple(sh)} {t.dtype} on {t.device}")
+    ld, one = t.stride()
+    if one != 1 and Cc > 1 or ld < Cc and T > 1:
+        raise ValueError(f"{name} must have contiguous rows that do not overlap")
+    return ld
 
 
-class _on:
-    """Current device set to `device` for the call (a no-op, without torch's context manager, where it already is)."""
+def _vec(t, name, n, dtypes, dev):
+    """Check a contiguous [n] CUDA vector of one of the types; returns its address."""
+    sh = t.shape
+    if len(sh) != 1 or sh[0] != n or t.dtype not in dtypes or t.get_device() != dev or n > 1 and t.stride(0) != 1:
+        raise ValueError(f"{name} must be a contiguous [{n}] vector of {' or '.join(map(str, dtypes))} on cuda:{dev}")
+    return t.data_ptr()
 
-    def __init__(self, device):
-        import torch
-        self.ctx = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
 
-    def __enter__(self):
-        if self.ctx is not None:
-            self.ctx.__enter__()
+def _call(k, dev, fn, what, args, stream):
+    """fn(*args, stream) with `dev` current."""
+    if k.current_device() == dev:
+        rc = fn(*args, k.raw_stream(dev) if stream is None else stream.cuda_stream)
+    else:
+        with k.torch.cuda.device(dev):
+            rc = fn(*args, k.raw_stream(dev) if stream is None else stream.cuda_stream)
+    if rc:
+        _chk(rc, what)
 
-    def __exit__(self, *a):
-        if self.ctx is not None:
-            self.ctx.__exit__(*a)
+
+def _rows_x(k, x):
+    """(T, C, row stride, device index, type) of an activation matrix."""
+    if not isinstance(x, k.Tensor) or x.dim() != 2 or x.dtype not in k.row_types or not x.is_cuda:
+        raise ValueError("x must be a [T][C] float32, float16 or bfloat16 CUDA tensor")
+    T, Cc = x.shape
+    dt, dev = x.dtype, x.get_device()
+    return T, Cc, _ld(x, "x", T, Cc, dt, dev), dev, dt
 
 
 def ubp_rmsnorm(x, gamma, eps: float = 1e-6, residual=None, out_dtype=None, out=None, scales=None, residual_out=None,
@@ -564,62 +596,64 @@ def ubp_rmsnorm(x, gamma, eps: float = 1e-6, residual=None, out_dtype=None, out=
     h = x + residual; y = h * gamma / sqrt(mean(h^2) + eps). Returns (y, scales, h): y in x's type with scales None, or
     (out_dtype=torch.float8_e4m3fn) in 8 bits with one float32 scale a row; h is x + residual in x's type, or None without
     a residual. residual_out may be the residual or x itself."""
-    import torch
-    L = load()
-    if not (isinstance(x, torch.Tensor) and x.is_cuda and x.dim() == 2 and x.dtype in _dtypes()) or x.dtype == torch.float8_e4m3fn:
-        raise ValueError("x must be a [T][C] float32, float16 or bfloat16 CUDA tensor")
-    T, Cc = x.shape
-    dev, dt = x.device, x.dtype
-    ldx = _rows(x, "x", T, Cc, dt, dev)
-    if gamma.dim() != 1 or gamma.shape[0] != Cc or gamma.stride(0) != 1 and Cc > 1 or gamma.device != dev or gamma.dtype not in (dt, torch.float32):
-        raise ValueError("gamma must be a contiguous [C] tensor of x's type or float32 on x's device")
+    k = _tk()
+    L = _lib or load()
+    T, Cc, ldx, dev, dt = _rows_x(k, x)
+    pg = _vec(gamma, "gamma", Cc, (dt, k.f32), dev)
     if out_dtype is None:
         out_dtype = out.dtype if out is not None else dt
-    q = out_dtype == torch.float8_e4m3fn
+    q = out_dtype == k.f8
     if not q and out_dtype != dt:
         raise ValueError("out_dtype must be x's type or torch.float8_e4m3fn")
+    ldy = ldr = ldh = Cc
+    like = k.empty_like if x.is_contiguous() else k.empty
+    arg, at = (x, {}) if like is k.empty_like else ((T, Cc), {"device": x.device})
     if out is None:
-        out = torch.empty((T, Cc), dtype=out_dtype, device=dev)
-    ldy = _rows(out, "out", T, Cc, out_dtype, dev)
-    if q and scales is None:
-        scales = torch.empty(T, dtype=torch.float32, device=dev)
-    if q and not (scales.dtype == torch.float32 and scales.device == dev and tuple(scales.shape) == (T,) and scales.is_contiguous()):
-        raise ValueError("scales must be a contiguous float32 [T] tensor on x's device")
-    ldr = ldh = 0
+        out = like(arg, dtype=out_dtype, **at)
+    else:
+        ldy = _ld(out, "out", T, Cc, out_dtype, dev)
+    ps = None
+    if q:
+        if scales is None:
+            scales = k.empty(T, dtype=k.f32, device=x.device)
+            ps = scales.data_ptr()
+        else:
+            ps = _vec(scales, "scales", T, (k.f32,), dev)
+    else:
+        scales = None
+    pr = ph = None
     if residual is not None:
-        ldr = _rows(residual, "residual", T, Cc, dt, dev)
+        ldr = _ld(residual, "residual", T, Cc, dt, dev)
+        pr = residual.data_ptr()
         if residual_out is None:
-            residual_out = torch.empty((T, Cc), dtype=dt, device=dev)
-    if residual_out is not None:
-        ldh = _rows(residual_out, "residual_out", T, Cc, dt, dev)
-    with _on(dev):
-        _chk(L.ubp_rmsnorm(x.data_ptr(), ldx, None if residual is None else residual.data_ptr(), ldr, gamma.data_ptr(),
-                           _dtypes()[gamma.dtype], _dtypes()[dt], T, Cc, eps,
-                           None if residual_out is None else residual_out.data_ptr(), ldh, out.data_ptr(), ldy,
-                           _dtypes()[out_dtype], scales.data_ptr() if q else None, _stream_ptr(stream)), "ubp_rmsnorm")
-    return out, (scales if q else None), residual_out
+            residual_out = like(arg, dtype=dt, **at)
+            ph = residual_out.data_ptr()
+    if residual_out is not None and ph is None:
+        ldh = _ld(residual_out, "residual_out", T, Cc, dt, dev)
+        ph = residual_out.data_ptr()
+    codes = k.codes
+    _call(k, dev, L.ubp_rmsnorm, "ubp_rmsnorm", (x.data_ptr(), ldx, pr, ldr, pg, codes[gamma.dtype], codes[dt], T, Cc, eps,
+                                                 ph, ldh, out.data_ptr(), ldy, codes[out_dtype], ps), stream)
+    return out, scales, residual_out
 
 
 def ubp_quant_rows(x, out=None, scales=None, stream=None):
     """Rows of x [T][C] (float32, float16 or bfloat16) in 8 bits: (q float8_e4m3fn [T][C], scales float32 [T]) with
     x ~= q * scales[:, None]."""
-    import torch
-    L = load()
-    if not (isinstance(x, torch.Tensor) and x.is_cuda and x.dim() == 2 and x.dtype in _dtypes()) or x.dtype == torch.float8_e4m3fn:
-        raise ValueError("x must be a [T][C] float32, float16 or bfloat16 CUDA tensor")
-    T, Cc = x.shape
-    dev = x.device
-    ldx = _rows(x, "x", T, Cc, x.dtype, dev)
+    k = _tk()
+    L = _lib or load()
+    T, Cc, ldx, dev, dt = _rows_x(k, x)
+    ldq = Cc
     if out is None:
-        out = torch.empty((T, Cc), dtype=torch.float8_e4m3fn, device=dev)
-    ldq = _rows(out, "out", T, Cc, torch.float8_e4m3fn, dev)
+        out = k.empty_like(x, dtype=k.f8) if x.is_contiguous() else k.empty((T, Cc), dtype=k.f8, device=x.device)
+    else:
+        ldq = _ld(out, "out", T, Cc, k.f8, dev)
     if scales is None:
-        scales = torch.empty(T, dtype=torch.float32, device=dev)
-    if not (scales.dtype == torch.float32 and scales.device == dev and tuple(scales.shape) == (T,) and scales.is_contiguous()):
-        raise ValueError("scales must be a contiguous float32 [T] tensor on x's device")
-    with _on(dev):
-        _chk(L.ubp_quant_rows(x.data_ptr(), ldx, _dtypes()[x.dtype], T, Cc, out.data_ptr(), ldq, scales.data_ptr(),
-                              _stream_ptr(stream)), "ubp_quant_rows")
+        scales = k.empty(T, dtype=k.f32, device=x.device)
+        ps = scales.data_ptr()
+    else:
+        ps = _vec(scales, "scales", T, (k.f32,), dev)
+    _call(k, dev, L.ubp_quant_rows, "ubp_quant_rows", (x.data_ptr(), ldx, k.codes[dt], T, Cc, out.data_ptr(), ldq, ps), stream)
     return out, scales
 
 
@@ -660,6 +694,8 @@ class LinearPlan:
         self.out_features = v.M // 2 if gated else v.M
         self.buffer = torch.empty(n.value + 256, dtype=torch.uint8, device=device)
         self.device = self.buffer.device
+        self._index = self.buffer.get_device()
+        self._dtype_code, self._bytes = _dtypes()[dtype], 1 if dtype == torch.float8_e4m3fn else 2
         self._dev = (self.buffer.data_ptr() + 255) // 256 * 256
         h = C.c_void_p()
         with torch.cuda.device(self.device):
@@ -686,17 +722,20 @@ class LinearPlan:
         """(kernel, tile, split) a call with T tokens takes: kernel 0 = kept blocks on the CUDA cores, 1 = tensor cores with
         `tile` tokens a block and `split` blocks to a reduction, 2 = tensor cores, CTA pairs on 256 tokens x `tile` rows."""
         k, t, s = C.c_int32(), C.c_int32(), C.c_int32()
-        with _on(self.device):
+        import torch
+        with torch.cuda.device(self.device):
             _chk(self._lib.ubp_linear_choice(self.handle, int(T), C.byref(k), C.byref(t), C.byref(s)), "ubp_linear_choice")
         return k.value, t.value, s.value
 
     def check(self, stream=None):
         """Synchronise the stream and raise if a kernel reported a failed bounded wait."""
-        with _on(self.device):
+        import torch
+        with torch.cuda.device(self.device):
             _chk(self._lib.ubp_linear_plan_check(self.handle, _stream_ptr(stream)), "ubp_linear_plan_check")
 
     def clear_status(self, stream=None):
-        with _on(self.device):
+        import torch
+        with torch.cuda.device(self.device):
             _chk(self._lib.ubp_linear_plan_clear_status(self.handle, _stream_ptr(stream)), "ubp_linear_plan_clear_status")
 
     def free(self):
@@ -717,42 +756,45 @@ def ubp_linear(plan: LinearPlan, x, bias=None, activation: str = "none", residua
     x: [T][C] in the plan's type, rows contiguous; 8-bit plans need x_scales (float32 [T]). bias: float32 [M]. residual:
     [T][F] in the output's type, may be `out` itself. out_dtype: the plan's type (8-bit plans: bfloat16) unless given.
     workspace: a CUDA tensor for inputs whose rows are not 16-byte aligned (allocated here when needed and not given)."""
-    import torch
-    L = plan._lib
-    dev, F = plan.device, plan.out_features
-    if not (isinstance(x, torch.Tensor) and x.dim() == 2):
+    k = _tk()
+    L, dev, F, T = plan._lib, plan._index, plan.out_features, 0
+    if not isinstance(x, k.Tensor) or x.dim() != 2:
         raise ValueError("x must be a [T][C] CUDA tensor")
     T = x.shape[0]
-    ldx = _rows(x, "x", T, plan.C, plan.dtype, dev)
-    if activation not in ACTIVATIONS:
+    ldx = _ld(x, "x", T, plan.C, plan.dtype, dev)
+    act = ACTIVATIONS.get(activation)
+    if act is None:
         raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}")
-    if (plan.dtype == torch.float8_e4m3fn) != (x_scales is not None):
+    if (plan._bytes == 1) != (x_scales is not None):
         raise ValueError("x_scales goes with an 8-bit plan")
-    for t, n, k in ((x_scales, "x_scales", T), (bias, "bias", plan.M)):
-        if t is not None and not (t.dtype == torch.float32 and t.device == dev and tuple(t.shape) == (k,) and t.is_contiguous()):
-            raise ValueError(f"{n} must be a contiguous float32 [{k}] tensor on the plan's device")
     if out_dtype is None:
-        out_dtype = out.dtype if out is not None else torch.bfloat16 if plan.dtype == torch.float8_e4m3fn else plan.dtype
-    if out_dtype not in _dtypes():
+        out_dtype = out.dtype if out is not None else k.bf16 if plan._bytes == 1 else plan.dtype
+    ydt = k.codes.get(out_dtype)
+    if ydt is None:
         raise ValueError("out_dtype must be float32, float16 or bfloat16")
+    ldy, ldr = F, 0
     if out is None:
-        out = torch.empty((T, F), dtype=out_dtype, device=dev)
-    ldy = _rows(out, "out", T, F, out_dtype, dev)
-    ldr = 0 if residual is None else _rows(residual, "residual", T, F, out_dtype, dev)
-    with _on(dev):
-        px = x.data_ptr()
-        need = L.ubp_linear_workspace_size(plan.handle, px, ldx, T)
-        own_ws = need and workspace is None
-        if own_ws:
-            workspace = torch.empty(need, dtype=torch.uint8, device=dev)
-        if workspace is not None and workspace.device != dev:
-            raise ValueError("workspace is on another device than the plan")
-        _chk(L.ubp_linear(plan.handle, px, ldx, None if x_scales is None else x_scales.data_ptr(), T,
-                          None if bias is None else bias.data_ptr(), ACTIVATIONS[activation],
-                          None if residual is None else residual.data_ptr(), ldr, out.data_ptr(), ldy, _dtypes()[out_dtype],
-                          None if workspace is None else workspace.data_ptr(),
-                          0 if workspace is None else workspace.numel() * workspace.element_size(), _stream_ptr(stream)),
-             "ubp_linear")
-        if own_ws and stream is not None:
-            workspace.record_stream(stream)
+        out = x.new_empty((T, F)) if out_dtype == plan.dtype else k.empty((T, F), dtype=out_dtype, device=x.device)
+    else:
+        ldy = _ld(out, "out", T, F, out_dtype, dev)
+    if residual is not None:
+        ldr = _ld(residual, "residual", T, F, out_dtype, dev)
+    px = x.data_ptr()
+    nws = 0
+    if workspace is not None:
+        if workspace.get_device() != dev or not workspace.is_contiguous():
+            raise ValueError("workspace must be a contiguous tensor on the plan's device")
+        nws = workspace.numel() * workspace.element_size()
+    elif (px | ldx * plan._bytes) & 15:                    # rows a tensor copy cannot take: the call may need room to lay them out
+        with k.torch.cuda.device(dev):
+            nws = L.ubp_linear_workspace_size(plan.handle, px, ldx, T)
+        if nws:
+            workspace = k.empty(nws, dtype=k.torch.uint8, device=x.device)
+            if stream is not None:
+                workspace.record_stream(stream)
+    _call(k, dev, L.ubp_linear, "ubp_linear",
+          (plan.handle, px, ldx, None if x_scales is None else _vec(x_scales, "x_scales", T, (k.f32,), dev), T,
+           None if bias is None else _vec(bias, "bias", plan.M, (k.f32,), dev), act,
+           None if residual is None else residual.data_ptr(), ldr, out.data_ptr(), ldy, ydt,
+           None if workspace is None else workspace.data_ptr(), nws), stream)
     return out
