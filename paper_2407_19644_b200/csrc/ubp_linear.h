@@ -12,16 +12,17 @@
 
 namespace ubp {
 
-// Input channels per slab: the sparse form's entries of a start row are in channel order with an offset kept at every slab
-// boundary, so that a launch may cut the reduction at any of them.
-constexpr int LIN_SLAB = 512;
+// Input channels per slab of the sparse form: its entries lie slab by slab, inside a slab by start row, so that the entries a
+// block of threads needs for its rows and one slab's activations are one contiguous run.
+constexpr int LIN_SLAB = 4096;
 
 // Device image (all offsets from its base, which is 256-byte aligned):
 //   [0, 256)      header; int32 status word at byte 0
 //   scale_off     float[M]: scale of each weight row (8-bit plans only)
-//   off_off       uint32[(M * nslab) + 1]: first entry of (start row i, slab s) at i * nslab + s
-//   idx_off       uint16[entries]: input channel of an entry
+//   off_off       uint32[nslab * M + 1]: first entry of (slab s, start row i) at s * M + i
+//   idx_off       uint16[entries]: input channel of an entry, counted from its slab's first
 //   val_off       weights of an entry: nbk consecutive output rows from its start row (plan's type)
+//                 (both arrays are readable up to the next multiple of 16 entries)
 //   dense_off     the densified weight [Mp][Kp] (plan's type), K contiguous. Gated plans interleave the two halves in
 //                 groups of 16 rows: dense row 32 g + i is gate row 16 g + i, dense row 32 g + 16 + i is up row 16 g + i.
 //                 Kp = C rounded up to 128 bytes, Mp = rows rounded up to 128; the padding is zero.

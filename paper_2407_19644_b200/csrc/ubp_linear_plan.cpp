@@ -74,12 +74,12 @@ int build_linear_image(const ubp_view_t &v, int dtype, bool gated, bool count_on
         for (auto &s : scale) s = std::max(s / 448.f, 1.17549435e-38f);
         std::memcpy(base + img.scale_off, scale.data(), (size_t)M * 4);
     }
-    // entries of (start row, slab), then their places
+    // entries of (slab, start row), then their places
     uint32_t *off = reinterpret_cast<uint32_t *>(base + img.off_off);
     const int ns = img.nslab;
     for (int i = 0; i < M; ++i)
         for (int32_t k = v.indptr[i]; k < v.indptr[i + 1]; ++k)
-            for (int s = 0; s < sub; ++s) ++off[(size_t)(i + s * nbk) * ns + (size_t)(v.indices[k] / LIN_SLAB) + 1];
+            for (int s = 0; s < sub; ++s) ++off[(size_t)(v.indices[k] / LIN_SLAB) * M + (size_t)(i + s * nbk) + 1];
     for (size_t q = 0; q < (size_t)M * ns; ++q) off[q + 1] += off[q];
     std::vector<uint32_t> next(off, off + (size_t)M * ns);
     uint16_t *idx = reinterpret_cast<uint16_t *>(base + img.idx_off);
@@ -88,8 +88,8 @@ int build_linear_image(const ubp_view_t &v, int dtype, bool gated, bool count_on
         for (int32_t k = v.indptr[i]; k < v.indptr[i + 1]; ++k) {
             const int j = v.indices[k];
             for (int s = 0; s < sub; ++s) {
-                const uint32_t e = next[(size_t)(i + s * nbk) * ns + (size_t)(j / LIN_SLAB)]++;
-                idx[e] = (uint16_t)j;
+                const uint32_t e = next[(size_t)(j / LIN_SLAB) * M + (size_t)(i + s * nbk)]++;
+                idx[e] = (uint16_t)(j % LIN_SLAB);
                 for (int t = 0; t < nbk; ++t) {
                     const int row = i + s * nbk + t;
                     uint8_t *w = val + ((size_t)e * nbk + (size_t)t) * b;

@@ -12,9 +12,12 @@
 // The statistics are fp32; x + r is not rounded before it is squared and multiplied.
 //
 // TPR threads work on a row, each on NV groups of eight elements (16-byte accesses) where every row starts on a 16-byte
-// boundary, else on single elements. Rows that do not fit the registers of 512 threads are read twice (the second time
-// from L2): nothing is written before the row's statistics are complete, and every element is read and written by one
-// thread, so h may be written over x or r in every form.
+// boundary, else on single elements. The grid stays on the SMs and walks the rows; a row's loads are issued before the
+// statistics of the row before it are reduced, so that the reduction's two barrier-and-shuffle latencies and the stores pass
+// under loads in flight (one row per block without that: 103 us instead of 61 for rows 8192 x 16384, HBM 45 % busy).
+// Rows that do not fit the registers of 512 threads are read twice (the second time from L2): there nothing is written before
+// the row's statistics are complete. Every element is read and written by one thread, so h may be written over x or r in
+// every form.
 #include <cuda_runtime.h>
 
 #include <cstdint>
@@ -24,8 +27,6 @@
 
 namespace ubp {
 namespace {
-
-constexpr int ROWS_MAX_TPR = 512;   // threads of a row at most (128 registers each)
 
 struct RowArgs {
     const void *x;
@@ -41,22 +42,23 @@ struct RowArgs {
     int gamma_f32;
 };
 
-// (sum, max) over the TPR threads of a row; TPR is a power of two, rows of one block lie in consecutive threads. Every
-// thread of the row gets the same two values: the partial results are combined in one fixed order.
-template <bool NORM, bool Q>
-__device__ __forceinline__ void row_reduce(float &sum, float &mx, int tpr, float2 *scratch)
+// (sum, max) over the TPR threads of a row, in one fixed order, to every one of them. `scratch` alternates between two
+// buffers from row to row: a warp that is one row ahead does not touch what the others still read.
+template <bool NORM, bool Q, int TPR>
+__device__ __forceinline__ void row_reduce(float &sum, float &mx, float2 *scratch)
 {
-    const int w = tpr < 32 ? tpr : 32;
-    for (int o = w >> 1; o > 0; o >>= 1) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
         if (NORM) sum += __shfl_xor_sync(0xffffffffu, sum, o);
         if (Q) mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, o));
     }
-    if (tpr > 32) {
-        const int warp = threadIdx.x >> 5, nw = tpr >> 5, first = warp / nw * nw;
-        if ((threadIdx.x & 31) == 0) scratch[warp] = make_float2(sum, mx);
+    if constexpr (TPR > 32) {
+        constexpr int NW = TPR / 32;
+        if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = make_float2(sum, mx);
         __syncthreads();
-        float2 v = (int)(threadIdx.x & 31) < nw ? scratch[first + (threadIdx.x & 31)] : make_float2(0.f, 0.f);
-        for (int o = 16; o > 0; o >>= 1) {
+        float2 v = scratch[threadIdx.x & (NW - 1)];
+#pragma unroll
+        for (int o = NW / 2; o > 0; o >>= 1) {
             if (NORM) v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
             if (Q) v.y = max_nan(v.y, __shfl_xor_sync(0xffffffffu, v.y, o));
         }
@@ -74,159 +76,224 @@ template <typename T> __device__ __forceinline__ float gamma1(const RowArgs &a, 
     return a.gamma_f32 ? static_cast<const float *>(a.gamma)[c] : to_f32<T>(static_cast<const T *>(a.gamma)[c]);
 }
 
-// T: type of x, r, h; TO: output type; VEC: eight elements an access, else one; NV: accesses a thread keeps in registers,
-// 0 = any length, read twice
-template <typename T, typename TO, bool NORM, bool VEC, int NV>
-__global__ void __launch_bounds__(ROWS_MAX_TPR) ubp_rows_kernel(const RowArgs a, const int tpr)
-{
-    constexpr bool Q = sizeof(TO) == 1;
-    constexpr int E = VEC ? 8 : 1;
-    __shared__ float2 scratch[ROWS_MAX_TPR / 32];
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int rows = blockDim.x / tpr, lane = threadIdx.x % tpr;
-    const int64_t row = (int64_t)blockIdx.x * rows + threadIdx.x / tpr;
-    const bool live = row < a.T;
-    const T *x = static_cast<const T *>(a.x) + (live ? row : 0) * a.ldx;
-    const T *r = a.r ? static_cast<const T *>(a.r) + (live ? row : 0) * a.ldr : nullptr;
-    T *hrow = a.h ? static_cast<T *>(a.h) + (live ? row : 0) * a.ldh : nullptr;
-    TO *y = static_cast<TO *>(a.y) + (live ? row : 0) * a.ldy;
-    const int step = tpr * E;
-
-    auto load = [&](int c, float (&v)[E]) {
-        if constexpr (VEC) {
-            load8<T>(x + c, v);
-            if (r) {
-                float w[8];
-                load8<T>(r + c, w);
+// E elements of x (or r) as they lie in memory
+template <typename T, int E> struct Raw {
+    static constexpr int N = E * (int)sizeof(T) / 16;
+    uint4 w[N];
+    __device__ __forceinline__ void load(const T *p)
+    {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] += w[e];
+        for (int i = 0; i < N; ++i) w[i] = reinterpret_cast<const uint4 *>(p)[i];
+    }
+    __device__ __forceinline__ void get(float (&v)[E]) const
+    {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                v[4 * i] = __uint_as_float(w[i].x); v[4 * i + 1] = __uint_as_float(w[i].y);
+                v[4 * i + 2] = __uint_as_float(w[i].z); v[4 * i + 3] = __uint_as_float(w[i].w);
             }
         } else {
-            v[0] = to_f32<T>(x[c]);
-            if (r) v[0] += to_f32<T>(r[c]);
-        }
-    };
-    auto gamma = [&](int c, float (&g)[E]) {
-        if constexpr (VEC) gamma8<T>(a, c, g);
-        else g[0] = gamma1<T>(a, c);
-    };
-    auto put_h = [&](int c, const float (&h)[E]) {
-        if constexpr (VEC) {
-            if (hrow) store8<T>(hrow + c, h);
-        } else {
-            if (hrow) hrow[c] = from_f32<T>(h[0]);
-        }
-    };
-    auto put = [&](int c, const float (&t)[E], float rinv, float sinv) {
-        float o[E];
+            const uint32_t u[4] = {w[0].x, w[0].y, w[0].z, w[0].w};
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            o[e] = NORM ? t[e] * rinv : t[e];
-            if (Q) o[e] *= sinv;
+            for (int i = 0; i < 4; ++i) {
+                const float2 f = unpack2<T>(u[i]);
+                v[2 * i] = f.x; v[2 * i + 1] = f.y;
+            }
         }
-        if constexpr (VEC) store8<TO>(y + c, o);
-        else y[c] = from_f32<TO>(o[0]);
-    };
+    }
+};
+template <typename T> struct Raw<T, 1> {
+    T w;
+    __device__ __forceinline__ void load(const T *p) { w = *p; }
+    __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = to_f32<T>(w); }
+};
 
-    float sum = 0.f, mx = 0.f;
+__host__ __device__ constexpr int rows_block(int tpr) { return tpr < 128 ? 128 : tpr; }          // threads of a block
+// Blocks an SM holds: 1024 threads of 64 registers, or 512 of 128 where a thread keeps more than 48 values of the row and
+// the next one (nv accesses of e values; the next row's x and r as they lie in memory).
+__host__ __device__ constexpr int rows_blocks_per_sm(int tpr, bool norm, int e, int nv, int size)
+{
+    return (nv * e + nv * (e * size + 3) / 4 * (norm ? 2 : 1) > 48 ? 512 : 1024) / rows_block(tpr);
+}
+
+// T: type of x, r, h; TO: output type; E: elements an access (8 or 1); TPR: threads a row; NV: accesses a thread keeps in
+// registers, 0 = any length, read twice
+template <typename T, typename TO, bool NORM, int E, int TPR, int NV>
+__global__ void __launch_bounds__(rows_block(TPR), rows_blocks_per_sm(TPR, NORM, E, NV, (int)sizeof(T))) ubp_rows_kernel(const RowArgs a)
+{
+    constexpr bool Q = sizeof(TO) == 1;
+    constexpr int STEP = TPR * E, ROWS = rows_block(TPR) / TPR;
+    __shared__ float2 scratch[2][16];
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int lane = threadIdx.x % TPR, c0 = lane * E;
+    const int64_t stride = (int64_t)gridDim.x * ROWS;
+    int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / TPR;
+    const T *x = static_cast<const T *>(a.x) + c0, *r = static_cast<const T *>(a.r) + c0;
+    T *h = static_cast<T *>(a.h) + c0;
+    TO *y = static_cast<TO *>(a.y) + c0;
+    const bool has_r = NORM && a.r, has_h = NORM && a.h;
+
+    float sum, mx;
+    auto store_h = [&](int64_t at, const float (&v)[E]) {
+        if constexpr (E == 8) store8<T>(h + at, v);
+        else h[at] = from_f32<T>(v[0]);
+    };
     // h -> t = h * gamma (t = h without a norm), and both into the row's statistics
     auto stats = [&](int c, float (&v)[E]) {
         float g[E];
-        if constexpr (NORM) gamma(c, g);
+        if constexpr (NORM) {
+            if constexpr (E == 8) gamma8<T>(a, c, g);
+            else g[0] = gamma1<T>(a, c);
+        }
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             if (NORM) { sum = fmaf(v[e], v[e], sum); v[e] *= g[e]; }
             if (Q) mx = max_nan(mx, fabsf(v[e]));
         }
     };
-    constexpr int NK = NV > 0 ? NV : 1;
-    float v[NK][E];
-    if constexpr (NV > 0) {
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const int c = k * step + lane * E;
-            if (live && c < a.C) load(c, v[k]);
-        }
-#pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const int c = k * step + lane * E;
-            if (live && c < a.C) {
-                if constexpr (NORM) put_h(c, v[k]);
-                stats(c, v[k]);
-            }
-        }
-    } else {
-        if (live)
-            for (int c = lane * E; c < a.C; c += step) { load(c, v[0]); stats(c, v[0]); }
-    }
-    row_reduce<NORM, Q>(sum, mx, tpr, scratch);
-    const float rinv = NORM ? rsqrtf(sum / (float)a.C + a.eps) : 1.f;
+    float rinv, sinv;
     // A product with 1 / s instead of a division for each value (which made the kernel ALU-bound: 336 us instead of HBM's
     // 143 on 16384 x 8192): the quotient is off by at most 1.5 units of 2^-24, against half a code step of 2^-4. s is at
     // least 2^-126, so 1 / s is finite. rinv and 1 / s stay two products: theirs could overflow for a row of tiny values.
-    float sinv = 1.f;
-    if (Q) {
-        const float s = max_nan(__fdiv_rn(NORM ? mx * rinv : mx, E4M3_MAX), ROW_SCALE_MIN);
-        sinv = __fdiv_rn(1.f, s);
-        if (live && lane == 0) a.scales[row] = s;
-    }
-    if constexpr (NV > 0) {
+    auto finish = [&](bool live) {
+        rinv = NORM ? rsqrtf(sum / (float)a.C + a.eps) : 1.f;
+        sinv = 1.f;
+        if (Q) {
+            const float s = max_nan(__fdiv_rn(NORM ? mx * rinv : mx, E4M3_MAX), ROW_SCALE_MIN);
+            sinv = __fdiv_rn(1.f, s);
+            if (live && lane == 0) a.scales[row] = s;
+        }
+    };
+    auto put = [&](int64_t at, const float (&v)[E]) {
+        float o[E];
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-            const int c = k * step + lane * E;
-            if (live && c < a.C) put(c, v[k], rinv, sinv);
+        for (int e = 0; e < E; ++e) {
+            o[e] = NORM ? v[e] * rinv : v[e];
+            if (Q) o[e] *= sinv;
+        }
+        if constexpr (E == 8) store8<TO>(y + at, o);
+        else y[at] = from_f32<TO>(o[0]);
+    };
+
+    // (rows of one block differ by less than ROWS, so all its threads make the same number of rounds)
+    const int64_t rounds = ((int64_t)blockIdx.x * ROWS < a.T) ? (a.T - (int64_t)blockIdx.x * ROWS + stride - 1) / stride : 0;
+    if constexpr (NV > 0) {
+        Raw<T, E> nx[NV], nr[NORM ? NV : 1];
+        auto fetch = [&](int64_t t) {
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+                if (t < a.T && c0 + k * STEP < a.C) {
+                    nx[k].load(x + t * a.ldx + k * STEP);
+                    if (NORM && has_r) nr[NORM ? k : 0].load(r + t * a.ldr + k * STEP);
+                }
+        };
+        fetch(row);
+        for (int64_t i = 0; i < rounds; ++i, row += stride) {
+            const bool live = row < a.T;
+            float v[NV][E];
+            sum = 0.f; mx = 0.f;
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+                if (live && c0 + k * STEP < a.C) {
+                    nx[k].get(v[k]);
+                    if constexpr (NORM) {
+                        if (has_r) {
+                            float w[E];
+                            nr[k].get(w);
+#pragma unroll
+                            for (int e = 0; e < E; ++e) v[k][e] += w[e];
+                        }
+                        if (has_h) store_h(row * a.ldh + k * STEP, v[k]);
+                    }
+                    stats(c0 + k * STEP, v[k]);
+                }
+            fetch(row + stride);
+            row_reduce<NORM, Q, TPR>(sum, mx, scratch[i & 1]);
+            finish(live);
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+                if (live && c0 + k * STEP < a.C) put(row * a.ldy + k * STEP, v[k]);
         }
     } else {
-        if (live)
-            for (int c = lane * E; c < a.C; c += step) {
-                load(c, v[0]);
-                if constexpr (NORM) put_h(c, v[0]);
-                stats(c, v[0]);      // (the statistics are complete; this only applies gamma)
-                put(c, v[0], rinv, sinv);
+        for (int64_t i = 0; i < rounds; ++i, row += stride) {      // (one row a block: every thread's row is live)
+            sum = 0.f; mx = 0.f;
+            auto load = [&](int64_t c, float (&v)[E]) {
+                Raw<T, E> q;
+                q.load(x + row * a.ldx + c);
+                q.get(v);
+                if (has_r) {
+                    float w[E];
+                    q.load(r + row * a.ldr + c);
+                    q.get(w);
+#pragma unroll
+                    for (int e = 0; e < E; ++e) v[e] += w[e];
+                }
+            };
+#pragma unroll 4
+            for (int c = 0; c < a.C - c0; c += STEP) {
+                float v[E];
+                load(c, v);
+                stats(c0 + c, v);
             }
+            row_reduce<NORM, Q, TPR>(sum, mx, scratch[i & 1]);
+            finish(true);
+#pragma unroll 2
+            for (int c = 0; c < a.C - c0; c += STEP) {
+                float v[E];
+                load(c, v);
+                if (has_h) store_h(row * a.ldh + c, v);
+                stats(c0 + c, v);      // (the statistics are complete; this only applies gamma)
+                put(row * a.ldy + c, v);
+            }
+        }
     }
 }
 
-template <typename T, typename TO, bool NORM>
-int launch_rows_t(const RowArgs &a, bool vec, cudaStream_t stream)
+template <typename T, typename TO, bool NORM, int E, int TPR, int NV>
+int launch_rows_k(const RowArgs &a, int sms, cudaStream_t stream)
 {
-    // Threads per row: enough for at most four (vector) or eight (scalar) accesses a thread; blocks of at least 128 threads.
-    const int e = vec ? 8 : 1;
-    const int64_t groups = ((int64_t)a.C + e - 1) / e;
-    int tpr = 32;
-    while (tpr < ROWS_MAX_TPR && (int64_t)tpr * (vec ? 4 : 8) < groups) tpr *= 2;
-    // few rows: the latency of one row is what counts, so spread it
-    while (tpr < ROWS_MAX_TPR && a.T * tpr < 148 * 512 && tpr < groups) tpr *= 2;
-    const int threads = tpr < 128 ? 128 : tpr, rows = threads / tpr;
-    const int64_t blocks = (a.T + rows - 1) / rows;
-    if (blocks > 0x7fffffff) return UBP_E_UNSUPPORTED;
-    const int nv = (int)((groups + tpr - 1) / tpr);
-    using Fn = void (*)(const RowArgs, const int);
-    Fn fn;
-    if (vec) {
-        if (nv <= 1) fn = ubp_rows_kernel<T, TO, NORM, true, 1>;
-        else if (nv <= 2) fn = ubp_rows_kernel<T, TO, NORM, true, 2>;
-        else if (nv <= 4) fn = ubp_rows_kernel<T, TO, NORM, true, 4>;
-        else fn = ubp_rows_kernel<T, TO, NORM, true, 0>;
-    } else {
-        if (nv <= 8) fn = ubp_rows_kernel<T, TO, NORM, false, 8>;
-        else if (nv <= 16) fn = ubp_rows_kernel<T, TO, NORM, false, 16>;
-        else fn = ubp_rows_kernel<T, TO, NORM, false, 0>;
-    }
+    const int64_t rows = rows_block(TPR) / TPR, need = (a.T + rows - 1) / rows, fit = (int64_t)sms * rows_blocks_per_sm(TPR, NORM, E, NV, (int)sizeof(T));
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)blocks);
-    cfg.blockDim = dim3((unsigned)threads);
+    cfg.gridDim = dim3((unsigned)(need < fit ? need : fit));
+    cfg.blockDim = dim3((unsigned)rows_block(TPR));
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    cudaError_t err = cudaLaunchKernelEx(&cfg, fn, a, tpr);
+    cudaError_t err = cudaLaunchKernelEx(&cfg, ubp_rows_kernel<T, TO, NORM, E, TPR, NV>, a);
     if (err == cudaSuccess) err = cudaGetLastError();
     if (err != cudaSuccess) { set_last_cuda_error((int)err); return UBP_E_CUDA; }
     return UBP_OK;
+}
+
+// Threads and accesses a row by its length alone: the fewest threads whose registers hold it, 32 (a warp a row, no barrier),
+// 128 or 512.
+template <typename T, typename TO, bool NORM>
+int launch_rows_t(const RowArgs &a, bool vec, cudaStream_t st)
+{
+    int sms = 148, dev = 0;
+    if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    if (vec) {
+        if (a.C <= 256) return launch_rows_k<T, TO, NORM, 8, 32, 1>(a, sms, st);
+        if (a.C <= 512) return launch_rows_k<T, TO, NORM, 8, 32, 2>(a, sms, st);
+        if (a.C <= 1024) return launch_rows_k<T, TO, NORM, 8, 128, 1>(a, sms, st);
+        if (a.C <= 2048) return launch_rows_k<T, TO, NORM, 8, 128, 2>(a, sms, st);
+        if (a.C <= 4096) return launch_rows_k<T, TO, NORM, 8, 512, 1>(a, sms, st);
+        if (a.C <= 8192) return launch_rows_k<T, TO, NORM, 8, 512, 2>(a, sms, st);
+        // (a norm of fp32 rows would need 32 + 64 registers for the row and the next one: read twice instead)
+        if constexpr (!(NORM && sizeof(T) == 4))
+            if (a.C <= 16384) return launch_rows_k<T, TO, NORM, 8, 512, 4>(a, sms, st);
+        return launch_rows_k<T, TO, NORM, 8, 512, 0>(a, sms, st);
+    }
+    if (a.C <= 256) return launch_rows_k<T, TO, NORM, 1, 32, 8>(a, sms, st);
+    if (a.C <= 1024) return launch_rows_k<T, TO, NORM, 1, 128, 8>(a, sms, st);
+    if (a.C <= 4096) return launch_rows_k<T, TO, NORM, 1, 512, 8>(a, sms, st);
+    if (a.C <= 8192) return launch_rows_k<T, TO, NORM, 1, 512, 16>(a, sms, st);
+    return launch_rows_k<T, TO, NORM, 1, 512, 0>(a, sms, st);
 }
 
 template <bool NORM>

@@ -20,11 +20,11 @@ def replay(img, geom, offs, M, C, dtype):
     val = np.frombuffer(img, "<u2" if b == 2 else "u1", n * nbk, offs["val"]).reshape(n, nbk)
     out, hits = np.zeros((M, C), val.dtype), np.zeros((M, C), np.int32)
     assert off[0] == 0 and (np.diff(off.astype(np.int64)) >= 0).all()
-    for i in range(M):
-        for s in range(ns):
-            for e in range(off[i * ns + s], off[i * ns + s + 1]):
-                j = int(idx[e])
-                assert s * 512 <= j < min(C, (s + 1) * 512) and i + nbk <= M
+    for s in range(ns):
+        for i in range(M):
+            for e in range(off[s * M + i], off[s * M + i + 1]):
+                j = s * 4096 + int(idx[e])
+                assert int(idx[e]) < 4096 and j < C and i + nbk <= M
                 out[i:i + nbk, j] = val[e]
                 hits[i:i + nbk, j] += 1
     return out, hits
@@ -32,7 +32,7 @@ def replay(img, geom, offs, M, C, dtype):
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, F8], ids=["bf16", "f16", "e4m3"])
 @pytest.mark.parametrize("M,C,Nb,p,gated", [(1, 1, 1, 0, False), (64, 600, 4, 60, False), (66, 37, 5, 40, True), (50, 1100, 16, 70, True),
-                                            (34, 513, 6, 50, True), (130, 512, 2, 80, False), (32, 20, 8, 100, True)])
+                                            (34, 4097, 6, 50, True), (130, 512, 2, 80, False), (40, 8200, 4, 80, True), (32, 20, 8, 100, True)])
 def test_plan_image_holds_the_weight(dtype, M, C, Nb, p, gated):
     W, mask = make_weight(M, C, Nb, p, 5)
     img, geom, offs = ubp.linear_plan_image(ubp.ubp_pack(W, mask, Nb), dtype, gated)
