@@ -432,9 +432,9 @@ int ubp_quant_rows(const void *x, int64_t ldx, int dtype, int64_t T, int C, void
  * features or 2^31 entries. */
 typedef struct ubp_linear_plan ubp_linear_plan_t;
 int ubp_linear_plan_size(const void *blob, size_t len, int dtype, int gated, size_t *dev_bytes);
-/* geom receives {nbk, nslab, Mp, Kp, bytes per value}; offs the byte offsets of {row scales, entry offsets, channel
- * indices, weights, dense matrix} in the image. */
-int ubp_linear_plan_image(const void *blob, size_t len, int dtype, int gated, void *host_buf, size_t cap, int32_t geom[5],
+/* geom receives {weights per entry, entries per 16-byte chunk, dense rows, dense row length, bytes per value, lanes per
+ * row}; offs the byte offsets of {row scales, bundle offsets, channel indices, weights, dense matrix} in the image. */
+int ubp_linear_plan_image(const void *blob, size_t len, int dtype, int gated, void *host_buf, size_t cap, int32_t geom[6],
                           int64_t offs[5]);
 int ubp_linear_plan_build(const void *blob, size_t len, int dtype, int gated, void *dev_buf, size_t dev_bytes, void *stream,
                           ubp_linear_plan_t **plan);

@@ -665,9 +665,9 @@ def linear_plan_image(blob: bytes, dtype, gated: bool = False):
     dt = _dtypes()[dtype]
     _chk(L.ubp_linear_plan_size(_np_ptr(b), b.size, dt, int(gated), C.byref(n)), "ubp_linear_plan_size")
     buf = np.zeros(n.value, np.uint8)
-    geom, offs = (C.c_int32 * 5)(), (C.c_int64 * 5)()
+    geom, offs = (C.c_int32 * 6)(), (C.c_int64 * 5)()
     _chk(L.ubp_linear_plan_image(_np_ptr(b), b.size, dt, int(gated), _np_ptr(buf), n.value, geom, offs), "ubp_linear_plan_image")
-    return (buf, dict(zip(["nbk", "nslab", "Mp", "Kp", "bytes"], [int(g) for g in geom])),
+    return (buf, dict(zip(["nbk", "epc", "Mp", "Kp", "bytes", "lanes"], [int(g) for g in geom])),
             dict(zip(["scale", "off", "idx", "val", "dense"], [int(o) for o in offs])))
 
 

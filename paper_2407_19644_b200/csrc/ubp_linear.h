@@ -12,25 +12,23 @@
 
 namespace ubp {
 
-// Input channels per slab of the sparse form: its entries lie slab by slab, inside a slab by start row, so that the entries a
-// block of threads needs for its rows and one slab's activations are one contiguous run.
-constexpr int LIN_SLAB = 4096;
-
 // Device image (all offsets from its base, which is 256-byte aligned):
 //   [0, 256)      header; int32 status word at byte 0
 //   scale_off     float[M]: scale of each weight row (8-bit plans only)
-//   off_off       uint32[nslab * M + 1]: first entry of (slab s, start row i) at s * M + i
-//   idx_off       uint16[entries]: input channel of an entry, counted from its slab's first
-//   val_off       weights of an entry: nbk consecutive output rows from its start row (plan's type)
-//                 (both arrays are readable up to the next multiple of 16 entries)
+//   off_off       uint32[bundles + 1]: first step of a bundle. A bundle is 32 / lanes consecutive start rows, a row is dealt
+//                 to `lanes` lanes of a warp in chunks of 16 bytes of weights = epc entries of nbk weights each, and a step is
+//                 one chunk for each of the warp's 32 lanes (lane = row in the bundle * lanes + place): chunk i of a row lies in
+//                 step i / lanes, place i mod lanes. Rows are filled up to their bundle's steps with entries of weight zero.
+//   idx_off       uint16[steps][32][epc]: input channel of an entry (of a filler: the row's last channel, 0 in an empty row)
+//   val_off       weights [steps][32][epc][nbk]: consecutive output rows from the entry's start row (plan's type)
 //   dense_off     the densified weight [Mp][Kp] (plan's type), K contiguous. Gated plans interleave the two halves in
 //                 groups of 16 rows: dense row 32 g + i is gate row 16 g + i, dense row 32 g + 16 + i is up row 16 g + i.
 //                 Kp = C rounded up to 128 bytes, Mp = rows rounded up to 128; the padding is zero.
 struct LinearImage {
     std::vector<uint8_t> bytes;
     size_t scale_off = 0, off_off = 0, idx_off = 0, val_off = 0, dense_off = 0, total = 0;
-    int nbk = 1, nslab = 1, Mp = 0, Kp = 0;
-    int64_t entries = 0;
+    int nbk = 1, epc = 1, lanes = 8, bundles = 0, Mp = 0, Kp = 0;
+    int64_t entries = 0, steps = 0;
 };
 int build_linear_image(const ubp_view_t &v, int dtype, bool gated, bool count_only, LinearImage &img);
 

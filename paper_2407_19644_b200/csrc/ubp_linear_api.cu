@@ -43,13 +43,15 @@ int ubp_linear_plan_size(const void *blob, size_t len, int dtype, int gated, siz
     if (!dev_bytes) return UBP_E_ARG;
     ubp_view_t v;
     if (int rc = ubp::blob_view(blob, len, &v)) return rc;
-    ubp::LinearImage img;
-    if (int rc = ubp::build_linear_image(v, dtype, gated != 0, true, img)) return rc;
-    *dev_bytes = img.total;
+    try {
+        ubp::LinearImage img;
+        if (int rc = ubp::build_linear_image(v, dtype, gated != 0, true, img)) return rc;
+        *dev_bytes = img.total;
+    } catch (const std::bad_alloc &) { return UBP_E_SPACE; }
     return UBP_OK;
 }
 
-int ubp_linear_plan_image(const void *blob, size_t len, int dtype, int gated, void *host_buf, size_t cap, int32_t geom[5],
+int ubp_linear_plan_image(const void *blob, size_t len, int dtype, int gated, void *host_buf, size_t cap, int32_t geom[6],
                           int64_t offs[5])
 {
     if (!host_buf || !geom || !offs) return UBP_E_ARG;
@@ -60,7 +62,8 @@ int ubp_linear_plan_image(const void *blob, size_t len, int dtype, int gated, vo
         if (int rc = ubp::build_linear_image(v, dtype, gated != 0, false, img)) return rc;
         if (cap < img.total) return UBP_E_SPACE;
         std::memcpy(host_buf, img.bytes.data(), img.total);
-        geom[0] = img.nbk; geom[1] = img.nslab; geom[2] = img.Mp; geom[3] = img.Kp; geom[4] = ubp::dtype_size(dtype);
+        geom[0] = img.nbk; geom[1] = img.epc; geom[2] = img.Mp; geom[3] = img.Kp; geom[4] = ubp::dtype_size(dtype);
+        geom[5] = img.lanes;
         offs[0] = (int64_t)img.scale_off; offs[1] = (int64_t)img.off_off; offs[2] = (int64_t)img.idx_off;
         offs[3] = (int64_t)img.val_off; offs[4] = (int64_t)img.dense_off;
     } catch (const std::bad_alloc &) { return UBP_E_SPACE; }

@@ -11,22 +11,30 @@ from linear_ref import F8, make_weight, quantise
 DT = {torch.float16: 1, torch.bfloat16: 2, F8: 3}
 
 
-def replay(img, geom, offs, M, C, dtype):
+def replay(img, geom, offs, M, C, mask_at):
     """The image's sparse entries scattered into a dense [M][C] array of codes, and how often each place was written."""
-    nbk, ns, b = geom["nbk"], geom["nslab"], geom["bytes"]
-    off = np.frombuffer(img, "<u4", M * ns + 1, offs["off"])
+    nbk, epc, b, lanes = geom["nbk"], geom["epc"], geom["bytes"], geom["lanes"]
+    rb = 32 // lanes
+    assert nbk * epc * b == 16 and lanes in (8, 16, 32)
+    nb = -(-M // rb)
+    off = np.frombuffer(img, "<u4", nb + 1, offs["off"])
     n = int(off[-1])
-    idx = np.frombuffer(img, "<u2", n, offs["idx"])
-    val = np.frombuffer(img, "<u2" if b == 2 else "u1", n * nbk, offs["val"]).reshape(n, nbk)
+    idx = np.frombuffer(img, "<u2", n * 32 * epc, offs["idx"]).reshape(n, rb, lanes * epc)
+    val = np.frombuffer(img, "<u2" if b == 2 else "u1", n * 32 * epc * nbk, offs["val"]).reshape(n, rb, lanes * epc, nbk)
     out, hits = np.zeros((M, C), val.dtype), np.zeros((M, C), np.int32)
     assert off[0] == 0 and (np.diff(off.astype(np.int64)) >= 0).all()
-    for s in range(ns):
-        for i in range(M):
-            for e in range(off[s * M + i], off[s * M + i + 1]):
-                j = s * 4096 + int(idx[e])
-                assert int(idx[e]) < 4096 and j < C and i + nbk <= M
-                out[i:i + nbk, j] = val[e]
-                hits[i:i + nbk, j] += 1
+    for i in range(nb * rb):
+        q, u = divmod(i, rb)
+        js, ws = idx[off[q]:off[q + 1], u].reshape(-1), val[off[q]:off[q + 1], u].reshape(-1, nbk)
+        seen = set()
+        for e, j in enumerate(js.tolist()):
+            assert j < C
+            if i >= M or j in seen or not (i + nbk <= M and mask_at(i, j)):   # a filler: the row's last channel again, weight zero
+                assert not ws[e].any() and (j == js[e - 1] if e and seen else j == 0)
+                continue
+            seen.add(j)
+            out[i:i + nbk, j] = ws[e]
+            hits[i:i + nbk, j] += 1
     return out, hits
 
 
@@ -42,7 +50,10 @@ def test_plan_image_holds_the_weight(dtype, M, C, Nb, p, gated):
         assert np.array_equal(np.frombuffer(img, "<f4", M, offs["scale"]), s.numpy())
     else:
         want = torch.from_numpy(W).to(dtype).view(torch.int16).numpy().view(np.uint16) * (mask != 0)
-    got, hits = replay(img, geom, offs, M, C, dtype)
+    # start rows of the entries: the blocks' own, and every nbk rows inside them
+    v = ubp.blob_view(ubp.ubp_pack(W, mask, Nb))
+    starts = {(i + s, int(j)) for i in range(M) for j in v["indices"][v["indptr"][i]:v["indptr"][i + 1]] for s in range(0, Nb, geom["nbk"])}
+    got, hits = replay(img, geom, offs, M, C, lambda i, j: (i, j) in starts)
     assert np.array_equal(hits, (mask != 0).astype(np.int32))
     assert np.array_equal(got, want)
     Mp, Kp, b = geom["Mp"], geom["Kp"], geom["bytes"]
