@@ -12,16 +12,35 @@ namespace ubp {
 // u < -88, where the quotient is -0 or 0, as the exact value rounds to (below 2^-120).
 __device__ __forceinline__ float v_sigmoid(float v, float u) { return __fdividef(v, 1.f + __expf(fminf(-u, 80.f))); }
 
-__device__ __forceinline__ float apply_act(float v, int act)
+// (the choice outside the loop: with the switch inside an unrolled one, all five activations sit in the path N times over and
+// the epilogue of the tensor-core kernel ran from instruction cache misses, 4 us for 32 x 32 outputs)
+template <int N> __device__ __forceinline__ void apply_act(float (&v)[N], int act)
 {
     switch (act) {
-        case UBP_ACT_RELU: return fmaxf(v, 0.f);
-        case UBP_ACT_GELU: return 0.5f * v * (1.f + erff(v * 0.70710678118654752f));
+        case UBP_ACT_RELU:
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = fmaxf(v[i], 0.f);
+            break;
+        case UBP_ACT_GELU:
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = 0.5f * v[i] * (1.f + erff(v[i] * 0.70710678118654752f));
+            break;
         case UBP_ACT_GELU_TANH:   // 0.5 v (1 + tanh(u)) = v sigmoid(2 u), u = sqrt(2 / pi) (v + 0.044715 v^3)
-            return v_sigmoid(v, 1.5957691216057308f * (v + 0.044715f * v * v * v));
-        case UBP_ACT_SILU: return v_sigmoid(v, v);
-        default: return v;
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = v_sigmoid(v[i], 1.5957691216057308f * (v[i] + 0.044715f * v[i] * v[i] * v[i]));
+            break;
+        case UBP_ACT_SILU:
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = v_sigmoid(v[i], v[i]);
+            break;
+        default: break;
     }
+}
+__device__ __forceinline__ float apply_act(float v, int act)
+{
+    float a[1] = {v};
+    apply_act<1>(a, act);
+    return a[0];
 }
 
 // one output element of type ydt at index i of a row-major array

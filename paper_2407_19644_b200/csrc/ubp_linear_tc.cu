@@ -43,6 +43,7 @@ struct TcLinArgs {
     int ydt;
     int nk;              // chunks of the reduction
     int rows;            // dense rows that hold the layer (M, or 2 x F rounded up to 16)
+    int unaligned_bias;  // 1: bias is not 16-byte aligned
 };
 
 __device__ __forceinline__ uint64_t kmajor_desc(uint32_t saddr) { return make_desc(saddr, 16, 1024, LT_SWZ_128B); }
@@ -231,25 +232,39 @@ ubp_linear_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
             const int up = a.F + f;
             const float b0 = a.bias ? a.bias[f] : 0.f, b1 = (a.gated && a.bias) ? a.bias[up] : 0.f;
             const float w0 = F8 ? p.wscale[f] : 1.f, w1 = (F8 && a.gated) ? p.wscale[up] : 1.f;
-            for (int t = ta + (int)threadIdx.x / nout; t < tb; t += 256 / nout) {
-                const float *src = red + (size_t)t * 128 + dl;
-                float z0 = 0.f, z1 = 0.f;
-                if (S > 1) {
-                    for (int k = 0; k < S; ++k) z0 += ld_rank(src, (uint32_t)k);
-                    if (a.gated) for (int k = 0; k < S; ++k) z1 += ld_rank(src + 16, (uint32_t)k);
-                } else {
-                    z0 = src[0];
-                    if (a.gated) z1 = src[16];
+            // four tokens at a time: their loads and arithmetic overlap (one at a time was 0.1 us a token)
+            constexpr int TB = 4;
+            const int step = 256 / nout;
+            for (int t1 = ta + (int)threadIdx.x / nout; t1 < tb; t1 += TB * step) {
+                float z0[TB], z1[TB], add[TB], xs[TB];
+#pragma unroll
+                for (int i = 0; i < TB; ++i) {
+                    const int t = t1 + i * step;
+                    z0[i] = z1[i] = add[i] = 0.f;
+                    xs[i] = 1.f;
+                    if (t < tb) {
+                        if (a.res) add[i] = load_elem(a.res, (t0 + t) * a.ldr + f, p.ydt);
+                        if (F8) xs[i] = a.xs[t0 + t];
+                    }
                 }
-                if (F8) {
-                    const float xs = a.xs[t0 + t];
-                    z0 *= xs * w0;
-                    z1 *= xs * w1;
+                for (int k = 0; k < S; ++k)
+#pragma unroll
+                    for (int i = 0; i < TB; ++i) {
+                        const float *src = red + (size_t)(t1 + i * step < tb ? t1 + i * step : t1) * 128 + dl;
+                        z0[i] += S > 1 ? ld_rank(src, (uint32_t)k) : *src;
+                        if (a.gated) z1[i] += S > 1 ? ld_rank(src + 16, (uint32_t)k) : src[16];
+                    }
+#pragma unroll
+                for (int i = 0; i < TB; ++i) {
+                    z0[i] = z0[i] * (F8 ? xs[i] * w0 : 1.f) + b0;
+                    z1[i] = z1[i] * (F8 ? xs[i] * w1 : 1.f) + b1;
                 }
-                float v = apply_act(z0 + b0, a.act);
-                if (a.gated) v *= z1 + b1;
-                if (a.res) v += load_elem(a.res, (t0 + t) * a.ldr + f, p.ydt);
-                store_elem(a.y, (t0 + t) * a.ldy + f, v, p.ydt);
+                apply_act<TB>(z0, a.act);
+#pragma unroll
+                for (int i = 0; i < TB; ++i) {
+                    const int t = t1 + i * step;
+                    if (t < tb) store_elem(a.y, (t0 + t) * a.ldy + f, (a.gated ? z0[i] * z1[i] : z0[i]) + add[i], p.ydt);
+                }
             }
         }
     }
@@ -266,6 +281,35 @@ constexpr int MANY_STAGES = 6;
 constexpr uint32_t MANY_TURN = 32 * 32 * 4;      // staging of one epilogue warp
 constexpr int MANY_GROUP = 8;                    // token tiles that walk the features together (their lines stay in L2)
 __host__ __device__ constexpr uint32_t many_stage(int nt) { return 128 * LT_LINE + (uint32_t)(nt / 2) * LT_LINE; }
+
+// One warp's 32 tokens x 32 values -> y, with the residual: four lanes hold a token's 32 values, eight each.
+template <typename T>
+__device__ __forceinline__ void store_turned(const uint8_t *turn, const LinearArgs &a, int64_t trow, int f0, int lane)
+{
+    const int sg = lane & 3;
+    float w[4][8];
+    if (a.res) {
+#pragma unroll
+        for (int it = 0; it < 4; ++it) {
+            const int64_t t = trow + it * 8 + (lane >> 2);
+            if (t < a.T) load8(static_cast<const T *>(a.res) + t * a.ldr + f0 + 8 * sg, w[it]);
+        }
+    }
+#pragma unroll
+    for (int it = 0; it < 4; ++it) {
+        const int r = it * 8 + (lane >> 2);
+        const int64_t t = trow + r;
+        const float4 lo = *reinterpret_cast<const float4 *>(turn + r * 128 + (((2 * sg) ^ (r & 7)) << 4));
+        const float4 hi = *reinterpret_cast<const float4 *>(turn + r * 128 + (((2 * sg + 1) ^ (r & 7)) << 4));
+        float o[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+        if (t >= a.T) continue;
+        if (a.res) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) o[j] += w[it][j];
+        }
+        store8(static_cast<T *>(a.y) + t * a.ldy + f0 + 8 * sg, o);
+    }
+}
 
 // NT: features (dense rows) per tile, 128 or 256. vec: y's and the residual's rows are 16-byte aligned.
 template <bool F8, int NT>
@@ -408,37 +452,59 @@ ubp_linear_many_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t acc = tmem + (uint32_t)b * 256u + ((uint32_t)(q * 32) << 16);
             bool released = false;
-            for (int c = half; c < nchunk; c += 2) {
-                const int f0 = (a.gated ? n * (NT / 2) : n * NT) + c * 32;           // first output feature of the chunk
-                float v[32];
-                // 16 accumulator columns -> scaled and biased; `row` = weight row of the first
-                auto scaled16 = [&](uint32_t col, int row, float (&z)[16]) {
-                    uint32_t r[16];
-                    tmem_ld16(acc + col, r);
-                    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-                    const int hi = a.M - 1;
+            // 16 accumulator columns -> scaled and biased; `row` = weight row of the first
+            auto scaled16 = [&](const uint32_t (&r)[16], int row, float (&z)[16]) {
+#pragma unroll
+                for (int j = 0; j < 16; ++j) z[j] = __uint_as_float(r[j]);
+                if (row + 16 <= a.M && ((row | p.unaligned_bias) & 3) == 0) {
+#pragma unroll
+                    for (int j = 0; j < 16; j += 4) {
+                        if (F8) {
+                            const float4 s4 = __ldg(reinterpret_cast<const float4 *>(p.wscale + row + j));
+                            z[j] *= xs * s4.x; z[j + 1] *= xs * s4.y; z[j + 2] *= xs * s4.z; z[j + 3] *= xs * s4.w;
+                        }
+                        if (a.bias) {
+                            const float4 b4 = __ldg(reinterpret_cast<const float4 *>(a.bias + row + j));
+                            z[j] += b4.x; z[j + 1] += b4.y; z[j + 2] += b4.z; z[j + 3] += b4.w;
+                        }
+                    }
+                } else if (F8 || a.bias) {
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
-                        const int o = row + j < hi ? row + j : hi;                   // (rows past the layer are not stored)
-                        z[j] = __uint_as_float(r[j]);
+                        const int o = row + j < a.M ? row + j : a.M - 1;                 // (rows past the layer are not stored)
                         if (F8) z[j] *= xs * __ldg(p.wscale + o);
                         if (a.bias) z[j] += __ldg(a.bias + o);
                     }
-                };
-#pragma unroll
+                }
+            };
+#pragma unroll 1
+            for (int c = half; c < nchunk; c += 2) {
+                const int f0 = (a.gated ? n * (NT / 2) : n * NT) + c * 32;           // first output feature of the chunk
+#pragma unroll 1
                 for (int h = 0; h < 2; ++h) {
                     float z[16];
+                    uint32_t r[16];
                     if (a.gated) {
                         float u[16];
-                        scaled16((uint32_t)(c * 64 + h * 32), f0 + h * 16, z);
-                        scaled16((uint32_t)(c * 64 + h * 32 + 16), a.F + f0 + h * 16, u);
+                        uint32_t r2[16];
+                        tmem_ld16(acc + (uint32_t)(c * 64 + h * 32), r);
+                        tmem_ld16(acc + (uint32_t)(c * 64 + h * 32 + 16), r2);
+                        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                        scaled16(r, f0 + h * 16, z);
+                        scaled16(r2, a.F + f0 + h * 16, u);
+                        apply_act<16>(z, a.act);
 #pragma unroll
-                        for (int j = 0; j < 16; ++j) v[h * 16 + j] = apply_act(z[j], a.act) * u[j];
+                        for (int j = 0; j < 16; ++j) z[j] *= u[j];
                     } else {
-                        scaled16((uint32_t)(c * 32 + h * 16), f0 + h * 16, z);
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) v[h * 16 + j] = apply_act(z[j], a.act);
+                        tmem_ld16(acc + (uint32_t)(c * 32 + h * 16), r);
+                        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+                        scaled16(r, f0 + h * 16, z);
+                        apply_act<16>(z, a.act);
                     }
+                    // turn: lane = token row writes its 16 values, 16-byte pieces XORed with the row
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        *reinterpret_cast<float4 *>(turn + lane * 128 + (((4 * h + j) ^ (lane & 7)) << 4)) = make_float4(z[4 * j], z[4 * j + 1], z[4 * j + 2], z[4 * j + 3]);
                 }
                 if (c + 2 >= nchunk) {                           // last read of this accumulator by this warp
                     released = true;
@@ -448,46 +514,17 @@ ubp_linear_many_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
                         else mbar_arrive_remote(smem_u32(&bar_acc_empty[b]), 0);
                     }
                 }
-                if (f0 >= a.F) continue;
-                // turn: lane = token row writes its 32 values, 16-byte pieces XORed with the row
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    *reinterpret_cast<float4 *>(turn + lane * 128 + ((j ^ (lane & 7)) << 4)) = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
                 __syncwarp();
                 if (vec && f0 + 32 <= a.F) {
-#pragma unroll
-                    for (int it = 0; it < 4; ++it) {
-                        const int r = it * 8 + (lane >> 2), sg = lane & 3;
-                        const int64_t t = trow + r;
-                        float o[8], w[8];
-                        const float4 lo = *reinterpret_cast<const float4 *>(turn + r * 128 + (((2 * sg) ^ (r & 7)) << 4));
-                        const float4 hi = *reinterpret_cast<const float4 *>(turn + r * 128 + (((2 * sg + 1) ^ (r & 7)) << 4));
-                        o[0] = lo.x; o[1] = lo.y; o[2] = lo.z; o[3] = lo.w; o[4] = hi.x; o[5] = hi.y; o[6] = hi.z; o[7] = hi.w;
-                        if (t >= a.T) continue;
-                        const int64_t at = t * a.ldy + f0 + 8 * sg, rt = t * a.ldr + f0 + 8 * sg;
-                        if (p.ydt == UBP_BF16) {
-                            if (a.res) { load8(static_cast<const __nv_bfloat16 *>(a.res) + rt, w);
-#pragma unroll
-                                for (int j = 0; j < 8; ++j) o[j] += w[j]; }
-                            store8(static_cast<__nv_bfloat16 *>(a.y) + at, o);
-                        } else if (p.ydt == UBP_F16) {
-                            if (a.res) { load8(static_cast<const __half *>(a.res) + rt, w);
-#pragma unroll
-                                for (int j = 0; j < 8; ++j) o[j] += w[j]; }
-                            store8(static_cast<__half *>(a.y) + at, o);
-                        } else {
-                            if (a.res) { load8(static_cast<const float *>(a.res) + rt, w);
-#pragma unroll
-                                for (int j = 0; j < 8; ++j) o[j] += w[j]; }
-                            store8(static_cast<float *>(a.y) + at, o);
-                        }
-                    }
-                } else {                                         // unaligned rows or the layer's last features: one token a step
+                    if (p.ydt == UBP_BF16) store_turned<__nv_bfloat16>(turn, a, trow, f0, lane);
+                    else if (p.ydt == UBP_F16) store_turned<__half>(turn, a, trow, f0, lane);
+                    else store_turned<float>(turn, a, trow, f0, lane);
+                } else if (f0 + lane < a.F) {                    // unaligned rows or the layer's last features: one token a step
                     const int f = f0 + lane;
+#pragma unroll 8
                     for (int r = 0; r < 32; ++r) {
                         const int64_t t = trow + r;
-                        if (t >= a.T) break;
-                        if (f < a.F) {
+                        if (t < a.T) {
                             float o = *reinterpret_cast<const float *>(turn + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4);
                             if (a.res) o += load_elem(a.res, t * a.ldr + f, p.ydt);
                             store_elem(a.y, t * a.ldy + f, o, p.ydt);
@@ -671,6 +708,7 @@ int launch_linear_tc(const ubp_linear_plan *pl, const LinearArgs &args, int y_dt
     p.wscale = reinterpret_cast<const float *>(pl->dev + pl->img.scale_off);
     p.ydt = y_dtype;
     p.nk = pl->img.Kp * b / LT_LINE;
+    p.unaligned_bias = (reinterpret_cast<uintptr_t>(args.bias) & 15) != 0;
     p.rows = pl->gated ? (pl->F + 15) / 16 * 32 : pl->M;
     if (args.T > 0x7fffffff) return UBP_E_UNSUPPORTED;
     const void *x = args.x;
