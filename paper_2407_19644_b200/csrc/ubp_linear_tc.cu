@@ -34,7 +34,10 @@ using namespace tc;
 constexpr uint32_t LT_SWZ_128B = 2;
 constexpr int LT_LINE = 128;                    // bytes of a row in one chunk
 constexpr int LT_EPI_WARPS = 8;                 // warps 2..9
-constexpr int LT_THREADS = (2 + LT_EPI_WARPS) * 32;
+// Copies are issued by two threads, lane 0 of warp 0 (weights, and the announcement of a stage's bytes) and of the last warp
+// (activations): an issue holds its thread for more than a hundred cycles, and with one thread that is what a chunk waits for.
+constexpr int LT_X_WARP = 2 + LT_EPI_WARPS;
+constexpr int LT_THREADS = (3 + LT_EPI_WARPS) * 32;
 constexpr int LT_MAX_STAGES = 12;
 
 struct TcLinArgs {
@@ -43,6 +46,7 @@ struct TcLinArgs {
     int ydt;
     int nk;              // chunks of the reduction
     int rows;            // dense rows that hold the layer (M, or 2 x F rounded up to 16)
+    int vec4;            // rows of y and of the residual are aligned to four elements
     int unaligned_bias;  // 1: bias is not 16-byte aligned
 };
 
@@ -92,13 +96,43 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16])
           "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(taddr) : "memory");
 }
-__device__ __forceinline__ float ld_rank(const float *p, uint32_t rank)
+// 16 bytes at this place in the shared memory of another block of the cluster
+__device__ __forceinline__ float4 ld_rank4(const float *p, uint32_t rank)
 {
     uint32_t a;
-    float v;
+    float4 v;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(a) : "memory");
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(a) : "memory");
     return v;
+}
+__device__ __forceinline__ void add4(float (&z)[4], const float4 &v) { z[0] += v.x; z[1] += v.y; z[2] += v.z; z[3] += v.w; }
+// four elements of a row, of which the first n exist; whole accesses where the row is aligned to them
+template <typename T> __device__ __forceinline__ void load4(const T *p, int n, bool vec, float (&v)[4])
+{
+    if (vec) {
+        if constexpr (sizeof(T) == 4) {
+            const float4 q = *reinterpret_cast<const float4 *>(p);
+            v[0] = q.x; v[1] = q.y; v[2] = q.z; v[3] = q.w;
+        } else {
+            const uint2 q = *reinterpret_cast<const uint2 *>(p);
+            const float2 a = unpack2<T>(q.x), b = unpack2<T>(q.y);
+            v[0] = a.x; v[1] = a.y; v[2] = b.x; v[3] = b.y;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = j < n ? to_f32<T>(p[j]) : 0.f;
+    }
+}
+template <typename T> __device__ __forceinline__ void store4(T *p, int n, bool vec, const float (&v)[4])
+{
+    if (vec) {
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
+        else *reinterpret_cast<uint2 *>(p) = make_uint2(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j < n) p[j] = from_f32<T>(v[j]);
+    }
 }
 
 // ------------------------------------------------------------------ few tokens
@@ -110,6 +144,53 @@ __host__ __device__ constexpr int few_stages(int nt)
 {
     const int s = (int)(FEW_BUDGET / few_stage(nt));
     return s > LT_MAX_STAGES ? LT_MAX_STAGES : s;
+}
+
+// Tokens ta .. tb of a tile: the cluster's partial sums red[token][128], in the ranks' order, to y.
+template <bool F8, typename T>
+__device__ __forceinline__ void few_epilogue(const TcLinArgs &p, const float *red, int rt, int64_t t0, int ta, int tb, int S)
+{
+    const LinearArgs &a = p.a;
+    const int per = a.gated ? 16 : 32;                          // threads of a token
+    const int o = ((int)threadIdx.x & (per - 1)) * 4, f = rt * (per * 4) + o, dl = a.gated ? (o >> 4) * 32 + (o & 15) : o;
+    const int n = a.F - f;
+    if (n <= 0) return;
+    float w0[4], w1[4], b0[4], b1[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int r = j < n ? f + j : f, u = a.gated ? a.F + r : r;
+        w0[j] = F8 ? __ldg(p.wscale + r) : 1.f;
+        w1[j] = F8 ? __ldg(p.wscale + u) : 1.f;
+        b0[j] = a.bias ? __ldg(a.bias + r) : 0.f;
+        b1[j] = a.bias ? __ldg(a.bias + u) : 0.f;
+    }
+    const bool vec = p.vec4 && n >= 4;
+    const int step = LT_THREADS / per;
+#pragma unroll 2
+    for (int t = ta + (int)threadIdx.x / per; t < tb; t += step) {
+        float z[4] = {0.f, 0.f, 0.f, 0.f}, u[4] = {0.f, 0.f, 0.f, 0.f}, r[4] = {0.f, 0.f, 0.f, 0.f};
+        const float *src = red + t * 128 + dl;
+        if (a.res) load4(static_cast<const T *>(a.res) + (t0 + t) * a.ldr + f, n, vec, r);
+        const float xs = F8 ? a.xs[t0 + t] : 1.f;
+        if (S > 1) {
+            for (int k = 0; k < S; ++k) {
+                add4(z, ld_rank4(src, (uint32_t)k));
+                if (a.gated) add4(u, ld_rank4(src + 16, (uint32_t)k));
+            }
+        } else {
+            add4(z, *reinterpret_cast<const float4 *>(src));
+            if (a.gated) add4(u, *reinterpret_cast<const float4 *>(src + 16));
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            z[j] = (F8 ? z[j] * (xs * w0[j]) : z[j]) + b0[j];
+            u[j] = (F8 ? u[j] * (xs * w1[j]) : u[j]) + b1[j];
+        }
+        apply_act<4>(z, a.act);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) z[j] = (a.gated ? z[j] * u[j] : z[j]) + r[j];
+        store4(static_cast<T *>(a.y) + (t0 + t) * a.ldy + f, n, vec, z);
+    }
 }
 
 // grid: (row tile, token tile, rank) with the rank fastest; clusters of S blocks. NT: tokens per tile (multiple of 16).
@@ -158,7 +239,7 @@ ubp_linear_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
     const uint32_t tmem = tmem_base_slot;
     bool ok = true;
 
-    if (warp == 0) {
+    if (warp == 0 || warp == LT_X_WARP) {
         if (lane == 0) {
             auto issue_w = [&](int i) {
                 const int st = i % stages;
@@ -174,15 +255,16 @@ ubp_linear_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
                                 (k0 + i * KCH + u) * line, (int)t0, bar);
             };
             // the ring's first weight lines are constants of the layer: under way before the wait for the earlier kernel
-            const int pre = nst < stages ? nst : stages;
+            // (the activations' bytes may land before the stage's bytes are announced: its phase cannot end before)
+            const bool w = warp == 0;
+            const int pre = w ? (nst < stages ? nst : stages) : 0;
             for (int i = 0; i < pre; ++i) issue_w(i);
             asm volatile("griddepcontrol.wait;" ::: "memory");
-            for (int i = 0; i < pre; ++i) issue_x(i);
             for (int i = pre; i < nst && ok; ++i) {
-                ok = mbar_wait(smem_u32(&bar_empty[i % stages]), (uint32_t)(i / stages - 1) & 1u, &abort_flag);
+                if (i >= stages) ok = mbar_wait(smem_u32(&bar_empty[i % stages]), (uint32_t)(i / stages - 1) & 1u, &abort_flag);
                 if (!ok) break;
-                issue_w(i);
-                issue_x(i);
+                if (w) issue_w(i);
+                else issue_x(i);
             }
         }
     } else if (warp == 1) {
@@ -202,9 +284,9 @@ ubp_linear_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
         }
         if (ok) commit_one(smem_u32(&bar_acc));
     }
-    if (threadIdx.x != 0) asm volatile("griddepcontrol.wait;" ::: "memory");
+    if (!(lane == 0 && (warp == 0 || warp == LT_X_WARP))) asm volatile("griddepcontrol.wait;" ::: "memory");
     float *red = reinterpret_cast<float *>(smem);              // [NT][128] partial sums, over the (finished) ring
-    if (warp >= 2) {
+    if (warp >= 2 && warp < LT_X_WARP) {
         ok = mbar_wait_relaxed(smem_u32(&bar_acc), 0, &abort_flag);
         if (ok) {
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
@@ -222,51 +304,12 @@ ubp_linear_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     if (S > 1) cluster_sync();
     else __syncthreads();
-    // ---- epilogue of this rank's share of the tokens; neighbouring threads hold neighbouring features
+    // ---- epilogue of this rank's share of the tokens: four features a thread, a token's 128 (gated: 64) a warp (half a warp)
     {
-        const int nout = a.gated ? 64 : 128;
         const int ta = (int)((int64_t)nt * rank / S), tb = (int)((int64_t)nt * (rank + 1) / S);
-        const int o = (int)threadIdx.x % nout;
-        const int dl = a.gated ? (o >> 4) * 32 + (o & 15) : o, f = rt * nout + o;
-        if (threadIdx.x < 256 && f < a.F) {
-            const int up = a.F + f;
-            const float b0 = a.bias ? a.bias[f] : 0.f, b1 = (a.gated && a.bias) ? a.bias[up] : 0.f;
-            const float w0 = F8 ? p.wscale[f] : 1.f, w1 = (F8 && a.gated) ? p.wscale[up] : 1.f;
-            // four tokens at a time: their loads and arithmetic overlap (one at a time was 0.1 us a token)
-            constexpr int TB = 4;
-            const int step = 256 / nout;
-            for (int t1 = ta + (int)threadIdx.x / nout; t1 < tb; t1 += TB * step) {
-                float z0[TB], z1[TB], add[TB], xs[TB];
-#pragma unroll
-                for (int i = 0; i < TB; ++i) {
-                    const int t = t1 + i * step;
-                    z0[i] = z1[i] = add[i] = 0.f;
-                    xs[i] = 1.f;
-                    if (t < tb) {
-                        if (a.res) add[i] = load_elem(a.res, (t0 + t) * a.ldr + f, p.ydt);
-                        if (F8) xs[i] = a.xs[t0 + t];
-                    }
-                }
-                for (int k = 0; k < S; ++k)
-#pragma unroll
-                    for (int i = 0; i < TB; ++i) {
-                        const float *src = red + (size_t)(t1 + i * step < tb ? t1 + i * step : t1) * 128 + dl;
-                        z0[i] += S > 1 ? ld_rank(src, (uint32_t)k) : *src;
-                        if (a.gated) z1[i] += S > 1 ? ld_rank(src + 16, (uint32_t)k) : src[16];
-                    }
-#pragma unroll
-                for (int i = 0; i < TB; ++i) {
-                    z0[i] = z0[i] * (F8 ? xs[i] * w0 : 1.f) + b0;
-                    z1[i] = z1[i] * (F8 ? xs[i] * w1 : 1.f) + b1;
-                }
-                apply_act<TB>(z0, a.act);
-#pragma unroll
-                for (int i = 0; i < TB; ++i) {
-                    const int t = t1 + i * step;
-                    if (t < tb) store_elem(a.y, (t0 + t) * a.ldy + f, (a.gated ? z0[i] * z1[i] : z0[i]) + add[i], p.ydt);
-                }
-            }
-        }
+        if (p.ydt == UBP_BF16) few_epilogue<F8, __nv_bfloat16>(p, red, rt, t0, ta, tb, S);
+        else if (p.ydt == UBP_F16) few_epilogue<F8, __half>(p, red, rt, t0, ta, tb, S);
+        else few_epilogue<F8, float>(p, red, rt, t0, ta, tb, S);
     }
     if (S > 1) cluster_sync();                                  // nobody leaves while its partial sums are being read
     else __syncthreads();
@@ -367,7 +410,7 @@ ubp_linear_many_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
     const uint32_t tmem = tmem_base_slot;
     bool ok = true;
 
-    if (warp == 0) {
+    if (warp == 0 || warp == LT_X_WARP) {
         if (lane == 0) {
             auto issue_w = [&](int st, int n, int k) {
                 const uint32_t bar = smem_u32(&bar_full[st]);
@@ -378,11 +421,11 @@ ubp_linear_many_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
                 tma_load_2d(smem_u32(smem + (size_t)st * STAGE), &tmX, k * line, m * 256 + (int)rank * 128, smem_u32(&bar_full[st]));
             };
             int m = 0, n = 0, f = 0;
-            const int pre = nmy > 0 ? (p.nk < S ? p.nk : S) : 0;       // first tile: the ring's weight lines before the wait
+            const bool w = warp == 0;
+            const int pre = w && nmy > 0 ? (p.nk < S ? p.nk : S) : 0;  // first tile: the ring's weight lines before the wait
             if (nmy > 0) tile_at(0, m, n);
             for (int k = 0; k < pre; ++k) issue_w(k, n, k);
             asm volatile("griddepcontrol.wait;" ::: "memory");
-            for (int k = 0; k < pre; ++k) issue_x(k, m, k);
             int st = 0, round = 0;
             for (int i = 0; i < nmy && ok; ++i) {
                 tile_at(i, m, n);
@@ -392,8 +435,8 @@ ubp_linear_many_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
                             ok = mbar_wait(smem_u32(&bar_empty[st]), (uint32_t)(round - 1) & 1u, &abort_flag);
                             if (!ok) break;
                         }
-                        issue_w(st, n, k);
-                        issue_x(st, m, k);
+                        if (w) issue_w(st, n, k);
+                        else issue_x(st, m, k);
                     }
                     if (++st == S) { st = 0; ++round; }
                 }
@@ -711,6 +754,9 @@ int launch_linear_tc(const ubp_linear_plan *pl, const LinearArgs &args, int y_dt
     p.unaligned_bias = (reinterpret_cast<uintptr_t>(args.bias) & 15) != 0;
     p.rows = pl->gated ? (pl->F + 15) / 16 * 32 : pl->M;
     if (args.T > 0x7fffffff) return UBP_E_UNSUPPORTED;
+    const uintptr_t ob = (uintptr_t)(y_dtype == UBP_F32 ? 4 : 2);
+    auto rows_on = [&](const void *q, int64_t ld, uintptr_t n) { return (reinterpret_cast<uintptr_t>(q) & (n - 1)) == 0 && (args.T <= 1 || ((uint64_t)ld * ob) % n == 0); };
+    p.vec4 = rows_on(args.y, args.ldy, 4 * ob) && (!args.res || rows_on(args.res, args.ldr, 4 * ob));
     const void *x = args.x;
     int64_t ldx = args.ldx;
     int C = pl->C;
@@ -740,9 +786,7 @@ int launch_linear_tc(const ubp_linear_plan *pl, const LinearArgs &args, int y_dt
     }
     if (int rc = encode_w(&tmW, pl, ch.cols / 2, 1)) return rc;
     if (int rc = encode_x(&tmX, x, pl->dtype, ldx, args.T, C, 128)) return rc;
-    const uintptr_t ob = (uintptr_t)(y_dtype == UBP_F32 ? 4 : 2);
-    auto al = [&](const void *q, int64_t ld) { return (reinterpret_cast<uintptr_t>(q) & 15) == 0 && (args.T <= 1 || ((uint64_t)ld * ob) % 16 == 0); };
-    const int vec = al(args.y, args.ldy) && (!args.res || al(args.res, args.ldr));
+    const int vec = rows_on(args.y, args.ldy, 16) && (!args.res || rows_on(args.res, args.ldr, 16));
     if (ch.cols == 128) return f8 ? launch_many<true, 128>(tmW, tmX, p, fmt, sms, vec, st) : launch_many<false, 128>(tmW, tmX, p, fmt, sms, vec, st);
     return f8 ? launch_many<true, 256>(tmW, tmX, p, fmt, sms, vec, st) : launch_many<false, 256>(tmW, tmX, p, fmt, sms, vec, st);
 }
