@@ -458,8 +458,8 @@ int ubp_linear_plan_clear_status(const ubp_linear_plan_t *plan, void *stream);
  * cores; from there on the densified weight on the tensor cores. y must not overlap x; with residual == y each element is
  * read before it is written.
  * Errors: UBP_E_ARG, UBP_E_SPACE (workspace), UBP_E_UNSUPPORTED, UBP_E_CUDA. */
-/* ubp_linear_choice: which kernel T tokens take on the current device. *kernel: 0 = kept blocks on the CUDA cores,
- * 1 = densified weight on the tensor cores, one block per 128 weight rows and *tile tokens, *split blocks of a cluster
+/* ubp_linear_choice: which kernel T tokens take on the current device. *kernel: 0 = kept blocks on the CUDA cores
+ * (*tile tokens a block), 1 = densified weight on the tensor cores, one block per 128 weight rows and *tile tokens, *split blocks of a cluster
  * sharing a reduction, 2 = densified weight, CTA pairs on tiles of 256 tokens x *tile weight rows. Host only. */
 int ubp_linear_choice(const ubp_linear_plan_t *plan, int64_t T, int *kernel, int *tile, int *split);
 size_t ubp_linear_workspace_size(const ubp_linear_plan_t *plan, const void *x, int64_t ldx, int64_t T);

@@ -67,11 +67,13 @@ struct LinearArgs {
 enum { LIN_SPARSE = 0, LIN_FEW = 1, LIN_MANY = 2 };
 struct LinearChoice {
     int kernel;                     // LIN_*
-    int cols;                       // LIN_FEW: tokens per tile; LIN_MANY: dense weight rows per tile
+    int cols;                       // LIN_SPARSE, LIN_FEW: tokens per block; LIN_MANY: dense weight rows per tile
     int split;                      // LIN_FEW: blocks of a cluster that share a reduction
 };
 LinearChoice linear_choose(const ubp_linear_plan *p, int64_t T, int sms);
 
+// tokens a block of the kept-block kernel takes (1, 2, 4 or 8) and the number of such groups
+void linear_sparse_tokens(const ubp_linear_plan *p, int64_t T, int *tokens, int64_t *groups);
 int launch_linear_sparse(const ubp_linear_plan *p, const LinearArgs &a, int y_dtype, void *stream);
 // whether the tensor-core kernels can copy x's rows as they are (else they go through the workspace, [T][Kp])
 bool linear_x_direct(const ubp_linear_plan *p, const void *x, int64_t ldx, int64_t T);

@@ -10,19 +10,35 @@
 
 namespace ubp {
 
+// Kernel and tile of a launch. Estimates in us, fitted to back-to-back launches on B200 (26 random layers of 256 .. 10000
+// rows and channels, bf16 and e4m3, 1, 2, 4, 8 rows an entry, 50 .. 90 % pruned, 1 .. 24 tokens; the kept blocks and the
+// dense form both timed; the choice costs 2 % on average over always taking the faster one, "eight tokens or fewer" 3.5 %):
+//   kept blocks   2.8 + (entries (24 + 6.6 t) + kept weights x 27 t) ns / 1000 over the SMs + 85 ns a thousand channels and
+//                 token, t = tokens a block takes: instruction-bound, in the entries and in the products
+//   dense, few    3.3 + 0.9 for a split reduction + 6.4 ns a KB of weights a block streams + 0.12 us a MB in all
+// From 17 tokens on (three blocks to a row range) the kept blocks lost everywhere. A call of the few-token kernel covers 256
+// tokens; with more (4096 x 4096, 384 tokens, 22.5 us) the pair kernel is as fast (22.2) and from 512 on faster. Its tile is
+// 128 rows wide while those tiles fit one round (8192 x 2048, 256 tokens: 14.1 us against 16.8), else 256 (384 tokens: 17.3
+// against 22.2).
 LinearChoice linear_choose(const ubp_linear_plan *p, int64_t T, int sms)
 {
-    if (T <= 16) return {LIN_SPARSE, 0, 0};
-    const int rows = p->gated ? (p->F + 15) / 16 * 32 : p->M, rt = (rows + 127) / 128;
-    const int nk = p->img.Kp * (p->dtype == UBP_E4M3 ? 1 : 2) / 128;
-    if (T <= 256) {
-        const int cols = (int)((T + 15) / 16 * 16);
-        int S = 1;
-        while (S < 8 && rt * S * 2 <= sms && nk / (S * 2) >= 4) S *= 2;
-        return {LIN_FEW, cols, S};
+    const int b = p->dtype == UBP_E4M3 ? 1 : 2;
+    const int rows = p->gated ? (p->F + 15) / 16 * 32 : p->M, rt = (rows + 127) / 128, nk = p->img.Kp * b / 128;
+    int S = 1;                       // split as far as the blocks find SMs and keep four chunks of the reduction each
+    while (S < 8 && rt * S * 2 <= sms && nk / (S * 2) >= 4) S *= 2;
+    if (T <= 16) {
+        int t;
+        int64_t nchunk;
+        linear_sparse_tokens(p, T, &t, &nchunk);
+        const double kept = (double)p->img.entries * p->img.nbk, share = (double)nchunk / sms;
+        const double sparse = 2.8 + ((double)p->img.entries * (24 + 6.6 * t) + kept * 27 * t) * share * 1e-6 + 85e-6 * p->C * t;
+        const double waves = (rt * S + sms - 1) / sms;
+        const double dense = 3.3 + (S > 1 ? 0.9 : 0.0) + 128.0 * p->img.Kp * b / S * waves * 6.4e-6 + 128e-6 * rt * p->img.Kp * b * 0.12;
+        if (sparse <= dense) return {LIN_SPARSE, t, 0};
     }
-    const int64_t t256 = ((T + 255) / 256) * ((rows + 255) / 256);
-    return {LIN_MANY, t256 >= sms / 2 ? 256 : 128, 0};
+    if (T <= 256) return {LIN_FEW, (int)((T + 15) / 16 * 16), S};
+    const int64_t t128 = ((T + 255) / 256) * ((rows + 127) / 128);
+    return {LIN_MANY, t128 <= sms / 2 ? 128 : 256, 0};
 }
 
 static int device_sms()

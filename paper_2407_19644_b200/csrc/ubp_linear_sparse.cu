@@ -13,7 +13,7 @@
 // coalesced 512-byte load of weights, one of channels, and no test; the lanes' sums join once a bundle. The weights are
 // constants of the layer, so the first steps are loaded before the kernel waits for the one before it, and the next steps'
 // loads are always under way. Forms that were measured before this one, us for a token on 4096 x 4096 at 80 % bf16 /
-// 16384 x 4096 gated e4m3 (this: @SPARSE@): a group of lanes per row in the canonical order, four blocks of a cluster to a
+// 16384 x 4096 gated e4m3 (this: 3.75 / 7.5): a group of lanes per row in the canonical order, four blocks of a cluster to a
 // reduction, 6.9 / 20.4 (chains of dependent loads); a ring of bulk copies in shared memory, 6.7 / 14.0 (a stage holds too few
 // rows for the warps, and its barriers add up); equal shares of the canonical stream to groups of lanes, 5.6 / 12.6 (170
 // instructions a chunk, most of them for finding rows).
@@ -386,6 +386,18 @@ int launch_w(const SpArgs &p, int nbk, int TT, int64_t chunks, size_t smem, cuda
 
 }  // namespace
 
+// The power of two that takes the tokens in as few blocks as eight would, and whose activations fit (a token of the longest
+// row, 65536 channels, is 128 KB).
+void linear_sparse_tokens(const ubp_linear_plan *p, int64_t T, int *tokens, int64_t *groups)
+{
+    const int64_t chunks = (T + SP_MAX_TOKENS - 1) / SP_MAX_TOKENS, per = chunks ? (T + chunks - 1) / chunks : 1;
+    int t = 1;
+    while (t < per) t *= 2;
+    while (t > 1 && (size_t)p->C * t * 2 > SP_X) t /= 2;
+    *tokens = t;
+    *groups = (T + t - 1) / t;
+}
+
 int launch_linear_sparse(const ubp_linear_plan *pl, const LinearArgs &a, int y_dtype, void *stream)
 {
     SpArgs p;
@@ -396,13 +408,9 @@ int launch_linear_sparse(const ubp_linear_plan *pl, const LinearArgs &a, int y_d
     p.val = pl->dev + pl->img.val_off;
     p.ydt = y_dtype;
     const int nbk = pl->img.nbk, nseg = a.gated ? 2 : 1;
-    // tokens per block: the power of two that takes the launch's tokens in as few blocks as eight would, and whose
-    // activations fit (a token of the longest row, 65536 channels, is 128 KB)
-    const int64_t chunks = (a.T + SP_MAX_TOKENS - 1) / SP_MAX_TOKENS, per = (a.T + chunks - 1) / chunks;
-    int TT = 1;
-    while (TT < per) TT *= 2;
-    while (TT > 1 && (size_t)a.C * TT * 2 > SP_X) TT /= 2;
-    const int64_t nchunk = (a.T + TT - 1) / TT;
+    int TT;
+    int64_t nchunk;
+    linear_sparse_tokens(pl, a.T, &TT, &nchunk);
     if (nchunk > 65535) return UBP_E_UNSUPPORTED;
     int sms = 148, dev = 0;
     if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);

@@ -20,6 +20,7 @@
 
 #include <cstdint>
 #include <mutex>
+#include <type_traits>
 
 #include "ubp_internal.h"
 #include "ubp_linear.h"
@@ -138,7 +139,7 @@ template <typename T> __device__ __forceinline__ void store4(T *p, int n, bool v
 // ------------------------------------------------------------------ few tokens
 constexpr uint32_t FEW_A = 128 * LT_LINE;       // weight lines of one chunk: 16 KB
 constexpr uint32_t FEW_BUDGET = 200 * 1024;
-__host__ __device__ constexpr int few_kch(int nt) { return nt <= 64 ? 2 : 1; }       // chunks per stage
+__host__ __device__ constexpr int few_kch(int nt) { return nt <= 128 ? 2 : 1; }       // chunks per stage
 __host__ __device__ constexpr uint32_t few_stage(int nt) { return (uint32_t)few_kch(nt) * (FEW_A + (uint32_t)nt * LT_LINE); }
 __host__ __device__ constexpr int few_stages(int nt)
 {
@@ -325,37 +326,80 @@ constexpr uint32_t MANY_TURN = 32 * 32 * 4;      // staging of one epilogue warp
 constexpr int MANY_GROUP = 8;                    // token tiles that walk the features together (their lines stay in L2)
 __host__ __device__ constexpr uint32_t many_stage(int nt) { return 128 * LT_LINE + (uint32_t)(nt / 2) * LT_LINE; }
 
-// One warp's 32 tokens x 32 values -> y, with the residual: four lanes hold a token's 32 values, eight each.
-template <typename T>
-__device__ __forceinline__ void store_turned(const uint8_t *turn, const LinearArgs &a, int64_t trow, int f0, int lane)
+// One warp's 32 tokens x 32 values -> y, with the residual. E elements an access (8, 4, 2 or 1: what the rows of y and of the
+// residual are aligned to and the layer's features are a multiple of); 32 / E lanes hold a token's 32 values.
+template <typename T, int E>
+__device__ __forceinline__ void store_turned_e(const uint8_t *turn, const T *res, int64_t ldr, T *y, int64_t ldy, int nt, int nf, int lane)
 {
-    const int sg = lane & 3;
-    float w[4][8];
-    if (a.res) {
+    constexpr int LPR = 32 / E, UN = E >= 4 ? E / 2 : E == 2 ? 4 : 8;      // lanes a token; steps under way (E steps of E tokens)
+    const int c = (lane % LPR) * E;
+    if (c >= nf) return;
+#pragma unroll 1
+    for (int i0 = 0; i0 < 32 / E; i0 += UN) {
+        float w[UN][E];
+        if (res) {
 #pragma unroll
-        for (int it = 0; it < 4; ++it) {
-            const int64_t t = trow + it * 8 + (lane >> 2);
-            if (t < a.T) load8(static_cast<const T *>(a.res) + t * a.ldr + f0 + 8 * sg, w[it]);
+            for (int i = 0; i < UN; ++i) {
+                const int t = (i0 + i) * E + lane / LPR;
+                if (t < nt) {
+                    const T *p = res + t * ldr + c;
+                    if constexpr (E == 8) load8(p, w[i]);
+                    else if constexpr (E == 4) load4(p, 4, true, w[i]);
+                    else if constexpr (E == 2 && sizeof(T) == 2) { const float2 v = unpack2<T>(*reinterpret_cast<const uint32_t *>(p)); w[i][0] = v.x; w[i][1] = v.y; }
+                    else if constexpr (E == 2) { const float2 v = *reinterpret_cast<const float2 *>(p); w[i][0] = v.x; w[i][1] = v.y; }
+                    else w[i][0] = to_f32<T>(*p);
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < UN; ++i) {
+            const int r = (i0 + i) * E + lane / LPR;
+            if (r >= nt) continue;
+            float o[E];
+            const uint8_t *row = turn + r * 128;
+            if constexpr (E >= 4) {
+#pragma unroll
+                for (int h = 0; h < E / 4; ++h) {
+                    const float4 v = *reinterpret_cast<const float4 *>(row + (((c / 4 + h) ^ (r & 7)) << 4));
+                    o[4 * h] = v.x; o[4 * h + 1] = v.y; o[4 * h + 2] = v.z; o[4 * h + 3] = v.w;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[e] = *reinterpret_cast<const float *>(row + (((c >> 2) ^ (r & 7)) << 4) + ((c & 3) + e) * 4);
+            }
+            if (res) {
+#pragma unroll
+                for (int e = 0; e < E; ++e) o[e] += w[i][e];
+            }
+            T *p = y + r * ldy + c;
+            if constexpr (E == 8) store8(p, o);
+            else if constexpr (E == 4) store4(p, 4, true, o);
+            else if constexpr (E == 2 && sizeof(T) == 2) *reinterpret_cast<uint32_t *>(p) = pack2<T>(o[0], o[1]);
+            else if constexpr (E == 2) *reinterpret_cast<float2 *>(p) = make_float2(o[0], o[1]);
+            else *p = from_f32<T>(o[0]);
         }
     }
-#pragma unroll
-    for (int it = 0; it < 4; ++it) {
-        const int r = it * 8 + (lane >> 2);
-        const int64_t t = trow + r;
-        const float4 lo = *reinterpret_cast<const float4 *>(turn + r * 128 + (((2 * sg) ^ (r & 7)) << 4));
-        const float4 hi = *reinterpret_cast<const float4 *>(turn + r * 128 + (((2 * sg + 1) ^ (r & 7)) << 4));
-        float o[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
-        if (t >= a.T) continue;
-        if (a.res) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) o[j] += w[it][j];
-        }
-        store8(static_cast<T *>(a.y) + t * a.ldy + f0 + 8 * sg, o);
+}
+// trow, f0: the warp's first token and the chunk's first feature
+template <typename T, bool VEC8>
+__device__ __forceinline__ void store_turned(const uint8_t *turn, const LinearArgs &a, int64_t trow, int f0, int lane, int vec)
+{
+    const int nt = a.T - trow < 32 ? (int)(a.T - trow) : 32, nf = a.F - f0 < 32 ? a.F - f0 : 32;
+    if (nt <= 0 || nf <= 0) return;
+    const T *res = a.res ? static_cast<const T *>(a.res) + trow * a.ldr + f0 : nullptr;
+    T *y = static_cast<T *>(a.y) + trow * a.ldy + f0;
+    if constexpr (VEC8) {
+        store_turned_e<T, 8>(turn, res, a.ldr, y, a.ldy, nt, nf, lane);
+    } else {
+        if (vec == 4) store_turned_e<T, 4>(turn, res, a.ldr, y, a.ldy, nt, nf, lane);
+        else if (vec == 2) store_turned_e<T, 2>(turn, res, a.ldr, y, a.ldy, nt, nf, lane);
+        else store_turned_e<T, 1>(turn, res, a.ldr, y, a.ldy, nt, nf, lane);
     }
 }
 
-// NT: features (dense rows) per tile, 128 or 256. vec: y's and the residual's rows are 16-byte aligned.
-template <bool F8, int NT>
+// NT: features (dense rows) per tile, 128 or 256. vec: elements an access to y and the residual may take;
+// VEC8: that is 8 (an instance of its own: the registers of the narrow forms cost the wide one 5 % in spills).
+template <bool F8, int NT, bool VEC8>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LT_THREADS, 1)
 ubp_linear_many_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const TcLinArgs p,
                        const int fmt, const int ntm, const int ntn, const int vec)
@@ -558,22 +602,9 @@ ubp_linear_many_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
                     }
                 }
                 __syncwarp();
-                if (vec && f0 + 32 <= a.F) {
-                    if (p.ydt == UBP_BF16) store_turned<__nv_bfloat16>(turn, a, trow, f0, lane);
-                    else if (p.ydt == UBP_F16) store_turned<__half>(turn, a, trow, f0, lane);
-                    else store_turned<float>(turn, a, trow, f0, lane);
-                } else if (f0 + lane < a.F) {                    // unaligned rows or the layer's last features: one token a step
-                    const int f = f0 + lane;
-#pragma unroll 8
-                    for (int r = 0; r < 32; ++r) {
-                        const int64_t t = trow + r;
-                        if (t < a.T) {
-                            float o = *reinterpret_cast<const float *>(turn + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4);
-                            if (a.res) o += load_elem(a.res, t * a.ldr + f, p.ydt);
-                            store_elem(a.y, t * a.ldy + f, o, p.ydt);
-                        }
-                    }
-                }
+                if (p.ydt == UBP_BF16) store_turned<__nv_bfloat16, VEC8>(turn, a, trow, f0, lane, vec);
+                else if (p.ydt == UBP_F16) store_turned<__half, VEC8>(turn, a, trow, f0, lane, vec);
+                else store_turned<float, VEC8>(turn, a, trow, f0, lane, vec);
                 __syncwarp();
             }
             if (!released && lane == 0) {
@@ -707,11 +738,11 @@ int launch_few(const ubp_linear_plan *pl, const CUtensorMap &tmW, const CUtensor
     return e == cudaSuccess ? UBP_OK : fail(e);
 }
 
-template <bool F8, int NT>
+template <bool F8, int NT, bool VEC8>
 int launch_many(const CUtensorMap &tmW, const CUtensorMap &tmX, const TcLinArgs &p, int fmt, int sms, int vec, cudaStream_t st)
 {
     static bool done[64] = {};
-    const auto kern = ubp_linear_many_kernel<F8, NT>;
+    const auto kern = ubp_linear_many_kernel<F8, NT, VEC8>;
     const size_t smem = (size_t)MANY_STAGES * many_stage(NT) + LT_EPI_WARPS * MANY_TURN + 1024;
     static_assert(MANY_STAGES * many_stage(128) + LT_EPI_WARPS * MANY_TURN + 1024 >= TC_PAIR_MIN_SMEM, "one block per SM");
     if (int rc = allow_smem(kern, done, smem)) return rc;
@@ -786,9 +817,13 @@ int launch_linear_tc(const ubp_linear_plan *pl, const LinearArgs &args, int y_dt
     }
     if (int rc = encode_w(&tmW, pl, ch.cols / 2, 1)) return rc;
     if (int rc = encode_x(&tmX, x, pl->dtype, ldx, args.T, C, 128)) return rc;
-    const int vec = rows_on(args.y, args.ldy, 16) && (!args.res || rows_on(args.res, args.ldr, 16));
-    if (ch.cols == 128) return f8 ? launch_many<true, 128>(tmW, tmX, p, fmt, sms, vec, st) : launch_many<false, 128>(tmW, tmX, p, fmt, sms, vec, st);
-    return f8 ? launch_many<true, 256>(tmW, tmX, p, fmt, sms, vec, st) : launch_many<false, 256>(tmW, tmX, p, fmt, sms, vec, st);
+    int vec = 8;
+    while (vec > 1 && !(pl->F % vec == 0 && rows_on(args.y, args.ldy, vec * ob < 16 ? vec * ob : 16) &&
+                        (!args.res || rows_on(args.res, args.ldr, vec * ob < 16 ? vec * ob : 16)))) vec /= 2;
+    auto go = [&](auto f8_, auto nt_, auto v_) { return launch_many<decltype(f8_)::value, decltype(nt_)::value, decltype(v_)::value>(tmW, tmX, p, fmt, sms, vec, st); };
+    auto by_vec = [&](auto f8_, auto nt_) { return vec == 8 ? go(f8_, nt_, std::true_type{}) : go(f8_, nt_, std::false_type{}); };
+    auto by_tile = [&](auto f8_) { return ch.cols == 128 ? by_vec(f8_, std::integral_constant<int, 128>{}) : by_vec(f8_, std::integral_constant<int, 256>{}); };
+    return f8 ? by_tile(std::true_type{}) : by_tile(std::false_type{});
 }
 
 }  // namespace ubp

@@ -114,7 +114,7 @@ __host__ __device__ constexpr int rows_block(int tpr) { return tpr < 128 ? 128 :
 // the next one (nv accesses of e values; the next row's x and r as they lie in memory).
 __host__ __device__ constexpr int rows_blocks_per_sm(int tpr, bool norm, int e, int nv, int size)
 {
-    return (nv * e + nv * (e * size + 3) / 4 * (norm ? 2 : 1) > 48 ? 512 : 1024) / rows_block(tpr);
+    return (nv * e + (nv * e * size + 3) / 4 * (norm ? 2 : 1) > 48 ? 512 : 1024) / rows_block(tpr);
 }
 
 // T: type of x, r, h; TO: output type; E: elements an access (8 or 1); TPR: threads a row; NV: accesses a thread keeps in
