@@ -2,7 +2,6 @@
 #include <cuda_runtime.h>
 
 #include <cstring>
-#include <new>
 
 #include "ubp_internal.h"
 #include "ubp_linear.h"
@@ -63,7 +62,7 @@ int ubp_linear_plan_size(const void *blob, size_t len, int dtype, int gated, siz
         ubp::LinearImage img;
         if (int rc = ubp::build_linear_image(v, dtype, gated != 0, true, img)) return rc;
         *dev_bytes = img.total;
-    } catch (const std::bad_alloc &) { return UBP_E_SPACE; }
+    } catch (...) { return UBP_E_SPACE; }
     return UBP_OK;
 }
 
@@ -82,7 +81,7 @@ int ubp_linear_plan_image(const void *blob, size_t len, int dtype, int gated, vo
         geom[5] = img.lanes;
         offs[0] = (int64_t)img.scale_off; offs[1] = (int64_t)img.off_off; offs[2] = (int64_t)img.idx_off;
         offs[3] = (int64_t)img.val_off; offs[4] = (int64_t)img.dense_off;
-    } catch (const std::bad_alloc &) { return UBP_E_SPACE; }
+    } catch (...) { return UBP_E_SPACE; }
     return UBP_OK;
 }
 
@@ -100,7 +99,7 @@ int ubp_linear_plan_build(const void *blob, size_t len, int dtype, int gated, vo
         if (!rc && dev_bytes < p->img.total) rc = UBP_E_SPACE;
         if (!rc) rc = ubp::build_linear_image(v, dtype, gated != 0, false, p->img);
         if (rc) { delete p; return rc; }
-    } catch (const std::bad_alloc &) { delete p; return UBP_E_SPACE; }
+    } catch (...) { delete p; return UBP_E_SPACE; }
     p->magic = ubp::kLinearMagic;
     p->M = v.M; p->C = v.C; p->Nb = v.Nb; p->m = v.m;
     p->dtype = dtype; p->gated = gated != 0;

@@ -7,6 +7,8 @@
 #include <algorithm>
 #include <cmath>
 #include <cstring>
+#include <exception>
+#include <thread>
 
 #include "ubp_linear.h"
 #include "ubp_internal.h"
@@ -29,6 +31,31 @@ inline void put_weight(uint8_t *dst, float w, float scale, int dtype)
     } else {
         *dst = __nv_cvt_float_to_fp8(w / scale, __NV_SATFINITE, __NV_E4M3);
     }
+}
+
+// fn(first, last) over [0, n) in contiguous shares, a thread each where the work is worth it (a plan of a large layer is tens
+// of millions of weights: 0.8 s on one core). An exception in a share is passed on; threads that cannot be had are done
+// without.
+template <typename Fn> void in_shares(int n, size_t work, Fn &&fn)
+{
+    unsigned most = std::thread::hardware_concurrency();
+    most = most > 16 ? 16 : most;
+    const int shares = work < (1u << 20) || most < 2 ? 1 : std::min((int)most, n);
+    std::vector<std::exception_ptr> failed((size_t)shares);
+    auto run = [&](int k) {
+        try { fn((int)((int64_t)n * k / shares), (int)((int64_t)n * (k + 1) / shares)); }
+        catch (...) { failed[(size_t)k] = std::current_exception(); }
+    };
+    std::vector<std::thread> threads;
+    threads.reserve((size_t)shares);
+    int started = 1;
+    try { for (; started < shares; ++started) threads.emplace_back(run, started); }
+    catch (...) {}
+    run(0);
+    for (int k = started; k < shares; ++k) run(k);
+    for (auto &t : threads) t.join();
+    for (auto &e : failed)
+        if (e) std::rethrow_exception(e);
 }
 
 }  // namespace
@@ -86,15 +113,16 @@ int build_linear_image(const ubp_view_t &v, int dtype, bool gated, bool count_on
     // weight of output row `row` in block blk: the rotation keeps it in slot row mod Nb
     auto weight = [&](int32_t blk, int row) { return v.values[(size_t)blk * Nb + (size_t)(row % Nb)]; };
     if (dtype == UBP_E4M3) {
-        std::fill(scale.begin(), scale.end(), 0.f);
-        for (int i = 0; i < M; ++i)
-            for (int32_t k = v.indptr[i]; k < v.indptr[i + 1]; ++k)
-                for (int t = 0; t < Nb; ++t) scale[(size_t)(i + t)] = std::max(scale[(size_t)(i + t)], std::fabs(weight(k, i + t)));
-        for (auto &s : scale) s = std::max(s / 448.f, 1.17549435e-38f);
+        in_shares(M, (size_t)v.m * Nb, [&](int r0, int r1) {
+            for (int r = r0; r < r1; ++r) scale[(size_t)r] = 0.f;
+            for (int i = std::max(0, r0 - Nb + 1); i < r1; ++i)
+                for (int32_t k = v.indptr[i]; k < v.indptr[i + 1]; ++k)
+                    for (int r = std::max(i, r0); r < std::min(i + Nb, r1); ++r) scale[(size_t)r] = std::max(scale[(size_t)r], std::fabs(weight(k, r)));
+            for (int r = r0; r < r1; ++r) scale[(size_t)r] = std::max(scale[(size_t)r] / 448.f, 1.17549435e-38f);
+        });
         std::memcpy(base + img.scale_off, scale.data(), (size_t)M * 4);
     }
     std::memcpy(base + img.off_off, off.data(), off.size() * 4);
-    std::vector<uint32_t> next((size_t)M, 0);                        // entries of each start row placed so far
     // place of entry n of start row i
     auto place = [&](int i, uint32_t n) {
         const uint32_t c = n / (uint32_t)epc, step = off[(size_t)(i / rb)] + c / (uint32_t)lanes;
@@ -102,27 +130,33 @@ int build_linear_image(const ubp_view_t &v, int dtype, bool gated, bool count_on
     };
     uint16_t *idx = reinterpret_cast<uint16_t *>(base + img.idx_off);
     uint8_t *val = base + img.val_off, *dense = base + img.dense_off;
-    for (int i = 0; i < M; ++i)
-        for (int32_t k = v.indptr[i]; k < v.indptr[i + 1]; ++k) {
-            const int j = v.indices[k];
+    // Start row i of entries: the blocks that start s * nbk rows above it, s-th part of each. Every row's entries and every
+    // weight's place in the dense matrix belong to one start row, so shares of rows do not meet.
+    in_shares(M, (size_t)img.entries * nbk, [&](int r0, int r1) {
+        for (int i = r0; i < r1; ++i) {
+            uint32_t n = 0;
+            uint16_t last = 0;
             for (int s = 0; s < sub; ++s) {
-                const size_t e = place(i + s * nbk, next[(size_t)(i + s * nbk)]++);
-                idx[e] = (uint16_t)j;
-                for (int t = 0; t < nbk; ++t) {
-                    const int row = i + s * nbk + t;
-                    uint8_t *w = val + (e * (size_t)nbk + (size_t)t) * b;
-                    put_weight(w, weight(k, row), scale[(size_t)row], dtype);
-                    const int f = row < F ? row : row - F;
-                    const size_t d = !gated ? (size_t)row : (size_t)(f / 16) * 32 + (row < F ? 0 : 16) + (size_t)(f % 16);
-                    std::memcpy(dense + (d * (size_t)img.Kp + (size_t)j) * b, w, (size_t)b);
+                const int start = i - s * nbk;
+                if (start < 0) break;
+                for (int32_t k = v.indptr[start]; k < v.indptr[start + 1]; ++k) {
+                    const int j = v.indices[k];
+                    const size_t e = place(i, n++);
+                    idx[e] = last = (uint16_t)j;
+                    for (int t = 0; t < nbk; ++t) {
+                        const int row = i + t;
+                        uint8_t *w = val + (e * (size_t)nbk + (size_t)t) * b;
+                        put_weight(w, weight(k, row), scale[(size_t)row], dtype);
+                        const int f = row < F ? row : row - F;
+                        const size_t d = !gated ? (size_t)row : (size_t)(f / 16) * 32 + (row < F ? 0 : 16) + (size_t)(f % 16);
+                        std::memcpy(dense + (d * (size_t)img.Kp + (size_t)j) * b, w, (size_t)b);
+                    }
                 }
             }
+            const uint32_t all = (off[(size_t)(i / rb) + 1] - off[(size_t)(i / rb)]) * (uint32_t)(lanes * epc);
+            for (; n < all; ++n) idx[place(i, n)] = last;
         }
-    for (int i = 0; i < M; ++i) {
-        const uint32_t all = (off[(size_t)(i / rb) + 1] - off[(size_t)(i / rb)]) * (uint32_t)(lanes * epc);
-        const uint16_t last = next[(size_t)i] ? idx[place(i, next[(size_t)i] - 1)] : 0;
-        for (uint32_t n = next[(size_t)i]; n < all; ++n) idx[place(i, n)] = last;
-    }
+    });
     return UBP_OK;
 }
 
