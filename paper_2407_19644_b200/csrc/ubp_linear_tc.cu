@@ -138,6 +138,8 @@ template <typename T> __device__ __forceinline__ void store4(T *p, int n, bool v
 
 // ------------------------------------------------------------------ few tokens
 constexpr uint32_t FEW_A = 128 * LT_LINE;       // weight lines of one chunk: 16 KB
+// One block an SM (TC_PAIR_MIN_SMEM). Half the shared memory, so that the next launch's blocks could set up and start their
+// weight copies beside these, was slower: 24 tokens on 4096 x 8192 f16 17.0 us against 15.4, the ring is then too short.
 constexpr uint32_t FEW_BUDGET = 200 * 1024;
 __host__ __device__ constexpr int few_kch(int nt) { return nt <= 128 ? 2 : 1; }       // chunks per stage
 __host__ __device__ constexpr uint32_t few_stage(int nt) { return (uint32_t)few_kch(nt) * (FEW_A + (uint32_t)nt * LT_LINE); }
@@ -147,31 +149,44 @@ __host__ __device__ constexpr int few_stages(int nt)
     return s > LT_MAX_STAGES ? LT_MAX_STAGES : s;
 }
 
-// Tokens ta .. tb of a tile: the cluster's partial sums red[token][128], in the ranks' order, to y.
-template <bool F8, typename T>
-__device__ __forceinline__ void few_epilogue(const TcLinArgs &p, const float *red, int rt, int64_t t0, int ta, int tb, int S)
+// Epilogue of a few-token tile: every thread holds four features (32 threads a token, 16 of a gated layer); the epilogue
+// warps load their scales and biases while the main loop runs.
+struct FewCols {
+    float w0[4], w1[4], b0[4], b1[4];
+    int f, n, dl;                                               // first feature, features that exist, first dense row in the tile
+};
+template <bool F8>
+__device__ __forceinline__ FewCols few_cols(const TcLinArgs &p, int rt, int tid)
 {
     const LinearArgs &a = p.a;
-    const int per = a.gated ? 16 : 32;                          // threads of a token
-    const int o = ((int)threadIdx.x & (per - 1)) * 4, f = rt * (per * 4) + o, dl = a.gated ? (o >> 4) * 32 + (o & 15) : o;
-    const int n = a.F - f;
-    if (n <= 0) return;
-    float w0[4], w1[4], b0[4], b1[4];
+    const int per = a.gated ? 16 : 32, o = (tid & (per - 1)) * 4;
+    FewCols c;
+    c.f = rt * (per * 4) + o;
+    c.dl = a.gated ? (o >> 4) * 32 + (o & 15) : o;
+    c.n = a.F - c.f;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const int r = j < n ? f + j : f, u = a.gated ? a.F + r : r;
-        w0[j] = F8 ? __ldg(p.wscale + r) : 1.f;
-        w1[j] = F8 ? __ldg(p.wscale + u) : 1.f;
-        b0[j] = a.bias ? __ldg(a.bias + r) : 0.f;
-        b1[j] = a.bias ? __ldg(a.bias + u) : 0.f;
+        const int r = j < c.n ? c.f + j : a.F - 1, u = a.gated ? a.F + r : r;
+        c.w0[j] = F8 ? __ldg(p.wscale + r) : 1.f;
+        c.w1[j] = F8 ? __ldg(p.wscale + u) : 1.f;
+        c.b0[j] = a.bias ? __ldg(a.bias + r) : 0.f;
+        c.b1[j] = a.bias ? __ldg(a.bias + u) : 0.f;
     }
-    const bool vec = p.vec4 && n >= 4;
-    const int step = LT_THREADS / per;
+    return c;
+}
+// Tokens ta .. tb of the tile: the cluster's partial sums red[token][128], in the ranks' order, to y.
+template <bool F8, typename T>
+__device__ __forceinline__ void few_epilogue(const TcLinArgs &p, const FewCols &c, const float *red, int tid, int64_t t0, int ta, int tb, int S)
+{
+    const LinearArgs &a = p.a;
+    if (c.n <= 0) return;
+    const bool vec = p.vec4 && c.n >= 4;
+    const int per = a.gated ? 16 : 32, step = LT_THREADS / per;
 #pragma unroll 2
-    for (int t = ta + (int)threadIdx.x / per; t < tb; t += step) {
+    for (int t = ta + tid / per; t < tb; t += step) {
         float z[4] = {0.f, 0.f, 0.f, 0.f}, u[4] = {0.f, 0.f, 0.f, 0.f}, r[4] = {0.f, 0.f, 0.f, 0.f};
-        const float *src = red + t * 128 + dl;
-        if (a.res) load4(static_cast<const T *>(a.res) + (t0 + t) * a.ldr + f, n, vec, r);
+        const float *src = red + t * 128 + c.dl;
+        if (a.res) load4(static_cast<const T *>(a.res) + (t0 + t) * a.ldr + c.f, c.n, vec, r);
         const float xs = F8 ? a.xs[t0 + t] : 1.f;
         if (S > 1) {
             for (int k = 0; k < S; ++k) {
@@ -184,13 +199,13 @@ __device__ __forceinline__ void few_epilogue(const TcLinArgs &p, const float *re
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            z[j] = (F8 ? z[j] * (xs * w0[j]) : z[j]) + b0[j];
-            u[j] = (F8 ? u[j] * (xs * w1[j]) : u[j]) + b1[j];
+            z[j] = (F8 ? z[j] * (xs * c.w0[j]) : z[j]) + c.b0[j];
+            u[j] = (F8 ? u[j] * (xs * c.w1[j]) : u[j]) + c.b1[j];
         }
         apply_act<4>(z, a.act);
 #pragma unroll
         for (int j = 0; j < 4; ++j) z[j] = (a.gated ? z[j] * u[j] : z[j]) + r[j];
-        store4(static_cast<T *>(a.y) + (t0 + t) * a.ldy + f, n, vec, z);
+        store4(static_cast<T *>(a.y) + (t0 + t) * a.ldy + c.f, c.n, vec, z);
     }
 }
 
@@ -219,14 +234,23 @@ ubp_linear_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
     uint32_t cols = 32;
     while (cols < (uint32_t)NT) cols <<= 1;
 
+    auto issue_w = [&](int f) {
+        const int st = f % stages;
+        const uint32_t bar = smem_u32(&bar_full[st]);
+        mbar_expect_tx(bar, stage_bytes);
+        tma_load_3d(smem_u32(smem + (size_t)st * stage_bytes), &tmW, 0, rt * 128, k0 + f * KCH, bar);
+    };
+    // the ring's first weight lines are constants of the layer: under way before anything else
+    // (the activations' bytes may land before a stage's bytes are announced: its phase cannot end before)
+    const int pre = nst < stages ? nst : stages;
     if (threadIdx.x == 0) {
-        prefetch_tensormap(&tmW);
         prefetch_tensormap(&tmX);
         abort_flag = 0;
         for (int s = 0; s < stages; ++s) { mbar_init(smem_u32(&bar_full[s]), 1); mbar_init(smem_u32(&bar_empty[s]), 1); }
         mbar_init(smem_u32(&bar_acc), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        for (int f = 0; f < pre; ++f) issue_w(f);
     }
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_base_slot)), "r"(cols) : "memory");
@@ -242,12 +266,6 @@ ubp_linear_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
 
     if (warp == 0 || warp == LT_X_WARP) {
         if (lane == 0) {
-            auto issue_w = [&](int i) {
-                const int st = i % stages;
-                const uint32_t bar = smem_u32(&bar_full[st]);
-                mbar_expect_tx(bar, stage_bytes);
-                tma_load_3d(smem_u32(smem + (size_t)st * stage_bytes), &tmW, 0, rt * 128, k0 + i * KCH, bar);
-            };
             auto issue_x = [&](int i) {
                 const int st = i % stages;
                 const uint32_t bar = smem_u32(&bar_full[st]);
@@ -255,13 +273,9 @@ ubp_linear_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
                     tma_load_2d(smem_u32(smem + (size_t)st * stage_bytes + boff + (uint32_t)(u * NT * LT_LINE)), &tmX,
                                 (k0 + i * KCH + u) * line, (int)t0, bar);
             };
-            // the ring's first weight lines are constants of the layer: under way before the wait for the earlier kernel
-            // (the activations' bytes may land before the stage's bytes are announced: its phase cannot end before)
             const bool w = warp == 0;
-            const int pre = w ? (nst < stages ? nst : stages) : 0;
-            for (int i = 0; i < pre; ++i) issue_w(i);
             asm volatile("griddepcontrol.wait;" ::: "memory");
-            for (int i = pre; i < nst && ok; ++i) {
+            for (int i = w ? pre : 0; i < nst && ok; ++i) {
                 if (i >= stages) ok = mbar_wait(smem_u32(&bar_empty[i % stages]), (uint32_t)(i / stages - 1) & 1u, &abort_flag);
                 if (!ok) break;
                 if (w) issue_w(i);
@@ -287,6 +301,8 @@ ubp_linear_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
     }
     if (!(lane == 0 && (warp == 0 || warp == LT_X_WARP))) asm volatile("griddepcontrol.wait;" ::: "memory");
     float *red = reinterpret_cast<float *>(smem);              // [NT][128] partial sums, over the (finished) ring
+    const int tid = (int)threadIdx.x;
+    const FewCols fc = few_cols<F8>(p, rt, tid);
     if (warp >= 2 && warp < LT_X_WARP) {
         ok = mbar_wait_relaxed(smem_u32(&bar_acc), 0, &abort_flag);
         if (ok) {
@@ -305,12 +321,12 @@ ubp_linear_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     if (S > 1) cluster_sync();
     else __syncthreads();
-    // ---- epilogue of this rank's share of the tokens: four features a thread, a token's 128 (gated: 64) a warp (half a warp)
+    // ---- epilogue of this rank's share of the tokens
     {
         const int ta = (int)((int64_t)nt * rank / S), tb = (int)((int64_t)nt * (rank + 1) / S);
-        if (p.ydt == UBP_BF16) few_epilogue<F8, __nv_bfloat16>(p, red, rt, t0, ta, tb, S);
-        else if (p.ydt == UBP_F16) few_epilogue<F8, __half>(p, red, rt, t0, ta, tb, S);
-        else few_epilogue<F8, float>(p, red, rt, t0, ta, tb, S);
+        if (p.ydt == UBP_BF16) few_epilogue<F8, __nv_bfloat16>(p, fc, red, tid, t0, ta, tb, S);
+        else if (p.ydt == UBP_F16) few_epilogue<F8, __half>(p, fc, red, tid, t0, ta, tb, S);
+        else few_epilogue<F8, float>(p, fc, red, tid, t0, ta, tb, S);
     }
     if (S > 1) cluster_sync();                                  // nobody leaves while its partial sums are being read
     else __syncthreads();
@@ -709,14 +725,12 @@ template <typename K> int allow_smem(K kern, bool (&done)[64], size_t least)
 }
 
 template <bool F8>
-int launch_few(const ubp_linear_plan *pl, const CUtensorMap &tmW, const CUtensorMap &tmX, const TcLinArgs &p, int fmt, int NT, int ntt, int S, cudaStream_t st)
+int launch_few(const CUtensorMap &tmW, const CUtensorMap &tmX, const TcLinArgs &p, int fmt, int NT, int ntt, int S, cudaStream_t st)
 {
     static bool done[64] = {};
     const auto kern = ubp_linear_few_kernel<F8>;
     if (int rc = allow_smem(kern, done, TC_PAIR_MIN_SMEM)) return rc;
-    size_t smem = (size_t)few_stages(NT) * few_stage(NT);
-    if (smem < (size_t)NT * 512) smem = (size_t)NT * 512;
-    smem += 1024;
+    size_t smem = (size_t)few_stages(NT) * few_stage(NT) + 1024;
     if (smem < TC_PAIR_MIN_SMEM) smem = TC_PAIR_MIN_SMEM;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((p.rows + 127) / 128 * ntt * S));
@@ -732,7 +746,6 @@ int launch_few(const ubp_linear_plan *pl, const CUtensorMap &tmW, const CUtensor
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    (void)pl;
     cudaError_t e = cudaLaunchKernelEx(&cfg, kern, tmW, tmX, p, fmt, NT, ntt, S);
     if (e == cudaSuccess) e = cudaGetLastError();
     return e == cudaSuccess ? UBP_OK : fail(e);
@@ -813,7 +826,7 @@ int launch_linear_tc(const ubp_linear_plan *pl, const LinearArgs &args, int y_dt
         if (int rc = encode_w(&tmW, pl, 128, few_kch(ch.cols))) return rc;
         if (int rc = encode_x(&tmX, x, pl->dtype, ldx, args.T, C, ch.cols)) return rc;
         const int ntt = (int)((args.T + ch.cols - 1) / ch.cols);
-        return f8 ? launch_few<true>(pl, tmW, tmX, p, fmt, ch.cols, ntt, ch.split, st) : launch_few<false>(pl, tmW, tmX, p, fmt, ch.cols, ntt, ch.split, st);
+        return f8 ? launch_few<true>(tmW, tmX, p, fmt, ch.cols, ntt, ch.split, st) : launch_few<false>(tmW, tmX, p, fmt, ch.cols, ntt, ch.split, st);
     }
     if (int rc = encode_w(&tmW, pl, ch.cols / 2, 1)) return rc;
     if (int rc = encode_x(&tmX, x, pl->dtype, ldx, args.T, C, 128)) return rc;
