@@ -199,3 +199,103 @@ def test_refusals(ubp):
     plan.free()
     with pytest.raises(RuntimeError):
         ubp.ubp_linear(plan, x)
+
+
+#: (tokens, rows, input features, block rows, sparsity, kernel and tile the call has to take): every kernel and tile once, on
+#: layers where the other kernel would be the choice at nearby sizes
+PATHS = [(1, 2048, 2048, 4, 0, (0, 1)), (2, 2048, 2048, 4, 60, (0, 2)), (3, 2048, 2048, 4, 80, (0, 4)), (8, 2048, 2048, 4, 90, (0, 8)),
+         (16, 512, 512, 8, 95, (0, 8)), (16, 2048, 2048, 4, 0, (1, 16)), (20, 300, 3000, 2, 70, (1, 32)), (77, 4000, 260, 4, 70, (1, 80)),
+         (256, 130, 600, 4, 70, (1, 256)), (257, 130, 600, 4, 70, (2, 128)), (2600, 1030, 70, 2, 60, (2, 256)), (2100, 4100, 96, 4, 80, (2, 256))]
+
+
+@pytest.mark.parametrize("T,M,C,Nb,p,path", PATHS)
+def test_every_kernel(ubp, T, M, C, Nb, p, path):
+    W, mask = make_weight(M, C, Nb, p, 7 * M + C)
+    for dtype, out in ((BF16, BF16), (F16, F32), (F8, BF16)):
+        plan = check(ubp, W, mask, Nb, T, dtype, out, pad=8, seed=41)[0]
+        if dtype == BF16:
+            assert plan.choice(T)[:2] == path
+        check(ubp, W, mask, Nb, T, dtype, out, act="silu", gated=True, residual=False, seed=43)
+
+
+@pytest.mark.parametrize("ypad,rpad", [(0, 0), (4, 4), (2, 2), (1, 1), (8, 2), (0, 8)])
+def test_output_alignments(ubp, ypad, rpad):
+    """Rows of y and of the residual aligned to 16, 8, 4 and 2 bytes, features a multiple of that or not."""
+    for M in (512, 500, 508, 502, 501):
+        W, mask = make_weight(M, 96, 1, 60, M)
+        for T, out in ((300, BF16), (300, F32), (40, BF16), (2, BF16)):
+            check(ubp, W, mask, 1, T, BF16, out, act="relu", pad=rpad, ypad=ypad, seed=51)
+
+
+def test_offsets_beyond_32_bits(ubp):
+    W, mask = make_weight(96, 200, 4, 60, 8)
+    plan = ubp.LinearPlan(ubp.ubp_pack(W, mask, 4), BF16)
+    for T, ld in ((3, (1 << 30) + 8), (18, (1 << 27) + 8)):
+        buf = torch.empty(T * ld, dtype=BF16, device="cuda")
+        x = buf.view(T, ld)[:, :200]
+        x.copy_(torch.randn(T, 200, device="cuda", generator=torch.Generator(device="cuda").manual_seed(4)))
+        y = buf.view(T, ld)[:, 1024:1120]
+        want = ubp.ubp_linear(plan, x.contiguous())
+        ubp.ubp_linear(plan, x, out=y)
+        assert torch.equal(y, want)
+        del buf, x, y
+
+
+@pytest.mark.parametrize("T", [1, 5, 30, 300])
+def test_launches_back_to_back(ubp, T):
+    """The calls' kernels start before the ones before them have finished: a chain in which every call reads what the call
+    before wrote, over buffers that are used again, gives the same values every time."""
+    C, F = 512, 1024
+    Wg, mg = make_weight(2 * F, C, 4, 80, 1)
+    Wd, md = make_weight(C, F, 4, 80, 2)
+    up, down = ubp.LinearPlan(ubp.ubp_pack(Wg, mg, 4), F8, gated=True), ubp.LinearPlan(ubp.ubp_pack(Wd, md, 4), F8)
+    g = torch.Generator(device="cuda").manual_seed(0)
+    x0, h0 = (torch.randn(T, C, device="cuda", generator=g).to(BF16) for _ in range(2))
+    gamma = torch.ones(C, device="cuda", dtype=BF16)
+    q, s, a = torch.empty(T, C, device="cuda", dtype=F8), torch.empty(T, device="cuda"), torch.empty(T, F, device="cuda", dtype=BF16)
+    p, t, h = torch.empty(T, F, device="cuda", dtype=F8), torch.empty(T, device="cuda"), torch.empty_like(h0)
+
+    def chain(sync):
+        h.copy_(h0)
+        for _ in range(6):
+            for call in (lambda: ubp.ubp_rmsnorm(x0, gamma, 1e-5, residual=h, residual_out=h, out=q, scales=s),
+                         lambda: ubp.ubp_linear(up, q, activation="silu", x_scales=s, out=a),
+                         lambda: ubp.ubp_quant_rows(a, out=p, scales=t),
+                         lambda: ubp.ubp_linear(down, p, residual=h, x_scales=t, out=h)):
+                call()
+                if sync:
+                    torch.cuda.synchronize()
+        return h.clone()
+
+    want = chain(True)
+    assert torch.isfinite(want.float()).all()
+    for _ in range(20):
+        assert torch.equal(chain(False), want)
+    up.check()
+    down.check()
+
+
+def test_example_runs():
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    r = subprocess.run([sys.executable, os.path.join(root, "examples", "pruned_feed_forward.py"), "--width", "512", "--hidden", "1024"],
+                       cwd=root, capture_output=True, text=True, timeout=600)
+    assert r.returncode == 0 and "pruned feed-forward ok" in r.stdout, r.stdout[-2000:] + r.stderr[-2000:]
+
+
+def test_checked_build():
+    """The same cases on the checked build of the library, whose kernels compare the plan's indices with their extents."""
+    import os
+    import subprocess
+    import sys
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    lib = os.path.join(root, "paper_2407_19644_b200", "libubp_b200_debug.so")
+    if not os.path.exists(lib):
+        from paper_2407_19644_b200 import build
+        build.build(debug=True)
+    r = subprocess.run([sys.executable, "-m", "pytest", "tests/test_gpu_linear.py", "tests/test_gpu_rows.py", "-q", "-x", "-m", "gpu", "-k",
+                        "test_product or test_every_kernel or test_rows_without_blocks or test_special"], cwd=root,
+                       env=dict(os.environ, UBP_B200_LIBRARY=lib), capture_output=True, text=True, timeout=900)
+    assert r.returncode == 0 and "passed" in r.stdout, r.stdout[-3000:] + r.stderr[-2000:]
