@@ -533,7 +533,8 @@ class _Torch:
         self.f32, self.bf16, self.f8 = torch.float32, torch.bfloat16, torch.float8_e4m3fn
         self.codes = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.float8_e4m3fn: 3}
         self.row_types = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
-        self.current_device = torch.cuda.current_device
+        self.only_f32 = (torch.float32,)
+        self.current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
         self.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
             (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
@@ -573,22 +574,26 @@ def _vec(t, name, n, dtypes, dev):
 
 def _call(k, dev, fn, what, args, stream):
     """fn(*args, stream) with `dev` current."""
+    st = k.raw_stream(dev) if stream is None else stream.cuda_stream
     if k.current_device() == dev:
-        rc = fn(*args, k.raw_stream(dev) if stream is None else stream.cuda_stream)
+        rc = fn(*args, st)
     else:
         with k.torch.cuda.device(dev):
-            rc = fn(*args, k.raw_stream(dev) if stream is None else stream.cuda_stream)
+            rc = fn(*args, st)
     if rc:
         _chk(rc, what)
 
 
 def _rows_x(k, x):
-    """(T, C, row stride, device index, type) of an activation matrix."""
-    if not isinstance(x, k.Tensor) or x.dim() != 2 or x.dtype not in k.row_types or not x.is_cuda:
+    """(T, C, row stride, device index, type, its code) of an activation matrix."""
+    code = k.row_types.get(x.dtype) if isinstance(x, k.Tensor) else None
+    if code is None or not x.is_cuda or len(x.shape) != 2:
         raise ValueError("x must be a [T][C] float32, float16 or bfloat16 CUDA tensor")
     T, Cc = x.shape
-    dt, dev = x.dtype, x.get_device()
-    return T, Cc, _ld(x, "x", T, Cc, dt, dev), dev, dt
+    ld, one = x.stride()
+    if one != 1 and Cc > 1 or ld < Cc and T > 1:
+        raise ValueError("x must have contiguous rows that do not overlap")
+    return T, Cc, ld, x.get_device(), x.dtype, code
 
 
 def ubp_rmsnorm(x, gamma, eps: float = 1e-6, residual=None, out_dtype=None, out=None, scales=None, residual_out=None,
@@ -599,7 +604,7 @@ def ubp_rmsnorm(x, gamma, eps: float = 1e-6, residual=None, out_dtype=None, out=
     a residual. residual_out may be the residual or x itself."""
     k = _tk()
     L = _lib or load()
-    T, Cc, ldx, dev, dt = _rows_x(k, x)
+    T, Cc, ldx, dev, dt, code = _rows_x(k, x)
     pg = _vec(gamma, "gamma", Cc, (dt, k.f32), dev)
     if out_dtype is None:
         out_dtype = out.dtype if out is not None else dt
@@ -618,7 +623,7 @@ def ubp_rmsnorm(x, gamma, eps: float = 1e-6, residual=None, out_dtype=None, out=
             scales = k.empty(T, dtype=k.f32, device=device)
             ps = scales.data_ptr()
         else:
-            ps = _vec(scales, "scales", T, (k.f32,), dev)
+            ps = _vec(scales, "scales", T, k.only_f32, dev)
     else:
         scales = None
     pr = ph = None
@@ -631,9 +636,8 @@ def ubp_rmsnorm(x, gamma, eps: float = 1e-6, residual=None, out_dtype=None, out=
     if residual_out is not None and ph is None:
         ldh = _ld(residual_out, "residual_out", T, Cc, dt, dev)
         ph = residual_out.data_ptr()
-    codes = k.codes
-    _call(k, dev, L.ubp_rmsnorm, "ubp_rmsnorm", (x.data_ptr(), ldx, pr, ldr, pg, codes[gamma.dtype], codes[dt], T, Cc, eps,
-                                                 ph, ldh, out.data_ptr(), ldy, codes[out_dtype], ps), stream)
+    _call(k, dev, L.ubp_rmsnorm, "ubp_rmsnorm", (x.data_ptr(), ldx, pr, ldr, pg, k.codes[gamma.dtype], code, T, Cc, eps,
+                                                 ph, ldh, out.data_ptr(), ldy, 3 if q else code, ps), stream)
     return out, scales, residual_out
 
 
@@ -642,7 +646,7 @@ def ubp_quant_rows(x, out=None, scales=None, stream=None):
     x ~= q * scales[:, None]."""
     k = _tk()
     L = _lib or load()
-    T, Cc, ldx, dev, dt = _rows_x(k, x)
+    T, Cc, ldx, dev, _, code = _rows_x(k, x)
     ldq = Cc
     if out is None:
         out = k.empty(T, Cc, dtype=k.f8, device=x.device)
@@ -652,8 +656,8 @@ def ubp_quant_rows(x, out=None, scales=None, stream=None):
         scales = k.empty(T, dtype=k.f32, device=x.device)
         ps = scales.data_ptr()
     else:
-        ps = _vec(scales, "scales", T, (k.f32,), dev)
-    _call(k, dev, L.ubp_quant_rows, "ubp_quant_rows", (x.data_ptr(), ldx, k.codes[dt], T, Cc, out.data_ptr(), ldq, ps), stream)
+        ps = _vec(scales, "scales", T, k.only_f32, dev)
+    _call(k, dev, L.ubp_quant_rows, "ubp_quant_rows", (x.data_ptr(), ldx, code, T, Cc, out.data_ptr(), ldq, ps), stream)
     return out, scales
 
 
@@ -757,43 +761,45 @@ def ubp_linear(plan: LinearPlan, x, bias=None, activation: str = "none", residua
     [T][F] in the output's type, may be `out` itself. out_dtype: the plan's type (8-bit plans: bfloat16) unless given.
     workspace: a CUDA tensor for inputs whose rows are not 16-byte aligned (allocated here when needed and not given)."""
     k = _tk()
-    L, dev, F, T = plan._lib, plan._index, plan.out_features, 0
-    if not isinstance(x, k.Tensor) or x.dim() != 2:
+    L, dev, F, Cc, b, handle = plan._lib, plan._index, plan.out_features, plan.C, plan._bytes, plan._handle
+    if handle is None:
+        raise RuntimeError("plan was freed")
+    if not isinstance(x, k.Tensor) or len(x.shape) != 2:
         raise ValueError("x must be a [T][C] CUDA tensor")
     T = x.shape[0]
-    ldx = _ld(x, "x", T, plan.C, plan.dtype, dev)
+    ldx = _ld(x, "x", T, Cc, plan.dtype, dev)
     act = ACTIVATIONS.get(activation)
     if act is None:
         raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}")
-    if (plan._bytes == 1) != (x_scales is not None):
+    if (b == 1) != (x_scales is not None):
         raise ValueError("x_scales goes with an 8-bit plan")
     if out_dtype is None:
-        out_dtype = out.dtype if out is not None else k.bf16 if plan._bytes == 1 else plan.dtype
+        out_dtype = out.dtype if out is not None else k.bf16 if b == 1 else plan.dtype
     ydt = k.codes.get(out_dtype)
     if ydt is None:
         raise ValueError("out_dtype must be float32, float16 or bfloat16")
-    ldy, ldr = F, 0
+    ldy, ldr, pr = F, 0, None
     if out is None:
-        out = k.empty(T, F, dtype=out_dtype, device=x.device)
+        out = k.empty(T, F, dtype=out_dtype, device=plan.device)
     else:
         ldy = _ld(out, "out", T, F, out_dtype, dev)
     if residual is not None:
         ldr = _ld(residual, "residual", T, F, out_dtype, dev)
+        pr = residual.data_ptr()
     px = x.data_ptr()
-    nws = 0
+    pw, nws = None, 0
     if workspace is not None:
         if workspace.get_device() != dev or not workspace.is_contiguous():
             raise ValueError("workspace must be a contiguous tensor on the plan's device")
-        nws = workspace.numel() * workspace.element_size()
-    elif (px | ldx * plan._bytes) & 15:                    # rows a tensor copy cannot take: the call may need room to lay them out
-        nws = L.ubp_linear_workspace_size(plan.handle, px, ldx, T)
+        pw, nws = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    elif (px | ldx * b) & 15:                              # rows a tensor copy cannot take: the call may need room to lay them out
+        nws = L.ubp_linear_workspace_size(handle, px, ldx, T)
         if nws:
-            workspace = k.empty(nws, dtype=k.torch.uint8, device=x.device)
+            workspace = k.empty(nws, dtype=k.torch.uint8, device=plan.device)
+            pw = workspace.data_ptr()
             if stream is not None:
                 workspace.record_stream(stream)
-    _call(k, dev, L.ubp_linear, "ubp_linear",
-          (plan.handle, px, ldx, None if x_scales is None else _vec(x_scales, "x_scales", T, (k.f32,), dev), T,
-           None if bias is None else _vec(bias, "bias", plan.M, (k.f32,), dev), act,
-           None if residual is None else residual.data_ptr(), ldr, out.data_ptr(), ldy, ydt,
-           None if workspace is None else workspace.data_ptr(), nws), stream)
+    args = (handle, px, ldx, None if x_scales is None else _vec(x_scales, "x_scales", T, k.only_f32, dev), T,
+            None if bias is None else _vec(bias, "bias", plan.M, k.only_f32, dev), act, pr, ldr, out.data_ptr(), ldy, ydt, pw, nws)
+    _call(k, dev, L.ubp_linear, "ubp_linear", args, stream)
     return out

@@ -74,7 +74,8 @@ LinearChoice linear_choose(const ubp_linear_plan *p, int64_t T, int sms);
 
 // tokens a block of the kept-block kernel takes (1, 2, 4 or 8) and the number of such groups
 void linear_sparse_tokens(const ubp_linear_plan *p, int64_t T, int *tokens, int64_t *groups);
-int launch_linear_sparse(const ubp_linear_plan *p, const LinearArgs &a, int y_dtype, void *stream);
+int launch_linear_sparse(const ubp_linear_plan *p, const LinearArgs &a, int y_dtype, int sms, void *stream);
+int device_sms();
 // whether the tensor-core kernels can copy x's rows as they are (else they go through the workspace, [T][Kp])
 bool linear_x_direct(const ubp_linear_plan *p, const void *x, int64_t ldx, int64_t T);
 int launch_linear_tc(const ubp_linear_plan *p, const LinearArgs &a, int y_dtype, const LinearChoice &ch, void *workspace, int sms,

@@ -40,10 +40,15 @@ LinearChoice linear_choose(const ubp_linear_plan *p, int64_t T, int sms)
     return {LIN_MANY, t128 <= sms / 2 ? 128 : 256, 0};
 }
 
-static int device_sms()
+// SMs of the current device (asked once per device)
+int device_sms()
 {
-    int sms = 148, dev = 0;
-    if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    static int known[64] = {};
+    int dev = 0, sms = 148;
+    if (cudaGetDevice(&dev) != cudaSuccess) return sms;
+    if (dev < 64 && known[dev]) return known[dev];
+    if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 148;
+    if (dev < 64) known[dev] = sms;
     return sms;
 }
 
@@ -172,7 +177,7 @@ int ubp_linear(const ubp_linear_plan_t *plan, const void *x, int64_t ldx, const 
     a.M = plan->M; a.C = plan->C; a.F = plan->F; a.gated = plan->gated;
     const int sms = ubp::device_sms();
     const ubp::LinearChoice ch = ubp::linear_choose(plan, T, sms);
-    if (ch.kernel == ubp::LIN_SPARSE) return ubp::launch_linear_sparse(plan, a, y_dtype, stream);
+    if (ch.kernel == ubp::LIN_SPARSE) return ubp::launch_linear_sparse(plan, a, y_dtype, sms, stream);
     return ubp::launch_linear_tc(plan, a, y_dtype, ch, workspace, sms, stream);
 }
 

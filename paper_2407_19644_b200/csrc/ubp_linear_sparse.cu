@@ -398,7 +398,7 @@ void linear_sparse_tokens(const ubp_linear_plan *p, int64_t T, int *tokens, int6
     *groups = (T + t - 1) / t;
 }
 
-int launch_linear_sparse(const ubp_linear_plan *pl, const LinearArgs &a, int y_dtype, void *stream)
+int launch_linear_sparse(const ubp_linear_plan *pl, const LinearArgs &a, int y_dtype, int sms, void *stream)
 {
     SpArgs p;
     p.a = a;
@@ -412,8 +412,6 @@ int launch_linear_sparse(const ubp_linear_plan *pl, const LinearArgs &a, int y_d
     int64_t nchunk;
     linear_sparse_tokens(pl, a.T, &TT, &nchunk);
     if (nchunk > 65535) return UBP_E_UNSUPPORTED;
-    int sms = 148, dev = 0;
-    if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
     // Blocks per chunk of tokens: together one for every SM, and not one less while there are rows for it: an SM without a
     // block has room for two of the next launch (whose blocks come early, see above), and those two take twice the time of
     // the others. Large layers: as many rows as shared memory leaves room for.

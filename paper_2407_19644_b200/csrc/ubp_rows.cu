@@ -23,6 +23,7 @@
 #include <cstdint>
 
 #include "ubp_internal.h"
+#include "ubp_linear.h"
 #include "ubp_types.cuh"
 
 namespace ubp {
@@ -275,8 +276,7 @@ int launch_rows_k(const RowArgs &a, int sms, cudaStream_t stream)
 template <typename T, typename TO, bool NORM>
 int launch_rows_t(const RowArgs &a, bool vec, cudaStream_t st)
 {
-    int sms = 148, dev = 0;
-    if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev);
+    const int sms = device_sms();
     if (vec) {
         if (a.C <= 256) return launch_rows_k<T, TO, NORM, 8, 32, 1>(a, sms, st);
         if (a.C <= 512) return launch_rows_k<T, TO, NORM, 8, 32, 2>(a, sms, st);
