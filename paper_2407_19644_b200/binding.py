@@ -520,80 +520,31 @@ def ubp_bed_select(W, Nb: int, m: int, stream=None):
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 
 
-class _Torch:
-    """What the token-major calls need of torch, looked up once (importing the package does not import torch). A call on a
-    token or two is bound by the host, so these calls check what they are given without context managers or stream objects
-    (a torch.cuda.current_stream() is 3 us, the raw handle 0.1 us) and pass sizes to torch.empty one by one (0.8 us less
-    than as a tuple)."""
-
-    def __init__(self):
-        import torch
-        self.torch = torch
-        self.Tensor, self.empty, self.empty_like = torch.Tensor, torch.empty, torch.empty_like
-        self.f32, self.bf16, self.f8 = torch.float32, torch.bfloat16, torch.float8_e4m3fn
-        self.codes = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.float8_e4m3fn: 3}
-        self.row_types = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}
-        self.only_f32 = (torch.float32,)
-        self.current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
-        self.raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
-            (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_calls = None
 
 
-_torch = None
-
-
-def _tk() -> _Torch:
-    global _torch
-    if _torch is None:
-        _torch = _Torch()
-    return _torch
+def _native():
+    """The extension module that checks the arguments of the token-major calls and allocates their outputs, bound to the
+    entry points of the loaded library. A call on one token is bound by the host: through ctypes its marshalling took as long
+    as the launch."""
+    global _calls
+    if _calls is None:
+        import torch  # noqa: F401  (its libraries have to be loaded first)
+        L = load()
+        try:
+            from . import _torch_calls
+        except ImportError as e:
+            raise RuntimeError("paper_2407_19644_b200/_torch_calls.so is missing or does not match this torch: build it with "
+                               "`python -m paper_2407_19644_b200.build` (there is no fallback implementation)") from e
+        _torch_calls.bind(*(C.cast(f, C.c_void_p).value for f in (L.ubp_rmsnorm, L.ubp_quant_rows, L.ubp_linear, L.ubp_linear_workspace_size)))
+        _calls = _torch_calls
+    return _calls
 
 
 def _dtypes():
-    return _tk().codes
-
-
-def _ld(t, name, T, Cc, dtype, dev):
-    """Check a [T][Cc] CUDA tensor with contiguous, disjoint rows of one type on device `dev`; returns its row stride."""
-    sh = t.shape
-    if len(sh) != 2 or sh[0] != T or sh[1] != Cc or t.dtype != dtype or t.get_device() != dev:
-        raise ValueError(f"{name} must be a [{T}][{Cc}] tensor of {dtype} on cuda:{dev}, got {tuple(sh)} {t.dtype} on {t.device}")
-    ld, one = t.stride()
-    if one != 1 and Cc > 1 or ld < Cc and T > 1:
-        raise ValueError(f"{name} must have contiguous rows that do not overlap")
-    return ld
-
-
-def _vec(t, name, n, dtypes, dev):
-    """Check a contiguous [n] CUDA vector of one of the types; returns its address."""
-    sh = t.shape
-    if len(sh) != 1 or sh[0] != n or t.dtype not in dtypes or t.get_device() != dev or n > 1 and t.stride(0) != 1:
-        raise ValueError(f"{name} must be a contiguous [{n}] vector of {' or '.join(map(str, dtypes))} on cuda:{dev}")
-    return t.data_ptr()
-
-
-def _call(k, dev, fn, what, args, stream):
-    """fn(*args, stream) with `dev` current."""
-    st = k.raw_stream(dev) if stream is None else stream.cuda_stream
-    if k.current_device() == dev:
-        rc = fn(*args, st)
-    else:
-        with k.torch.cuda.device(dev):
-            rc = fn(*args, st)
-    if rc:
-        _chk(rc, what)
-
-
-def _rows_x(k, x):
-    """(T, C, row stride, device index, type, its code) of an activation matrix."""
-    code = k.row_types.get(x.dtype) if isinstance(x, k.Tensor) else None
-    if code is None or not x.is_cuda or len(x.shape) != 2:
-        raise ValueError("x must be a [T][C] float32, float16 or bfloat16 CUDA tensor")
-    T, Cc = x.shape
-    ld, one = x.stride()
-    if one != 1 and Cc > 1 or ld < Cc and T > 1:
-        raise ValueError("x must have contiguous rows that do not overlap")
-    return T, Cc, ld, x.get_device(), x.dtype, code
+    """torch dtype -> ubp_dtype."""
+    import torch
+    return {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2, torch.float8_e4m3fn: 3}
 
 
 def ubp_rmsnorm(x, gamma, eps: float = 1e-6, residual=None, out_dtype=None, out=None, scales=None, residual_out=None,
@@ -602,63 +553,20 @@ def ubp_rmsnorm(x, gamma, eps: float = 1e-6, residual=None, out_dtype=None, out=
     h = x + residual; y = h * gamma / sqrt(mean(h^2) + eps). Returns (y, scales, h): y in x's type with scales None, or
     (out_dtype=torch.float8_e4m3fn) in 8 bits with one float32 scale a row; h is x + residual in x's type, or None without
     a residual. residual_out may be the residual or x itself."""
-    k = _tk()
-    L = _lib or load()
-    T, Cc, ldx, dev, dt, code = _rows_x(k, x)
-    pg = _vec(gamma, "gamma", Cc, (dt, k.f32), dev)
-    if out_dtype is None:
-        out_dtype = out.dtype if out is not None else dt
-    q = out_dtype == k.f8
-    if not q and out_dtype != dt:
-        raise ValueError("out_dtype must be x's type or torch.float8_e4m3fn")
-    ldy = ldr = ldh = Cc
-    device = x.device
-    if out is None:
-        out = k.empty(T, Cc, dtype=out_dtype, device=device)
-    else:
-        ldy = _ld(out, "out", T, Cc, out_dtype, dev)
-    ps = None
-    if q:
-        if scales is None:
-            scales = k.empty(T, dtype=k.f32, device=device)
-            ps = scales.data_ptr()
-        else:
-            ps = _vec(scales, "scales", T, k.only_f32, dev)
-    else:
-        scales = None
-    pr = ph = None
-    if residual is not None:
-        ldr = _ld(residual, "residual", T, Cc, dt, dev)
-        pr = residual.data_ptr()
-        if residual_out is None:
-            residual_out = k.empty(T, Cc, dtype=dt, device=device)
-            ph = residual_out.data_ptr()
-    if residual_out is not None and ph is None:
-        ldh = _ld(residual_out, "residual_out", T, Cc, dt, dev)
-        ph = residual_out.data_ptr()
-    _call(k, dev, L.ubp_rmsnorm, "ubp_rmsnorm", (x.data_ptr(), ldx, pr, ldr, pg, k.codes[gamma.dtype], code, T, Cc, eps,
-                                                 ph, ldh, out.data_ptr(), ldy, 3 if q else code, ps), stream)
-    return out, scales, residual_out
+    r = (_calls or _native()).rmsnorm(x, gamma, eps, residual, out_dtype, out, scales, residual_out,
+                                      None if stream is None else stream.cuda_stream)
+    if type(r) is int:
+        _chk(r, "ubp_rmsnorm")
+    return r
 
 
 def ubp_quant_rows(x, out=None, scales=None, stream=None):
     """Rows of x [T][C] (float32, float16 or bfloat16) in 8 bits: (q float8_e4m3fn [T][C], scales float32 [T]) with
     x ~= q * scales[:, None]."""
-    k = _tk()
-    L = _lib or load()
-    T, Cc, ldx, dev, _, code = _rows_x(k, x)
-    ldq = Cc
-    if out is None:
-        out = k.empty(T, Cc, dtype=k.f8, device=x.device)
-    else:
-        ldq = _ld(out, "out", T, Cc, k.f8, dev)
-    if scales is None:
-        scales = k.empty(T, dtype=k.f32, device=x.device)
-        ps = scales.data_ptr()
-    else:
-        ps = _vec(scales, "scales", T, k.only_f32, dev)
-    _call(k, dev, L.ubp_quant_rows, "ubp_quant_rows", (x.data_ptr(), ldx, code, T, Cc, out.data_ptr(), ldq, ps), stream)
-    return out, scales
+    r = (_calls or _native()).quant_rows(x, out, scales, None if stream is None else stream.cuda_stream)
+    if type(r) is int:
+        _chk(r, "ubp_quant_rows")
+    return r
 
 
 def linear_plan_image(blob: bytes, dtype, gated: bool = False):
@@ -684,7 +592,7 @@ class LinearPlan:
         import torch
         L = load()
         self._lib = L
-        self._handle = None
+        self._handle = self._spec = None
         if dtype not in _dtypes() or dtype == torch.float32:
             raise ValueError("dtype must be torch.bfloat16, torch.float16 or torch.float8_e4m3fn")
         d = np.frombuffer(blob, np.uint8)
@@ -698,14 +606,13 @@ class LinearPlan:
         self.out_features = v.M // 2 if gated else v.M
         self.buffer = torch.empty(n.value + 256, dtype=torch.uint8, device=device)
         self.device = self.buffer.device
-        self._index = self.buffer.get_device()
-        self._dtype_code, self._bytes = _dtypes()[dtype], 1 if dtype == torch.float8_e4m3fn else 2
         self._dev = (self.buffer.data_ptr() + 255) // 256 * 256
         h = C.c_void_p()
         with torch.cuda.device(self.device):
             _chk(L.ubp_linear_plan_build(_np_ptr(d), d.size, _dtypes()[dtype], int(gated), C.c_void_p(self._dev), n.value,
                                          _stream_ptr(stream), C.byref(h)), "ubp_linear_plan_build")
         self._handle = h
+        self._spec = (h.value, self.M, self.C, self.out_features, _dtypes()[dtype], self.buffer.get_device())
 
     @property
     def handle(self):
@@ -745,7 +652,7 @@ class LinearPlan:
     def free(self):
         if self._handle is not None:
             self._lib.ubp_linear_plan_free(self._handle)
-            self._handle = None
+            self._handle = self._spec = None
 
     def __del__(self):
         try:
@@ -760,46 +667,14 @@ def ubp_linear(plan: LinearPlan, x, bias=None, activation: str = "none", residua
     x: [T][C] in the plan's type, rows contiguous; 8-bit plans need x_scales (float32 [T]). bias: float32 [M]. residual:
     [T][F] in the output's type, may be `out` itself. out_dtype: the plan's type (8-bit plans: bfloat16) unless given.
     workspace: a CUDA tensor for inputs whose rows are not 16-byte aligned (allocated here when needed and not given)."""
-    k = _tk()
-    L, dev, F, Cc, b, handle = plan._lib, plan._index, plan.out_features, plan.C, plan._bytes, plan._handle
-    if handle is None:
+    spec = plan._spec
+    if spec is None:
         raise RuntimeError("plan was freed")
-    if not isinstance(x, k.Tensor) or len(x.shape) != 2:
-        raise ValueError("x must be a [T][C] CUDA tensor")
-    T = x.shape[0]
-    ldx = _ld(x, "x", T, Cc, plan.dtype, dev)
     act = ACTIVATIONS.get(activation)
     if act is None:
         raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}")
-    if (b == 1) != (x_scales is not None):
-        raise ValueError("x_scales goes with an 8-bit plan")
-    if out_dtype is None:
-        out_dtype = out.dtype if out is not None else k.bf16 if b == 1 else plan.dtype
-    ydt = k.codes.get(out_dtype)
-    if ydt is None:
-        raise ValueError("out_dtype must be float32, float16 or bfloat16")
-    ldy, ldr, pr = F, 0, None
-    if out is None:
-        out = k.empty(T, F, dtype=out_dtype, device=plan.device)
-    else:
-        ldy = _ld(out, "out", T, F, out_dtype, dev)
-    if residual is not None:
-        ldr = _ld(residual, "residual", T, F, out_dtype, dev)
-        pr = residual.data_ptr()
-    px = x.data_ptr()
-    pw, nws = None, 0
-    if workspace is not None:
-        if workspace.get_device() != dev or not workspace.is_contiguous():
-            raise ValueError("workspace must be a contiguous tensor on the plan's device")
-        pw, nws = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    elif (px | ldx * b) & 15:                              # rows a tensor copy cannot take: the call may need room to lay them out
-        nws = L.ubp_linear_workspace_size(handle, px, ldx, T)
-        if nws:
-            workspace = k.empty(nws, dtype=k.torch.uint8, device=plan.device)
-            pw = workspace.data_ptr()
-            if stream is not None:
-                workspace.record_stream(stream)
-    args = (handle, px, ldx, None if x_scales is None else _vec(x_scales, "x_scales", T, k.only_f32, dev), T,
-            None if bias is None else _vec(bias, "bias", plan.M, k.only_f32, dev), act, pr, ldr, out.data_ptr(), ldy, ydt, pw, nws)
-    _call(k, dev, L.ubp_linear, "ubp_linear", args, stream)
-    return out
+    r = (_calls or _native()).linear(spec, x, bias, act, residual, x_scales, out, out_dtype,
+                                     None if stream is None else stream.cuda_stream, workspace)
+    if type(r) is int:
+        _chk(r, "ubp_linear")
+    return r

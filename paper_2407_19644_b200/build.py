@@ -17,6 +17,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libubp_b200.so")
+TORCH_SRC = os.path.join(CSRC, "python", "torch_calls.cpp")
+TORCH_LIB = os.path.join(HERE, "_torch_calls.so")          # checks and allocations of the token-major calls, against torch
 LIB_DEBUG = os.path.join(HERE, "libubp_b200_debug.so")     # the checked build (-DUBP_DEBUG): same entry points
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 
@@ -34,6 +36,7 @@ def _stale(lib: str = LIB) -> bool:
 
 
 def build(force: bool = False, verbose: bool = False, debug: bool = False) -> str:
+    build_torch_calls(force)
     lib = LIB_DEBUG if debug else LIB
     if not force and not _stale(lib):
         return lib
@@ -60,6 +63,27 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
     subprocess.run([NVCC, "-shared", "-o", tmp] + objs + ["-gencode", "arch=compute_100a,code=sm_100a"], check=True)
     os.replace(tmp, lib)
     return lib
+
+
+def build_torch_calls(force: bool = False) -> str:
+    """The extension module of the token-major calls (host code only; no CUDA source in it)."""
+    deps = [TORCH_SRC, os.path.join(ROOT, "include", "ubp.h")]
+    if not force and os.path.exists(TORCH_LIB) and all(os.path.getmtime(TORCH_LIB) >= os.path.getmtime(d) for d in deps):
+        return TORCH_LIB
+    import sysconfig
+    import torch
+    base = os.path.join(os.path.dirname(torch.__file__))
+    inc = [os.path.join(base, "include"), os.path.join(base, "include", "torch", "csrc", "api", "include"),
+           os.path.join(os.path.dirname(os.path.dirname(NVCC)), "include"), sysconfig.get_paths()["include"]]
+    tmp = TORCH_LIB + f".tmp{os.getpid()}"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", TORCH_SRC, "-o", tmp,
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", os.path.join(ROOT, "include")]
+    for d in inc:
+        cmd += ["-isystem", d]
+    cmd += ["-L", os.path.join(base, "lib"), "-Wl,--no-as-needed", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"]
+    subprocess.run(cmd, check=True)
+    os.replace(tmp, TORCH_LIB)
+    return TORCH_LIB
 
 
 if __name__ == "__main__":
