@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from linear_ref import F8, TINY, UNIT, make_weight, product64, quantise, typed_weight
+from linear_ref import F8, TINY, UNIT, act64, make_weight, product64, quantise, typed_weight
 
 pytestmark = pytest.mark.gpu
 
@@ -84,6 +84,28 @@ def test_activations(ubp, act, T):
     for gated in (False, True):
         for dtype, out in ((BF16, BF16), (F16, F16), (F8, F16), (F8, F32)):
             check(ubp, W, mask, 4, T, dtype, out, act=act, gated=gated, seed=21)
+
+
+@pytest.mark.parametrize("act", ["none", "relu", "gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("T", [1, 40, 300])
+def test_activations_at_the_ends_of_the_range(ubp, act, T):
+    """Arguments up to the largest finite ones, +infinity and NaN (handed in as biases): 0 far below, v far above, NaN stays NaN."""
+    a = [1e-30, 1e-3, 0.7, 3.0, 5.5, 9.0, 13.0, 50.0, 86.0, 87.5, 89.0, 200.0, 1e4, 1e20, 3e38]
+    v = torch.tensor([0.0] + a + [-k for k in a] + [float("inf"), float("nan")], device="cuda")
+    M = v.numel() + 1
+    W, mask = make_weight(M, 64, 4, 50, 5)
+    b = torch.cat([v, v.new_zeros(1)])
+    x = torch.zeros(T, 64, device="cuda", dtype=F16)
+    y = ubp.ubp_linear(ubp.LinearPlan(ubp.ubp_pack(W, mask, 4), F16), x, bias=b, activation=act, out=torch.empty(T, M, device="cuda"))
+    v64 = b.double()
+    want = act64(v64, act)
+    if act != "none":
+        want = torch.where(v64 < -80, torch.zeros_like(want), want)
+    d = 2.0 ** -18 * torch.where(v64 < -80, v64.new_tensor(1e-20), v64.abs()) if act != "none" else torch.zeros_like(want)
+    for row in y.double():
+        assert row[v.numel() - 1].isnan() and row[v.numel() - 2].item() == float("inf")
+        f = torch.isfinite(v64)
+        assert ((row - want)[f].abs() <= d[f]).all(), (act, v64[f][((row - want)[f].abs() > d[f])])
 
 
 @pytest.mark.parametrize("T", [1, 4, 70, 300])
