@@ -15,7 +15,7 @@
 // boundary, else on single elements. The grid stays on the SMs and walks the rows; a row's loads are issued before the
 // statistics of the row before it are reduced, so that the reduction's two barrier-and-shuffle latencies and the stores pass
 // under loads in flight (one row per block without that: 103 us instead of 61 for rows 8192 x 16384, HBM 45 % busy).
-// Rows that do not fit the registers of 512 threads are read twice (the second time from L2): there nothing is written before
+// Rows that do not fit the registers of a block are read twice (the second time from L2): there nothing is written before
 // the row's statistics are complete. Every element is read and written by one thread, so h may be written over x or r in
 // every form.
 #include <cuda_runtime.h>
@@ -125,7 +125,7 @@ __global__ void __launch_bounds__(rows_block(TPR), rows_blocks_per_sm(TPR, NORM,
 {
     constexpr bool Q = sizeof(TO) == 1;
     constexpr int STEP = TPR * E, ROWS = rows_block(TPR) / TPR;
-    __shared__ float2 scratch[2][16];
+    __shared__ float2 scratch[2][32];
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const int lane = threadIdx.x % TPR, c0 = lane * E;
@@ -272,7 +272,11 @@ int launch_rows_k(const RowArgs &a, int sms, cudaStream_t stream)
 }
 
 // Threads and accesses a row by its length alone: the fewest threads whose registers hold it, 32 (a warp a row, no barrier),
-// 128 or 512.
+// 128 and more. Single elements cost their instructions, idle places too, and two to four rows an SM have to be under way:
+// hence the close steps there. f16 rows, 1531 of them, on single elements, norm / 8-bit rows: 2051 elements 9.7 / 5.5 us with
+// 256 threads (512 threads: 11.6 / 7.8), 4099 16.1 / 9.6 with 512 x 10 (512 x 16, whose registers spill: 28.5 / 16.8), 8191
+// 35.6 / 15.5 with 1024 x 8 (512 x 16: 50.5 / 19.9), 9001 37.7 / 19.1 with 1024 x 10 (read twice: 45.6 / 25.9). At 16 places of
+// 1024 threads reading twice is faster again (12001: rows 33.6 / 44.5).
 template <typename T, typename TO, bool NORM>
 int launch_rows_t(const RowArgs &a, bool vec, cudaStream_t st)
 {
@@ -291,8 +295,11 @@ int launch_rows_t(const RowArgs &a, bool vec, cudaStream_t st)
     }
     if (a.C <= 256) return launch_rows_k<T, TO, NORM, 1, 32, 8>(a, sms, st);
     if (a.C <= 1024) return launch_rows_k<T, TO, NORM, 1, 128, 8>(a, sms, st);
+    if (a.C <= 2560) return launch_rows_k<T, TO, NORM, 1, 256, 10>(a, sms, st);
     if (a.C <= 4096) return launch_rows_k<T, TO, NORM, 1, 512, 8>(a, sms, st);
-    if (a.C <= 8192) return launch_rows_k<T, TO, NORM, 1, 512, 16>(a, sms, st);
+    if (a.C <= 5120) return launch_rows_k<T, TO, NORM, 1, 512, 10>(a, sms, st);
+    if (a.C <= 8192) return launch_rows_k<T, TO, NORM, 1, 1024, 8>(a, sms, st);
+    if (a.C <= 10240) return launch_rows_k<T, TO, NORM, 1, 1024, 10>(a, sms, st);
     return launch_rows_k<T, TO, NORM, 1, 512, 0>(a, sms, st);
 }
 
