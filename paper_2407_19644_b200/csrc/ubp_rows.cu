@@ -180,7 +180,69 @@ __global__ void __launch_bounds__(rows_block(TPR), rows_blocks_per_sm(TPR, NORM,
 
     // (rows of one block differ by less than ROWS, so all its threads make the same number of rounds)
     const int64_t rounds = ((int64_t)blockIdx.x * ROWS < a.T) ? (a.T - (int64_t)blockIdx.x * ROWS + stride - 1) / stride : 0;
-    if constexpr (NV > 0) {
+    if constexpr (NV > 0 && E == 1) {
+        // Single elements: whole loops under one condition each and no branch an element (with the conditions inside it was 61
+        // instructions an element, which bound the kernel: norm 1531 x 2051 9.7 us, now 7.4). Places past the row stay 0 and count for nothing; gamma stays in
+        // registers from row to row.
+        Raw<T, 1> nx[NV], nr[NORM ? NV : 1];
+        float g[NORM ? NV : 1];
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            nx[k].w = from_f32<T>(0.f);
+            if constexpr (NORM) {
+                nr[k].w = from_f32<T>(0.f);
+                g[k] = c0 + k * STEP < a.C ? gamma1<T>(a, c0 + k * STEP) : 0.f;
+            }
+        }
+        auto fetch = [&](int64_t t) {
+            if (t >= a.T) return;
+            const T *p = x + t * a.ldx;
+#pragma unroll
+            for (int k = 0; k < NV; ++k)
+                if (c0 + k * STEP < a.C) nx[k].load(p + k * STEP);
+            if (has_r) {
+                p = r + t * a.ldr;
+#pragma unroll
+                for (int k = 0; k < NV; ++k)
+                    if (c0 + k * STEP < a.C) nr[NORM ? k : 0].load(p + k * STEP);
+            }
+        };
+        fetch(row);
+        for (int64_t i = 0; i < rounds; ++i, row += stride) {
+            const bool live = row < a.T;
+            float v[NV];
+            sum = 0.f; mx = 0.f;
+#pragma unroll
+            for (int k = 0; k < NV; ++k) v[k] = to_f32<T>(nx[k].w);
+            if (has_r) {
+#pragma unroll
+                for (int k = 0; k < NV; ++k) v[k] += to_f32<T>(nr[NORM ? k : 0].w);
+            }
+            if (has_h && live) {
+                T *p = h + row * a.ldh;
+#pragma unroll
+                for (int k = 0; k < NV; ++k)
+                    if (c0 + k * STEP < a.C) p[k * STEP] = from_f32<T>(v[k]);
+            }
+#pragma unroll
+            for (int k = 0; k < NV; ++k) {
+                if (NORM) { sum = fmaf(v[k], v[k], sum); v[k] *= g[NORM ? k : 0]; }
+                if (Q) mx = max_nan(mx, fabsf(v[k]));
+            }
+            fetch(row + stride);
+            row_reduce<NORM, Q, TPR>(sum, mx, scratch[i & 1]);
+            finish(live);
+            if (live) {
+                TO *p = y + row * a.ldy;
+#pragma unroll
+                for (int k = 0; k < NV; ++k) {
+                    float o = NORM ? v[k] * rinv : v[k];
+                    if (Q) o *= sinv;
+                    if (c0 + k * STEP < a.C) p[k * STEP] = from_f32<TO>(o);
+                }
+            }
+        }
+    } else if constexpr (NV > 0) {
         Raw<T, E> nx[NV], nr[NORM ? NV : 1];
         auto fetch = [&](int64_t t) {
 #pragma unroll
@@ -271,12 +333,15 @@ int launch_rows_k(const RowArgs &a, int sms, cudaStream_t stream)
     return UBP_OK;
 }
 
-// Threads and accesses a row by its length alone: the fewest threads whose registers hold it, 32 (a warp a row, no barrier),
-// 128 and more. Single elements cost their instructions, idle places too, and two to four rows an SM have to be under way:
-// hence the close steps there. f16 rows, 1531 of them, on single elements, norm / 8-bit rows: 2051 elements 9.7 / 5.5 us with
-// 256 threads (512 threads: 11.6 / 7.8), 4099 16.1 / 9.6 with 512 x 10 (512 x 16, whose registers spill: 28.5 / 16.8), 8191
-// 35.6 / 15.5 with 1024 x 8 (512 x 16: 50.5 / 19.9), 9001 37.7 / 19.1 with 1024 x 10 (read twice: 45.6 / 25.9). At 16 places of
-// 1024 threads reading twice is faster again (12001: rows 33.6 / 44.5).
+// Threads and accesses a row by its length: the fewest threads whose registers hold it, 32 (a warp a row, no barrier), 128 and
+// more. On 16-byte accesses a row of 513 to 1024 or 2049 to 4096 elements takes four times the threads where the SMs hold every
+// row at once anyway (f16, norm / 8-bit rows: 3 x 1024 1.75 / 1.35 us, on 32 threads 2.5 / 1.54; 3000 x 1024 5.65 / 4.1 on 128,
+// 5.15 / 2.97 on 32; 3 x 4096 norm 2.2 on 512, 2.36 on 256; 16384 x 4096 79.5 / 54.5 on 512, 79.7 / 34.8 on 256).
+// Single elements cost their instructions, idle places too, and two to four rows an SM have to be under way: hence the close
+// steps there. f16, 1531 rows, norm / 8-bit rows: 2051 elements 9.7 / 5.5 us with 256 threads (512 threads: 11.6 / 7.8), 4099
+// 16.1 / 9.6 with 512 x 10 (512 x 16, whose registers spill: 28.5 / 16.8), 8191 35.6 / 15.5 with 1024 x 8 (512 x 16: 50.5 /
+// 19.9), 9001 37.7 / 19.1 with 1024 x 10 (read twice: 45.6 / 25.9). At 16 places of 1024 threads reading twice is faster again
+// (12001: rows 33.6 / 44.5). (Measured with branches an element; without them 7.4 / 4.3, 13.6 / 6.9, 30.0 / 13.7, 33.7 / 14.6.)
 template <typename T, typename TO, bool NORM>
 int launch_rows_t(const RowArgs &a, bool vec, cudaStream_t st)
 {
@@ -284,9 +349,15 @@ int launch_rows_t(const RowArgs &a, bool vec, cudaStream_t st)
     if (vec) {
         if (a.C <= 256) return launch_rows_k<T, TO, NORM, 8, 32, 1>(a, sms, st);
         if (a.C <= 512) return launch_rows_k<T, TO, NORM, 8, 32, 2>(a, sms, st);
-        if (a.C <= 1024) return launch_rows_k<T, TO, NORM, 8, 128, 1>(a, sms, st);
+        if (a.C <= 1024) {
+            if (a.T <= (int64_t)sms * rows_blocks_per_sm(128, NORM, 8, 1, (int)sizeof(T))) return launch_rows_k<T, TO, NORM, 8, 128, 1>(a, sms, st);
+            return launch_rows_k<T, TO, NORM, 8, 32, 4>(a, sms, st);
+        }
         if (a.C <= 2048) return launch_rows_k<T, TO, NORM, 8, 128, 2>(a, sms, st);
-        if (a.C <= 4096) return launch_rows_k<T, TO, NORM, 8, 512, 1>(a, sms, st);
+        if (a.C <= 4096) {
+            if (NORM && a.T <= (int64_t)sms * rows_blocks_per_sm(512, NORM, 8, 1, (int)sizeof(T))) return launch_rows_k<T, TO, NORM, 8, 512, 1>(a, sms, st);
+            return launch_rows_k<T, TO, NORM, 8, 256, 2>(a, sms, st);
+        }
         if (a.C <= 8192) return launch_rows_k<T, TO, NORM, 8, 512, 2>(a, sms, st);
         // (a norm of fp32 rows would need 32 + 64 registers for the row and the next one: read twice instead)
         if constexpr (!(NORM && sizeof(T) == 4))

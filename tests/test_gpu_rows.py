@@ -48,7 +48,8 @@ def check_q(q, s, y, tol):
 
 
 SHAPES = [(1, 1), (3, 7), (1, 4096), (5, 64), (7, 100), (33, 513), (200, 1024), (9, 2051), (4, 8192), (3, 16384), (2, 16392), (2, 40000), (2, 9001),
-          (1300, 1500), (3, 2560), (700, 2561), (2, 4097), (310, 5120), (310, 5121), (160, 8191), (150, 8193), (2, 10240), (2, 10241)]
+          (1300, 1500), (3, 2560), (700, 2561), (2, 4097), (310, 5120), (310, 5121), (160, 8191), (150, 8193), (2, 10240), (2, 10241),
+          (1300, 800), (5300, 1000), (310, 4000)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=["bf16", "f16", "f32"])
