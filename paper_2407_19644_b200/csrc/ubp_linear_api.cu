@@ -9,35 +9,57 @@
 
 namespace ubp {
 
-// Kernel and tile of a launch. Estimates in us, fitted to back-to-back launches on B200 (26 random layers of 256 .. 10000
-// rows and channels, bf16 and e4m3, 1, 2, 4, 8 rows an entry, 50 .. 90 % pruned, 1 .. 24 tokens; the kept blocks and the
-// dense form both timed; the choice costs 2 % on average over always taking the faster one, "eight tokens or fewer" 3.5 %):
+// Kernel and tile of a launch, by estimates in us that were fitted to back-to-back launches on B200.
 //   kept blocks   2.8 + (entries (24 + 6.6 t) + kept weights x 27 t) ns / 1000 over the SMs + 85 ns a thousand channels and
-//                 token, t = tokens a block takes: instruction-bound, in the entries and in the products
-//   dense, few    3.3 + 0.9 for a split reduction + 6.4 ns a KB of weights a block streams + 0.12 us a MB in all
-// From 17 tokens on (three blocks to a row range) the kept blocks lost everywhere. A call of the few-token kernel covers 256
-// tokens; with more (4096 x 4096, 384 tokens, 22.5 us) the pair kernel is as fast (22.2) and from 512 on faster. Its tile is
-// 128 rows wide while those tiles fit one round (8192 x 2048, 256 tokens: 14.1 us against 16.8), else 256 (384 tokens: 17.3
-// against 22.2).
+//                 token, t = tokens a block takes: instruction-bound, in the entries and in the products (26 random layers of
+//                 256 .. 10000 rows and channels, bf16 and e4m3, 1, 2, 4, 8 rows an entry, 50 .. 90 % pruned, 1 .. 24 tokens;
+//                 from 17 tokens on, three blocks to a row range, the kept blocks lost everywhere)
+//   few           2.9 + 0.55 for a split reduction + rounds x (chunks a block takes (0.15 + 0.0008 n) + 0.023 n) + 0.052 a MB
+//                 of weights, n = tokens of a tile: bound by what the copies bring a block, 16 KB + 128 n bytes a chunk
+//   many          4.2 / 5.2 + rounds x (chunks x 0.233 / 0.26 + 2.1 / 4.6) for tiles of 128 / 256 rows, + 0.02 a MB of weights;
+//                 a round after the first starts under the one before it: 0.022 / 0.043 a chunk less
+// (The dense forms: 60 layers of 256 .. 18000 rows, 256 .. 8192 channels, bf16 and e4m3, 8 .. 5600 tokens, 1200 launches,
+// error 7 and 11 %. Choosing by them costs 1 % on average over the best of all tiles and splits. A few-token tile of all
+// tokens up to 256 and the pair kernel beyond cost 10 %: 512 x 5000, 1024 tokens, 24.4 us where 128 tokens x 4 parts take 12.1;
+// 2048 x 8192, 24 tokens, 16.3 in 8 parts, two rounds, where 4 parts take 11.0.)
+// A round is what the SMs hold at once: clusters of 2, 4, 8 blocks leave 0, 16, 28 of the 148 SMs without one
+// (cudaOccupancyMaxActiveClusters).
 LinearChoice linear_choose(const ubp_linear_plan *p, int64_t T, int sms)
 {
     const int b = p->dtype == UBP_E4M3 ? 1 : 2;
     const int rows = p->gated ? (p->F + 15) / 16 * 32 : p->M, rt = (rows + 127) / 128, nk = p->img.Kp * b / 128;
-    int S = 1;                       // split as far as the blocks find SMs and keep four chunks of the reduction each
-    while (S < 8 && rt * S * 2 <= sms && nk / (S * 2) >= 4) S *= 2;
+    const double mb = 128e-6 * rt * p->img.Kp * b;
+    LinearChoice best{LIN_MANY, 256, 0};
+    double least = 1e30;
+    auto offer = [&](double us, LinearChoice c) { if (us < least) { least = us; best = c; } };
+    for (int S = 1; S <= 8 && (S == 1 || nk >= 2 * S); S *= 2) {
+        const int64_t fit = (int64_t)sms * (S == 4 ? 132 : S == 8 ? 120 : 148) / 148, ranges = fit / ((int64_t)rt * S);
+        if (ranges == 0 && S > 1) break;
+        // as many token tiles as one round holds, of 64 tokens at least, all alike
+        int64_t n = (T + (ranges > 1 ? ranges : 1) - 1) / (ranges > 1 ? ranges : 1);
+        if (n < 64) n = T < 64 ? T : 64;
+        const int64_t ntt = (T + n - 1) / n;
+        n = ((T + ntt - 1) / ntt + 15) / 16 * 16;
+        if (n > 256) continue;
+        const double rounds = (double)((rt * ntt * S + fit - 1) / fit), chunks = (nk + S - 1) / S;
+        offer(2.9 + (S > 1 ? 0.55 : 0.0) + rounds * (chunks * (0.15 + 0.0008 * n) + 0.023 * n) + 0.052 * mb, {LIN_FEW, (int)n, S});
+    }
     if (T <= 16) {
         int t;
         int64_t nchunk;
         linear_sparse_tokens(p, T, &t, &nchunk);
         const double kept = (double)p->img.entries * p->img.nbk, share = (double)nchunk / sms;
-        const double sparse = 2.8 + ((double)p->img.entries * (24 + 6.6 * t) + kept * 27 * t) * share * 1e-6 + 85e-6 * p->C * t;
-        const double waves = (rt * S + sms - 1) / sms;
-        const double dense = 3.3 + (S > 1 ? 0.9 : 0.0) + 128.0 * p->img.Kp * b / S * waves * 6.4e-6 + 128e-6 * rt * p->img.Kp * b * 0.12;
-        if (sparse <= dense) return {LIN_SPARSE, t, 0};
+        offer(2.8 + ((double)p->img.entries * (24 + 6.6 * t) + kept * 27 * t) * share * 1e-6 + 85e-6 * p->C * t, {LIN_SPARSE, t, 0});
+    } else if (T > 64) {
+        for (int wide = 0; wide < 2; ++wide) {
+            const int nt = wide ? 256 : 128;
+            const double tiles = (double)((T + 255) / 256) * ((rows + nt - 1) / nt), pairs = sms / 2;
+            const double rounds = (double)(int64_t)((tiles + pairs - 1) / pairs), more = tiles > pairs ? tiles / pairs - 1 : 0;
+            offer((wide ? 5.2 : 4.2) + rounds * (nk * (wide ? 0.26 : 0.233) + (wide ? 4.6 : 2.1)) + 0.02 * mb - more * nk * (wide ? 0.043 : 0.022),
+                  {LIN_MANY, nt, 0});
+        }
     }
-    if (T <= 256) return {LIN_FEW, (int)((T + 15) / 16 * 16), S};
-    const int64_t t128 = ((T + 255) / 256) * ((rows + 127) / 128);
-    return {LIN_MANY, t128 <= sms / 2 ? 128 : 256, 0};
+    return best;
 }
 
 // SMs of the current device (asked once per device)

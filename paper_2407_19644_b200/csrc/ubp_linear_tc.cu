@@ -3,7 +3,9 @@
 // (8-bit) values of a row = one 128-byte line = a "chunk", four MMAs of 32 bytes each. TMA brings the lines, out-of-range
 // rows and channels as zeros.
 //
-// ubp_linear_few_kernel -- up to some hundred tokens: bound by reading the dense weight (HBM), so every SM has to stream.
+// ubp_linear_few_kernel -- up to some hundred tokens, and more of them where the pair kernel's large tiles would leave SMs
+//   idle (777 tokens x 1500 x 1003: 120 blocks, 12.2 us; 48 pairs 14.7): bound by reading the dense weight, so every SM has to
+//   stream.
 //   The weight is the A operand (128 rows of it per block: with tokens as A the tensor core would read 128 mostly empty
 //   rows per MMA for a handful of weight rows), the tokens are B (N = tokens rounded up to 16). S blocks of a cluster split
 //   the reduction; partial sums meet in distributed shared memory, and rank k finishes its share of the tokens.
