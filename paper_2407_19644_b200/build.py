@@ -80,7 +80,7 @@ def build_torch_calls(force: bool = False) -> str:
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", os.path.join(ROOT, "include")]
     for d in inc:
         cmd += ["-isystem", d]
-    cmd += ["-L", os.path.join(base, "lib"), "-Wl,--no-as-needed", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_python"]
+    cmd += ["-L", os.path.join(base, "lib"), "-Wl,--no-as-needed", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python"]
     subprocess.run(cmd, check=True)
     os.replace(tmp, TORCH_LIB)
     return TORCH_LIB

@@ -1,12 +1,13 @@
 // Argument checks and output allocation of the token-major calls (ubp_rmsnorm, ubp_quant_rows, ubp_linear), compiled against
 // torch: a call on one token is bound by the host, and marshalling it in Python costs as much as the launch (a product 8.2 us a
-// call through ctypes, of which the library's own part is 3.8; 4.2 here; a norm with 8-bit rows 13.3 and 5.8). The library is still reached through its C
+// call through ctypes, of which the library's own part is 3.8; 4.4 here; a norm with 8-bit rows 13.3 and 5.6). The library is still reached through its C
 // ABI: bind() receives the addresses of its entry points, so that whichever build of it the package loaded is the one that runs.
 // A call returns its outputs, or the library's negative status; refusals of arguments raise ValueError.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Dtype.h>
@@ -85,28 +86,32 @@ X activations(const at::Tensor *x)
     return r;
 }
 
-// the stream a call runs on: the caller's handle, or the device's current stream
+// The stream a call runs on: the caller's handle, or the device's current stream. A given stream is the current one while the
+// call allocates: memory that the allocator has handed back from another stream may still be in use there.
 struct On {
     c10::cuda::OptionalCUDAGuard guard;
+    c10::cuda::OptionalCUDAStreamGuard current;
     void *stream;
     On(int dev, PyObject *given) : guard(c10::Device(c10::kCUDA, (c10::DeviceIndex)dev))
     {
+        const auto d = (c10::DeviceIndex)dev;
         if (given != Py_None) {
             stream = PyLong_AsVoidPtr(given);
             if (!stream && PyErr_Occurred()) throw Refused();
+            current.reset_stream(stream ? c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(stream), d) : c10::cuda::getDefaultCUDAStream(d));
         } else {
-            stream = c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)dev).stream();
+            stream = c10::cuda::getCurrentCUDAStream(d).stream();
         }
     }
 };
 
 at::Tensor make(int64_t T, int64_t C, at::ScalarType type, int dev)
 {
-    return at::empty({T, C}, at::TensorOptions().dtype(type).device(c10::Device(c10::kCUDA, (c10::DeviceIndex)dev)));
+    return at::detail::empty_cuda({T, C}, type, c10::Device(c10::kCUDA, (c10::DeviceIndex)dev), std::nullopt);
 }
 at::Tensor make(int64_t T, at::ScalarType type, int dev)
 {
-    return at::empty({T}, at::TensorOptions().dtype(type).device(c10::Device(c10::kCUDA, (c10::DeviceIndex)dev)));
+    return at::detail::empty_cuda({T}, type, c10::Device(c10::kCUDA, (c10::DeviceIndex)dev), std::nullopt);
 }
 
 // the given output, or a new tensor
@@ -248,7 +253,6 @@ PyObject *linear(PyObject *, PyObject *const *a, Py_ssize_t n)
         if (!ws && (nws = p_workspace(plan, px, ldx, T)) != 0) {
             room = make((int64_t)nws, at::kByte, dev);
             pw = room.data_ptr();
-            if (a[8] != Py_None) room.record_stream(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(on.stream), (c10::DeviceIndex)dev));
         }
         const int rc = p_linear(plan, px, ldx, (const float *)ps, T, (const float *)pb, (int)act, residual ? residual->data_ptr() : nullptr, ldr,
                                 out ? out->data_ptr() : y.data_ptr(), ldy, ydt, pw, nws, on.stream);

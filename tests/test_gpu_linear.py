@@ -149,6 +149,30 @@ def test_bad_token_stays_alone(ubp, T):
     assert got[1][touched].isnan().all()
 
 
+@pytest.mark.parametrize("pad", [0, 1])
+def test_outputs_on_a_given_stream(ubp, pad):
+    """A call on a given stream takes its outputs' (and its workspace's) memory from that stream: a block that the current
+    stream has freed may still be written there."""
+    W, mask = make_weight(1024, 1536, 4, 60, 8)
+    plan = ubp.LinearPlan(ubp.ubp_pack(W, mask, 4), BF16)
+    x = inputs(300, 1536, BF16, pad, 0, 5)[0]
+    gamma = torch.ones(1536, device="cuda", dtype=BF16)
+    calls = [lambda st: ubp.ubp_linear(plan, x, stream=st), lambda st: ubp.ubp_rmsnorm(x, gamma, stream=st)[0],
+             lambda st: ubp.ubp_quant_rows(x, stream=st)[0]]
+    st = torch.cuda.Stream()
+    for call in calls:
+        want = call(None)
+        torch.cuda.synchronize()
+        busy = [torch.empty(n, device="cuda", dtype=torch.uint8) for n in (want.nbytes, 300 * 1536 * 2)]
+        torch.cuda._sleep(20_000_000)                # some ten milliseconds, after which the freed blocks are written
+        for b in busy:
+            b.fill_(0xff)
+        del busy, b
+        got = call(st)
+        torch.cuda.synchronize()
+        assert torch.equal(got.view(torch.uint8), want.view(torch.uint8))
+
+
 @pytest.mark.parametrize("T", [2, 100])
 def test_other_stream_and_no_tokens(ubp, T):
     W, mask = make_weight(256, 320, 4, 60, 8)
