@@ -13,7 +13,7 @@
 // coalesced 512-byte load of weights, one of channels, and no test; the lanes' sums join once a bundle. The weights are
 // constants of the layer, so the first steps are loaded before the kernel waits for the one before it, and the next steps'
 // loads are always under way. Forms that were measured before this one, us for a token on 4096 x 4096 at 80 % bf16 /
-// 16384 x 4096 gated e4m3 (this: 3.75 / 7.5): a group of lanes per row in the canonical order, four blocks of a cluster to a
+// 16384 x 4096 gated e4m3 (this: 3.65 / 6.4): a group of lanes per row in the canonical order, four blocks of a cluster to a
 // reduction, 6.9 / 20.4 (chains of dependent loads); a ring of bulk copies in shared memory, 6.7 / 14.0 (a stage holds too few
 // rows for the warps, and its barriers add up); equal shares of the canonical stream to groups of lanes, 5.6 / 12.6 (170
 // instructions a chunk, most of them for finding rows).
@@ -32,8 +32,7 @@
 namespace ubp {
 namespace {
 
-constexpr int SP_THREADS = 512;
-constexpr int SP_WARPS = SP_THREADS / 32;
+constexpr int SP_THREADS = 512;       // and twice that for large layers, see launch_linear_sparse
 constexpr int SP_MAX_TOKENS = 8;      // tokens per block (more tokens: further blocks)
 constexpr size_t SP_X = 128 * 1024;   // staged activations at most (fewer tokens per block where a row is long)
 constexpr size_t SP_SMEM = 224 * 1024;
@@ -46,6 +45,7 @@ struct SpArgs {
     const uint8_t *val;
     int lanes;                        // lanes per start row
     int grid, ydt;
+    bool wide;                        // twice the threads
 };
 
 struct F8 {};                         // 8-bit weights (staged activations are f16)
@@ -102,13 +102,41 @@ __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
     return r;
 }
 
+// a * b + c of two 16-bit values and an fp32 sum (the product is not rounded)
+template <typename X> __device__ __forceinline__ float fma_mixed(uint16_t a, uint16_t b, float c)
+{
+    float d;
+    if constexpr (std::is_same<X, __half>::value) asm("fma.rn.f32.f16 %0, %1, %2, %3;" : "=f"(d) : "h"(a), "h"(b), "f"(c));
+    else asm("fma.rn.f32.bf16 %0, %1, %2, %3;" : "=f"(d) : "h"(a), "h"(b), "f"(c));
+    return d;
+}
+// weight i of a chunk as 16 bits (8-bit codes: f16, which holds every one of them)
+template <typename W> struct Chunk16 {
+    uint32_t w[8 / wsize<W>];
+    __device__ __forceinline__ explicit Chunk16(const uint4 &c)
+    {
+        const uint32_t r[4] = {c.x, c.y, c.z, c.w};
+        if constexpr (std::is_same<W, F8>::value) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = e4m3x2_to_f16x2(r[i >> 1] >> (16 * (i & 1)));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = r[i];
+        }
+    }
+    __device__ __forceinline__ uint16_t at(int i) const { return (uint16_t)(w[i / 2] >> (16 * (i & 1))); }
+};
+
 // Steps a lane has in flight beside the ones it works on, and blocks of a kernel an SM should have room for: a step is four
 // registers of weights and epc / 2 of channels, twice; two blocks (one of the kernel before) have 64 registers a thread.
 __host__ __device__ constexpr int sp_unroll(int nacc, int epc) { return (nacc <= 8 && epc <= 2) || (nacc <= 4 && epc <= 4) ? 4 : 2; }
 __host__ __device__ constexpr int sp_blocks(int nacc, int epc) { return nacc <= 8 && epc <= 8 ? 2 : 1; }
+// a block of twice the threads has 64 registers a thread too: no more sums than fit
+__host__ __device__ constexpr bool sp_wide(int nacc) { return nacc <= 32; }
 
-template <typename W, int NBK, int TT>
-__global__ void __launch_bounds__(SP_THREADS, sp_blocks(NBK * TT, 16 / (NBK * wsize<W>))) ubp_linear_sparse_kernel(const SpArgs p)
+template <typename W, int NBK, int TT, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS > SP_THREADS ? 1 : sp_blocks(NBK * TT, 16 / (NBK * wsize<W>)))
+ubp_linear_sparse_kernel(const SpArgs p)
 {
     using X = typename XOf<W>::type;
     constexpr int NACC = NBK * TT, EPC = 16 / (NBK * wsize<W>);     // accumulators of a start row; entries of a chunk
@@ -159,7 +187,7 @@ __global__ void __launch_bounds__(SP_THREADS, sp_blocks(NBK * TT, 16 / (NBK * ws
         const uint8_t *x = static_cast<const uint8_t *>(a.x) + t0 * a.ldx * xb;
         if (TT == 1 && reinterpret_cast<uintptr_t>(x) % (8 * xb) == 0) {
             // one token: eight channels a thread
-            for (int c = 8 * (int)threadIdx.x; c < a.C; c += 8 * SP_THREADS) {
+            for (int c = 8 * (int)threadIdx.x; c < a.C; c += 8 * THREADS) {
                 if (c + 8 <= a.C) {
                     if constexpr (xb == 2) {
                         *reinterpret_cast<uint4 *>(xs + c) = *reinterpret_cast<const uint4 *>(x + (size_t)c * 2);
@@ -178,7 +206,7 @@ __global__ void __launch_bounds__(SP_THREADS, sp_blocks(NBK * TT, 16 / (NBK * ws
             // two channels a thread
             const bool pair = (reinterpret_cast<uintptr_t>(x) % (2 * xb) == 0) && (a.ldx * xb) % (2 * xb) == 0;
 #pragma unroll 4
-            for (int c = 2 * (int)threadIdx.x; c < a.C; c += 2 * SP_THREADS) {
+            for (int c = 2 * (int)threadIdx.x; c < a.C; c += 2 * THREADS) {
                 const bool two = c + 1 < a.C;
                 uint32_t v[TT];                                     // two channels of token t as two 16-bit values
 #pragma unroll
@@ -232,7 +260,7 @@ __global__ void __launch_bounds__(SP_THREADS, sp_blocks(NBK * TT, 16 / (NBK * ws
         uint32_t ns = s + U, ns1 = s1;
         int ntask_ = task;
         if (ns >= s1) {
-            ntask_ += SP_WARPS;
+            ntask_ += (THREADS / 32);
             ns = ns1 = 0;
             if (ntask_ < ntask) { ns = __ldg(p.off + bundle_of(ntask_)); ns1 = __ldg(p.off + bundle_of(ntask_) + 1); }
         }
@@ -241,20 +269,20 @@ __global__ void __launch_bounds__(SP_THREADS, sp_blocks(NBK * TT, 16 / (NBK * ws
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (s + u >= s1) break;
-            float wt[16 / wsize<W>];
-            unpack_chunk<W>(cur.val[u], wt);
+            float wt[TT == 1 ? 1 : 16 / wsize<W>];
+            const Chunk16<W> w16(cur.val[u]);
+            if constexpr (TT > 1) unpack_chunk<W>(cur.val[u], wt);
 #pragma unroll
             for (int e = 0; e < EPC; ++e) {
                 const uint32_t j = EPC == 1 ? cur.j[u][0] : (e & 1) ? cur.j[u][e / 2] >> 16 : cur.j[u][e / 2] & 0xffffu;
                 if (!UBP_CHK_SMEM((int)j < a.C, a.status)) continue;
                 const X *xp = xs + j * TT;
                 if constexpr (TT == 1) {
-                    const float x = to_f32<X>(*xp);
-                    if constexpr (NBK == 1) {
-                        acc2[0].x = fmaf(wt[e], x, acc2[0].x);
-                    } else {
+                    const uint16_t x = *reinterpret_cast<const uint16_t *>(xp);
 #pragma unroll
-                        for (int b = 0; b < NBK / 2; ++b) acc2[b] = fma2(make_float2(wt[e * NBK + 2 * b], wt[e * NBK + 2 * b + 1]), make_float2(x, x), acc2[b]);
+                    for (int b = 0; b < NBK; ++b) {
+                        float &v = (b & 1) ? acc2[b / 2].y : acc2[b / 2].x;
+                        v = fma_mixed<X>(w16.at(e * NBK + b), x, v);
                     }
                 } else {
                     uint32_t xw[TT / 2];
@@ -313,7 +341,7 @@ __global__ void __launch_bounds__(SP_THREADS, sp_blocks(NBK * TT, 16 / (NBK * ws
     }
     __syncthreads();
     // ---- output rows and epilogue: neighbouring threads hold neighbouring features
-    for (int i = threadIdx.x; i < nf * nt; i += SP_THREADS) {
+    for (int i = threadIdx.x; i < nf * nt; i += THREADS) {
         const int t = TT == 1 ? 0 : i / nf, f = i - t * nf;
         float z[2] = {0.f, 0.f};
 #pragma unroll
@@ -335,10 +363,10 @@ __global__ void __launch_bounds__(SP_THREADS, sp_blocks(NBK * TT, 16 / (NBK * ws
     }
 }
 
-template <typename W, int NBK, int TT>
-int launch_t(const SpArgs &p, int64_t chunks, size_t smem, cudaStream_t stream)
+template <typename W, int NBK, int TT, int THREADS>
+int launch_n(const SpArgs &p, int64_t chunks, size_t smem, cudaStream_t stream)
 {
-    const auto kern = ubp_linear_sparse_kernel<W, NBK, TT>;
+    const auto kern = ubp_linear_sparse_kernel<W, NBK, TT, THREADS>;
     static bool done[64] = {};
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) dev = -1;
@@ -349,7 +377,7 @@ int launch_t(const SpArgs &p, int64_t chunks, size_t smem, cudaStream_t stream)
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)p.grid, (unsigned)chunks);
-    cfg.blockDim = dim3(SP_THREADS);
+    cfg.blockDim = dim3(THREADS);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
@@ -361,6 +389,14 @@ int launch_t(const SpArgs &p, int64_t chunks, size_t smem, cudaStream_t stream)
     if (e == cudaSuccess) e = cudaGetLastError();
     if (e != cudaSuccess) { set_last_cuda_error((int)e); return UBP_E_CUDA; }
     return UBP_OK;
+}
+
+template <typename W, int NBK, int TT>
+int launch_t(const SpArgs &p, int64_t chunks, size_t smem, cudaStream_t stream)
+{
+    if constexpr (sp_wide(NBK * TT))
+        if (p.wide) return launch_n<W, NBK, TT, 2 * SP_THREADS>(p, chunks, smem, stream);
+    return launch_n<W, NBK, TT, SP_THREADS>(p, chunks, smem, stream);
 }
 
 template <typename W, int NBK>
@@ -417,7 +453,15 @@ int launch_linear_sparse(const ubp_linear_plan *pl, const LinearArgs &a, int y_d
     // the others. Large layers: as many rows as shared memory leaves room for.
     const int rb = 32 / pl->img.lanes;
     const int64_t fb = ((int64_t)a.F + rb - 1) / rb;
-    int64_t grid = (sms + nchunk - 1) / nchunk;
+    // A layer whose loads take long gains more from twice the loads under way on an SM than from the next launch's early start,
+    // from some 18 MB of kept weights on: two blocks an SM for a token and blocks of up to four rows, whose neighbours'
+    // recomputed start rows are few (bf16, blocks of 4: 25 MB 6.1 us, 6.8 with one, 6.6 with one of twice the threads; 15 MB
+    // 5.7, 5.1, 5.3), else a block of twice the threads (f16, blocks of 8, 45 MB: a token 11.0 us, 13.3 with 512 threads, 12.4
+    // with two blocks; two tokens 14.3, 19.9, 27; 4 tokens on the 25 MB 8.7, 10.5, 13.4).
+    const size_t kept = (size_t)pl->img.entries * (nbk * dtype_size(pl->dtype) + 2);
+    const bool large = kept >= ((size_t)18 << 20), two = large && TT == 1 && nbk <= 4 && nchunk == 1;
+    p.wide = large && !two;
+    int64_t grid = ((two ? 2 : 1) * sms + nchunk - 1) / nchunk;
     size_t smem;
     for (;; grid *= 2) {
         if (grid > fb) grid = fb;
