@@ -51,6 +51,7 @@ struct TcLinArgs {
     int rows;            // dense rows that hold the layer (M, or 2 x F rounded up to 16)
     int vec4;            // rows of y and of the residual are aligned to four elements
     int unaligned_bias;  // 1: bias is not 16-byte aligned
+    int group;           // pair kernel: token tiles that walk the features together
 };
 
 __device__ __forceinline__ uint64_t kmajor_desc(uint32_t saddr) { return make_desc(saddr, 16, 1024, LT_SWZ_128B); }
@@ -341,7 +342,11 @@ ubp_linear_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
 // ------------------------------------------------------------------ many tokens
 constexpr int MANY_STAGES = 6;
 constexpr uint32_t MANY_TURN = 32 * 32 * 4;      // staging of one epilogue warp
-constexpr int MANY_GROUP = 8;                    // token tiles that walk the features together (their lines stay in L2)
+// Token tiles that walk the features together: as many as keep 32 MB of activations in L2, eight at least. Sustained, 8 / 16 /
+// 32 / 64 tiles: 8192 tokens x 16384 x 4096 e4m3 (1 MB a tile) 439 / 432 / 428 / 428 us; 16384 x 8192 x 2048 bf16 (1 MB) 417 /
+// 411 / 410 / 445; 8192 x 4096 x 4096 bf16 (2 MB) 207 / 207 / 223 / 223; 8192 x 4096 x 8192 bf16 (4 MB) 423 / 431.
+constexpr int64_t MANY_GROUP_BYTES = 32 << 20;
+constexpr int MANY_GROUP_LEAST = 8;
 __host__ __device__ constexpr uint32_t many_stage(int nt) { return 128 * LT_LINE + (uint32_t)(nt / 2) * LT_LINE; }
 
 // One warp's 32 tokens x 32 values -> y, with the residual. E elements an access (8, 4, 2 or 1: what the rows of y and of the
@@ -438,10 +443,10 @@ ubp_linear_many_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
     const int nmy = pair < ntiles ? (ntiles - pair + npairs - 1) / npairs : 0;
     const int line = F8 ? 128 : 64;
     auto tile_at = [&](int i, int &m, int &n) {
-        const int t = pair + i * npairs, per = MANY_GROUP * ntn, g = t / per, r = t - g * per;
-        const int gm = ntm - g * MANY_GROUP < MANY_GROUP ? ntm - g * MANY_GROUP : MANY_GROUP;
+        const int t = pair + i * npairs, per = p.group * ntn, g = t / per, r = t - g * per;
+        const int gm = ntm - g * p.group < p.group ? ntm - g * p.group : p.group;
         n = r / gm;
-        m = g * MANY_GROUP + (r - n * gm);
+        m = g * p.group + (r - n * gm);
     };
 
     if (threadIdx.x == 0) {
@@ -798,6 +803,8 @@ int launch_linear_tc(const ubp_linear_plan *pl, const LinearArgs &args, int y_dt
     p.ydt = y_dtype;
     p.nk = pl->img.Kp * b / LT_LINE;
     p.unaligned_bias = (reinterpret_cast<uintptr_t>(args.bias) & 15) != 0;
+    const int64_t group = MANY_GROUP_BYTES / ((int64_t)256 * pl->img.Kp * b);
+    p.group = (int)(group > MANY_GROUP_LEAST ? group : MANY_GROUP_LEAST);
     p.rows = pl->gated ? (pl->F + 15) / 16 * 32 : pl->M;
     if (args.T > 0x7fffffff) return UBP_E_UNSUPPORTED;
     const uintptr_t ob = (uintptr_t)(y_dtype == UBP_F32 ? 4 : 2);
