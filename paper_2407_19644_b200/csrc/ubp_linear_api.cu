@@ -31,6 +31,7 @@ LinearChoice linear_choose(const ubp_linear_plan *p, int64_t T, int sms)
     const int b = p->dtype == UBP_E4M3 ? 1 : 2;
     const int rows = p->gated ? (p->F + 15) / 16 * 32 : p->M, rt = (rows + 127) / 128, nk = p->img.Kp * b / 128;
     const double mb = 128e-6 * rt * p->img.Kp * b;
+    if (T < 1) T = 1;                // (asked for no tokens: as for one)
     LinearChoice best{LIN_MANY, 256, 0};
     double least = 1e30;
     auto offer = [&](double us, LinearChoice c) { if (us < least) { least = us; best = c; } };

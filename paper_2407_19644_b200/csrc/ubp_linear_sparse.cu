@@ -36,6 +36,7 @@ constexpr int SP_THREADS = 512;       // and twice that for large layers, see la
 constexpr int SP_MAX_TOKENS = 8;      // tokens per block (more tokens: further blocks)
 constexpr size_t SP_X = 128 * 1024;   // staged activations at most (fewer tokens per block where a row is long)
 constexpr size_t SP_SMEM = 224 * 1024;
+constexpr int SP_TWO_C = 48 * 1024;   // channels of a token that leave room for a second block on the SM
 
 struct SpArgs {
     LinearArgs a;
@@ -459,7 +460,7 @@ int launch_linear_sparse(const ubp_linear_plan *pl, const LinearArgs &a, int y_d
     // 5.7, 5.1, 5.3), else a block of twice the threads (f16, blocks of 8, 45 MB: a token 11.0 us, 13.3 with 512 threads, 12.4
     // with two blocks; two tokens 14.3, 19.9, 27; 4 tokens on the 25 MB 8.7, 10.5, 13.4).
     const size_t kept = (size_t)pl->img.entries * (nbk * dtype_size(pl->dtype) + 2);
-    const bool large = kept >= ((size_t)18 << 20), two = large && TT == 1 && nbk <= 4 && nchunk == 1;
+    const bool large = kept >= ((size_t)18 << 20), two = large && TT == 1 && nbk <= 4 && nchunk == 1 && pl->C <= SP_TWO_C;
     p.wide = large && !two;
     int64_t grid = ((two ? 2 : 1) * sms + nchunk - 1) / nchunk;
     size_t smem;

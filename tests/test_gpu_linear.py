@@ -189,7 +189,7 @@ def test_other_stream_and_no_tokens(ubp, T):
     got = ubp.ubp_linear(plan, x, bias=b, residual=r, stream=st)
     st.synchronize()
     assert torch.equal(got, y)
-    assert ubp.ubp_linear(plan, x[:0]).shape == (0, 256)
+    assert ubp.ubp_linear(plan, x[:0]).shape == (0, 256) and plan.choice(0) == plan.choice(1)
 
 
 def test_row_scales(ubp):
@@ -248,10 +248,10 @@ def test_refusals(ubp):
         ubp.ubp_linear(plan, x)
 
 
-#: (tokens, rows, input features, block rows, sparsity, kernel and tile the call has to take): every kernel and tile once, on
-#: every kernel and tile: (0, tokens a block), (1, tokens of a tile, parts of the reduction), (2, rows of a tile)
+#: (tokens, rows, input features, block rows, sparsity, what the call has to take): every kernel and tile,
+#: (0, tokens a block), (1, tokens of a tile, parts of the reduction), (2, rows of a tile)
 PATHS = [(1, 2048, 2048, 4, 0, (0, 1)), (2, 2048, 2048, 4, 60, (0, 2)), (3, 2048, 2048, 4, 80, (0, 4)), (8, 2048, 2048, 4, 90, (0, 8)),
-         (1, 9000, 6000, 2, 70, (0, 1)), (1, 6000, 6000, 8, 70, (0, 1)), (2, 9000, 6000, 4, 70, (0, 2)), (4, 6000, 6000, 8, 70, (0, 4)),
+         (1, 9000, 6000, 2, 70, (0, 1)), (1, 6000, 6000, 8, 70, (0, 1)), (1, 400, 50000, 2, 50, (0, 1)), (2, 9000, 6000, 4, 70, (0, 2)), (4, 6000, 6000, 8, 70, (0, 4)),
          (16, 512, 512, 8, 95, (0, 8)), (16, 2048, 2048, 4, 0, (1, 16, 4)), (20, 300, 3000, 2, 70, (1, 32, 8)), (77, 4000, 260, 4, 70, (1, 48, 1)),
          (256, 130, 600, 4, 70, (1, 64, 4)), (257, 130, 600, 4, 70, (1, 64, 4)), (777, 770, 1000, 4, 70, (1, 80, 2)), (1000, 4000, 260, 4, 70, (1, 256, 1)),
          (2600, 1030, 70, 2, 60, (1, 176, 1)), (5000, 300, 3000, 4, 70, (1, 224, 2)), (2100, 4100, 96, 4, 80, (2, 128)), (5000, 1030, 70, 2, 60, (2, 128)),
