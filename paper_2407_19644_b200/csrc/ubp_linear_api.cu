@@ -10,11 +10,11 @@
 namespace ubp {
 
 // Kernel and tile of a launch, by estimates in us that were fitted to back-to-back launches on B200.
-//   kept blocks   2.4 + (entries x 2.3 t + kept weights (64 + 4.8 t) + rows (4400 + 700 b t)) / 10^6 over the SMs + 106 a
-//                 million channels and token; t = tokens a block takes, b = rows of an entry: instructions for the entries, the
+//   kept blocks   2.4 + (entries x 10 t + kept weights x 70 + rows (1000 + 700 b t)) / 10^6 over the SMs + 100 a million
+//                 channels and token; t = tokens a block takes, b = rows of an entry: instructions for the entries, the
 //                 products and the joining of a row's sums (40 random layers of 256 .. 16000 rows, 256 .. 8192 channels, all
-//                 types, blocks of 2 .. 16 rows, 50 .. 90 % pruned, 1 .. 16 tokens: error 10 %; choosing by it costs 1.1 % on
-//                 average over the faster of the two forms, the dense form always 19 %, the kept blocks always 15 %). From 17
+//                 types, blocks of 2 .. 16 rows, 50 .. 90 % pruned, 1 .. 16 tokens: error 11 %; choosing by it costs 1.3 % on
+//                 average over the faster of the two forms, the dense form always 20 %, the kept blocks always 13 %). From 17
 //                 tokens on, three blocks to a row range, the kept blocks lost everywhere.
 //   few           2.9 + 0.55 for a split reduction + rounds x (chunks a block takes (0.15 + 0.0008 n) + 0.023 n) + 0.052 a MB
 //                 of weights, n = tokens of a tile: bound by what the copies bring a block, 16 KB + 128 n bytes a chunk
@@ -52,8 +52,8 @@ LinearChoice linear_choose(const ubp_linear_plan *p, int64_t T, int sms)
         int64_t nchunk;
         linear_sparse_tokens(p, T, &t, &nchunk);
         const double e = (double)p->img.entries, nbk = p->img.nbk;
-        const double ns = e * 2.3 * t + e * nbk * (64 + 4.8 * t) + (double)p->M * (4400 + 700 * nbk * t);
-        offer(2.4 + ns * (double)nchunk / sms * 1e-6 + 106e-6 * p->C * t, {LIN_SPARSE, t, 0});
+        const double ns = e * 10 * t + e * nbk * 70 + (double)p->M * (1000 + 700 * nbk * t);
+        offer(2.4 + ns * (double)nchunk / sms * 1e-6 + 100e-6 * p->C * t, {LIN_SPARSE, t, 0});
     } else if (T > 64) {
         for (int wide = 0; wide < 2; ++wide) {
             const int nt = wide ? 256 : 128;

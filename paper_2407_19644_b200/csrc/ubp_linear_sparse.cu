@@ -54,24 +54,6 @@ template <typename W> struct XOf { using type = W; };
 template <> struct XOf<F8> { using type = __half; };
 template <typename W> constexpr int wsize = std::is_same<W, F8>::value ? 1 : 2;
 
-// the 32-bit words of one chunk -> its weights, fp32
-template <typename W> __device__ __forceinline__ void unpack_chunk(const uint4 &c, float (&w)[16 / wsize<W>])
-{
-    const uint32_t r[4] = {c.x, c.y, c.z, c.w};
-    if constexpr (std::is_same<W, F8>::value) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float2 f = unpack2<__half>(e4m3x2_to_f16x2(r[i >> 1] >> (16 * (i & 1))));
-            w[2 * i] = f.x; w[2 * i + 1] = f.y;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 f = unpack2<W>(r[i]);
-            w[2 * i] = f.x; w[2 * i + 1] = f.y;
-        }
-    }
-}
 // EPC 16-bit channel numbers of a chunk, two a word (aligned to their size up to 16 bytes)
 template <int EPC> __device__ __forceinline__ void load_channels(const uint16_t *p, uint32_t (&j)[EPC > 1 ? EPC / 2 : 1])
 {
@@ -90,19 +72,6 @@ template <int EPC> __device__ __forceinline__ void load_channels(const uint16_t 
         }
     }
 }
-// two fp32 multiply-adds in one instruction
-__device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
-{
-    unsigned long long x, y, z, d;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(a.x), "f"(a.y));
-    asm("mov.b64 %0, {%1, %2};" : "=l"(y) : "f"(b.x), "f"(b.y));
-    asm("mov.b64 %0, {%1, %2};" : "=l"(z) : "f"(c.x), "f"(c.y));
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(x), "l"(y), "l"(z));
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(d));
-    return r;
-}
-
 // a * b + c of two 16-bit values and an fp32 sum (the product is not rounded)
 template <typename X> __device__ __forceinline__ float fma_mixed(uint16_t a, uint16_t b, float c)
 {
@@ -254,9 +223,9 @@ ubp_linear_sparse_kernel(const SpArgs p)
     __syncthreads();
 
     // ---- this warp's bundles
-    float2 acc2[NACC >= 2 ? NACC / 2 : 1];                          // pairs of accumulators: of two tokens, or of two rows for a single token
+    float acc[NACC];                                                // [row of the block][token]
 #pragma unroll
-    for (auto &v : acc2) v = make_float2(0.f, 0.f);
+    for (float &v : acc) v = 0.f;
     while (task < ntask) {
         uint32_t ns = s + U, ns1 = s1;
         int ntask_ = task;
@@ -270,42 +239,27 @@ ubp_linear_sparse_kernel(const SpArgs p)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (s + u >= s1) break;
-            float wt[TT == 1 ? 1 : 16 / wsize<W>];
-            const Chunk16<W> w16(cur.val[u]);
-            if constexpr (TT > 1) unpack_chunk<W>(cur.val[u], wt);
+            const Chunk16<W> w(cur.val[u]);
 #pragma unroll
             for (int e = 0; e < EPC; ++e) {
                 const uint32_t j = EPC == 1 ? cur.j[u][0] : (e & 1) ? cur.j[u][e / 2] >> 16 : cur.j[u][e / 2] & 0xffffu;
                 if (!UBP_CHK_SMEM((int)j < a.C, a.status)) continue;
                 const X *xp = xs + j * TT;
-                if constexpr (TT == 1) {
-                    const uint16_t x = *reinterpret_cast<const uint16_t *>(xp);
+                uint32_t xw[TT > 1 ? TT / 2 : 1];
+                if constexpr (TT == 1) xw[0] = *reinterpret_cast<const uint16_t *>(xp);
+                else if constexpr (TT == 2) xw[0] = *reinterpret_cast<const uint32_t *>(xp);
+                else if constexpr (TT == 4) { const uint2 v = *reinterpret_cast<const uint2 *>(xp); xw[0] = v.x; xw[1] = v.y; }
+                else { const uint4 v = *reinterpret_cast<const uint4 *>(xp); xw[0] = v.x; xw[1] = v.y; xw[2] = v.z; xw[3] = v.w; }
 #pragma unroll
-                    for (int b = 0; b < NBK; ++b) {
-                        float &v = (b & 1) ? acc2[b / 2].y : acc2[b / 2].x;
-                        v = fma_mixed<X>(w16.at(e * NBK + b), x, v);
-                    }
-                } else {
-                    uint32_t xw[TT / 2];
-                    if constexpr (TT == 2) xw[0] = *reinterpret_cast<const uint32_t *>(xp);
-                    else if constexpr (TT == 4) { const uint2 v = *reinterpret_cast<const uint2 *>(xp); xw[0] = v.x; xw[1] = v.y; }
-                    else { const uint4 v = *reinterpret_cast<const uint4 *>(xp); xw[0] = v.x; xw[1] = v.y; xw[2] = v.z; xw[3] = v.w; }
+                for (int b = 0; b < NBK; ++b)
 #pragma unroll
-                    for (int t = 0; t < TT / 2; ++t) {
-                        const float2 x = unpack2<X>(xw[t]);
-#pragma unroll
-                        for (int b = 0; b < NBK; ++b)
-                            acc2[b * (TT / 2) + t] = fma2(make_float2(wt[e * NBK + b], wt[e * NBK + b]), x, acc2[b * (TT / 2) + t]);
-                    }
-                }
+                    for (int t = 0; t < TT; ++t)
+                        acc[b * TT + t] = fma_mixed<X>(w.at(e * NBK + b), (uint16_t)(xw[t / 2] >> (16 * (t & 1))), acc[b * TT + t]);
             }
         }
         if (ntask_ != task) {
             // the bundle's last batch: join the lanes of each row. In the first three steps a lane keeps half of its sums and
             // hands over the other half as long as it has more than one.
-            float acc[NACC];
-#pragma unroll
-            for (int i = 0; i < NACC; ++i) acc[i] = (i & 1) ? acc2[i / 2].y : acc2[i / 2].x;
             int at = 0;
 #pragma unroll
             for (int o = 1, m = NACC; o < 8; o <<= 1) {
@@ -335,7 +289,7 @@ ubp_linear_sparse_kernel(const SpArgs p)
                 for (int i = 0; i < left; ++i) dst[i] = acc[i];
             }
 #pragma unroll
-            for (auto &v : acc2) v = make_float2(0.f, 0.f);
+            for (float &v : acc) v = 0.f;
         }
         task = ntask_; s = ns; s1 = ns1;
         cur = next;
