@@ -229,6 +229,14 @@ def _stream_ptr(stream=None):
     return C.c_void_p(s.cuda_stream)
 
 
+def _on(stream):
+    """The given stream as the current one (nothing for None): what is allocated inside belongs to the stream that writes it.
+    A block that another stream has freed may still be written there."""
+    import contextlib
+    import torch
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
 def _dev_ptr(t, name, allow_none=False):
     import torch
     if t is None:
@@ -586,7 +594,10 @@ def linear_plan_image(blob: bytes, dtype, gated: bool = False):
 class LinearPlan:
     """Device plan of one block-pruned linear layer for ubp_linear. `blob` comes from ubp_pack (R = 1); dtype is the type
     of weights and activations: torch.bfloat16, torch.float16, or torch.float8_e4m3fn (weights are quantised here with one
-    scale a row, `row_scales`). gated: the layer's rows are [gate; up] and the product returns act(gate) * up."""
+    scale a row, `row_scales`). gated: the layer's rows are [gate; up] and the product returns act(gate) * up.
+    stream: the stream the upload runs on (default: the current one); the device buffer belongs to it. Calls may use the plan
+    on any stream that runs after the upload; such streams are recorded with the buffer, which is not handed out again before
+    their calls have finished, also when the plan dies first."""
 
     def __init__(self, blob: bytes, dtype, gated: bool = False, device="cuda", stream=None):
         import torch
@@ -604,15 +615,16 @@ class LinearPlan:
         _chk(L.ubp_linear_plan_size(_np_ptr(d), d.size, _dtypes()[dtype], int(gated), C.byref(n)), "ubp_linear_plan_size")
         self.dev_bytes = n.value
         self.out_features = v.M // 2 if gated else v.M
-        self.buffer = torch.empty(n.value + 256, dtype=torch.uint8, device=device)
-        self.device = self.buffer.device
-        self._dev = (self.buffer.data_ptr() + 255) // 256 * 256
         h = C.c_void_p()
-        with torch.cuda.device(self.device):
+        with torch.cuda.device(device), _on(stream):
+            self.buffer = torch.empty(n.value + 256, dtype=torch.uint8, device=device)
+            self.device = self.buffer.device
+            self._dev = (self.buffer.data_ptr() + 255) // 256 * 256
+            s = _stream_ptr()
             _chk(L.ubp_linear_plan_build(_np_ptr(d), d.size, _dtypes()[dtype], int(gated), C.c_void_p(self._dev), n.value,
-                                         _stream_ptr(stream), C.byref(h)), "ubp_linear_plan_build")
+                                         s, C.byref(h)), "ubp_linear_plan_build")
         self._handle = h
-        self._spec = (h.value, self.M, self.C, self.out_features, _dtypes()[dtype], self.buffer.get_device())
+        self._spec = (h.value, self.M, self.C, self.out_features, _dtypes()[dtype], self.buffer.get_device(), s.value or 0, self.buffer)
 
     @property
     def handle(self):

@@ -8,6 +8,7 @@
 
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDACachingAllocator.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Dtype.h>
@@ -219,15 +220,16 @@ PyObject *quant_rows(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
-// linear((handle, M, C, F, type code, device), x, bias, activation code, residual, x_scales, out, out_dtype, stream, workspace)
+// linear((handle, M, C, F, type code, device, the buffer's stream, the buffer), x, bias, activation code, residual, x_scales, out, out_dtype, stream, workspace)
 PyObject *linear(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return guarded([&]() -> PyObject * {
         count(n, 10);
-        if (!PyTuple_Check(a[0]) || PyTuple_GET_SIZE(a[0]) != 6) { PyErr_SetString(PyExc_TypeError, "bad plan"); throw Refused(); }
+        if (!PyTuple_Check(a[0]) || PyTuple_GET_SIZE(a[0]) != 8) { PyErr_SetString(PyExc_TypeError, "bad plan"); throw Refused(); }
         const auto *plan = static_cast<const ubp_linear_plan_t *>(PyLong_AsVoidPtr(PyTuple_GET_ITEM(a[0], 0)));
         int64_t d[5];
         for (int i = 0; i < 5; ++i) d[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(a[0], i + 1));
+        void *home = PyLong_AsVoidPtr(PyTuple_GET_ITEM(a[0], 6));
         const long act = PyLong_AsLong(a[3]);
         if (PyErr_Occurred()) throw Refused();
         const int64_t M = d[0], C = d[1], F = d[2];
@@ -245,6 +247,9 @@ PyObject *linear(PyObject *, PyObject *const *a, Py_ssize_t n)
         const int64_t ldy = out ? rows(*out, "out", T, F, type, dev) : F, ldr = residual ? rows(*residual, "residual", T, F, type, dev) : 0;
         if (ws && (!ws->is_cuda() || ws->get_device() != dev || !ws->is_contiguous())) refuse("workspace must be a contiguous tensor on the plan's device");
         On on(dev, a[8]);
+        if (on.stream != home)              // the plan's memory is in use on this stream too
+            c10::cuda::CUDACachingAllocator::recordStream(tensor(PyTuple_GET_ITEM(a[0], 7), "the plan's buffer")->storage().data_ptr(),
+                                                          c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)dev));
         at::Tensor y, room;
         if (!out) y = make(T, F, type, dev);
         const void *px = x->data_ptr();

@@ -1,0 +1,64 @@
+"""Plans built on a given stream, used on streams other than their own, and dropped while calls are still pending."""
+import pytest
+import torch
+
+from linear_ref import F8, make_weight
+
+pytestmark = pytest.mark.gpu
+
+BF16 = torch.bfloat16
+LONG = 20_000_000                # clock cycles of a pause on the GPU: some ten milliseconds
+
+
+@pytest.fixture(scope="module")
+def ubp():
+    import paper_2407_19644_b200 as m
+    m.load()
+    return m
+
+
+def leave_writes_pending(nbytes):
+    """Blocks of about this size that the current stream has freed and will still write to."""
+    busy = [torch.empty(n, device="cuda", dtype=torch.uint8) for n in (nbytes, nbytes, nbytes)]
+    torch.cuda._sleep(LONG)
+    for b in busy:
+        b.zero_()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F8], ids=["bf16", "e4m3"])
+def test_linear_plan_built_on_a_given_stream(ubp, dtype):
+    """The plan's memory comes from the stream that uploads it, so nothing that the current stream has yet to write reaches it."""
+    W, mask = make_weight(1024, 1536, 4, 60, 8)
+    blob = ubp.ubp_pack(W, mask, 4)
+    want = torch.from_numpy(ubp.linear_plan_image(blob, dtype)[0])
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    leave_writes_pending(want.numel() + 256)
+    plan = ubp.LinearPlan(blob, dtype, stream=st)
+    torch.cuda.synchronize()
+    at = plan._dev - plan.buffer.data_ptr()
+    assert torch.equal(plan.buffer[at:at + want.numel()].cpu(), want)
+
+
+@pytest.mark.parametrize("T", [1, 40, 300])
+@pytest.mark.parametrize("given", [False, True])
+def test_linear_plan_dropped_while_another_stream_uses_it(ubp, T, given):
+    """A call on another stream than the plan's keeps the plan's memory until it has run (a zeroed plan would give zeros)."""
+    W, mask = make_weight(1024, 1536, 4, 60, 8)
+    blob = ubp.ubp_pack(W, mask, 4)
+    x = torch.randn(T, 1536, device="cuda").to(BF16)
+    plan = ubp.LinearPlan(blob, BF16)
+    want, n = ubp.ubp_linear(plan, x), plan.buffer.numel()
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(st):
+        torch.cuda._sleep(LONG)
+        if not given:
+            got = ubp.ubp_linear(plan, x)
+    if given:
+        got = ubp.ubp_linear(plan, x, stream=st)
+    del plan
+    for _ in range(3):
+        torch.empty(n, device="cuda", dtype=torch.uint8).zero_()
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
