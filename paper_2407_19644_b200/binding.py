@@ -1,6 +1,7 @@
 """ctypes binding for libubp_b200.so. Names follow include/ubp.h."""
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 from typing import Optional, Tuple
@@ -232,7 +233,6 @@ def _stream_ptr(stream=None):
 def _on(stream):
     """The given stream as the current one (nothing for None): what is allocated inside belongs to the stream that writes it.
     A block that another stream has freed may still be written there."""
-    import contextlib
     import torch
     return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
 
@@ -253,20 +253,21 @@ class Plan:
     tensor owned by this object; the library holds only a small host handle."""
 
     def __init__(self, blob: bytes, variant: int = 0, device="cuda", stream=None, kmajor: bool = False):
-        """kmajor: `blob` comes from ubp_pack_kmajor (blocks of consecutive input channels inside one output row)."""
+        """kmajor: `blob` comes from ubp_pack_kmajor (blocks of consecutive input channels inside one output row).
+        stream: the stream the upload runs on (default: the current one); the device buffer belongs to it."""
         import torch
         L = load()
         self._lib = L
         self._handle = None
         b = np.frombuffer(blob, np.uint8)
         n = plan_size(blob, variant, kmajor)
-        self.buffer = torch.empty(n + 256, dtype=torch.uint8, device=device)
-        base = self.buffer.data_ptr()
-        self._dev = (base + 255) // 256 * 256
         h = C.c_void_p()
-        with torch.cuda.device(self.buffer.device):
+        with torch.cuda.device(device), _on(stream):
+            self.buffer = torch.empty(n + 256, dtype=torch.uint8, device=device)
+            self._dev = (self.buffer.data_ptr() + 255) // 256 * 256
+            self._home = _stream_ptr().value
             build = L.ubp_plan_build_kmajor if kmajor else L.ubp_plan_build
-            _chk(build(_np_ptr(b), b.size, variant, C.c_void_p(self._dev), n, _stream_ptr(stream), C.byref(h)),
+            _chk(build(_np_ptr(b), b.size, variant, C.c_void_p(self._dev), n, C.c_void_p(self._home), C.byref(h)),
                  "ubp_plan_build")
         self._handle = h
         info = _PlanInfo()
@@ -280,6 +281,15 @@ class Plan:
         if self._handle is None:
             raise RuntimeError("plan was freed")
         return self._handle
+
+    def _on_stream(self, stream):
+        """The stream of a call as a pointer; one that is not the buffer's own is recorded with the buffer, which is then not
+        handed out again before the call has finished, also when the plan dies first."""
+        import torch
+        s = torch.cuda.current_stream() if stream is None else stream
+        if (s.cuda_stream or None) != self._home:
+            self.buffer.record_stream(s)
+        return C.c_void_p(s.cuda_stream)
 
     def check(self, stream=None):
         """Synchronise the stream and raise if a kernel reported a failed bounded wait."""
@@ -335,16 +345,17 @@ def ubp_spmm(plan: Plan, X, bias=None, relu: bool = False, out=None, stream=None
         raise ValueError("X must be [C][Nc] with unit column stride")
     Nc = X.shape[1]
     if out is None:
-        out = torch.empty((plan.M, Nc), dtype=torch.float32, device=X.device)
+        with _on(stream):
+            out = torch.empty((plan.M, Nc), dtype=torch.float32, device=X.device)
     if out.shape != (plan.M, Nc) or (out.stride(1) != 1 and Nc > 1):
         raise ValueError("out must be [M][Nc] with unit column stride")
     with torch.cuda.device(X.device):
         _chk(plan._lib.ubp_spmm(plan.handle, _dev_ptr(X, "X"), X.stride(0), Nc, _dev_ptr(bias, "bias", True),
-                                int(bool(relu)), _dev_ptr(out, "out"), out.stride(0), _stream_ptr(stream)), "ubp_spmm")
+                                int(bool(relu)), _dev_ptr(out, "out"), out.stride(0), plan._on_stream(stream)), "ubp_spmm")
     return out
 
 
-def _conv_args(plan, x, out, layout, stride=1):
+def _conv_args(plan, x, out, layout, stride, stream):
     import torch
     if stride < 1:
         raise ValueError("stride must be >= 1")
@@ -361,7 +372,8 @@ def _conv_args(plan, x, out, layout, stride=1):
     if Cin != plan.C or x.stride(3) != 1 or x.stride(2) != Wd:
         raise ValueError("input planes must be contiguous [H][W] and have plan.C channels")
     if out is None:
-        out = torch.empty(oshape, dtype=torch.float32, device=x.device)
+        with _on(stream):
+            out = torch.empty(oshape, dtype=torch.float32, device=x.device)
     if tuple(out.shape) != oshape or out.stride(3) != 1 or out.stride(2) != oshape[3]:
         raise ValueError("bad output tensor")
     osb, osc = (out.stride(1), out.stride(0)) if layout == "CNHW" else (out.stride(0), out.stride(1))
@@ -374,21 +386,22 @@ def ubp_conv1x1(plan: Plan, x, bias=None, relu: bool = False, out=None, layout: 
     the pixels read are gathered into `scratch` first (a float32 CUDA tensor of at least C*B*Ho*Wo elements; allocated
     here when not given)."""
     import torch
-    B, H, Wd, sb, sc, out, osb, osc = _conv_args(plan, x, out, layout, stride)
+    B, H, Wd, sb, sc, out, osb, osc = _conv_args(plan, x, out, layout, stride, stream)
     if stride != 1:
         need = plan._lib.ubp_conv1x1_strided_scratch(plan.C, B, H, Wd, stride)
         if scratch is None:
-            scratch = torch.empty(need // 4, dtype=torch.float32, device=x.device)
+            with _on(stream):
+                scratch = torch.empty(need // 4, dtype=torch.float32, device=x.device)
         with torch.cuda.device(x.device):
             _chk(plan._lib.ubp_conv1x1_strided(plan.handle, _dev_ptr(x, "x"), B, H, Wd, stride, sb, sc,
                                                _dev_ptr(scratch, "scratch"), scratch.numel() * 4,
                                                _dev_ptr(bias, "bias", True), int(bool(relu)), _dev_ptr(out, "out"),
-                                               osb, osc, _stream_ptr(stream)), "ubp_conv1x1_strided")
+                                               osb, osc, plan._on_stream(stream)), "ubp_conv1x1_strided")
             scratch.record_stream(torch.cuda.current_stream() if stream is None else stream)
         return out
     with torch.cuda.device(x.device):
         _chk(plan._lib.ubp_conv1x1(plan.handle, _dev_ptr(x, "x"), B, H, Wd, sb, sc, _dev_ptr(bias, "bias", True),
-                                   int(bool(relu)), _dev_ptr(out, "out"), osb, osc, _stream_ptr(stream)), "ubp_conv1x1")
+                                   int(bool(relu)), _dev_ptr(out, "out"), osb, osc, plan._on_stream(stream)), "ubp_conv1x1")
     return out
 
 
@@ -399,23 +412,24 @@ def ubp_conv3x3_implicit(plan: Plan, x, bias=None, relu: bool = False, out=None,
     given), then the padded-grid kernel runs on them where the plan and layout allow; other strides > 1: the one-CTA
     tensor-core kernel or one lane per output pixel."""
     import torch
-    B, H, Wd, sb, sc, out, osb, osc = _conv_args(plan, x, out, layout, stride)
+    B, H, Wd, sb, sc, out, osb, osc = _conv_args(plan, x, out, layout, stride, stream)
     if stride != 1:
         need = plan._lib.ubp_conv3x3_strided_scratch(plan.C, B, H, Wd, stride)
         if scratch is None and need:
-            scratch = torch.empty(need // 4, dtype=torch.float32, device=x.device)
+            with _on(stream):
+                scratch = torch.empty(need // 4, dtype=torch.float32, device=x.device)
         with torch.cuda.device(x.device):
             _chk(plan._lib.ubp_conv3x3_strided_ws(plan.handle, _dev_ptr(x, "x"), B, H, Wd, stride, sb, sc,
                                                   _dev_ptr(scratch, "scratch", True), scratch.numel() * 4 if scratch is not None else 0,
                                                   _dev_ptr(bias, "bias", True), int(bool(relu)), _dev_ptr(out, "out"),
-                                                  osb, osc, _stream_ptr(stream)), "ubp_conv3x3_strided_ws")
+                                                  osb, osc, plan._on_stream(stream)), "ubp_conv3x3_strided_ws")
             if scratch is not None:
                 scratch.record_stream(torch.cuda.current_stream() if stream is None else stream)
         return out
     with torch.cuda.device(x.device):
         _chk(plan._lib.ubp_conv3x3_implicit(plan.handle, _dev_ptr(x, "x"), B, H, Wd, sb, sc,
                                             _dev_ptr(bias, "bias", True), int(bool(relu)), _dev_ptr(out, "out"),
-                                            osb, osc, _stream_ptr(stream)), "ubp_conv3x3_implicit")
+                                            osb, osc, plan._on_stream(stream)), "ubp_conv3x3_implicit")
     return out
 
 
@@ -434,7 +448,8 @@ def ubp_spmm_static(blob: bytes, X, bias=None, relu: bool = False, out=None, str
         raise ValueError("X must be [C][Nc] with unit column stride")
     Nc = X.shape[1]
     if out is None:
-        out = torch.empty((d["M"], Nc), dtype=torch.float32, device=X.device)
+        with _on(stream):
+            out = torch.empty((d["M"], Nc), dtype=torch.float32, device=X.device)
     if tuple(out.shape) != (d["M"], Nc) or (out.stride(1) != 1 and Nc > 1):
         raise ValueError("out must be [M][Nc] with unit column stride")
     with torch.cuda.device(X.device):
@@ -451,7 +466,8 @@ def static_plan_capacity() -> int:
 # ------------------------------------------------------------------ block selection (Section 4.1)
 class BedSelector:
     """Device scratch for block selection on layers of one shape ([M][C][R] weights, block size Nb); the scratch
-    is a torch uint8 tensor owned by this object, so repeated calls allocate nothing but their outputs."""
+    is a torch uint8 tensor owned by this object, so repeated calls allocate nothing but their outputs. It belongs to the
+    stream that is current here; a call on another stream has to be ordered after that one, as with any tensor."""
 
     def __init__(self, M: int, Cin: int, R: int, Nb: int, device="cuda"):
         import torch
@@ -477,7 +493,8 @@ class BedSelector:
         the weights."""
         import torch
         if out is None:
-            out = torch.empty((self.C, self.M), dtype=torch.float32, device=W.device)
+            with _on(stream):
+                out = torch.empty((self.C, self.M), dtype=torch.float32, device=W.device)
         with torch.cuda.device(W.device):
             _chk(self._lib.ubp_block_scores(self._w(W), self.M, self.C, self.R, self.Nb, C.c_void_p(self._base),
                                             self.bytes, C.c_void_p(out.data_ptr()), _stream_ptr(stream)),
@@ -488,9 +505,11 @@ class BedSelector:
         """Block expansion and division: (mask uint8 CUDA tensor [M][C], n_selected int64 CUDA tensor [1])."""
         import torch
         if mask is None:
-            mask = torch.empty((self.M, self.C), dtype=torch.uint8, device=W.device)
+            with _on(stream):
+                mask = torch.empty((self.M, self.C), dtype=torch.uint8, device=W.device)
         if n_selected is None:
-            n_selected = torch.zeros(1, dtype=torch.int64, device=W.device)
+            with _on(stream):
+                n_selected = torch.zeros(1, dtype=torch.int64, device=W.device)
         if mask.dtype != torch.uint8 or tuple(mask.shape) != (self.M, self.C) or not mask.is_contiguous():
             raise ValueError("mask must be a contiguous uint8 CUDA tensor [M][C]")
         with torch.cuda.device(W.device):
@@ -509,7 +528,8 @@ def _selector_for(W, Nb: int) -> BedSelector:
 def ubp_block_scores(W, Nb: int, stream=None):
     """One-shot form of BedSelector.scores (allocates its scratch; synchronises before freeing it)."""
     import torch
-    sel = _selector_for(W, Nb)
+    with _on(stream):
+        sel = _selector_for(W, Nb)
     S = sel.scores(W, stream=stream)
     torch.cuda.synchronize(W.device)
     return S
@@ -518,7 +538,8 @@ def ubp_block_scores(W, Nb: int, stream=None):
 def ubp_bed_select(W, Nb: int, m: int, stream=None):
     """One-shot form of BedSelector.select (allocates its scratch; synchronises before freeing it)."""
     import torch
-    sel = _selector_for(W, Nb)
+    with _on(stream):
+        sel = _selector_for(W, Nb)
     out = sel.select(W, m, stream=stream)
     torch.cuda.synchronize(W.device)
     return out

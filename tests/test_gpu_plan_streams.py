@@ -62,3 +62,58 @@ def test_linear_plan_dropped_while_another_stream_uses_it(ubp, T, given):
         torch.empty(n, device="cuda", dtype=torch.uint8).zero_()
     torch.cuda.synchronize()
     assert torch.equal(got, want)
+
+
+def test_image_plan_and_outputs_on_a_given_stream(ubp):
+    """The same for the plans and calls on images: plan, outputs and scratch belong to the stream that writes them."""
+    import numpy as np
+    import ubp_synth
+    L = ubp_synth.make_layer("streams", 256, 512, 4, 70, 3, Nc=64)
+    blob = ubp.ubp_pack(L.W, L.mask, 4)
+    st = torch.cuda.Stream()
+    plan = ubp.Plan(blob)
+    want = torch.from_numpy(ubp.plan_image(blob, plan.variant)[0])
+    torch.cuda.synchronize()
+    leave_writes_pending(plan.buffer.numel())
+    late = ubp.Plan(blob, stream=st)
+    torch.cuda.synchronize()
+    at = late._dev - late.buffer.data_ptr()
+    assert torch.equal(late.buffer[at:at + want.numel()].cpu(), want)
+    x = torch.randn(512, 4, 32, 32, device="cuda")
+    r = ubp_synth.make_layer("streams", 64, 64, 4, 70, 4, B=2, H=32, Wd=32, R=9)
+    p3, x3 = ubp.Plan(ubp.ubp_pack(r.W, r.mask, 4)), torch.from_numpy(r.X).cuda()
+    W = torch.from_numpy(np.ascontiguousarray(L.W[:, :, 0])).cuda()
+    calls = [lambda s: ubp.ubp_spmm(plan, x.view(512, -1), stream=s), lambda s: ubp.ubp_conv1x1(plan, x, stream=s),
+             lambda s: ubp.ubp_conv1x1(plan, x, stride=2, stream=s), lambda s: ubp.ubp_conv3x3_implicit(p3, x3, stream=s),
+             lambda s: ubp.ubp_conv3x3_implicit(p3, x3, stride=2, stream=s), lambda s: ubp.ubp_block_scores(W, 4, stream=s),
+             lambda s: ubp.ubp_bed_select(W, 4, 500, stream=s)[0], lambda s: ubp.ubp_bed_select(W, 4, 500, stream=s)[1]]
+    for call in calls:
+        want = call(None)
+        torch.cuda.synchronize()
+        leave_writes_pending(want.nbytes)
+        got = call(st)
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+
+
+def test_image_plan_dropped_while_another_stream_uses_it(ubp):
+    import ubp_synth
+    L = ubp_synth.make_layer("streams", 256, 512, 4, 70, 3, Nc=64)
+    blob = ubp.ubp_pack(L.W, L.mask, 4)
+    x = torch.randn(512, 4096, device="cuda")
+    for given in (False, True):
+        plan = ubp.Plan(blob)
+        want, n = ubp.ubp_spmm(plan, x), plan.buffer.numel()
+        st = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(st):
+            torch.cuda._sleep(LONG)
+            if not given:
+                got = ubp.ubp_spmm(plan, x)
+        if given:
+            got = ubp.ubp_spmm(plan, x, stream=st)
+        del plan
+        for _ in range(3):
+            torch.empty(n, device="cuda", dtype=torch.uint8).zero_()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
