@@ -427,9 +427,9 @@ int ubp_quant_rows(const void *x, int64_t ldx, int dtype, int64_t T, int C, void
  * rounded; the scales are part of the plan). gated != 0: the layer is [gate; up] with M / 2 rows each (M even) and the
  * product returns act(gate) * up. The device image holds the layer twice: the kept blocks (few tokens, bound by reading the
  * weights) and a densified matrix (many tokens, tensor cores).
- * Same division of labour as ubp_plan_*: size and image are host only, the caller owns dev_buf (256-byte aligned), the
- * upload is one cudaMemcpyAsync on `stream`. Errors as there; UBP_E_UNSUPPORTED for R != 1, more than 65536 input
- * features or 2^31 entries. */
+ * Same division of labour as ubp_plan_*: size and image are host only, the caller owns dev_buf (256-byte aligned). The
+ * upload is one cudaMemcpyAsync on `stream`, which the call waits for; no host copy of the image stays. Errors as there;
+ * UBP_E_UNSUPPORTED for R != 1, more than 65536 input features or 2^31 entries. */
 typedef struct ubp_linear_plan ubp_linear_plan_t;
 int ubp_linear_plan_size(const void *blob, size_t len, int dtype, int gated, size_t *dev_bytes);
 /* geom receives {weights per entry, entries per 16-byte chunk, dense rows, dense row length, bytes per value, lanes per

@@ -41,7 +41,7 @@ struct ubp_linear_plan {
     int M, C, Nb, m;
     int dtype, gated;
     int F;                          // output features: M, or M / 2 of a gated plan
-    ubp::LinearImage img;           // host copy (kept until free)
+    ubp::LinearImage img;           // geometry and offsets (its bytes are released after the upload)
     uint8_t *dev;                   // caller's device buffer
 };
 

@@ -136,8 +136,16 @@ int ubp_linear_plan_build(const void *blob, size_t len, int dtype, int gated, vo
     p->dtype = dtype; p->gated = gated != 0;
     p->F = p->gated ? v.M / 2 : v.M;
     p->dev = static_cast<uint8_t *>(dev_buf);
-    const cudaError_t e = cudaMemcpyAsync(dev_buf, p->img.bytes.data(), p->img.total, cudaMemcpyHostToDevice,
-                                          static_cast<cudaStream_t>(stream));
+    // The copy is waited for, so the host image (as large as the device's, 168 MB for 16384 x 4096 in 16 bits) need not stay:
+    // launches read the geometry only. A stream under capture cannot be waited for and may replay the copy: there it stays.
+    const cudaStream_t st = static_cast<cudaStream_t>(stream);
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    cudaError_t e = cudaStreamIsCapturing(st, &capture);
+    if (e == cudaSuccess) e = cudaMemcpyAsync(dev_buf, p->img.bytes.data(), p->img.total, cudaMemcpyHostToDevice, st);
+    if (e == cudaSuccess && capture == cudaStreamCaptureStatusNone) {
+        e = cudaStreamSynchronize(st);
+        std::vector<uint8_t>().swap(p->img.bytes);
+    }
     if (e != cudaSuccess) { ubp::set_last_cuda_error((int)e); delete p; return UBP_E_CUDA; }
     *plan = p;
     return UBP_OK;
