@@ -411,8 +411,8 @@ typedef enum {
  * x, residual, h have type `dtype` (UBP_F32, UBP_F16, UBP_BF16); gamma [C] has that type or UBP_F32. h (nullable) receives
  * the sum rounded to `dtype` (the norm itself uses the unrounded sum); it may be x's or residual's own buffer with the same
  * stride. y_dtype is `dtype`, or UBP_E4M3: then scales[t] = max(max |y| / 448, 2^-126) and the row holds
- * e4m3(y / scales[t]), rounded to nearest even; a row of zeros has scale 2^-126 and codes 0. Arithmetic and statistics are
- * fp32. scales is ignored for other output types.
+ * e4m3(y / scales[t]), the quotient rounded to fp32 and then to the nearest code, ties to even; a row of zeros has scale
+ * 2^-126 and codes 0. Arithmetic and statistics are fp32. scales is ignored for other output types.
  * Errors: UBP_E_ARG (null, types, sizes, a stride below C, a misaligned pointer), UBP_E_UNSUPPORTED (more than 2^31 row
  * groups), UBP_E_CUDA. */
 int ubp_rmsnorm(const void *x, int64_t ldx, const void *residual, int64_t ldr, const void *gamma, int gamma_dtype, int dtype,

@@ -20,6 +20,7 @@
 // every form.
 #include <cuda_runtime.h>
 
+#include <cfloat>
 #include <cstdint>
 
 #include "ubp_internal.h"
@@ -154,26 +155,32 @@ __global__ void __launch_bounds__(rows_block(TPR), rows_blocks_per_sm(TPR, NORM,
             if (Q) mx = max_nan(mx, fabsf(v[e]));
         }
     };
-    float rinv, sinv;
-    // A product with 1 / s instead of a division for each value (which made the kernel ALU-bound: 336 us instead of HBM's
-    // 143 on 16384 x 8192): the quotient is off by at most 1.5 units of 2^-24, against half a code step of 2^-4. s is at
-    // least 2^-126, so 1 / s is finite. rinv and 1 / s stay two products: theirs could overflow for a row of tiny values.
+    // The quotient y / s, two operations a value (a division for each made the kernel ALU-bound: 336 us instead of HBM's 143 on
+    // 16384 x 8192). 1 / s in two fp32 numbers: r = 1 / s rounded down, r2 = (1 - r s) r, the difference exact in fp32. y r + y r2
+    // with one rounding at the end is off by less than 2^-46 of the quotient before that rounding (2^-30 for scales beyond
+    // 2^102, whose r2 is subnormal), so the codes are those of the divided values; y / s by r alone gave one f16 value in
+    // 15 000 its neighbour's code. r2 >= 0 keeps the sign of a zero. An infinite scale has r = r2 = 0: finite values become 0,
+    // infinities NaN. s is at least 2^-126, so 1 / s is finite. rinv and 1 / s stay two products: theirs could overflow for a
+    // row of tiny values.
+    float rinv, sinv, sinv2;
     auto finish = [&](bool live) {
         rinv = NORM ? rsqrtf(sum / (float)a.C + a.eps) : 1.f;
-        sinv = 1.f;
         if (Q) {
             const float s = max_nan(__fdiv_rn(NORM ? mx * rinv : mx, E4M3_MAX), ROW_SCALE_MIN);
-            sinv = __fdiv_rn(1.f, s);
+            sinv = __frcp_rd(s);
+            sinv2 = s <= FLT_MAX ? fmaf(-sinv, s, 1.f) * sinv : 0.f;
             if (live && lane == 0) a.scales[row] = s;
         }
+    };
+    // t -> the value that is stored
+    auto out = [&](float t) {
+        const float o = NORM ? t * rinv : t;
+        return Q ? fmaf(o, sinv, o * sinv2) : o;
     };
     auto put = [&](int64_t at, const float (&v)[E]) {
         float o[E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            o[e] = NORM ? v[e] * rinv : v[e];
-            if (Q) o[e] *= sinv;
-        }
+        for (int e = 0; e < E; ++e) o[e] = out(v[e]);
         if constexpr (E == 8) store8<TO>(y + at, o);
         else y[at] = from_f32<TO>(o[0]);
     };
@@ -236,8 +243,7 @@ __global__ void __launch_bounds__(rows_block(TPR), rows_blocks_per_sm(TPR, NORM,
                 TO *p = y + row * a.ldy;
 #pragma unroll
                 for (int k = 0; k < NV; ++k) {
-                    float o = NORM ? v[k] * rinv : v[k];
-                    if (Q) o *= sinv;
+                    const float o = out(v[k]);
                     if (c0 + k * STEP < a.C) p[k * STEP] = from_f32<TO>(o);
                 }
             }
