@@ -385,10 +385,12 @@ int launch_rows(const RowArgs &a, int dtype, int y_dtype, void *stream)
 {
     const int b = dtype_size(dtype), bo = dtype_size(y_dtype);
     auto al = [](const void *p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; };
-    // eight elements an access: whole groups only, and every row of every operand on a boundary of its access
-    const bool vec = a.C % 8 == 0 && al(a.x, 16) && a.ldx * b % 16 == 0 && (!a.r || (al(a.r, 16) && a.ldr * b % 16 == 0)) &&
-                     (!a.h || (al(a.h, 16) && a.ldh * b % 16 == 0)) && al(a.y, bo == 1 ? 8 : 16) && a.ldy * bo % (bo == 1 ? 8 : 16) == 0 &&
-                     (!NORM || al(a.gamma, 16));
+    // eight elements an access: whole groups only, and every row of every operand on a boundary of its access (a single row has
+    // no pitch)
+    auto rows_on = [&](const void *p, int64_t ld, int size, int n) { return al(p, (uintptr_t)n) && (a.T <= 1 || ld * size % n == 0); };
+    const int no = bo == 1 ? 8 : 16;
+    const bool vec = a.C % 8 == 0 && rows_on(a.x, a.ldx, b, 16) && (!a.r || rows_on(a.r, a.ldr, b, 16)) &&
+                     (!a.h || rows_on(a.h, a.ldh, b, 16)) && rows_on(a.y, a.ldy, bo, no) && (!NORM || al(a.gamma, 16));
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (y_dtype == UBP_E4M3) {
         switch (dtype) {

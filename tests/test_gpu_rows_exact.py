@@ -84,3 +84,21 @@ def test_infinite_rows(ubp):
         x[1, 5] = float("inf")
         q, s = ubp.ubp_quant_rows(x)
         assert s[1].isinf() and torch.equal(q.float().nan_to_num(7.0), codes(x, s).view(F8).float().nan_to_num(7.0))
+
+
+@pytest.mark.parametrize("C", [96, 1000, 4096, 8192])
+def test_one_row_of_a_wider_buffer(ubp, C):
+    """The pitch of a single row says nothing about its alignment: the same kernel as for a contiguous row, the same bits."""
+    for seed in range(8):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+
+        def row(v):
+            b = torch.empty(2, C + 3, device="cuda")
+            b[0, :C] = v
+            return b[:1, :C]
+
+        x, r = (torch.randn(1, C, device="cuda", generator=g) for _ in range(2))
+        gamma = torch.ones(C, device="cuda")
+        want, _, h = ubp.ubp_rmsnorm(x, gamma, 1e-5, residual=r)
+        got, _, h1 = ubp.ubp_rmsnorm(row(x), gamma, 1e-5, residual=row(r), out=row(0.0), residual_out=row(0.0))
+        assert torch.equal(got, want) and torch.equal(h1, h)
