@@ -311,7 +311,7 @@ ubp_linear_sparse_kernel(const SpArgs p)
                 if (row - b >= 0) sum += src[-b * (NACC - TT)];       // start row row - b, its weight b: (-b rows + b) * TT
             z[q] = sum * ws + b0;
         }
-        float v = apply_act(z[0], a.act);
+        float v = apply_act(z[0], a.act, p.ydt);
         if (nseg == 2) v *= z[1];
         if (a.res) v += load_elem(a.res, (t0 + t) * a.ldr + f0 + f, p.ydt);
         store_elem(a.y, (t0 + t) * a.ldy + f0 + f, v, p.ydt);

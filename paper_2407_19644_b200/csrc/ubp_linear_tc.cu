@@ -205,7 +205,7 @@ __device__ __forceinline__ void few_epilogue(const TcLinArgs &p, const FewCols &
             z[j] = (F8 ? z[j] * (xs * c.w0[j]) : z[j]) + c.b0[j];
             u[j] = (F8 ? u[j] * (xs * c.w1[j]) : u[j]) + c.b1[j];
         }
-        apply_act<4>(z, a.act);
+        apply_act<sizeof(T) == 4>(z, a.act);
 #pragma unroll
         for (int j = 0; j < 4; ++j) z[j] = (a.gated ? z[j] * u[j] : z[j]) + r[j];
         store4(static_cast<T *>(a.y) + (t0 + t) * a.ldy + c.f, c.n, vec, z);
@@ -422,7 +422,8 @@ __device__ __forceinline__ void store_turned(const uint8_t *turn, const LinearAr
 
 // NT: features (dense rows) per tile, 128 or 256. vec: elements an access to y and the residual may take;
 // VEC8: that is 8 (an instance of its own: the registers of the narrow forms cost the wide one 5 % in spills).
-template <bool F8, int NT, bool VEC8>
+// F32: fp32 output (its activations beside the 16-bit ones in one instance cost those 2 to 5 %).
+template <bool F8, int NT, bool VEC8, bool F32>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(LT_THREADS, 1)
 ubp_linear_many_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, const TcLinArgs p,
                        const int fmt, const int ntm, const int ntn, const int vec)
@@ -602,14 +603,14 @@ ubp_linear_many_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
                         asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
                         scaled16(r, f0 + h * 16, z);
                         scaled16(r2, a.F + f0 + h * 16, u);
-                        apply_act<16>(z, a.act);
+                        apply_act<F32>(z, a.act);
 #pragma unroll
                         for (int j = 0; j < 16; ++j) z[j] *= u[j];
                     } else {
                         tmem_ld16(acc + (uint32_t)(c * 32 + h * 16), r);
                         asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
                         scaled16(r, f0 + h * 16, z);
-                        apply_act<16>(z, a.act);
+                        apply_act<F32>(z, a.act);
                     }
                     // turn: lane = token row writes its 16 values, 16-byte pieces XORed with the row
 #pragma unroll
@@ -625,9 +626,9 @@ ubp_linear_many_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
                     }
                 }
                 __syncwarp();
-                if (p.ydt == UBP_BF16) store_turned<__nv_bfloat16, VEC8>(turn, a, trow, f0, lane, vec);
-                else if (p.ydt == UBP_F16) store_turned<__half, VEC8>(turn, a, trow, f0, lane, vec);
-                else store_turned<float, VEC8>(turn, a, trow, f0, lane, vec);
+                if constexpr (F32) store_turned<float, VEC8>(turn, a, trow, f0, lane, vec);
+                else if (p.ydt == UBP_BF16) store_turned<__nv_bfloat16, VEC8>(turn, a, trow, f0, lane, vec);
+                else store_turned<__half, VEC8>(turn, a, trow, f0, lane, vec);
                 __syncwarp();
             }
             if (!released && lane == 0) {
@@ -758,11 +759,11 @@ int launch_few(const CUtensorMap &tmW, const CUtensorMap &tmX, const TcLinArgs &
     return e == cudaSuccess ? UBP_OK : fail(e);
 }
 
-template <bool F8, int NT, bool VEC8>
+template <bool F8, int NT, bool VEC8, bool F32>
 int launch_many(const CUtensorMap &tmW, const CUtensorMap &tmX, const TcLinArgs &p, int fmt, int sms, int vec, cudaStream_t st)
 {
     static bool done[64] = {};
-    const auto kern = ubp_linear_many_kernel<F8, NT, VEC8>;
+    const auto kern = ubp_linear_many_kernel<F8, NT, VEC8, F32>;
     const size_t smem = (size_t)MANY_STAGES * many_stage(NT) + LT_EPI_WARPS * MANY_TURN + 1024;
     static_assert(MANY_STAGES * many_stage(128) + LT_EPI_WARPS * MANY_TURN + 1024 >= TC_PAIR_MIN_SMEM, "one block per SM");
     if (int rc = allow_smem(kern, done, smem)) return rc;
@@ -842,8 +843,12 @@ int launch_linear_tc(const ubp_linear_plan *pl, const LinearArgs &args, int y_dt
     int vec = 8;
     while (vec > 1 && !(pl->F % vec == 0 && rows_on(args.y, args.ldy, vec * ob < 16 ? vec * ob : 16) &&
                         (!args.res || rows_on(args.res, args.ldr, vec * ob < 16 ? vec * ob : 16)))) vec /= 2;
-    auto go = [&](auto f8_, auto nt_, auto v_) { return launch_many<decltype(f8_)::value, decltype(nt_)::value, decltype(v_)::value>(tmW, tmX, p, fmt, sms, vec, st); };
-    auto by_vec = [&](auto f8_, auto nt_) { return vec == 8 ? go(f8_, nt_, std::true_type{}) : go(f8_, nt_, std::false_type{}); };
+    auto by_out = [&](auto f8_, auto nt_, auto v_) {
+        constexpr bool f = decltype(f8_)::value, v = decltype(v_)::value;
+        constexpr int n = decltype(nt_)::value;
+        return y_dtype == UBP_F32 ? launch_many<f, n, v, true>(tmW, tmX, p, fmt, sms, vec, st) : launch_many<f, n, v, false>(tmW, tmX, p, fmt, sms, vec, st);
+    };
+    auto by_vec = [&](auto f8_, auto nt_) { return vec == 8 ? by_out(f8_, nt_, std::true_type{}) : by_out(f8_, nt_, std::false_type{}); };
     auto by_tile = [&](auto f8_) { return ch.cols == 128 ? by_vec(f8_, std::integral_constant<int, 128>{}) : by_vec(f8_, std::integral_constant<int, 256>{}); };
     return f8 ? by_tile(std::true_type{}) : by_tile(std::false_type{});
 }
