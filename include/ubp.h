@@ -389,7 +389,9 @@ int ubp_bed_select(const float *W, int M, int C, int R, int Nb, int64_t m, void 
  *     y = D p + h                ubp_linear with a residual
  * is four calls. Strides (ld*) are in elements between the rows of consecutive tokens; rows are contiguous. T == 0 is a
  * no-op. Pointers need the alignment of their element type only; 16-byte aligned rows are faster. Infinities and NaNs in
- * a row stay in that row's outputs. */
+ * a row stay in that row's outputs (ubp_linear on the kept blocks: in those outputs of the row that keep their channel; on
+ * the densified weight a pruned place times an infinity or NaN is NaN, as in a dense product. ubp_linear_choice tells which
+ * form a number of tokens takes). */
 typedef enum {
     UBP_F32 = 0,
     UBP_F16 = 1,

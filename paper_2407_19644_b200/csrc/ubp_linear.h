@@ -24,9 +24,10 @@ namespace ubp {
 //   dense_off     the densified weight [Mp][Kp] (plan's type), K contiguous. Gated plans interleave the two halves in
 //                 groups of 16 rows: dense row 32 g + i is gate row 16 g + i, dense row 32 g + 16 + i is up row 16 g + i.
 //                 Kp = C rounded up to 128 bytes, Mp = rows rounded up to 128; the padding is zero.
+//   cnt_off       uint32[M]: entries of a start row without the fillers
 struct LinearImage {
     std::vector<uint8_t> bytes;
-    size_t scale_off = 0, off_off = 0, idx_off = 0, val_off = 0, dense_off = 0, total = 0;
+    size_t scale_off = 0, off_off = 0, idx_off = 0, val_off = 0, dense_off = 0, cnt_off = 0, total = 0;
     int nbk = 1, epc = 1, lanes = 8, bundles = 0, Mp = 0, Kp = 0;
     int64_t entries = 0, steps = 0;
 };

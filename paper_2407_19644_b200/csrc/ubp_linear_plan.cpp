@@ -104,6 +104,7 @@ int build_linear_image(const ubp_view_t &v, int dtype, bool gated, bool count_on
     img.idx_off = at; at += round_up((size_t)img.steps * 32 * epc * 2, 256);
     img.val_off = at; at += round_up((size_t)img.steps * 512, 256);
     img.dense_off = at; at += round_up((size_t)img.Mp * img.Kp * b, 256);
+    img.cnt_off = at; at += round_up((size_t)M * 4, 256);
     img.total = at;
     if (count_only) return UBP_OK;
 
@@ -123,6 +124,7 @@ int build_linear_image(const ubp_view_t &v, int dtype, bool gated, bool count_on
         std::memcpy(base + img.scale_off, scale.data(), (size_t)M * 4);
     }
     std::memcpy(base + img.off_off, off.data(), off.size() * 4);
+    std::memcpy(base + img.cnt_off, count.data(), count.size() * 4);
     // place of entry n of start row i
     auto place = [&](int i, uint32_t n) {
         const uint32_t c = n / (uint32_t)epc, step = off[(size_t)(i / rb)] + c / (uint32_t)lanes;

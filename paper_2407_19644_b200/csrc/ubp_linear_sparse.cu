@@ -19,6 +19,10 @@
 // instructions a chunk, most of them for finding rows).
 // The activations lie in shared memory as [channel][token] (16-bit; 8-bit codes become f16, which holds every one of them),
 // so an entry gathers all its tokens with one access. Every sum has a fixed order: results are bitwise reproducible.
+//
+// Infinities and NaN in x reach the outputs that keep their channel and no other. The plan fills rows up with entries of weight
+// zero at a channel of its own choice, whose product with an infinity would be NaN: a warp whose sums are not finite does the
+// bundle once more without them (two or three instructions a bundle for every other call).
 #include <cuda_runtime.h>
 
 #include <cstdint>
@@ -44,6 +48,7 @@ struct SpArgs {
     const uint32_t *off;
     const uint16_t *idx;
     const uint8_t *val;
+    const uint32_t *cnt;              // entries of a start row
     int lanes;                        // lanes per start row
     int grid, ydt;
     bool wide;                        // twice the threads
@@ -103,6 +108,55 @@ __host__ __device__ constexpr int sp_unroll(int nacc, int epc) { return (nacc <=
 __host__ __device__ constexpr int sp_blocks(int nacc, int epc) { return nacc <= 8 && epc <= 8 ? 2 : 1; }
 // a block of twice the threads has 64 registers a thread too: no more sums than fit
 __host__ __device__ constexpr bool sp_wide(int nacc) { return nacc <= 32; }
+
+// The tokens of channel j, two a word
+template <typename X, int TT> __device__ __forceinline__ void load_tokens(const X *xs, uint32_t j, uint32_t (&xw)[TT > 1 ? TT / 2 : 1])
+{
+    const X *xp = xs + j * TT;
+    if constexpr (TT == 1) xw[0] = *reinterpret_cast<const uint16_t *>(xp);
+    else if constexpr (TT == 2) xw[0] = *reinterpret_cast<const uint32_t *>(xp);
+    else if constexpr (TT == 4) { const uint2 v = *reinterpret_cast<const uint2 *>(xp); xw[0] = v.x; xw[1] = v.y; }
+    else { const uint4 v = *reinterpret_cast<const uint4 *>(xp); xw[0] = v.x; xw[1] = v.y; xw[2] = v.z; xw[3] = v.w; }
+}
+
+// The sums of one bundle's rows without the fillers: `steps` steps from val and idx on, n entries of this lane's row. Same order
+// of additions as in the kernel, so a row without infinities gets the value it has without them. Out of line, to keep its
+// registers out of the main loop.
+template <typename W, int NBK, int TT>
+__device__ __noinline__ void sums_without_fillers(const typename XOf<W>::type *xs, const uint8_t *val, const uint16_t *idx, uint32_t steps, uint32_t n,
+                                                  int lanes, int C, float *sums, int *status)
+{
+    using X = typename XOf<W>::type;
+    constexpr int NACC = NBK * TT, EPC = 16 / (NBK * wsize<W>);
+    const uint32_t lane = threadIdx.x & 31, own = lane & (uint32_t)(lanes - 1);
+    float acc[NACC];
+#pragma unroll
+    for (float &v : acc) v = 0.f;
+#pragma unroll 1
+    for (uint32_t s = 0; s < steps; ++s) {
+        const uint32_t first = (s * (uint32_t)lanes + own) * EPC;
+        if (first >= n) continue;
+        const Chunk16<W> w(__ldg(reinterpret_cast<const uint4 *>(val) + (size_t)s * 32 + lane));
+        uint32_t j[EPC > 1 ? EPC / 2 : 1];
+        load_channels<EPC>(idx + ((size_t)s * 32 + lane) * EPC, j);
+#pragma unroll
+        for (int e = 0; e < EPC; ++e) {
+            const uint32_t c = EPC == 1 ? j[0] : (e & 1) ? j[e / 2] >> 16 : j[e / 2] & 0xffffu;
+            if (first + e >= n || !UBP_CHK_SMEM((int)c < C, status)) continue;
+            uint32_t xw[TT > 1 ? TT / 2 : 1];
+            load_tokens<X, TT>(xs, c, xw);
+#pragma unroll
+            for (int i = 0; i < NACC; ++i)
+                acc[i] = fma_mixed<X>(w.at(e * NBK + i / TT), (uint16_t)(xw[i % TT / 2] >> (16 * (i % TT & 1))), acc[i]);
+        }
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < NACC; ++i) {
+        for (int o = 1; o < lanes; o <<= 1) acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], o);
+        if (own == 0) sums[i] = acc[i];
+    }
+}
 
 template <typename W, int NBK, int TT, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS > SP_THREADS ? 1 : sp_blocks(NBK * TT, 16 / (NBK * wsize<W>)))
@@ -244,12 +298,8 @@ ubp_linear_sparse_kernel(const SpArgs p)
             for (int e = 0; e < EPC; ++e) {
                 const uint32_t j = EPC == 1 ? cur.j[u][0] : (e & 1) ? cur.j[u][e / 2] >> 16 : cur.j[u][e / 2] & 0xffffu;
                 if (!UBP_CHK_SMEM((int)j < a.C, a.status)) continue;
-                const X *xp = xs + j * TT;
                 uint32_t xw[TT > 1 ? TT / 2 : 1];
-                if constexpr (TT == 1) xw[0] = *reinterpret_cast<const uint16_t *>(xp);
-                else if constexpr (TT == 2) xw[0] = *reinterpret_cast<const uint32_t *>(xp);
-                else if constexpr (TT == 4) { const uint2 v = *reinterpret_cast<const uint2 *>(xp); xw[0] = v.x; xw[1] = v.y; }
-                else { const uint4 v = *reinterpret_cast<const uint4 *>(xp); xw[0] = v.x; xw[1] = v.y; xw[2] = v.z; xw[3] = v.w; }
+                load_tokens<X, TT>(xs, j, xw);
 #pragma unroll
                 for (int b = 0; b < NBK; ++b)
 #pragma unroll
@@ -287,6 +337,16 @@ ubp_linear_sparse_kernel(const SpArgs p)
                 float *dst = part + ((size_t)task * rb + lane / p.lanes) * NACC + at;
 #pragma unroll
                 for (int i = 0; i < left; ++i) dst[i] = acc[i];
+            }
+            float none = 0.f;                                       // (not zero: an infinity or NaN among the sums)
+#pragma unroll
+            for (int i = 0; i < left; ++i) none = fmaf(acc[i], 0.f, none);
+            if (__any_sync(0xffffffffu, !(none == 0.f))) {
+                const int q = bundle_of(task), row = q * rb + lane / p.lanes;
+                const uint32_t first = __ldg(p.off + q);
+                sums_without_fillers<W, NBK, TT>(xs, p.val + (size_t)first * 512, p.idx + (size_t)first * (32 * EPC), __ldg(p.off + q + 1) - first,
+                                                 row < a.M ? __ldg(p.cnt + row) : 0u, p.lanes, a.C,
+                                                 part + ((size_t)task * rb + lane / p.lanes) * NACC, a.status);
             }
 #pragma unroll
             for (float &v : acc) v = 0.f;
@@ -397,6 +457,7 @@ int launch_linear_sparse(const ubp_linear_plan *pl, const LinearArgs &a, int y_d
     p.off = reinterpret_cast<const uint32_t *>(pl->dev + pl->img.off_off);
     p.idx = reinterpret_cast<const uint16_t *>(pl->dev + pl->img.idx_off);
     p.val = pl->dev + pl->img.val_off;
+    p.cnt = reinterpret_cast<const uint32_t *>(pl->dev + pl->img.cnt_off);
     p.ydt = y_dtype;
     const int nbk = pl->img.nbk, nseg = a.gated ? 2 : 1;
     int TT;

@@ -49,3 +49,55 @@ def test_fp32_outputs_have_fp32_activations(ubp, act, T):
         err = (y.double() - want).abs()
         bound = rel * want.abs() + 2.0 ** -118
         assert (err <= bound).all(), float((err / bound).max())
+
+
+def without_rows(W, mask, Nb, n):
+    """The layer without the blocks that start in its first n rows."""
+    mask = mask.copy()
+    for j in range(mask.shape[1]):
+        i = n
+        while i < mask.shape[0] and mask[i, j]:
+            i += 1
+        mask[:n + (i - n) % Nb, j] = 0
+    return W * mask, mask
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16, F8], ids=IDS.get)
+@pytest.mark.parametrize("T", [1, 2, 5, 16])
+@pytest.mark.parametrize("M,C,Nb,gated", [(512, 512, 8, False), (640, 300, 4, True), (300, 1003, 2, False), (256, 256, 3, False)])
+def test_kept_blocks_alone_see_infinities(ubp, dtype, T, M, C, Nb, gated):
+    """The kept-block kernel multiplies kept weights only: an infinity or NaN in a channel reaches the outputs that keep this
+    channel, as the product with their weight, and no other; rows without blocks stay what they are."""
+    W, mask = make_weight(M, C, Nb, 90, 9)
+    W, mask = without_rows(W, mask, Nb, 48)            # whole rows empty, beside rows that are not
+    plan = ubp.LinearPlan(ubp.ubp_pack(W, mask, Nb), dtype, gated=gated)
+    assert plan.choice(T)[0] == 0
+    g = torch.Generator(device="cuda").manual_seed(T)
+    x = torch.randn(T, C, device="cuda", generator=g).to(dtype)
+    xs = torch.ones(T, device="cuda") if dtype == F8 else None
+    kept = torch.from_numpy(mask != 0).cuda()
+    w = torch.from_numpy(W).cuda().double()
+    t = T - 1
+    specials = [(0, "nan"), (C - 1, "nan")] + ([] if dtype == F8 else [(0, "inf"), (C - 1, "inf"), (C // 2, "-inf")])
+    for j, v in specials:
+        zeroed, bad = x.clone(), x.clone()
+        zeroed[t, j] = 0.0
+        bad[t, j] = float(v)
+        z = ubp.ubp_linear(plan, zeroed, x_scales=xs, out_dtype=torch.float32).double()
+        y = ubp.ubp_linear(plan, bad, x_scales=xs, out_dtype=torch.float32).double()
+        want = z.clone()
+        add = torch.where(kept[:, j], w[:, j] * float(v), torch.zeros_like(w[:, j]))
+        if gated:
+            touched = kept[:M // 2, j] | kept[M // 2:, j]
+            assert torch.equal(y[t][~touched], z[t][~touched]) and not torch.isfinite(y[t][touched]).any()
+        else:
+            want[t] += add
+            assert torch.equal(y[t].nan_to_num(7.0, 8.0, 9.0), want[t].nan_to_num(7.0, 8.0, 9.0))
+        assert torch.equal(y[:t], z[:t])
+    if dtype != F8 and not gated:                      # every channel infinite: each output is its weights' infinities
+        bad = torch.full_like(x, float("inf"))
+        y = ubp.ubp_linear(plan, bad, out_dtype=torch.float32)
+        pos, neg = ((w > 0) & kept).any(1), ((w < 0) & kept).any(1)
+        zero = ((w.to(dtype) == 0) & kept).any(1)
+        assert (y[:, pos & ~neg & ~zero] == float("inf")).all() and (y[:, neg & ~pos & ~zero] == float("-inf")).all()
+        assert y[:, pos & neg].isnan().all() and (y[:, ~kept.any(1)] == 0).all()
