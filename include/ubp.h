@@ -415,8 +415,8 @@ typedef enum {
  * stride. y_dtype is `dtype`, or UBP_E4M3: then scales[t] = max(max |y| / 448, 2^-126) and the row holds
  * e4m3(y / scales[t]), the quotient rounded to fp32 and then to the nearest code, ties to even; a row of zeros has scale
  * 2^-126 and codes 0. Arithmetic and statistics are fp32. scales is ignored for other output types.
- * Errors: UBP_E_ARG (null, types, sizes, a stride below C, a misaligned pointer), UBP_E_UNSUPPORTED (more than 2^31 row
- * groups), UBP_E_CUDA. */
+ * Errors: UBP_E_ARG (null, types, sizes, a stride below C, a misaligned pointer, h at y's place, or at x's or residual's with
+ * another stride), UBP_E_CUDA. */
 int ubp_rmsnorm(const void *x, int64_t ldx, const void *residual, int64_t ldr, const void *gamma, int gamma_dtype, int dtype,
                 int64_t T, int C, float eps, void *h, int64_t ldh, void *y, int64_t ldy, int y_dtype, float *scales,
                 void *stream);
@@ -461,7 +461,7 @@ int ubp_linear_plan_clear_status(const ubp_linear_plan_t *plan, void *stream);
  * run in a fixed order: results are bitwise reproducible. Up to a few tokens the kept blocks are multiplied on the CUDA
  * cores; from there on the densified weight on the tensor cores. y must not overlap x; with residual == y each element is
  * read before it is written.
- * Errors: UBP_E_ARG, UBP_E_SPACE (workspace), UBP_E_UNSUPPORTED, UBP_E_CUDA. */
+ * Errors: UBP_E_ARG (also y == x, and residual == y with another stride), UBP_E_SPACE (workspace), UBP_E_UNSUPPORTED, UBP_E_CUDA. */
 /* ubp_linear_choice: which kernel T tokens take on the current device. *kernel: 0 = kept blocks on the CUDA cores
  * (*tile tokens a block), 1 = densified weight on the tensor cores, one block per 128 weight rows and *tile tokens, *split blocks of a cluster
  * sharing a reduction, 2 = densified weight, CTA pairs on tiles of 256 tokens x *tile weight rows. Host only. */

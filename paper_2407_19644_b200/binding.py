@@ -698,7 +698,7 @@ def ubp_linear(plan: LinearPlan, x, bias=None, activation: str = "none", residua
                out_dtype=None, stream=None, workspace=None):
     """y[T][F] = act(x @ W.T + bias) + residual with the plan's block-pruned W (gated plan: act(gate) * up + residual).
     x: [T][C] in the plan's type, rows contiguous; 8-bit plans need x_scales (float32 [T]). bias: float32 [M]. residual:
-    [T][F] in the output's type, may be `out` itself. out_dtype: the plan's type (8-bit plans: bfloat16) unless given.
+    [T][F] in the output's type, may be `out` itself; `out` must not overlap x. out_dtype: the plan's type (8-bit plans: bfloat16) unless given.
     workspace: a CUDA tensor for inputs whose rows are not 16-byte aligned (allocated here when needed and not given)."""
     spec = plan._spec
     if spec is None:

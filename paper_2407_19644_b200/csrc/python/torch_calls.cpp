@@ -67,6 +67,11 @@ int64_t rows(const at::Tensor &t, const char *name, int64_t T, int64_t C, at::Sc
     if ((C > 1 && t.stride(1) != 1) || (T > 1 && ld < C)) refuse(std::string(name) + " must have contiguous rows that do not overlap");
     return ld;
 }
+// Two operands in one place: only element by element, so with one row stride.
+void same_rows(const at::Tensor *a, int64_t lda, const at::Tensor *b, int64_t ldb, int64_t T, const char *what)
+{
+    if (a && b && T > 1 && lda != ldb && a->data_ptr() == b->data_ptr()) refuse(std::string(what) + " start at one place but differ in their row stride");
+}
 // a contiguous [n] vector
 void *vec(const at::Tensor &t, const char *name, int64_t n, at::ScalarType type, int dev)
 {
@@ -176,6 +181,9 @@ PyObject *rmsnorm(PyObject *, PyObject *const *a, Py_ssize_t n)
         const int64_t ldr = residual ? rows(*residual, "residual", x.T, x.C, x.type, x.dev) : 0;
         int64_t ldh = rout ? rows(*rout, "residual_out", x.T, x.C, x.type, x.dev) : x.C;
         void *ps = q && scales ? vec(*scales, "scales", x.T, at::kFloat, x.dev) : nullptr;
+        same_rows(rout, ldh, tensor(a[0], "x"), x.ld, x.T, "residual_out and x");
+        same_rows(rout, ldh, residual, ldr, x.T, "residual_out and residual");
+        if (out && rout && x.T > 0 && out->data_ptr() == rout->data_ptr()) refuse("out and residual_out are one place");
         On on(x.dev, a[8]);
         at::Tensor y, s, h;
         if (!out) y = make(x.T, x.C, type, x.dev);
@@ -245,6 +253,8 @@ PyObject *linear(PyObject *, PyObject *const *a, Py_ssize_t n)
         const int ydt = code_of(type);
         if (ydt < 0) refuse("out_dtype must be float32, float16 or bfloat16");
         const int64_t ldy = out ? rows(*out, "out", T, F, type, dev) : F, ldr = residual ? rows(*residual, "residual", T, F, type, dev) : 0;
+        if (out && T > 0 && out->data_ptr() == x->data_ptr()) refuse("out must not be x: every output reads a whole row of it");
+        same_rows(out, ldy, residual, ldr, T, "out and residual");
         if (ws && (!ws->is_cuda() || ws->get_device() != dev || !ws->is_contiguous())) refuse("workspace must be a contiguous tensor on the plan's device");
         On on(dev, a[8]);
         if (on.stream != home)              // the plan's memory is in use on this stream too

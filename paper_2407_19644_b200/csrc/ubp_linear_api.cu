@@ -201,6 +201,7 @@ int ubp_linear(const ubp_linear_plan_t *plan, const void *x, int64_t ldx, const 
     if (T == 0) return UBP_OK;
     const uintptr_t b = (uintptr_t)ubp::dtype_size(plan->dtype), o = (uintptr_t)ubp::dtype_size(y_dtype);
     if (!x || !y || (T > 1 && (ldx < plan->C || ldy < plan->F || (residual && ldr < plan->F)))) return UBP_E_ARG;
+    if (y == x || (residual == y && T > 1 && ldr != ldy)) return UBP_E_ARG;      // (read whole rows; element by element)
     auto off = [](const void *p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) != 0; };
     if (off(x, b) || off(y, o) || off(residual, o) || off(bias, 4) || off(x_scales, 4) || off(workspace, 16)) return UBP_E_ARG;
     if (workspace_bytes < ubp_linear_workspace_size(plan, x, ldx, T)) return UBP_E_SPACE;

@@ -425,6 +425,7 @@ extern "C" int ubp_rmsnorm(const void *x, int64_t ldx, const void *residual, int
     if (T == 0) return UBP_OK;
     if (!x || !gamma || !y || (y_dtype == UBP_E4M3 && !scales)) return UBP_E_ARG;
     if ((T > 1 && (ldx < C || ldy < C || (residual && ldr < C) || (h && ldh < C)))) return UBP_E_ARG;
+    if (h && (h == y || (T > 1 && ((h == x && ldh != ldx) || (h == residual && ldh != ldr))))) return UBP_E_ARG;
     if (!ubp::aligned_to(x, b) || !ubp::aligned_to(residual, b) || !ubp::aligned_to(h, b) || !ubp::aligned_to(y, bo) ||
         !ubp::aligned_to(gamma, ubp::dtype_size(gamma_dtype)) || !ubp::aligned_to(scales, 4)) return UBP_E_ARG;
     const ubp::RowArgs a{x, residual, gamma, h, y, scales, ldx, ldr, ldh, ldy, T, C, eps, gamma_dtype == UBP_F32};

@@ -101,3 +101,22 @@ def test_kept_blocks_alone_see_infinities(ubp, dtype, T, M, C, Nb, gated):
         zero = ((w.to(dtype) == 0) & kept).any(1)
         assert (y[:, pos & ~neg & ~zero] == float("inf")).all() and (y[:, neg & ~pos & ~zero] == float("-inf")).all()
         assert y[:, pos & neg].isnan().all() and (y[:, ~kept.any(1)] == 0).all()
+
+
+def test_outputs_over_inputs(ubp):
+    """Every output reads a whole row of x: writing over x is refused. The residual may be the output, with its stride."""
+    W, mask = make_weight(128, 128, 4, 50, 1)
+    for T in (1, 5, 40):
+        plan = ubp.LinearPlan(ubp.ubp_pack(W, mask, 4), BF16)
+        x = torch.randn(T, 128, device="cuda").to(BF16)
+        with pytest.raises(ValueError):
+            ubp.ubp_linear(plan, x, out=x)
+    buf = torch.zeros(5, 256, device="cuda", dtype=BF16)
+    with pytest.raises(ValueError):
+        ubp.ubp_linear(plan, x[:5].clone(), residual=buf[:, :128], out=buf.view(-1)[:640].view(5, 128))
+    gamma = torch.ones(128, device="cuda", dtype=BF16)
+    rows, tight = buf[:, :128], buf.view(-1)[:640].view(5, 128)
+    for bad in (lambda: ubp.ubp_rmsnorm(rows, gamma, residual=x[:5], residual_out=tight), lambda: ubp.ubp_rmsnorm(x[:5], gamma, residual=rows, residual_out=tight),
+                lambda: ubp.ubp_rmsnorm(x[:5], gamma, residual=rows, residual_out=tight, out=tight)):
+        with pytest.raises(ValueError):
+            bad()

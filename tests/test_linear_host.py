@@ -113,3 +113,13 @@ def test_c_entry_refusals():
         a = list(ok)
         a[at] = v
         assert L.ubp_quant_rows(*a) == -1, (at, v)
+
+
+def test_c_entry_refuses_outputs_over_inputs():
+    L, p, q = ubp.load(), 1 << 20, 1 << 21                                                # (never dereferenced)
+    ok = [p, 64, None, 0, q, 2, 2, 4, 64, 1e-5, None, 64, p + 4096, 64, 2, None, None]
+    for changes in ({2: p + 8192, 3: 64, 10: p + 4096}, {10: p, 11: 72}, {2: p + 8192, 3: 64, 10: p + 8192, 11: 72}):
+        a = list(ok)
+        for at, v in changes.items():
+            a[at] = v
+        assert L.ubp_rmsnorm(*a) == -1, changes
