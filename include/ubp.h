@@ -414,7 +414,9 @@ typedef enum {
  * the sum rounded to `dtype` (the norm itself uses the unrounded sum); it may be x's or residual's own buffer with the same
  * stride. y_dtype is `dtype`, or UBP_E4M3: then scales[t] = max(max |y| / 448, 2^-126) and the row holds
  * e4m3(y / scales[t]), the quotient rounded to fp32 and then to the nearest code, ties to even; a row of zeros has scale
- * 2^-126 and codes 0. Arithmetic and statistics are fp32. scales is ignored for other output types.
+ * 2^-126 and codes 0. Arithmetic and statistics are fp32: with eps == 0 a row whose squares vanish (zeros among them) has no
+ * norm, its outputs are NaN or infinities; a row whose squares overflow (beyond 1.8e19) is 0. scales is ignored for other
+ * output types.
  * Errors: UBP_E_ARG (null, types, sizes, a stride below C, a misaligned pointer, h at y's place, or at x's or residual's with
  * another stride), UBP_E_CUDA. */
 int ubp_rmsnorm(const void *x, int64_t ldx, const void *residual, int64_t ldr, const void *gamma, int gamma_dtype, int dtype,

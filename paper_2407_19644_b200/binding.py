@@ -546,6 +546,7 @@ def ubp_bed_select(W, Nb: int, m: int, stream=None):
 
 
 # ------------------------------------------------------------------ token-major operators (language-model layers)
+# Inference only: no gradient is recorded, also when an argument requires one.
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 
 
@@ -581,7 +582,8 @@ def ubp_rmsnorm(x, gamma, eps: float = 1e-6, residual=None, out_dtype=None, out=
     """Root mean square norm of the rows of x [T][C] (float32, float16 or bfloat16), with the residual's addition:
     h = x + residual; y = h * gamma / sqrt(mean(h^2) + eps). Returns (y, scales, h): y in x's type with scales None, or
     (out_dtype=torch.float8_e4m3fn) in 8 bits with one float32 scale a row; h is x + residual in x's type, or None without
-    a residual. residual_out may be the residual or x itself."""
+    a residual. residual_out may be the residual or x itself. eps should be positive: a row of zeros has no norm without it.
+    No gradient is recorded."""
     r = (_calls or _native()).rmsnorm(x, gamma, eps, residual, out_dtype, out, scales, residual_out,
                                       None if stream is None else stream.cuda_stream)
     if type(r) is int:
@@ -591,7 +593,7 @@ def ubp_rmsnorm(x, gamma, eps: float = 1e-6, residual=None, out_dtype=None, out=
 
 def ubp_quant_rows(x, out=None, scales=None, stream=None):
     """Rows of x [T][C] (float32, float16 or bfloat16) in 8 bits: (q float8_e4m3fn [T][C], scales float32 [T]) with
-    x ~= q * scales[:, None]."""
+    x ~= q * scales[:, None]. No gradient is recorded."""
     r = (_calls or _native()).quant_rows(x, out, scales, None if stream is None else stream.cuda_stream)
     if type(r) is int:
         _chk(r, "ubp_quant_rows")
@@ -699,7 +701,8 @@ def ubp_linear(plan: LinearPlan, x, bias=None, activation: str = "none", residua
     """y[T][F] = act(x @ W.T + bias) + residual with the plan's block-pruned W (gated plan: act(gate) * up + residual).
     x: [T][C] in the plan's type, rows contiguous; 8-bit plans need x_scales (float32 [T]). bias: float32 [M]. residual:
     [T][F] in the output's type, may be `out` itself; `out` must not overlap x. out_dtype: the plan's type (8-bit plans: bfloat16) unless given.
-    workspace: a CUDA tensor for inputs whose rows are not 16-byte aligned (allocated here when needed and not given)."""
+    workspace: a CUDA tensor for inputs whose rows are not 16-byte aligned (allocated here when needed and not given).
+    No gradient is recorded."""
     spec = plan._spec
     if spec is None:
         raise RuntimeError("plan was freed")

@@ -102,3 +102,23 @@ def test_one_row_of_a_wider_buffer(ubp, C):
         want, _, h = ubp.ubp_rmsnorm(x, gamma, 1e-5, residual=r)
         got, _, h1 = ubp.ubp_rmsnorm(row(x), gamma, 1e-5, residual=row(r), out=row(0.0), residual_out=row(0.0))
         assert torch.equal(got, want) and torch.equal(h1, h)
+
+
+def test_rows_without_a_norm(ubp):
+    """eps = 0: a row of zeros is 0 / 0, one whose squares vanish in fp32 is not finite; a positive eps gives zeros their zeros."""
+    for C in (64, 65):
+        x = torch.randn(3, C, device="cuda")
+        x[1], x[2] = 0, 1e-30
+        gamma = torch.ones(C, device="cuda")
+        for out in (torch.float32, F8):
+            y, s, _ = ubp.ubp_rmsnorm(x, gamma, 0.0, out_dtype=out)
+            y = y.float()
+            assert torch.isfinite(y[0]).all() and y[1].isnan().all() and not torch.isfinite(y[2]).any()
+            y, s, _ = ubp.ubp_rmsnorm(x, gamma, 1e-6, out_dtype=out)
+            assert (y.float()[1] == 0).all() and torch.isfinite(y.float()).all()
+
+
+def test_no_gradient_is_recorded(ubp):
+    x = torch.randn(3, 64, device="cuda", requires_grad=True)
+    gamma = torch.ones(64, device="cuda", requires_grad=True)
+    assert not any(t.requires_grad for t in ubp.ubp_rmsnorm(x, gamma, 1e-5, residual=x, out_dtype=F8) + ubp.ubp_quant_rows(x))
