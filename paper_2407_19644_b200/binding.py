@@ -565,7 +565,7 @@ def _native():
             from . import _torch_calls
         except ImportError as e:
             raise RuntimeError("paper_2407_19644_b200/_torch_calls.so is missing or does not match this torch: build it with "
-                               "`python -m paper_2407_19644_b200.build` (there is no fallback implementation)") from e
+                               "`python -m paper_2407_19644_b200.build`, or with --force (there is no fallback implementation)") from e
         _torch_calls.bind(*(C.cast(f, C.c_void_p).value for f in (L.ubp_rmsnorm, L.ubp_quant_rows, L.ubp_linear, L.ubp_linear_workspace_size)))
         _calls = _torch_calls
     return _calls

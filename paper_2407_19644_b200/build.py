@@ -9,7 +9,9 @@ word and skip the access (nothing traps). Load it by setting UBP_B200_LIBRARY to
 from __future__ import annotations
 
 import glob
+import importlib.util
 import os
+import shutil
 import subprocess
 import sys
 
@@ -19,6 +21,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libubp_b200.so")
 TORCH_SRC = os.path.join(CSRC, "python", "torch_calls.cpp")
 TORCH_LIB = os.path.join(HERE, "_torch_calls.so")          # checks and allocations of the token-major calls, against torch
+TORCH_MADE_FOR = os.path.join(HERE, "build", "torch_calls.txt")   # the torch and Python that it was built against
 LIB_DEBUG = os.path.join(HERE, "libubp_b200_debug.so")     # the checked build (-DUBP_DEBUG): same entry points
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 
@@ -36,7 +39,15 @@ def _stale(lib: str = LIB) -> bool:
 
 
 def build(force: bool = False, verbose: bool = False, debug: bool = False) -> str:
-    build_torch_calls(force)
+    """The library, and where torch is installed the extension module of the token-major calls. The library comes first: it
+    needs neither torch nor its headers."""
+    lib = build_library(force, verbose, debug)
+    if importlib.util.find_spec("torch") is not None:
+        build_torch_calls(force)
+    return lib
+
+
+def build_library(force: bool = False, verbose: bool = False, debug: bool = False) -> str:
     lib = LIB_DEBUG if debug else LIB
     if not force and not _stale(lib):
         return lib
@@ -65,16 +76,28 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
     return lib
 
 
-def build_torch_calls(force: bool = False) -> str:
-    """The extension module of the token-major calls (host code only; no CUDA source in it)."""
+def _torch_calls_stale(made_for: str) -> bool:
     deps = [TORCH_SRC, os.path.join(ROOT, "include", "ubp.h")]
-    if not force and os.path.exists(TORCH_LIB) and all(os.path.getmtime(TORCH_LIB) >= os.path.getmtime(d) for d in deps):
-        return TORCH_LIB
+    if not os.path.exists(TORCH_LIB) or any(os.path.getmtime(d) > os.path.getmtime(TORCH_LIB) for d in deps):
+        return True
+    try:
+        with open(TORCH_MADE_FOR) as f:
+            return f.read() != made_for
+    except OSError:
+        return True
+
+
+def build_torch_calls(force: bool = False) -> str:
+    """The extension module of the token-major calls (host code only; no CUDA source in it). It fits one torch and one Python:
+    another version of either makes it stale."""
     import sysconfig
     import torch
-    base = os.path.join(os.path.dirname(torch.__file__))
+    made_for = f"torch {torch.__version__}, {sysconfig.get_config_var('SOABI')}"
+    if not force and not _torch_calls_stale(made_for):
+        return TORCH_LIB
+    base = os.path.dirname(torch.__file__)
     inc = [os.path.join(base, "include"), os.path.join(base, "include", "torch", "csrc", "api", "include"),
-           os.path.join(os.path.dirname(os.path.dirname(NVCC)), "include"), sysconfig.get_paths()["include"]]
+           os.path.join(os.path.dirname(os.path.dirname(shutil.which(NVCC) or NVCC)), "include"), sysconfig.get_paths()["include"]]
     tmp = TORCH_LIB + f".tmp{os.getpid()}"
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", TORCH_SRC, "-o", tmp,
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", os.path.join(ROOT, "include")]
@@ -83,6 +106,9 @@ def build_torch_calls(force: bool = False) -> str:
     cmd += ["-L", os.path.join(base, "lib"), "-Wl,--no-as-needed", "-lc10", "-lc10_cuda", "-ltorch_cpu", "-ltorch_cuda", "-ltorch_python"]
     subprocess.run(cmd, check=True)
     os.replace(tmp, TORCH_LIB)
+    os.makedirs(os.path.dirname(TORCH_MADE_FOR), exist_ok=True)
+    with open(TORCH_MADE_FOR, "w") as f:
+        f.write(made_for)
     return TORCH_LIB
 
 
