@@ -49,6 +49,7 @@ struct SpArgs {
     const uint16_t *idx;
     const uint8_t *val;
     const uint32_t *cnt;              // entries of a start row
+    uint32_t steps;                   // of the whole plan
     int lanes;                        // lanes per start row
     int grid, ydt;
     bool wide;                        // twice the threads
@@ -201,7 +202,12 @@ ubp_linear_sparse_kernel(const SpArgs p)
     int task = warp;
     uint32_t s = 0, s1 = 0;
     Batch cur;
-    if (task < ntask) { s = __ldg(p.off + bundle_of(task)); s1 = __ldg(p.off + bundle_of(task) + 1); }
+    auto steps_of = [&](int task, uint32_t &s, uint32_t &s1) {
+        const uint32_t first = __ldg(p.off + bundle_of(task)), end = __ldg(p.off + bundle_of(task) + 1);
+        if (!UBP_CHK_SMEM(first <= end && end <= p.steps, a.status)) return;
+        s = first; s1 = end;
+    };
+    if (task < ntask) steps_of(task, s, s1);
     load(s, s1, cur);
 
     asm volatile("griddepcontrol.wait;" ::: "memory");
@@ -286,7 +292,7 @@ ubp_linear_sparse_kernel(const SpArgs p)
         if (ns >= s1) {
             ntask_ += (THREADS / 32);
             ns = ns1 = 0;
-            if (ntask_ < ntask) { ns = __ldg(p.off + bundle_of(ntask_)); ns1 = __ldg(p.off + bundle_of(ntask_) + 1); }
+            if (ntask_ < ntask) steps_of(ntask_, ns, ns1);
         }
         Batch next;
         load(ns, ns1, next);
@@ -333,8 +339,9 @@ ubp_linear_sparse_kernel(const SpArgs p)
                 for (int i = 0; i < left; ++i) acc[i] += __shfl_xor_sync(0xffffffffu, acc[i], o);
             // one lane per sum writes it (with fewer sums than lanes several lanes hold the same one)
             const int own = lane & (p.lanes - 1);
-            if (own < (NACC >= 8 ? 8 : NACC)) {
-                float *dst = part + ((size_t)task * rb + lane / p.lanes) * NACC + at;
+            float *dst = part + ((size_t)task * rb + lane / p.lanes) * NACC + at;
+            if (own < (NACC >= 8 ? 8 : NACC) &&
+                UBP_CHK_SMEM((uint64_t)(reinterpret_cast<uint8_t *>(dst + left) - smem) <= tc::dbg_dynamic_smem(), a.status)) {
 #pragma unroll
                 for (int i = 0; i < left; ++i) dst[i] = acc[i];
             }
@@ -342,9 +349,10 @@ ubp_linear_sparse_kernel(const SpArgs p)
 #pragma unroll
             for (int i = 0; i < left; ++i) none = fmaf(acc[i], 0.f, none);
             if (__any_sync(0xffffffffu, !(none == 0.f))) {
-                const int q = bundle_of(task), row = q * rb + lane / p.lanes;
-                const uint32_t first = __ldg(p.off + q);
-                sums_without_fillers<W, NBK, TT>(xs, p.val + (size_t)first * 512, p.idx + (size_t)first * (32 * EPC), __ldg(p.off + q + 1) - first,
+                const int row = bundle_of(task) * rb + lane / p.lanes;
+                uint32_t first = 0, end = 0;
+                steps_of(task, first, end);
+                sums_without_fillers<W, NBK, TT>(xs, p.val + (size_t)first * 512, p.idx + (size_t)first * (32 * EPC), end - first,
                                                  row < a.M ? __ldg(p.cnt + row) : 0u, p.lanes, a.C,
                                                  part + ((size_t)task * rb + lane / p.lanes) * NACC, a.status);
             }
@@ -363,6 +371,7 @@ ubp_linear_sparse_kernel(const SpArgs p)
         for (int q = 0; q < 2; ++q) {
             if (q == nseg) break;
             const int row = q * a.F + f0 + f;
+            if (!UBP_CHK_GMEM(row < a.M && f0 + f < a.F && t0 + t < a.T, a.status)) break;
             const float *src = part + ((size_t)(q ? n0 : 0) * rb + row - (q ? lo1 : lo0) * rb) * NACC + t;
             const float ws = std::is_same<W, F8>::value ? a.xs[t0 + t] * p.wscale[row] : 1.f, b0 = a.bias ? a.bias[row] : 0.f;
             float sum = 0.f;
@@ -457,6 +466,7 @@ int launch_linear_sparse(const ubp_linear_plan *pl, const LinearArgs &a, int y_d
     p.off = reinterpret_cast<const uint32_t *>(pl->dev + pl->img.off_off);
     p.idx = reinterpret_cast<const uint16_t *>(pl->dev + pl->img.idx_off);
     p.val = pl->dev + pl->img.val_off;
+    p.steps = (uint32_t)pl->img.steps;
     p.cnt = reinterpret_cast<const uint32_t *>(pl->dev + pl->img.cnt_off);
     p.ydt = y_dtype;
     const int nbk = pl->img.nbk, nseg = a.gated ? 2 : 1;

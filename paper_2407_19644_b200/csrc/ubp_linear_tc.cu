@@ -188,6 +188,8 @@ __device__ __forceinline__ void few_epilogue(const TcLinArgs &p, const FewCols &
 #pragma unroll 2
     for (int t = ta + tid / per; t < tb; t += step) {
         float z[4] = {0.f, 0.f, 0.f, 0.f}, u[4] = {0.f, 0.f, 0.f, 0.f}, r[4] = {0.f, 0.f, 0.f, 0.f};
+        if (!UBP_CHK_GMEM(t0 + t < a.T && c.f < a.F && c.f + (vec ? 4 : 1) <= a.F, a.status)) continue;
+        if (!UBP_CHK_SMEM((uint32_t)(t * 128 + c.dl + (a.gated ? 20 : 4)) * 4u <= tc::dbg_dynamic_smem(), a.status)) continue;
         const float *src = red + t * 128 + c.dl;
         if (a.res) load4(static_cast<const T *>(a.res) + (t0 + t) * a.ldr + c.f, c.n, vec, r);
         const float xs = F8 ? a.xs[t0 + t] : 1.f;
@@ -352,7 +354,8 @@ __host__ __device__ constexpr uint32_t many_stage(int nt) { return 128 * LT_LINE
 // One warp's 32 tokens x 32 values -> y, with the residual. E elements an access (8, 4, 2 or 1: what the rows of y and of the
 // residual are aligned to and the layer's features are a multiple of); 32 / E lanes hold a token's 32 values.
 template <typename T, int E>
-__device__ __forceinline__ void store_turned_e(const uint8_t *turn, const T *res, int64_t ldr, T *y, int64_t ldy, int nt, int nf, int lane)
+__device__ __forceinline__ void store_turned_e(const uint8_t *turn, const T *res, int64_t ldr, T *y, int64_t ldy, int nt, int nf, int lane,
+                                               int *status)
 {
     constexpr int LPR = 32 / E, UN = E >= 4 ? E / 2 : E == 2 ? 4 : 8;      // lanes a token; steps under way (E steps of E tokens)
     const int c = (lane % LPR) * E;
@@ -377,7 +380,7 @@ __device__ __forceinline__ void store_turned_e(const uint8_t *turn, const T *res
 #pragma unroll
         for (int i = 0; i < UN; ++i) {
             const int r = (i0 + i) * E + lane / LPR;
-            if (r >= nt) continue;
+            if (r >= nt || !UBP_CHK_GMEM(r < 32 && c + E <= nf, status)) continue;
             float o[E];
             const uint8_t *row = turn + r * 128;
             if constexpr (E >= 4) {
@@ -412,11 +415,11 @@ __device__ __forceinline__ void store_turned(const uint8_t *turn, const LinearAr
     const T *res = a.res ? static_cast<const T *>(a.res) + trow * a.ldr + f0 : nullptr;
     T *y = static_cast<T *>(a.y) + trow * a.ldy + f0;
     if constexpr (VEC8) {
-        store_turned_e<T, 8>(turn, res, a.ldr, y, a.ldy, nt, nf, lane);
+        store_turned_e<T, 8>(turn, res, a.ldr, y, a.ldy, nt, nf, lane, a.status);
     } else {
-        if (vec == 4) store_turned_e<T, 4>(turn, res, a.ldr, y, a.ldy, nt, nf, lane);
-        else if (vec == 2) store_turned_e<T, 2>(turn, res, a.ldr, y, a.ldy, nt, nf, lane);
-        else store_turned_e<T, 1>(turn, res, a.ldr, y, a.ldy, nt, nf, lane);
+        if (vec == 4) store_turned_e<T, 4>(turn, res, a.ldr, y, a.ldy, nt, nf, lane, a.status);
+        else if (vec == 2) store_turned_e<T, 2>(turn, res, a.ldr, y, a.ldy, nt, nf, lane, a.status);
+        else store_turned_e<T, 1>(turn, res, a.ldr, y, a.ldy, nt, nf, lane, a.status);
     }
 }
 
@@ -650,7 +653,8 @@ ubp_linear_many_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
 
 // Rows of x that a tensor copy cannot take (not 16-byte aligned) -> [T][Kp] rows, zeros past C.
 template <typename T>
-__global__ void __launch_bounds__(256) ubp_linear_pad_kernel(const T *__restrict__ x, int64_t ldx, int64_t T_, int C, T *__restrict__ out, int Kp)
+__global__ void __launch_bounds__(256) ubp_linear_pad_kernel(const T *__restrict__ x, int64_t ldx, int64_t T_, int C, T *__restrict__ out, int Kp,
+                                                              int *status)
 {
     constexpr int E = 16 / (int)sizeof(T);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -660,6 +664,7 @@ __global__ void __launch_bounds__(256) ubp_linear_pad_kernel(const T *__restrict
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x) {
         const int64_t t = i / groups;
         const int c = (int)(i - t * groups) * E;
+        if (!UBP_CHK_GMEM(t < T_ && c + E <= Kp, status)) continue;
         alignas(16) T v[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) v[e] = c + e < C ? x[t * ldx + c + e] : T(0);
@@ -825,8 +830,8 @@ int launch_linear_tc(const ubp_linear_plan *pl, const LinearArgs &args, int y_dt
         attr[0].val.programmaticStreamSerializationAllowed = 1;
         cfg.attrs = attr;
         cfg.numAttrs = 1;
-        cudaError_t e = f8 ? cudaLaunchKernelEx(&cfg, ubp_linear_pad_kernel<uint8_t>, static_cast<const uint8_t *>(x), ldx, args.T, C, static_cast<uint8_t *>(workspace), pl->img.Kp)
-                           : cudaLaunchKernelEx(&cfg, ubp_linear_pad_kernel<uint16_t>, static_cast<const uint16_t *>(x), ldx, args.T, C, static_cast<uint16_t *>(workspace), pl->img.Kp);
+        cudaError_t e = f8 ? cudaLaunchKernelEx(&cfg, ubp_linear_pad_kernel<uint8_t>, static_cast<const uint8_t *>(x), ldx, args.T, C, static_cast<uint8_t *>(workspace), pl->img.Kp, args.status)
+                           : cudaLaunchKernelEx(&cfg, ubp_linear_pad_kernel<uint16_t>, static_cast<const uint16_t *>(x), ldx, args.T, C, static_cast<uint16_t *>(workspace), pl->img.Kp, args.status);
         if (e == cudaSuccess) e = cudaGetLastError();
         if (e != cudaSuccess) return fail(e);
         x = workspace; ldx = pl->img.Kp; C = pl->img.Kp;

@@ -151,8 +151,8 @@ __device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t (&r)[32])
 constexpr size_t TC_PAIR_MIN_SMEM = 118 * 1024;
 
 // ---------------------------------------------------------------- the checked build (-DUBP_DEBUG)
-// Every index that a kernel takes from the plan or computes for shared or global memory is compared with the extent it
-// has to stay in before it is used. A failing check sets the plan's status word (2: shared memory or plan contents,
+// The indices that a kernel takes from a plan or computes for shared or global memory are compared with the extents they
+// have to stay in before they are used (tensor copies are bounded by their maps). A failing check sets the plan's status word (2: shared memory or plan contents,
 // 3: global memory; the first failure wins) and the access is skipped: nothing traps, the kernel runs to its end and
 // ubp_plan_check reports UBP_E_DEVICE. The ordinary build compiles the checks away.
 #ifdef UBP_DEBUG
