@@ -139,6 +139,17 @@ template <typename T> __device__ __forceinline__ void store4(T *p, int n, bool v
     }
 }
 
+// A block whose waits ran out leaves nothing under way that could still write to the shared or tensor memory it gives up: the
+// threads that issued copies wait for the last ones of every stage, and the warp that issued MMAs for those, a millisecond at
+// most (a stage whose other half was never issued does not complete).
+constexpr uint64_t LT_DRAIN_NS = 1000000;
+__device__ __forceinline__ void drain_copies(const uint64_t *bar_full, int stages, int issued)
+{
+    int gave_up = 0;
+    for (int f = issued > stages ? issued - stages : 0; f < issued; ++f)
+        mbar_wait(smem_u32(&bar_full[f % stages]), (uint32_t)(f / stages) & 1u, &gave_up, LT_DRAIN_NS);
+}
+
 // ------------------------------------------------------------------ few tokens
 constexpr uint32_t FEW_A = 128 * LT_LINE;       // weight lines of one chunk: 16 KB
 // One block an SM (TC_PAIR_MIN_SMEM). Half the shared memory, so that the next launch's blocks could set up and start their
@@ -222,7 +233,7 @@ ubp_linear_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
 {
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
-    __shared__ __align__(8) uint64_t bar_full[LT_MAX_STAGES], bar_empty[LT_MAX_STAGES], bar_acc;
+    __shared__ __align__(8) uint64_t bar_full[LT_MAX_STAGES], bar_empty[LT_MAX_STAGES], bar_acc, bar_drain;
     __shared__ uint32_t tmem_base_slot;
     __shared__ int abort_flag;
 
@@ -253,6 +264,7 @@ ubp_linear_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
         abort_flag = 0;
         for (int s = 0; s < stages; ++s) { mbar_init(smem_u32(&bar_full[s]), 1); mbar_init(smem_u32(&bar_empty[s]), 1); }
         mbar_init(smem_u32(&bar_acc), 1);
+        mbar_init(smem_u32(&bar_drain), 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         for (int f = 0; f < pre; ++f) issue_w(f);
@@ -268,6 +280,7 @@ ubp_linear_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const uint32_t tmem = tmem_base_slot;
     bool ok = true;
+    int issued = 0;                                             // stages that this thread has issued copies for
 
     if (warp == 0 || warp == LT_X_WARP) {
         if (lane == 0) {
@@ -280,11 +293,11 @@ ubp_linear_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
             };
             const bool w = warp == 0;
             asm volatile("griddepcontrol.wait;" ::: "memory");
-            for (int i = w ? pre : 0; i < nst && ok; ++i) {
-                if (i >= stages) ok = mbar_wait(smem_u32(&bar_empty[i % stages]), (uint32_t)(i / stages - 1) & 1u, &abort_flag);
+            for (issued = w ? pre : 0; issued < nst; ++issued) {
+                if (issued >= stages) ok = mbar_wait(smem_u32(&bar_empty[issued % stages]), (uint32_t)(issued / stages - 1) & 1u, &abort_flag);
                 if (!ok) break;
-                if (w) issue_w(i);
-                else issue_x(i);
+                if (w) issue_w(issued);
+                else issue_x(issued);
             }
         }
     } else if (warp == 1) {
@@ -332,6 +345,15 @@ ubp_linear_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_cons
         if (p.ydt == UBP_BF16) few_epilogue<F8, __nv_bfloat16>(p, fc, red, tid, t0, ta, tb, S);
         else if (p.ydt == UBP_F16) few_epilogue<F8, __half>(p, fc, red, tid, t0, ta, tb, S);
         else few_epilogue<F8, float>(p, fc, red, tid, t0, ta, tb, S);
+    }
+    if (*(volatile int *)&abort_flag) {
+        if (issued) drain_copies(bar_full, stages, issued);
+        if (warp == 1) {
+            int gave_up = 0;
+            commit_one(smem_u32(&bar_drain));
+            mbar_wait(smem_u32(&bar_drain), 0, &gave_up, LT_DRAIN_NS);
+        }
+        __syncwarp();
     }
     if (S > 1) cluster_sync();                                  // nobody leaves while its partial sums are being read
     else __syncthreads();
@@ -436,7 +458,7 @@ ubp_linear_many_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     // identical layout in both CTAs: multicast commits and remote arrives address barriers by offset
-    __shared__ __align__(8) uint64_t bar_full[S], bar_peer[S], bar_empty[S], bar_acc_full[2], bar_acc_empty[2];
+    __shared__ __align__(8) uint64_t bar_full[S], bar_peer[S], bar_empty[S], bar_acc_full[2], bar_acc_empty[2], bar_drain;
     __shared__ uint32_t tmem_base_slot;
     __shared__ int abort_flag;
 
@@ -462,6 +484,7 @@ ubp_linear_many_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
             mbar_init(smem_u32(&bar_peer[s]), 1);              // leader: the other CTA's lines have landed
             mbar_init(smem_u32(&bar_empty[s]), 1);
         }
+        mbar_init(smem_u32(&bar_drain), 1);
         for (int b = 0; b < 2; ++b) {
             mbar_init(smem_u32(&bar_acc_full[b]), 1);
             mbar_init(smem_u32(&bar_acc_empty[b]), 2 * LT_EPI_WARPS);    // leader only
@@ -480,6 +503,7 @@ ubp_linear_many_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const uint32_t tmem = tmem_base_slot;
     bool ok = true;
+    int issued = 0;                                             // stages that this thread has issued copies for
 
     if (warp == 0 || warp == LT_X_WARP) {
         if (lane == 0) {
@@ -491,7 +515,7 @@ ubp_linear_many_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
             auto issue_x = [&](int st, int m, int k) {
                 tma_load_2d(smem_u32(smem + (size_t)st * STAGE), &tmX, k * line, m * 256 + (int)rank * 128, smem_u32(&bar_full[st]));
             };
-            int m = 0, n = 0, f = 0;
+            int m = 0, n = 0;
             const bool w = warp == 0;
             const int pre = w && nmy > 0 ? (p.nk < S ? p.nk : S) : 0;  // first tile: the ring's weight lines before the wait
             if (nmy > 0) tile_at(0, m, n);
@@ -500,8 +524,8 @@ ubp_linear_many_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
             int st = 0, round = 0;
             for (int i = 0; i < nmy && ok; ++i) {
                 tile_at(i, m, n);
-                for (int k = 0; k < p.nk; ++k, ++f) {
-                    if (f >= pre) {
+                for (int k = 0; k < p.nk; ++k, ++issued) {
+                    if (issued >= pre) {
                         if (round > 0) {
                             ok = mbar_wait(smem_u32(&bar_empty[st]), (uint32_t)(round - 1) & 1u, &abort_flag);
                             if (!ok) break;
@@ -644,6 +668,15 @@ ubp_linear_many_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_con
     // neither CTA frees tensor memory or leaves while the other could still be the target of the pair's MMAs or commits
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();
+    if (*(volatile int *)&abort_flag) {
+        if (issued) drain_copies(bar_full, S, issued);
+        if (warp == 1 && rank == 0) {
+            int gave_up = 0;
+            mma2_commit_both(smem_u32(&bar_drain));
+            mbar_wait(smem_u32(&bar_drain), 0, &gave_up, LT_DRAIN_NS);
+        }
+        __syncwarp();
+    }
     cluster_sync();
     if (warp == 1) {
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
