@@ -1,6 +1,7 @@
 // extern "C" surface of the token-major products: plan life cycle, argument checks, choice of the kernel.
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstring>
 
 #include "ubp_internal.h"
@@ -69,12 +70,13 @@ LinearChoice linear_choose(const ubp_linear_plan *p, int64_t T, int sms)
 // SMs of the current device (asked once per device)
 int device_sms()
 {
-    static int known[64] = {};
+    static std::atomic<int> known[64] = {};          // (calls come from any thread)
     int dev = 0, sms = 148;
     if (cudaGetDevice(&dev) != cudaSuccess) return sms;
-    if (dev < 64 && known[dev]) return known[dev];
+    if (dev < 64)
+        if (const int n = known[dev].load(std::memory_order_relaxed)) return n;
     if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 148;
-    if (dev < 64) known[dev] = sms;
+    if (dev < 64) known[dev].store(sms, std::memory_order_relaxed);
     return sms;
 }
 

@@ -25,6 +25,7 @@
 // bundle once more without them (two or three instructions a bundle for every other call).
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 #include <type_traits>
 
@@ -391,7 +392,7 @@ template <typename W, int NBK, int TT, int THREADS>
 int launch_n(const SpArgs &p, int64_t chunks, size_t smem, cudaStream_t stream)
 {
     const auto kern = ubp_linear_sparse_kernel<W, NBK, TT, THREADS>;
-    static bool done[64] = {};
+    static std::atomic<bool> done[64] = {};          // (calls come from any thread)
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) dev = -1;
     if (dev < 0 || dev >= 64 || !done[dev]) {

@@ -20,6 +20,7 @@
 #include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 #include <mutex>
 #include <type_traits>
@@ -754,8 +755,8 @@ int encode_x(CUtensorMap *tm, const void *x, int dtype, int64_t ldx, int64_t T, 
 
 int fail(cudaError_t e) { set_last_cuda_error((int)e); return UBP_E_CUDA; }
 
-// dynamic shared memory once per device and kernel; one block per SM (see TC_PAIR_MIN_SMEM)
-template <typename K> int allow_smem(K kern, bool (&done)[64], size_t least)
+// dynamic shared memory once per device and kernel (calls come from any thread); one block per SM (see TC_PAIR_MIN_SMEM)
+template <typename K> int allow_smem(K kern, std::atomic<bool> (&done)[64], size_t least)
 {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) dev = -1;
@@ -773,7 +774,7 @@ template <typename K> int allow_smem(K kern, bool (&done)[64], size_t least)
 template <bool F8>
 int launch_few(const CUtensorMap &tmW, const CUtensorMap &tmX, const TcLinArgs &p, int fmt, int NT, int ntt, int S, cudaStream_t st)
 {
-    static bool done[64] = {};
+    static std::atomic<bool> done[64] = {};
     const auto kern = ubp_linear_few_kernel<F8>;
     if (int rc = allow_smem(kern, done, TC_PAIR_MIN_SMEM)) return rc;
     size_t smem = (size_t)few_stages(NT) * few_stage(NT) + 1024;
@@ -800,7 +801,7 @@ int launch_few(const CUtensorMap &tmW, const CUtensorMap &tmX, const TcLinArgs &
 template <bool F8, int NT, bool VEC8, bool F32>
 int launch_many(const CUtensorMap &tmW, const CUtensorMap &tmX, const TcLinArgs &p, int fmt, int sms, int vec, cudaStream_t st)
 {
-    static bool done[64] = {};
+    static std::atomic<bool> done[64] = {};
     const auto kern = ubp_linear_many_kernel<F8, NT, VEC8, F32>;
     const size_t smem = (size_t)MANY_STAGES * many_stage(NT) + LT_EPI_WARPS * MANY_TURN + 1024;
     static_assert(MANY_STAGES * many_stage(128) + LT_EPI_WARPS * MANY_TURN + 1024 >= TC_PAIR_MIN_SMEM, "one block per SM");

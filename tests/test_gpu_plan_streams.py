@@ -117,3 +117,37 @@ def test_image_plan_dropped_while_another_stream_uses_it(ubp):
             torch.empty(n, device="cuda", dtype=torch.uint8).zero_()
         torch.cuda.synchronize()
         assert torch.equal(got, want)
+
+
+def test_two_threads_use_one_plan_at_once(ubp):
+    """Through the C entry point, which ctypes calls without the interpreter's lock; the kernels' first calls among them."""
+    import threading
+    W, mask = make_weight(2048, 1024, 2, 70, 8)
+    plan = ubp.LinearPlan(ubp.ubp_pack(W, mask, 2), torch.float16)
+    sizes = [1, 2, 5, 24, 200, 2500]
+    x = [torch.randn(T, 1024, device="cuda").half() for T in sizes]
+    L, failed = ubp.load(), []
+    out = [[torch.empty(T, 2048, device="cuda", dtype=torch.float16) for T in sizes] for _ in range(2)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+
+    def work(k):
+        torch.cuda.set_device(0)
+        for _ in range(20):
+            for i, T in enumerate(sizes):
+                rc = L.ubp_linear(plan.handle, x[i].data_ptr(), 1024, None, T, None, 0, None, 0, out[k][i].data_ptr(), 2048, 1, None, 0,
+                                  streams[k].cuda_stream)
+                if rc:
+                    failed.append(rc)
+
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    torch.cuda.synchronize()
+    plan.check()
+    assert not failed
+    for i in range(len(sizes)):
+        want = ubp.ubp_linear(plan, x[i])
+        assert torch.equal(out[0][i], want) and torch.equal(out[1][i], want)
