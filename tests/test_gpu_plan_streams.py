@@ -119,6 +119,28 @@ def test_image_plan_dropped_while_another_stream_uses_it(ubp):
         assert torch.equal(got, want)
 
 
+@pytest.mark.parametrize("dtype", [BF16, F8], ids=["bf16", "e4m3"])
+def test_two_streams_use_one_plan_at_once(ubp, dtype):
+    W, mask = make_weight(2048, 1024, 4, 70, 8)
+    plan = ubp.LinearPlan(ubp.ubp_pack(W, mask, 4), dtype)
+    sizes = [1, 3, 24, 200, 2500]
+    xs = [torch.randn(T, 1024, device="cuda").to(dtype) for T in sizes]
+    sc = [torch.ones(T, device="cuda") if dtype == F8 else None for T in sizes]
+    want = [ubp.ubp_linear(plan, x, x_scales=s) for x, s in zip(xs, sc)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for _ in range(10):
+        for k, st in enumerate(streams):
+            order = range(len(sizes)) if k == 0 else reversed(range(len(sizes)))
+            with torch.cuda.stream(st):
+                got[k] += [(i, ubp.ubp_linear(plan, xs[i], x_scales=sc[i])) for i in order]
+    torch.cuda.synchronize()
+    plan.check()
+    for i, y in got[0] + got[1]:
+        assert torch.equal(y, want[i])
+
+
 def test_two_threads_use_one_plan_at_once(ubp):
     """Through the C entry point, which ctypes calls without the interpreter's lock; the kernels' first calls among them."""
     import threading
@@ -151,3 +173,39 @@ def test_two_threads_use_one_plan_at_once(ubp):
     for i in range(len(sizes)):
         want = ubp.ubp_linear(plan, x[i])
         assert torch.equal(out[0][i], want) and torch.equal(out[1][i], want)
+
+
+@pytest.mark.parametrize("T", [1, 8, 40, 300, 5000])
+@pytest.mark.parametrize("pad", [0, 1])
+def test_calls_are_captured_into_a_graph(ubp, T, pad):
+    """A feed-forward block as one graph: replays read the inputs as they are then and give the values of plain calls."""
+    C, F = 512, 1024
+    Wg, mg = make_weight(2 * F, C, 4, 80, 1)
+    Wd, md = make_weight(C, F, 4, 80, 2)
+    up, down = ubp.LinearPlan(ubp.ubp_pack(Wg, mg, 4), F8, gated=True), ubp.LinearPlan(ubp.ubp_pack(Wd, md, 4), BF16)
+    gamma = torch.ones(C, device="cuda", dtype=BF16)
+    x = torch.randn(T, C + pad, device="cuda").to(BF16)[:, :C]
+    r = torch.randn(T, C, device="cuda").to(BF16)
+
+    def block():
+        q, s, h = ubp.ubp_rmsnorm(x, gamma, 1e-5, residual=r, out_dtype=F8)
+        a = ubp.ubp_linear(up, q, activation="silu", x_scales=s)
+        b = torch.empty(T, F + pad, device="cuda", dtype=BF16)[:, :F]
+        b.copy_(a)
+        p, t = ubp.ubp_quant_rows(b)
+        return ubp.ubp_linear(down, b, residual=h), p, t
+
+    block()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        got = block()
+    for seed in range(3):
+        x.copy_(torch.randn(T, C, device="cuda", generator=torch.Generator(device="cuda").manual_seed(seed)))
+        g.replay()
+        want = block()
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert torch.equal(a.float(), b.float())
+    up.check()
+    down.check()
