@@ -458,8 +458,8 @@ int ubp_linear_plan_clear_status(const ubp_linear_plan_t *plan, void *stream);
  *             an 8-bit one
  *   workspace device, 16-byte aligned, at least ubp_linear_workspace_size(...) bytes of it (0: may be NULL)
  * Products and sums are fp32 (8-bit products are exact in fp32), everything after the sum is fp32, y is rounded once. The
- * activations of UBP_F32 outputs are good to a few units of 2^-23 (gelu_tanh: times its argument), those of 16-bit outputs are
- * approximations within 2^-18 of the value before the activation. Sums
+ * activations of UBP_F32 outputs are good to a few units of 2^-23 (gelu_tanh: times its argument), those of 16-bit outputs to
+ * 2^-15 of their value. Sums
  * run in a fixed order: results are bitwise reproducible. Up to a few tokens the kept blocks are multiplied on the CUDA
  * cores; from there on the densified weight on the tensor cores. y must not overlap x; with residual == y each element is
  * read before it is written.

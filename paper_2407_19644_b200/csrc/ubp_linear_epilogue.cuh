@@ -15,31 +15,34 @@ namespace ubp {
 // every finite v (the exact value is below 2^-120); unstopped it would be infinity, for which no quotient is defined.
 __device__ __forceinline__ float v_sigmoid(float v, float u) { return __fdividef(v, 1.f + __expf(fminf(-u, 88.f))); }
 
-// GELU with erf, 0.5 v (1 + erf(v / sqrt 2)) = max(v, 0) - 0.5 |v| erfc(|v| / sqrt 2). erfc(x) = t (a1 + t (a2 + ...)) e^(-x^2),
-// t = 1 / (1 + p x): Abramowitz and Stegun, Handbook of Mathematical Functions, 7.1.26, |error| <= 1.5 10^-7. Half the
-// instructions of erff, which were what a tile's epilogue waited for (777 tokens on 1500 x 1003: 15.3 us a call, 14.95 this
-// way). max(v, 0) is written as 0.5 v + 0.5 |v|, which keeps a NaN; from |v| = 20 on the second term is 0 (e^-200).
+// GELU with erf, 0.5 v (1 + erf(v / sqrt 2)) = v Phi(v), Phi the normal distribution function; with m = |v|: Phi(-m) =
+// g(m) e^(-m^2 / 2), and g / t is a polynomial in t = 1 / (1 + p m), fitted here to the least relative error on [0, 15] (degree 6,
+// p = 0.265: 6.5 10^-7). Phi(-15) is below 2^-149. Relative errors below 2^-17 down to the smallest results: 1 + erf and
+// approximations of erfc with an absolute error lose the digits of the negative tail (1.5 10^-7 is a quarter of Phi(-5)).
+__device__ __forceinline__ float phi_of(float v, float tail) { return v < 0.f ? tail : 1.f - tail; }
 __device__ __forceinline__ float gelu_erf(float v)
 {
-    const float m = fminf(fabsf(v), 20.f), x = m * 0.70710678118654752f;
-    const float t = __fdividef(1.f, fmaf(0.3275911f, x, 1.f));
-    const float poly = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
-    return fmaf(-0.5f * m, poly * __expf(-x * x), fmaf(0.5f, v, 0.5f * fabsf(v)));
+    const float m = fminf(fabsf(v), 15.f), t = __fdividef(1.f, fmaf(0.265f, m, 1.f));
+    float g = -0.0677110404f;
+    g = fmaf(g, t, 0.195008963f);
+    g = fmaf(g, t, -0.0659952313f);
+    g = fmaf(g, t, 0.142232031f);
+    g = fmaf(g, t, 0.0830461904f);
+    g = fmaf(g, t, 0.107817546f);
+    g = fmaf(g, t, 0.105601303f);
+    return v * phi_of(v, g * t * __expf(-0.5f * m * m));
 }
 
-// FULL: relative errors of a few units of 2^-23 over the whole range (in fp32 the forms above are off by up to 5 10^-5 of a GELU
-// around -3 and by all of it below -5, and __expf loses a unit for every unit of its argument). The exponent is carried in two
-// numbers: x log2(e) = th + tl, e^x = 2^th (1 + tl ln 2).
+// FULL: relative errors of a few units of 2^-23 over the whole range (__expf loses a unit for every unit of its argument). The
+// exponent is carried in two numbers: x log2(e) = th + tl, e^x = 2^th (1 + tl ln 2).
 __device__ __forceinline__ float exp_two(float th, float tl) { return exp2f(th) * fmaf(tl, 0.69314718056f, 1.f); }
 __device__ __forceinline__ float v_sigmoid_full(float v, float u)
 {
     const float x = fmaxf(fminf(-u, 100.f), -100.f), th = x * 1.44269502f;                     // log2(e) = 1.44269502 + 1.9259630e-8
     return __fdividef(v, 1.f + exp_two(th, fmaf(x, 1.9259630e-8f, fmaf(x, 1.44269502f, -th))));
 }
-// v Phi(v), Phi the normal distribution function; with m = |v|: Phi(-m) = g(m) e^(-m^2 / 2), and g / t is a polynomial of degree
-// 8 in t = 1 / (1 + 0.35 m), fitted here to the least relative error on [0, 15] (3.2 10^-8). m^2 is carried in two numbers.
-// Phi(-15) is below 2^-149. (1 + erf would lose the digits of the negative tail. normcdff is as good, but with it 777 tokens on
-// 4096 x 2048 in bf16 took 31.4 us; this 21.7, the 16-bit form 20.9.)
+// v Phi(v) as above with degree 8 and p = 0.35 (3.2 10^-8), m^2 in two numbers. (normcdff is as good, but with it 777 tokens on
+// 4096 x 2048 in bf16 took 31.4 us; this 21.8, the 16-bit form 21.0.)
 __device__ __forceinline__ float gelu_full(float v)
 {
     const float m = fminf(fabsf(v), 15.f), t = __fdividef(1.f, fmaf(0.35f, m, 1.f));
@@ -54,7 +57,7 @@ __device__ __forceinline__ float gelu_full(float v)
     g = fmaf(g, t, 0.139621258f);
     const float h = m * m, l = fmaf(m, m, -h), th = h * -0.72134751f;                            // -log2(e) / 2 = -0.72134751 - 9.629815e-9
     const float tail = g * t * exp_two(th, fmaf(l, -0.72134751f, fmaf(h, -9.629815e-9f, fmaf(h, -0.72134751f, -th))));
-    return v * (v < 0.f ? tail : 1.f - tail);
+    return v * phi_of(v, tail);
 }
 
 // (the choice outside the loop: with the switch inside an unrolled one, all five activations sit in the path N times over and

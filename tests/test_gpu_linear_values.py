@@ -120,3 +120,24 @@ def test_outputs_over_inputs(ubp):
                 lambda: ubp.ubp_rmsnorm(x[:5], gamma, residual=rows, residual_out=tight, out=tight)):
         with pytest.raises(ValueError):
             bad()
+
+
+@pytest.mark.parametrize("act", ["gelu", "gelu_tanh", "silu"])
+@pytest.mark.parametrize("T", [1, 40, 40000])
+@pytest.mark.parametrize("out", [BF16, F16], ids=IDS.get)
+def test_16_bit_outputs_of_activations(ubp, act, T, out):
+    """One rounding of the output on top of the activation's own error: 105 units of 2^-23 of __expf at its largest argument (CUDA:
+    2 + 1.173 |x|), the exponent's rounding 88 x 2^-24 at most, the fit and the rest a few units: below 2^-15 in all. Below
+    2^-118 the forms may give 0."""
+    v = torch.cat([torch.linspace(-12, 12, 1501), torch.linspace(-1, 1, 501), torch.tensor([-90.0, -40.0, -20.0, 20.0, 90.0, 1e4, -1e4, 0.0])]).cuda()
+    if T > 1000:
+        v = v[::40].contiguous()
+    W, mask = make_weight(v.numel(), 64, 1, 50, 5)
+    plan = ubp.LinearPlan(ubp.ubp_pack(W, mask, 1), out)
+    y = ubp.ubp_linear(plan, torch.zeros(T, 64, device="cuda", dtype=out), bias=v, activation=act).double()
+    assert plan.choice(T)[0] == {1: 0, 40: 1, 40000: 2}[T]
+    want = act64(v.double(), act)[0]
+    unit, tiny = (2.0 ** -8, 2.0 ** -118) if out == BF16 else (2.0 ** -11, 2.0 ** -25)
+    err = (y - want).abs()
+    bound = (unit + 2.0 ** -15) * want.abs() + tiny
+    assert (err <= bound).all(), float((err / bound).max())
