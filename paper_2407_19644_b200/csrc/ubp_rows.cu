@@ -189,8 +189,8 @@ __global__ void __launch_bounds__(rows_block(TPR), rows_blocks_per_sm(TPR, NORM,
     const int64_t rounds = ((int64_t)blockIdx.x * ROWS < a.T) ? (a.T - (int64_t)blockIdx.x * ROWS + stride - 1) / stride : 0;
     if constexpr (NV > 0 && E == 1) {
         // Single elements: whole loops under one condition each and no branch an element (with the conditions inside it was 61
-        // instructions an element, which bound the kernel: norm 1531 x 2051 9.7 us, now 7.4). Places past the row stay 0 and count for nothing; gamma stays in
-        // registers from row to row.
+        // instructions an element, which bound the kernel: norm 1531 x 2051 9.7 us, 7.6 so). Places past the row stay 0 and count for
+        // nothing; gamma stays in registers from row to row.
         Raw<T, 1> nx[NV], nr[NORM ? NV : 1];
         float g[NORM ? NV : 1];
 #pragma unroll
@@ -341,13 +341,19 @@ int launch_rows_k(const RowArgs &a, int sms, cudaStream_t stream)
 
 // Threads and accesses a row by its length: the fewest threads whose registers hold it, 32 (a warp a row, no barrier), 128 and
 // more. On 16-byte accesses a row of 513 to 1024 or 2049 to 4096 elements takes four times the threads where the SMs hold every
-// row at once anyway (f16, norm / 8-bit rows: 3 x 1024 1.75 / 1.35 us, on 32 threads 2.5 / 1.54; 3000 x 1024 5.65 / 4.1 on 128,
-// 5.15 / 2.97 on 32; 3 x 4096 norm 2.2 on 512, 2.36 on 256; 16384 x 4096 79.5 / 54.5 on 512, 79.7 / 34.8 on 256).
+// row at once anyway (f16, us, norm with 8-bit rows / 8-bit rows: 3 x 1024 1.77 / 1.39 on 128 threads, 2.56 / 1.54 on 32; 3000 x
+// 1024 6.05 / 4.29 and 5.14 / 3.06; 3 x 4096 norm 2.21 on 512, 2.36 on 256; 16384 x 4096 80.2 / 58.6 and 79.9 / 35.0). Longer
+// ones: 4096 x 8192 37.9 / 19.1 on 512 threads, 43.6 / 25.7 on 1024, 55.2 / 36.9 read twice; 2048 x 16384 38.8 / 16.8, read
+// twice 49.6 / 24.3.
 // Single elements cost their instructions, idle places too, and two to four rows an SM have to be under way: hence the close
-// steps there. f16, 1531 rows, norm / 8-bit rows: 2051 elements 9.7 / 5.5 us with 256 threads (512 threads: 11.6 / 7.8), 4099
-// 16.1 / 9.6 with 512 x 10 (512 x 16, whose registers spill: 28.5 / 16.8), 8191 35.6 / 15.5 with 1024 x 8 (512 x 16: 50.5 /
-// 19.9), 9001 37.7 / 19.1 with 1024 x 10 (read twice: 45.6 / 25.9). At 16 places of 1024 threads reading twice is faster again
-// (12001: rows 33.6 / 44.5). (Measured with branches an element; without them 7.4 / 4.3, 13.6 / 6.9, 30.0 / 13.7, 33.7 / 14.6.)
+// steps there. f16, 1531 rows, us as above:
+//   255 elements     32 x 8 3.17 / 1.88, 128 x 8 4.34 / 3.28          1023   128 x 8 4.81 / 3.41, 256 x 8 6.30 / 3.60
+//   2559             256 x 10 9.61 / 4.51, 512 x 8 11.3 / 6.22        3001   512 x 8 11.6 / 6.32, 512 x 10 12.8 / 6.77
+//   4099             512 x 10 14.8 / 7.14, 512 x 16 24.9 / 8.73, 1024 x 8 21.5 / 11.4
+//   6001             1024 x 8 22.4 / 12.2, 512 x 16 32.4 / 9.38       8191   1024 x 8 29.4 / 13.7, 512 x 16 40.8 / 11.8
+//   9001             1024 x 10 34.0 / 14.4, 1024 x 16 55.5 / 16.9, read twice 45.9 / 30.8
+//   12001            read twice 63.6 / 36.7, 1024 x 16 67.1 / 17.8    16001  read twice 88.8 / 46.5, 1024 x 16 82.7 / 24.9
+// Sixteen places spill with the norm's two inputs and gamma beside them; without a norm they hold the row.
 template <typename T, typename TO, bool NORM>
 int launch_rows_t(const RowArgs &a, bool vec, cudaStream_t st)
 {
@@ -375,8 +381,10 @@ int launch_rows_t(const RowArgs &a, bool vec, cudaStream_t st)
     if (a.C <= 2560) return launch_rows_k<T, TO, NORM, 1, 256, 10>(a, sms, st);
     if (a.C <= 4096) return launch_rows_k<T, TO, NORM, 1, 512, 8>(a, sms, st);
     if (a.C <= 5120) return launch_rows_k<T, TO, NORM, 1, 512, 10>(a, sms, st);
-    if (a.C <= 8192) return launch_rows_k<T, TO, NORM, 1, 1024, 8>(a, sms, st);
+    if (a.C <= 8192) return launch_rows_k<T, TO, NORM, 1, NORM ? 1024 : 512, NORM ? 8 : 16>(a, sms, st);
     if (a.C <= 10240) return launch_rows_k<T, TO, NORM, 1, 1024, 10>(a, sms, st);
+    if constexpr (!NORM)
+        if (a.C <= 16384) return launch_rows_k<T, TO, NORM, 1, 1024, 16>(a, sms, st);
     return launch_rows_k<T, TO, NORM, 1, 512, 0>(a, sms, st);
 }
 

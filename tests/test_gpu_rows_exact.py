@@ -29,7 +29,8 @@ def codes(v, s):
 
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=IDS)
-@pytest.mark.parametrize("T,C,pad", [(4001, 4096, 0), (1531, 2051, 3), (700, 16384, 8), (300, 20001, 1), (9000, 250, 0), (64, 40000, 0)])
+@pytest.mark.parametrize("T,C,pad", [(4001, 4096, 0), (1531, 2051, 3), (700, 16384, 8), (300, 20001, 1), (9000, 250, 0), (64, 40000, 0), (400, 5121, 1), (300, 8191, 1),
+                                     (300, 9001, 1), (300, 10241, 1), (200, 16383, 2)])
 def test_codes_are_the_rounded_quotients(ubp, dtype, T, C, pad):
     g = torch.Generator(device="cuda").manual_seed(T)
     x = torch.empty(T, C + pad, device="cuda", dtype=dtype)[:, :C]
