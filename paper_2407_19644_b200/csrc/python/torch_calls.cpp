@@ -1,6 +1,6 @@
 // Argument checks and output allocation of the token-major calls (ubp_rmsnorm, ubp_quant_rows, ubp_linear), compiled against
-// torch: a call on one token is bound by the host, and marshalling it in Python costs as much as the launch (a product 8.2 us a
-// call through ctypes, of which the library's own part is 3.8; 4.4 here; a norm with 8-bit rows 13.3 and 5.6). The library is still reached through its C
+// torch: a call on one token is bound by the host, and marshalling it in Python cost as much again as the launch (a product 8.2 us
+// a call through ctypes, 4.0 here; a norm with 8-bit rows 13.3 and 5.2). The library is still reached through its C
 // ABI: bind() receives the addresses of its entry points, so that whichever build of it the package loaded is the one that runs.
 // A call returns its outputs, or the library's negative status; refusals of arguments raise ValueError.
 #define PY_SSIZE_T_CLEAN

@@ -23,8 +23,8 @@ namespace ubp {
 //                 a round after the first starts under the one before it: 0.022 / 0.043 a chunk less
 // (The dense forms: 60 layers of 256 .. 18000 rows, 256 .. 8192 channels, bf16 and e4m3, 8 .. 5600 tokens, 1200 launches,
 // error 7 and 11 %. Choosing by them costs 1 % on average over the best of all tiles and splits. A few-token tile of all
-// tokens up to 256 and the pair kernel beyond cost 10 %: 512 x 5000, 1024 tokens, 24.4 us where 128 tokens x 4 parts take 12.1;
-// 2048 x 8192, 24 tokens, 16.3 in 8 parts, two rounds, where 4 parts take 11.0.)
+// tokens up to 256 and the pair kernel beyond cost 10 %: 512 x 5000, 1024 tokens, 24.4 us where 128 tokens x 4 parts take 12.3;
+// 2048 x 8192, 24 tokens, 15.7 in 8 parts, two rounds, where 4 parts take 10.9.)
 // A round is what the SMs hold at once: clusters of 2, 4, 8 blocks leave 0, 16, 28 of the 148 SMs without one
 // (cudaOccupancyMaxActiveClusters).
 LinearChoice linear_choose(const ubp_linear_plan *p, int64_t T, int sms)

@@ -13,7 +13,7 @@
 // coalesced 512-byte load of weights, one of channels, and no test; the lanes' sums join once a bundle. The weights are
 // constants of the layer, so the first steps are loaded before the kernel waits for the one before it, and the next steps'
 // loads are always under way. Forms that were measured before this one, us for a token on 4096 x 4096 at 80 % bf16 /
-// 16384 x 4096 gated e4m3 (this: 3.65 / 6.4): a group of lanes per row in the canonical order, four blocks of a cluster to a
+// 16384 x 4096 gated e4m3 (this: 3.65 / 6.5): a group of lanes per row in the canonical order, four blocks of a cluster to a
 // reduction, 6.9 / 20.4 (chains of dependent loads); a ring of bulk copies in shared memory, 6.7 / 14.0 (a stage holds too few
 // rows for the warps, and its barriers add up); equal shares of the canonical stream to groups of lanes, 5.6 / 12.6 (170
 // instructions a chunk, most of them for finding rows).

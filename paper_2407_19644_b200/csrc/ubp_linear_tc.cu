@@ -4,7 +4,7 @@
 // rows and channels as zeros.
 //
 // ubp_linear_few_kernel -- up to some hundred tokens, and more of them where the pair kernel's large tiles would leave SMs
-//   idle (777 tokens x 1500 x 1003: 120 blocks, 12.2 us; 48 pairs 14.7): bound by reading the dense weight, so every SM has to
+//   idle (777 tokens x 1500 x 1003: 120 blocks, 12.3 us; 48 pairs 14.8): bound by reading the dense weight, so every SM has to
 //   stream.
 //   The weight is the A operand (128 rows of it per block: with tokens as A the tensor core would read 128 mostly empty
 //   rows per MMA for a handful of weight rows), the tokens are B (N = tokens rounded up to 16). S blocks of a cluster split
