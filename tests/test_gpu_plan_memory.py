@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from linear_ref import F8, make_weight
+from linear_ref import make_weight
 
 pytestmark = pytest.mark.gpu
 
