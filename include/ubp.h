@@ -473,6 +473,69 @@ int ubp_linear(const ubp_linear_plan_t *plan, const void *x, int64_t ldx, const 
                int act, const void *residual, int64_t ldr, void *y, int64_t ldy, int y_dtype, void *workspace,
                size_t workspace_bytes, void *stream);
 
+/* ------------------------------------------------ attention over a paged cache
+ * What lies between the query / key / value projection and the output projection of a decoder layer (both of them ubp_linear
+ * calls): norms of query and key heads, position rotation and append to the cache in one call, and attention over the cache.
+ * Inference only; 16-bit types.
+ *
+ * The cache: k and v of [pages][kv_heads][page_size][head_dim] values (any strides, multiples of 8 elements, the same for both;
+ * the head_dim values of a token are contiguous; both pointers 16-byte aligned). Sequence b's tokens p = 0 .. lengths[b] - 1 lie
+ * in page table[b][p / page_size], place p % page_size. Its NEW tokens are the last ones: rows starts[b] .. starts[b + 1] - 1 of
+ * a call's T rows are the tokens at positions lengths[b] - n .. lengths[b] - 1, n = starts[b + 1] - starts[b]; without starts
+ * every sequence has one new token (batch == T). lengths, starts and table are device memory, read when the work runs: a captured
+ * call follows them. Rows from starts[batch] on belong to no sequence: their outputs are left as they were.
+ * Numbers on the device that make no sense do no harm: starts are cut to 0 .. T, lengths to 0 .. table_width * page_size; a page
+ * outside 0 .. pages - 1 reads as zeros and is not written. kv_heads divides the number of query heads; query head h goes with
+ * key head h / (q_heads / kv_heads).
+ * Errors of both calls: UBP_E_ARG (null, sizes, strides, alignment, q_heads not a multiple of kv_heads, batch != T without
+ * starts, types), UBP_E_UNSUPPORTED (head_dim not a multiple of 8 or above 128, page_size not a power of two or below 8),
+ * UBP_E_SPACE, UBP_E_CUDA. T == 0 is a no-op. */
+typedef struct {
+    void *k, *v;                                    /* device */
+    int64_t page_stride, head_stride, token_stride; /* elements */
+    int64_t pages;
+    int page_size, kv_heads, head_dim;
+    int dtype;                                      /* UBP_BF16 or UBP_F16; queries and outputs have it too */
+    const int32_t *table;                           /* device, [batch][table_width], rows table_stride apart */
+    int64_t table_stride;
+    int table_width;
+    int64_t batch;
+    const int32_t *lengths;                         /* device, [batch] */
+    const int32_t *starts;                          /* device, [batch + 1], ascending; or NULL */
+} ubp_cache_t;
+
+/* ubp_rotate_append: qkv, T rows (ld elements apart) of q_heads + 2 kv_heads heads: queries, keys, values.
+ *     u = x / sqrt(mean(x^2) + eps) * gamma            each query head if q_gamma is given, each key head if k_gamma is
+ *     (u_i, u_j) -> (u_i c_i - u_j s_i, u_j c_i + u_i s_i)        query and key heads, i < rotated / 2
+ * with j = i + rotated / 2, or pairs (2 i, 2 i + 1) if interleaved; values from `rotated` on pass. c and s are row p of `rotation`
+ * (device fp32, `positions` rows of rotated / 2 cosines and rotated / 2 sines; NULL: no rotation), p the token's position in its
+ * sequence. The queries go to q (any strides; may be the queries' own place in qkv), keys and values to their places in the cache.
+ * gammas have the cache's type. Arithmetic is fp32, each value is rounded once; eps as in ubp_rmsnorm. A token whose position is
+ * negative or has no row in the rotation is not appended and its queries are 0; one behind the table's end is not appended. Two
+ * tokens with one place (a page given to two sequences) leave either's values. */
+int ubp_rotate_append(const ubp_cache_t *cache, const void *qkv, int64_t ld, int64_t T, int q_heads, const void *q_gamma,
+                      const void *k_gamma, float eps, const float *rotation, int64_t rotation_stride, int64_t positions,
+                      int rotated, int interleaved, void *q, int64_t q_token_stride, int64_t q_head_stride, void *stream);
+
+/* ubp_attention: for the query at position p of its sequence
+ *     o = sum_j w_j v_j / sum_j w_j,  w_j = exp(scale q.k_j),  over j <= p with window == 0 or j > p - window or j < sinks
+ * A query that sees no key (p < 0) gives 0. prefix > 0: the caller states that the first `prefix` tokens are the same for all
+ * sequences; they are read once, through row 0 of the table, for all of them together (the result is that of prefix == 0 up to
+ * rounding). max_new: most new tokens of a sequence, if the caller knows (else T); only the choice of kernel depends on it.
+ * scale > 0. Strides of q and out are between tokens and heads, in elements; heads are contiguous; no alignment beyond the
+ * type's. out must not overlap q or the cache.
+ * Scores, sums and outputs are fp32 until the end; the weights w_j are rounded to the cache's type for the product with v.
+ * Sums run in an order fixed by the lengths: results are bitwise reproducible. What the cache holds outside the tokens that some
+ * query of a sequence sees does not reach its outputs, infinities and NaNs included. An infinity or NaN in a value that some new
+ * tokens of a sequence see and others do not may make these NaN too.
+ * workspace: device, 256-byte aligned, ubp_attention_workspace_size bytes (same arguments); its contents need not be set and
+ * belong to one call at a time. */
+size_t ubp_attention_workspace_size(const ubp_cache_t *cache, int64_t T, int q_heads, int window, int sinks, int64_t prefix,
+                                    int64_t max_new);
+int ubp_attention(const ubp_cache_t *cache, const void *q, int64_t q_token_stride, int64_t q_head_stride, int64_t T, int q_heads,
+                  float scale, int window, int sinks, int64_t prefix, int64_t max_new, void *out, int64_t out_token_stride,
+                  int64_t out_head_stride, void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

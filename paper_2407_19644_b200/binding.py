@@ -25,6 +25,13 @@ class _View(C.Structure):
                 ("indptr", C.POINTER(C.c_int32)), ("indices", C.POINTER(C.c_int32)), ("values", C.POINTER(C.c_float))]
 
 
+class _Cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("token_stride", C.c_int64),
+                ("pages", C.c_int64), ("page_size", C.c_int), ("kv_heads", C.c_int), ("head_dim", C.c_int), ("dtype", C.c_int),
+                ("table", C.c_void_p), ("table_stride", C.c_int64), ("table_width", C.c_int), ("batch", C.c_int64),
+                ("lengths", C.c_void_p), ("starts", C.c_void_p)]
+
+
 class _PlanInfo(C.Structure):
     _fields_ = [("M", C.c_int32), ("C", C.c_int32), ("R", C.c_int32), ("Nb", C.c_int32), ("m", C.c_int32),
                 ("variant", C.c_int32), ("panel_rows", C.c_int32), ("k_tile", C.c_int32),
@@ -99,6 +106,10 @@ def load():
     L.ubp_linear_workspace_size.argtypes = [vp, vp, i64, i64]
     L.ubp_linear_workspace_size.restype = sz
     L.ubp_linear.argtypes = [vp, vp, i64, vp, i64, vp, i32, vp, i64, vp, i64, i32, vp, sz, vp]
+    L.ubp_rotate_append.argtypes = [C.POINTER(_Cache), vp, i64, i64, i32, vp, vp, C.c_float, vp, i64, i64, i32, i32, vp, i64, i64, vp]
+    L.ubp_attention.argtypes = [C.POINTER(_Cache), vp, i64, i64, i64, i32, C.c_float, i32, i32, i64, i64, vp, i64, i64, vp, sz, vp]
+    L.ubp_attention_workspace_size.argtypes = [C.POINTER(_Cache), i64, i32, i32, i32, i64, i64]
+    L.ubp_attention_workspace_size.restype = sz
     _lib = L
     return L
 
@@ -566,7 +577,8 @@ def _native():
         except ImportError as e:
             raise RuntimeError("paper_2407_19644_b200/_torch_calls.so is missing or does not match this torch: build it with "
                                "`python -m paper_2407_19644_b200.build`, or with --force (there is no fallback implementation)") from e
-        _torch_calls.bind(*(C.cast(f, C.c_void_p).value for f in (L.ubp_rmsnorm, L.ubp_quant_rows, L.ubp_linear, L.ubp_linear_workspace_size)))
+        _torch_calls.bind(*(C.cast(f, C.c_void_p).value for f in (L.ubp_rmsnorm, L.ubp_quant_rows, L.ubp_linear, L.ubp_linear_workspace_size,
+                                                                      L.ubp_rotate_append, L.ubp_attention, L.ubp_attention_workspace_size)))
         _calls = _torch_calls
     return _calls
 
@@ -713,4 +725,59 @@ def ubp_linear(plan: LinearPlan, x, bias=None, activation: str = "none", residua
                                      None if stream is None else stream.cuda_stream, workspace)
     if type(r) is int:
         _chk(r, "ubp_linear")
+    return r
+
+
+def rotation_table(positions: int, rotated: int, base: float = 10000.0, scale: float = 1.0, device="cuda"):
+    """The position rotation of ubp_rotate_append: float32 [positions][rotated], cosines and then sines of
+    position * scale * base^(-2 i / rotated), i < rotated / 2. Angles are computed in 64 bits."""
+    import torch
+    if positions < 1 or rotated < 2 or rotated % 2:
+        raise ValueError("positions must be positive and rotated an even number of values")
+    f = base ** (-torch.arange(0, rotated, 2, device=device, dtype=torch.float64) / rotated)
+    angle = torch.arange(positions, device=device, dtype=torch.float64)[:, None] * scale * f
+    return torch.cat([angle.cos(), angle.sin()], 1).float()
+
+
+def ubp_rotate_append(qkv, q_heads: int, k_cache, v_cache, page_table, lengths, starts=None, rotation=None, interleaved: bool = False,
+                      q_gamma=None, k_gamma=None, eps: float = 1e-6, out=None, stream=None):
+    """Rows of a query, key and value projection, qkv [T][(q_heads + 2 kv heads) * head size], into queries and a paged cache: norm of
+    each query and key head (where a gamma [head size] is given), position rotation, append. Returns the queries [T][q_heads][head
+    size]; `out` may be their own place in qkv.
+    k_cache, v_cache: bfloat16 or float16 [pages][kv heads][page size][head size], with equal strides. page_table: int32
+    [sequences][pages of a sequence]; lengths: int32 [sequences], the new tokens among them; starts: int32 [sequences + 1], the rows
+    of sequence b are starts[b] .. starts[b + 1] - 1 and hold its last tokens (None: one new token a sequence). Rows from
+    starts[-1] on are left alone. rotation: float32 [positions][rotated], cosines and sines (rotation_table); interleaved: pairs
+    (2 i, 2 i + 1) instead of (i, i + rotated / 2). No gradient is recorded."""
+    r = (_calls or _native()).rotate_append(qkv, q_heads, k_cache, v_cache, page_table, lengths, starts, rotation, interleaved, q_gamma, k_gamma,
+                                            eps, out, None if stream is None else stream.cuda_stream)
+    if type(r) is int:
+        _chk(r, "ubp_rotate_append")
+    return r
+
+
+def ubp_attention(q, k_cache, v_cache, page_table, lengths, starts=None, window: int = 0, sinks: int = 0, scale: Optional[float] = None,
+                  max_new: Optional[int] = None, out=None, stream=None, workspace=None):
+    """Attention of the new tokens' queries q [T][heads][head size] over a paged cache (k_cache, v_cache, page_table, lengths and starts
+    as in ubp_rotate_append, which appends the new tokens first). The query at position p sees the keys j <= p; with a window only
+    j > p - window, and the first `sinks` tokens. scale: of the scores, 1 / sqrt(head size) unless given. max_new: the most new
+    tokens a sequence has, where the caller knows (a kernel for few rows is taken then; the result does not depend on it).
+    Returns [T][heads][head size]; rows of no sequence are left as they were in `out`. workspace: a CUDA tensor (allocated here when
+    not given). No gradient is recorded."""
+    r = (_calls or _native()).attention(q, k_cache, v_cache, page_table, lengths, starts, 0, window, sinks, scale, max_new, out,
+                                        None if stream is None else stream.cuda_stream, workspace)
+    if type(r) is int:
+        _chk(r, "ubp_attention")
+    return r
+
+
+def ubp_prefix_attention(q, k_cache, v_cache, page_table, lengths, prefix: int, starts=None, window: int = 0, sinks: int = 0,
+                         scale: Optional[float] = None, max_new: Optional[int] = None, out=None, stream=None, workspace=None):
+    """ubp_attention for sequences whose first `prefix` tokens are the same: these are read once, through the table's first row, for all
+    sequences together; then each sequence's own tokens. The result is ubp_attention's up to rounding. prefix need not fill its
+    last page (every sequence's own page then starts with copies of the prefix's last tokens)."""
+    r = (_calls or _native()).attention(q, k_cache, v_cache, page_table, lengths, starts, prefix, window, sinks, scale, max_new, out,
+                                        None if stream is None else stream.cuda_stream, workspace)
+    if type(r) is int:
+        _chk(r, "ubp_prefix_attention")
     return r

@@ -1,4 +1,5 @@
-// Argument checks and output allocation of the token-major calls (ubp_rmsnorm, ubp_quant_rows, ubp_linear), compiled against
+// Argument checks and output allocation of the token-major calls (ubp_rmsnorm, ubp_quant_rows, ubp_linear,
+// ubp_rotate_append, ubp_attention), compiled against
 // torch: a call on one token is bound by the host, and marshalling it in Python cost as much again as the launch (a product 8.2 us
 // a call through ctypes, 4.0 here; a norm with 8-bit rows 13.3 and 5.2). The library is still reached through its C
 // ABI: bind() receives the addresses of its entry points, so that whichever build of it the package loaded is the one that runs.
@@ -15,6 +16,8 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
+#include <cmath>
 #include <cstdint>
 #include <string>
 
@@ -26,6 +29,9 @@ decltype(&ubp_rmsnorm) p_rmsnorm = nullptr;
 decltype(&ubp_quant_rows) p_quant_rows = nullptr;
 decltype(&ubp_linear) p_linear = nullptr;
 decltype(&ubp_linear_workspace_size) p_workspace = nullptr;
+decltype(&ubp_rotate_append) p_rotate_append = nullptr;
+decltype(&ubp_attention) p_attention = nullptr;
+decltype(&ubp_attention_workspace_size) p_attention_workspace = nullptr;
 
 struct Refused {};                      // a Python exception is set
 
@@ -150,13 +156,16 @@ template <typename Fn> PyObject *guarded(Fn &&fn)
 PyObject *bind(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     return guarded([&]() -> PyObject * {
-        count(n, 4);
-        void *p[4];
-        for (int i = 0; i < 4; ++i) if (!(p[i] = PyLong_AsVoidPtr(a[i]))) throw Refused();
+        count(n, 7);
+        void *p[7];
+        for (int i = 0; i < 7; ++i) if (!(p[i] = PyLong_AsVoidPtr(a[i]))) throw Refused();
         p_rmsnorm = reinterpret_cast<decltype(p_rmsnorm)>(p[0]);
         p_quant_rows = reinterpret_cast<decltype(p_quant_rows)>(p[1]);
         p_linear = reinterpret_cast<decltype(p_linear)>(p[2]);
         p_workspace = reinterpret_cast<decltype(p_workspace)>(p[3]);
+        p_rotate_append = reinterpret_cast<decltype(p_rotate_append)>(p[4]);
+        p_attention = reinterpret_cast<decltype(p_attention)>(p[5]);
+        p_attention_workspace = reinterpret_cast<decltype(p_attention_workspace)>(p[6]);
         Py_RETURN_NONE;
     });
 }
@@ -276,12 +285,138 @@ PyObject *linear(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// k_cache, v_cache, page_table, lengths and starts as the library's description of a cache; T rows are given.
+ubp_cache_t cache_of(const at::Tensor *k, const at::Tensor *v, const at::Tensor *table, const at::Tensor *lengths, const at::Tensor *starts, int64_t T)
+{
+    if (!k || !k->is_cuda() || k->dim() != 4 || (k->scalar_type() != at::kBFloat16 && k->scalar_type() != at::kHalf))
+        refuse("k_cache must be a [pages][heads][page size][head size] bfloat16 or float16 CUDA tensor");
+    const int dev = k->get_device();
+    if (!v || !v->is_cuda() || v->get_device() != dev || v->scalar_type() != k->scalar_type() || v->sizes() != k->sizes() || v->strides() != k->strides())
+        refuse("v_cache must have k_cache's type, device, sizes and strides");
+    for (int i = 0; i < 4; ++i) if (k->size(i) < 1 || k->size(i) > INT32_MAX) refuse("k_cache must have pages, heads, tokens and values");
+    if (k->stride(3) != 1 && k->size(3) > 1) refuse("the values of a token in the cache must be contiguous");
+    if (!table || !table->is_cuda() || table->get_device() != dev || table->scalar_type() != at::kInt || table->dim() != 2 ||
+        (table->size(1) > 1 && table->stride(1) != 1) || table->size(1) < 1 || table->size(1) > INT32_MAX)
+        refuse("page_table must be a [sequences][pages of a sequence] int32 tensor with contiguous rows on cuda:" + std::to_string(dev));
+    const int64_t B = table->size(0);
+    if (!lengths) refuse("lengths is required");
+    ubp_cache_t c{};
+    c.k = k->data_ptr(); c.v = v->data_ptr();
+    c.page_stride = k->stride(0); c.head_stride = k->stride(1); c.token_stride = k->stride(2);
+    c.pages = k->size(0); c.kv_heads = (int)k->size(1); c.page_size = (int)k->size(2); c.head_dim = (int)k->size(3);
+    c.dtype = code_of(k->scalar_type());
+    c.table = table->data_ptr<int32_t>(); c.table_stride = table->stride(0); c.table_width = (int)table->size(1);
+    c.batch = B;
+    c.lengths = static_cast<const int32_t *>(vec(*lengths, "lengths", B, at::kInt, dev));
+    if (starts) c.starts = static_cast<const int32_t *>(vec(*starts, "starts", B + 1, at::kInt, dev));
+    else if (T != B) refuse("without starts there is one new token a sequence");
+    // (a stride that is never used may be anything in a tensor, and has to be a possible one here)
+    if (c.page_size == 1) c.token_stride = c.head_dim;
+    if (c.pages == 1) c.page_stride = 0;
+    if (c.kv_heads == 1) c.head_stride = 0;
+    return c;
+}
+// a [T][H][D] tensor of the cache's type and device; strides between tokens and heads
+void heads(const at::Tensor &t, const char *name, int64_t T, int64_t H, int64_t D, at::ScalarType type, int dev, int64_t &ts, int64_t &hs)
+{
+    if (t.dim() != 3 || t.size(0) != T || t.size(1) != H || t.size(2) != D || t.scalar_type() != type || !t.is_cuda() || t.get_device() != dev)
+        refuse(std::string(name) + " must be a [" + std::to_string(T) + "][" + std::to_string(H) + "][" + std::to_string(D) + "] tensor of " +
+               c10::toString(type) + " on cuda:" + std::to_string(dev));
+    ts = T > 1 ? t.stride(0) : H * D;
+    hs = H > 1 ? t.stride(1) : D;
+    if ((D > 1 && t.stride(2) != 1) || hs < D || ts < D) refuse(std::string(name) + " must have contiguous heads that do not overlap");
+}
+at::Tensor make(int64_t T, int64_t H, int64_t D, at::ScalarType type, int dev)
+{
+    return at::detail::empty_cuda({T, H, D}, type, c10::Device(c10::kCUDA, (c10::DeviceIndex)dev), std::nullopt);
+}
+
+// rotate_append(qkv, q_heads, k_cache, v_cache, page_table, lengths, starts, rotation, interleaved, q_gamma, k_gamma, eps, out, stream)
+PyObject *rotate_append(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        count(n, 14);
+        const at::Tensor *qkv = tensor(a[0], "qkv"), *k = tensor(a[2], "k_cache"), *starts = tensor(a[6], "starts"), *rot = tensor(a[7], "rotation"),
+                         *qg = tensor(a[9], "q_gamma"), *kg = tensor(a[10], "k_gamma"), *out = tensor(a[12], "out");
+        const int64_t Hq = PyLong_AsLongLong(a[1]);
+        const int inter = PyObject_IsTrue(a[8]);
+        const double eps = PyFloat_AsDouble(a[11]);
+        if (PyErr_Occurred()) throw Refused();
+        if (!qkv || qkv->dim() != 2) refuse("qkv must be a [T][heads * head size] CUDA tensor");
+        const int64_t T = qkv->size(0);
+        const ubp_cache_t c = cache_of(k, tensor(a[3], "v_cache"), tensor(a[4], "page_table"), tensor(a[5], "lengths"), starts, T);
+        const int dev = k->get_device();
+        const at::ScalarType type = k->scalar_type();
+        if (Hq < 1 || Hq > INT32_MAX || Hq % c.kv_heads) refuse("q_heads must be a multiple of the cache's heads");
+        const int64_t D = c.head_dim, ld = rows(*qkv, "qkv", T, (Hq + 2 * (int64_t)c.kv_heads) * D, type, dev);
+        const void *pqg = qg ? vec(*qg, "q_gamma", D, type, dev) : nullptr, *pkg = kg ? vec(*kg, "k_gamma", D, type, dev) : nullptr;
+        if (rot && (rot->dim() != 2 || rot->scalar_type() != at::kFloat || !rot->is_cuda() || rot->get_device() != dev || rot->size(0) < 1 || rot->size(1) < 2 ||
+                    rot->size(1) > D || rot->size(1) % 2 || rot->stride(1) != 1 || (rot->size(0) > 1 && rot->stride(0) < rot->size(1))))
+            refuse("rotation must be a [positions][rotated values] float32 tensor with contiguous rows on cuda:" + std::to_string(dev) +
+                   ", an even number of them up to the head size");
+        int64_t ts = Hq * D, hs = D;
+        if (out) heads(*out, "out", T, Hq, D, type, dev, ts, hs);
+        On on(dev, a[13]);
+        at::Tensor q;
+        if (!out) q = make(T, Hq, D, type, dev);
+        const int rc = p_rotate_append(&c, qkv->data_ptr(), ld, T, (int)Hq, pqg, pkg, (float)eps, rot ? rot->data_ptr<float>() : nullptr, rot ? rot->stride(0) : 0,
+                                       rot ? rot->size(0) : 0, rot ? (int)rot->size(1) : 0, inter, out ? out->data_ptr() : q.data_ptr(), ts, hs, on.stream);
+        if (rc) return PyLong_FromLong(rc);
+        return give(a[12], std::move(q));
+    });
+}
+
+// attention(q, k_cache, v_cache, page_table, lengths, starts, prefix, window, sinks, scale, max_new, out, stream, workspace)
+PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded([&]() -> PyObject * {
+        count(n, 14);
+        const at::Tensor *q = tensor(a[0], "q"), *k = tensor(a[1], "k_cache"), *starts = tensor(a[5], "starts"), *out = tensor(a[11], "out"),
+                         *ws = tensor(a[13], "workspace");
+        const int64_t prefix = PyLong_AsLongLong(a[6]), window = PyLong_AsLongLong(a[7]), sinks = PyLong_AsLongLong(a[8]);
+        if (PyErr_Occurred()) throw Refused();
+        if (!q || q->dim() != 3) refuse("q must be a [T][heads][head size] CUDA tensor");
+        const int64_t T = q->size(0), Hq = q->size(1);
+        const ubp_cache_t c = cache_of(k, tensor(a[2], "v_cache"), tensor(a[3], "page_table"), tensor(a[4], "lengths"), starts, T);
+        const double scale = a[9] == Py_None ? 1.0 / std::sqrt((double)c.head_dim) : PyFloat_AsDouble(a[9]);
+        const int64_t most = a[10] == Py_None ? std::max<int64_t>(1, starts ? T : 1) : PyLong_AsLongLong(a[10]);
+        if (PyErr_Occurred()) throw Refused();
+        const int dev = k->get_device();
+        const at::ScalarType type = k->scalar_type();
+        if (Hq < 1 || Hq > INT32_MAX || Hq % c.kv_heads) refuse("q's heads must be a multiple of the cache's heads");
+        if (window < 0 || window > INT32_MAX || sinks < 0 || sinks > INT32_MAX) refuse("window and sinks must be numbers of tokens");
+        int64_t qts, qhs, ots = Hq * c.head_dim, ohs = c.head_dim;
+        heads(*q, "q", T, Hq, c.head_dim, type, dev, qts, qhs);
+        if (out) heads(*out, "out", T, Hq, c.head_dim, type, dev, ots, ohs);
+        if (out && T > 0 && out->data_ptr() == q->data_ptr()) refuse("out must not be q: heads of a group read each other's queries");
+        if (ws && (!ws->is_cuda() || ws->get_device() != dev || !ws->is_contiguous())) refuse("workspace must be a contiguous tensor on the cache's device");
+        On on(dev, a[12]);
+        at::Tensor y, room;
+        if (!out) y = make(T, Hq, c.head_dim, type, dev);
+        void *pw = ws ? ws->data_ptr() : nullptr;
+        size_t nws = ws ? ws->numel() * ws->element_size() : 0;
+        if (!ws && (nws = p_attention_workspace(&c, T, (int)Hq, (int)window, (int)sinks, prefix, most)) != 0) {
+            room = make((int64_t)nws, at::kByte, dev);
+            pw = room.data_ptr();
+        }
+        const int rc = p_attention(&c, q->data_ptr(), qts, qhs, T, (int)Hq, (float)scale, (int)window, (int)sinks, prefix, most, out ? out->data_ptr() : y.data_ptr(),
+                                   ots, ohs, pw, nws, on.stream);
+        if (rc) return PyLong_FromLong(rc);
+        return give(a[11], std::move(y));
+    });
+}
+
 PyMethodDef methods[] = {
-    {"bind", (PyCFunction)(void (*)(void))bind, METH_FASTCALL, "addresses of ubp_rmsnorm, ubp_quant_rows, ubp_linear, ubp_linear_workspace_size"},
+    {"bind", (PyCFunction)(void (*)(void))bind, METH_FASTCALL, "addresses of ubp_rmsnorm, ubp_quant_rows, ubp_linear, ubp_linear_workspace_size, ubp_rotate_append, ubp_attention, "
+     "ubp_attention_workspace_size"},
     {"rmsnorm", (PyCFunction)(void (*)(void))rmsnorm, METH_FASTCALL, "rmsnorm(x, gamma, eps, residual, out_dtype, out, scales, residual_out, stream)"},
     {"quant_rows", (PyCFunction)(void (*)(void))quant_rows, METH_FASTCALL, "quant_rows(x, out, scales, stream)"},
     {"linear", (PyCFunction)(void (*)(void))linear, METH_FASTCALL,
      "linear(plan, x, bias, activation, residual, x_scales, out, out_dtype, stream, workspace)"},
+    {"rotate_append", (PyCFunction)(void (*)(void))rotate_append, METH_FASTCALL,
+     "rotate_append(qkv, q_heads, k_cache, v_cache, page_table, lengths, starts, rotation, interleaved, q_gamma, k_gamma, eps, out, stream)"},
+    {"attention", (PyCFunction)(void (*)(void))attention, METH_FASTCALL,
+     "attention(q, k_cache, v_cache, page_table, lengths, starts, prefix, window, sinks, scale, max_new, out, stream, workspace)"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_torch_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

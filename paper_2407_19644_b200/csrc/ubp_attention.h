@@ -1,0 +1,169 @@
+// Attention over a paged cache: what its kernels share -- arguments, the tiles a row block has to visit, and how the steps of a
+// call are dealt to the blocks of a grid.
+//
+// Rows. The query heads that share a key head are rows of one product, together with neighbouring tokens: row r of a row block is
+// token r / gc, head r % gc of a group of gc query heads ("unit head"; a group is the Hq / Hkv heads of a key head, cut into
+// pieces of at most the row block's rows). An item is (sequence, unit head, row block); its steps are the tiles of keys that some
+// of its rows see, at least one (an item whose rows see nothing still writes its zeros).
+//
+// Steps. All items of a call lie one behind the other, sequence by sequence, unit head by unit head, and block c of G takes the
+// steps [c total / G, (c + 1) total / G): every block gets the same number to within one whatever the lengths are, which only
+// the device knows. An item that ends up with several blocks is joined by a second kernel from their partial results.
+#ifndef UBP_ATTENTION_H_
+#define UBP_ATTENTION_H_
+
+#include <cuda_runtime.h>
+
+#include <climits>
+#include <cstddef>
+#include <cstdint>
+
+#include "ubp.h"
+
+#define UBP_HD __host__ __device__ __forceinline__
+
+namespace ubp {
+
+struct AttnArgs {
+    const void *q;
+    int64_t q_ts, q_hs;             // strides of q between tokens and heads (elements)
+    void *out;
+    int64_t o_ts, o_hs;
+    const void *k, *v;
+    int64_t c_ps, c_hs, c_ts;       // strides of the cache between pages, heads and tokens
+    const int32_t *table;
+    int64_t ldt;
+    const int32_t *lengths;
+    const int32_t *starts;          // null: one new token a sequence
+    int pages, pshift, cap;         // cap: tokens a table row holds
+    int T, B, Hq, Hkv, G, D;
+    int rows;                       // rows of a row block, and tokens (rows / gc) of each of its `tiles` tiles
+    int tiles;                      // row tiles of a row block (each rows / tiles rows)
+    int gc, chunks, HU;             // heads of a unit head, unit heads of a key head, unit heads in all
+    int tpt;                        // tokens a row block takes
+    int bn;                         // keys a step takes
+    float sc;                       // scale * log2(e)
+    int window, sinks;
+    int kv0, kv1;                   // keys outside [kv0, kv1) are left out (a shared prefix is a call of its own)
+    int common;                     // 1: the rows are all tokens of all sequences, the pages those of table row 0
+    // partial results: rows x {reference maximum, sum} and rows x D of a slot
+    float2 *ml;
+    float *po;
+    int4 *desc;                     // [grid] the item that begins in a block and does not end there
+    // partial results of the shared prefix, to be joined in (null without one); its call's numbers follow
+    const float2 *pml;
+    const float *ppo;
+    int p_grid, p_rows, p_tiles, p_gc, p_chunks, p_tpt, p_nt;
+};
+
+UBP_HD int imin(int a, int b) { return a < b ? a : b; }
+UBP_HD int imax(int a, int b) { return a > b ? a : b; }
+
+// new tokens of sequence b: [s, s + n) of the call's; len tokens in all (numbers that make no sense are cut to what does)
+struct AttnSeq { int s, n, len; };
+UBP_HD AttnSeq attn_seq(const AttnArgs &a, int b)
+{
+    AttnSeq q;
+    if (a.common) {
+        q.s = 0;
+        q.n = a.starts ? imin(imax(a.starts[a.B], 0), a.T) : a.T;
+        q.len = a.kv1;
+        return q;
+    }
+    if (a.starts) {
+        q.s = imin(imax(a.starts[b], 0), a.T);
+        q.n = imin(imax(a.starts[b + 1], q.s), a.T) - q.s;
+    } else {
+        q.s = b; q.n = 1;
+    }
+    q.len = imin(imax(a.lengths[b], 0), a.cap);
+    return q;
+}
+
+// The tiles of bn keys that a row block with positions p0 .. p1 visits: ns from s0 on (first tokens), the rest from lo on.
+// Keys below w0 are seen by none of the rows unless they are among the first `sinks`, keys from `end` on by none.
+struct AttnTiles { int s0, ns, lo, nt, w0, end; };
+UBP_HD AttnTiles attn_tiles(const AttnArgs &a, int p0, int p1)
+{
+    AttnTiles t;
+    t.end = imin(p1 + 1, a.kv1);
+    t.w0 = a.window > 0 && !a.common ? imax(a.kv0, p0 - a.window + 1) : a.kv0;
+    t.s0 = a.kv0 / a.bn;
+    t.lo = t.w0 / a.bn;
+    t.ns = 0;
+    if (t.end <= a.kv0) { t.end = a.kv0; t.lo = t.s0; t.nt = 1; return t; }
+    if (t.lo > t.s0 && a.sinks > a.kv0) t.ns = imin((imin(a.sinks, t.end) + a.bn - 1) / a.bn - t.s0, t.lo - t.s0);
+    t.nt = t.ns + imax(0, (t.end + a.bn - 1) / a.bn - t.lo);
+    if (t.nt < 1) t.nt = 1;
+    return t;
+}
+UBP_HD int attn_tile_at(const AttnTiles &t, int i) { return i < t.ns ? t.s0 + i : t.lo + i - t.ns; }
+
+UBP_HD int attn_row_blocks(const AttnArgs &a, const AttnSeq &q) { return (q.n + a.tpt - 1) / a.tpt; }
+UBP_HD AttnTiles attn_block_tiles(const AttnArgs &a, const AttnSeq &q, int rt)
+{
+    if (a.common) return attn_tiles(a, 0, a.kv1 - 1);
+    const int first = q.len - q.n + rt * a.tpt, last = q.len - q.n + imin(q.n, (rt + 1) * a.tpt) - 1;
+    return attn_tiles(a, first, last);
+}
+
+// Where a block is in its steps: an item, and the next of its tiles.
+struct AttnCursor {
+    int b, hu, rt, tile;
+    AttnSeq q;
+    AttnTiles t;
+    UBP_HD void set(const AttnArgs &a, int b_, int hu_, int rt_, int tile_)
+    {
+        b = b_; hu = hu_; rt = rt_; tile = tile_;
+        q = attn_seq(a, b);
+        t = attn_block_tiles(a, q, rt);
+    }
+    UBP_HD void next_item(const AttnArgs &a)        // (only while steps are left: there is a next item)
+    {
+        tile = 0;
+        if (++rt * a.tpt >= q.n) {
+            rt = 0;
+            if (++hu == a.HU) {
+                hu = 0;
+                do q = attn_seq(a, ++b); while (q.n == 0);
+            }
+        }
+        t = attn_block_tiles(a, q, rt);
+    }
+    UBP_HD void next(const AttnArgs &a, bool more)
+    {
+        if (++tile == t.nt && more) next_item(a);
+    }
+};
+
+UBP_HD int64_t attn_first_step(int64_t total, int c, int grid) { return total / grid * c + total % grid * c / grid; }
+// block that has step x (grid <= total): the last one whose first step is not behind x
+UBP_HD int attn_owner(int64_t total, int64_t x, int grid)
+{
+    int c = (int)((double)x / (double)total * grid);
+    c = imin(imax(c, 0), grid - 1);
+    while (c > 0 && attn_first_step(total, c, grid) > x) --c;
+    while (c + 1 < grid && attn_first_step(total, c + 1, grid) <= x) ++c;
+    return c;
+}
+
+// slots of partial results that a call needs, and its workspace: [desc][ml][po]
+struct AttnSpace { size_t ml, po, total; };
+inline AttnSpace attn_space(int64_t grid, int64_t slots, int rows, int D)
+{
+    AttnSpace s;
+    auto up = [](size_t n) { return (n + 255) / 256 * 256; };
+    s.ml = up((size_t)grid * sizeof(int4));
+    s.po = s.ml + up((size_t)slots * rows * sizeof(float2));
+    s.total = s.po + up((size_t)slots * rows * D * sizeof(float));
+    return s;
+}
+
+// ---- launches; both kernels follow the same scheme and leave the same partial results
+int launch_attn_few(const AttnArgs &a, int dtype, int grid, void *stream);       // 16 rows an item (ubp_attention_few.cu)
+int launch_attn_join(const AttnArgs &a, int dtype, int grid, void *stream);
+int device_sms();
+void set_last_cuda_error(int e);
+
+}  // namespace ubp
+#endif

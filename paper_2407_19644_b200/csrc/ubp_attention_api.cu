@@ -1,0 +1,149 @@
+// C entry points of the attention operators: argument checks, choice of kernel and grid, workspace.
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "ubp_attention.h"
+#include "ubp_types.cuh"
+
+namespace ubp {
+namespace {
+
+bool on(const void *p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
+int log2_of(int n) { int s = 0; while ((1 << s) < n) ++s; return s; }
+
+}  // namespace
+
+// What every call on a cache asks of it. B sequences; T new tokens.
+int check_cache(const ubp_cache_t *c, int64_t T, int q_heads)
+{
+    if (!c) return UBP_E_ARG;
+    if (c->dtype != UBP_BF16 && c->dtype != UBP_F16) return UBP_E_ARG;
+    if (c->batch < 0 || T < 0 || c->kv_heads < 1 || q_heads < 1 || c->head_dim < 1 || c->page_size < 1 || c->pages < 1 || c->table_width < 1) return UBP_E_ARG;
+    if (q_heads % c->kv_heads) return UBP_E_ARG;
+    if (!c->starts && c->batch != T) return UBP_E_ARG;
+    if (c->head_dim % 8 || c->head_dim > 128 || c->page_size < 8 || (c->page_size & (c->page_size - 1))) return UBP_E_UNSUPPORTED;
+    if (T > INT32_MAX || c->batch >= INT32_MAX || c->pages > INT32_MAX) return UBP_E_UNSUPPORTED;
+    if (T == 0 || c->batch == 0) return UBP_OK;
+    if (!c->k || !c->v || !c->table || !c->lengths) return UBP_E_ARG;
+    if (!on(c->k, 16) || !on(c->v, 16) || !on(c->table, 4) || !on(c->lengths, 4) || !on(c->starts, 4)) return UBP_E_ARG;
+    const int D = c->head_dim;
+    if (c->page_stride % 8 || c->head_stride % 8 || c->token_stride % 8) return UBP_E_ARG;
+    if (c->token_stride < D || (c->kv_heads > 1 && c->head_stride < D) || (c->pages > 1 && c->page_stride < D)) return UBP_E_ARG;
+    if (c->batch > 1 && c->table_stride < c->table_width) return UBP_E_ARG;
+    return UBP_OK;
+}
+
+namespace {
+
+// Rows of an item and how the heads of a group are dealt to them.
+void set_rows(AttnArgs &a, int rows, int tiles, int bn)
+{
+    const int per = rows / tiles;
+    a.rows = rows; a.tiles = tiles; a.bn = bn;
+    a.chunks = (a.G + per - 1) / per;
+    a.gc = (a.G + a.chunks - 1) / a.chunks;
+    a.HU = a.Hq / a.G * a.chunks;
+    a.tpt = per / a.gc * tiles;
+}
+
+// A call's kernels, grids and the layout of its workspace; the same for the size query and the call.
+struct AttnCall {
+    AttnArgs own, common;
+    int own_grid = 0, common_grid = 0;
+    AttnSpace own_space{}, common_space{};
+    size_t bytes = 0;
+};
+
+int attn_plan(const ubp_cache_t *c, int64_t T, int q_heads, float scale, int window, int sinks, int64_t prefix, int64_t max_new, AttnCall &p)
+{
+    const int sms = device_sms();
+    AttnArgs a{};
+    a.T = (int)T; a.B = (int)c->batch; a.Hq = q_heads; a.Hkv = c->kv_heads; a.G = q_heads / c->kv_heads; a.D = c->head_dim;
+    a.k = c->k; a.v = c->v;
+    a.c_ps = c->page_stride; a.c_hs = c->head_stride; a.c_ts = c->token_stride;
+    a.table = c->table; a.ldt = c->batch > 1 ? c->table_stride : 0;
+    a.lengths = c->lengths; a.starts = c->starts;
+    a.pages = (int)c->pages; a.pshift = log2_of(c->page_size);
+    a.cap = (int)std::min<int64_t>((int64_t)c->table_width << a.pshift, INT32_MAX - 4096);
+    a.sc = scale * 1.44269504088896340736f;
+    a.window = window; a.sinks = window > 0 ? sinks : 0;
+    a.kv0 = (int)prefix; a.kv1 = INT32_MAX;
+    set_rows(a, 16, 1, 128);
+    (void)max_new;
+    // more blocks than steps would have nothing to do
+    const int64_t seen = window > 0 ? std::min<int64_t>(a.cap, (int64_t)window + sinks + a.tpt + 2 * a.bn) : a.cap;
+    const int64_t items = (a.T / a.tpt + (int64_t)a.B) * a.HU;
+    p.own_grid = (int)std::min<int64_t>(sms, items * ((seen + a.bn - 1) / a.bn + 1));
+    p.own_space = attn_space(p.own_grid, 2 * (int64_t)p.own_grid, a.rows, a.D);
+    p.bytes = p.own_space.total;
+    if (prefix > 0) {
+        AttnArgs b = a;
+        b.common = 1;
+        b.kv0 = 0; b.kv1 = (int)prefix;
+        set_rows(b, 16, 1, 128);
+        const int64_t units = (int64_t)((b.T + b.tpt - 1) / b.tpt) * b.HU;
+        const int nt = (int)((prefix + b.bn - 1) / b.bn);
+        p.common_grid = (int)std::min<int64_t>(sms, units * nt);
+        p.common_space = attn_space(p.common_grid, units + p.common_grid, b.rows, b.D);
+        p.bytes += p.common_space.total;
+        a.p_grid = p.common_grid; a.p_rows = b.rows; a.p_tiles = b.tiles; a.p_gc = b.gc; a.p_chunks = b.chunks; a.p_tpt = b.tpt; a.p_nt = nt;
+        p.common = b;
+    }
+    p.own = a;
+    return UBP_OK;
+}
+
+int check_attention(const ubp_cache_t *c, int64_t T, int q_heads, float scale, int window, int sinks, int64_t prefix, int64_t max_new)
+{
+    if (const int rc = check_cache(c, T, q_heads)) return rc;
+    if (!(scale > 0.f) || !std::isfinite(scale) || window < 0 || sinks < 0 || max_new < 1) return UBP_E_ARG;
+    if (prefix < 0 || prefix > (int64_t)c->table_width * c->page_size) return UBP_E_ARG;
+    if (prefix > INT32_MAX - 4096) return UBP_E_UNSUPPORTED;
+    return UBP_OK;
+}
+
+}  // namespace
+}  // namespace ubp
+
+extern "C" size_t ubp_attention_workspace_size(const ubp_cache_t *cache, int64_t T, int q_heads, int window, int sinks, int64_t prefix, int64_t max_new)
+{
+    if (ubp::check_attention(cache, T, q_heads, 1.f, window, sinks, prefix, max_new) || T == 0 || cache->batch == 0) return 0;
+    ubp::AttnCall p;
+    return ubp::attn_plan(cache, T, q_heads, 1.f, window, sinks, prefix, max_new, p) ? 0 : p.bytes;
+}
+
+extern "C" int ubp_attention(const ubp_cache_t *cache, const void *q, int64_t q_token_stride, int64_t q_head_stride, int64_t T, int q_heads,
+                             float scale, int window, int sinks, int64_t prefix, int64_t max_new, void *out, int64_t out_token_stride,
+                             int64_t out_head_stride, void *workspace, size_t workspace_bytes, void *stream)
+{
+    using namespace ubp;
+    if (const int rc = check_attention(cache, T, q_heads, scale, window, sinks, prefix, max_new)) return rc;
+    if (T == 0 || cache->batch == 0) return UBP_OK;
+    if (!q || !out || !on(q, 2) || !on(out, 2)) return UBP_E_ARG;
+    const int D = cache->head_dim;
+    if ((q_heads > 1 && (q_head_stride < D || out_head_stride < D)) || (T > 1 && (q_token_stride < D || out_token_stride < D))) return UBP_E_ARG;
+    AttnCall p;
+    if (const int rc = attn_plan(cache, T, q_heads, scale, window, sinks, prefix, max_new, p)) return rc;
+    if (!workspace || !on(workspace, 256)) return UBP_E_ARG;
+    if (workspace_bytes < p.bytes) return UBP_E_SPACE;
+    uint8_t *w = static_cast<uint8_t *>(workspace);
+    auto finish = [&](AttnArgs &a, const AttnSpace &s) {
+        a.q = q; a.q_ts = q_token_stride; a.q_hs = q_head_stride;
+        a.out = out; a.o_ts = out_token_stride; a.o_hs = out_head_stride;
+        a.desc = reinterpret_cast<int4 *>(w);
+        a.ml = reinterpret_cast<float2 *>(w + s.ml);
+        a.po = reinterpret_cast<float *>(w + s.po);
+        w += s.total;
+    };
+    finish(p.own, p.own_space);
+    if (prefix > 0) {
+        finish(p.common, p.common_space);
+        p.own.pml = p.common.ml;
+        p.own.ppo = p.common.po;
+        if (const int rc = launch_attn_few(p.common, cache->dtype, p.common_grid, stream)) return rc;
+    }
+    if (const int rc = launch_attn_few(p.own, cache->dtype, p.own_grid, stream)) return rc;
+    return launch_attn_join(p.own, cache->dtype, p.own_grid, stream);
+}
