@@ -530,11 +530,19 @@ int ubp_rotate_append(const ubp_cache_t *cache, const void *qkv, int64_t ld, int
  * tokens of a sequence see and others do not may make these NaN too.
  * workspace: device, 256-byte aligned, ubp_attention_workspace_size bytes (same arguments); its contents need not be set and
  * belong to one call at a time. */
+/* ubp_attention_choice: which kernel a call takes for the sequences' own tokens, and for the shared prefix (-1 without one): 0 =
+ * blocks of 16 rows (tokens times heads of a group), bound by reading the cache, 1 = blocks of 256 rows on the tensor cores.
+ * ubp_attention_check synchronises `stream` and returns UBP_E_DEVICE if a kernel of kind 1 on the current device has reported a
+ * bounded wait that ran out (its call's outputs are then incomplete); ubp_attention_clear_status takes the report back. */
 size_t ubp_attention_workspace_size(const ubp_cache_t *cache, int64_t T, int q_heads, int window, int sinks, int64_t prefix,
                                     int64_t max_new);
 int ubp_attention(const ubp_cache_t *cache, const void *q, int64_t q_token_stride, int64_t q_head_stride, int64_t T, int q_heads,
                   float scale, int window, int sinks, int64_t prefix, int64_t max_new, void *out, int64_t out_token_stride,
                   int64_t out_head_stride, void *workspace, size_t workspace_bytes, void *stream);
+int ubp_attention_choice(const ubp_cache_t *cache, int64_t T, int q_heads, int64_t prefix, int64_t max_new, int *kernel,
+                         int *prefix_kernel);
+int ubp_attention_check(void *stream);
+int ubp_attention_clear_status(void *stream);
 
 #ifdef __cplusplus
 }

@@ -110,6 +110,9 @@ def load():
     L.ubp_attention.argtypes = [C.POINTER(_Cache), vp, i64, i64, i64, i32, C.c_float, i32, i32, i64, i64, vp, i64, i64, vp, sz, vp]
     L.ubp_attention_workspace_size.argtypes = [C.POINTER(_Cache), i64, i32, i32, i32, i64, i64]
     L.ubp_attention_workspace_size.restype = sz
+    L.ubp_attention_choice.argtypes = [C.POINTER(_Cache), i64, i32, i64, i64, C.POINTER(i32), C.POINTER(i32)]
+    L.ubp_attention_check.argtypes = [vp]
+    L.ubp_attention_clear_status.argtypes = [vp]
     _lib = L
     return L
 
@@ -781,3 +784,12 @@ def ubp_prefix_attention(q, k_cache, v_cache, page_table, lengths, prefix: int, 
     if type(r) is int:
         _chk(r, "ubp_prefix_attention")
     return r
+
+
+def attention_check(stream=None):
+    """Synchronise the stream and raise if an attention kernel on the current device reported a failed bounded wait."""
+    _chk(load().ubp_attention_check(_stream_ptr(stream)), "ubp_attention_check")
+
+
+def attention_clear_status(stream=None):
+    _chk(load().ubp_attention_clear_status(_stream_ptr(stream)), "ubp_attention_clear_status")

@@ -161,6 +161,7 @@ inline AttnSpace attn_space(int64_t grid, int64_t slots, int rows, int D)
 
 // ---- launches; both kernels follow the same scheme and leave the same partial results
 int launch_attn_few(const AttnArgs &a, int dtype, int grid, void *stream);       // 16 rows an item (ubp_attention_few.cu)
+int launch_attn_tc(const AttnArgs &a, int dtype, int grid, void *stream);        // 256 rows an item (ubp_attention_tc.cu)
 int launch_attn_join(const AttnArgs &a, int dtype, int grid, void *stream);
 int device_sms();
 void set_last_cuda_error(int e);

@@ -51,6 +51,7 @@ void set_rows(AttnArgs &a, int rows, int tiles, int bn)
 // A call's kernels, grids and the layout of its workspace; the same for the size query and the call.
 struct AttnCall {
     AttnArgs own, common;
+    bool own_tc = false, common_tc = false;
     int own_grid = 0, common_grid = 0;
     AttnSpace own_space{}, common_space{};
     size_t bytes = 0;
@@ -70,8 +71,9 @@ int attn_plan(const ubp_cache_t *c, int64_t T, int q_heads, float scale, int win
     a.sc = scale * 1.44269504088896340736f;
     a.window = window; a.sinks = window > 0 ? sinks : 0;
     a.kv0 = (int)prefix; a.kv1 = INT32_MAX;
-    set_rows(a, 16, 1, 128);
-    (void)max_new;
+    p.own_tc = std::min<int64_t>(max_new, T) * a.G > 16;
+    if (p.own_tc) set_rows(a, 256, 2, 128);
+    else set_rows(a, 16, 1, 128);
     // more blocks than steps would have nothing to do
     const int64_t seen = window > 0 ? std::min<int64_t>(a.cap, (int64_t)window + sinks + a.tpt + 2 * a.bn) : a.cap;
     const int64_t items = (a.T / a.tpt + (int64_t)a.B) * a.HU;
@@ -82,7 +84,9 @@ int attn_plan(const ubp_cache_t *c, int64_t T, int q_heads, float scale, int win
         AttnArgs b = a;
         b.common = 1;
         b.kv0 = 0; b.kv1 = (int)prefix;
-        set_rows(b, 16, 1, 128);
+        p.common_tc = T * b.G > 16;
+        if (p.common_tc) set_rows(b, 256, 2, 128);
+        else set_rows(b, 16, 1, 128);
         const int64_t units = (int64_t)((b.T + b.tpt - 1) / b.tpt) * b.HU;
         const int nt = (int)((prefix + b.bn - 1) / b.bn);
         p.common_grid = (int)std::min<int64_t>(sms, units * nt);
@@ -114,6 +118,18 @@ extern "C" size_t ubp_attention_workspace_size(const ubp_cache_t *cache, int64_t
     return ubp::attn_plan(cache, T, q_heads, 1.f, window, sinks, prefix, max_new, p) ? 0 : p.bytes;
 }
 
+extern "C" int ubp_attention_choice(const ubp_cache_t *cache, int64_t T, int q_heads, int64_t prefix, int64_t max_new, int *kernel, int *prefix_kernel)
+{
+    using namespace ubp;
+    if (const int rc = check_attention(cache, T, q_heads, 1.f, 0, 0, prefix, max_new)) return rc;
+    if (!kernel || !prefix_kernel) return UBP_E_ARG;
+    AttnCall p;
+    if (const int rc = attn_plan(cache, T, q_heads, 1.f, 0, 0, prefix, max_new, p)) return rc;
+    *kernel = p.own_tc;
+    *prefix_kernel = prefix > 0 ? (int)p.common_tc : -1;
+    return UBP_OK;
+}
+
 extern "C" int ubp_attention(const ubp_cache_t *cache, const void *q, int64_t q_token_stride, int64_t q_head_stride, int64_t T, int q_heads,
                              float scale, int window, int sinks, int64_t prefix, int64_t max_new, void *out, int64_t out_token_stride,
                              int64_t out_head_stride, void *workspace, size_t workspace_bytes, void *stream)
@@ -142,8 +158,8 @@ extern "C" int ubp_attention(const ubp_cache_t *cache, const void *q, int64_t q_
         finish(p.common, p.common_space);
         p.own.pml = p.common.ml;
         p.own.ppo = p.common.po;
-        if (const int rc = launch_attn_few(p.common, cache->dtype, p.common_grid, stream)) return rc;
+        if (const int rc = (p.common_tc ? launch_attn_tc : launch_attn_few)(p.common, cache->dtype, p.common_grid, stream)) return rc;
     }
-    if (const int rc = launch_attn_few(p.own, cache->dtype, p.own_grid, stream)) return rc;
+    if (const int rc = (p.own_tc ? launch_attn_tc : launch_attn_few)(p.own, cache->dtype, p.own_grid, stream)) return rc;
     return launch_attn_join(p.own, cache->dtype, p.own_grid, stream);
 }

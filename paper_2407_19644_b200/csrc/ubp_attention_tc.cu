@@ -1,0 +1,525 @@
+// Attention of many query rows over a paged cache on the tensor cores: prompts, their continuations, and a prefix that a batch
+// shares.
+//
+//   S = Q K^T (128 rows x 128 keys, fp32 in tensor memory), P = 2^(S scale log2e - m) in 16 bits, O = O + P V (fp32 in tensor memory)
+//
+// A block owns 256 rows (tokens times heads of a group) in two tiles of 128 that share the staged keys and values: while one
+// tile's scores go through the softmax, the tensor cores work on the other's products. Eight warps hold the softmax, a thread a
+// row: scores come from tensor memory, weights go back over them and are the second product's A operand from there; nothing passes
+// through shared memory. One warp issues the products, one the copies: a page of the cache is a TMA box (64 values x tokens), in
+// the 128-byte swizzle, so that K is the K-major and V the MN-major operand as they lie in the cache.
+// O is rescaled only when a score lies more than 2^8 above the row's reference (weights stay below 2^8, sums far from overflow);
+// the sum over the weights takes them before they are rounded to 16 bits.
+// Steps are dealt to the blocks as in ubp_attention.h: one block an SM, the same number of key tiles for each.
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <atomic>
+#include <mutex>
+#include <type_traits>
+
+#include "ubp_attention_steps.cuh"
+#include "ubp_tc_common.cuh"
+
+namespace ubp {
+
+__device__ int attn_status_word;         // 1: a bounded wait ran out
+
+namespace {
+
+using namespace tc;
+
+constexpr int AT_BN = 128, AT_TILE = 128, AT_THREADS = 320;
+constexpr int AT_COPY_WARP = 8, AT_MMA_WARP = 9;
+constexpr uint32_t AT_PANEL = 128 * 128;                       // 128 rows of 64 values
+constexpr uint32_t AT_SWZ = 2;                                 // 128-byte swizzle
+__host__ __device__ constexpr int at_stages(int dp) { return dp == 128 ? 2 : 4; }
+__host__ __device__ constexpr uint32_t at_part(int dp) { return (uint32_t)(dp / 64) * AT_PANEL; }
+__host__ __device__ constexpr uint32_t at_smem(int dp) { return (2 + 2 * (uint32_t)at_stages(dp)) * at_part(dp) + 1024; }
+static_assert(at_smem(64) >= TC_PAIR_MIN_SMEM, "one block an SM: a block holds all tensor memory");
+
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *tm, int c0, int c1, int c2, int c3, uint32_t bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+        ::"r"(dst), "l"(tm), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar) : "memory");
+}
+// D (tensor memory) (+)= A B: A from shared memory, or the 16-bit values of tensor memory from column `a` on
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+{
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
+        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+          "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+          "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// instruction descriptor: D = f32, A and B of one 16-bit type (0 = f16, 1 = bf16), A K-major, M = 128
+__device__ __forceinline__ uint32_t at_idesc(int n, int fmt, int b_mn)
+{
+    return (1u << 4) | ((uint32_t)fmt << 7) | ((uint32_t)fmt << 10) | ((uint32_t)b_mn << 16) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(128 >> 4) << 24);
+}
+
+struct AtBars {
+    uint64_t q_full[2], s_full[2], p_full[2], o_full[2];
+    uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], patch, drain;
+};
+
+// Segments of a block's steps: consecutive tiles of one item.
+struct AtSegments {
+    AttnCursor cur;
+    int64_t left;
+    int tile0, n;
+    __device__ __forceinline__ bool get()
+    {
+        if (left <= 0) return false;
+        tile0 = cur.tile;
+        n = (int)(cur.t.nt - cur.tile < left ? cur.t.nt - cur.tile : left);
+        return true;
+    }
+    __device__ __forceinline__ void done(const AttnArgs &a)
+    {
+        left -= n;
+        if (left > 0) cur.next_item(a);
+    }
+    // whether the item's second tile has rows
+    __device__ __forceinline__ bool two(const AttnArgs &a) const { return cur.q.n - cur.rt * a.tpt > a.tpt / 2; }
+};
+
+template <typename T, int DP>
+__global__ void __launch_bounds__(AT_THREADS, 1)
+ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const AttnArgs a)
+{
+    constexpr int ST = at_stages(DP);
+    constexpr uint32_t PART = at_part(DP);
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    __shared__ __align__(8) AtBars bars;
+    __shared__ AttnPlace place;
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_flag;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (threadIdx.x == 0) {
+        prefetch_tensormap(&tmK);
+        prefetch_tensormap(&tmV);
+        abort_flag = 0;
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&bars.q_full[i]), 4);
+            mbar_init(smem_u32(&bars.s_full[i]), 1);
+            mbar_init(smem_u32(&bars.p_full[i]), 4);
+            mbar_init(smem_u32(&bars.o_full[i]), 1);
+        }
+        for (int i = 0; i < ST; ++i) {
+            mbar_init(smem_u32(&bars.k_full[i]), 1);
+            mbar_init(smem_u32(&bars.k_empty[i]), 1);
+            mbar_init(smem_u32(&bars.v_full[i]), 1);
+            mbar_init(smem_u32(&bars.v_empty[i]), 1);
+        }
+        mbar_init(smem_u32(&bars.patch), 1);
+        mbar_init(smem_u32(&bars.drain), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == AT_MMA_WARP) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&tmem_slot)), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tmem_before();
+    __syncthreads();
+    tmem_after();
+    const uint32_t tmem = tmem_slot;
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+
+    int64_t total, first;
+    int grid;
+    AtSegments sg;
+    bool ok = true;
+    int filled = 0;                        // copy warp: stages filled so far (keys and values alike)
+    if (!attn_locate(a, place, total, first, sg.left, grid, sg.cur)) {
+        sg.left = 0;
+        if (threadIdx.x == 0 && !a.common) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
+    }
+    const int64_t count = sg.left;
+    const uint32_t s_q = smem_u32(smem), s_k = s_q + 2 * PART, s_v = s_k + ST * PART;
+
+    if (warp == AT_COPY_WARP) {
+        const int page_mask = (1 << a.pshift) - 1, box = imin(1 << a.pshift, AT_BN), nbox = AT_BN / box;
+        int patches = 0;
+        for (; ok && sg.get(); sg.done(a)) {
+            const int kvh = sg.cur.hu / a.chunks;
+            const int32_t *row = a.table + (a.common ? 0 : (int64_t)sg.cur.b * a.ldt);
+            const AttnTiles &t = sg.cur.t;
+            for (int i = 0; ok && i < sg.n; ++i, ++filled) {
+                const int st = filled % ST, j0 = attn_tile_at(t, sg.tile0 + i) * AT_BN;
+                // the boxes of this tile, a lane each: a page that no row sees a key of, or that the cache does not have, is
+                // out of range for the copy and comes as zeros
+                auto page_at = [&](int u) {
+                    const int j = j0 + u * box;
+                    if (j >= t.end || j + box <= a.kv0 || (j + box <= t.w0 && j >= a.sinks)) return a.pages;
+                    const int p = row[j >> a.pshift];
+                    return (uint32_t)p < (uint32_t)a.pages ? p : a.pages;
+                };
+                const int page = __shfl_sync(0xffffffffu, lane < nbox ? page_at(lane) : a.pages, lane % nbox);
+                // Places of a page whose keys no row sees: whatever they hold, a weight of 0 times it has to be 0, so the values
+                // there are overwritten with zeros before the product reads them.
+                const bool patch = (j0 + AT_BN > t.end && (t.end & (box - 1))) || (j0 < a.kv0 && j0 + AT_BN > a.kv0 && (a.kv0 & (box - 1))) ||
+                                   (j0 < t.w0 && j0 + AT_BN > t.w0) || (j0 < a.sinks && j0 + AT_BN > a.sinks && j0 < t.w0);
+                for (int kv = 0; ok && kv < 2; ++kv) {
+                    const uint32_t full = smem_u32(kv ? &bars.v_full[st] : &bars.k_full[st]), empty = smem_u32(kv ? &bars.v_empty[st] : &bars.k_empty[st]);
+                    const uint32_t dst = (kv ? s_v : s_k) + (uint32_t)st * PART;
+                    const uint32_t bar = kv && patch ? smem_u32(&bars.patch) : full;
+                    if (filled >= ST) ok = mbar_wait(empty, (uint32_t)(filled / ST - 1) & 1u, &abort_flag);
+                    ok = __all_sync(0xffffffffu, ok);
+                    if (!ok) break;
+                    if (lane == 0) mbar_expect_tx(bar, PART);
+                    __syncwarp();
+                    if (lane < nbox * (DP / 64)) {          // (16 boxes of 8 tokens at most, in two halves)
+                        const int b = lane % nbox, p = lane / nbox;
+                        tma_load_4d(dst + (uint32_t)p * AT_PANEL + (uint32_t)(b * box) * 128u, kv ? &tmV : &tmK, p * 64, (j0 + b * box) & page_mask, kvh, page, bar);
+                    }
+                    __syncwarp();
+                    if (kv && patch) {
+                        ok = __all_sync(0xffffffffu, mbar_wait(bar, (uint32_t)patches & 1u, &abort_flag));
+                        ++patches;
+                        if (!ok) break;
+                        for (int x = lane; x < AT_BN * DP / 8; x += 32) {
+                            const int r = x / (DP / 8), c = x % (DP / 8), j = j0 + r;
+                            if (!(j >= a.kv0 && j < t.end && (j >= t.w0 || j < a.sinks)))
+                                *reinterpret_cast<uint4 *>(smem + (dst - s_q) + (uint32_t)(c / 8) * AT_PANEL + (uint32_t)r * 128u + (uint32_t)(c % 8) * 16u) = make_uint4(0, 0, 0, 0);
+                        }
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(full);
+                    }
+                }
+            }
+        }
+    } else if (warp == AT_MMA_WARP) {
+        if (lane == 0) {
+            const int fmt = std::is_same_v<T, __nv_bfloat16> ? 1 : 0, nk = (a.D + 15) / 16;
+            const uint32_t id_s = at_idesc(AT_BN, fmt, 0), id_o = at_idesc(nk * 16, fmt, 1);
+            int segs[2] = {0, 0}, steps[2] = {0, 0}, nkey = 0, nval = 0;
+            auto scores = [&](int i, int st) {            // S_i = Q_i K^T
+                const uint64_t q0 = make_desc(s_q + (uint32_t)i * PART, 16, 1024, AT_SWZ), k0 = make_desc(s_k + (uint32_t)st * PART, 16, 1024, AT_SWZ);
+                for (int k = 0; k < nk; ++k) {
+                    const uint64_t o = (uint64_t)((k >> 2) * (int)(AT_PANEL >> 4) + (k & 3) * 2);
+                    mma_ss(tmem + (uint32_t)i * 128u, q0 + o, k0 + o, id_s, k > 0);
+                }
+                mma_commit(smem_u32(&bars.s_full[i]));
+            };
+            for (; ok && sg.get(); sg.done(a)) {
+                const int nt = sg.two(a) ? 2 : 1;
+                ok = mbar_wait(smem_u32(&bars.k_full[nkey % ST]), (uint32_t)(nkey / ST) & 1u, &abort_flag);
+                for (int i = 0; ok && i < nt; ++i) {
+                    ok = mbar_wait(smem_u32(&bars.q_full[i]), (uint32_t)segs[i]++ & 1u, &abort_flag);
+                    if (!ok) break;
+                    tmem_after();
+                    scores(i, nkey % ST);
+                }
+                if (!ok) break;
+                mma_commit(smem_u32(&bars.k_empty[nkey % ST]));
+                ++nkey;
+                for (int j = 0; ok && j < sg.n; ++j) {
+                    const bool more = j + 1 < sg.n;
+                    ok = mbar_wait(smem_u32(&bars.v_full[nval % ST]), (uint32_t)(nval / ST) & 1u, &abort_flag);
+                    for (int i = 0; ok && i < nt; ++i) {
+                        ok = mbar_wait(smem_u32(&bars.p_full[i]), (uint32_t)steps[i]++ & 1u, &abort_flag);
+                        if (!ok) break;
+                        tmem_after();
+                        const uint64_t v0 = make_desc(s_v + (uint32_t)(nval % ST) * PART, AT_PANEL, 1024, AT_SWZ);
+#pragma unroll
+                        for (int k = 0; k < AT_BN / 16; ++k)
+                            mma_ts(tmem + 256u + (uint32_t)i * 128u, tmem + (uint32_t)i * 128u + (uint32_t)k * 8u, v0 + (uint64_t)(k * 128), id_o, j > 0 || k > 0);
+                        if (!more) mma_commit(smem_u32(&bars.o_full[i]));
+                        else {
+                            if (i == 0) ok = mbar_wait(smem_u32(&bars.k_full[nkey % ST]), (uint32_t)(nkey / ST) & 1u, &abort_flag);
+                            if (!ok) break;
+                            scores(i, nkey % ST);
+                        }
+                    }
+                    if (!ok) break;
+                    mma_commit(smem_u32(&bars.v_empty[nval % ST]));
+                    ++nval;
+                    if (more) { mma_commit(smem_u32(&bars.k_empty[nkey % ST])); ++nkey; }
+                }
+            }
+        }
+        __syncwarp();
+    } else {
+        const int tile = warp >> 2, r = (warp & 3) * 32 + lane;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, t_s = tmem + lanes + (uint32_t)tile * 128u, t_o = t_s + 256u;
+        uint8_t *const qs = smem + (uint32_t)tile * PART;
+        int steps = 0, segs = 0;
+        for (; ok && sg.get(); sg.done(a)) {
+            if (tile == 1 && !sg.two(a)) continue;
+            const AttnRow row = attn_row(a, sg.cur.q, sg.cur.hu, sg.cur.rt, tile * AT_TILE + r);
+            {
+                const T *p = static_cast<const T *>(a.q) + (row.token < 0 ? 0 : row.token * a.q_ts + row.head * a.q_hs);
+                const bool whole = (reinterpret_cast<uintptr_t>(p) & 15) == 0;
+#pragma unroll 4
+                for (int c = 0; c < DP / 8; ++c) {
+                    uint4 v = make_uint4(0, 0, 0, 0);
+                    if (row.token >= 0 && c * 8 < a.D) {
+                        if (whole) v = *reinterpret_cast<const uint4 *>(p + c * 8);
+                        else {
+                            const uint16_t *h = reinterpret_cast<const uint16_t *>(p + c * 8);
+                            v = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16);
+                        }
+                    }
+                    *reinterpret_cast<uint4 *>(qs + (uint32_t)(c / 8) * AT_PANEL + (uint32_t)r * 128u + (uint32_t)(((c & 7) ^ (r & 7)) << 4)) = v;
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                tmem_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&bars.q_full[tile]));
+            }
+            // keys that all (existing) rows of the warp see need no comparison
+            int all_hi = row.token >= 0 ? row.hi : INT_MAX, all_lo = row.token >= 0 ? row.lo : 0;
+#pragma unroll
+            for (int o = 16; o > 0; o >>= 1) {
+                all_hi = imin(all_hi, __shfl_xor_sync(0xffffffffu, all_hi, o));
+                all_lo = imax(all_lo, __shfl_xor_sync(0xffffffffu, all_lo, o));
+            }
+            float m = -INFINITY, l = 0.f;
+            for (int j = 0; j < sg.n; ++j) {
+                const int j0 = attn_tile_at(sg.cur.t, sg.tile0 + j) * AT_BN;
+                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars.s_full[tile]), (uint32_t)steps & 1u, &abort_flag));
+                if (!ok) break;
+                ++steps;
+                tmem_after();
+                uint32_t s[4][32];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) tmem_ld32(t_s + (uint32_t)c * 32u, s[c]);
+                tmem_wait_ld();
+                if (!(j0 + AT_BN <= all_hi && j0 >= a.kv0 && (j0 >= all_lo || j0 + AT_BN <= a.sinks))) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e)
+                            if (!attn_sees(a, row, j0 + c * 32 + e)) s[c][e] = 0xff800000u;
+                }
+                float mx[4];
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    mx[c] = __uint_as_float(s[c][0]);
+#pragma unroll
+                    for (int e = 1; e < 32; ++e) mx[c] = fmaxf(mx[c], __uint_as_float(s[c][e]));
+                }
+                const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.sc;
+                if (__any_sync(0xffffffffu, top > m + 8.f)) {
+                    const float to = fmaxf(m, top), f = m == -INFINITY ? 0.f : attn_exp2(m - to);
+                    m = to;
+                    l *= f;
+                    if (j > 0) {
+#pragma unroll 1
+                        for (int c = 0; c < (a.D + 15) / 16; ++c) {
+                            uint32_t o[16];
+                            asm volatile(
+                                "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                                : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3]), "=r"(o[4]), "=r"(o[5]), "=r"(o[6]), "=r"(o[7]),
+                                  "=r"(o[8]), "=r"(o[9]), "=r"(o[10]), "=r"(o[11]), "=r"(o[12]), "=r"(o[13]), "=r"(o[14]), "=r"(o[15])
+                                : "r"(t_o + (uint32_t)c * 16u) : "memory");
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                            asm volatile(
+                                "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+                                ::"r"(t_o + (uint32_t)c * 16u), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]),
+                                  "r"(o[8]), "r"(o[9]), "r"(o[10]), "r"(o[11]), "r"(o[12]), "r"(o[13]), "r"(o[14]), "r"(o[15]) : "memory");
+                        }
+                    }
+                }
+                const float ref = m == -INFINITY ? 0.f : m;
+                float sum[2] = {0.f, 0.f};
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t p[32];
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        const float x = attn_exp2(fmaf(__uint_as_float(s[2 * h + e / 16][(2 * e) & 31]), a.sc, -ref));
+                        const float y = attn_exp2(fmaf(__uint_as_float(s[2 * h + e / 16][(2 * e + 1) & 31]), a.sc, -ref));
+                        sum[e & 1] += x + y;
+                        p[e] = pack2<T>(x, y);
+                    }
+                    tmem_st32(t_s + (uint32_t)h * 32u, p);
+                }
+                l += sum[0] + sum[1];
+                tmem_wait_st();
+                tmem_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&bars.p_full[tile]));
+            }
+            if (!ok) break;
+            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars.o_full[tile]), (uint32_t)segs & 1u, &abort_flag));
+            if (!ok) break;
+            ++segs;
+            tmem_after();
+            const bool complete = sg.n == sg.cur.t.nt && !a.common;
+            const int c = (int)blockIdx.x;
+            int64_t at = (2 * (int64_t)c + (sg.left < count ? 1 : 0)) * a.rows;
+            if (a.common) at = ((int64_t)sg.cur.hu * attn_row_blocks(a, sg.cur.q) + sg.cur.rt + c) * a.rows;
+            at += tile * AT_TILE + r;
+            if (!complete && row.token >= 0) a.ml[at] = make_float2(m, l);
+#pragma unroll 1
+            for (int d = 0; d < a.D; d += 16) {
+                uint32_t o[16];
+                asm volatile(
+                    "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                    : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3]), "=r"(o[4]), "=r"(o[5]), "=r"(o[6]), "=r"(o[7]),
+                      "=r"(o[8]), "=r"(o[9]), "=r"(o[10]), "=r"(o[11]), "=r"(o[12]), "=r"(o[13]), "=r"(o[14]), "=r"(o[15])
+                    : "r"(t_o + (uint32_t)d) : "memory");
+                tmem_wait_ld();
+                if (row.token < 0) continue;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (d + h * 8 >= a.D) break;
+                    float v[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(o[h * 8 + e]);
+                    if (complete) attn_finish<T>(a, row, d + h * 8, m, l, v);
+                    else {
+                        float *p = a.po + at * a.D + d + h * 8;
+                        *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
+                        *reinterpret_cast<float4 *>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+                    }
+                }
+            }
+            if (tile == 0 && r == 0 && !a.common && sg.left == sg.n)
+                attn_describe(a, sg.cur, total, grid, c, first, first + count - sg.n, sg.tile0, sg.n);
+        }
+    }
+    if (!ok && lane == 0) atomicExch(&attn_status_word, 1);
+    tmem_before();
+    __syncthreads();
+    if (*(volatile int *)&abort_flag) {
+        // a block whose waits ran out leaves no copy and no product under way (a millisecond at most each)
+        int gave_up = 0;
+        if (warp == AT_COPY_WARP) {
+            for (int f = filled > ST ? filled - ST : 0; f <= filled; ++f) {
+                mbar_wait(smem_u32(&bars.k_full[f % ST]), (uint32_t)(f / ST) & 1u, &gave_up, 1000000);
+                mbar_wait(smem_u32(&bars.v_full[f % ST]), (uint32_t)(f / ST) & 1u, &gave_up, 1000000);
+                mbar_wait(smem_u32(&bars.patch), (uint32_t)(f & 1), &gave_up, 1000000);
+            }
+        }
+        if (warp == AT_MMA_WARP && lane == 0) {
+            mma_commit(smem_u32(&bars.drain));
+            mbar_wait(smem_u32(&bars.drain), 0, &gave_up, 1000000);
+        }
+        __syncthreads();
+    }
+    if (warp == AT_MMA_WARP) {
+        tmem_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    }
+}
+
+// ------------------------------------------------------------------ host side
+typedef CUresult (*EncodeTiledFn)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *,
+                                  const cuuint32_t *, const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle,
+                                  CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encoder()
+{
+    static EncodeTiledFn fn = nullptr;
+    static std::once_flag once;
+    std::call_once(once, [] {
+        void *p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) == cudaSuccess && q == cudaDriverEntryPointSuccess)
+            fn = reinterpret_cast<EncodeTiledFn>(p);
+    });
+    return fn;
+}
+// (head values, tokens of a page, heads, pages); a stride that is never used has to be a possible one
+int encode_cache(CUtensorMap *tm, const AttnArgs &a, const void *base, int dtype)
+{
+    const EncodeTiledFn enc = encoder();
+    if (!enc) return UBP_E_CUDA;
+    const int page = 1 << a.pshift;
+    const cuuint64_t dims[4] = {(cuuint64_t)a.D, (cuuint64_t)page, (cuuint64_t)a.Hkv, (cuuint64_t)a.pages};
+    const cuuint64_t unit = (cuuint64_t)a.c_ts * 2;
+    const cuuint64_t strides[3] = {unit, a.Hkv > 1 ? (cuuint64_t)a.c_hs * 2 : unit, a.pages > 1 ? (cuuint64_t)a.c_ps * 2 : unit};
+    const cuuint32_t box[4] = {64, (cuuint32_t)(page < AT_BN ? page : AT_BN), 1, 1}, one[4] = {1, 1, 1, 1};
+    const CUresult r = enc(tm, dtype == UBP_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void *>(base), dims, strides, box, one,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) { set_last_cuda_error((int)cudaErrorInvalidValue); return UBP_E_CUDA; }
+    return UBP_OK;
+}
+
+int at_fail(cudaError_t e) { set_last_cuda_error((int)e); return UBP_E_CUDA; }
+
+template <typename T, int DP> int launch_tc_t(const CUtensorMap &k, const CUtensorMap &v, const AttnArgs &a, int grid, void *stream)
+{
+    static std::atomic<bool> done[64] = {};
+    const auto kern = ubp_attention_tc_kernel<T, DP>;
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) dev = -1;
+    if (dev < 0 || dev >= 64 || !done[dev]) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)at_smem(DP));
+        if (e != cudaSuccess) return at_fail(e);
+        if (dev >= 0 && dev < 64) done[dev] = true;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3(AT_THREADS);
+    cfg.dynamicSmemBytes = at_smem(DP);
+    cfg.stream = static_cast<cudaStream_t>(stream);
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    cudaError_t e = cudaLaunchKernelEx(&cfg, kern, k, v, a);
+    if (e == cudaSuccess) e = cudaGetLastError();
+    return e == cudaSuccess ? UBP_OK : at_fail(e);
+}
+
+}  // namespace
+
+int launch_attn_tc(const AttnArgs &a, int dtype, int grid, void *stream)
+{
+    CUtensorMap k, v;
+    if (const int rc = encode_cache(&k, a, a.k, dtype)) return rc;
+    if (const int rc = encode_cache(&v, a, a.v, dtype)) return rc;
+    if (dtype == UBP_BF16) return a.D <= 64 ? launch_tc_t<__nv_bfloat16, 64>(k, v, a, grid, stream) : launch_tc_t<__nv_bfloat16, 128>(k, v, a, grid, stream);
+    return a.D <= 64 ? launch_tc_t<__half, 64>(k, v, a, grid, stream) : launch_tc_t<__half, 128>(k, v, a, grid, stream);
+}
+
+}  // namespace ubp
+
+extern "C" int ubp_attention_check(void *stream)
+{
+    int v = 0;
+    cudaError_t e = cudaMemcpyFromSymbolAsync(&v, ubp::attn_status_word, sizeof v, 0, cudaMemcpyDeviceToHost, static_cast<cudaStream_t>(stream));
+    if (e == cudaSuccess) e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) { ubp::set_last_cuda_error((int)e); return UBP_E_CUDA; }
+    return v ? UBP_E_DEVICE : UBP_OK;
+}
+
+extern "C" int ubp_attention_clear_status(void *stream)
+{
+    const int v = 0;
+    cudaError_t e = cudaMemcpyToSymbolAsync(ubp::attn_status_word, &v, sizeof v, 0, cudaMemcpyHostToDevice, static_cast<cudaStream_t>(stream));
+    if (e == cudaSuccess) e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) { ubp::set_last_cuda_error((int)e); return UBP_E_CUDA; }
+    return UBP_OK;
+}
