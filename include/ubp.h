@@ -532,7 +532,7 @@ int ubp_rotate_append(const ubp_cache_t *cache, const void *qkv, int64_t ld, int
  * belong to one call at a time. */
 /* ubp_attention_choice: which kernel a call takes for the sequences' own tokens, and for the shared prefix (-1 without one): 0 =
  * blocks of 16 rows (tokens times heads of a group), bound by reading the cache, 1 = blocks of 256 rows on the tensor cores.
- * ubp_attention_check synchronises `stream` and returns UBP_E_DEVICE if a kernel of kind 1 on the current device has reported a
+ * ubp_attention_check synchronises `stream` and returns UBP_E_DEVICE if an attention kernel on the current device has reported a
  * bounded wait that ran out (its call's outputs are then incomplete); ubp_attention_clear_status takes the report back. */
 size_t ubp_attention_workspace_size(const ubp_cache_t *cache, int64_t T, int q_heads, int window, int sinks, int64_t prefix,
                                     int64_t max_new);

@@ -49,6 +49,7 @@ struct AttnArgs {
     // partial results: rows x {reference maximum, sum} and rows x D of a slot
     float2 *ml;
     float *po;
+    int *status;                    // of the device: 1 once a bounded wait has run out
     int4 *desc;                     // [grid] the item that begins in a block and does not end there
     // partial results of the shared prefix, to be joined in (null without one); its call's numbers follow
     const float2 *pml;

@@ -2,13 +2,31 @@
 #include <cuda_runtime.h>
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 
 #include "ubp_attention.h"
 #include "ubp_types.cuh"
 
 namespace ubp {
+__device__ int attn_status_word;         // 1: a bounded wait ran out
+
 namespace {
+
+// its address on the current device (found once a device)
+int status_word(int **p)
+{
+    static std::atomic<int *> known[64] = {};
+    int dev = 0;
+    cudaError_t e = cudaGetDevice(&dev);
+    if (e == cudaSuccess && dev < 64 && (*p = known[dev])) return UBP_OK;
+    void *q = nullptr;
+    if (e == cudaSuccess) e = cudaGetSymbolAddress(&q, attn_status_word);
+    if (e != cudaSuccess) { set_last_cuda_error((int)e); return UBP_E_CUDA; }
+    *p = static_cast<int *>(q);
+    if (dev < 64) known[dev] = *p;
+    return UBP_OK;
+}
 
 bool on(const void *p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 int log2_of(int n) { int s = 0; while ((1 << s) < n) ++s; return s; }
@@ -144,8 +162,11 @@ extern "C" int ubp_attention(const ubp_cache_t *cache, const void *q, int64_t q_
     if (const int rc = attn_plan(cache, T, q_heads, scale, window, sinks, prefix, max_new, p)) return rc;
     if (!workspace || !on(workspace, 256)) return UBP_E_ARG;
     if (workspace_bytes < p.bytes) return UBP_E_SPACE;
+    int *status = nullptr;
+    if (const int rc = status_word(&status)) return rc;
     uint8_t *w = static_cast<uint8_t *>(workspace);
     auto finish = [&](AttnArgs &a, const AttnSpace &s) {
+        a.status = status;
         a.q = q; a.q_ts = q_token_stride; a.q_hs = q_head_stride;
         a.out = out; a.o_ts = out_token_stride; a.o_hs = out_head_stride;
         a.desc = reinterpret_cast<int4 *>(w);
@@ -162,4 +183,22 @@ extern "C" int ubp_attention(const ubp_cache_t *cache, const void *q, int64_t q_
     }
     if (const int rc = (p.own_tc ? launch_attn_tc : launch_attn_few)(p.own, cache->dtype, p.own_grid, stream)) return rc;
     return launch_attn_join(p.own, cache->dtype, p.own_grid, stream);
+}
+
+extern "C" int ubp_attention_check(void *stream)
+{
+    int v = 0;
+    cudaError_t e = cudaMemcpyFromSymbolAsync(&v, ubp::attn_status_word, sizeof v, 0, cudaMemcpyDeviceToHost, static_cast<cudaStream_t>(stream));
+    if (e == cudaSuccess) e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) { ubp::set_last_cuda_error((int)e); return UBP_E_CUDA; }
+    return v ? UBP_E_DEVICE : UBP_OK;
+}
+
+extern "C" int ubp_attention_clear_status(void *stream)
+{
+    const int v = 0;
+    cudaError_t e = cudaMemcpyToSymbolAsync(ubp::attn_status_word, &v, sizeof v, 0, cudaMemcpyHostToDevice, static_cast<cudaStream_t>(stream));
+    if (e == cudaSuccess) e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
+    if (e != cudaSuccess) { ubp::set_last_cuda_error((int)e); return UBP_E_CUDA; }
+    return UBP_OK;
 }

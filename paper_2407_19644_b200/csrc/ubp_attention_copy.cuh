@@ -1,0 +1,65 @@
+// Copies of a paged cache's tiles to shared memory, and the launch of the kernels that use them.
+#ifndef UBP_ATTENTION_COPY_CUH_
+#define UBP_ATTENTION_COPY_CUH_
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+
+#include <atomic>
+
+#include "ubp_attention.h"
+#include "ubp_tc_common.cuh"
+
+namespace ubp {
+
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *tm, int c0, int c1, int c2, int c3, uint32_t bar)
+{
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+        ::"r"(dst), "l"(tm), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar) : "memory");
+}
+
+// Page of the box of `box` keys from j on, which lie in one page: out of the cache's range (its copy brings zeros) where no row of
+// the item sees a key of it, or where the table names none.
+__device__ __forceinline__ int attn_box_page(const AttnArgs &a, const AttnTiles &t, const int32_t *row, int j, int box)
+{
+    if (j >= t.end || j + box <= a.kv0 || (j + box <= t.w0 && j >= a.sinks)) return a.pages;
+    const int p = row[j >> a.pshift];
+    return (uint32_t)p < (uint32_t)a.pages ? p : a.pages;
+}
+
+// Tensor map of the keys or values (head values, tokens of a page, heads, pages), boxes of 64 values x `keys` tokens (a page's if
+// it has fewer), 128-byte swizzle.
+int attn_encode_cache(CUtensorMap *tm, const AttnArgs &a, const void *base, int dtype, int keys);
+
+// A launch that may begin before the kernel in front of it has ended; dynamic shared memory is allowed once a device and kernel.
+template <typename K, typename... A>
+int attn_launch(K kern, std::atomic<bool> (&done)[64], dim3 grid, int threads, size_t smem, void *stream, const A &...args)
+{
+    cudaError_t e = cudaSuccess;
+    if (smem > 48 * 1024) {
+        int dev = 0;
+        if (cudaGetDevice(&dev) != cudaSuccess) dev = -1;
+        if (dev < 0 || dev >= 64 || !done[dev]) {
+            e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+            if (e == cudaSuccess && dev >= 0 && dev < 64) done[dev] = true;
+        }
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = static_cast<cudaStream_t>(stream);
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, kern, args...);
+    if (e == cudaSuccess) e = cudaGetLastError();
+    if (e != cudaSuccess) { set_last_cuda_error((int)e); return UBP_E_CUDA; }
+    return UBP_OK;
+}
+
+}  // namespace ubp
+#endif

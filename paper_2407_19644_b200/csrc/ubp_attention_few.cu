@@ -6,34 +6,38 @@
 // of an item are the query heads of one key head (and neighbouring tokens), so that a key is read once for all of them, and they
 // are the rows of an m16n8k16 product: at 16 rows it is 16 multiply-adds a value read, a tenth of what the SM could do in the time
 // HBM takes for that value, so the unused rows of small groups cost nothing.
-// Eight warps a block; a warp has its own 16 keys of a step's 128, its own ring of copies (16-byte cp.async, so that any strides,
-// pages and ends of sequences are taken row by row) and its own running sums: nothing in the loop waits for another warp. They
-// meet once an item. Copies run ahead over the ends of items.
-// Keys outside what any row of the item sees are not read: their places hold zeros, so that nothing an unused slot of a page
-// holds reaches a result. The weights are rounded to 16 bits for the second product (relative 2^-9 / 2^-12 each, the sum of
-// weights is of the unrounded ones); scores, references, sums and outputs are fp32 until the end.
+// Eight warps a block; a warp has its own 16 keys of a step's 128, its own ring of copies and its own running sums: nothing in the
+// loop waits for another warp. They meet once an item. Copies are TMA boxes of 64 values x 16 keys (8 where pages are smaller),
+// which run ahead over the ends of items: with 16-byte cp.async, whose addresses every lane computed, a step took 930 instructions
+// and the kernel ran at 45 % of HBM.
+// Pages that no row of the item sees, or that the cache does not have, are out of range for the copy and come as zeros; values of
+// unseen keys within a page are overwritten with zeros, so that nothing an unused slot holds reaches a result. The weights are
+// rounded to 16 bits for the second product (relative 2^-9 / 2^-12 each, the sum of weights is of the unrounded ones); scores,
+// references, sums and outputs are fp32 until the end.
+#include <cuda.h>
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "ubp_attention_steps.cuh"
+#include "ubp_attention_copy.cuh"
 
 namespace ubp {
 namespace {
 
+using namespace tc;
+
 constexpr int FEW_WARPS = 8, FEW_KEYS = 16, FEW_ROWS = 16;
 constexpr int FEW_BN = FEW_WARPS * FEW_KEYS;
 static_assert(FEW_ROWS == 16 && FEW_BN == 128, "as the launch fills AttnArgs");
+constexpr uint32_t FEW_PANEL = FEW_KEYS * 128;                  // 64 values of each of a warp's keys
 __host__ __device__ constexpr int few_stages(int dp) { return dp == 128 ? 3 : 6; }
-__host__ __device__ constexpr int few_part(int dp) { return FEW_KEYS * dp * 2; }                    // keys (or values) of a warp's step
-__host__ __device__ constexpr int few_ring(int dp) { return few_stages(dp) * 2 * few_part(dp); }     // a warp's
-__host__ __device__ constexpr int few_smem(int dp) { return FEW_WARPS * (few_ring(dp) + 8 * dp * 4 + FEW_ROWS * 8); }
+__host__ __device__ constexpr uint32_t few_part(int dp) { return (uint32_t)(dp / 64) * FEW_PANEL; }            // keys (or values) of a warp's step
+__host__ __device__ constexpr uint32_t few_ring(int dp) { return (uint32_t)few_stages(dp) * 2 * few_part(dp); }  // a warp's
+__host__ __device__ constexpr uint32_t few_smem(int dp) { return FEW_WARPS * (few_ring(dp) + 8 * (uint32_t)dp * 4 + FEW_ROWS * 8) + 1024; }
+static_assert(few_smem(128) <= 227 * 1024 - 1024, "with the static part");
 
-__device__ __forceinline__ uint32_t smem_at(const void *p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void cp16(uint32_t dst, const void *src, bool valid)
-{
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(valid ? 16 : 0) : "memory");
-}
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t at)
 {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
@@ -59,60 +63,71 @@ template <typename T> __device__ __forceinline__ uint32_t load_pair(const T *p)
     return (uint32_t)h[0] | (uint32_t)h[1] << 16;
 }
 
-// The copies of a warp's steps: a cursor that runs ahead, with the page of the next step's keys already loaded.
-template <typename T, int DP> struct FewCopies {
+// The copies of a warp's steps: a cursor that runs ahead. Lanes 0 .. 7 hold a box each (values or keys, half of the head, eight keys
+// where pages are that small), with its page of the next step already loaded.
+template <int DP> struct FewCopies {
     AttnCursor c;
     int64_t left;            // steps that are not issued yet
-    int page0, page1;        // pages of the step's first and last eight keys
-    int j0;
+    int page, j0, kvh;
+    const int32_t *row;
+    int box, nbox, bx, px, kv;   // this lane's
 
-    __device__ __forceinline__ int page_of(const AttnArgs &a, int j) const
+    __device__ __forceinline__ void begin(const AttnArgs &a, int lane)
     {
-        return j < c.t.end ? a.table[(a.common ? 0 : (int64_t)c.b * a.ldt) + (j >> a.pshift)] : -1;
+        box = imin(1 << a.pshift, FEW_KEYS);
+        nbox = FEW_KEYS / box;
+        bx = lane % nbox; px = lane / nbox % (DP / 64); kv = lane / nbox / (DP / 64);
+        item(a);
+    }
+    __device__ __forceinline__ void item(const AttnArgs &a)
+    {
+        kvh = c.hu / a.chunks;
+        row = a.table + (a.common ? 0 : (int64_t)c.b * a.ldt);
     }
     __device__ __forceinline__ void peek(const AttnArgs &a, int warp)
     {
         j0 = attn_tile_at(c.t, c.tile) * FEW_BN + warp * FEW_KEYS;
-        page0 = page_of(a, j0);
-        page1 = a.pshift > 3 ? page0 : page_of(a, j0 + 8);
+        if (kv < 2) page = attn_box_page(a, c.t, row, j0 + bx * box, box);
     }
-    __device__ __forceinline__ void issue(const AttnArgs &a, uint32_t stage, int warp, int lane)
+    __device__ __forceinline__ void issue(const AttnArgs &a, const CUtensorMap *tmK, const CUtensorMap *tmV, uint32_t stage, uint32_t bar, int warp, int lane)
     {
-        if (left > 0) {
-            constexpr int CH = DP / 8, RPI = 32 / CH;
-            const int ch = lane % CH;
-            const int kvh = c.hu / a.chunks;
-            if (ch * 8 < (a.D + 15) / 16 * 16) {
-#pragma unroll
-                for (int i = 0; i < FEW_KEYS / RPI; ++i) {
-                    const int r = i * RPI + lane / CH, j = j0 + r, page = r < 8 ? page0 : page1;
-                    const bool in = ch * 8 < a.D && j >= a.kv0 && j < c.t.end && (j >= c.t.w0 || j < a.sinks) && (uint32_t)page < (uint32_t)a.pages;
-                    const int64_t at = in ? page * a.c_ps + kvh * a.c_hs + (j & ((1 << a.pshift) - 1)) * a.c_ts + ch * 8 : 0;
-                    const uint32_t to = stage + (uint32_t)(r * DP * 2 + ((ch ^ (r & 7)) << 4));
-                    cp16(to, static_cast<const T *>(a.k) + at, in);
-                    cp16(to + few_part(DP), static_cast<const T *>(a.v) + at, in);
-                }
-            }
-            --left;
-            c.next(a, left > 0);
-            if (left > 0) peek(a, warp);
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (left <= 0) return;
+        if (lane == 0) mbar_expect_tx(bar, 2 * few_part(DP));
+        __syncwarp();
+        if (kv < 2)
+            tma_load_4d(stage + (uint32_t)kv * few_part(DP) + (uint32_t)px * FEW_PANEL + (uint32_t)(bx * box) * 128u, kv ? tmV : tmK, px * 64,
+                        (j0 + bx * box) & ((1 << a.pshift) - 1), kvh, page, bar);
+        --left;
+        if (++c.tile == c.t.nt && left > 0) { c.next_item(a); item(a); }
+        if (left > 0) peek(a, warp);
     }
 };
 
 template <typename T, int DP>
-__global__ void __launch_bounds__(FEW_WARPS * 32, 1) ubp_attention_few_kernel(const AttnArgs a)
+__global__ void __launch_bounds__(FEW_WARPS * 32, 1)
+ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const AttnArgs a)
 {
     constexpr int ST = few_stages(DP), NK = DP / 16;
-    extern __shared__ __align__(128) uint8_t smem[];
+    constexpr uint32_t PART = few_part(DP);
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    uint8_t *const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    __shared__ __align__(8) uint64_t bar_full[FEW_WARPS][ST];
     __shared__ AttnPlace place;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    __shared__ int2 rows[FEW_ROWS];         // token and head of the item's rows
+    __shared__ int abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, tq = lane & 3;
     float *const meet = reinterpret_cast<float *>(smem + FEW_WARPS * few_ring(DP));                  // [warp][8 rows][DP]
     float2 *const meet_ml = reinterpret_cast<float2 *>(meet + FEW_WARPS * 8 * DP);                    // [warp][row]
-    const uint32_t ring = smem_at(smem) + (uint32_t)(warp * few_ring(DP));
+    const uint32_t ring = smem_u32(smem) + (uint32_t)warp * few_ring(DP);
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    if (lane == 0) {
+        if (warp == 0) { prefetch_tensormap(&tmK); prefetch_tensormap(&tmV); abort_flag = 0; }
+        for (int i = 0; i < ST; ++i) mbar_init(smem_u32(&bar_full[warp][i]), 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    __syncthreads();
+    asm volatile("griddepcontrol.wait;" ::: "memory");
 
     int64_t total, first, count;
     int grid;
@@ -121,26 +136,38 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 1) ubp_attention_few_kernel(co
         if (threadIdx.x == 0 && !a.common) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
         return;
     }
-    FewCopies<T, DP> copies;
+    FewCopies<DP> copies;
     copies.c = cur;
     copies.left = count;
+    copies.begin(a, lane);
     copies.peek(a, warp);
-    for (int s = 0; s < ST - 1; ++s) copies.issue(a, ring + (uint32_t)(s * 2 * few_part(DP)), warp, lane);
+    for (int s = 0; s < ST - 1; ++s) copies.issue(a, &tmK, &tmV, ring + (uint32_t)s * 2 * PART, smem_u32(&bar_full[warp][s]), warp, lane);
+
+    // where the lane's rows of matrix instructions' operands lie in a part: piece (2 k + h) of 16 bytes at k * 32 (within 128 bytes)
+    // xor h and the row; the same for keys (rows = keys) and values (transposed)
+    const int rk = (lane & 7) + (lane >> 4) * 8, rv = (lane & 7) + (lane >> 3 & 1) * 8;
+    const uint32_t at_k = (uint32_t)(rk * 128), xk = (uint32_t)(((lane >> 3 & 1) ^ (rk & 7)) << 4);
+    const uint32_t at_v = PART + (uint32_t)(rv * 128), xv = (uint32_t)(((lane >> 4) ^ (rv & 7)) << 4);
 
     uint32_t qf[NK][4];
     float o[DP / 8][4], m[2], l[2];
     AttnRow row[2];
-    int tile0 = cur.tile, st = 0;
-    bool fresh = true;
+    int tile0 = cur.tile, st = 0, all_lo = 0, all_hi = 0;
+    uint32_t phase = 0;
+    bool fresh = true, ok = true;
     for (int64_t step = 0; step < count; ++step) {
         __syncwarp();                       // (all lanes have read the stage that is copied to now)
-        copies.issue(a, ring + (uint32_t)((st + ST - 1) % ST * 2 * few_part(DP)), warp, lane);
+        const int nx = st == 0 ? ST - 1 : st - 1;
+        copies.issue(a, &tmK, &tmV, ring + (uint32_t)nx * 2 * PART, smem_u32(&bar_full[warp][nx]), warp, lane);
         if (fresh) {
             fresh = false;
             tile0 = cur.tile;
+            all_lo = 0; all_hi = INT_MAX;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 row[i] = attn_row(a, cur.q, cur.hu, cur.rt, g + 8 * i);
+                if (warp == 0 && tq == 0) rows[g + 8 * i] = make_int2(row[i].token, row[i].head);
+                if (row[i].token >= 0) { all_lo = imax(all_lo, row[i].lo); all_hi = imin(all_hi, row[i].hi); }
                 m[i] = -INFINITY; l[i] = 0.f;
                 const T *p = static_cast<const T *>(a.q) + (row[i].token < 0 ? 0 : row[i].token * a.q_ts + row[i].head * a.q_hs);
 #pragma unroll
@@ -152,40 +179,50 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 1) ubp_attention_few_kernel(co
                     }
             }
 #pragma unroll
+            for (int s = 4; s < 32; s <<= 1) {
+                all_lo = imax(all_lo, __shfl_xor_sync(0xffffffffu, all_lo, s));
+                all_hi = imin(all_hi, __shfl_xor_sync(0xffffffffu, all_hi, s));
+            }
+#pragma unroll
             for (int n = 0; n < DP / 8; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
         }
-        asm volatile("cp.async.wait_group %0;" ::"n"(ST - 1) : "memory");
-        __syncwarp();
+        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_full[warp][st]), phase, &abort_flag));
         const int j0 = attn_tile_at(cur.t, cur.tile) * FEW_BN + warp * FEW_KEYS;
-        const uint32_t ks = ring + (uint32_t)(st * 2 * few_part(DP)), vs = ks + few_part(DP);
-        if (j0 < cur.t.end && (j0 + FEW_KEYS > cur.t.w0 || j0 < a.sinks)) {
+        const uint32_t base = ring + (uint32_t)st * 2 * PART;
+        if (ok && j0 < cur.t.end && j0 + FEW_KEYS > a.kv0 && (j0 + FEW_KEYS > cur.t.w0 || j0 < a.sinks)) {
             float s[2][4] = {};
-            {
-                const int r = (lane & 7) + (lane >> 4) * 8;
-                const uint32_t at = ks + (uint32_t)(r * DP * 2);
 #pragma unroll
-                for (int k = 0; k < NK; ++k)
-                    if (k * 16 < a.D) {
-                        uint32_t b[4];
-                        ldsm4(b, at + (uint32_t)(((2 * k + (lane >> 3 & 1)) ^ (r & 7)) << 4));
-                        mma16<T>(s[0], qf[k], b[0], b[1]);
-                        mma16<T>(s[1], qf[k], b[2], b[3]);
-                    }
-            }
-            float mx[2] = {-INFINITY, -INFINITY};
-#pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s[n][e] = attn_sees(a, row[e >> 1], j0 + n * 8 + tq * 2 + (e & 1)) ? s[n][e] * a.sc : -INFINITY;
-                    mx[e >> 1] = fmaxf(mx[e >> 1], s[n][e]);
+            for (int k = 0; k < NK; ++k)
+                if (k * 16 < a.D) {
+                    uint32_t b[4];
+                    ldsm4(b, base + at_k + (uint32_t)(k / 4) * FEW_PANEL + ((uint32_t)(k % 4 * 32) ^ xk));
+                    mma16<T>(s[0], qf[k], b[0], b[1]);
+                    mma16<T>(s[1], qf[k], b[2], b[3]);
                 }
+            const bool all = j0 + FEW_KEYS <= all_hi && j0 >= a.kv0 && (j0 >= all_lo || j0 + FEW_KEYS <= a.sinks);
+            if (!all) {
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (!attn_sees(a, row[e >> 1], j0 + n * 8 + tq * 2 + (e & 1))) s[n][e] = -INFINITY;
+                // values of keys that no row sees
+                for (int x = lane; x < FEW_KEYS * DP / 8; x += 32) {
+                    const int r = x / (DP / 8), ch = x % (DP / 8), j = j0 + r;
+                    if (!(j >= a.kv0 && j < cur.t.end && (j >= cur.t.w0 || j < a.sinks)))
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(base + PART + (uint32_t)(ch / 8) * FEW_PANEL + (uint32_t)(r * 128 + ch % 8 * 16)), "r"(0) : "memory");
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // (before the next copy to these places)
+                __syncwarp();
+            }
+            float mx[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
+                mx[i] = fmaxf(fmaxf(s[0][2 * i], s[0][2 * i + 1]), fmaxf(s[1][2 * i], s[1][2 * i + 1]));
                 mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 1));
-                mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 2));
+                mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 2)) * a.sc;
             }
             // The reference only moves when a score lies more than 2^8 above it: weights stay below 2^8, sums far from overflow.
             if (__any_sync(0xffffffffu, mx[0] > m[0] + 8.f || mx[1] > m[1] + 8.f)) {
@@ -204,25 +241,21 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 1) ubp_attention_few_kernel(co
                 const float ref = m[i] == -INFINITY ? 0.f : m[i];
 #pragma unroll
                 for (int n = 0; n < 2; ++n) {
-                    const float p0 = attn_exp2(s[n][2 * i] - ref), p1 = attn_exp2(s[n][2 * i + 1] - ref);
+                    const float p0 = attn_exp2(fmaf(s[n][2 * i], a.sc, -ref)), p1 = attn_exp2(fmaf(s[n][2 * i + 1], a.sc, -ref));
                     l[i] += p0 + p1;
                     p[n * 2 + i] = pack2<T>(p0, p1);
                 }
             }
-            {
-                const int r = (lane & 7) + (lane >> 3 & 1) * 8;
-                const uint32_t at = vs + (uint32_t)(r * DP * 2);
 #pragma unroll
-                for (int n = 0; n < NK; ++n)
-                    if (n * 16 < a.D) {
-                        uint32_t b[4];
-                        ldsm4t(b, at + (uint32_t)(((2 * n + (lane >> 4)) ^ (r & 7)) << 4));
-                        mma16<T>(o[2 * n], p, b[0], b[1]);
-                        mma16<T>(o[2 * n + 1], p, b[2], b[3]);
-                    }
-            }
+            for (int n = 0; n < NK; ++n)
+                if (n * 16 < a.D) {
+                    uint32_t b[4];
+                    ldsm4t(b, base + at_v + (uint32_t)(n / 4) * FEW_PANEL + ((uint32_t)(n % 4 * 32) ^ xv));
+                    mma16<T>(o[2 * n], p, b[0], b[1]);
+                    mma16<T>(o[2 * n + 1], p, b[2], b[3]);
+                }
         }
-        st = st + 1 == ST ? 0 : st + 1;
+        if (++st == ST) { st = 0; phase ^= 1u; }
         const bool last = step + 1 == count;
         if (cur.tile + 1 == cur.t.nt || last) {
             // ---- the warps' sums meet: rows 0 .. 7, then 8 .. 15 where the item has them
@@ -248,8 +281,8 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 1) ubp_attention_few_kernel(co
                 constexpr int N = 4, TPR = DP / N;          // threads a row
                 for (int x = (int)threadIdx.x; x < 8 * TPR; x += FEW_WARPS * 32) {
                     const int r = x / TPR, col = x % TPR * N;
-                    const AttnRow w = attn_row(a, cur.q, cur.hu, cur.rt, i * 8 + r);
-                    if (col < a.D && (w.token >= 0 || !whole)) {
+                    const int2 w = rows[i * 8 + r];
+                    if (col < a.D && (w.x >= 0 || !whole)) {
                         float M = -INFINITY, L = 0.f, v[N] = {};
 #pragma unroll
                         for (int k = 0; k < FEW_WARPS; ++k) {
@@ -258,7 +291,7 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 1) ubp_attention_few_kernel(co
                             attn_load(meet + (k * 8 + r) * DP + col, u);
                             attn_add(M, L, v, ml.x, ml.y, u);
                         }
-                        if (whole) attn_finish<T>(a, w, col, M, L, v);
+                        if (whole) attn_finish<T>(a, w.x, w.y, col, M, L, v);
                         else {
                             if (col == 0) a.ml[slot * FEW_ROWS + i * 8 + r] = make_float2(M, L);
                             *reinterpret_cast<float4 *>(a.po + (slot * FEW_ROWS + i * 8 + r) * a.D + col) = make_float4(v[0], v[1], v[2], v[3]);
@@ -271,6 +304,12 @@ __global__ void __launch_bounds__(FEW_WARPS * 32, 1) ubp_attention_few_kernel(co
             fresh = true;
         }
         cur.next(a, !last);
+    }
+    if (!ok) {                              // copies that are still under way end before the block does (a millisecond at most each)
+        int gave_up = 0;
+        for (int i = 0; i < ST; ++i)
+            for (uint32_t ph = 0; ph < 2; ++ph) mbar_wait(smem_u32(&bar_full[warp][i]), ph, &gave_up, 1000000);
+        if (lane == 0) atomicExch(a.status, 1);
     }
 }
 
@@ -300,51 +339,33 @@ __global__ void __launch_bounds__(256) ubp_attention_join_kernel(const AttnArgs 
             attn_load(a.po + at * a.D + col, v);
             attn_add(M, L, o, ml.x, ml.y, v);
         }
-        attn_finish<T>(a, w, col, M, L, o);
+        attn_finish<T>(a, w.token, w.head, col, M, L, o);
     }
 }
 
-int attn_fail(cudaError_t e) { set_last_cuda_error((int)e); return UBP_E_CUDA; }
-
-template <typename K>
-int launch_after(K kern, dim3 grid, int threads, size_t smem, const AttnArgs &a, void *stream)
+template <typename T, int DP> int launch_few_t(const CUtensorMap &k, const CUtensorMap &v, const AttnArgs &a, int grid, void *stream)
 {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
-    cfg.blockDim = dim3((unsigned)threads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = static_cast<cudaStream_t>(stream);
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    cudaError_t e = cudaLaunchKernelEx(&cfg, kern, a);
-    if (e == cudaSuccess) e = cudaGetLastError();
-    return e == cudaSuccess ? UBP_OK : attn_fail(e);
-}
-
-template <typename T, int DP> int launch_few_t(const AttnArgs &a, int grid, void *stream)
-{
-    const auto kern = ubp_attention_few_kernel<T, DP>;
-    const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, few_smem(DP));
-    if (e != cudaSuccess) return attn_fail(e);
-    return launch_after(kern, dim3((unsigned)grid), FEW_WARPS * 32, few_smem(DP), a, stream);
+    static std::atomic<bool> done[64] = {};
+    return attn_launch(ubp_attention_few_kernel<T, DP>, done, dim3((unsigned)grid), FEW_WARPS * 32, few_smem(DP), stream, k, v, a);
 }
 
 }  // namespace
 
 int launch_attn_few(const AttnArgs &a, int dtype, int grid, void *stream)
 {
-    if (dtype == UBP_BF16) return a.D <= 64 ? launch_few_t<__nv_bfloat16, 64>(a, grid, stream) : launch_few_t<__nv_bfloat16, 128>(a, grid, stream);
-    return a.D <= 64 ? launch_few_t<__half, 64>(a, grid, stream) : launch_few_t<__half, 128>(a, grid, stream);
+    CUtensorMap k, v;
+    if (const int rc = attn_encode_cache(&k, a, a.k, dtype, FEW_KEYS)) return rc;
+    if (const int rc = attn_encode_cache(&v, a, a.v, dtype, FEW_KEYS)) return rc;
+    if (dtype == UBP_BF16) return a.D <= 64 ? launch_few_t<__nv_bfloat16, 64>(k, v, a, grid, stream) : launch_few_t<__nv_bfloat16, 128>(k, v, a, grid, stream);
+    return a.D <= 64 ? launch_few_t<__half, 64>(k, v, a, grid, stream) : launch_few_t<__half, 128>(k, v, a, grid, stream);
 }
 
 int launch_attn_join(const AttnArgs &a, int dtype, int grid, void *stream)
 {
     const dim3 g((unsigned)grid, (unsigned)((a.rows + 15) / 16));
-    return dtype == UBP_BF16 ? launch_after(ubp_attention_join_kernel<__nv_bfloat16>, g, 256, 0, a, stream)
-                             : launch_after(ubp_attention_join_kernel<__half>, g, 256, 0, a, stream);
+    static std::atomic<bool> done[64] = {};
+    return dtype == UBP_BF16 ? attn_launch(ubp_attention_join_kernel<__nv_bfloat16>, done, g, 256, 0, stream, a)
+                             : attn_launch(ubp_attention_join_kernel<__half>, done, g, 256, 0, stream, a);
 }
 
 }  // namespace ubp

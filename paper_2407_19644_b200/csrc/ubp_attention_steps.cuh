@@ -14,7 +14,7 @@ __device__ __forceinline__ float attn_exp2(float x)
     return y;
 }
 
-struct AttnPlace { int64_t warp[32]; int64_t rem; int b, hu, rt, tile; };
+struct AttnPlace { int64_t warp[32]; int64_t rem; int b; };
 
 // Steps of sequence b (none where !valid); called by whole warps. A lane counts its own sequence's row blocks while they are few,
 // the warp counts those of long prompts together.
@@ -43,12 +43,68 @@ __device__ __forceinline__ int64_t attn_seq_steps(const AttnArgs &a, int b, bool
     return c * a.HU;
 }
 
+// The cursor at step rem of sequence b; called by whole warps.
+__device__ __forceinline__ void attn_place(const AttnArgs &a, int b, int64_t rem, AttnCursor &cur)
+{
+    const int lane = threadIdx.x & 31;
+    const AttnSeq q = attn_seq(a, b);
+    const int m = attn_row_blocks(a, q);
+    if (m == 1) {
+        const int n = attn_block_tiles(a, q, 0).nt, hu = rem >> 32 ? (int)(rem / n) : (int)((uint32_t)rem / (uint32_t)n);
+        cur.set(a, b, hu, 0, (int)(rem - (int64_t)hu * n));
+        return;
+    }
+    int64_t per = 0;
+    for (int i = lane; i < m; i += 32) per += attn_block_tiles(a, q, i).nt;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) per += __shfl_xor_sync(0xffffffffu, per, o);
+    const int hu = (int)(rem / per);
+    int rt = 0;
+    rem -= (int64_t)hu * per;
+    for (int i = 0; i < m; i += 32) {
+        const int n = i + lane < m ? attn_block_tiles(a, q, i + lane).nt : 0;
+        int64_t x = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x += y;
+        }
+        const uint32_t in = __ballot_sync(0xffffffffu, x > rem);
+        if (in) {
+            const int src = __ffs(in) - 1;
+            rem -= __shfl_sync(0xffffffffu, x - n, src);
+            rt = i + src;
+            break;
+        }
+        rem -= __shfl_sync(0xffffffffu, x, 31);
+    }
+    cur.set(a, b, hu, rt, (int)rem);
+}
+
 // The block's steps: [first, first + count) of `total`, and the cursor at the first one. Called by all threads of the block (a
 // multiple of 32); returns false, to all of them, if there is nothing to do. `grid`: blocks that have steps.
 __device__ __forceinline__ bool attn_locate(const AttnArgs &a, AttnPlace &sh, int64_t &total, int64_t &first, int64_t &count, int &grid, AttnCursor &cur)
 {
     const int nt = (int)blockDim.x, tid = (int)threadIdx.x, lane = tid & 31, warp = tid >> 5, nw = nt >> 5;
     const int nb = a.common ? 1 : a.B;
+    if (nb <= 32) {                     // every warp for itself: no barrier
+        const int64_t mine = attn_seq_steps(a, lane, lane < nb);
+        int64_t x = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
+            if (lane >= o) x += y;
+        }
+        total = __shfl_sync(0xffffffffu, x, 31);
+        grid = total < (int64_t)gridDim.x ? (int)total : (int)gridDim.x;
+        const int c = (int)blockIdx.x;
+        if (c >= grid) return false;
+        first = attn_first_step(total, c, grid);
+        count = attn_first_step(total, c + 1, grid) - first;
+        const int b = __ffs(__ballot_sync(0xffffffffu, x > first)) - 1;
+        attn_place(a, b, first - __shfl_sync(0xffffffffu, x - mine, b), cur);
+        return true;
+    }
     total = 0;
     int64_t mine = 0, before = 0;       // steps of this thread's sequence, and of all sequences before it in the chunk
     auto scan = [&](int base) {         // -> steps of the chunk of nt sequences from base on
@@ -88,42 +144,7 @@ __device__ __forceinline__ bool attn_locate(const AttnArgs &a, AttnPlace &sh, in
         at -= all;
     }
     __syncthreads();
-    if (warp == 0) {
-        const AttnSeq q = attn_seq(a, sh.b);
-        const int m = attn_row_blocks(a, q);
-        int hu, rt = 0;
-        int64_t rem = sh.rem;
-        if (m == 1) {
-            const int n = attn_block_tiles(a, q, 0).nt;
-            hu = (int)(rem / n); rem -= (int64_t)hu * n;
-        } else {
-            int64_t per = 0;
-            for (int i = lane; i < m; i += 32) per += attn_block_tiles(a, q, i).nt;
-#pragma unroll
-            for (int o = 16; o > 0; o >>= 1) per += __shfl_xor_sync(0xffffffffu, per, o);
-            hu = (int)(rem / per); rem -= (int64_t)hu * per;
-            for (int i = 0; i < m; i += 32) {
-                const int n = i + lane < m ? attn_block_tiles(a, q, i + lane).nt : 0;
-                int64_t x = n;
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
-                    if (lane >= o) x += y;
-                }
-                const uint32_t in = __ballot_sync(0xffffffffu, x > rem);
-                if (in) {
-                    const int src = __ffs(in) - 1;
-                    rem -= __shfl_sync(0xffffffffu, x - n, src);
-                    rt = i + src;
-                    break;
-                }
-                rem -= __shfl_sync(0xffffffffu, x, 31);
-            }
-        }
-        if (lane == 0) { sh.hu = hu; sh.rt = rt; sh.tile = (int)rem; }
-    }
-    __syncthreads();
-    cur.set(a, sh.b, sh.hu, sh.rt, sh.tile);
+    attn_place(a, sh.b, sh.rem, cur);
     return true;
 }
 
@@ -217,13 +238,13 @@ template <typename T, int N> __device__ __forceinline__ void attn_store(T *p, co
     }
 }
 // Finished sums of a row, from column col on, to the output: o / L, 0 where nothing was seen.
-template <typename T, int N> __device__ __forceinline__ void attn_finish(const AttnArgs &a, const AttnRow &w, int col, float M, float L, float (&o)[N])
+template <typename T, int N> __device__ __forceinline__ void attn_finish(const AttnArgs &a, int token, int head, int col, float M, float L, float (&o)[N])
 {
-    if (a.pml) attn_add_prefix(a, w.token, w.head, col, M, L, o);
+    if (a.pml) attn_add_prefix(a, token, head, col, M, L, o);
     const float r = L == 0.f ? 0.f : 1.f / L;
 #pragma unroll
     for (int i = 0; i < N; ++i) o[i] *= r;
-    attn_store(static_cast<T *>(a.out) + w.token * a.o_ts + w.head * a.o_hs + col, o);
+    attn_store(static_cast<T *>(a.out) + token * a.o_ts + head * a.o_hs + col, o);
 }
 
 // What block c leaves behind for the join: its last item if that begins here and ends in a later block.

@@ -18,12 +18,10 @@
 #include <mutex>
 #include <type_traits>
 
+#include "ubp_attention_copy.cuh"
 #include "ubp_attention_steps.cuh"
-#include "ubp_tc_common.cuh"
 
 namespace ubp {
-
-__device__ int attn_status_word;         // 1: a bounded wait ran out
 
 namespace {
 
@@ -38,12 +36,6 @@ __host__ __device__ constexpr uint32_t at_part(int dp) { return (uint32_t)(dp / 
 __host__ __device__ constexpr uint32_t at_smem(int dp) { return (2 + 2 * (uint32_t)at_stages(dp)) * at_part(dp) + 1024; }
 static_assert(at_smem(64) >= TC_PAIR_MIN_SMEM, "one block an SM: a block holds all tensor memory");
 
-__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *tm, int c0, int c1, int c2, int c3, uint32_t bar)
-{
-    asm volatile(
-        "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
-        ::"r"(dst), "l"(tm), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar) : "memory");
-}
 // D (tensor memory) (+)= A B: A from shared memory, or the 16-bit values of tensor memory from column `a` on
 __device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
 {
@@ -171,15 +163,8 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
             const AttnTiles &t = sg.cur.t;
             for (int i = 0; ok && i < sg.n; ++i, ++filled) {
                 const int st = filled % ST, j0 = attn_tile_at(t, sg.tile0 + i) * AT_BN;
-                // the boxes of this tile, a lane each: a page that no row sees a key of, or that the cache does not have, is
-                // out of range for the copy and comes as zeros
-                auto page_at = [&](int u) {
-                    const int j = j0 + u * box;
-                    if (j >= t.end || j + box <= a.kv0 || (j + box <= t.w0 && j >= a.sinks)) return a.pages;
-                    const int p = row[j >> a.pshift];
-                    return (uint32_t)p < (uint32_t)a.pages ? p : a.pages;
-                };
-                const int page = __shfl_sync(0xffffffffu, lane < nbox ? page_at(lane) : a.pages, lane % nbox);
+                // (a lane a box)
+                const int page = __shfl_sync(0xffffffffu, lane < nbox ? attn_box_page(a, t, row, j0 + lane * box, box) : a.pages, lane % nbox);
                 // Places of a page whose keys no row sees: whatever they hold, a weight of 0 times it has to be 0, so the values
                 // there are overwritten with zeros before the product reads them.
                 const bool patch = (j0 + AT_BN > t.end && (t.end & (box - 1))) || (j0 < a.kv0 && j0 + AT_BN > a.kv0 && (a.kv0 & (box - 1))) ||
@@ -396,7 +381,7 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                     float v[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(o[h * 8 + e]);
-                    if (complete) attn_finish<T>(a, row, d + h * 8, m, l, v);
+                    if (complete) attn_finish<T>(a, row.token, row.head, d + h * 8, m, l, v);
                     else {
                         float *p = a.po + at * a.D + d + h * 8;
                         *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
@@ -408,7 +393,7 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                 attn_describe(a, sg.cur, total, grid, c, first, first + count - sg.n, sg.tile0, sg.n);
         }
     }
-    if (!ok && lane == 0) atomicExch(&attn_status_word, 1);
+    if (!ok && lane == 0) atomicExch(a.status, 1);
     tmem_before();
     __syncthreads();
     if (*(volatile int *)&abort_flag) {
@@ -449,8 +434,10 @@ EncodeTiledFn encoder()
     });
     return fn;
 }
-// (head values, tokens of a page, heads, pages); a stride that is never used has to be a possible one
-int encode_cache(CUtensorMap *tm, const AttnArgs &a, const void *base, int dtype)
+}  // namespace
+
+// (a stride that is never used has to be a possible one)
+int attn_encode_cache(CUtensorMap *tm, const AttnArgs &a, const void *base, int dtype, int keys)
 {
     const EncodeTiledFn enc = encoder();
     if (!enc) return UBP_E_CUDA;
@@ -458,39 +445,19 @@ int encode_cache(CUtensorMap *tm, const AttnArgs &a, const void *base, int dtype
     const cuuint64_t dims[4] = {(cuuint64_t)a.D, (cuuint64_t)page, (cuuint64_t)a.Hkv, (cuuint64_t)a.pages};
     const cuuint64_t unit = (cuuint64_t)a.c_ts * 2;
     const cuuint64_t strides[3] = {unit, a.Hkv > 1 ? (cuuint64_t)a.c_hs * 2 : unit, a.pages > 1 ? (cuuint64_t)a.c_ps * 2 : unit};
-    const cuuint32_t box[4] = {64, (cuuint32_t)(page < AT_BN ? page : AT_BN), 1, 1}, one[4] = {1, 1, 1, 1};
+    const cuuint32_t box[4] = {64, (cuuint32_t)imin(page, keys), 1, 1}, one[4] = {1, 1, 1, 1};
     const CUresult r = enc(tm, dtype == UBP_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 4, const_cast<void *>(base), dims, strides, box, one,
                            CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) { set_last_cuda_error((int)cudaErrorInvalidValue); return UBP_E_CUDA; }
     return UBP_OK;
 }
 
-int at_fail(cudaError_t e) { set_last_cuda_error((int)e); return UBP_E_CUDA; }
+namespace {
 
 template <typename T, int DP> int launch_tc_t(const CUtensorMap &k, const CUtensorMap &v, const AttnArgs &a, int grid, void *stream)
 {
     static std::atomic<bool> done[64] = {};
-    const auto kern = ubp_attention_tc_kernel<T, DP>;
-    int dev = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess) dev = -1;
-    if (dev < 0 || dev >= 64 || !done[dev]) {
-        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)at_smem(DP));
-        if (e != cudaSuccess) return at_fail(e);
-        if (dev >= 0 && dev < 64) done[dev] = true;
-    }
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid);
-    cfg.blockDim = dim3(AT_THREADS);
-    cfg.dynamicSmemBytes = at_smem(DP);
-    cfg.stream = static_cast<cudaStream_t>(stream);
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    cudaError_t e = cudaLaunchKernelEx(&cfg, kern, k, v, a);
-    if (e == cudaSuccess) e = cudaGetLastError();
-    return e == cudaSuccess ? UBP_OK : at_fail(e);
+    return attn_launch(ubp_attention_tc_kernel<T, DP>, done, dim3((unsigned)grid), AT_THREADS, at_smem(DP), stream, k, v, a);
 }
 
 }  // namespace
@@ -498,28 +465,10 @@ template <typename T, int DP> int launch_tc_t(const CUtensorMap &k, const CUtens
 int launch_attn_tc(const AttnArgs &a, int dtype, int grid, void *stream)
 {
     CUtensorMap k, v;
-    if (const int rc = encode_cache(&k, a, a.k, dtype)) return rc;
-    if (const int rc = encode_cache(&v, a, a.v, dtype)) return rc;
+    if (const int rc = attn_encode_cache(&k, a, a.k, dtype, AT_BN)) return rc;
+    if (const int rc = attn_encode_cache(&v, a, a.v, dtype, AT_BN)) return rc;
     if (dtype == UBP_BF16) return a.D <= 64 ? launch_tc_t<__nv_bfloat16, 64>(k, v, a, grid, stream) : launch_tc_t<__nv_bfloat16, 128>(k, v, a, grid, stream);
     return a.D <= 64 ? launch_tc_t<__half, 64>(k, v, a, grid, stream) : launch_tc_t<__half, 128>(k, v, a, grid, stream);
 }
 
 }  // namespace ubp
-
-extern "C" int ubp_attention_check(void *stream)
-{
-    int v = 0;
-    cudaError_t e = cudaMemcpyFromSymbolAsync(&v, ubp::attn_status_word, sizeof v, 0, cudaMemcpyDeviceToHost, static_cast<cudaStream_t>(stream));
-    if (e == cudaSuccess) e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
-    if (e != cudaSuccess) { ubp::set_last_cuda_error((int)e); return UBP_E_CUDA; }
-    return v ? UBP_E_DEVICE : UBP_OK;
-}
-
-extern "C" int ubp_attention_clear_status(void *stream)
-{
-    const int v = 0;
-    cudaError_t e = cudaMemcpyToSymbolAsync(ubp::attn_status_word, &v, sizeof v, 0, cudaMemcpyHostToDevice, static_cast<cudaStream_t>(stream));
-    if (e == cudaSuccess) e = cudaStreamSynchronize(static_cast<cudaStream_t>(stream));
-    if (e != cudaSuccess) { ubp::set_last_cuda_error((int)e); return UBP_E_CUDA; }
-    return UBP_OK;
-}
