@@ -7,7 +7,7 @@
 // of its rows see, at least one (an item whose rows see nothing still writes its zeros).
 //
 // Steps. All items of a call lie one behind the other, sequence by sequence, unit head by unit head, and block c of G takes the
-// steps [c total / G, (c + 1) total / G): every block gets the same number to within one whatever the lengths are, which only
+// c-th share of them: every block gets the same number to within one whatever the lengths are, which only
 // the device knows. An item that ends up with several blocks is joined by a second kernel from their partial results.
 #ifndef UBP_ATTENTION_H_
 #define UBP_ATTENTION_H_
@@ -50,11 +50,10 @@ struct AttnArgs {
     float2 *ml;
     float *po;
     int *status;                    // of the device: 1 once a bounded wait has run out
-    int4 *desc;                     // [grid] the item that begins in a block and does not end there
-    // partial results of the shared prefix, to be joined in (null without one); its call's numbers follow
-    const float2 *pml;
-    const float *ppo;
-    int p_grid, p_rows, p_tiles, p_gc, p_chunks, p_tpt, p_nt;
+    int4 *desc;                     // [grid] the item that begins in a block and does not end there (AttnPart)
+    // the shared prefix's results of each row, [T][Hq] and [T][Hq][D] (null without one): written by its join, read by the others
+    float2 *pml;
+    float *ppo;
 };
 
 UBP_HD int imin(int a, int b) { return a < b ? a : b; }
@@ -137,16 +136,25 @@ struct AttnCursor {
     }
 };
 
-UBP_HD int64_t attn_first_step(int64_t total, int c, int grid) { return total / grid * c + total % grid * c / grid; }
-// block that has step x (grid <= total): the last one whose first step is not behind x
-UBP_HD int attn_owner(int64_t total, int64_t x, int grid)
-{
-    int c = (int)((double)x / (double)total * grid);
-    c = imin(imax(c, 0), grid - 1);
-    while (c > 0 && attn_first_step(total, c, grid) > x) --c;
-    while (c + 1 < grid && attn_first_step(total, c + 1, grid) <= x) ++c;
-    return c;
-}
+// How `total` steps are dealt to `grid` blocks (grid <= total): the first r blocks take q + 1, the others q.
+struct AttnDeal {
+    int64_t q;
+    int r, grid;
+    UBP_HD AttnDeal(int64_t total, int blocks)
+    {
+        grid = total < (int64_t)blocks ? (int)total : blocks;
+        if (total >> 32) { q = total / grid; r = (int)(total - q * grid); }
+        else if (grid) { q = (uint32_t)total / (uint32_t)grid; r = (int)((uint32_t)total - (uint32_t)q * (uint32_t)grid); }
+        else { q = 0; r = 0; }
+    }
+    UBP_HD int64_t first(int c) const { return q * c + imin(c, r); }
+    UBP_HD int64_t count(int c) const { return q + (c < r ? 1 : 0); }
+    UBP_HD int owner(int64_t x) const       // block that has step x
+    {
+        const int64_t y = x - (q + 1) * r;
+        return y < 0 ? (int)(x / (q + 1)) : r + (int)(y / q);
+    }
+};
 
 // slots of partial results that a call needs, and its workspace: [desc][ml][po]
 struct AttnSpace { size_t ml, po, total; };
@@ -163,7 +171,7 @@ inline AttnSpace attn_space(int64_t grid, int64_t slots, int rows, int D)
 // ---- launches; both kernels follow the same scheme and leave the same partial results
 int launch_attn_few(const AttnArgs &a, int dtype, int grid, void *stream);       // 16 rows an item (ubp_attention_few.cu)
 int launch_attn_tc(const AttnArgs &a, int dtype, int grid, void *stream);        // 256 rows an item (ubp_attention_tc.cu)
-int launch_attn_join(const AttnArgs &a, int dtype, int grid, void *stream);
+int launch_attn_join(const AttnArgs &a, int dtype, int grid, void *stream);       // `grid`: the kernel's before it
 int device_sms();
 void set_last_cuda_error(int e);
 

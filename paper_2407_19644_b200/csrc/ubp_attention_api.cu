@@ -71,7 +71,7 @@ struct AttnCall {
     AttnArgs own, common;
     bool own_tc = false, common_tc = false;
     int own_grid = 0, common_grid = 0;
-    AttnSpace own_space{}, common_space{};
+    AttnSpace own_space{}, common_space{}, row_space{};
     size_t bytes = 0;
 };
 
@@ -108,9 +108,10 @@ int attn_plan(const ubp_cache_t *c, int64_t T, int q_heads, float scale, int win
         const int64_t units = (int64_t)((b.T + b.tpt - 1) / b.tpt) * b.HU;
         const int nt = (int)((prefix + b.bn - 1) / b.bn);
         p.common_grid = (int)std::min<int64_t>(sms, units * nt);
-        p.common_space = attn_space(p.common_grid, units + p.common_grid, b.rows, b.D);
-        p.bytes += p.common_space.total;
-        a.p_grid = p.common_grid; a.p_rows = b.rows; a.p_tiles = b.tiles; a.p_gc = b.gc; a.p_chunks = b.chunks; a.p_tpt = b.tpt; a.p_nt = nt;
+        if (units + p.common_grid > INT32_MAX) return UBP_E_UNSUPPORTED;
+        p.common_space = attn_space(0, units + p.common_grid, b.rows, b.D);
+        p.row_space = attn_space(0, T, q_heads, b.D);          // a row's sums over the prefix
+        p.bytes += p.common_space.total + p.row_space.total;
         p.common = b;
     }
     p.own = a;
@@ -177,9 +178,10 @@ extern "C" int ubp_attention(const ubp_cache_t *cache, const void *q, int64_t q_
     finish(p.own, p.own_space);
     if (prefix > 0) {
         finish(p.common, p.common_space);
-        p.own.pml = p.common.ml;
-        p.own.ppo = p.common.po;
+        p.own.pml = p.common.pml = reinterpret_cast<float2 *>(w + p.row_space.ml);
+        p.own.ppo = p.common.ppo = reinterpret_cast<float *>(w + p.row_space.po);
         if (const int rc = (p.common_tc ? launch_attn_tc : launch_attn_few)(p.common, cache->dtype, p.common_grid, stream)) return rc;
+        if (const int rc = launch_attn_join(p.common, cache->dtype, p.common_grid, stream)) return rc;
     }
     if (const int rc = (p.own_tc ? launch_attn_tc : launch_attn_few)(p.own, cache->dtype, p.own_grid, stream)) return rc;
     return launch_attn_join(p.own, cache->dtype, p.own_grid, stream);

@@ -55,13 +55,8 @@ template <typename T> __device__ __forceinline__ void mma16(float (&c)[4], const
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// two neighbouring elements, whatever their alignment
-template <typename T> __device__ __forceinline__ uint32_t load_pair(const T *p)
-{
-    if ((reinterpret_cast<uintptr_t>(p) & 3) == 0) return *reinterpret_cast<const uint32_t *>(p);
-    const uint16_t *h = reinterpret_cast<const uint16_t *>(p);
-    return (uint32_t)h[0] | (uint32_t)h[1] << 16;
-}
+// two neighbouring 16-bit values off their alignment
+__device__ __forceinline__ uint32_t load_pair(const uint16_t *p) { return (uint32_t)p[0] | (uint32_t)p[1] << 16; }
 
 // The copies of a warp's steps: a cursor that runs ahead. Lanes 0 .. 7 hold a box each (values or keys, half of the head, eight keys
 // where pages are that small), with its page of the next step already loaded.
@@ -103,11 +98,12 @@ template <int DP> struct FewCopies {
     }
 };
 
-template <typename T, int DP>
+// NK: head size in steps of 16 (the copies bring zeros past it)
+template <typename T, int NK>
 __global__ void __launch_bounds__(FEW_WARPS * 32, 1)
 ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const AttnArgs a)
 {
-    constexpr int ST = few_stages(DP), NK = DP / 16;
+    constexpr int DP = NK > 4 ? 128 : 64, ST = few_stages(DP);
     constexpr uint32_t PART = few_part(DP);
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t *const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -129,10 +125,10 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     __syncthreads();
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
-    int64_t total, first, count;
-    int grid;
+    int64_t first, count;
+    AttnDeal deal(0, 0);
     AttnCursor cur;
-    if (!attn_locate(a, place, total, first, count, grid, cur)) {
+    if (!attn_locate(a, place, deal, first, count, cur)) {
         if (threadIdx.x == 0 && !a.common) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
         return;
     }
@@ -150,7 +146,7 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     const uint32_t at_v = PART + (uint32_t)(rv * 128), xv = (uint32_t)(((lane >> 4) ^ (rv & 7)) << 4);
 
     uint32_t qf[NK][4];
-    float o[DP / 8][4], m[2], l[2];
+    float o[2 * NK][4], m[2], l[2];
     AttnRow row[2];
     int tile0 = cur.tile, st = 0, all_lo = 0, all_hi = 0;
     uint32_t phase = 0;
@@ -162,29 +158,33 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
         if (fresh) {
             fresh = false;
             tile0 = cur.tile;
-            all_lo = 0; all_hi = INT_MAX;
+            const AttnRow w = attn_row(a, cur.q, cur.hu, cur.rt, lane & 15);
+            if (warp == 0 && lane < 16) rows[lane] = make_int2(w.token, w.head);
+            all_lo = w.token >= 0 ? w.lo : 0;
+            all_hi = w.token >= 0 ? w.hi : INT_MAX;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                row[i] = attn_row(a, cur.q, cur.hu, cur.rt, g + 8 * i);
-                if (warp == 0 && tq == 0) rows[g + 8 * i] = make_int2(row[i].token, row[i].head);
-                if (row[i].token >= 0) { all_lo = imax(all_lo, row[i].lo); all_hi = imin(all_hi, row[i].hi); }
-                m[i] = -INFINITY; l[i] = 0.f;
-                const T *p = static_cast<const T *>(a.q) + (row[i].token < 0 ? 0 : row[i].token * a.q_ts + row[i].head * a.q_hs);
-#pragma unroll
-                for (int k = 0; k < NK; ++k)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int d = k * 16 + h * 8 + tq * 2;
-                        qf[k][h * 2 + i] = row[i].token >= 0 && d < a.D ? load_pair<T>(p + d) : 0u;
-                    }
-            }
-#pragma unroll
-            for (int s = 4; s < 32; s <<= 1) {
+            for (int s = 1; s < 16; s <<= 1) {
                 all_lo = imax(all_lo, __shfl_xor_sync(0xffffffffu, all_lo, s));
                 all_hi = imin(all_hi, __shfl_xor_sync(0xffffffffu, all_hi, s));
             }
 #pragma unroll
-            for (int n = 0; n < DP / 8; ++n)
+            for (int i = 0; i < 2; ++i) {
+                const int token = __shfl_sync(0xffffffffu, w.token, g + 8 * i), head = __shfl_sync(0xffffffffu, w.head, g + 8 * i);
+                row[i].lo = __shfl_sync(0xffffffffu, w.lo, g + 8 * i);
+                row[i].hi = __shfl_sync(0xffffffffu, w.hi, g + 8 * i);
+                m[i] = -INFINITY; l[i] = 0.f;
+                const T *p = static_cast<const T *>(a.q) + (token < 0 ? 0 : token * a.q_ts + head * a.q_hs) + tq * 2;
+                if ((reinterpret_cast<uintptr_t>(p) & 3) == 0) {
+#pragma unroll
+                    for (int k = 0; k < 2 * NK; ++k) qf[k / 2][k % 2 * 2 + i] = token >= 0 && k * 8 < a.D ? *reinterpret_cast<const uint32_t *>(p + k * 8) : 0u;
+                } else {
+#pragma unroll
+                    for (int k = 0; k < 2 * NK; ++k)
+                        qf[k / 2][k % 2 * 2 + i] = token >= 0 && k * 8 < a.D ? load_pair(reinterpret_cast<const uint16_t *>(p + k * 8)) : 0u;
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < 2 * NK; ++n)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
         }
@@ -192,15 +192,18 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
         const int j0 = attn_tile_at(cur.t, cur.tile) * FEW_BN + warp * FEW_KEYS;
         const uint32_t base = ring + (uint32_t)st * 2 * PART;
         if (ok && j0 < cur.t.end && j0 + FEW_KEYS > a.kv0 && (j0 + FEW_KEYS > cur.t.w0 || j0 < a.sinks)) {
-            float s[2][4] = {};
+            float s[2][4] = {}, s1[2][4] = {};          // (two sums each, half as long a chain)
 #pragma unroll
-            for (int k = 0; k < NK; ++k)
-                if (k * 16 < a.D) {
-                    uint32_t b[4];
-                    ldsm4(b, base + at_k + (uint32_t)(k / 4) * FEW_PANEL + ((uint32_t)(k % 4 * 32) ^ xk));
-                    mma16<T>(s[0], qf[k], b[0], b[1]);
-                    mma16<T>(s[1], qf[k], b[2], b[3]);
-                }
+            for (int k = 0; k < NK; ++k) {
+                uint32_t b[4];
+                ldsm4(b, base + at_k + (uint32_t)(k / 4) * FEW_PANEL + ((uint32_t)(k % 4 * 32) ^ xk));
+                mma16<T>(k & 1 ? s1[0] : s[0], qf[k], b[0], b[1]);
+                mma16<T>(k & 1 ? s1[1] : s[1], qf[k], b[2], b[3]);
+            }
+#pragma unroll
+            for (int n = 0; n < 2; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[n][e] += s1[n][e];
             const bool all = j0 + FEW_KEYS <= all_hi && j0 >= a.kv0 && (j0 >= all_lo || j0 + FEW_KEYS <= a.sinks);
             if (!all) {
 #pragma unroll
@@ -232,7 +235,7 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
                     m[i] = to;
                     l[i] *= f;
 #pragma unroll
-                    for (int n = 0; n < DP / 8; ++n) { o[n][2 * i] *= f; o[n][2 * i + 1] *= f; }
+                    for (int n = 0; n < 2 * NK; ++n) { o[n][2 * i] *= f; o[n][2 * i + 1] *= f; }
                 }
             }
             uint32_t p[4];
@@ -247,13 +250,12 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
                 }
             }
 #pragma unroll
-            for (int n = 0; n < NK; ++n)
-                if (n * 16 < a.D) {
-                    uint32_t b[4];
-                    ldsm4t(b, base + at_v + (uint32_t)(n / 4) * FEW_PANEL + ((uint32_t)(n % 4 * 32) ^ xv));
-                    mma16<T>(o[2 * n], p, b[0], b[1]);
-                    mma16<T>(o[2 * n + 1], p, b[2], b[3]);
-                }
+            for (int n = 0; n < NK; ++n) {
+                uint32_t b[4];
+                ldsm4t(b, base + at_v + (uint32_t)(n / 4) * FEW_PANEL + ((uint32_t)(n % 4 * 32) ^ xv));
+                mma16<T>(o[2 * n], p, b[0], b[1]);
+                mma16<T>(o[2 * n + 1], p, b[2], b[3]);
+            }
         }
         if (++st == ST) { st = 0; phase ^= 1u; }
         const bool last = step + 1 == count;
@@ -275,7 +277,7 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
                 if (i * 8 >= nr) break;
                 if (i) __syncthreads();
 #pragma unroll
-                for (int k = 0; k < DP / 8; ++k)
+                for (int k = 0; k < 2 * NK; ++k)
                     *reinterpret_cast<float2 *>(meet + (warp * 8 + g) * DP + k * 8 + tq * 2) = make_float2(o[k][2 * i], o[k][2 * i + 1]);
                 __syncthreads();
                 constexpr int N = 4, TPR = DP / N;          // threads a row
@@ -300,7 +302,7 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
                 }
             }
             __syncthreads();
-            if (last && threadIdx.x == 0 && !a.common) attn_describe(a, cur, total, grid, c, first, first + step + 1 - n, tile0, n);
+            if (last && threadIdx.x == 0 && !a.common) attn_describe(a, cur, deal, c, step + 1 - n, tile0, n);
             fresh = true;
         }
         cur.next(a, !last);
@@ -313,40 +315,71 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     }
 }
 
-// Joins the partial results of an item that several blocks have worked on: block (c, i) rows 16 i .. 16 i + 15 of the item that
-// begins in block c, in the order of its keys.
-template <typename T>
-__global__ void __launch_bounds__(256) ubp_attention_join_kernel(const AttnArgs a)
+// Joins the partial results of an item that several blocks have worked on, in the order of its keys: 16 rows a block.
+// COMMON: block (u, i) takes rows 16 i .. of item u of the shared prefix; all of its blocks' results lie in slots u + block, and the
+// sums go to pml and ppo. Else block (c, i) takes those of the item that begins in block c, if it does not end there.
+template <typename T, bool COMMON>
+__global__ void __launch_bounds__(256) ubp_attention_join_kernel(const AttnArgs a, const int blocks)
 {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int c = (int)blockIdx.x;
-    const int4 d = a.desc[c];
-    const int parts = d.w >> 1;
+    int t0, n, hu, parts;
+    int64_t slot0, slot1;                   // of the first part, and of the second one (the others follow)
+    if constexpr (COMMON) {
+        const AttnSeq q = attn_seq(a, 0);
+        const int nrt = attn_row_blocks(a, q), nt = attn_block_tiles(a, q, 0).nt, u = (int)blockIdx.x;
+        if (u >= nrt * a.HU) return;
+        const AttnDeal deal((int64_t)nrt * a.HU * nt, blocks);
+        hu = u / nrt;
+        t0 = (u - hu * nrt) * a.tpt;
+        n = q.n - t0;
+        const int c = deal.owner((int64_t)u * nt);
+        parts = deal.owner((int64_t)(u + 1) * nt - 1) - c + 1;
+        slot0 = u + c; slot1 = slot0 + 1;
+    } else {
+        const int c = (int)blockIdx.x;
+        const int4 d = a.desc[c];
+        t0 = d.x; n = d.y; hu = d.z; parts = d.w >> 1;
+        slot0 = 2 * (int64_t)c + (d.w & 1);
+        slot1 = 2 * (int64_t)(c + 1);
+    }
     if (parts == 0) return;
-    const AttnSeq q = attn_seq(a, d.x);
     constexpr int N = 4;
-    const int per = a.D / N;
+    const int per = a.D / N, step = COMMON ? 1 : 2;
     for (int x = (int)threadIdx.x; x < 16 * per; x += 256) {
         const int r = (int)blockIdx.y * 16 + x / per, col = x % per * N;
-        const AttnRow w = attn_row(a, q, d.y, d.z, r);
-        if (w.token < 0) continue;
+        const int2 w = attn_row_at(a, t0, n, hu, r);
+        if (w.x < 0) continue;
         float M = -INFINITY, L = 0.f, o[N] = {};
+#pragma unroll 4
         for (int k = 0; k < parts; ++k) {
-            const int64_t at = (2 * (int64_t)(c + k) + (k == 0 ? (d.w & 1) : 0)) * a.rows + r;
+            const int64_t at = (k == 0 ? slot0 : slot1 + (int64_t)(k - 1) * step) * a.rows + r;
             const float2 ml = a.ml[at];
             float v[N];
             attn_load(a.po + at * a.D + col, v);
             attn_add(M, L, o, ml.x, ml.y, v);
         }
-        attn_finish<T>(a, w.token, w.head, col, M, L, o);
+        if constexpr (COMMON) {
+            const int64_t at = (int64_t)w.x * a.Hq + w.y;
+            if (col == 0) a.pml[at] = make_float2(M, L);
+            *reinterpret_cast<float4 *>(a.ppo + at * a.D + col) = make_float4(o[0], o[1], o[2], o[3]);
+        } else {
+            attn_finish<T>(a, w.x, w.y, col, M, L, o);
+        }
     }
 }
 
-template <typename T, int DP> int launch_few_t(const CUtensorMap &k, const CUtensorMap &v, const AttnArgs &a, int grid, void *stream)
+template <typename T> int launch_few_t(const CUtensorMap &k, const CUtensorMap &v, const AttnArgs &a, int grid, void *stream)
 {
-    static std::atomic<bool> done[64] = {};
-    return attn_launch(ubp_attention_few_kernel<T, DP>, done, dim3((unsigned)grid), FEW_WARPS * 32, few_smem(DP), stream, k, v, a);
+    static std::atomic<bool> done[5][64] = {};
+    const dim3 g((unsigned)grid);
+    switch (a.D <= 64 ? 4 : (a.D + 15) / 16) {
+        case 4: return attn_launch(ubp_attention_few_kernel<T, 4>, done[0], g, FEW_WARPS * 32, few_smem(64), stream, k, v, a);
+        case 5: return attn_launch(ubp_attention_few_kernel<T, 5>, done[1], g, FEW_WARPS * 32, few_smem(128), stream, k, v, a);
+        case 6: return attn_launch(ubp_attention_few_kernel<T, 6>, done[2], g, FEW_WARPS * 32, few_smem(128), stream, k, v, a);
+        case 7: return attn_launch(ubp_attention_few_kernel<T, 7>, done[3], g, FEW_WARPS * 32, few_smem(128), stream, k, v, a);
+        default: return attn_launch(ubp_attention_few_kernel<T, 8>, done[4], g, FEW_WARPS * 32, few_smem(128), stream, k, v, a);
+    }
 }
 
 }  // namespace
@@ -356,16 +389,19 @@ int launch_attn_few(const AttnArgs &a, int dtype, int grid, void *stream)
     CUtensorMap k, v;
     if (const int rc = attn_encode_cache(&k, a, a.k, dtype, FEW_KEYS)) return rc;
     if (const int rc = attn_encode_cache(&v, a, a.v, dtype, FEW_KEYS)) return rc;
-    if (dtype == UBP_BF16) return a.D <= 64 ? launch_few_t<__nv_bfloat16, 64>(k, v, a, grid, stream) : launch_few_t<__nv_bfloat16, 128>(k, v, a, grid, stream);
-    return a.D <= 64 ? launch_few_t<__half, 64>(k, v, a, grid, stream) : launch_few_t<__half, 128>(k, v, a, grid, stream);
+    return dtype == UBP_BF16 ? launch_few_t<__nv_bfloat16>(k, v, a, grid, stream) : launch_few_t<__half>(k, v, a, grid, stream);
 }
 
 int launch_attn_join(const AttnArgs &a, int dtype, int grid, void *stream)
 {
-    const dim3 g((unsigned)grid, (unsigned)((a.rows + 15) / 16));
     static std::atomic<bool> done[64] = {};
-    return dtype == UBP_BF16 ? attn_launch(ubp_attention_join_kernel<__nv_bfloat16>, done, g, 256, 0, stream, a)
-                             : attn_launch(ubp_attention_join_kernel<__half>, done, g, 256, 0, stream, a);
+    const unsigned y = (unsigned)((a.rows + 15) / 16);
+    if (a.common) {
+        const int64_t units = (int64_t)((a.T + a.tpt - 1) / a.tpt) * a.HU;
+        return attn_launch(ubp_attention_join_kernel<__half, true>, done, dim3((unsigned)units, y), 256, 0, stream, a, grid);
+    }
+    return dtype == UBP_BF16 ? attn_launch(ubp_attention_join_kernel<__nv_bfloat16, false>, done, dim3((unsigned)grid, y), 256, 0, stream, a, grid)
+                             : attn_launch(ubp_attention_join_kernel<__half, false>, done, dim3((unsigned)grid, y), 256, 0, stream, a, grid);
 }
 
 }  // namespace ubp

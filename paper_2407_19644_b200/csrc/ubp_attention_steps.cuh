@@ -81,9 +81,9 @@ __device__ __forceinline__ void attn_place(const AttnArgs &a, int b, int64_t rem
     cur.set(a, b, hu, rt, (int)rem);
 }
 
-// The block's steps: [first, first + count) of `total`, and the cursor at the first one. Called by all threads of the block (a
-// multiple of 32); returns false, to all of them, if there is nothing to do. `grid`: blocks that have steps.
-__device__ __forceinline__ bool attn_locate(const AttnArgs &a, AttnPlace &sh, int64_t &total, int64_t &first, int64_t &count, int &grid, AttnCursor &cur)
+// The block's steps, [first, first + count), and the cursor at the first one. Called by all threads of the block (a multiple of
+// 32); returns false, to all of them, if there is nothing to do.
+__device__ __forceinline__ bool attn_locate(const AttnArgs &a, AttnPlace &sh, AttnDeal &deal, int64_t &first, int64_t &count, AttnCursor &cur)
 {
     const int nt = (int)blockDim.x, tid = (int)threadIdx.x, lane = tid & 31, warp = tid >> 5, nw = nt >> 5;
     const int nb = a.common ? 1 : a.B;
@@ -95,18 +95,16 @@ __device__ __forceinline__ bool attn_locate(const AttnArgs &a, AttnPlace &sh, in
             const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
             if (lane >= o) x += y;
         }
-        total = __shfl_sync(0xffffffffu, x, 31);
-        grid = total < (int64_t)gridDim.x ? (int)total : (int)gridDim.x;
+        deal = AttnDeal(__shfl_sync(0xffffffffu, x, 31), (int)gridDim.x);
         const int c = (int)blockIdx.x;
-        if (c >= grid) return false;
-        first = attn_first_step(total, c, grid);
-        count = attn_first_step(total, c + 1, grid) - first;
+        if (c >= deal.grid) return false;
+        first = deal.first(c);
+        count = deal.count(c);
         const int b = __ffs(__ballot_sync(0xffffffffu, x > first)) - 1;
         attn_place(a, b, first - __shfl_sync(0xffffffffu, x - mine, b), cur);
         return true;
     }
-    total = 0;
-    int64_t mine = 0, before = 0;       // steps of this thread's sequence, and of all sequences before it in the chunk
+    int64_t total = 0, mine = 0, before = 0;       // steps of this thread's sequence, and of all sequences before it in the chunk
     auto scan = [&](int base) {         // -> steps of the chunk of nt sequences from base on
         const int b = base + tid;
         mine = attn_seq_steps(a, b, b < nb);
@@ -129,11 +127,11 @@ __device__ __forceinline__ bool attn_locate(const AttnArgs &a, AttnPlace &sh, in
         return all;
     };
     for (int base = 0; base < nb; base += nt) total += scan(base);
-    grid = total < (int64_t)gridDim.x ? (int)total : (int)gridDim.x;
+    deal = AttnDeal(total, (int)gridDim.x);
     const int c = (int)blockIdx.x;
-    if (c >= grid) return false;
-    first = attn_first_step(total, c, grid);
-    count = attn_first_step(total, c + 1, grid) - first;
+    if (c >= deal.grid) return false;
+    first = deal.first(c);
+    count = deal.count(c);
     int64_t at = first;
     for (int base = 0; base < nb; base += nt) {
         const int64_t all = nb > nt ? scan(base) : total;
@@ -161,24 +159,30 @@ __device__ __forceinline__ int attn_seq_of(const int32_t *starts, int B, int t)
     return t < starts[lo + 1] ? lo : -1;
 }
 
+// Row r of a row block with n tokens from token t0 on: its token (-1 if the row does not exist) and query head.
+__device__ __forceinline__ int2 attn_row_at(const AttnArgs &a, int t0, int n, int hu, int r)
+{
+    const int per = a.rows / a.tiles, tile = r >= per ? 1 : 0, i = r - tile * per, tpt = a.tpt / a.tiles;
+    const int ti = (int)((uint32_t)i / (uint32_t)a.gc), kvh = (int)((uint32_t)hu / (uint32_t)a.chunks);
+    const int g = (hu - kvh * a.chunks) * a.gc + i - ti * a.gc, t = tile * tpt + ti;
+    return ti < tpt && g < a.G && t < n ? make_int2(t0 + t, kvh * a.G + g) : make_int2(-1, 0);
+}
+
 // A row of an item: its token among the call's, its query head, and the keys that it sees: j < hi and (j >= lo or j < sinks), of
 // [kv0, kv1). A row that does not exist has token -1 and sees nothing.
 struct AttnRow { int token, head, lo, hi; };
 __device__ __forceinline__ AttnRow attn_row(const AttnArgs &a, const AttnSeq &q, int hu, int rt, int r)
 {
-    const int per = a.rows / a.tiles, tile = r / per, i = r - tile * per, ti = i / a.gc, g = hu % a.chunks * a.gc + i % a.gc;
-    const int t = rt * a.tpt + tile * (a.tpt / a.tiles) + ti;
-    AttnRow w{-1, 0, 0, 0};
-    if (i >= a.tpt / a.tiles * a.gc || g >= a.G || t >= q.n) return w;
-    int pos = q.len - q.n + t;
+    const int2 at = attn_row_at(a, q.s + rt * a.tpt, q.n - rt * a.tpt, hu, r);
+    AttnRow w{at.x, at.y, 0, 0};
+    if (w.token < 0) return w;
+    int pos = q.len - q.n + w.token - q.s;
     if (a.common) {
-        const int b = a.starts ? attn_seq_of(a.starts, a.B, t) : t;
-        if (b < 0) return w;
+        const int t = w.token, b = a.starts ? attn_seq_of(a.starts, a.B, t) : t;
+        if (b < 0) { w.token = -1; return w; }
         const int s = a.starts ? imax(a.starts[b], 0) : t, e = a.starts ? imin(a.starts[b + 1], a.T) : t + 1;
         pos = imin(imax(a.lengths[b], 0), a.cap) - (e - s) + (t - s);
     }
-    w.token = q.s + t;
-    w.head = hu / a.chunks * a.G + g;
     w.hi = imin(pos + 1, a.kv1);
     w.lo = a.window > 0 ? imax(pos - a.window + 1, 0) : 0;
     return w;
@@ -207,25 +211,6 @@ template <int N> __device__ __forceinline__ void attn_load(const float *p, float
         v[i] = f.x; v[i + 1] = f.y; v[i + 2] = f.z; v[i + 3] = f.w;
     }
 }
-// The shared prefix's partial results of a row, in their order: N values from column col on.
-template <int N> __device__ __forceinline__ void attn_add_prefix(const AttnArgs &a, int token, int head, int col, float &M, float &L, float (&o)[N])
-{
-    const int valid = a.starts ? imin(imax(a.starts[a.B], 0), a.T) : a.T;
-    const int g = head % a.G, hu = head / a.G * a.p_chunks + g / a.p_gc, nrt = (valid + a.p_tpt - 1) / a.p_tpt;
-    const int rt = token / a.p_tpt, ti = token % a.p_tpt, per = a.p_tpt / a.p_tiles;
-    const int row = ti / per * (a.p_rows / a.p_tiles) + ti % per * a.p_gc + g % a.p_gc;
-    const int64_t u = (int64_t)hu * nrt + rt, total = (int64_t)a.HU / a.chunks * a.p_chunks * nrt * a.p_nt;
-    const int grid = total < a.p_grid ? (int)total : a.p_grid;
-    const int c0 = attn_owner(total, u * a.p_nt, grid), c1 = attn_owner(total, (u + 1) * a.p_nt - 1, grid);
-    for (int c = c0; c <= c1; ++c) {
-        const int64_t at = (u + c) * a.p_rows + row;
-        const float2 ml = a.pml[at];
-        float v[N];
-        attn_load(a.ppo + at * a.D + col, v);
-        attn_add(M, L, o, ml.x, ml.y, v);
-    }
-}
-
 template <typename T, int N> __device__ __forceinline__ void attn_store(T *p, const float (&v)[N])
 {
     static_assert(N == 4 || N == 8, "");
@@ -240,22 +225,28 @@ template <typename T, int N> __device__ __forceinline__ void attn_store(T *p, co
 // Finished sums of a row, from column col on, to the output: o / L, 0 where nothing was seen.
 template <typename T, int N> __device__ __forceinline__ void attn_finish(const AttnArgs &a, int token, int head, int col, float M, float L, float (&o)[N])
 {
-    if (a.pml) attn_add_prefix(a, token, head, col, M, L, o);
+    if (a.pml) {
+        const int64_t at = (int64_t)token * a.Hq + head;
+        const float2 ml = a.pml[at];
+        float v[N];
+        attn_load(a.ppo + at * a.D + col, v);
+        attn_add(M, L, o, ml.x, ml.y, v);
+    }
     const float r = L == 0.f ? 0.f : 1.f / L;
 #pragma unroll
     for (int i = 0; i < N; ++i) o[i] *= r;
     attn_store(static_cast<T *>(a.out) + token * a.o_ts + head * a.o_hs + col, o);
 }
 
-// What block c leaves behind for the join: its last item if that begins here and ends in a later block.
-// x: steps before the block's last segment, done: tiles of that segment's item before it, n: its tiles here, nt: the item's.
-__device__ __forceinline__ void attn_describe(const AttnArgs &a, const AttnCursor &at, int64_t total, int grid, int c, int64_t first, int64_t x,
-                                              int tile0, int n)
+// What block c leaves behind for the join: its last item if that begins here and ends in a later block, as {first token, tokens,
+// unit head, 2 * blocks that share it + (the item is not the block's first segment)}.
+// x: the block's steps before its last segment, n: that segment's tiles, tile0: the first of them.
+__device__ __forceinline__ void attn_describe(const AttnArgs &a, const AttnCursor &at, const AttnDeal &deal, int c, int64_t x, int tile0, int n)
 {
     int4 d = make_int4(0, 0, 0, 0);
     if (tile0 == 0 && n < at.t.nt) {
-        const int last = attn_owner(total, x + at.t.nt - 1, grid);
-        d = make_int4(at.b, at.hu, at.rt, (last - c + 1) << 1 | (x > first ? 1 : 0));
+        const int last = deal.owner(deal.first(c) + x + at.t.nt - 1);
+        d = make_int4(at.q.s + at.rt * a.tpt, at.q.n - at.rt * a.tpt, at.hu, (last - c + 1) << 1 | (x > 0 ? 1 : 0));
     }
     a.desc[c] = d;
 }

@@ -142,12 +142,12 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
     const uint32_t tmem = tmem_slot;
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
-    int64_t total, first;
-    int grid;
+    int64_t first;
+    AttnDeal deal(0, 0);
     AtSegments sg;
     bool ok = true;
     int filled = 0;                        // copy warp: stages filled so far (keys and values alike)
-    if (!attn_locate(a, place, total, first, sg.left, grid, sg.cur)) {
+    if (!attn_locate(a, place, deal, first, sg.left, sg.cur)) {
         sg.left = 0;
         if (threadIdx.x == 0 && !a.common) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
     }
@@ -390,7 +390,7 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                 }
             }
             if (tile == 0 && r == 0 && !a.common && sg.left == sg.n)
-                attn_describe(a, sg.cur, total, grid, c, first, first + count - sg.n, sg.tile0, sg.n);
+                attn_describe(a, sg.cur, deal, c, count - sg.n, sg.tile0, sg.n);
         }
     }
     if (!ok && lane == 0) atomicExch(a.status, 1);
