@@ -24,6 +24,8 @@
 
 namespace ubp {
 
+constexpr int ATTN_BN = 128;        // keys a step takes
+
 struct AttnArgs {
     const void *q;
     int64_t q_ts, q_hs;             // strides of q between tokens and heads (elements)
@@ -41,7 +43,6 @@ struct AttnArgs {
     int tiles;                      // row tiles of a row block (each rows / tiles rows)
     int gc, chunks, HU;             // heads of a unit head, unit heads of a key head, unit heads in all
     int tpt;                        // tokens a row block takes
-    int bn;                         // keys a step takes
     float sc;                       // scale * log2(e)
     int window, sinks;
     int kv0, kv1;                   // keys outside [kv0, kv1) are left out (a shared prefix is a call of its own)
@@ -88,12 +89,12 @@ UBP_HD AttnTiles attn_tiles(const AttnArgs &a, int p0, int p1)
     AttnTiles t;
     t.end = imin(p1 + 1, a.kv1);
     t.w0 = a.window > 0 && !a.common ? imax(a.kv0, p0 - a.window + 1) : a.kv0;
-    t.s0 = a.kv0 / a.bn;
-    t.lo = t.w0 / a.bn;
+    t.s0 = a.kv0 / ATTN_BN;
+    t.lo = t.w0 / ATTN_BN;
     t.ns = 0;
     if (t.end <= a.kv0) { t.end = a.kv0; t.lo = t.s0; t.nt = 1; return t; }
-    if (t.lo > t.s0 && a.sinks > a.kv0) t.ns = imin((imin(a.sinks, t.end) + a.bn - 1) / a.bn - t.s0, t.lo - t.s0);
-    t.nt = t.ns + imax(0, (t.end + a.bn - 1) / a.bn - t.lo);
+    if (t.lo > t.s0 && a.sinks > a.kv0) t.ns = imin((imin(a.sinks, t.end) + ATTN_BN - 1) / ATTN_BN - t.s0, t.lo - t.s0);
+    t.nt = t.ns + imax(0, (t.end + ATTN_BN - 1) / ATTN_BN - t.lo);
     if (t.nt < 1) t.nt = 1;
     return t;
 }

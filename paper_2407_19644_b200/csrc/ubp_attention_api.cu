@@ -56,10 +56,10 @@ int check_cache(const ubp_cache_t *c, int64_t T, int q_heads)
 namespace {
 
 // Rows of an item and how the heads of a group are dealt to them.
-void set_rows(AttnArgs &a, int rows, int tiles, int bn)
+void set_rows(AttnArgs &a, int rows, int tiles)
 {
     const int per = rows / tiles;
-    a.rows = rows; a.tiles = tiles; a.bn = bn;
+    a.rows = rows; a.tiles = tiles;
     a.chunks = (a.G + per - 1) / per;
     a.gc = (a.G + a.chunks - 1) / a.chunks;
     a.HU = a.Hq / a.G * a.chunks;
@@ -90,12 +90,12 @@ int attn_plan(const ubp_cache_t *c, int64_t T, int q_heads, float scale, int win
     a.window = window; a.sinks = window > 0 ? sinks : 0;
     a.kv0 = (int)prefix; a.kv1 = INT32_MAX;
     p.own_tc = std::min<int64_t>(max_new, T) * a.G > 16;
-    if (p.own_tc) set_rows(a, 256, 2, 128);
-    else set_rows(a, 16, 1, 128);
+    if (p.own_tc) set_rows(a, 256, 2);
+    else set_rows(a, 16, 1);
     // more blocks than steps would have nothing to do
-    const int64_t seen = window > 0 ? std::min<int64_t>(a.cap, (int64_t)window + sinks + a.tpt + 2 * a.bn) : a.cap;
+    const int64_t seen = window > 0 ? std::min<int64_t>(a.cap, (int64_t)window + sinks + a.tpt + 2 * ATTN_BN) : a.cap;
     const int64_t items = (a.T / a.tpt + (int64_t)a.B) * a.HU;
-    p.own_grid = (int)std::min<int64_t>(sms, items * ((seen + a.bn - 1) / a.bn + 1));
+    p.own_grid = (int)std::min<int64_t>(sms, items * ((seen + ATTN_BN - 1) / ATTN_BN + 1));
     p.own_space = attn_space(p.own_grid, 2 * (int64_t)p.own_grid, a.rows, a.D);
     p.bytes = p.own_space.total;
     if (prefix > 0) {
@@ -103,10 +103,10 @@ int attn_plan(const ubp_cache_t *c, int64_t T, int q_heads, float scale, int win
         b.common = 1;
         b.kv0 = 0; b.kv1 = (int)prefix;
         p.common_tc = T * b.G > 16;
-        if (p.common_tc) set_rows(b, 256, 2, 128);
-        else set_rows(b, 16, 1, 128);
+        if (p.common_tc) set_rows(b, 256, 2);
+        else set_rows(b, 16, 1);
         const int64_t units = (int64_t)((b.T + b.tpt - 1) / b.tpt) * b.HU;
-        const int nt = (int)((prefix + b.bn - 1) / b.bn);
+        const int nt = (int)((prefix + ATTN_BN - 1) / ATTN_BN);
         p.common_grid = (int)std::min<int64_t>(sms, units * nt);
         if (units + p.common_grid > INT32_MAX) return UBP_E_UNSUPPORTED;
         p.common_space = attn_space(0, units + p.common_grid, b.rows, b.D);

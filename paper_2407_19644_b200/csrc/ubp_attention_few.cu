@@ -30,7 +30,7 @@ using namespace tc;
 
 constexpr int FEW_WARPS = 8, FEW_KEYS = 16, FEW_ROWS = 16;
 constexpr int FEW_BN = FEW_WARPS * FEW_KEYS;
-static_assert(FEW_ROWS == 16 && FEW_BN == 128, "as the launch fills AttnArgs");
+static_assert(FEW_BN == ATTN_BN, "");
 constexpr uint32_t FEW_PANEL = FEW_KEYS * 128;                  // 64 values of each of a warp's keys
 __host__ __device__ constexpr int few_stages(int dp) { return dp == 128 ? 3 : 6; }
 __host__ __device__ constexpr uint32_t few_part(int dp) { return (uint32_t)(dp / 64) * FEW_PANEL; }            // keys (or values) of a warp's step
@@ -58,40 +58,44 @@ template <typename T> __device__ __forceinline__ void mma16(float (&c)[4], const
 // two neighbouring 16-bit values off their alignment
 __device__ __forceinline__ uint32_t load_pair(const uint16_t *p) { return (uint32_t)p[0] | (uint32_t)p[1] << 16; }
 
-// The copies of a warp's steps: a cursor that runs ahead. Lanes 0 .. 7 hold a box each (values or keys, half of the head, eight keys
-// where pages are that small), with its page of the next step already loaded.
+// The copies of a warp's steps: a cursor that runs ahead, with the pages of the next step already loaded (one, or two of eight keys).
+// Everything is the same in all lanes; lane 0 issues.
 template <int DP> struct FewCopies {
     AttnCursor c;
     int64_t left;            // steps that are not issued yet
-    int page, j0, kvh;
+    int page[2], j0, kvh;
     const int32_t *row;
-    int box, nbox, bx, px, kv;   // this lane's
 
-    __device__ __forceinline__ void begin(const AttnArgs &a, int lane)
-    {
-        box = imin(1 << a.pshift, FEW_KEYS);
-        nbox = FEW_KEYS / box;
-        bx = lane % nbox; px = lane / nbox % (DP / 64); kv = lane / nbox / (DP / 64);
-        item(a);
-    }
     __device__ __forceinline__ void item(const AttnArgs &a)
     {
-        kvh = c.hu / a.chunks;
+        kvh = (int)((uint32_t)c.hu / (uint32_t)a.chunks);
         row = a.table + (a.common ? 0 : (int64_t)c.b * a.ldt);
     }
     __device__ __forceinline__ void peek(const AttnArgs &a, int warp)
     {
         j0 = attn_tile_at(c.t, c.tile) * FEW_BN + warp * FEW_KEYS;
-        if (kv < 2) page = attn_box_page(a, c.t, row, j0 + bx * box, box);
+        page[0] = attn_box_page(a, c.t, row, j0, imin(1 << a.pshift, FEW_KEYS));
+        if (a.pshift == 3) page[1] = attn_box_page(a, c.t, row, j0 + 8, 8);
     }
     __device__ __forceinline__ void issue(const AttnArgs &a, const CUtensorMap *tmK, const CUtensorMap *tmV, uint32_t stage, uint32_t bar, int warp, int lane)
     {
         if (left <= 0) return;
-        if (lane == 0) mbar_expect_tx(bar, 2 * few_part(DP));
-        __syncwarp();
-        if (kv < 2)
-            tma_load_4d(stage + (uint32_t)kv * few_part(DP) + (uint32_t)px * FEW_PANEL + (uint32_t)(bx * box) * 128u, kv ? tmV : tmK, px * 64,
-                        (j0 + bx * box) & ((1 << a.pshift) - 1), kvh, page, bar);
+        if (lane == 0) {
+            const int at = j0 & ((1 << a.pshift) - 1);
+            mbar_expect_tx(bar, 2 * few_part(DP));
+#pragma unroll
+            for (int p = 0; p < DP / 64; ++p) {
+                tma_load_4d(stage + (uint32_t)p * FEW_PANEL, tmK, p * 64, at, kvh, page[0], bar);
+                tma_load_4d(stage + few_part(DP) + (uint32_t)p * FEW_PANEL, tmV, p * 64, at, kvh, page[0], bar);
+            }
+            if (a.pshift == 3) {
+#pragma unroll
+                for (int p = 0; p < DP / 64; ++p) {
+                    tma_load_4d(stage + (uint32_t)p * FEW_PANEL + 1024u, tmK, p * 64, 0, kvh, page[1], bar);
+                    tma_load_4d(stage + few_part(DP) + (uint32_t)p * FEW_PANEL + 1024u, tmV, p * 64, 0, kvh, page[1], bar);
+                }
+            }
+        }
         --left;
         if (++c.tile == c.t.nt && left > 0) { c.next_item(a); item(a); }
         if (left > 0) peek(a, warp);
@@ -135,7 +139,7 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     FewCopies<DP> copies;
     copies.c = cur;
     copies.left = count;
-    copies.begin(a, lane);
+    copies.item(a);
     copies.peek(a, warp);
     for (int s = 0; s < ST - 1; ++s) copies.issue(a, &tmK, &tmV, ring + (uint32_t)s * 2 * PART, smem_u32(&bar_full[warp][s]), warp, lane);
 

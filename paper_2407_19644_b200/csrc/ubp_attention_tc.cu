@@ -27,8 +27,10 @@ namespace {
 
 using namespace tc;
 
-constexpr int AT_BN = 128, AT_TILE = 128, AT_THREADS = 320;
-constexpr int AT_COPY_WARP = 8, AT_MMA_WARP = 9;
+constexpr int AT_BN = ATTN_BN, AT_TILE = 128, AT_THREADS = 384;
+constexpr int AT_COPY_WARP = 8, AT_MMA_WARP = 9;               // (of a third warpgroup, so that registers can be dealt)
+// Registers a thread: 168 at the launch (384 threads), then 208 for the softmax's two warpgroups and 80 for the third.
+constexpr int AT_POLY = 4;                                     // every fourth pair of weights on the multiply-add pipes
 constexpr uint32_t AT_PANEL = 128 * 128;                       // 128 rows of 64 values
 constexpr uint32_t AT_SWZ = 2;                                 // 128-byte swizzle
 __host__ __device__ constexpr int at_stages(int dp) { return dp == 128 ? 2 : 4; }
@@ -47,22 +49,76 @@ __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint3
     asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
                  ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
-__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t (&r)[32])
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16])
 {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], "
-        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, "
-        "%17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31, %32};"
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
         ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
-          "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
-          "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31])
-        : "memory");
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
 __device__ __forceinline__ void tmem_wait_ld() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tmem_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// two fp32 values at a time
+__device__ __forceinline__ uint64_t pair(float a, float b)
+{
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void halves(uint64_t v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
+{
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+// 2^x of two values on the multiply-add pipes, for finite x below 127 (a NaN stays one; below -126: at most 2^-126): the nearest
+// integer n by adding 1.5 2^23, a polynomial of degree 4 for 2^(x - n) on [-1/2, 1/2] (a fit of our own for the relative error:
+// 2.6 10^-6), times 2^n. The special function unit takes 16 results a cycle and SM, as long for a tile's weights as the tensor
+// cores for its products; a share of them here relieves it.
+__device__ __forceinline__ uint64_t exp2_poly(uint64_t x2)
+{
+    float a, b;
+    halves(x2, a, b);
+    x2 = pair(max_nan(a, -126.f), max_nan(b, -126.f));
+    const uint64_t big = pair(12582912.f, 12582912.f), t = add2(x2, big);
+    const uint64_t f = fma2(add2(t, pair(-12582912.f, -12582912.f)), pair(-1.f, -1.f), x2);
+    uint64_t p = fma2(f, pair(0.0095701f, 0.0095701f), pair(0.05591786f, 0.05591786f));
+    p = fma2(p, f, pair(0.24024745f, 0.24024745f));
+    p = fma2(p, f, pair(0.69312181f, 0.69312181f));
+    p = fma2(p, f, pair(0.99999926f, 0.99999926f));
+    halves(t, a, b);
+    return mul2(p, pair(__uint_as_float((__float_as_uint(a) << 23) + 0x3f800000u), __uint_as_float((__float_as_uint(b) << 23) + 0x3f800000u)));
+}
 
 // instruction descriptor: D = f32, A and B of one 16-bit type (0 = f16, 1 = bf16), A K-major, M = 128
 __device__ __forceinline__ uint32_t at_idesc(int n, int fmt, int b_mn)
@@ -154,7 +210,9 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
     const int64_t count = sg.left;
     const uint32_t s_q = smem_u32(smem), s_k = s_q + 2 * PART, s_v = s_k + ST * PART;
 
-    if (warp == AT_COPY_WARP) {
+    if (warp >= AT_COPY_WARP) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
+        if (warp == AT_COPY_WARP) {
         const int page_mask = (1 << a.pshift) - 1, box = imin(1 << a.pshift, AT_BN), nbox = AT_BN / box;
         int patches = 0;
         for (; ok && sg.get(); sg.done(a)) {
@@ -164,7 +222,7 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
             for (int i = 0; ok && i < sg.n; ++i, ++filled) {
                 const int st = filled % ST, j0 = attn_tile_at(t, sg.tile0 + i) * AT_BN;
                 // (a lane a box)
-                const int page = __shfl_sync(0xffffffffu, lane < nbox ? attn_box_page(a, t, row, j0 + lane * box, box) : a.pages, lane % nbox);
+                const int page = lane < nbox ? attn_box_page(a, t, row, j0 + lane * box, box) : a.pages;
                 // Places of a page whose keys no row sees: whatever they hold, a weight of 0 times it has to be 0, so the values
                 // there are overwritten with zeros before the product reads them.
                 const bool patch = (j0 + AT_BN > t.end && (t.end & (box - 1))) || (j0 < a.kv0 && j0 + AT_BN > a.kv0 && (a.kv0 & (box - 1))) ||
@@ -177,10 +235,13 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                     ok = __all_sync(0xffffffffu, ok);
                     if (!ok) break;
                     if (lane == 0) mbar_expect_tx(bar, PART);
-                    __syncwarp();
-                    if (lane < nbox * (DP / 64)) {          // (16 boxes of 8 tokens at most, in two halves)
-                        const int b = lane % nbox, p = lane / nbox;
-                        tma_load_4d(dst + (uint32_t)p * AT_PANEL + (uint32_t)(b * box) * 128u, kv ? &tmV : &tmK, p * 64, (j0 + b * box) & page_mask, kvh, page, bar);
+                    for (int b = 0; b < nbox; ++b) {
+                        const int pg = __shfl_sync(0xffffffffu, page, b);
+                        if (lane == 0) {
+#pragma unroll
+                            for (int p = 0; p < DP / 64; ++p)
+                                tma_load_4d(dst + (uint32_t)p * AT_PANEL + (uint32_t)(b * box) * 128u, kv ? &tmV : &tmK, p * 64, (j0 + b * box) & page_mask, kvh, pg, bar);
+                        }
                     }
                     __syncwarp();
                     if (kv && patch) {
@@ -199,7 +260,7 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                 }
             }
         }
-    } else if (warp == AT_MMA_WARP) {
+        } else if (warp == AT_MMA_WARP) {
         if (lane == 0) {
             const int fmt = std::is_same_v<T, __nv_bfloat16> ? 1 : 0, nk = (a.D + 15) / 16;
             const uint32_t id_s = at_idesc(AT_BN, fmt, 0), id_o = at_idesc(nk * 16, fmt, 1);
@@ -250,7 +311,9 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
             }
         }
         __syncwarp();
+        }
     } else {
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         const int tile = warp >> 2, r = (warp & 3) * 32 + lane;
         const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, t_s = tmem + lanes + (uint32_t)tile * 128u, t_o = t_s + 256u;
         uint8_t *const qs = smem + (uint32_t)tile * PART;
@@ -296,7 +359,8 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tmem_ld32(t_s + (uint32_t)c * 32u, s[c]);
                 tmem_wait_ld();
-                if (!(j0 + AT_BN <= all_hi && j0 >= a.kv0 && (j0 >= all_lo || j0 + AT_BN <= a.sinks))) {
+                const bool all = j0 + AT_BN <= all_hi && j0 >= a.kv0 && (j0 >= all_lo || j0 + AT_BN <= a.sinks);
+                if (!all) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
 #pragma unroll
@@ -306,11 +370,12 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                 float mx[4];
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    mx[c] = __uint_as_float(s[c][0]);
+                    mx[c] = max3(__uint_as_float(s[c][0]), __uint_as_float(s[c][1]), __uint_as_float(s[c][2]));
 #pragma unroll
-                    for (int e = 1; e < 32; ++e) mx[c] = fmaxf(mx[c], __uint_as_float(s[c][e]));
+                    for (int e = 3; e < 31; e += 2) mx[c] = max3(mx[c], __uint_as_float(s[c][e]), __uint_as_float(s[c][e + 1]));
+                    mx[c] = fmaxf(mx[c], __uint_as_float(s[c][31]));
                 }
-                const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * a.sc;
+                const float top = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * a.sc;
                 if (__any_sync(0xffffffffu, top > m + 8.f)) {
                     const float to = fmaxf(m, top), f = m == -INFINITY ? 0.f : attn_exp2(m - to);
                     m = to;
@@ -319,36 +384,46 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
 #pragma unroll 1
                         for (int c = 0; c < (a.D + 15) / 16; ++c) {
                             uint32_t o[16];
-                            asm volatile(
-                                "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-                                : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3]), "=r"(o[4]), "=r"(o[5]), "=r"(o[6]), "=r"(o[7]),
-                                  "=r"(o[8]), "=r"(o[9]), "=r"(o[10]), "=r"(o[11]), "=r"(o[12]), "=r"(o[13]), "=r"(o[14]), "=r"(o[15])
-                                : "r"(t_o + (uint32_t)c * 16u) : "memory");
+                            tmem_ld16(t_o + (uint32_t)c * 16u, o);
                             tmem_wait_ld();
 #pragma unroll
                             for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
-                            asm volatile(
-                                "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
-                                ::"r"(t_o + (uint32_t)c * 16u), "r"(o[0]), "r"(o[1]), "r"(o[2]), "r"(o[3]), "r"(o[4]), "r"(o[5]), "r"(o[6]), "r"(o[7]),
-                                  "r"(o[8]), "r"(o[9]), "r"(o[10]), "r"(o[11]), "r"(o[12]), "r"(o[13]), "r"(o[14]), "r"(o[15]) : "memory");
+                            tmem_st16(t_o + (uint32_t)c * 16u, o);
                         }
                     }
                 }
                 const float ref = m == -INFINITY ? 0.f : m;
-                float sum[2] = {0.f, 0.f};
+                const uint64_t sc2 = pair(a.sc, a.sc), ref2 = pair(-ref, -ref);
+                uint64_t sum[2] = {0, 0};
+                auto weights = [&](auto polynomial) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    uint32_t p[32];
+                    for (int c = 0; c < 4; ++c) {
+                        uint32_t p[16];
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) {
-                        const float x = attn_exp2(fmaf(__uint_as_float(s[2 * h + e / 16][(2 * e) & 31]), a.sc, -ref));
-                        const float y = attn_exp2(fmaf(__uint_as_float(s[2 * h + e / 16][(2 * e + 1) & 31]), a.sc, -ref));
-                        sum[e & 1] += x + y;
-                        p[e] = pack2<T>(x, y);
+                        for (int e = 0; e < 16; ++e) {
+                            const uint64_t x2 = fma2(pair(__uint_as_float(s[c][2 * e]), __uint_as_float(s[c][2 * e + 1])), sc2, ref2);
+                            uint64_t w2;
+                            float x, y;
+                            if (decltype(polynomial)::value && e % AT_POLY == AT_POLY - 1) {
+                                w2 = exp2_poly(x2);
+                                halves(w2, x, y);
+                            } else {
+                                halves(x2, x, y);
+                                x = attn_exp2(x); y = attn_exp2(y);
+                                w2 = pair(x, y);
+                            }
+                            sum[e & 1] = add2(sum[e & 1], w2);
+                            p[e] = pack2<T>(x, y);
+                        }
+                        tmem_st16(t_s + (uint32_t)c * 16u, p);
                     }
-                    tmem_st32(t_s + (uint32_t)h * 32u, p);
-                }
-                l += sum[0] + sum[1];
+                };
+                if (all) weights(std::true_type{});
+                else weights(std::false_type{});     // (hidden keys' weights have to be 0)
+                float sums[4];
+                halves(sum[0], sums[0], sums[1]);
+                halves(sum[1], sums[2], sums[3]);
+                l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
                 tmem_wait_st();
                 tmem_before();
                 __syncwarp();
@@ -368,11 +443,7 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
 #pragma unroll 1
             for (int d = 0; d < a.D; d += 16) {
                 uint32_t o[16];
-                asm volatile(
-                    "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-                    : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3]), "=r"(o[4]), "=r"(o[5]), "=r"(o[6]), "=r"(o[7]),
-                      "=r"(o[8]), "=r"(o[9]), "=r"(o[10]), "=r"(o[11]), "=r"(o[12]), "=r"(o[13]), "=r"(o[14]), "=r"(o[15])
-                    : "r"(t_o + (uint32_t)d) : "memory");
+                tmem_ld16(t_o + (uint32_t)d, o);
                 tmem_wait_ld();
                 if (row.token < 0) continue;
 #pragma unroll
