@@ -38,16 +38,36 @@ __host__ __device__ constexpr uint32_t at_part(int dp) { return (uint32_t)(dp / 
 __host__ __device__ constexpr uint32_t at_smem(int dp) { return (2 + 2 * (uint32_t)at_stages(dp)) * at_part(dp) + 1024; }
 static_assert(at_smem(64) >= TC_PAIR_MIN_SMEM, "one block an SM: a block holds all tensor memory");
 
-// D (tensor memory) (+)= A B: A from shared memory, or the 16-bit values of tensor memory from column `a` on
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+// N steps of 16 along the reduction: D (tensor memory) (+)= A B, A from shared memory, or the 16-bit values of tensor memory from
+// column `a` on. The whole warp calls with equal arguments, one elected lane issues: from a branch of a single lane the operands
+// had to be made uniform one by one, 120 cycles a product instead of the 64 that it takes.
+#define AT_MMA_BEGIN "{\n\t.reg .pred pe, pa, pt;\n\t.reg .b64 x, y;\n\t.reg .b32 z;\n\telect.sync _|pe, 0xffffffff;\n\tsetp.ne.b32 pa, %4, 0;\n\tsetp.eq.b32 pt, 0, 0;\n\t"
+#define AT_MMA_SS(X, Y, P) "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], " X ", " Y ", %3, " P ";\n\t"
+#define AT_MMA_TS(X, Y, P) "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [" X "], " Y ", %3, " P ";\n\t"
+__device__ __forceinline__ void mma_ss1(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+    asm volatile(AT_MMA_BEGIN AT_MMA_SS("%1", "%2", "pa") "}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void mma_ss4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)     // 32 bytes a step
+{
+    asm volatile(AT_MMA_BEGIN AT_MMA_SS("%1", "%2", "pa")
+                 "add.s64 x, %1, 2;\n\tadd.s64 y, %2, 2;\n\t" AT_MMA_SS("x", "y", "pt")
+                 "add.s64 x, %1, 4;\n\tadd.s64 y, %2, 4;\n\t" AT_MMA_SS("x", "y", "pt")
+                 "add.s64 x, %1, 6;\n\tadd.s64 y, %2, 6;\n\t" AT_MMA_SS("x", "y", "pt") "}"
                  ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
 }
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+__device__ __forceinline__ void mma_ts4(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)     // 8 columns, 16 rows of 128 bytes a step
 {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+    asm volatile(AT_MMA_BEGIN AT_MMA_TS("%1", "%2", "pa")
+                 "add.s32 z, %1, 8;\n\tadd.s64 y, %2, 128;\n\t" AT_MMA_TS("z", "y", "pt")
+                 "add.s32 z, %1, 16;\n\tadd.s64 y, %2, 256;\n\t" AT_MMA_TS("z", "y", "pt")
+                 "add.s32 z, %1, 24;\n\tadd.s64 y, %2, 384;\n\t" AT_MMA_TS("z", "y", "pt") "}"
                  ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void commit_one(uint32_t bar)     // whole warp calls, one elected lane issues
+{
+    asm volatile("{\n\t.reg .pred pe;\n\telect.sync _|pe, 0xffffffff;\n\t"
+                 "@pe tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16])
 {
@@ -120,6 +140,9 @@ __device__ __forceinline__ uint64_t exp2_poly(uint64_t x2)
     return mul2(p, pair(__uint_as_float((__float_as_uint(a) << 23) + 0x3f800000u), __uint_as_float((__float_as_uint(b) << 23) + 0x3f800000u)));
 }
 
+// bits 0 .. n - 1
+__device__ __forceinline__ uint32_t bits_below(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
+
 // instruction descriptor: D = f32, A and B of one 16-bit type (0 = f16, 1 = bf16), A K-major, M = 128
 __device__ __forceinline__ uint32_t at_idesc(int n, int fmt, int b_mn)
 {
@@ -152,11 +175,12 @@ struct AtSegments {
     __device__ __forceinline__ bool two(const AttnArgs &a) const { return cur.q.n - cur.rt * a.tpt > a.tpt / 2; }
 };
 
-template <typename T, int DP>
+// NK: head size in steps of 16 (the copies bring zeros past it)
+template <typename T, int NK>
 __global__ void __launch_bounds__(AT_THREADS, 1)
 ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const AttnArgs a)
 {
-    constexpr int ST = at_stages(DP);
+    constexpr int DP = NK > 4 ? 128 : 64, ST = at_stages(DP);
     constexpr uint32_t PART = at_part(DP);
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
@@ -261,53 +285,64 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
             }
         }
         } else if (warp == AT_MMA_WARP) {
-        if (lane == 0) {
-            const int fmt = std::is_same_v<T, __nv_bfloat16> ? 1 : 0, nk = (a.D + 15) / 16;
-            const uint32_t id_s = at_idesc(AT_BN, fmt, 0), id_o = at_idesc(nk * 16, fmt, 1);
-            int segs[2] = {0, 0}, steps[2] = {0, 0}, nkey = 0, nval = 0;
-            auto scores = [&](int i, int st) {            // S_i = Q_i K^T
-                const uint64_t q0 = make_desc(s_q + (uint32_t)i * PART, 16, 1024, AT_SWZ), k0 = make_desc(s_k + (uint32_t)st * PART, 16, 1024, AT_SWZ);
-                for (int k = 0; k < nk; ++k) {
-                    const uint64_t o = (uint64_t)((k >> 2) * (int)(AT_PANEL >> 4) + (k & 3) * 2);
-                    mma_ss(tmem + (uint32_t)i * 128u, q0 + o, k0 + o, id_s, k > 0);
-                }
-                mma_commit(smem_u32(&bars.s_full[i]));
-            };
-            for (; ok && sg.get(); sg.done(a)) {
-                const int nt = sg.two(a) ? 2 : 1;
-                ok = mbar_wait(smem_u32(&bars.k_full[nkey % ST]), (uint32_t)(nkey / ST) & 1u, &abort_flag);
-                for (int i = 0; ok && i < nt; ++i) {
-                    ok = mbar_wait(smem_u32(&bars.q_full[i]), (uint32_t)segs[i]++ & 1u, &abort_flag);
+        constexpr uint32_t fmt = std::is_same_v<T, __nv_bfloat16> ? 1 : 0;
+        const uint32_t id_s = at_idesc(AT_BN, fmt, 0), id_o = at_idesc(NK * 16, fmt, 1);
+        const uint64_t q0 = make_desc(s_q, 16, 1024, AT_SWZ), k0 = make_desc(s_k, 16, 1024, AT_SWZ), v0 = make_desc(s_v, AT_PANEL, 1024, AT_SWZ);
+        uint32_t q_phase[2] = {0, 0}, p_phase[2] = {0, 0}, k_phase = 0, v_phase = 0;
+        int ks = 0, vs = 0;                                  // stages of the next keys and values
+        auto scores = [&](int i) {                            // S_i = Q_i K^T
+            const uint64_t q = q0 + (uint64_t)((uint32_t)i * (PART >> 4)), k = k0 + (uint64_t)((uint32_t)ks * (PART >> 4));
+            const uint32_t d = tmem + (uint32_t)i * 128u;
+            mma_ss4(d, q, k, id_s, 0);
+            if constexpr (NK == 8) mma_ss4(d, q + (AT_PANEL >> 4), k + (AT_PANEL >> 4), id_s, 1);
+            else {
+#pragma unroll
+                for (int n = 4; n < NK; ++n) mma_ss1(d, q + (AT_PANEL >> 4) + (uint64_t)((n - 4) * 2), k + (AT_PANEL >> 4) + (uint64_t)((n - 4) * 2), id_s, 1);
+            }
+            commit_one(smem_u32(&bars.s_full[i]));
+        };
+        auto wait = [&](uint64_t &bar, uint32_t phase) { ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar), phase, &abort_flag)); };
+        auto next_keys = [&] {
+            commit_one(smem_u32(&bars.k_empty[ks]));
+            if (++ks == ST) { ks = 0; k_phase ^= 1u; }
+        };
+        for (; ok && sg.get(); sg.done(a)) {
+            const int nt = sg.two(a) ? 2 : 1;
+            wait(bars.k_full[ks], k_phase);
+            for (int i = 0; ok && i < nt; ++i) {
+                wait(bars.q_full[i], q_phase[i]);
+                if (!ok) break;
+                q_phase[i] ^= 1u;
+                tmem_after();
+                scores(i);
+            }
+            if (!ok) break;
+            next_keys();
+            for (int j = 0; ok && j < sg.n; ++j) {
+                const bool more = j + 1 < sg.n;
+                wait(bars.v_full[vs], v_phase);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    if (!ok || i >= nt) break;
+                    wait(bars.p_full[i], p_phase[i]);
                     if (!ok) break;
+                    p_phase[i] ^= 1u;
                     tmem_after();
-                    scores(i, nkey % ST);
+                    const uint64_t v = v0 + (uint64_t)((uint32_t)vs * (PART >> 4));
+                    const uint32_t d = tmem + 256u + (uint32_t)i * 128u, p = tmem + (uint32_t)i * 128u;
+                    mma_ts4(d, p, v, id_o, j > 0);
+                    mma_ts4(d, p + 32u, v + 512, id_o, 1);
+                    if (!more) commit_one(smem_u32(&bars.o_full[i]));
+                    else {
+                        if (i == 0) wait(bars.k_full[ks], k_phase);
+                        if (!ok) break;
+                        scores(i);
+                    }
                 }
                 if (!ok) break;
-                mma_commit(smem_u32(&bars.k_empty[nkey % ST]));
-                ++nkey;
-                for (int j = 0; ok && j < sg.n; ++j) {
-                    const bool more = j + 1 < sg.n;
-                    ok = mbar_wait(smem_u32(&bars.v_full[nval % ST]), (uint32_t)(nval / ST) & 1u, &abort_flag);
-                    for (int i = 0; ok && i < nt; ++i) {
-                        ok = mbar_wait(smem_u32(&bars.p_full[i]), (uint32_t)steps[i]++ & 1u, &abort_flag);
-                        if (!ok) break;
-                        tmem_after();
-                        const uint64_t v0 = make_desc(s_v + (uint32_t)(nval % ST) * PART, AT_PANEL, 1024, AT_SWZ);
-#pragma unroll
-                        for (int k = 0; k < AT_BN / 16; ++k)
-                            mma_ts(tmem + 256u + (uint32_t)i * 128u, tmem + (uint32_t)i * 128u + (uint32_t)k * 8u, v0 + (uint64_t)(k * 128), id_o, j > 0 || k > 0);
-                        if (!more) mma_commit(smem_u32(&bars.o_full[i]));
-                        else {
-                            if (i == 0) ok = mbar_wait(smem_u32(&bars.k_full[nkey % ST]), (uint32_t)(nkey / ST) & 1u, &abort_flag);
-                            if (!ok) break;
-                            scores(i, nkey % ST);
-                        }
-                    }
-                    if (!ok) break;
-                    mma_commit(smem_u32(&bars.v_empty[nval % ST]));
-                    ++nval;
-                    if (more) { mma_commit(smem_u32(&bars.k_empty[nkey % ST])); ++nkey; }
-                }
+                commit_one(smem_u32(&bars.v_empty[vs]));
+                if (++vs == ST) { vs = 0; v_phase ^= 1u; }
+                if (more) next_keys();
             }
         }
         __syncwarp();
@@ -361,11 +396,15 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                 tmem_wait_ld();
                 const bool all = j0 + AT_BN <= all_hi && j0 >= a.kv0 && (j0 >= all_lo || j0 + AT_BN <= a.sinks);
                 if (!all) {
+                    // keys first .. last - 1 of the tile (the first `early` ones too) are seen: a bit each, 32 at a time
+                    const int first = imax(row.lo, a.kv0) - j0, last = row.hi - j0, early = imin(a.sinks, row.hi) - j0, least = a.kv0 - j0;
 #pragma unroll
-                    for (int c = 0; c < 4; ++c)
+                    for (int c = 0; c < 4; ++c) {
+                        const uint32_t seen = (bits_below(last - c * 32) & ~bits_below(first - c * 32)) | (bits_below(early - c * 32) & ~bits_below(least - c * 32));
 #pragma unroll
                         for (int e = 0; e < 32; ++e)
-                            if (!attn_sees(a, row, j0 + c * 32 + e)) s[c][e] = 0xff800000u;
+                            if (!(seen & (1u << e))) s[c][e] = 0xff800000u;
+                    }
                 }
                 float mx[4];
 #pragma unroll
@@ -382,7 +421,7 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                     l *= f;
                     if (j > 0) {
 #pragma unroll 1
-                        for (int c = 0; c < (a.D + 15) / 16; ++c) {
+                        for (int c = 0; c < NK; ++c) {
                             uint32_t o[16];
                             tmem_ld16(t_o + (uint32_t)c * 16u, o);
                             tmem_wait_ld();
@@ -477,8 +516,8 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                 mbar_wait(smem_u32(&bars.patch), (uint32_t)(f & 1), &gave_up, 1000000);
             }
         }
-        if (warp == AT_MMA_WARP && lane == 0) {
-            mma_commit(smem_u32(&bars.drain));
+        if (warp == AT_MMA_WARP) {
+            commit_one(smem_u32(&bars.drain));
             mbar_wait(smem_u32(&bars.drain), 0, &gave_up, 1000000);
         }
         __syncthreads();
@@ -525,10 +564,17 @@ int attn_encode_cache(CUtensorMap *tm, const AttnArgs &a, const void *base, int 
 
 namespace {
 
-template <typename T, int DP> int launch_tc_t(const CUtensorMap &k, const CUtensorMap &v, const AttnArgs &a, int grid, void *stream)
+template <typename T> int launch_tc_t(const CUtensorMap &k, const CUtensorMap &v, const AttnArgs &a, int grid, void *stream)
 {
-    static std::atomic<bool> done[64] = {};
-    return attn_launch(ubp_attention_tc_kernel<T, DP>, done, dim3((unsigned)grid), AT_THREADS, at_smem(DP), stream, k, v, a);
+    static std::atomic<bool> done[5][64] = {};
+    const dim3 g((unsigned)grid);
+    switch (a.D <= 64 ? 4 : (a.D + 15) / 16) {
+        case 4: return attn_launch(ubp_attention_tc_kernel<T, 4>, done[0], g, AT_THREADS, at_smem(64), stream, k, v, a);
+        case 5: return attn_launch(ubp_attention_tc_kernel<T, 5>, done[1], g, AT_THREADS, at_smem(128), stream, k, v, a);
+        case 6: return attn_launch(ubp_attention_tc_kernel<T, 6>, done[2], g, AT_THREADS, at_smem(128), stream, k, v, a);
+        case 7: return attn_launch(ubp_attention_tc_kernel<T, 7>, done[3], g, AT_THREADS, at_smem(128), stream, k, v, a);
+        default: return attn_launch(ubp_attention_tc_kernel<T, 8>, done[4], g, AT_THREADS, at_smem(128), stream, k, v, a);
+    }
 }
 
 }  // namespace
@@ -538,8 +584,7 @@ int launch_attn_tc(const AttnArgs &a, int dtype, int grid, void *stream)
     CUtensorMap k, v;
     if (const int rc = attn_encode_cache(&k, a, a.k, dtype, AT_BN)) return rc;
     if (const int rc = attn_encode_cache(&v, a, a.v, dtype, AT_BN)) return rc;
-    if (dtype == UBP_BF16) return a.D <= 64 ? launch_tc_t<__nv_bfloat16, 64>(k, v, a, grid, stream) : launch_tc_t<__nv_bfloat16, 128>(k, v, a, grid, stream);
-    return a.D <= 64 ? launch_tc_t<__half, 64>(k, v, a, grid, stream) : launch_tc_t<__half, 128>(k, v, a, grid, stream);
+    return dtype == UBP_BF16 ? launch_tc_t<__nv_bfloat16>(k, v, a, grid, stream) : launch_tc_t<__half>(k, v, a, grid, stream);
 }
 
 }  // namespace ubp
