@@ -35,8 +35,9 @@ constexpr uint32_t AT_PANEL = 128 * 128;                       // 128 rows of 64
 constexpr uint32_t AT_SWZ = 2;                                 // 128-byte swizzle
 __host__ __device__ constexpr int at_stages(int dp) { return dp == 128 ? 2 : 4; }
 __host__ __device__ constexpr uint32_t at_part(int dp) { return (uint32_t)(dp / 64) * AT_PANEL; }
-__host__ __device__ constexpr uint32_t at_smem(int dp) { return (2 + 2 * (uint32_t)at_stages(dp)) * at_part(dp) + 1024; }
-static_assert(at_smem(64) >= TC_PAIR_MIN_SMEM, "one block an SM: a block holds all tensor memory");
+constexpr uint32_t AT_TURN = 32 * 128;                         // a softmax warp's: 128 bytes of each of its rows
+__host__ __device__ constexpr uint32_t at_smem(int dp) { return (2 + 2 * (uint32_t)at_stages(dp)) * at_part(dp) + 8 * AT_TURN + 1024; }
+static_assert(at_smem(64) >= TC_PAIR_MIN_SMEM && at_smem(128) <= 226 * 1024, "one block an SM: a block holds all tensor memory");
 
 // N steps of 16 along the reduction: D (tensor memory) (+)= A B, A from shared memory, or the 16-bit values of tensor memory from
 // column `a` on. The whole warp calls with equal arguments, one elected lane issues: from a branch of a single lane the operands
@@ -68,6 +69,11 @@ __device__ __forceinline__ void commit_one(uint32_t bar)     // whole warp calls
 {
     asm volatile("{\n\t.reg .pred pe;\n\telect.sync _|pe, 0xffffffff;\n\t"
                  "@pe tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&r)[8])
+{
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16])
 {
@@ -150,7 +156,7 @@ __device__ __forceinline__ uint32_t at_idesc(int n, int fmt, int b_mn)
 }
 
 struct AtBars {
-    uint64_t q_full[2], s_full[2], p_full[2], o_full[2];
+    uint64_t q_full[2], s_full[2], p_half[2], p_full[2], o_full[2];
     uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], patch, drain;
 };
 
@@ -198,6 +204,7 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&bars.q_full[i]), 4);
             mbar_init(smem_u32(&bars.s_full[i]), 1);
+            mbar_init(smem_u32(&bars.p_half[i]), 4);
             mbar_init(smem_u32(&bars.p_full[i]), 4);
             mbar_init(smem_u32(&bars.o_full[i]), 1);
         }
@@ -324,13 +331,16 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     if (!ok || i >= nt) break;
-                    wait(bars.p_full[i], p_phase[i]);
+                    wait(bars.p_half[i], p_phase[i]);
                     if (!ok) break;
-                    p_phase[i] ^= 1u;
                     tmem_after();
                     const uint64_t v = v0 + (uint64_t)((uint32_t)vs * (PART >> 4));
                     const uint32_t d = tmem + 256u + (uint32_t)i * 128u, p = tmem + (uint32_t)i * 128u;
                     mma_ts4(d, p, v, id_o, j > 0);
+                    wait(bars.p_full[i], p_phase[i]);
+                    if (!ok) break;
+                    p_phase[i] ^= 1u;
+                    tmem_after();
                     mma_ts4(d, p + 32u, v + 512, id_o, 1);
                     if (!more) commit_one(smem_u32(&bars.o_full[i]));
                     else {
@@ -350,45 +360,51 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
         const int tile = warp >> 2, r = (warp & 3) * 32 + lane;
-        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16, t_s = tmem + lanes + (uint32_t)tile * 128u, t_o = t_s + 256u;
-        uint8_t *const qs = smem + (uint32_t)tile * PART;
-        int steps = 0, segs = 0;
-        for (; ok && sg.get(); sg.done(a)) {
-            if (tile == 1 && !sg.two(a)) continue;
-            const AttnRow row = attn_row(a, sg.cur.q, sg.cur.hu, sg.cur.rt, tile * AT_TILE + r);
-            {
-                const T *p = static_cast<const T *>(a.q) + (row.token < 0 ? 0 : row.token * a.q_ts + row.head * a.q_hs);
-                const bool whole = (reinterpret_cast<uintptr_t>(p) & 15) == 0;
-#pragma unroll 4
-                for (int c = 0; c < DP / 8; ++c) {
-                    uint4 v = make_uint4(0, 0, 0, 0);
-                    if (row.token >= 0 && c * 8 < a.D) {
-                        if (whole) v = *reinterpret_cast<const uint4 *>(p + c * 8);
-                        else {
-                            const uint16_t *h = reinterpret_cast<const uint16_t *>(p + c * 8);
-                            v = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16);
-                        }
-                    }
-                    *reinterpret_cast<uint4 *>(qs + (uint32_t)(c / 8) * AT_PANEL + (uint32_t)r * 128u + (uint32_t)(((c & 7) ^ (r & 7)) << 4)) = v;
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                tmem_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&bars.q_full[tile]));
-            }
-            // keys that all (existing) rows of the warp see need no comparison
-            int all_hi = row.token >= 0 ? row.hi : INT_MAX, all_lo = row.token >= 0 ? row.lo : 0;
+        const uint32_t t_s = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)tile * 128u, t_o = t_s + 256u;
+        uint8_t *const qs = smem + (uint32_t)tile * PART, *const turn = smem + (2 + 2 * ST) * PART + (uint32_t)warp * AT_TURN;
+        uint32_t s_phase = 0, o_phase = 0;
+        AttnRow row;
+        int all_hi, all_lo;
+        // the next item that has rows in this tile, and its queries on their way to the first product
+        auto begin = [&]() {
+            while (sg.get() && tile == 1 && !sg.two(a)) sg.done(a);
+            if (sg.left <= 0) return false;
+            row = attn_row(a, sg.cur.q, sg.cur.hu, sg.cur.rt, tile * AT_TILE + r);
+            const T *p = static_cast<const T *>(a.q) + (row.token < 0 ? 0 : row.token * a.q_ts + row.head * a.q_hs);
+            uint4 v[2 * NK];
+            if (row.token < 0 || (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
 #pragma unroll
-            for (int o = 16; o > 0; o >>= 1) {
-                all_hi = imin(all_hi, __shfl_xor_sync(0xffffffffu, all_hi, o));
-                all_lo = imax(all_lo, __shfl_xor_sync(0xffffffffu, all_lo, o));
+                for (int c = 0; c < 2 * NK; ++c) v[c] = row.token >= 0 && c * 8 < a.D ? *reinterpret_cast<const uint4 *>(p + c * 8) : make_uint4(0, 0, 0, 0);
+            } else {
+#pragma unroll
+                for (int c = 0; c < 2 * NK; ++c) {
+                    const uint16_t *h = reinterpret_cast<const uint16_t *>(p + c * 8);
+                    v[c] = make_uint4(0, 0, 0, 0);
+                    if (c * 8 < a.D) v[c] = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16);
+                }
             }
+#pragma unroll
+            for (int c = 0; c < 2 * NK; ++c)
+                *reinterpret_cast<uint4 *>(qs + (uint32_t)(c / 8) * AT_PANEL + (uint32_t)r * 128u + (uint32_t)(((c & 7) ^ (r & 7)) << 4)) = v[c];
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            tmem_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&bars.q_full[tile]));
+            // keys that all (existing) rows of the warp see need no comparison
+            all_hi = row.token >= 0 ? row.hi : INT_MAX;
+            all_lo = row.token >= 0 ? row.lo : 0;
+            all_hi = __reduce_min_sync(0xffffffffu, all_hi);
+            all_lo = __reduce_max_sync(0xffffffffu, all_lo);
+            return true;
+        };
+        bool live = begin();
+        while (live) {
             float m = -INFINITY, l = 0.f;
             for (int j = 0; j < sg.n; ++j) {
                 const int j0 = attn_tile_at(sg.cur.t, sg.tile0 + j) * AT_BN;
-                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars.s_full[tile]), (uint32_t)steps & 1u, &abort_flag));
+                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars.s_full[tile]), s_phase, &abort_flag));
                 if (!ok) break;
-                ++steps;
+                s_phase ^= 1u;
                 tmem_after();
                 uint32_t s[4][32];
 #pragma unroll
@@ -455,52 +471,99 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                             p[e] = pack2<T>(x, y);
                         }
                         tmem_st16(t_s + (uint32_t)c * 16u, p);
+                        if (c == 1) {                   // the product with the first 64 values may begin
+                            tmem_wait_st();
+                            tmem_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive(smem_u32(&bars.p_half[tile]));
+                        }
                     }
                 };
                 if (all) weights(std::true_type{});
                 else weights(std::false_type{});     // (hidden keys' weights have to be 0)
-                float sums[4];
-                halves(sum[0], sums[0], sums[1]);
-                halves(sum[1], sums[2], sums[3]);
-                l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
                 tmem_wait_st();
                 tmem_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&bars.p_full[tile]));
+                float sums[4];
+                halves(sum[0], sums[0], sums[1]);
+                halves(sum[1], sums[2], sums[3]);
+                l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
             }
             if (!ok) break;
-            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars.o_full[tile]), (uint32_t)segs & 1u, &abort_flag));
-            if (!ok) break;
-            ++segs;
-            tmem_after();
+            // the item's outcome is on its way to tensor memory; the next item's queries go first
+            const int token = row.token, head = row.head, c = (int)blockIdx.x;
             const bool complete = sg.n == sg.cur.t.nt && !a.common;
-            const int c = (int)blockIdx.x;
-            int64_t at = (2 * (int64_t)c + (sg.left < count ? 1 : 0)) * a.rows;
-            if (a.common) at = ((int64_t)sg.cur.hu * attn_row_blocks(a, sg.cur.q) + sg.cur.rt + c) * a.rows;
-            at += tile * AT_TILE + r;
-            if (!complete && row.token >= 0) a.ml[at] = make_float2(m, l);
+            int64_t slot = 2 * (int64_t)c + (sg.left < count ? 1 : 0);
+            if (a.common) slot = (int64_t)sg.cur.hu * attn_row_blocks(a, sg.cur.q) + sg.cur.rt + c;
+            if (tile == 0 && r == 0 && !a.common && sg.left == sg.n) attn_describe(a, sg.cur, deal, c, count - sg.n, sg.tile0, sg.n);
+            sg.done(a);
+            live = begin();
+            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars.o_full[tile]), o_phase, &abort_flag));
+            if (!ok) break;
+            o_phase ^= 1u;
+            tmem_after();
+            const int64_t at = slot * a.rows + tile * AT_TILE + r;
+            if (complete && a.pml) {
 #pragma unroll 1
-            for (int d = 0; d < a.D; d += 16) {
-                uint32_t o[16];
-                tmem_ld16(t_o + (uint32_t)d, o);
-                tmem_wait_ld();
-                if (row.token < 0) continue;
+                for (int d = 0; d < a.D; d += 8) {
+                    uint32_t o[8];
+                    tmem_ld8(t_o + (uint32_t)d, o);
+                    tmem_wait_ld();
+                    float v[8], M = m, L = l;
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if (d + h * 8 >= a.D) break;
-                    float v[8];
+                    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(o[e]);
+                    if (token >= 0) attn_finish<T>(a, token, head, d, M, L, v);
+                }
+            } else {
+                // 128 bytes of each row at a time, turned in shared memory so that eight lanes store a row's (a thread a row: 32 rows
+                // a store, 5300 cycles an item)
+                if (!complete && token >= 0) a.ml[at] = make_float2(m, l);
+                const float scale = complete ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+                const int per = complete ? 64 : 32;
+                uint8_t *const dst = complete ? reinterpret_cast<uint8_t *>(static_cast<T *>(a.out) + (token < 0 ? 0 : token * a.o_ts + head * a.o_hs))
+                                              : reinterpret_cast<uint8_t *>(a.po + at * a.D);
+                const bool apart = (reinterpret_cast<uintptr_t>(dst) & 15) != 0;        // (any alignment of the output)
+#pragma unroll 1
+                for (int d = 0; d < a.D; d += per) {
+#pragma unroll 1
+                    for (int h = 0; h < per && d + h < a.D; h += 16) {
+                        uint32_t o[16];
+                        tmem_ld16(t_o + (uint32_t)(d + h), o);
+                        tmem_wait_ld();
+                        if (complete) {
+                            uint32_t w[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(o[h * 8 + e]);
-                    if (complete) attn_finish<T>(a, row.token, row.head, d + h * 8, m, l, v);
-                    else {
-                        float *p = a.po + at * a.D + d + h * 8;
-                        *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
-                        *reinterpret_cast<float4 *>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+                            for (int e = 0; e < 8; ++e) w[e] = pack2<T>(__uint_as_float(o[2 * e]) * scale, __uint_as_float(o[2 * e + 1]) * scale);
+#pragma unroll
+                            for (int e = 0; e < 2; ++e)
+                                *reinterpret_cast<uint4 *>(turn + lane * 128 + (((h / 8 + e) ^ (lane & 7)) << 4)) = make_uint4(w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]);
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                *reinterpret_cast<uint4 *>(turn + lane * 128 + (((h / 4 + e) ^ (lane & 7)) << 4)) = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                        }
                     }
+                    __syncwarp();
+                    const int ch = lane & 7, col = d + ch * (per / 8);
+#pragma unroll 2
+                    for (int i = 0; i < 8; ++i) {
+                        const int from = i * 4 + (lane >> 3);
+                        const uint4 v = *reinterpret_cast<const uint4 *>(turn + from * 128 + ((ch ^ (from & 7)) << 4));
+                        const uint64_t base = __shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(dst), from);
+                        const bool there = __shfl_sync(0xffffffffu, token, from) >= 0, odd = __shfl_sync(0xffffffffu, (int)apart, from) != 0;
+                        if (!there || col >= a.D) continue;
+                        uint8_t *const to = reinterpret_cast<uint8_t *>(base) + d * 128 / per + ch * 16;
+                        if (!odd) *reinterpret_cast<uint4 *>(to) = v;
+                        else {
+                            uint16_t *const h = reinterpret_cast<uint16_t *>(to);
+                            h[0] = (uint16_t)v.x; h[1] = (uint16_t)(v.x >> 16); h[2] = (uint16_t)v.y; h[3] = (uint16_t)(v.y >> 16);
+                            h[4] = (uint16_t)v.z; h[5] = (uint16_t)(v.z >> 16); h[6] = (uint16_t)v.w; h[7] = (uint16_t)(v.w >> 16);
+                        }
+                    }
+                    __syncwarp();
                 }
             }
-            if (tile == 0 && r == 0 && !a.common && sg.left == sg.n)
-                attn_describe(a, sg.cur, deal, c, count - sg.n, sg.tile0, sg.n);
         }
     }
     if (!ok && lane == 0) atomicExch(a.status, 1);
