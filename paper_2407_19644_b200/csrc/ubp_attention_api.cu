@@ -95,7 +95,10 @@ int attn_plan(const ubp_cache_t *c, int64_t T, int q_heads, float scale, int win
     // more blocks than steps would have nothing to do
     const int64_t seen = window > 0 ? std::min<int64_t>(a.cap, (int64_t)window + sinks + a.tpt + 2 * ATTN_BN) : a.cap;
     const int64_t items = (a.T / a.tpt + (int64_t)a.B) * a.HU;
-    p.own_grid = (int)std::min<int64_t>(sms, items * ((seen + ATTN_BN - 1) / ATTN_BN + 1));
+    const int64_t tiles = (seen + ATTN_BN - 1) / ATTN_BN + 1;
+    // (the kernels count the steps of a unit head, and a block's, in 32 bits)
+    if (items / a.HU > INT32_MAX / tiles || (a.cap / ATTN_BN + 2) > INT32_MAX / a.HU || items * tiles / sms >= INT32_MAX) return UBP_E_UNSUPPORTED;
+    p.own_grid = (int)std::min<int64_t>(sms, items * tiles);
     p.own_space = attn_space(p.own_grid, 2 * (int64_t)p.own_grid, a.rows, a.D);
     p.bytes = p.own_space.total;
     if (prefix > 0) {
@@ -108,7 +111,7 @@ int attn_plan(const ubp_cache_t *c, int64_t T, int q_heads, float scale, int win
         const int64_t units = (int64_t)((b.T + b.tpt - 1) / b.tpt) * b.HU;
         const int nt = (int)((prefix + ATTN_BN - 1) / ATTN_BN);
         p.common_grid = (int)std::min<int64_t>(sms, units * nt);
-        if (units + p.common_grid > INT32_MAX) return UBP_E_UNSUPPORTED;
+        if (units + p.common_grid > INT32_MAX || units / b.HU > INT32_MAX / nt || units * nt / sms >= INT32_MAX) return UBP_E_UNSUPPORTED;
         p.common_space = attn_space(0, units + p.common_grid, b.rows, b.D);
         p.row_space = attn_space(0, T, q_heads, b.D);          // a row's sums over the prefix
         p.bytes += p.common_space.total + p.row_space.total;

@@ -62,7 +62,7 @@ __device__ __forceinline__ uint32_t load_pair(const uint16_t *p) { return (uint3
 // Everything is the same in all lanes; lane 0 issues.
 template <int DP> struct FewCopies {
     AttnCursor c;
-    int64_t left;            // steps that are not issued yet
+    int left;                // steps that are not issued yet
     int page[2], j0, kvh;
     const int32_t *row;
 
@@ -112,7 +112,6 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t *const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     __shared__ __align__(8) uint64_t bar_full[FEW_WARPS][ST];
-    __shared__ AttnPlace place;
     __shared__ int2 rows[FEW_ROWS];         // token and head of the item's rows
     __shared__ int abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, tq = lane & 3;
@@ -129,10 +128,12 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     __syncthreads();
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
-    int64_t first, count;
-    AttnDeal deal(0, 0);
+    int64_t first;
+    int count;
+    AttnDeal deal;
     AttnCursor cur;
-    if (!attn_locate(a, place, deal, first, count, cur)) {
+    static_assert(sizeof(AttnPlace<FEW_WARPS * 32>) <= FEW_WARPS * 8 * 64 * 4, "lies where the warps' sums meet");
+    if (!attn_locate<FEW_WARPS * 32>(a, *reinterpret_cast<AttnPlace<FEW_WARPS * 32> *>(meet), deal, first, count, cur)) {
         if (threadIdx.x == 0 && !a.common) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
         return;
     }
@@ -155,7 +156,7 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     int tile0 = cur.tile, st = 0, all_lo = 0, all_hi = 0;
     uint32_t phase = 0;
     bool fresh = true, ok = true;
-    for (int64_t step = 0; step < count; ++step) {
+    for (int step = 0; step < count; ++step) {
         __syncwarp();                       // (all lanes have read the stage that is copied to now)
         const int nx = st == 0 ? ST - 1 : st - 1;
         copies.issue(a, &tmK, &tmV, ring + (uint32_t)nx * 2 * PART, smem_u32(&bar_full[warp][nx]), warp, lane);
@@ -192,7 +193,7 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
         }
-        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar_full[warp][st]), phase, &abort_flag));
+        if (ok) ok = attn_wait(smem_u32(&bar_full[warp][st]), phase, &abort_flag);
         const int j0 = attn_tile_at(cur.t, cur.tile) * FEW_BN + warp * FEW_KEYS;
         const uint32_t base = ring + (uint32_t)st * 2 * PART;
         if (ok && j0 < cur.t.end && j0 + FEW_KEYS > a.kv0 && (j0 + FEW_KEYS > cur.t.w0 || j0 < a.sinks)) {
@@ -314,7 +315,7 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     if (!ok) {                              // copies that are still under way end before the block does (a millisecond at most each)
         int gave_up = 0;
         for (int i = 0; i < ST; ++i)
-            for (uint32_t ph = 0; ph < 2; ++ph) mbar_wait(smem_u32(&bar_full[warp][i]), ph, &gave_up, 1000000);
+            for (uint32_t ph = 0; ph < 2; ++ph) attn_wait(smem_u32(&bar_full[warp][i]), ph, &gave_up, 1);
         if (lane == 0) atomicExch(a.status, 1);
     }
 }

@@ -14,135 +14,115 @@ __device__ __forceinline__ float attn_exp2(float x)
     return y;
 }
 
-struct AttnPlace { int64_t warp[32]; int64_t rem; int b; };
+// Shared memory of attn_locate, for blocks of NT threads.
+template <int NT> struct AttnPlace { int warp[2][32]; int pre[NT + 1]; int b, rt, before, from, to; };
 
-// Steps of sequence b (none where !valid); called by whole warps. A lane counts its own sequence's row blocks while they are few,
-// the warp counts those of long prompts together.
-__device__ __forceinline__ int64_t attn_seq_steps(const AttnArgs &a, int b, bool valid)
+// The block's steps, [first, first + count), and the cursor at the first one. Called by all threads of the block, NT of them (a
+// multiple of 32); false, to all of them, if there is nothing to do. Row blocks (of all sequences, a thread each) are counted and
+// summed in parallel, for one unit head: all of a sequence's have equal steps, so that step x lies in the sequence that x / HU lies in.
+template <int NT>
+__device__ __forceinline__ bool attn_locate(const AttnArgs &a, AttnPlace<NT> &sh, AttnDeal &deal, int64_t &first, int &count, AttnCursor &cur)
 {
-    const int lane = threadIdx.x & 31;
-    int n = 0;
-    AttnSeq q{0, 0, 0};
-    if (valid) { q = attn_seq(a, b); n = attn_row_blocks(a, q); }
-    int64_t c = 0;
-    if (n <= 2)
-        for (int rt = 0; rt < n; ++rt) c += attn_block_tiles(a, q, rt).nt;
-    for (uint32_t big = __ballot_sync(0xffffffffu, n > 2); big; big &= big - 1) {
-        const int src = __ffs(big) - 1;
-        AttnSeq w;
-        w.s = __shfl_sync(0xffffffffu, q.s, src);
-        w.n = __shfl_sync(0xffffffffu, q.n, src);
-        w.len = __shfl_sync(0xffffffffu, q.len, src);
-        const int m = attn_row_blocks(a, w);
-        int64_t s = 0;
-        for (int rt = lane; rt < m; rt += 32) s += attn_block_tiles(a, w, rt).nt;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-        if (lane == src) c = s;
-    }
-    return c * a.HU;
-}
-
-// The cursor at step rem of sequence b; called by whole warps.
-__device__ __forceinline__ void attn_place(const AttnArgs &a, int b, int64_t rem, AttnCursor &cur)
-{
-    const int lane = threadIdx.x & 31;
-    const AttnSeq q = attn_seq(a, b);
-    const int m = attn_row_blocks(a, q);
-    if (m == 1) {
-        const int n = attn_block_tiles(a, q, 0).nt, hu = rem >> 32 ? (int)(rem / n) : (int)((uint32_t)rem / (uint32_t)n);
-        cur.set(a, b, hu, 0, (int)(rem - (int64_t)hu * n));
-        return;
-    }
-    int64_t per = 0;
-    for (int i = lane; i < m; i += 32) per += attn_block_tiles(a, q, i).nt;
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) per += __shfl_xor_sync(0xffffffffu, per, o);
-    const int hu = (int)(rem / per);
-    int rt = 0;
-    rem -= (int64_t)hu * per;
-    for (int i = 0; i < m; i += 32) {
-        const int n = i + lane < m ? attn_block_tiles(a, q, i + lane).nt : 0;
-        int64_t x = n;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
-            if (lane >= o) x += y;
-        }
-        const uint32_t in = __ballot_sync(0xffffffffu, x > rem);
-        if (in) {
-            const int src = __ffs(in) - 1;
-            rem -= __shfl_sync(0xffffffffu, x - n, src);
-            rt = i + src;
-            break;
-        }
-        rem -= __shfl_sync(0xffffffffu, x, 31);
-    }
-    cur.set(a, b, hu, rt, (int)rem);
-}
-
-// The block's steps, [first, first + count), and the cursor at the first one. Called by all threads of the block (a multiple of
-// 32); returns false, to all of them, if there is nothing to do.
-__device__ __forceinline__ bool attn_locate(const AttnArgs &a, AttnPlace &sh, AttnDeal &deal, int64_t &first, int64_t &count, AttnCursor &cur)
-{
-    const int nt = (int)blockDim.x, tid = (int)threadIdx.x, lane = tid & 31, warp = tid >> 5, nw = nt >> 5;
+    constexpr int NW = NT / 32;
+    const int tid = (int)threadIdx.x, lane = tid & 31, warp = tid >> 5, c = (int)blockIdx.x;
     const int nb = a.common ? 1 : a.B;
-    if (nb <= 32) {                     // every warp for itself: no barrier
-        const int64_t mine = attn_seq_steps(a, lane, lane < nb);
-        int64_t x = mine;
+    auto warp_sum = [&](int x) {        // inclusive
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
+            const int y = __shfl_up_sync(0xffffffffu, x, o);
             if (lane >= o) x += y;
         }
-        deal = AttnDeal(__shfl_sync(0xffffffffu, x, 31), (int)gridDim.x);
-        const int c = (int)blockIdx.x;
+        return x;
+    };
+    auto begin = [&](int64_t total) {
+        deal = AttnDeal(total * a.HU, (int)gridDim.x);
         if (c >= deal.grid) return false;
         first = deal.first(c);
         count = deal.count(c);
-        const int b = __ffs(__ballot_sync(0xffffffffu, x > first)) - 1;
-        attn_place(a, b, first - __shfl_sync(0xffffffffu, x - mine, b), cur);
         return true;
-    }
-    int64_t total = 0, mine = 0, before = 0;       // steps of this thread's sequence, and of all sequences before it in the chunk
-    auto scan = [&](int base) {         // -> steps of the chunk of nt sequences from base on
-        const int b = base + tid;
-        mine = attn_seq_steps(a, b, b < nb);
-        int64_t x = mine;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int64_t y = __shfl_up_sync(0xffffffffu, x, o);
-            if (lane >= o) x += y;
-        }
-        __syncthreads();
-        if (lane == 31) sh.warp[warp] = x;
-        __syncthreads();
-        int64_t w = 0, all = 0;
-        for (int i = 0; i < nw; ++i) {
-            const int64_t v = sh.warp[i];
-            if (i < warp) w += v;
-            all += v;
-        }
-        before = w + x - mine;
-        return all;
     };
-    for (int base = 0; base < nb; base += nt) total += scan(base);
-    deal = AttnDeal(total, (int)gridDim.x);
-    const int c = (int)blockIdx.x;
-    if (c >= deal.grid) return false;
-    first = deal.first(c);
-    count = deal.count(c);
-    int64_t at = first;
-    for (int base = 0; base < nb; base += nt) {
-        const int64_t all = nb > nt ? scan(base) : total;
-        if (at < all) {
-            if (at >= before && at < before + mine) { sh.b = base + tid; sh.rem = at - before; }
-            break;
+    if (nb <= 32) {                     // a few sequences of one row block each: every warp for itself, no barrier
+        AttnSeq q{0, 0, 0};
+        if (lane < nb) q = attn_seq(a, lane);
+        const int blocks = attn_row_blocks(a, q);
+        if (!__any_sync(0xffffffffu, blocks > 1)) {
+            const int mine = blocks ? attn_block_tiles(a, q, 0).nt : 0, x = warp_sum(mine);
+            if (!begin(__shfl_sync(0xffffffffu, x, 31))) return false;
+            const int b = __ffs(__ballot_sync(0xffffffffu, (int64_t)x * a.HU > first)) - 1;
+            cur.set(a, b, 0, 0, 0);
+            const uint32_t rem = (uint32_t)(first - (int64_t)__shfl_sync(0xffffffffu, x - mine, b) * a.HU);
+            cur.hu = (int)(rem / (uint32_t)cur.t.nt);
+            cur.tile = (int)(rem - (uint32_t)cur.hu * (uint32_t)cur.t.nt);
+            return true;
         }
-        at -= all;
     }
-    __syncthreads();
-    attn_place(a, sh.b, sh.rem, cur);
+    int turn = 0;
+    auto scan = [&](int v, int &all) {  // -> sum before this thread
+        const int x = warp_sum(v);
+        if (lane == 31) sh.warp[turn][warp] = x;
+        __syncthreads();
+        const int w = lane < NW ? sh.warp[turn][lane] : 0, ws = warp_sum(w);
+        turn ^= 1;
+        all = __shfl_sync(0xffffffffu, ws, 31);
+        return __shfl_sync(0xffffffffu, ws - w, warp) + x - v;
+    };
+    // all row blocks, NT at a time: visit(b, rt, steps before it, its steps) for this thread's; returns all steps
+    auto walk = [&](auto &&visit) {
+        int64_t sum = 0;
+        for (int base = 0; base < nb; base += NT) {
+            const int b = base + tid;
+            AttnSeq q{0, 0, 0};
+            if (b < nb) q = attn_seq(a, b);
+            int blocks;
+            const int at = scan(attn_row_blocks(a, q), blocks);
+            sh.pre[tid] = at;
+            if (tid == 0) sh.pre[NT] = blocks;
+            __syncthreads();
+            for (int i0 = 0; i0 < blocks; i0 += NT) {
+                const int i = i0 + tid;
+                int s = 0, nt = 0, all;
+                if (i < blocks) {
+                    for (int hi = imin(NT, nb - base); hi - s > 1;) {       // last sequence that begins at i or before (of empty ones: the one behind them)
+                        const int m = (s + hi) / 2;
+                        if (sh.pre[m] <= i) s = m;
+                        else hi = m;
+                    }
+                    nt = attn_block_tiles(a, attn_seq(a, base + s), i - sh.pre[s]).nt;
+                }
+                const int before = scan(nt, all);
+                if (nt) visit(base + s, i - sh.pre[s], sum + before, nt);
+                sum += all;
+            }
+            __syncthreads();
+        }
+        return sum;
+    };
+    int kb = -1, krt = 0, kbefore = 0, knt = 0;
+    const int64_t total = walk([&](int b, int rt, int64_t before, int nt) { kb = b; krt = rt; kbefore = (int)before; knt = nt; });
+    if (!begin(total)) return false;
+    const bool once = nb <= NT && sh.pre[NT] <= NT;         // (this thread still has its row block, the only one)
+    auto again = [&](auto &&visit) {
+        if (!once) walk(visit);
+        else if (kb >= 0) visit(kb, krt, (int64_t)kbefore, knt);
+        __syncthreads();
+    };
+    // the sequence of the first step; its steps for one unit head; the row block
+    const int64_t y = first / a.HU;
+    again([&](int b, int, int64_t before, int nt) { if (y >= before && y < before + nt) sh.b = b; });
+    const int b = sh.b;
+    const AttnSeq q = attn_seq(a, b);
+    const int last = attn_row_blocks(a, q) - 1;
+    again([&](int b_, int rt, int64_t before, int nt) {
+        if (b_ == b && rt == 0) sh.from = (int)before;
+        if (b_ == b && rt == last) sh.to = (int)before + nt;
+    });
+    const int from = sh.from;
+    const int64_t rem = first - (int64_t)from * a.HU;
+    const int hu = (int)(rem / (sh.to - from));
+    const int64_t z = from + (rem - (int64_t)hu * (sh.to - from));
+    again([&](int b_, int rt, int64_t before, int nt) { if (b_ == b && z >= before && z < before + nt) { sh.rt = rt; sh.before = (int)before; } });
+    cur.set(a, b, hu, sh.rt, (int)z - sh.before);
+    __syncthreads();                    // (sh may be something else from here on)
     return true;
 }
 

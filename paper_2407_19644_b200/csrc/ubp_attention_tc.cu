@@ -4,10 +4,11 @@
 //   S = Q K^T (128 rows x 128 keys, fp32 in tensor memory), P = 2^(S scale log2e - m) in 16 bits, O = O + P V (fp32 in tensor memory)
 //
 // A block owns 256 rows (tokens times heads of a group) in two tiles of 128 that share the staged keys and values: while one
-// tile's scores go through the softmax, the tensor cores work on the other's products. Eight warps hold the softmax, a thread a
-// row: scores come from tensor memory, weights go back over them and are the second product's A operand from there; nothing passes
-// through shared memory. One warp issues the products, one the copies: a page of the cache is a TMA box (64 values x tokens), in
-// the 128-byte swizzle, so that K is the K-major and V the MN-major operand as they lie in the cache.
+// tile's scores go through the softmax, the tensor cores work on the other's products. Four warps a tile hold its softmax, a thread
+// a row: scores come from tensor memory, weights go back over them and are the second product's A operand from there; nothing passes
+// through shared memory. (Two threads a row, eight warps a tile: 5 % slower, the halves wait for one another in every step.)
+// One warp issues the products, two the copies: a page of the cache is a TMA box (64 values x tokens), in the 128-byte swizzle, so
+// that K is the K-major and V the MN-major operand as they lie in the cache.
 // O is rescaled only when a score lies more than 2^8 above the row's reference (weights stay below 2^8, sums far from overflow);
 // the sum over the weights takes them before they are rounded to 16 bits.
 // Steps are dealt to the blocks as in ubp_attention.h: one block an SM, the same number of key tiles for each.
@@ -28,16 +29,17 @@ namespace {
 using namespace tc;
 
 constexpr int AT_BN = ATTN_BN, AT_TILE = 128, AT_THREADS = 384;
-constexpr int AT_COPY_WARP = 8, AT_MMA_WARP = 9;               // (of a third warpgroup, so that registers can be dealt)
-// Registers a thread: 168 at the launch (384 threads), then 208 for the softmax's two warpgroups and 80 for the third.
-constexpr int AT_POLY = 4;                                     // every fourth pair of weights on the multiply-add pipes
+// Warps of the first warpgroup copy keys, issue products and copy values; the others do the softmax. Registers a thread: 168 at the
+// launch (384 threads), then 80 for the first warpgroup and 208 for the two others.
+constexpr int AT_K_WARP = 0, AT_MMA_WARP = 1, AT_V_WARP = 2, AT_SOFT_WARP = 4;
 constexpr uint32_t AT_PANEL = 128 * 128;                       // 128 rows of 64 values
 constexpr uint32_t AT_SWZ = 2;                                 // 128-byte swizzle
+constexpr uint32_t AT_TURN = 32 * 128;                         // a softmax warp's: 128 bytes of each of its rows
 __host__ __device__ constexpr int at_stages(int dp) { return dp == 128 ? 2 : 4; }
 __host__ __device__ constexpr uint32_t at_part(int dp) { return (uint32_t)(dp / 64) * AT_PANEL; }
-constexpr uint32_t AT_TURN = 32 * 128;                         // a softmax warp's: 128 bytes of each of its rows
 __host__ __device__ constexpr uint32_t at_smem(int dp) { return (2 + 2 * (uint32_t)at_stages(dp)) * at_part(dp) + 8 * AT_TURN + 1024; }
 static_assert(at_smem(64) >= TC_PAIR_MIN_SMEM && at_smem(128) <= 226 * 1024, "one block an SM: a block holds all tensor memory");
+static_assert(sizeof(AttnPlace<AT_THREADS>) <= 8 * AT_TURN, "lies there until the steps are dealt");
 
 // N steps of 16 along the reduction: D (tensor memory) (+)= A B, A from shared memory, or the 16-bit values of tensor memory from
 // column `a` on. The whole warp calls with equal arguments, one elected lane issues: from a branch of a single lane the operands
@@ -115,37 +117,12 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
-{
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
 __device__ __forceinline__ float max3(float a, float b, float c)
 {
     float r;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
 }
-// 2^x of two values on the multiply-add pipes, for finite x below 127 (a NaN stays one; below -126: at most 2^-126): the nearest
-// integer n by adding 1.5 2^23, a polynomial of degree 4 for 2^(x - n) on [-1/2, 1/2] (a fit of our own for the relative error:
-// 2.6 10^-6), times 2^n. The special function unit takes 16 results a cycle and SM, as long for a tile's weights as the tensor
-// cores for its products; a share of them here relieves it.
-__device__ __forceinline__ uint64_t exp2_poly(uint64_t x2)
-{
-    float a, b;
-    halves(x2, a, b);
-    x2 = pair(max_nan(a, -126.f), max_nan(b, -126.f));
-    const uint64_t big = pair(12582912.f, 12582912.f), t = add2(x2, big);
-    const uint64_t f = fma2(add2(t, pair(-12582912.f, -12582912.f)), pair(-1.f, -1.f), x2);
-    uint64_t p = fma2(f, pair(0.0095701f, 0.0095701f), pair(0.05591786f, 0.05591786f));
-    p = fma2(p, f, pair(0.24024745f, 0.24024745f));
-    p = fma2(p, f, pair(0.69312181f, 0.69312181f));
-    p = fma2(p, f, pair(0.99999926f, 0.99999926f));
-    halves(t, a, b);
-    return mul2(p, pair(__uint_as_float((__float_as_uint(a) << 23) + 0x3f800000u), __uint_as_float((__float_as_uint(b) << 23) + 0x3f800000u)));
-}
-
 // bits 0 .. n - 1
 __device__ __forceinline__ uint32_t bits_below(int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1u; }
 
@@ -163,14 +140,12 @@ struct AtBars {
 // Segments of a block's steps: consecutive tiles of one item.
 struct AtSegments {
     AttnCursor cur;
-    int64_t left;
-    int tile0, n;
+    int left, tile0, n;
     __device__ __forceinline__ bool get()
     {
-        if (left <= 0) return false;
         tile0 = cur.tile;
-        n = (int)(cur.t.nt - cur.tile < left ? cur.t.nt - cur.tile : left);
-        return true;
+        n = imin(cur.t.nt - cur.tile, left);
+        return left > 0;
     }
     __device__ __forceinline__ void done(const AttnArgs &a)
     {
@@ -191,7 +166,6 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t *smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     __shared__ __align__(8) AtBars bars;
-    __shared__ AttnPlace place;
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -229,41 +203,42 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
     const uint32_t tmem = tmem_slot;
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
+    constexpr uint32_t TURN = (2 + 2 * ST) * PART;
     int64_t first;
-    AttnDeal deal(0, 0);
+    AttnDeal deal;
     AtSegments sg;
     bool ok = true;
-    int filled = 0;                        // copy warp: stages filled so far (keys and values alike)
-    if (!attn_locate(a, place, deal, first, sg.left, sg.cur)) {
+    int filled = 0;                        // copy warps: stages filled so far
+    if (!attn_locate<AT_THREADS>(a, *reinterpret_cast<AttnPlace<AT_THREADS> *>(smem + TURN), deal, first, sg.left, sg.cur)) {
         sg.left = 0;
         if (threadIdx.x == 0 && !a.common) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
     }
-    const int64_t count = sg.left;
+    const int count = sg.left;
     const uint32_t s_q = smem_u32(smem), s_k = s_q + 2 * PART, s_v = s_k + ST * PART;
 
-    if (warp >= AT_COPY_WARP) {
+    if (warp < AT_SOFT_WARP) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 80;");
-        if (warp == AT_COPY_WARP) {
-        const int page_mask = (1 << a.pshift) - 1, box = imin(1 << a.pshift, AT_BN), nbox = AT_BN / box;
-        int patches = 0;
-        for (; ok && sg.get(); sg.done(a)) {
-            const int kvh = sg.cur.hu / a.chunks;
-            const int32_t *row = a.table + (a.common ? 0 : (int64_t)sg.cur.b * a.ldt);
-            const AttnTiles &t = sg.cur.t;
-            for (int i = 0; ok && i < sg.n; ++i, ++filled) {
-                const int st = filled % ST, j0 = attn_tile_at(t, sg.tile0 + i) * AT_BN;
-                // (a lane a box)
-                const int page = lane < nbox ? attn_box_page(a, t, row, j0 + lane * box, box) : a.pages;
-                // Places of a page whose keys no row sees: whatever they hold, a weight of 0 times it has to be 0, so the values
-                // there are overwritten with zeros before the product reads them.
-                const bool patch = (j0 + AT_BN > t.end && (t.end & (box - 1))) || (j0 < a.kv0 && j0 + AT_BN > a.kv0 && (a.kv0 & (box - 1))) ||
-                                   (j0 < t.w0 && j0 + AT_BN > t.w0) || (j0 < a.sinks && j0 + AT_BN > a.sinks && j0 < t.w0);
-                for (int kv = 0; ok && kv < 2; ++kv) {
-                    const uint32_t full = smem_u32(kv ? &bars.v_full[st] : &bars.k_full[st]), empty = smem_u32(kv ? &bars.v_empty[st] : &bars.k_empty[st]);
-                    const uint32_t dst = (kv ? s_v : s_k) + (uint32_t)st * PART;
-                    const uint32_t bar = kv && patch ? smem_u32(&bars.patch) : full;
-                    if (filled >= ST) ok = mbar_wait(empty, (uint32_t)(filled / ST - 1) & 1u, &abort_flag);
-                    ok = __all_sync(0xffffffffu, ok);
+        if (warp == AT_K_WARP || warp == AT_V_WARP) {
+            const bool values = warp == AT_V_WARP;
+            const int page_mask = (1 << a.pshift) - 1, box = imin(1 << a.pshift, AT_BN), nbox = AT_BN / box;
+            const CUtensorMap *const tm = values ? &tmV : &tmK;
+            uint64_t *const bar_full = values ? bars.v_full : bars.k_full, *const bar_empty = values ? bars.v_empty : bars.k_empty;
+            const uint32_t ring = values ? s_v : s_k;
+            int patches = 0;
+            for (; ok && sg.get(); sg.done(a)) {
+                const int kvh = sg.cur.hu / a.chunks;
+                const int32_t *row = a.table + (a.common ? 0 : (int64_t)sg.cur.b * a.ldt);
+                const AttnTiles &t = sg.cur.t;
+                auto page_of = [&](int i) { return lane < nbox ? attn_box_page(a, t, row, attn_tile_at(t, sg.tile0 + i) * AT_BN + lane * box, box) : a.pages; };      // (a lane a box)
+                int page = page_of(0);
+                for (int i = 0; i < sg.n; ++i, ++filled) {
+                    const int st = filled % ST, j0 = attn_tile_at(t, sg.tile0 + i) * AT_BN, ahead = i + 1 < sg.n ? page_of(i + 1) : 0;
+                    // Places of a page whose keys no row sees: whatever they hold, a weight of 0 times it has to be 0, so the values
+                    // there are overwritten with zeros before the product reads them.
+                    const bool patch = values && ((j0 + AT_BN > t.end && (t.end & (box - 1))) || (j0 < a.kv0 && j0 + AT_BN > a.kv0 && (a.kv0 & (box - 1))) ||
+                                                  (j0 < t.w0 && j0 + AT_BN > t.w0) || (j0 < a.sinks && j0 + AT_BN > a.sinks && j0 < t.w0));
+                    const uint32_t full = smem_u32(&bar_full[st]), dst = ring + (uint32_t)st * PART, bar = patch ? smem_u32(&bars.patch) : full;
+                    if (filled >= ST) ok = attn_wait(smem_u32(&bar_empty[st]), (uint32_t)(filled / ST - 1) & 1u, &abort_flag);
                     if (!ok) break;
                     if (lane == 0) mbar_expect_tx(bar, PART);
                     for (int b = 0; b < nbox; ++b) {
@@ -271,12 +246,12 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                         if (lane == 0) {
 #pragma unroll
                             for (int p = 0; p < DP / 64; ++p)
-                                tma_load_4d(dst + (uint32_t)p * AT_PANEL + (uint32_t)(b * box) * 128u, kv ? &tmV : &tmK, p * 64, (j0 + b * box) & page_mask, kvh, pg, bar);
+                                tma_load_4d(dst + (uint32_t)p * AT_PANEL + (uint32_t)(b * box) * 128u, tm, p * 64, (j0 + b * box) & page_mask, kvh, pg, bar);
                         }
                     }
                     __syncwarp();
-                    if (kv && patch) {
-                        ok = __all_sync(0xffffffffu, mbar_wait(bar, (uint32_t)patches & 1u, &abort_flag));
+                    if (patch) {
+                        ok = attn_wait(bar, (uint32_t)patches & 1u, &abort_flag);
                         ++patches;
                         if (!ok) break;
                         for (int x = lane; x < AT_BN * DP / 8; x += 32) {
@@ -288,9 +263,9 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                         __syncwarp();
                         if (lane == 0) mbar_arrive(full);
                     }
+                    page = ahead;
                 }
             }
-        }
         } else if (warp == AT_MMA_WARP) {
         constexpr uint32_t fmt = std::is_same_v<T, __nv_bfloat16> ? 1 : 0;
         const uint32_t id_s = at_idesc(AT_BN, fmt, 0), id_o = at_idesc(NK * 16, fmt, 1);
@@ -308,7 +283,7 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
             }
             commit_one(smem_u32(&bars.s_full[i]));
         };
-        auto wait = [&](uint64_t &bar, uint32_t phase) { ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bar), phase, &abort_flag)); };
+        auto wait = [&](uint64_t &bar, uint32_t phase) { ok = attn_wait(smem_u32(&bar), phase, &abort_flag); };
         auto next_keys = [&] {
             commit_one(smem_u32(&bars.k_empty[ks]));
             if (++ks == ST) { ks = 0; k_phase ^= 1u; }
@@ -359,50 +334,112 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
-        const int tile = warp >> 2, r = (warp & 3) * 32 + lane;
+        const int tile = (warp - AT_SOFT_WARP) >> 2, r = (warp & 3) * 32 + lane;
         const uint32_t t_s = tmem + ((uint32_t)((warp & 3) * 32) << 16) + (uint32_t)tile * 128u, t_o = t_s + 256u;
-        uint8_t *const qs = smem + (uint32_t)tile * PART, *const turn = smem + (2 + 2 * ST) * PART + (uint32_t)warp * AT_TURN;
+        uint8_t *const turn = smem + TURN + (uint32_t)(warp - AT_SOFT_WARP) * AT_TURN;
         uint32_t s_phase = 0, o_phase = 0;
-        AttnRow row;
-        int all_hi, all_lo;
-        // the next item that has rows in this tile, and its queries on their way to the first product
-        auto begin = [&]() {
+        AttnRow row{-1, 0, 0, 0};
+        float m = 0.f, l = 0.f;
+        int64_t slot = 0;
+        bool before = false, complete = false;               // an item whose outcome is not stored yet
+        while (ok) {
+            const int token = row.token, head = row.head;
             while (sg.get() && tile == 1 && !sg.two(a)) sg.done(a);
-            if (sg.left <= 0) return false;
-            row = attn_row(a, sg.cur.q, sg.cur.hu, sg.cur.rt, tile * AT_TILE + r);
-            const T *p = static_cast<const T *>(a.q) + (row.token < 0 ? 0 : row.token * a.q_ts + row.head * a.q_hs);
-            uint4 v[2 * NK];
-            if (row.token < 0 || (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+            const bool live = sg.left > 0;
+            if (live) {                                       // the next item's queries
+                row = attn_row(a, sg.cur.q, sg.cur.hu, sg.cur.rt, tile * AT_TILE + r);
+                const T *p = static_cast<const T *>(a.q) + (row.token < 0 ? 0 : row.token * a.q_ts + row.head * a.q_hs);
+                auto put = [&](int c, const uint4 &v) {
+                    *reinterpret_cast<uint4 *>(smem + (uint32_t)tile * PART + (uint32_t)(c / 8) * AT_PANEL + (uint32_t)r * 128u + (uint32_t)(((c & 7) ^ (r & 7)) << 4)) = v;
+                };
+                if (row.token < 0 || (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+                    uint4 v[2 * NK];
 #pragma unroll
-                for (int c = 0; c < 2 * NK; ++c) v[c] = row.token >= 0 && c * 8 < a.D ? *reinterpret_cast<const uint4 *>(p + c * 8) : make_uint4(0, 0, 0, 0);
-            } else {
+                    for (int c = 0; c < 2 * NK; ++c) v[c] = row.token >= 0 && c * 8 < a.D ? *reinterpret_cast<const uint4 *>(p + c * 8) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-                for (int c = 0; c < 2 * NK; ++c) {
-                    const uint16_t *h = reinterpret_cast<const uint16_t *>(p + c * 8);
-                    v[c] = make_uint4(0, 0, 0, 0);
-                    if (c * 8 < a.D) v[c] = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16);
+                    for (int c = 0; c < 2 * NK; ++c) put(c, v[c]);
+                } else {
+#pragma unroll 1
+                    for (int c = 0; c < 2 * NK; ++c) {
+                        const uint16_t *h = reinterpret_cast<const uint16_t *>(p + c * 8);
+                        put(c, c * 8 < a.D ? make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16)
+                                           : make_uint4(0, 0, 0, 0));
+                    }
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                tmem_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&bars.q_full[tile]));
+            }
+            if (before) {
+                ok = attn_wait(smem_u32(&bars.o_full[tile]), o_phase, &abort_flag);
+                if (!ok) break;
+                o_phase ^= 1u;
+                tmem_after();
+                if (complete && a.pml) {                      // (with a shared prefix's sums: rare here, a thread a row)
+#pragma unroll 1
+                    for (int d = 0; d < a.D; d += 8) {
+                        uint32_t o[8];
+                        tmem_ld8(t_o + (uint32_t)d, o);
+                        tmem_wait_ld();
+                        float v[8], M = m, L = l;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(o[e]);
+                        if (token >= 0) attn_finish<T>(a, token, head, d, M, L, v);
+                    }
+                } else {
+                    // 128 bytes of each row at a time, turned in shared memory so that eight lanes store a row's (a thread a row: 32 lines a
+                    // store, 5300 cycles an item)
+                    const int64_t at = slot * a.rows + tile * AT_TILE + r;
+                    if (!complete && token >= 0) a.ml[at] = make_float2(m, l);
+                    const float scale = complete ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
+                    const int per = complete ? 64 : 32;       // values of 128 bytes
+                    uint8_t *const dst = complete ? reinterpret_cast<uint8_t *>(static_cast<T *>(a.out) + (token < 0 ? 0 : token * a.o_ts + head * a.o_hs))
+                                                  : reinterpret_cast<uint8_t *>(a.po + at * a.D);
+                    const int how = token < 0 ? 0 : (reinterpret_cast<uintptr_t>(dst) & 15) != 0 ? 2 : 1;        // (any alignment of the output)
+#pragma unroll 1
+                    for (int d = 0; d < a.D; d += per) {
+#pragma unroll 1
+                        for (int h = 0; h < per && d + h < a.D; h += 16) {
+                            uint32_t o[16];
+                            tmem_ld16(t_o + (uint32_t)(d + h), o);
+                            tmem_wait_ld();
+                            if (complete) {
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) o[e] = pack2<T>(__uint_as_float(o[2 * e]) * scale, __uint_as_float(o[2 * e + 1]) * scale);
+                            }
+                            const int at0 = complete ? h / 8 : h / 4;
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (e < 2 || !complete)
+                                    *reinterpret_cast<uint4 *>(turn + lane * 128 + (((at0 + e) ^ (lane & 7)) << 4)) = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
+                        }
+                        __syncwarp();
+                        const int ch = lane & 7, col = d + ch * (per / 8);
+#pragma unroll 4
+                        for (int i = 0; i < 8; ++i) {
+                            const int from = i * 4 + (lane >> 3);
+                            const uint4 v = *reinterpret_cast<const uint4 *>(turn + from * 128 + ((ch ^ (from & 7)) << 4));
+                            uint8_t *const to = reinterpret_cast<uint8_t *>(__shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(dst), from)) + d * 128 / per + ch * 16;
+                            const int kind = __shfl_sync(0xffffffffu, how, from);
+                            if (col < a.D && kind == 1) *reinterpret_cast<uint4 *>(to) = v;
+                            else if (col < a.D && kind == 2) {
+                                uint16_t *const q = reinterpret_cast<uint16_t *>(to);
+                                q[0] = (uint16_t)v.x; q[1] = (uint16_t)(v.x >> 16); q[2] = (uint16_t)v.y; q[3] = (uint16_t)(v.y >> 16);
+                                q[4] = (uint16_t)v.z; q[5] = (uint16_t)(v.z >> 16); q[6] = (uint16_t)v.w; q[7] = (uint16_t)(v.w >> 16);
+                            }
+                        }
+                        __syncwarp();
+                    }
                 }
             }
-#pragma unroll
-            for (int c = 0; c < 2 * NK; ++c)
-                *reinterpret_cast<uint4 *>(qs + (uint32_t)(c / 8) * AT_PANEL + (uint32_t)r * 128u + (uint32_t)(((c & 7) ^ (r & 7)) << 4)) = v[c];
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            tmem_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&bars.q_full[tile]));
+            if (!live) break;
             // keys that all (existing) rows of the warp see need no comparison
-            all_hi = row.token >= 0 ? row.hi : INT_MAX;
-            all_lo = row.token >= 0 ? row.lo : 0;
-            all_hi = __reduce_min_sync(0xffffffffu, all_hi);
-            all_lo = __reduce_max_sync(0xffffffffu, all_lo);
-            return true;
-        };
-        bool live = begin();
-        while (live) {
-            float m = -INFINITY, l = 0.f;
+            const int all_hi = __reduce_min_sync(0xffffffffu, row.token >= 0 ? row.hi : INT_MAX), all_lo = __reduce_max_sync(0xffffffffu, row.token >= 0 ? row.lo : 0);
+            m = -INFINITY; l = 0.f;
             for (int j = 0; j < sg.n; ++j) {
                 const int j0 = attn_tile_at(sg.cur.t, sg.tile0 + j) * AT_BN;
-                ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars.s_full[tile]), s_phase, &abort_flag));
+                ok = attn_wait(smem_u32(&bars.s_full[tile]), s_phase, &abort_flag);
                 if (!ok) break;
                 s_phase ^= 1u;
                 tmem_after();
@@ -410,8 +447,7 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
 #pragma unroll
                 for (int c = 0; c < 4; ++c) tmem_ld32(t_s + (uint32_t)c * 32u, s[c]);
                 tmem_wait_ld();
-                const bool all = j0 + AT_BN <= all_hi && j0 >= a.kv0 && (j0 >= all_lo || j0 + AT_BN <= a.sinks);
-                if (!all) {
+                if (!(j0 + AT_BN <= all_hi && j0 >= a.kv0 && (j0 >= all_lo || j0 + AT_BN <= a.sinks))) {
                     // keys first .. last - 1 of the tile (the first `early` ones too) are seen: a bit each, 32 at a time
                     const int first = imax(row.lo, a.kv0) - j0, last = row.hi - j0, early = imin(a.sinks, row.hi) - j0, least = a.kv0 - j0;
 #pragma unroll
@@ -450,41 +486,25 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                 const float ref = m == -INFINITY ? 0.f : m;
                 const uint64_t sc2 = pair(a.sc, a.sc), ref2 = pair(-ref, -ref);
                 uint64_t sum[2] = {0, 0};
-                auto weights = [&](auto polynomial) {
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) {
-                        uint32_t p[16];
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t p[16];
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const uint64_t x2 = fma2(pair(__uint_as_float(s[c][2 * e]), __uint_as_float(s[c][2 * e + 1])), sc2, ref2);
-                            uint64_t w2;
-                            float x, y;
-                            if (decltype(polynomial)::value && e % AT_POLY == AT_POLY - 1) {
-                                w2 = exp2_poly(x2);
-                                halves(w2, x, y);
-                            } else {
-                                halves(x2, x, y);
-                                x = attn_exp2(x); y = attn_exp2(y);
-                                w2 = pair(x, y);
-                            }
-                            sum[e & 1] = add2(sum[e & 1], w2);
-                            p[e] = pack2<T>(x, y);
-                        }
-                        tmem_st16(t_s + (uint32_t)c * 16u, p);
-                        if (c == 1) {                   // the product with the first 64 values may begin
-                            tmem_wait_st();
-                            tmem_before();
-                            __syncwarp();
-                            if (lane == 0) mbar_arrive(smem_u32(&bars.p_half[tile]));
-                        }
+                    for (int e = 0; e < 16; ++e) {
+                        float x, y;
+                        halves(fma2(pair(__uint_as_float(s[c][2 * e]), __uint_as_float(s[c][2 * e + 1])), sc2, ref2), x, y);
+                        x = attn_exp2(x); y = attn_exp2(y);
+                        sum[e & 1] = add2(sum[e & 1], pair(x, y));
+                        p[e] = pack2<T>(x, y);
                     }
-                };
-                if (all) weights(std::true_type{});
-                else weights(std::false_type{});     // (hidden keys' weights have to be 0)
-                tmem_wait_st();
-                tmem_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&bars.p_full[tile]));
+                    tmem_st16(t_s + (uint32_t)c * 16u, p);
+                    if (c & 1) {                            // the product with the first 64 values may begin
+                        tmem_wait_st();
+                        tmem_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem_u32(c == 1 ? &bars.p_half[tile] : &bars.p_full[tile]));
+                    }
+                }
                 float sums[4];
                 halves(sum[0], sums[0], sums[1]);
                 halves(sum[1], sums[2], sums[3]);
@@ -492,78 +512,12 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
             }
             if (!ok) break;
             // the item's outcome is on its way to tensor memory; the next item's queries go first
-            const int token = row.token, head = row.head, c = (int)blockIdx.x;
-            const bool complete = sg.n == sg.cur.t.nt && !a.common;
-            int64_t slot = 2 * (int64_t)c + (sg.left < count ? 1 : 0);
-            if (a.common) slot = (int64_t)sg.cur.hu * attn_row_blocks(a, sg.cur.q) + sg.cur.rt + c;
-            if (tile == 0 && r == 0 && !a.common && sg.left == sg.n) attn_describe(a, sg.cur, deal, c, count - sg.n, sg.tile0, sg.n);
+            const int c = (int)blockIdx.x;
+            before = true;
+            complete = sg.n == sg.cur.t.nt && !a.common;
+            slot = a.common ? ((int64_t)sg.cur.hu * attn_row_blocks(a, sg.cur.q) + sg.cur.rt) + c : 2 * (int64_t)c + (sg.left < count ? 1 : 0);
+            if (warp == AT_SOFT_WARP && lane == 0 && !a.common && sg.left == sg.n) attn_describe(a, sg.cur, deal, c, count - sg.n, sg.tile0, sg.n);
             sg.done(a);
-            live = begin();
-            ok = __all_sync(0xffffffffu, mbar_wait(smem_u32(&bars.o_full[tile]), o_phase, &abort_flag));
-            if (!ok) break;
-            o_phase ^= 1u;
-            tmem_after();
-            const int64_t at = slot * a.rows + tile * AT_TILE + r;
-            if (complete && a.pml) {
-#pragma unroll 1
-                for (int d = 0; d < a.D; d += 8) {
-                    uint32_t o[8];
-                    tmem_ld8(t_o + (uint32_t)d, o);
-                    tmem_wait_ld();
-                    float v[8], M = m, L = l;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(o[e]);
-                    if (token >= 0) attn_finish<T>(a, token, head, d, M, L, v);
-                }
-            } else {
-                // 128 bytes of each row at a time, turned in shared memory so that eight lanes store a row's (a thread a row: 32 rows
-                // a store, 5300 cycles an item)
-                if (!complete && token >= 0) a.ml[at] = make_float2(m, l);
-                const float scale = complete ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
-                const int per = complete ? 64 : 32;
-                uint8_t *const dst = complete ? reinterpret_cast<uint8_t *>(static_cast<T *>(a.out) + (token < 0 ? 0 : token * a.o_ts + head * a.o_hs))
-                                              : reinterpret_cast<uint8_t *>(a.po + at * a.D);
-                const bool apart = (reinterpret_cast<uintptr_t>(dst) & 15) != 0;        // (any alignment of the output)
-#pragma unroll 1
-                for (int d = 0; d < a.D; d += per) {
-#pragma unroll 1
-                    for (int h = 0; h < per && d + h < a.D; h += 16) {
-                        uint32_t o[16];
-                        tmem_ld16(t_o + (uint32_t)(d + h), o);
-                        tmem_wait_ld();
-                        if (complete) {
-                            uint32_t w[8];
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) w[e] = pack2<T>(__uint_as_float(o[2 * e]) * scale, __uint_as_float(o[2 * e + 1]) * scale);
-#pragma unroll
-                            for (int e = 0; e < 2; ++e)
-                                *reinterpret_cast<uint4 *>(turn + lane * 128 + (((h / 8 + e) ^ (lane & 7)) << 4)) = make_uint4(w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]);
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                *reinterpret_cast<uint4 *>(turn + lane * 128 + (((h / 4 + e) ^ (lane & 7)) << 4)) = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
-                        }
-                    }
-                    __syncwarp();
-                    const int ch = lane & 7, col = d + ch * (per / 8);
-#pragma unroll 2
-                    for (int i = 0; i < 8; ++i) {
-                        const int from = i * 4 + (lane >> 3);
-                        const uint4 v = *reinterpret_cast<const uint4 *>(turn + from * 128 + ((ch ^ (from & 7)) << 4));
-                        const uint64_t base = __shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(dst), from);
-                        const bool there = __shfl_sync(0xffffffffu, token, from) >= 0, odd = __shfl_sync(0xffffffffu, (int)apart, from) != 0;
-                        if (!there || col >= a.D) continue;
-                        uint8_t *const to = reinterpret_cast<uint8_t *>(base) + d * 128 / per + ch * 16;
-                        if (!odd) *reinterpret_cast<uint4 *>(to) = v;
-                        else {
-                            uint16_t *const h = reinterpret_cast<uint16_t *>(to);
-                            h[0] = (uint16_t)v.x; h[1] = (uint16_t)(v.x >> 16); h[2] = (uint16_t)v.y; h[3] = (uint16_t)(v.y >> 16);
-                            h[4] = (uint16_t)v.z; h[5] = (uint16_t)(v.z >> 16); h[6] = (uint16_t)v.w; h[7] = (uint16_t)(v.w >> 16);
-                        }
-                    }
-                    __syncwarp();
-                }
-            }
         }
     }
     if (!ok && lane == 0) atomicExch(a.status, 1);
@@ -572,16 +526,15 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
     if (*(volatile int *)&abort_flag) {
         // a block whose waits ran out leaves no copy and no product under way (a millisecond at most each)
         int gave_up = 0;
-        if (warp == AT_COPY_WARP) {
+        if (warp == AT_K_WARP || warp == AT_V_WARP) {
             for (int f = filled > ST ? filled - ST : 0; f <= filled; ++f) {
-                mbar_wait(smem_u32(&bars.k_full[f % ST]), (uint32_t)(f / ST) & 1u, &gave_up, 1000000);
-                mbar_wait(smem_u32(&bars.v_full[f % ST]), (uint32_t)(f / ST) & 1u, &gave_up, 1000000);
-                mbar_wait(smem_u32(&bars.patch), (uint32_t)(f & 1), &gave_up, 1000000);
+                attn_wait(smem_u32(warp == AT_V_WARP ? &bars.v_full[f % ST] : &bars.k_full[f % ST]), (uint32_t)(f / ST) & 1u, &gave_up, 1);
+                if (warp == AT_V_WARP) attn_wait(smem_u32(&bars.patch), (uint32_t)(f & 1), &gave_up, 1);
             }
         }
         if (warp == AT_MMA_WARP) {
             commit_one(smem_u32(&bars.drain));
-            mbar_wait(smem_u32(&bars.drain), 0, &gave_up, 1000000);
+            attn_wait(smem_u32(&bars.drain), 0, &gave_up, 1);
         }
         __syncthreads();
     }
