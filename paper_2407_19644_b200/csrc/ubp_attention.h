@@ -9,7 +9,8 @@
 // Steps. All items of a call lie one behind the other -- sequence by sequence, unit head by unit head, row block by row block --
 // and block c of G takes the c-th share of their steps: every block gets the same number to within one whatever the lengths are,
 // which only the device knows. An item that ends up with several blocks is joined by a second kernel from their partial results.
-// (With the heads inside the row blocks, prompts of eight key heads ran at 757 TFLOP/s instead of 1197: the blocks at work then
+// An item counts for `extra` steps more than its tiles: what its beginning and end take. Without them, blocks that got many short
+// items (the first rows of a prompt, short sequences of a batch) took twice as long as the others. (With the heads inside the row blocks, prompts of eight key heads ran at 757 TFLOP/s instead of 1197: the blocks at work then
 // read eight times as many different keys at a time.)
 #ifndef UBP_ATTENTION_H_
 #define UBP_ATTENTION_H_
@@ -45,6 +46,8 @@ struct AttnArgs {
     int tiles;                      // row tiles of a row block (each rows / tiles rows)
     int gc, chunks, HU;             // heads of a unit head, unit heads of a key head, unit heads in all
     int tpt;                        // tokens a row block takes
+    int extra;                      // steps that an item counts for beside its tiles
+    int q_direct;                   // queries can be copied as they are (16-byte aligned)
     float sc;                       // scale * log2(e)
     int window, sinks;
     int kv0, kv1;                   // keys outside [kv0, kv1) are left out (a shared prefix is a call of its own)
@@ -134,9 +137,27 @@ struct AttnCursor {
         }
         t = attn_block_tiles(a, q, rt);
     }
-    UBP_HD void next(const AttnArgs &a, bool more)
+};
+
+// The steps of a block that are left: a cursor at the next tile, and how many steps its share still holds (extras included).
+struct AttnSteps {
+    AttnCursor c;
+    int left;
+    UBP_HD void seek(const AttnArgs &a)             // a share may begin in an item's extras
     {
-        if (++tile == t.nt && more) next_item(a);
+        if (left > 0 && c.tile >= c.t.nt) skip(a);
+    }
+    UBP_HD void skip(const AttnArgs &a)             // the rest of the item's steps
+    {
+        left -= c.t.nt + a.extra - c.tile;
+        if (left > 0) c.next_item(a);
+    }
+    UBP_HD int tiles() const { return imin(c.t.nt - c.tile, left); }      // of the item, in this share
+    UBP_HD void advance(const AttnArgs &a, int n)   // past n tiles
+    {
+        c.tile += n;
+        left -= n;
+        if (left > 0 && c.tile == c.t.nt) skip(a);
     }
 };
 

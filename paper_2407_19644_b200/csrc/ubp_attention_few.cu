@@ -61,25 +61,24 @@ __device__ __forceinline__ uint32_t load_pair(const uint16_t *p) { return (uint3
 // The copies of a warp's steps: a cursor that runs ahead, with the pages of the next step already loaded (one, or two of eight keys).
 // Everything is the same in all lanes; lane 0 issues.
 template <int DP> struct FewCopies {
-    AttnCursor c;
-    int left;                // steps that are not issued yet
+    AttnSteps s;
     int page[2], j0, kvh;
     const int32_t *row;
 
     __device__ __forceinline__ void item(const AttnArgs &a)
     {
-        kvh = (int)((uint32_t)c.hu / (uint32_t)a.chunks);
-        row = a.table + (a.common ? 0 : (int64_t)c.b * a.ldt);
+        kvh = (int)((uint32_t)s.c.hu / (uint32_t)a.chunks);
+        row = a.table + (a.common ? 0 : (int64_t)s.c.b * a.ldt);
     }
     __device__ __forceinline__ void peek(const AttnArgs &a, int warp)
     {
-        j0 = attn_tile_at(c.t, c.tile) * FEW_BN + warp * FEW_KEYS;
-        page[0] = attn_box_page(a, c.t, row, j0, imin(1 << a.pshift, FEW_KEYS));
-        if (a.pshift == 3) page[1] = attn_box_page(a, c.t, row, j0 + 8, 8);
+        j0 = attn_tile_at(s.c.t, s.c.tile) * FEW_BN + warp * FEW_KEYS;
+        page[0] = attn_box_page(a, s.c.t, row, j0, imin(1 << a.pshift, FEW_KEYS));
+        if (a.pshift == 3) page[1] = attn_box_page(a, s.c.t, row, j0 + 8, 8);
     }
     __device__ __forceinline__ void issue(const AttnArgs &a, const CUtensorMap *tmK, const CUtensorMap *tmV, uint32_t stage, uint32_t bar, int warp, int lane)
     {
-        if (left <= 0) return;
+        if (s.left <= 0) return;
         if (lane == 0) {
             const int at = j0 & ((1 << a.pshift) - 1);
             mbar_expect_tx(bar, 2 * few_part(DP));
@@ -96,9 +95,11 @@ template <int DP> struct FewCopies {
                 }
             }
         }
-        --left;
-        if (++c.tile == c.t.nt && left > 0) { c.next_item(a); item(a); }
-        if (left > 0) peek(a, warp);
+        const bool over = s.c.tile + 1 == s.c.t.nt;
+        s.advance(a, 1);
+        if (s.left <= 0) return;
+        if (over) item(a);
+        peek(a, warp);
     }
 };
 
@@ -128,20 +129,18 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     __syncthreads();
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
-    int64_t first;
-    int count;
     AttnDeal deal;
-    AttnCursor cur;
+    AttnSteps steps;
     static_assert(sizeof(AttnPlace<FEW_WARPS * 32>) <= FEW_WARPS * 8 * 64 * 4, "lies where the warps' sums meet");
-    if (!attn_locate<FEW_WARPS * 32>(a, *reinterpret_cast<AttnPlace<FEW_WARPS * 32> *>(meet), deal, first, count, cur)) {
+    if (!attn_locate<FEW_WARPS * 32>(a, *reinterpret_cast<AttnPlace<FEW_WARPS * 32> *>(meet), deal, steps)) {
         if (threadIdx.x == 0 && !a.common) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
         return;
     }
     FewCopies<DP> copies;
-    copies.c = cur;
-    copies.left = count;
+    copies.s = steps;
     copies.item(a);
-    copies.peek(a, warp);
+    if (steps.left > 0) copies.peek(a, warp);
+    const AttnCursor &cur = steps.c;
     for (int s = 0; s < ST - 1; ++s) copies.issue(a, &tmK, &tmV, ring + (uint32_t)s * 2 * PART, smem_u32(&bar_full[warp][s]), warp, lane);
 
     // where the lane's rows of matrix instructions' operands lie in a part: piece (2 k + h) of 16 bytes at k * 32 (within 128 bytes)
@@ -153,16 +152,18 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     uint32_t qf[NK][4];
     float o[2 * NK][4], m[2], l[2];
     AttnRow row[2];
-    int tile0 = cur.tile, st = 0, all_lo = 0, all_hi = 0;
+    int tile0 = 0, before = 0, st = 0, all_lo = 0, all_hi = 0;      // of the segment: its first tile, the share's steps before it
     uint32_t phase = 0;
     bool fresh = true, ok = true;
-    for (int step = 0; step < count; ++step) {
+    bool described = false;
+    while (steps.left > 0) {
         __syncwarp();                       // (all lanes have read the stage that is copied to now)
         const int nx = st == 0 ? ST - 1 : st - 1;
         copies.issue(a, &tmK, &tmV, ring + (uint32_t)nx * 2 * PART, smem_u32(&bar_full[warp][nx]), warp, lane);
         if (fresh) {
             fresh = false;
             tile0 = cur.tile;
+            before = deal.count((int)blockIdx.x) - steps.left;
             const AttnRow w = attn_row(a, cur.q, cur.hu, cur.rt, lane & 15);
             if (warp == 0 && lane < 16) rows[lane] = make_int2(w.token, w.head);
             all_lo = w.token >= 0 ? w.lo : 0;
@@ -263,8 +264,7 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
             }
         }
         if (++st == ST) { st = 0; phase ^= 1u; }
-        const bool last = step + 1 == count;
-        if (cur.tile + 1 == cur.t.nt || last) {
+        if (cur.tile + 1 == cur.t.nt || steps.left == 1) {
             // ---- the warps' sums meet: rows 0 .. 7, then 8 .. 15 where the item has them
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
@@ -275,7 +275,7 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
             const int nr = imin(imin(a.tpt, cur.q.n - cur.rt * a.tpt) * a.gc, FEW_ROWS), n = cur.tile + 1 - tile0;
             const bool whole = n == cur.t.nt && !a.common;
             const int c = (int)blockIdx.x;
-            int64_t slot = 2 * (int64_t)c + (step + 1 - n > 0 ? 1 : 0);
+            int64_t slot = 2 * (int64_t)c + (before > 0 ? 1 : 0);
             if (a.common) slot = (int64_t)cur.hu * attn_row_blocks(a, cur.q) + cur.rt + c;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
@@ -307,11 +307,12 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
                 }
             }
             __syncthreads();
-            if (last && threadIdx.x == 0 && !a.common) attn_describe(a, cur, deal, c, step + 1 - n, tile0, n);
+            if (threadIdx.x == 0 && !a.common && tile0 == 0 && !whole) { attn_describe(a, cur, deal, c, before, tile0, n); described = true; }
             fresh = true;
         }
-        cur.next(a, !last);
+        steps.advance(a, 1);
     }
+    if (threadIdx.x == 0 && !a.common && !described) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
     if (!ok) {                              // copies that are still under way end before the block does (a millisecond at most each)
         int gave_up = 0;
         for (int i = 0; i < ST; ++i)
@@ -320,26 +321,30 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     }
 }
 
-// Joins the partial results of an item that several blocks have worked on, in the order of its keys: 16 rows a block.
-// COMMON: block (u, i) takes rows 16 i .. of item u of the shared prefix; all of its blocks' results lie in slots u + block, and the
+// Joins the partial results of an item that several blocks have worked on, in the order of its keys: a warp a row, four values a
+// lane, eight parts under way at a time.
+// COMMON: block (u, i) takes rows 8 i .. of item u of the shared prefix; all of its blocks' results lie in slots u + block, and the
 // sums go to pml and ppo. Else block (c, i) takes those of the item that begins in block c, if it does not end there.
+constexpr int JOIN_ROWS = 8;
 template <typename T, bool COMMON>
-__global__ void __launch_bounds__(256) ubp_attention_join_kernel(const AttnArgs a, const int blocks)
+__global__ void __launch_bounds__(JOIN_ROWS * 32) ubp_attention_join_kernel(const AttnArgs a, const int blocks)
 {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int r = (int)blockIdx.y * JOIN_ROWS + (int)(threadIdx.x >> 5), col = (int)(threadIdx.x & 31) * 4;
     int t0, n, hu, parts;
     int64_t slot0, slot1;                   // of the first part, and of the second one (the others follow)
     if constexpr (COMMON) {
         const AttnSeq q = attn_seq(a, 0);
         const int nrt = attn_row_blocks(a, q), nt = attn_block_tiles(a, q, 0).nt, u = (int)blockIdx.x;
         if (u >= nrt * a.HU) return;
-        const AttnDeal deal((int64_t)nrt * a.HU * nt, blocks);
+        const AttnDeal deal((int64_t)nrt * a.HU * (nt + a.extra), blocks);
         hu = u / nrt;
         t0 = (u - hu * nrt) * a.tpt;
         n = q.n - t0;
-        const int c = deal.owner((int64_t)u * nt);
-        parts = deal.owner((int64_t)(u + 1) * nt - 1) - c + 1;
+        const int64_t x = (int64_t)u * (nt + a.extra);
+        const int c = deal.owner(x);
+        parts = deal.owner(x + nt - 1) - c + 1;
         slot0 = u + c; slot1 = slot0 + 1;
     } else {
         const int c = (int)blockIdx.x;
@@ -349,28 +354,32 @@ __global__ void __launch_bounds__(256) ubp_attention_join_kernel(const AttnArgs 
         slot1 = 2 * (int64_t)(c + 1);
     }
     if (parts == 0) return;
-    constexpr int N = 4;
-    const int per = a.D / N, step = COMMON ? 1 : 2;
-    for (int x = (int)threadIdx.x; x < 16 * per; x += 256) {
-        const int r = (int)blockIdx.y * 16 + x / per, col = x % per * N;
-        const int2 w = attn_row_at(a, t0, n, hu, r);
-        if (w.x < 0) continue;
-        float M = -INFINITY, L = 0.f, o[N] = {};
-#pragma unroll 4
-        for (int k = 0; k < parts; ++k) {
-            const int64_t at = (k == 0 ? slot0 : slot1 + (int64_t)(k - 1) * step) * a.rows + r;
-            const float2 ml = a.ml[at];
-            float v[N];
-            attn_load(a.po + at * a.D + col, v);
-            attn_add(M, L, o, ml.x, ml.y, v);
+    const int2 w = attn_row_at(a, t0, n, hu, r);
+    if (w.x < 0 || col >= a.D) return;
+    constexpr int N = 4, AHEAD = 8, STEP = COMMON ? 1 : 2;
+    float M = -INFINITY, L = 0.f, o[N] = {};
+    for (int k0 = 0; k0 < parts; k0 += AHEAD) {
+        float2 ml[AHEAD];
+        float v[AHEAD][N];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int k = k0 + i;
+            if (k < parts) {
+                const int64_t at = (k == 0 ? slot0 : slot1 + (int64_t)(k - 1) * STEP) * a.rows + r;
+                ml[i] = a.ml[at];
+                attn_load(a.po + at * a.D + col, v[i]);
+            }
         }
-        if constexpr (COMMON) {
-            const int64_t at = (int64_t)w.x * a.Hq + w.y;
-            if (col == 0) a.pml[at] = make_float2(M, L);
-            *reinterpret_cast<float4 *>(a.ppo + at * a.D + col) = make_float4(o[0], o[1], o[2], o[3]);
-        } else {
-            attn_finish<T>(a, w.x, w.y, col, M, L, o);
-        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+            if (k0 + i < parts) attn_add(M, L, o, ml[i].x, ml[i].y, v[i]);
+    }
+    if constexpr (COMMON) {
+        const int64_t at = (int64_t)w.x * a.Hq + w.y;
+        if (col == 0) a.pml[at] = make_float2(M, L);
+        *reinterpret_cast<float4 *>(a.ppo + at * a.D + col) = make_float4(o[0], o[1], o[2], o[3]);
+    } else {
+        attn_finish<T>(a, w.x, w.y, col, M, L, o);
     }
 }
 
@@ -400,13 +409,13 @@ int launch_attn_few(const AttnArgs &a, int dtype, int grid, void *stream)
 int launch_attn_join(const AttnArgs &a, int dtype, int grid, void *stream)
 {
     static std::atomic<bool> done[64] = {};
-    const unsigned y = (unsigned)((a.rows + 15) / 16);
+    const unsigned y = (unsigned)((a.rows + JOIN_ROWS - 1) / JOIN_ROWS);
     if (a.common) {
         const int64_t units = (int64_t)((a.T + a.tpt - 1) / a.tpt) * a.HU;
-        return attn_launch(ubp_attention_join_kernel<__half, true>, done, dim3((unsigned)units, y), 256, 0, stream, a, grid);
+        return attn_launch(ubp_attention_join_kernel<__half, true>, done, dim3((unsigned)units, y), JOIN_ROWS * 32, 0, stream, a, grid);
     }
-    return dtype == UBP_BF16 ? attn_launch(ubp_attention_join_kernel<__nv_bfloat16, false>, done, dim3((unsigned)grid, y), 256, 0, stream, a, grid)
-                             : attn_launch(ubp_attention_join_kernel<__half, false>, done, dim3((unsigned)grid, y), 256, 0, stream, a, grid);
+    return dtype == UBP_BF16 ? attn_launch(ubp_attention_join_kernel<__nv_bfloat16, false>, done, dim3((unsigned)grid, y), JOIN_ROWS * 32, 0, stream, a, grid)
+                             : attn_launch(ubp_attention_join_kernel<__half, false>, done, dim3((unsigned)grid, y), JOIN_ROWS * 32, 0, stream, a, grid);
 }
 
 }  // namespace ubp

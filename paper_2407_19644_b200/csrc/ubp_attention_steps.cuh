@@ -17,15 +17,16 @@ __device__ __forceinline__ float attn_exp2(float x)
 // Shared memory of attn_locate, for blocks of NT threads.
 template <int NT> struct AttnPlace { int warp[2][32]; int pre[NT + 1]; int b, rt, before, from, to; };
 
-// The block's steps, [first, first + count), and the cursor at the first one. Called by all threads of the block, NT of them (a
+// The block's share of the steps, from its first one on. Called by all threads of the block, NT of them (a
 // multiple of 32); false, to all of them, if there is nothing to do. Row blocks (of all sequences, a thread each) are counted and
 // summed in parallel, for one unit head: all of a sequence's have equal steps, so that step x lies in the sequence that x / HU lies in.
 template <int NT>
-__device__ __forceinline__ bool attn_locate(const AttnArgs &a, AttnPlace<NT> &sh, AttnDeal &deal, int64_t &first, int &count, AttnCursor &cur)
+__device__ __forceinline__ bool attn_locate(const AttnArgs &a, AttnPlace<NT> &sh, AttnDeal &deal, AttnSteps &steps)
 {
     constexpr int NW = NT / 32;
     const int tid = (int)threadIdx.x, lane = tid & 31, warp = tid >> 5, c = (int)blockIdx.x;
     const int nb = a.common ? 1 : a.B;
+    int64_t first = 0;
     auto warp_sum = [&](int x) {        // inclusive
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -38,7 +39,7 @@ __device__ __forceinline__ bool attn_locate(const AttnArgs &a, AttnPlace<NT> &sh
         deal = AttnDeal(total * a.HU, (int)gridDim.x);
         if (c >= deal.grid) return false;
         first = deal.first(c);
-        count = deal.count(c);
+        steps.left = deal.count(c);
         return true;
     };
     if (nb <= 32) {                     // a few sequences of one row block each: every warp for itself, no barrier
@@ -46,13 +47,14 @@ __device__ __forceinline__ bool attn_locate(const AttnArgs &a, AttnPlace<NT> &sh
         if (lane < nb) q = attn_seq(a, lane);
         const int blocks = attn_row_blocks(a, q);
         if (!__any_sync(0xffffffffu, blocks > 1)) {
-            const int mine = blocks ? attn_block_tiles(a, q, 0).nt : 0, x = warp_sum(mine);
+            const int mine = blocks ? attn_block_tiles(a, q, 0).nt + a.extra : 0, x = warp_sum(mine);
             if (!begin(__shfl_sync(0xffffffffu, x, 31))) return false;
             const int b = __ffs(__ballot_sync(0xffffffffu, (int64_t)x * a.HU > first)) - 1;
-            cur.set(a, b, 0, 0, 0);
-            const uint32_t rem = (uint32_t)(first - (int64_t)__shfl_sync(0xffffffffu, x - mine, b) * a.HU);
-            cur.hu = (int)(rem / (uint32_t)cur.t.nt);
-            cur.tile = (int)(rem - (uint32_t)cur.hu * (uint32_t)cur.t.nt);
+            steps.c.set(a, b, 0, 0, 0);
+            const uint32_t rem = (uint32_t)(first - (int64_t)__shfl_sync(0xffffffffu, x - mine, b) * a.HU), per = (uint32_t)__shfl_sync(0xffffffffu, mine, b);
+            steps.c.hu = (int)(rem / per);
+            steps.c.tile = (int)(rem - (uint32_t)steps.c.hu * per);
+            steps.seek(a);
             return true;
         }
     }
@@ -87,7 +89,7 @@ __device__ __forceinline__ bool attn_locate(const AttnArgs &a, AttnPlace<NT> &sh
                         if (sh.pre[m] <= i) s = m;
                         else hi = m;
                     }
-                    nt = attn_block_tiles(a, attn_seq(a, base + s), i - sh.pre[s]).nt;
+                    nt = attn_block_tiles(a, attn_seq(a, base + s), i - sh.pre[s]).nt + a.extra;
                 }
                 const int before = scan(nt, all);
                 if (nt) visit(base + s, i - sh.pre[s], sum + before, nt);
@@ -118,11 +120,12 @@ __device__ __forceinline__ bool attn_locate(const AttnArgs &a, AttnPlace<NT> &sh
     });
     const int from = sh.from;
     const int64_t rem = first - (int64_t)from * a.HU;
-    const int hu = (int)(rem / (sh.to - from));
+    const int hu = rem >> 32 ? (int)(rem / (sh.to - from)) : (int)((uint32_t)rem / (uint32_t)(sh.to - from));
     const int64_t z = from + (rem - (int64_t)hu * (sh.to - from));
     again([&](int b_, int rt, int64_t before, int nt) { if (b_ == b && z >= before && z < before + nt) { sh.rt = rt; sh.before = (int)before; } });
-    cur.set(a, b, hu, sh.rt, (int)z - sh.before);
+    steps.c.set(a, b, hu, sh.rt, (int)z - sh.before);
     __syncthreads();                    // (sh may be something else from here on)
+    steps.seek(a);
     return true;
 }
 

@@ -7,7 +7,7 @@
 // tile's scores go through the softmax, the tensor cores work on the other's products. Four warps a tile hold its softmax, a thread
 // a row: scores come from tensor memory, weights go back over them and are the second product's A operand from there; nothing passes
 // through shared memory. (Two threads a row, eight warps a tile: 5 % slower, the halves wait for one another in every step.)
-// One warp issues the products, two the copies: a page of the cache is a TMA box (64 values x tokens), in the 128-byte swizzle, so
+// One warp issues the products, three the copies: a page of the cache is a TMA box (64 values x tokens), in the 128-byte swizzle, so
 // that K is the K-major and V the MN-major operand as they lie in the cache.
 // O is rescaled only when a score lies more than 2^8 above the row's reference (weights stay below 2^8, sums far from overflow);
 // the sum over the weights takes them before they are rounded to 16 bits.
@@ -29,9 +29,9 @@ namespace {
 using namespace tc;
 
 constexpr int AT_BN = ATTN_BN, AT_TILE = 128, AT_THREADS = 384;
-// Warps of the first warpgroup copy keys, issue products and copy values; the others do the softmax. Registers a thread: 168 at the
+// Warps of the first warpgroup copy keys, issue products, copy values and queries; the others do the softmax. Registers a thread: 168 at the
 // launch (384 threads), then 80 for the first warpgroup and 208 for the two others.
-constexpr int AT_K_WARP = 0, AT_MMA_WARP = 1, AT_V_WARP = 2, AT_SOFT_WARP = 4;
+constexpr int AT_K_WARP = 0, AT_MMA_WARP = 1, AT_V_WARP = 2, AT_Q_WARP = 3, AT_SOFT_WARP = 4;
 constexpr uint32_t AT_PANEL = 128 * 128;                       // 128 rows of 64 values
 constexpr uint32_t AT_SWZ = 2;                                 // 128-byte swizzle
 constexpr uint32_t AT_TURN = 32 * 128;                         // a softmax warp's: 128 bytes of each of its rows
@@ -133,33 +133,28 @@ __device__ __forceinline__ uint32_t at_idesc(int n, int fmt, int b_mn)
 }
 
 struct AtBars {
-    uint64_t q_full[2], s_full[2], p_half[2], p_full[2], o_full[2];
+    uint64_t q_full[2], q_empty[2], s_full[2], p_half[2], p_full[2], o_full[2];
     uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], patch, drain;
 };
 
 // Segments of a block's steps: consecutive tiles of one item.
 struct AtSegments {
-    AttnCursor cur;
-    int left, tile0, n;
+    AttnSteps s;
+    int n;
     __device__ __forceinline__ bool get()
     {
-        tile0 = cur.tile;
-        n = imin(cur.t.nt - cur.tile, left);
-        return left > 0;
+        n = s.tiles();
+        return s.left > 0;
     }
-    __device__ __forceinline__ void done(const AttnArgs &a)
-    {
-        left -= n;
-        if (left > 0) cur.next_item(a);
-    }
+    __device__ __forceinline__ void done(const AttnArgs &a) { s.advance(a, n); }
     // whether the item's second tile has rows
-    __device__ __forceinline__ bool two(const AttnArgs &a) const { return cur.q.n - cur.rt * a.tpt > a.tpt / 2; }
+    __device__ __forceinline__ bool two(const AttnArgs &a) const { return s.c.q.n - s.c.rt * a.tpt > a.tpt / 2; }
 };
-
 // NK: head size in steps of 16 (the copies bring zeros past it)
 template <typename T, int NK>
 __global__ void __launch_bounds__(AT_THREADS, 1)
-ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const AttnArgs a)
+ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const __grid_constant__ CUtensorMap tmQ,
+                        const AttnArgs a)
 {
     constexpr int DP = NK > 4 ? 128 : 64, ST = at_stages(DP);
     constexpr uint32_t PART = at_part(DP);
@@ -176,7 +171,8 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
         prefetch_tensormap(&tmV);
         abort_flag = 0;
         for (int i = 0; i < 2; ++i) {
-            mbar_init(smem_u32(&bars.q_full[i]), 4);
+            mbar_init(smem_u32(&bars.q_full[i]), 1);
+            mbar_init(smem_u32(&bars.q_empty[i]), 1);
             mbar_init(smem_u32(&bars.s_full[i]), 1);
             mbar_init(smem_u32(&bars.p_half[i]), 4);
             mbar_init(smem_u32(&bars.p_full[i]), 4);
@@ -204,16 +200,11 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
     constexpr uint32_t TURN = (2 + 2 * ST) * PART;
-    int64_t first;
     AttnDeal deal;
     AtSegments sg;
     bool ok = true;
     int filled = 0;                        // copy warps: stages filled so far
-    if (!attn_locate<AT_THREADS>(a, *reinterpret_cast<AttnPlace<AT_THREADS> *>(smem + TURN), deal, first, sg.left, sg.cur)) {
-        sg.left = 0;
-        if (threadIdx.x == 0 && !a.common) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
-    }
-    const int count = sg.left;
+    if (!attn_locate<AT_THREADS>(a, *reinterpret_cast<AttnPlace<AT_THREADS> *>(smem + TURN), deal, sg.s)) sg.s.left = 0;
     const uint32_t s_q = smem_u32(smem), s_k = s_q + 2 * PART, s_v = s_k + ST * PART;
 
     if (warp < AT_SOFT_WARP) {
@@ -226,13 +217,13 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
             const uint32_t ring = values ? s_v : s_k;
             int patches = 0;
             for (; ok && sg.get(); sg.done(a)) {
-                const int kvh = sg.cur.hu / a.chunks;
-                const int32_t *row = a.table + (a.common ? 0 : (int64_t)sg.cur.b * a.ldt);
-                const AttnTiles &t = sg.cur.t;
-                auto page_of = [&](int i) { return lane < nbox ? attn_box_page(a, t, row, attn_tile_at(t, sg.tile0 + i) * AT_BN + lane * box, box) : a.pages; };      // (a lane a box)
+                const int kvh = sg.s.c.hu / a.chunks;
+                const int32_t *row = a.table + (a.common ? 0 : (int64_t)sg.s.c.b * a.ldt);
+                const AttnTiles &t = sg.s.c.t;
+                auto page_of = [&](int i) { return lane < nbox ? attn_box_page(a, t, row, attn_tile_at(t, sg.s.c.tile + i) * AT_BN + lane * box, box) : a.pages; };      // (a lane a box)
                 int page = page_of(0);
                 for (int i = 0; i < sg.n; ++i, ++filled) {
-                    const int st = filled % ST, j0 = attn_tile_at(t, sg.tile0 + i) * AT_BN, ahead = i + 1 < sg.n ? page_of(i + 1) : 0;
+                    const int st = filled % ST, j0 = attn_tile_at(t, sg.s.c.tile + i) * AT_BN, ahead = i + 1 < sg.n ? page_of(i + 1) : 0;
                     // Places of a page whose keys no row sees: whatever they hold, a weight of 0 times it has to be 0, so the values
                     // there are overwritten with zeros before the product reads them.
                     const bool patch = values && ((j0 + AT_BN > t.end && (t.end & (box - 1))) || (j0 < a.kv0 && j0 + AT_BN > a.kv0 && (a.kv0 & (box - 1))) ||
@@ -266,6 +257,44 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                     page = ahead;
                 }
             }
+        } else if (warp == AT_Q_WARP) {
+            int queries[2] = {0, 0};
+            for (; ok && sg.get(); sg.done(a)) {
+                const int kvh = sg.s.c.hu / a.chunks;
+                                // the item's queries, as soon as the products of the one before it have read theirs: the rows of a tile are the
+                                // group's heads of consecutive tokens, one box (rows past the sequence's end, whatever they hold, are not stored)
+                                for (int i = 0; ok && i < (sg.two(a) ? 2 : 1); ++i) {
+                                    if (queries[i]++) ok = attn_wait(smem_u32(&bars.q_empty[i]), (uint32_t)queries[i] & 1u, &abort_flag);
+                                    if (!ok) break;
+                                    const int per = a.tpt / 2, g0 = (sg.s.c.hu - kvh * a.chunks) * a.gc;
+                                    const uint32_t dst = s_q + (uint32_t)i * PART, bar = smem_u32(&bars.q_full[i]);
+                                    if (a.q_direct) {
+                                        if (lane == 0) {
+                                            mbar_expect_tx(bar, (uint32_t)(DP / 64 * a.gc * per) * 128u);
+                #pragma unroll
+                                            for (int p = 0; p < DP / 64; ++p)
+                                                tma_load_3d(dst + (uint32_t)p * AT_PANEL, &tmQ, p * 64, kvh * a.G + g0, sg.s.c.q.s + sg.s.c.rt * a.tpt + i * per, bar);
+                                        }
+                                    } else {
+                                        for (int r = lane; r < a.gc * per; r += 32) {
+                                            const int2 at = attn_row_at(a, sg.s.c.q.s + sg.s.c.rt * a.tpt, sg.s.c.q.n - sg.s.c.rt * a.tpt, sg.s.c.hu, i * AT_TILE + r);
+                                            const uint16_t *q = static_cast<const uint16_t *>(a.q) + (at.x < 0 ? 0 : at.x * a.q_ts + at.y * a.q_hs);
+                #pragma unroll 1
+                                            for (int c = 0; c < 2 * NK; ++c) {
+                                                uint4 v = make_uint4(0, 0, 0, 0);
+                                                if (at.x >= 0 && c * 8 < a.D) {
+                                                    const uint16_t *h = q + c * 8;
+                                                    v = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16);
+                                                }
+                                                *reinterpret_cast<uint4 *>(smem + (uint32_t)i * PART + (uint32_t)(c / 8) * AT_PANEL + (uint32_t)r * 128u + (uint32_t)(((c & 7) ^ (r & 7)) << 4)) = v;
+                                            }
+                                        }
+                                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                                        __syncwarp();
+                                        if (lane == 0) mbar_arrive(bar);
+                                    }
+                                }
+            }
         } else if (warp == AT_MMA_WARP) {
         constexpr uint32_t fmt = std::is_same_v<T, __nv_bfloat16> ? 1 : 0;
         const uint32_t id_s = at_idesc(AT_BN, fmt, 0), id_o = at_idesc(NK * 16, fmt, 1);
@@ -297,6 +326,7 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                 q_phase[i] ^= 1u;
                 tmem_after();
                 scores(i);
+                if (sg.n == 1) commit_one(smem_u32(&bars.q_empty[i]));
             }
             if (!ok) break;
             next_keys();
@@ -322,6 +352,7 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                         if (i == 0) wait(bars.k_full[ks], k_phase);
                         if (!ok) break;
                         scores(i);
+                        if (j + 2 == sg.n) commit_one(smem_u32(&bars.q_empty[i]));
                     }
                 }
                 if (!ok) break;
@@ -341,42 +372,23 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
         AttnRow row{-1, 0, 0, 0};
         float m = 0.f, l = 0.f;
         int64_t slot = 0;
-        bool before = false, complete = false;               // an item whose outcome is not stored yet
+        bool before = false, complete = false, described = false;               // before: an item whose outcome is not stored yet
         while (ok) {
             const int token = row.token, head = row.head;
             while (sg.get() && tile == 1 && !sg.two(a)) sg.done(a);
-            const bool live = sg.left > 0;
-            if (live) {                                       // the next item's queries
-                row = attn_row(a, sg.cur.q, sg.cur.hu, sg.cur.rt, tile * AT_TILE + r);
-                const T *p = static_cast<const T *>(a.q) + (row.token < 0 ? 0 : row.token * a.q_ts + row.head * a.q_hs);
-                auto put = [&](int c, const uint4 &v) {
-                    *reinterpret_cast<uint4 *>(smem + (uint32_t)tile * PART + (uint32_t)(c / 8) * AT_PANEL + (uint32_t)r * 128u + (uint32_t)(((c & 7) ^ (r & 7)) << 4)) = v;
-                };
-                if (row.token < 0 || (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
-                    uint4 v[2 * NK];
-#pragma unroll
-                    for (int c = 0; c < 2 * NK; ++c) v[c] = row.token >= 0 && c * 8 < a.D ? *reinterpret_cast<const uint4 *>(p + c * 8) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-                    for (int c = 0; c < 2 * NK; ++c) put(c, v[c]);
-                } else {
-#pragma unroll 1
-                    for (int c = 0; c < 2 * NK; ++c) {
-                        const uint16_t *h = reinterpret_cast<const uint16_t *>(p + c * 8);
-                        put(c, c * 8 < a.D ? make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16)
-                                           : make_uint4(0, 0, 0, 0));
-                    }
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                tmem_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&bars.q_full[tile]));
-            }
+            const bool live = sg.s.left > 0;
+            if (live) row = attn_row(a, sg.s.c.q, sg.s.c.hu, sg.s.c.rt, tile * AT_TILE + r);
             if (before) {
                 ok = attn_wait(smem_u32(&bars.o_full[tile]), o_phase, &abort_flag);
                 if (!ok) break;
                 o_phase ^= 1u;
                 tmem_after();
-                if (complete && a.pml) {                      // (with a shared prefix's sums: rare here, a thread a row)
+                const int64_t at = slot * a.rows + tile * AT_TILE + r;
+                uint8_t *const dst = complete ? reinterpret_cast<uint8_t *>(static_cast<T *>(a.out) + (token < 0 ? 0 : token * a.o_ts + head * a.o_hs))
+                                              : reinterpret_cast<uint8_t *>(a.po + at * a.D);
+                if (!complete && token >= 0) a.ml[at] = make_float2(m, l);
+                if (complete && (a.pml || __any_sync(0xffffffffu, token >= 0 && (reinterpret_cast<uintptr_t>(dst) & 15) != 0))) {
+                    // with a shared prefix's sums, or outputs off 16 bytes: a thread a row
 #pragma unroll 1
                     for (int d = 0; d < a.D; d += 8) {
                         uint32_t o[8];
@@ -390,46 +402,49 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                 } else {
                     // 128 bytes of each row at a time, turned in shared memory so that eight lanes store a row's (a thread a row: 32 lines a
                     // store, 5300 cycles an item)
-                    const int64_t at = slot * a.rows + tile * AT_TILE + r;
-                    if (!complete && token >= 0) a.ml[at] = make_float2(m, l);
-                    const float scale = complete ? (l == 0.f ? 0.f : 1.f / l) : 1.f;
-                    const int per = complete ? 64 : 32;       // values of 128 bytes
-                    uint8_t *const dst = complete ? reinterpret_cast<uint8_t *>(static_cast<T *>(a.out) + (token < 0 ? 0 : token * a.o_ts + head * a.o_hs))
-                                                  : reinterpret_cast<uint8_t *>(a.po + at * a.D);
-                    const int how = token < 0 ? 0 : (reinterpret_cast<uintptr_t>(dst) & 15) != 0 ? 2 : 1;        // (any alignment of the output)
-#pragma unroll 1
-                    for (int d = 0; d < a.D; d += per) {
-#pragma unroll 1
-                        for (int h = 0; h < per && d + h < a.D; h += 16) {
-                            uint32_t o[16];
-                            tmem_ld16(t_o + (uint32_t)(d + h), o);
-                            tmem_wait_ld();
-                            if (complete) {
+                    uint8_t *to[8];
+                    uint32_t there = 0;
 #pragma unroll
-                                for (int e = 0; e < 8; ++e) o[e] = pack2<T>(__uint_as_float(o[2 * e]) * scale, __uint_as_float(o[2 * e + 1]) * scale);
-                            }
-                            const int at0 = complete ? h / 8 : h / 4;
+                    for (int i = 0; i < 8; ++i) {
+                        to[i] = reinterpret_cast<uint8_t *>(__shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(dst), i * 4 + (lane >> 3))) + (lane & 7) * 16;
+                        there |= (uint32_t)(__shfl_sync(0xffffffffu, token, i * 4 + (lane >> 3)) >= 0) << i;
+                    }
+                    auto store = [&](const uint32_t (&w)[32], int at_byte, int bytes) {
 #pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                if (e < 2 || !complete)
-                                    *reinterpret_cast<uint4 *>(turn + lane * 128 + (((at0 + e) ^ (lane & 7)) << 4)) = make_uint4(o[4 * e], o[4 * e + 1], o[4 * e + 2], o[4 * e + 3]);
-                        }
+                        for (int e = 0; e < 8; ++e)
+                            *reinterpret_cast<uint4 *>(turn + lane * 128 + ((e ^ (lane & 7)) << 4)) = make_uint4(w[4 * e], w[4 * e + 1], w[4 * e + 2], w[4 * e + 3]);
                         __syncwarp();
-                        const int ch = lane & 7, col = d + ch * (per / 8);
-#pragma unroll 4
+                        uint4 v[8];
+#pragma unroll
                         for (int i = 0; i < 8; ++i) {
                             const int from = i * 4 + (lane >> 3);
-                            const uint4 v = *reinterpret_cast<const uint4 *>(turn + from * 128 + ((ch ^ (from & 7)) << 4));
-                            uint8_t *const to = reinterpret_cast<uint8_t *>(__shfl_sync(0xffffffffu, reinterpret_cast<uint64_t>(dst), from)) + d * 128 / per + ch * 16;
-                            const int kind = __shfl_sync(0xffffffffu, how, from);
-                            if (col < a.D && kind == 1) *reinterpret_cast<uint4 *>(to) = v;
-                            else if (col < a.D && kind == 2) {
-                                uint16_t *const q = reinterpret_cast<uint16_t *>(to);
-                                q[0] = (uint16_t)v.x; q[1] = (uint16_t)(v.x >> 16); q[2] = (uint16_t)v.y; q[3] = (uint16_t)(v.y >> 16);
-                                q[4] = (uint16_t)v.z; q[5] = (uint16_t)(v.z >> 16); q[6] = (uint16_t)v.w; q[7] = (uint16_t)(v.w >> 16);
-                            }
+                            v[i] = *reinterpret_cast<const uint4 *>(turn + from * 128 + (((lane & 7) ^ (from & 7)) << 4));
                         }
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            if ((there >> i & 1) && (lane & 7) * 16 < bytes) *reinterpret_cast<uint4 *>(to[i] + at_byte) = v[i];
                         __syncwarp();
+                    };
+                    uint32_t o[2][32], w[32];
+                    if (complete) {
+                        const float scale = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll 1
+                        for (int d = 0; d < a.D; d += 64) {
+                            tmem_ld32(t_o + (uint32_t)d, o[0]);
+                            tmem_ld32(t_o + (uint32_t)d + 32u, o[1]);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int e = 0; e < 32; ++e)
+                                w[e] = pack2<T>(__uint_as_float(o[e / 16][2 * e & 31]) * scale, __uint_as_float(o[e / 16][(2 * e & 31) + 1]) * scale);
+                            store(w, d * 2, (a.D - d) * 2);
+                        }
+                    } else {
+#pragma unroll 1
+                        for (int d = 0; d < a.D; d += 32) {
+                            tmem_ld32(t_o + (uint32_t)d, o[0]);
+                            tmem_wait_ld();
+                            store(o[0], d * 4, (a.D - d) * 4);
+                        }
                     }
                 }
             }
@@ -438,7 +453,7 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
             const int all_hi = __reduce_min_sync(0xffffffffu, row.token >= 0 ? row.hi : INT_MAX), all_lo = __reduce_max_sync(0xffffffffu, row.token >= 0 ? row.lo : 0);
             m = -INFINITY; l = 0.f;
             for (int j = 0; j < sg.n; ++j) {
-                const int j0 = attn_tile_at(sg.cur.t, sg.tile0 + j) * AT_BN;
+                const int j0 = attn_tile_at(sg.s.c.t, sg.s.c.tile + j) * AT_BN;
                 ok = attn_wait(smem_u32(&bars.s_full[tile]), s_phase, &abort_flag);
                 if (!ok) break;
                 s_phase ^= 1u;
@@ -511,14 +526,15 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                 l += (sums[0] + sums[1]) + (sums[2] + sums[3]);
             }
             if (!ok) break;
-            // the item's outcome is on its way to tensor memory; the next item's queries go first
-            const int c = (int)blockIdx.x;
+            // the item's outcome is on its way to tensor memory
+            const int c = (int)blockIdx.x, x = deal.count(c) - sg.s.left;
             before = true;
-            complete = sg.n == sg.cur.t.nt && !a.common;
-            slot = a.common ? ((int64_t)sg.cur.hu * attn_row_blocks(a, sg.cur.q) + sg.cur.rt) + c : 2 * (int64_t)c + (sg.left < count ? 1 : 0);
-            if (warp == AT_SOFT_WARP && lane == 0 && !a.common && sg.left == sg.n) attn_describe(a, sg.cur, deal, c, count - sg.n, sg.tile0, sg.n);
+            complete = sg.n == sg.s.c.t.nt && !a.common;
+            slot = a.common ? ((int64_t)sg.s.c.hu * attn_row_blocks(a, sg.s.c.q) + sg.s.c.rt) + c : 2 * (int64_t)c + (x > 0 ? 1 : 0);
+            if (warp == AT_SOFT_WARP && lane == 0 && !a.common && sg.s.c.tile == 0 && !complete) { attn_describe(a, sg.s.c, deal, c, x, 0, sg.n); described = true; }
             sg.done(a);
         }
+        if (warp == AT_SOFT_WARP && lane == 0 && !a.common && !described) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
     }
     if (!ok && lane == 0) atomicExch(a.status, 1);
     tmem_before();
@@ -526,6 +542,9 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
     if (*(volatile int *)&abort_flag) {
         // a block whose waits ran out leaves no copy and no product under way (a millisecond at most each)
         int gave_up = 0;
+        if (warp == AT_Q_WARP) {
+            for (int f = 0; f < 4; ++f) attn_wait(smem_u32(&bars.q_full[f >> 1]), (uint32_t)f & 1u, &gave_up, 1);
+        }
         if (warp == AT_K_WARP || warp == AT_V_WARP) {
             for (int f = filled > ST ? filled - ST : 0; f <= filled; ++f) {
                 attn_wait(smem_u32(warp == AT_V_WARP ? &bars.v_full[f % ST] : &bars.k_full[f % ST]), (uint32_t)(f / ST) & 1u, &gave_up, 1);
@@ -580,16 +599,30 @@ int attn_encode_cache(CUtensorMap *tm, const AttnArgs &a, const void *base, int 
 
 namespace {
 
-template <typename T> int launch_tc_t(const CUtensorMap &k, const CUtensorMap &v, const AttnArgs &a, int grid, void *stream)
+// (head values, heads, tokens): boxes of 64 values x the heads of a unit head x the tokens of a tile
+int encode_queries(CUtensorMap *tm, const AttnArgs &a, int dtype)
+{
+    const EncodeTiledFn enc = encoder();
+    if (!enc) return UBP_E_CUDA;
+    const cuuint64_t dims[3] = {(cuuint64_t)a.D, (cuuint64_t)a.Hq, (cuuint64_t)a.T};
+    const cuuint64_t unit = (cuuint64_t)a.D * 2, strides[2] = {a.Hq > 1 ? (cuuint64_t)a.q_hs * 2 : unit, a.T > 1 ? (cuuint64_t)a.q_ts * 2 : unit * a.Hq};
+    const cuuint32_t box[3] = {64, (cuuint32_t)a.gc, (cuuint32_t)(a.tpt / 2)}, one[3] = {1, 1, 1};
+    const CUresult r = enc(tm, dtype == UBP_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void *>(a.q), dims, strides, box, one,
+                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) { set_last_cuda_error((int)cudaErrorInvalidValue); return UBP_E_CUDA; }
+    return UBP_OK;
+}
+
+template <typename T> int launch_tc_t(const CUtensorMap &k, const CUtensorMap &v, const CUtensorMap &q, const AttnArgs &a, int grid, void *stream)
 {
     static std::atomic<bool> done[5][64] = {};
     const dim3 g((unsigned)grid);
     switch (a.D <= 64 ? 4 : (a.D + 15) / 16) {
-        case 4: return attn_launch(ubp_attention_tc_kernel<T, 4>, done[0], g, AT_THREADS, at_smem(64), stream, k, v, a);
-        case 5: return attn_launch(ubp_attention_tc_kernel<T, 5>, done[1], g, AT_THREADS, at_smem(128), stream, k, v, a);
-        case 6: return attn_launch(ubp_attention_tc_kernel<T, 6>, done[2], g, AT_THREADS, at_smem(128), stream, k, v, a);
-        case 7: return attn_launch(ubp_attention_tc_kernel<T, 7>, done[3], g, AT_THREADS, at_smem(128), stream, k, v, a);
-        default: return attn_launch(ubp_attention_tc_kernel<T, 8>, done[4], g, AT_THREADS, at_smem(128), stream, k, v, a);
+        case 4: return attn_launch(ubp_attention_tc_kernel<T, 4>, done[0], g, AT_THREADS, at_smem(64), stream, k, v, q, a);
+        case 5: return attn_launch(ubp_attention_tc_kernel<T, 5>, done[1], g, AT_THREADS, at_smem(128), stream, k, v, q, a);
+        case 6: return attn_launch(ubp_attention_tc_kernel<T, 6>, done[2], g, AT_THREADS, at_smem(128), stream, k, v, q, a);
+        case 7: return attn_launch(ubp_attention_tc_kernel<T, 7>, done[3], g, AT_THREADS, at_smem(128), stream, k, v, q, a);
+        default: return attn_launch(ubp_attention_tc_kernel<T, 8>, done[4], g, AT_THREADS, at_smem(128), stream, k, v, q, a);
     }
 }
 
@@ -597,10 +630,15 @@ template <typename T> int launch_tc_t(const CUtensorMap &k, const CUtensorMap &v
 
 int launch_attn_tc(const AttnArgs &a, int dtype, int grid, void *stream)
 {
-    CUtensorMap k, v;
+    CUtensorMap k, v, q;
     if (const int rc = attn_encode_cache(&k, a, a.k, dtype, AT_BN)) return rc;
     if (const int rc = attn_encode_cache(&v, a, a.v, dtype, AT_BN)) return rc;
-    return dtype == UBP_BF16 ? launch_tc_t<__nv_bfloat16>(k, v, a, grid, stream) : launch_tc_t<__half>(k, v, a, grid, stream);
+    AttnArgs b = a;
+    b.q_direct = (reinterpret_cast<uintptr_t>(a.q) & 15) == 0 && (a.T == 1 || a.q_ts % 8 == 0) && (a.Hq == 1 || a.q_hs % 8 == 0);
+    if (b.q_direct) {
+        if (const int rc = encode_queries(&q, a, dtype)) return rc;
+    } else q = k;
+    return dtype == UBP_BF16 ? launch_tc_t<__nv_bfloat16>(k, v, q, b, grid, stream) : launch_tc_t<__half>(k, v, q, b, grid, stream);
 }
 
 }  // namespace ubp
