@@ -27,8 +27,6 @@
 
 namespace ubp {
 
-constexpr int ATTN_BN = 128;        // keys a step takes
-
 struct AttnArgs {
     const void *q;
     int64_t q_ts, q_hs;             // strides of q between tokens and heads (elements)
@@ -46,6 +44,7 @@ struct AttnArgs {
     int tiles;                      // row tiles of a row block (each rows / tiles rows)
     int gc, chunks, HU;             // heads of a unit head, unit heads of a key head, unit heads in all
     int tpt;                        // tokens a row block takes
+    int bsh;                        // keys a step takes: 1 << bsh
     int extra;                      // steps that an item counts for beside its tiles
     int q_direct;                   // queries can be copied as they are (16-byte aligned)
     float sc;                       // scale * log2(e)
@@ -86,21 +85,21 @@ UBP_HD AttnSeq attn_seq(const AttnArgs &a, int b)
     return q;
 }
 
-// The tiles of bn keys that a row block with positions p0 .. p1 visits: ns from s0 on (first tokens), the rest from lo on.
+// The tiles of keys that a row block with positions p0 .. p1 visits: ns from s0 on (first tokens), the rest from lo on.
 // Keys below w0 are seen by none of the rows unless they are among the first `sinks`, keys from `end` on by none.
 struct AttnTiles { int s0, ns, lo, nt, w0, end; };
 UBP_HD AttnTiles attn_tiles(const AttnArgs &a, int p0, int p1)
 {
     AttnTiles t;
+    const int up = (1 << a.bsh) - 1;
     t.end = imin(p1 + 1, a.kv1);
     t.w0 = a.window > 0 && !a.common ? imax(a.kv0, p0 - a.window + 1) : a.kv0;
-    t.s0 = a.kv0 / ATTN_BN;
-    t.lo = t.w0 / ATTN_BN;
+    t.s0 = a.kv0 >> a.bsh;
+    t.lo = t.w0 >> a.bsh;
     t.ns = 0;
     if (t.end <= a.kv0) { t.end = a.kv0; t.lo = t.s0; t.nt = 1; return t; }
-    if (t.lo > t.s0 && a.sinks > a.kv0) t.ns = imin((imin(a.sinks, t.end) + ATTN_BN - 1) / ATTN_BN - t.s0, t.lo - t.s0);
-    t.nt = t.ns + imax(0, (t.end + ATTN_BN - 1) / ATTN_BN - t.lo);
-    if (t.nt < 1) t.nt = 1;
+    if (t.lo > t.s0 && a.sinks > a.kv0) t.ns = imin(((imin(a.sinks, t.end) + up) >> a.bsh) - t.s0, t.lo - t.s0);
+    t.nt = imax(1, t.ns + imax(0, ((t.end + up) >> a.bsh) - t.lo));
     return t;
 }
 UBP_HD int attn_tile_at(const AttnTiles &t, int i) { return i < t.ns ? t.s0 + i : t.lo + i - t.ns; }

@@ -6,8 +6,8 @@
 // of an item are the query heads of one key head (and neighbouring tokens), so that a key is read once for all of them, and they
 // are the rows of an m16n8k16 product: at 16 rows it is 16 multiply-adds a value read, a tenth of what the SM could do in the time
 // HBM takes for that value, so the unused rows of small groups cost nothing.
-// Eight warps a block; a warp has its own 16 keys of a step's 128, its own ring of copies and its own running sums: nothing in the
-// loop waits for another warp. They meet once an item. Copies are TMA boxes of 64 values x 16 keys (8 where pages are smaller),
+// Eight warps a block; a warp has its own 16 keys of a step's 128 (heads of up to 64 values: 32 of 256), its own ring of copies and its own running sums: nothing in the
+// loop waits for another warp. They meet once an item. Copies are TMA boxes of 64 values x those keys (fewer where pages are smaller),
 // which run ahead over the ends of items: with 16-byte cp.async, whose addresses every lane computed, a step took 930 instructions
 // and the kernel ran at 45 % of HBM.
 // Pages that no row of the item sees, or that the cache does not have, are out of range for the copy and come as zeros; values of
@@ -28,14 +28,11 @@ namespace {
 
 using namespace tc;
 
-constexpr int FEW_WARPS = 8, FEW_KEYS = 16, FEW_ROWS = 16;
-constexpr int FEW_BN = FEW_WARPS * FEW_KEYS;
-static_assert(FEW_BN == ATTN_BN, "");
-constexpr uint32_t FEW_PANEL = FEW_KEYS * 128;                  // 64 values of each of a warp's keys
-__host__ __device__ constexpr int few_stages(int dp) { return dp == 128 ? 3 : 6; }
-__host__ __device__ constexpr uint32_t few_part(int dp) { return (uint32_t)(dp / 64) * FEW_PANEL; }            // keys (or values) of a warp's step
-__host__ __device__ constexpr uint32_t few_ring(int dp) { return (uint32_t)few_stages(dp) * 2 * few_part(dp); }  // a warp's
-__host__ __device__ constexpr uint32_t few_smem(int dp) { return FEW_WARPS * (few_ring(dp) + 8 * (uint32_t)dp * 4 + FEW_ROWS * 8) + 1024; }
+constexpr int FEW_WARPS = 8, FEW_ROWS = 16, FEW_STAGES = 3;
+__host__ __device__ constexpr int few_keys(int dp) { return dp == 128 ? 16 : 32; }                        // a warp's of a step: 4 KB of keys, 4 KB of values
+constexpr uint32_t FEW_PART = 4096;
+constexpr uint32_t FEW_RING = FEW_STAGES * 2 * FEW_PART;                                                    // a warp's
+__host__ __device__ constexpr uint32_t few_smem(int dp) { return FEW_WARPS * (FEW_RING + 8 * (uint32_t)dp * 4 + FEW_ROWS * 8) + 1024; }
 static_assert(few_smem(128) <= 227 * 1024 - 1024, "with the static part");
 
 __device__ __forceinline__ void ldsm4(uint32_t (&r)[4], uint32_t at)
@@ -58,11 +55,11 @@ template <typename T> __device__ __forceinline__ void mma16(float (&c)[4], const
 // two neighbouring 16-bit values off their alignment
 __device__ __forceinline__ uint32_t load_pair(const uint16_t *p) { return (uint32_t)p[0] | (uint32_t)p[1] << 16; }
 
-// The copies of a warp's steps: a cursor that runs ahead, with the pages of the next step already loaded (one, or two of eight keys).
+// The copies of a warp's steps: a cursor that runs ahead, with the pages of the next step already loaded.
 // Everything is the same in all lanes; lane 0 issues.
 template <int DP> struct FewCopies {
     AttnSteps s;
-    int page[2], j0, kvh;
+    int page[few_keys(DP) / 8], j0, kvh;
     const int32_t *row;
 
     __device__ __forceinline__ void item(const AttnArgs &a)
@@ -72,28 +69,31 @@ template <int DP> struct FewCopies {
     }
     __device__ __forceinline__ void peek(const AttnArgs &a, int warp)
     {
-        j0 = attn_tile_at(s.c.t, s.c.tile) * FEW_BN + warp * FEW_KEYS;
-        page[0] = attn_box_page(a, s.c.t, row, j0, imin(1 << a.pshift, FEW_KEYS));
-        if (a.pshift == 3) page[1] = attn_box_page(a, s.c.t, row, j0 + 8, 8);
+        constexpr int KEYS = few_keys(DP);
+        j0 = attn_tile_at(s.c.t, s.c.tile) * (FEW_WARPS * KEYS) + warp * KEYS;
+        const int box = imin(1 << a.pshift, KEYS);
+#pragma unroll
+        for (int b = 0; b < KEYS / 8; ++b)
+            if (b * box < KEYS) page[b] = attn_box_page(a, s.c.t, row, j0 + b * box, box);
     }
     __device__ __forceinline__ void issue(const AttnArgs &a, const CUtensorMap *tmK, const CUtensorMap *tmV, uint32_t stage, uint32_t bar, int warp, int lane)
     {
+        constexpr int KEYS = few_keys(DP);
         if (s.left <= 0) return;
         if (lane == 0) {
-            const int at = j0 & ((1 << a.pshift) - 1);
-            mbar_expect_tx(bar, 2 * few_part(DP));
+            const int box = imin(1 << a.pshift, KEYS);
+            mbar_expect_tx(bar, 2 * FEW_PART);
 #pragma unroll
-            for (int p = 0; p < DP / 64; ++p) {
-                tma_load_4d(stage + (uint32_t)p * FEW_PANEL, tmK, p * 64, at, kvh, page[0], bar);
-                tma_load_4d(stage + few_part(DP) + (uint32_t)p * FEW_PANEL, tmV, p * 64, at, kvh, page[0], bar);
-            }
-            if (a.pshift == 3) {
+            for (int b = 0; b < KEYS / 8; ++b)
+                if (b * box < KEYS) {
+                    const int at = (j0 + b * box) & ((1 << a.pshift) - 1);
 #pragma unroll
-                for (int p = 0; p < DP / 64; ++p) {
-                    tma_load_4d(stage + (uint32_t)p * FEW_PANEL + 1024u, tmK, p * 64, 0, kvh, page[1], bar);
-                    tma_load_4d(stage + few_part(DP) + (uint32_t)p * FEW_PANEL + 1024u, tmV, p * 64, 0, kvh, page[1], bar);
+                    for (int p = 0; p < DP / 64; ++p) {
+                        const uint32_t to = stage + (uint32_t)(p * KEYS + b * box) * 128u;
+                        tma_load_4d(to, tmK, p * 64, at, kvh, page[b], bar);
+                        tma_load_4d(to + FEW_PART, tmV, p * 64, at, kvh, page[b], bar);
+                    }
                 }
-            }
         }
         const bool over = s.c.tile + 1 == s.c.t.nt;
         s.advance(a, 1);
@@ -108,17 +108,17 @@ template <typename T, int NK>
 __global__ void __launch_bounds__(FEW_WARPS * 32, 1)
 ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const AttnArgs a)
 {
-    constexpr int DP = NK > 4 ? 128 : 64, ST = few_stages(DP);
-    constexpr uint32_t PART = few_part(DP);
+    constexpr int DP = NK > 4 ? 128 : 64, ST = FEW_STAGES, KEYS = few_keys(DP), NB = KEYS / 8;
+    constexpr uint32_t PART = FEW_PART, PANEL = KEYS * 128;        // 64 values of each of a warp's keys
     extern __shared__ __align__(1024) uint8_t smem_raw[];
     uint8_t *const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
     __shared__ __align__(8) uint64_t bar_full[FEW_WARPS][ST];
-    __shared__ int2 rows[FEW_ROWS];         // token and head of the item's rows
+    __shared__ int2 rows[2][FEW_ROWS];      // token and head of the rows of an item, and of the next one
     __shared__ int abort_flag;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, tq = lane & 3;
-    float *const meet = reinterpret_cast<float *>(smem + FEW_WARPS * few_ring(DP));                  // [warp][8 rows][DP]
+    float *const meet = reinterpret_cast<float *>(smem + FEW_WARPS * FEW_RING);                      // [warp][8 rows][DP]
     float2 *const meet_ml = reinterpret_cast<float2 *>(meet + FEW_WARPS * 8 * DP);                    // [warp][row]
-    const uint32_t ring = smem_u32(smem) + (uint32_t)warp * few_ring(DP);
+    const uint32_t ring = smem_u32(smem) + (uint32_t)warp * FEW_RING;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (lane == 0) {
         if (warp == 0) { prefetch_tensormap(&tmK); prefetch_tensormap(&tmV); abort_flag = 0; }
@@ -136,11 +136,37 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
         if (threadIdx.x == 0 && !a.common) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
         return;
     }
+    const AttnCursor &cur = steps.c;
+    uint32_t qf[NK][4];
+    AttnRow row[2];                         // (their keys; tokens and heads are in `rows`)
+    int all_lo = 0, all_hi = 0, which = 0;  // keys that all rows see; the item's place in `rows`
+    // an item's rows and queries; under way while the item before it ends
+    auto begin = [&](const AttnCursor &c) {
+        const AttnRow w = attn_row(a, c.q, c.hu, c.rt, lane & 15);
+        if (warp == 0 && lane < 16) rows[which][lane] = make_int2(w.token, w.head);
+        all_lo = __reduce_max_sync(0xffffffffu, w.token >= 0 ? w.lo : 0);
+        all_hi = __reduce_min_sync(0xffffffffu, w.token >= 0 ? w.hi : INT_MAX);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int token = __shfl_sync(0xffffffffu, w.token, g + 8 * i), head = __shfl_sync(0xffffffffu, w.head, g + 8 * i);
+            row[i].lo = __shfl_sync(0xffffffffu, w.lo, g + 8 * i);
+            row[i].hi = __shfl_sync(0xffffffffu, w.hi, g + 8 * i);
+            const T *p = static_cast<const T *>(a.q) + (token < 0 ? 0 : token * a.q_ts + head * a.q_hs) + tq * 2;
+            if ((reinterpret_cast<uintptr_t>(p) & 3) == 0) {
+#pragma unroll
+                for (int k = 0; k < 2 * NK; ++k) qf[k / 2][k % 2 * 2 + i] = token >= 0 && k * 8 < a.D ? *reinterpret_cast<const uint32_t *>(p + k * 8) : 0u;
+            } else {
+#pragma unroll
+                for (int k = 0; k < 2 * NK; ++k)
+                    qf[k / 2][k % 2 * 2 + i] = token >= 0 && k * 8 < a.D ? load_pair(reinterpret_cast<const uint16_t *>(p + k * 8)) : 0u;
+            }
+        }
+    };
+    if (steps.left > 0) begin(cur);
     FewCopies<DP> copies;
     copies.s = steps;
     copies.item(a);
     if (steps.left > 0) copies.peek(a, warp);
-    const AttnCursor &cur = steps.c;
     for (int s = 0; s < ST - 1; ++s) copies.issue(a, &tmK, &tmV, ring + (uint32_t)s * 2 * PART, smem_u32(&bar_full[warp][s]), warp, lane);
 
     // where the lane's rows of matrix instructions' operands lie in a part: piece (2 k + h) of 16 bytes at k * 32 (within 128 bytes)
@@ -149,79 +175,57 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     const uint32_t at_k = (uint32_t)(rk * 128), xk = (uint32_t)(((lane >> 3 & 1) ^ (rk & 7)) << 4);
     const uint32_t at_v = PART + (uint32_t)(rv * 128), xv = (uint32_t)(((lane >> 4) ^ (rv & 7)) << 4);
 
-    uint32_t qf[NK][4];
-    float o[2 * NK][4], m[2], l[2];
-    AttnRow row[2];
-    int tile0 = 0, before = 0, st = 0, all_lo = 0, all_hi = 0;      // of the segment: its first tile, the share's steps before it
+    float o[2 * NK][4] = {}, m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+    int tile0 = cur.tile, before = 0, st = 0;      // of the segment: its first tile, the share's steps before it
     uint32_t phase = 0;
-    bool fresh = true, ok = true;
-    bool described = false;
+    bool ok = true, described = false;
+    before = deal.count((int)blockIdx.x) - steps.left;
     while (steps.left > 0) {
         __syncwarp();                       // (all lanes have read the stage that is copied to now)
         const int nx = st == 0 ? ST - 1 : st - 1;
         copies.issue(a, &tmK, &tmV, ring + (uint32_t)nx * 2 * PART, smem_u32(&bar_full[warp][nx]), warp, lane);
-        if (fresh) {
-            fresh = false;
-            tile0 = cur.tile;
-            before = deal.count((int)blockIdx.x) - steps.left;
-            const AttnRow w = attn_row(a, cur.q, cur.hu, cur.rt, lane & 15);
-            if (warp == 0 && lane < 16) rows[lane] = make_int2(w.token, w.head);
-            all_lo = w.token >= 0 ? w.lo : 0;
-            all_hi = w.token >= 0 ? w.hi : INT_MAX;
-#pragma unroll
-            for (int s = 1; s < 16; s <<= 1) {
-                all_lo = imax(all_lo, __shfl_xor_sync(0xffffffffu, all_lo, s));
-                all_hi = imin(all_hi, __shfl_xor_sync(0xffffffffu, all_hi, s));
-            }
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int token = __shfl_sync(0xffffffffu, w.token, g + 8 * i), head = __shfl_sync(0xffffffffu, w.head, g + 8 * i);
-                row[i].lo = __shfl_sync(0xffffffffu, w.lo, g + 8 * i);
-                row[i].hi = __shfl_sync(0xffffffffu, w.hi, g + 8 * i);
-                m[i] = -INFINITY; l[i] = 0.f;
-                const T *p = static_cast<const T *>(a.q) + (token < 0 ? 0 : token * a.q_ts + head * a.q_hs) + tq * 2;
-                if ((reinterpret_cast<uintptr_t>(p) & 3) == 0) {
-#pragma unroll
-                    for (int k = 0; k < 2 * NK; ++k) qf[k / 2][k % 2 * 2 + i] = token >= 0 && k * 8 < a.D ? *reinterpret_cast<const uint32_t *>(p + k * 8) : 0u;
-                } else {
-#pragma unroll
-                    for (int k = 0; k < 2 * NK; ++k)
-                        qf[k / 2][k % 2 * 2 + i] = token >= 0 && k * 8 < a.D ? load_pair(reinterpret_cast<const uint16_t *>(p + k * 8)) : 0u;
-                }
-            }
-#pragma unroll
-            for (int n = 0; n < 2 * NK; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[n][e] = 0.f;
-        }
         if (ok) ok = attn_wait(smem_u32(&bar_full[warp][st]), phase, &abort_flag);
-        const int j0 = attn_tile_at(cur.t, cur.tile) * FEW_BN + warp * FEW_KEYS;
+        const int j0 = attn_tile_at(cur.t, cur.tile) * (FEW_WARPS * KEYS) + warp * KEYS;
         const uint32_t base = ring + (uint32_t)st * 2 * PART;
-        if (ok && j0 < cur.t.end && j0 + FEW_KEYS > a.kv0 && (j0 + FEW_KEYS > cur.t.w0 || j0 < a.sinks)) {
-            float s[2][4] = {}, s1[2][4] = {};          // (two sums each, half as long a chain)
+        if (ok && j0 < cur.t.end && j0 + KEYS > a.kv0 && (j0 + KEYS > cur.t.w0 || j0 < a.sinks)) {
+            float s[NB][4] = {};
+            if constexpr (NB == 2) {
+                float s1[2][4] = {};                        // (two sums each, half as long a chain)
 #pragma unroll
-            for (int k = 0; k < NK; ++k) {
-                uint32_t b[4];
-                ldsm4(b, base + at_k + (uint32_t)(k / 4) * FEW_PANEL + ((uint32_t)(k % 4 * 32) ^ xk));
-                mma16<T>(k & 1 ? s1[0] : s[0], qf[k], b[0], b[1]);
-                mma16<T>(k & 1 ? s1[1] : s[1], qf[k], b[2], b[3]);
-            }
-#pragma unroll
-            for (int n = 0; n < 2; ++n)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) s[n][e] += s1[n][e];
-            const bool all = j0 + FEW_KEYS <= all_hi && j0 >= a.kv0 && (j0 >= all_lo || j0 + FEW_KEYS <= a.sinks);
-            if (!all) {
+                for (int k = 0; k < NK; ++k) {
+                    uint32_t b[4];
+                    ldsm4(b, base + at_k + (uint32_t)(k / 4) * PANEL + ((uint32_t)(k % 4 * 32) ^ xk));
+                    mma16<T>(k & 1 ? s1[0] : s[0], qf[k], b[0], b[1]);
+                    mma16<T>(k & 1 ? s1[1] : s[1], qf[k], b[2], b[3]);
+                }
 #pragma unroll
                 for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) s[n][e] += s1[n][e];
+            } else {
+#pragma unroll
+                for (int k = 0; k < NK; ++k)
+#pragma unroll
+                    for (int n = 0; n < NB; n += 2) {
+                        uint32_t b[4];
+                        ldsm4(b, base + at_k + (uint32_t)(n * 8 * 128) + ((uint32_t)(k % 4 * 32) ^ xk));
+                        mma16<T>(s[n], qf[k], b[0], b[1]);
+                        mma16<T>(s[n + 1], qf[k], b[2], b[3]);
+                    }
+            }
+            const bool all = j0 + KEYS <= all_hi && j0 >= a.kv0 && (j0 >= all_lo || j0 + KEYS <= a.sinks);
+            if (!all) {
+#pragma unroll
+                for (int n = 0; n < NB; ++n)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
                         if (!attn_sees(a, row[e >> 1], j0 + n * 8 + tq * 2 + (e & 1))) s[n][e] = -INFINITY;
                 // values of keys that no row sees
-                for (int x = lane; x < FEW_KEYS * DP / 8; x += 32) {
+#pragma unroll 1
+                for (int x = lane; x < KEYS * DP / 8; x += 32) {
                     const int r = x / (DP / 8), ch = x % (DP / 8), j = j0 + r;
                     if (!(j >= a.kv0 && j < cur.t.end && (j >= cur.t.w0 || j < a.sinks)))
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(base + PART + (uint32_t)(ch / 8) * FEW_PANEL + (uint32_t)(r * 128 + ch % 8 * 16)), "r"(0) : "memory");
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(base + PART + (uint32_t)(ch / 8) * PANEL + (uint32_t)(r * 128 + ch % 8 * 16)), "r"(0) : "memory");
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // (before the next copy to these places)
                 __syncwarp();
@@ -229,7 +233,9 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
             float mx[2];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                mx[i] = fmaxf(fmaxf(s[0][2 * i], s[0][2 * i + 1]), fmaxf(s[1][2 * i], s[1][2 * i + 1]));
+                mx[i] = fmaxf(s[0][2 * i], s[0][2 * i + 1]);
+#pragma unroll
+                for (int n = 1; n < NB; ++n) mx[i] = fmaxf(mx[i], fmaxf(s[n][2 * i], s[n][2 * i + 1]));
                 mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 1));
                 mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 2)) * a.sc;
             }
@@ -244,73 +250,84 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
                     for (int n = 0; n < 2 * NK; ++n) { o[n][2 * i] *= f; o[n][2 * i + 1] *= f; }
                 }
             }
-            uint32_t p[4];
+            uint32_t p[NB / 2][4];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const float ref = m[i] == -INFINITY ? 0.f : m[i];
 #pragma unroll
-                for (int n = 0; n < 2; ++n) {
+                for (int n = 0; n < NB; ++n) {
                     const float p0 = attn_exp2(fmaf(s[n][2 * i], a.sc, -ref)), p1 = attn_exp2(fmaf(s[n][2 * i + 1], a.sc, -ref));
                     l[i] += p0 + p1;
-                    p[n * 2 + i] = pack2<T>(p0, p1);
+                    p[n / 2][n % 2 * 2 + i] = pack2<T>(p0, p1);
                 }
             }
 #pragma unroll
-            for (int n = 0; n < NK; ++n) {
-                uint32_t b[4];
-                ldsm4t(b, base + at_v + (uint32_t)(n / 4) * FEW_PANEL + ((uint32_t)(n % 4 * 32) ^ xv));
-                mma16<T>(o[2 * n], p, b[0], b[1]);
-                mma16<T>(o[2 * n + 1], p, b[2], b[3]);
-            }
+            for (int h = 0; h < NB / 2; ++h)
+#pragma unroll
+                for (int n = 0; n < NK; ++n) {
+                    uint32_t b[4];
+                    ldsm4t(b, base + at_v + (uint32_t)(h * 16 * 128) + (uint32_t)(n / 4) * PANEL + ((uint32_t)(n % 4 * 32) ^ xv));
+                    mma16<T>(o[2 * n], p[h], b[0], b[1]);
+                    mma16<T>(o[2 * n + 1], p[h], b[2], b[3]);
+                }
         }
         if (++st == ST) { st = 0; phase ^= 1u; }
-        if (cur.tile + 1 == cur.t.nt || steps.left == 1) {
-            // ---- the warps' sums meet: rows 0 .. 7, then 8 .. 15 where the item has them
+        if (cur.tile + 1 < cur.t.nt && steps.left > 1) { steps.advance(a, 1); continue; }
+
+        // ---- the segment ends: the warps' sums meet, rows 0 .. 7, then 8 .. 15 where the item has them; meanwhile the next item's
+        // queries are on their way
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
-                l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
-                if (tq == 0) meet_ml[warp * FEW_ROWS + g + 8 * i] = make_float2(m[i], l[i]);
-            }
-            const int nr = imin(imin(a.tpt, cur.q.n - cur.rt * a.tpt) * a.gc, FEW_ROWS), n = cur.tile + 1 - tile0;
-            const bool whole = n == cur.t.nt && !a.common;
-            const int c = (int)blockIdx.x;
-            int64_t slot = 2 * (int64_t)c + (before > 0 ? 1 : 0);
-            if (a.common) slot = (int64_t)cur.hu * attn_row_blocks(a, cur.q) + cur.rt + c;
+        for (int i = 0; i < 2; ++i) {
+            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
+            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
+            if (tq == 0) meet_ml[warp * FEW_ROWS + g + 8 * i] = make_float2(m[i], l[i]);
+        }
+        const int c = (int)blockIdx.x, nr = imin(imin(a.tpt, cur.q.n - cur.rt * a.tpt) * a.gc, FEW_ROWS), n = cur.tile + 1 - tile0, now = which;
+        const bool whole = n == cur.t.nt && !a.common;
+        int64_t slot = 2 * (int64_t)c + (before > 0 ? 1 : 0);
+        if (a.common) slot = (int64_t)cur.hu * attn_row_blocks(a, cur.q) + cur.rt + c;
+        if (threadIdx.x == 0 && !a.common && tile0 == 0 && !whole) { attn_describe(a, cur, deal, c, before, tile0, n); described = true; }
+        steps.advance(a, 1);
+        which ^= 1;
+        if (steps.left > 0) begin(cur);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                if (i * 8 >= nr) break;
-                if (i) __syncthreads();
+        for (int i = 0; i < 2; ++i) {
+            if (i * 8 >= nr) break;
+            if (i) __syncthreads();
 #pragma unroll
-                for (int k = 0; k < 2 * NK; ++k)
-                    *reinterpret_cast<float2 *>(meet + (warp * 8 + g) * DP + k * 8 + tq * 2) = make_float2(o[k][2 * i], o[k][2 * i + 1]);
-                __syncthreads();
-                constexpr int N = 4, TPR = DP / N;          // threads a row
-                for (int x = (int)threadIdx.x; x < 8 * TPR; x += FEW_WARPS * 32) {
-                    const int r = x / TPR, col = x % TPR * N;
-                    const int2 w = rows[i * 8 + r];
-                    if (col < a.D && (w.x >= 0 || !whole)) {
-                        float M = -INFINITY, L = 0.f, v[N] = {};
+            for (int k = 0; k < 2 * NK; ++k)
+                *reinterpret_cast<float2 *>(meet + (warp * 8 + g) * DP + k * 8 + tq * 2) = make_float2(o[k][2 * i], o[k][2 * i + 1]);
+            __syncthreads();
+            constexpr int N = 4, TPR = DP / N;              // threads a row
+            for (int x = (int)threadIdx.x; x < 8 * TPR; x += FEW_WARPS * 32) {
+                const int r = x / TPR, col = x % TPR * N;
+                const int2 w = rows[now][i * 8 + r];
+                if (col < a.D && (w.x >= 0 || !whole)) {
+                    float M = -INFINITY, L = 0.f, v[N] = {}, u[FEW_WARPS][N];
+                    float2 ml[FEW_WARPS];
 #pragma unroll
-                        for (int k = 0; k < FEW_WARPS; ++k) {
-                            const float2 ml = meet_ml[k * FEW_ROWS + i * 8 + r];
-                            float u[N];
-                            attn_load(meet + (k * 8 + r) * DP + col, u);
-                            attn_add(M, L, v, ml.x, ml.y, u);
-                        }
-                        if (whole) attn_finish<T>(a, w.x, w.y, col, M, L, v);
-                        else {
-                            if (col == 0) a.ml[slot * FEW_ROWS + i * 8 + r] = make_float2(M, L);
-                            *reinterpret_cast<float4 *>(a.po + (slot * FEW_ROWS + i * 8 + r) * a.D + col) = make_float4(v[0], v[1], v[2], v[3]);
-                        }
+                    for (int k = 0; k < FEW_WARPS; ++k) {
+                        ml[k] = meet_ml[k * FEW_ROWS + i * 8 + r];
+                        attn_load(meet + (k * 8 + r) * DP + col, u[k]);
+                    }
+                    attn_add_all(M, L, v, ml, u, FEW_WARPS);
+                    if (whole) attn_finish<T>(a, w.x, w.y, col, M, L, v);
+                    else {
+                        if (col == 0) a.ml[slot * FEW_ROWS + i * 8 + r] = make_float2(M, L);
+                        *reinterpret_cast<float4 *>(a.po + (slot * FEW_ROWS + i * 8 + r) * a.D + col) = make_float4(v[0], v[1], v[2], v[3]);
                     }
                 }
             }
-            __syncthreads();
-            if (threadIdx.x == 0 && !a.common && tile0 == 0 && !whole) { attn_describe(a, cur, deal, c, before, tile0, n); described = true; }
-            fresh = true;
         }
-        steps.advance(a, 1);
+        __syncthreads();                                    // (all have read)
+        tile0 = cur.tile;
+        before = deal.count(c) - steps.left;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) { m[i] = -INFINITY; l[i] = 0.f; }
+#pragma unroll
+        for (int k = 0; k < 2 * NK; ++k)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[k][e] = 0.f;
     }
     if (threadIdx.x == 0 && !a.common && !described) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
     if (!ok) {                              // copies that are still under way end before the block does (a millisecond at most each)
@@ -323,15 +340,18 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
 
 // Joins the partial results of an item that several blocks have worked on, in the order of its keys: a warp a row, four values a
 // lane, eight parts under way at a time.
-// COMMON: block (u, i) takes rows 8 i .. of item u of the shared prefix; all of its blocks' results lie in slots u + block, and the
+// COMMON: block (u, i) takes the i-th rows of item u of the shared prefix; all of its blocks' results lie in slots u + block, and the
 // sums go to pml and ppo. Else block (c, i) takes those of the item that begins in block c, if it does not end there.
-constexpr int JOIN_ROWS = 8;
+// Rows a block: 8 for the prefix, whose few items have many parts (32: 64 blocks for a batch of 64, 20 us); 32 otherwise, where an
+// item has two or three (8: 4700 blocks for 148 items of 256 rows, 10 us).
+constexpr int JOIN_WARPS = 8;
+__host__ __device__ constexpr int join_rows(bool common) { return common ? 8 : 32; }
 template <typename T, bool COMMON>
-__global__ void __launch_bounds__(JOIN_ROWS * 32) ubp_attention_join_kernel(const AttnArgs a, const int blocks)
+__global__ void __launch_bounds__(JOIN_WARPS * 32) ubp_attention_join_kernel(const AttnArgs a, const int blocks)
 {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int r = (int)blockIdx.y * JOIN_ROWS + (int)(threadIdx.x >> 5), col = (int)(threadIdx.x & 31) * 4;
+    const int col = (int)(threadIdx.x & 31) * 4;
     int t0, n, hu, parts;
     int64_t slot0, slot1;                   // of the first part, and of the second one (the others follow)
     if constexpr (COMMON) {
@@ -354,32 +374,34 @@ __global__ void __launch_bounds__(JOIN_ROWS * 32) ubp_attention_join_kernel(cons
         slot1 = 2 * (int64_t)(c + 1);
     }
     if (parts == 0) return;
-    const int2 w = attn_row_at(a, t0, n, hu, r);
-    if (w.x < 0 || col >= a.D) return;
+    if (col >= a.D) return;
     constexpr int N = 4, AHEAD = 8, STEP = COMMON ? 1 : 2;
-    float M = -INFINITY, L = 0.f, o[N] = {};
-    for (int k0 = 0; k0 < parts; k0 += AHEAD) {
-        float2 ml[AHEAD];
-        float v[AHEAD][N];
+#pragma unroll 1
+    for (int r = (int)blockIdx.y * join_rows(COMMON) + (int)(threadIdx.x >> 5); r < imin(a.rows, ((int)blockIdx.y + 1) * join_rows(COMMON)); r += JOIN_WARPS) {
+        const int2 w = attn_row_at(a, t0, n, hu, r);
+        if (w.x < 0) continue;
+        float M = -INFINITY, L = 0.f, o[N] = {};
+        for (int k0 = 0; k0 < parts; k0 += AHEAD) {
+            float2 ml[AHEAD];
+            float v[AHEAD][N];
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) {
-            const int k = k0 + i;
-            if (k < parts) {
-                const int64_t at = (k == 0 ? slot0 : slot1 + (int64_t)(k - 1) * STEP) * a.rows + r;
-                ml[i] = a.ml[at];
-                attn_load(a.po + at * a.D + col, v[i]);
+            for (int i = 0; i < AHEAD; ++i) {
+                const int k = k0 + i;
+                if (k < parts) {
+                    const int64_t at = (k == 0 ? slot0 : slot1 + (int64_t)(k - 1) * STEP) * a.rows + r;
+                    ml[i] = a.ml[at];
+                    attn_load(a.po + at * a.D + col, v[i]);
+                }
             }
+            attn_add_all(M, L, o, ml, v, parts - k0);
         }
-#pragma unroll
-        for (int i = 0; i < AHEAD; ++i)
-            if (k0 + i < parts) attn_add(M, L, o, ml[i].x, ml[i].y, v[i]);
-    }
-    if constexpr (COMMON) {
-        const int64_t at = (int64_t)w.x * a.Hq + w.y;
-        if (col == 0) a.pml[at] = make_float2(M, L);
-        *reinterpret_cast<float4 *>(a.ppo + at * a.D + col) = make_float4(o[0], o[1], o[2], o[3]);
-    } else {
-        attn_finish<T>(a, w.x, w.y, col, M, L, o);
+        if constexpr (COMMON) {
+            const int64_t at = (int64_t)w.x * a.Hq + w.y;
+            if (col == 0) a.pml[at] = make_float2(M, L);
+            *reinterpret_cast<float4 *>(a.ppo + at * a.D + col) = make_float4(o[0], o[1], o[2], o[3]);
+        } else {
+            attn_finish<T>(a, w.x, w.y, col, M, L, o);
+        }
     }
 }
 
@@ -401,21 +423,21 @@ template <typename T> int launch_few_t(const CUtensorMap &k, const CUtensorMap &
 int launch_attn_few(const AttnArgs &a, int dtype, int grid, void *stream)
 {
     CUtensorMap k, v;
-    if (const int rc = attn_encode_cache(&k, a, a.k, dtype, FEW_KEYS)) return rc;
-    if (const int rc = attn_encode_cache(&v, a, a.v, dtype, FEW_KEYS)) return rc;
+    if (const int rc = attn_encode_cache(&k, a, a.k, dtype, few_keys(a.D <= 64 ? 64 : 128))) return rc;
+    if (const int rc = attn_encode_cache(&v, a, a.v, dtype, few_keys(a.D <= 64 ? 64 : 128))) return rc;
     return dtype == UBP_BF16 ? launch_few_t<__nv_bfloat16>(k, v, a, grid, stream) : launch_few_t<__half>(k, v, a, grid, stream);
 }
 
 int launch_attn_join(const AttnArgs &a, int dtype, int grid, void *stream)
 {
     static std::atomic<bool> done[64] = {};
-    const unsigned y = (unsigned)((a.rows + JOIN_ROWS - 1) / JOIN_ROWS);
+    const unsigned y = (unsigned)((a.rows + join_rows(a.common) - 1) / join_rows(a.common));
     if (a.common) {
         const int64_t units = (int64_t)((a.T + a.tpt - 1) / a.tpt) * a.HU;
-        return attn_launch(ubp_attention_join_kernel<__half, true>, done, dim3((unsigned)units, y), JOIN_ROWS * 32, 0, stream, a, grid);
+        return attn_launch(ubp_attention_join_kernel<__half, true>, done, dim3((unsigned)units, y), JOIN_WARPS * 32, 0, stream, a, grid);
     }
-    return dtype == UBP_BF16 ? attn_launch(ubp_attention_join_kernel<__nv_bfloat16, false>, done, dim3((unsigned)grid, y), JOIN_ROWS * 32, 0, stream, a, grid)
-                             : attn_launch(ubp_attention_join_kernel<__half, false>, done, dim3((unsigned)grid, y), JOIN_ROWS * 32, 0, stream, a, grid);
+    return dtype == UBP_BF16 ? attn_launch(ubp_attention_join_kernel<__nv_bfloat16, false>, done, dim3((unsigned)grid, y), JOIN_WARPS * 32, 0, stream, a, grid)
+                             : attn_launch(ubp_attention_join_kernel<__half, false>, done, dim3((unsigned)grid, y), JOIN_WARPS * 32, 0, stream, a, grid);
 }
 
 }  // namespace ubp

@@ -68,6 +68,26 @@ __device__ __forceinline__ bool attn_locate(const AttnArgs &a, AttnPlace<NT> &sh
         all = __shfl_sync(0xffffffffu, ws, 31);
         return __shfl_sync(0xffffffffu, ws - w, warp) + x - v;
     };
+    if (nb <= NT) {                     // sequences of one row block each, a thread a sequence
+        AttnSeq q{0, 0, 0};
+        if (tid < nb) q = attn_seq(a, tid);
+        const int blocks = attn_row_blocks(a, q);
+        if (!__syncthreads_or(blocks > 1)) {
+            const int mine = blocks ? attn_block_tiles(a, q, 0).nt + a.extra : 0;
+            int all;
+            const int before = scan(mine, all);
+            if (!begin(all)) return false;
+            if ((int64_t)before * a.HU <= first && (int64_t)(before + mine) * a.HU > first) { sh.b = tid; sh.before = before; sh.to = mine; }
+            __syncthreads();
+            steps.c.set(a, sh.b, 0, 0, 0);
+            const uint32_t rem = (uint32_t)(first - (int64_t)sh.before * a.HU), per = (uint32_t)sh.to;
+            steps.c.hu = (int)(rem / per);
+            steps.c.tile = (int)(rem - (uint32_t)steps.c.hu * per);
+            __syncthreads();            // (sh may be something else from here on)
+            steps.seek(a);
+            return true;
+        }
+    }
     // all row blocks, NT at a time: visit(b, rt, steps before it, its steps) for this thread's; returns all steps
     auto walk = [&](auto &&visit) {
         int64_t sum = 0;
@@ -184,6 +204,26 @@ template <int N> __device__ __forceinline__ void attn_add(float &M, float &L, fl
     L = L * x + l * y;
 #pragma unroll
     for (int i = 0; i < N; ++i) o[i] = (x == 0.f ? 0.f : o[i] * x) + (y == 0.f ? 0.f : v[i] * y);
+    M = to;
+}
+// The first `k` of K partial results onto (M, L, o): one common reference, so that no exponential waits for another.
+template <int K, int N> __device__ __forceinline__ void attn_add_all(float &M, float &L, float (&o)[N], const float2 (&ml)[K], const float (&v)[K][N], int k)
+{
+    float to = M, y[K];
+#pragma unroll
+    for (int i = 0; i < K; ++i) to = i < k ? fmaxf(to, ml[i].x) : to;
+    const float x = M == -INFINITY ? L : attn_exp2(M - to);
+    L *= x;
+#pragma unroll
+    for (int j = 0; j < N; ++j) o[j] = x == 0.f ? 0.f : o[j] * x;
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+        if (i >= k) break;
+        y[i] = ml[i].x == -INFINITY ? ml[i].y : attn_exp2(ml[i].x - to);
+        L = fmaf(ml[i].y, y[i], L);
+#pragma unroll
+        for (int j = 0; j < N; ++j) o[j] += y[i] == 0.f ? 0.f : v[i][j] * y[i];
+    }
     M = to;
 }
 template <int N> __device__ __forceinline__ void attn_load(const float *p, float (&v)[N])

@@ -28,7 +28,7 @@ namespace {
 
 using namespace tc;
 
-constexpr int AT_BN = ATTN_BN, AT_TILE = 128, AT_THREADS = 384;
+constexpr int AT_BN = 128, AT_TILE = 128, AT_THREADS = 384;
 // Warps of the first warpgroup copy keys, issue products, copy values and queries; the others do the softmax. Registers a thread: 168 at the
 // launch (384 threads), then 80 for the first warpgroup and 208 for the two others.
 constexpr int AT_K_WARP = 0, AT_MMA_WARP = 1, AT_V_WARP = 2, AT_Q_WARP = 3, AT_SOFT_WARP = 4;
