@@ -342,11 +342,10 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
 // lane, eight parts under way at a time.
 // COMMON: block (u, i) takes the i-th rows of item u of the shared prefix; all of its blocks' results lie in slots u + block, and the
 // sums go to pml and ppo. Else block (c, i) takes those of the item that begins in block c, if it does not end there.
-// Rows a block: 8 for the prefix, whose few items have many parts (32: 64 blocks for a batch of 64, 20 us); 32 otherwise, where an
-// item has two or three (8: 4700 blocks for 148 items of 256 rows, 10 us).
+// ROWS a block: 8 for the prefix and for items of 16 rows, which have many parts (32: 64 blocks for a batch of 64, 20 us); 32 for
+// items of 256 rows, which have two or three (8: 4700 blocks for 148 items, 10 us).
 constexpr int JOIN_WARPS = 8;
-__host__ __device__ constexpr int join_rows(bool common) { return common ? 8 : 32; }
-template <typename T, bool COMMON>
+template <typename T, bool COMMON, int ROWS>
 __global__ void __launch_bounds__(JOIN_WARPS * 32) ubp_attention_join_kernel(const AttnArgs a, const int blocks)
 {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
@@ -376,25 +375,13 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) ubp_attention_join_kernel(con
     if (parts == 0) return;
     if (col >= a.D) return;
     constexpr int N = 4, AHEAD = 8, STEP = COMMON ? 1 : 2;
-#pragma unroll 1
-    for (int r = (int)blockIdx.y * join_rows(COMMON) + (int)(threadIdx.x >> 5); r < imin(a.rows, ((int)blockIdx.y + 1) * join_rows(COMMON)); r += JOIN_WARPS) {
-        const int2 w = attn_row_at(a, t0, n, hu, r);
-        if (w.x < 0) continue;
-        float M = -INFINITY, L = 0.f, o[N] = {};
-        for (int k0 = 0; k0 < parts; k0 += AHEAD) {
-            float2 ml[AHEAD];
-            float v[AHEAD][N];
-#pragma unroll
-            for (int i = 0; i < AHEAD; ++i) {
-                const int k = k0 + i;
-                if (k < parts) {
-                    const int64_t at = (k == 0 ? slot0 : slot1 + (int64_t)(k - 1) * STEP) * a.rows + r;
-                    ml[i] = a.ml[at];
-                    attn_load(a.po + at * a.D + col, v[i]);
-                }
-            }
-            attn_add_all(M, L, o, ml, v, parts - k0);
-        }
+    const int r0 = (int)blockIdx.y * ROWS + (int)(threadIdx.x >> 5);
+    auto part = [&](int r, int k, float2 &ml, float (&v)[N]) {
+        const int64_t at = (k == 0 ? slot0 : slot1 + (int64_t)(k - 1) * STEP) * a.rows + r;
+        ml = a.ml[at];
+        attn_load(a.po + at * a.D + col, v);
+    };
+    auto finish = [&](const int2 &w, float M, float L, float (&o)[N]) {
         if constexpr (COMMON) {
             const int64_t at = (int64_t)w.x * a.Hq + w.y;
             if (col == 0) a.pml[at] = make_float2(M, L);
@@ -402,6 +389,43 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) ubp_attention_join_kernel(con
         } else {
             attn_finish<T>(a, w.x, w.y, col, M, L, o);
         }
+    };
+    if constexpr (ROWS > JOIN_WARPS) {
+        if (parts == 2) {                   // the rule for such items: all of the warp's rows together
+            constexpr int R = ROWS / JOIN_WARPS;
+            float2 ml[R][2];
+            float v[R][2][N];
+            int2 w[R];
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                const int r = r0 + i * JOIN_WARPS;
+                w[i] = r < a.rows ? attn_row_at(a, t0, n, hu, r) : make_int2(-1, 0);
+                if (w[i].x >= 0) { part(r, 0, ml[i][0], v[i][0]); part(r, 1, ml[i][1], v[i][1]); }
+            }
+#pragma unroll
+            for (int i = 0; i < R; ++i) {
+                float M = -INFINITY, L = 0.f, o[N] = {};
+                if (w[i].x < 0) continue;
+                attn_add_all(M, L, o, ml[i], v[i], 2);
+                finish(w[i], M, L, o);
+            }
+            return;
+        }
+    }
+#pragma unroll 1
+    for (int r = r0; r < imin(a.rows, ((int)blockIdx.y + 1) * ROWS); r += JOIN_WARPS) {
+        const int2 w = attn_row_at(a, t0, n, hu, r);
+        if (w.x < 0) continue;
+        float M = -INFINITY, L = 0.f, o[N] = {};
+        for (int k0 = 0; k0 < parts; k0 += AHEAD) {
+            float2 ml[AHEAD];
+            float v[AHEAD][N];
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i)
+                if (k0 + i < parts) part(r, k0 + i, ml[i], v[i]);
+            attn_add_all(M, L, o, ml, v, parts - k0);
+        }
+        finish(w, M, L, o);
     }
 }
 
@@ -430,14 +454,14 @@ int launch_attn_few(const AttnArgs &a, int dtype, int grid, void *stream)
 
 int launch_attn_join(const AttnArgs &a, int dtype, int grid, void *stream)
 {
-    static std::atomic<bool> done[64] = {};
-    const unsigned y = (unsigned)((a.rows + join_rows(a.common) - 1) / join_rows(a.common));
-    if (a.common) {
-        const int64_t units = (int64_t)((a.T + a.tpt - 1) / a.tpt) * a.HU;
-        return attn_launch(ubp_attention_join_kernel<__half, true>, done, dim3((unsigned)units, y), JOIN_WARPS * 32, 0, stream, a, grid);
-    }
-    return dtype == UBP_BF16 ? attn_launch(ubp_attention_join_kernel<__nv_bfloat16, false>, done, dim3((unsigned)grid, y), JOIN_WARPS * 32, 0, stream, a, grid)
-                             : attn_launch(ubp_attention_join_kernel<__half, false>, done, dim3((unsigned)grid, y), JOIN_WARPS * 32, 0, stream, a, grid);
+    static std::atomic<bool> done[64] = {};       // (no dynamic shared memory: not looked at)
+    auto go = [&](auto kern, int64_t x, int rows) {
+        return attn_launch(kern, done, dim3((unsigned)x, (unsigned)((a.rows + rows - 1) / rows)), JOIN_WARPS * 32, 0, stream, a, grid);
+    };
+    if (a.common) return go(ubp_attention_join_kernel<__half, true, 8>, (int64_t)((a.T + a.tpt - 1) / a.tpt) * a.HU, 8);
+    if (a.rows == FEW_ROWS)
+        return dtype == UBP_BF16 ? go(ubp_attention_join_kernel<__nv_bfloat16, false, 8>, grid, 8) : go(ubp_attention_join_kernel<__half, false, 8>, grid, 8);
+    return dtype == UBP_BF16 ? go(ubp_attention_join_kernel<__nv_bfloat16, false, 32>, grid, 32) : go(ubp_attention_join_kernel<__half, false, 32>, grid, 32);
 }
 
 }  // namespace ubp
