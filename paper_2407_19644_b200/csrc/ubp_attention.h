@@ -29,7 +29,7 @@ namespace ubp {
 
 struct AttnArgs {
     const void *q;
-    int64_t q_ts, q_hs;             // strides of q between tokens and heads (elements)
+    int64_t q_ts, q_hs;             // strides of q between tokens and heads (elements; rows on 16 bytes)
     void *out;
     int64_t o_ts, o_hs;
     const void *k, *v;
@@ -46,7 +46,6 @@ struct AttnArgs {
     int tpt;                        // tokens a row block takes
     int bsh;                        // keys a step takes: 1 << bsh
     int extra;                      // steps that an item counts for beside its tiles
-    int q_direct;                   // queries can be copied as they are (16-byte aligned)
     float sc;                       // scale * log2(e)
     int window, sinks;
     int kv0, kv1;                   // keys outside [kv0, kv1) are left out (a shared prefix is a call of its own)
@@ -196,6 +195,7 @@ inline AttnSpace attn_space(int64_t grid, int64_t slots, int rows, int D)
 // ---- launches; both kernels follow the same scheme and leave the same partial results
 int launch_attn_few(const AttnArgs &a, int dtype, int grid, void *stream);       // 16 rows an item (ubp_attention_few.cu)
 int launch_attn_tc(const AttnArgs &a, int dtype, int grid, void *stream);        // 256 rows an item (ubp_attention_tc.cu)
+int launch_attn_copy_queries(const void *q, int64_t ts, int64_t hs, int64_t T, int Hq, int D, void *to, void *stream);      // -> [T][Hq][D]
 int launch_attn_join(const AttnArgs &a, int dtype, int grid, void *stream);       // `grid`: the kernel's before it
 int device_sms();
 void set_last_cuda_error(int e);

@@ -74,7 +74,7 @@ struct AttnCall {
     bool own_tc = false, common_tc = false;
     int own_grid = 0, common_grid = 0;
     AttnSpace own_space{}, common_space{}, row_space{};
-    size_t bytes = 0;
+    size_t q_bytes = 0, bytes = 0;
 };
 
 int attn_plan(const ubp_cache_t *c, int64_t T, int q_heads, float scale, int window, int sinks, int64_t prefix, int64_t max_new, AttnCall &p)
@@ -102,7 +102,8 @@ int attn_plan(const ubp_cache_t *c, int64_t T, int q_heads, float scale, int win
     if (items / a.HU > INT32_MAX / tiles || ((a.cap >> a.bsh) + 2) > INT32_MAX / a.HU || items * tiles / sms >= INT32_MAX) return UBP_E_UNSUPPORTED;
     p.own_grid = (int)std::min<int64_t>(sms, items * tiles);
     p.own_space = attn_space(p.own_grid, 2 * (int64_t)p.own_grid, a.rows, a.D);
-    p.bytes = p.own_space.total;
+    p.q_bytes = ((size_t)T * q_heads * a.D * 2 + 255) / 256 * 256;      // (queries off 16 bytes are copied first)
+    p.bytes = p.own_space.total + p.q_bytes;
     if (prefix > 0) {
         AttnArgs b = a;
         b.common = 1;
@@ -180,6 +181,13 @@ extern "C" int ubp_attention(const ubp_cache_t *cache, const void *q, int64_t q_
         a.po = reinterpret_cast<float *>(w + s.po);
         w += s.total;
     };
+    if (!on(q, 16) || (T > 1 && q_token_stride % 8) || (q_heads > 1 && q_head_stride % 8)) {
+        if (const int rc = launch_attn_copy_queries(q, q_token_stride, q_head_stride, T, q_heads, D, w, stream)) return rc;
+        q = w;
+        q_head_stride = D;
+        q_token_stride = (int64_t)q_heads * D;
+    }
+    w += p.q_bytes;
     finish(p.own, p.own_space);
     if (prefix > 0) {
         finish(p.common, p.common_space);

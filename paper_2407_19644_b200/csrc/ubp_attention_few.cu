@@ -52,8 +52,6 @@ template <typename T> __device__ __forceinline__ void mma16(float (&c)[4], const
         asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// two neighbouring 16-bit values off their alignment
-__device__ __forceinline__ uint32_t load_pair(const uint16_t *p) { return (uint32_t)p[0] | (uint32_t)p[1] << 16; }
 
 // The copies of a warp's steps: a cursor that runs ahead, with the pages of the next step already loaded.
 // Everything is the same in all lanes; lane 0 issues.
@@ -152,21 +150,15 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
             row[i].lo = __shfl_sync(0xffffffffu, w.lo, g + 8 * i);
             row[i].hi = __shfl_sync(0xffffffffu, w.hi, g + 8 * i);
             const T *p = static_cast<const T *>(a.q) + (token < 0 ? 0 : token * a.q_ts + head * a.q_hs) + tq * 2;
-            if ((reinterpret_cast<uintptr_t>(p) & 3) == 0) {
 #pragma unroll
-                for (int k = 0; k < 2 * NK; ++k) qf[k / 2][k % 2 * 2 + i] = token >= 0 && k * 8 < a.D ? *reinterpret_cast<const uint32_t *>(p + k * 8) : 0u;
-            } else {
-#pragma unroll
-                for (int k = 0; k < 2 * NK; ++k)
-                    qf[k / 2][k % 2 * 2 + i] = token >= 0 && k * 8 < a.D ? load_pair(reinterpret_cast<const uint16_t *>(p + k * 8)) : 0u;
-            }
+            for (int k = 0; k < 2 * NK; ++k) qf[k / 2][k % 2 * 2 + i] = token >= 0 && k * 8 < a.D ? *reinterpret_cast<const uint32_t *>(p + k * 8) : 0u;
         }
     };
-    if (steps.left > 0) begin(cur);
     FewCopies<DP> copies;
     copies.s = steps;
     copies.item(a);
     if (steps.left > 0) copies.peek(a, warp);
+#pragma unroll 1
     for (int s = 0; s < ST - 1; ++s) copies.issue(a, &tmK, &tmV, ring + (uint32_t)s * 2 * PART, smem_u32(&bar_full[warp][s]), warp, lane);
 
     // where the lane's rows of matrix instructions' operands lie in a part: piece (2 k + h) of 16 bytes at k * 32 (within 128 bytes)
@@ -175,12 +167,71 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     const uint32_t at_k = (uint32_t)(rk * 128), xk = (uint32_t)(((lane >> 3 & 1) ^ (rk & 7)) << 4);
     const uint32_t at_v = PART + (uint32_t)(rv * 128), xv = (uint32_t)(((lane >> 4) ^ (rv & 7)) << 4);
 
-    float o[2 * NK][4] = {}, m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
-    int tile0 = cur.tile, before = 0, st = 0;      // of the segment: its first tile, the share's steps before it
+    float o[2 * NK][4], m[2], l[2];
+    int tile0 = 0, before = 0, st = 0;             // of the segment: its first tile, the share's steps before it
     uint32_t phase = 0;
-    bool ok = true, described = false;
-    before = deal.count((int)blockIdx.x) - steps.left;
-    while (steps.left > 0) {
+    bool ok = true, described = false, over = true, any = false;      // over: a segment has ended (or the first one begins); any: there was one
+    while (true) {
+        if (over) {
+            // The segment before has ended: its warps' sums meet, rows 0 .. 7, then 8 .. 15 where the item has them. Before that, the
+            // next item's queries are sent for. (Once in the code: a call of a few steps is bound by fetching instructions.)
+            const int c = (int)blockIdx.x, nr = any ? imin(imin(a.tpt, cur.q.n - cur.rt * a.tpt) * a.gc, FEW_ROWS) : 0, n = cur.tile + 1 - tile0, now = which;
+            const bool whole = n == cur.t.nt && !a.common;
+            int64_t slot = 2 * (int64_t)c + (before > 0 ? 1 : 0);
+            if (a.common) slot = (int64_t)cur.hu * attn_row_blocks(a, cur.q) + cur.rt + c;
+            if (any) {
+                if (threadIdx.x == 0 && !a.common && tile0 == 0 && !whole) { attn_describe(a, cur, deal, c, before, tile0, n); described = true; }
+                steps.advance(a, 1);
+                which ^= 1;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
+                    l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
+                    if (tq == 0) meet_ml[warp * FEW_ROWS + g + 8 * i] = make_float2(m[i], l[i]);
+                }
+            }
+            if (steps.left > 0) begin(cur);
+#pragma unroll 1
+            for (int i = 0; i * 8 < nr; ++i) {
+                if (i) __syncthreads();
+#pragma unroll
+                for (int k = 0; k < 2 * NK; ++k)
+                    *reinterpret_cast<float2 *>(meet + (warp * 8 + g) * DP + k * 8 + tq * 2) = i ? make_float2(o[k][2], o[k][3]) : make_float2(o[k][0], o[k][1]);
+                __syncthreads();
+                constexpr int N = 4, TPR = DP / N;          // threads a row
+                const int r = (int)threadIdx.x / TPR, col = (int)threadIdx.x % TPR * N;
+                if (r < 8) {
+                    const int2 w = rows[now][i * 8 + r];
+                    if (col < a.D && (w.x >= 0 || !whole)) {
+                        float M = -INFINITY, L = 0.f, v[N] = {}, u[FEW_WARPS][N];
+                        float2 ml[FEW_WARPS];
+#pragma unroll
+                        for (int k = 0; k < FEW_WARPS; ++k) {
+                            ml[k] = meet_ml[k * FEW_ROWS + i * 8 + r];
+                            attn_load(meet + (k * 8 + r) * DP + col, u[k]);
+                        }
+                        attn_add_all(M, L, v, ml, u, FEW_WARPS);
+                        if (whole) attn_finish<T>(a, w.x, w.y, col, M, L, v);
+                        else {
+                            if (col == 0) a.ml[slot * FEW_ROWS + i * 8 + r] = make_float2(M, L);
+                            *reinterpret_cast<float4 *>(a.po + (slot * FEW_ROWS + i * 8 + r) * a.D + col) = make_float4(v[0], v[1], v[2], v[3]);
+                        }
+                    }
+                }
+            }
+            if (steps.left <= 0) break;
+            if (any) __syncthreads();                       // (all have read)
+            any = true;
+            over = false;
+            tile0 = cur.tile;
+            before = deal.count(c) - steps.left;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) { m[i] = -INFINITY; l[i] = 0.f; }
+#pragma unroll
+            for (int k = 0; k < 2 * NK; ++k)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[k][e] = 0.f;
+        }
         __syncwarp();                       // (all lanes have read the stage that is copied to now)
         const int nx = st == 0 ? ST - 1 : st - 1;
         copies.issue(a, &tmK, &tmV, ring + (uint32_t)nx * 2 * PART, smem_u32(&bar_full[warp][nx]), warp, lane);
@@ -272,62 +323,8 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
                 }
         }
         if (++st == ST) { st = 0; phase ^= 1u; }
-        if (cur.tile + 1 < cur.t.nt && steps.left > 1) { steps.advance(a, 1); continue; }
-
-        // ---- the segment ends: the warps' sums meet, rows 0 .. 7, then 8 .. 15 where the item has them; meanwhile the next item's
-        // queries are on their way
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
-            l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
-            if (tq == 0) meet_ml[warp * FEW_ROWS + g + 8 * i] = make_float2(m[i], l[i]);
-        }
-        const int c = (int)blockIdx.x, nr = imin(imin(a.tpt, cur.q.n - cur.rt * a.tpt) * a.gc, FEW_ROWS), n = cur.tile + 1 - tile0, now = which;
-        const bool whole = n == cur.t.nt && !a.common;
-        int64_t slot = 2 * (int64_t)c + (before > 0 ? 1 : 0);
-        if (a.common) slot = (int64_t)cur.hu * attn_row_blocks(a, cur.q) + cur.rt + c;
-        if (threadIdx.x == 0 && !a.common && tile0 == 0 && !whole) { attn_describe(a, cur, deal, c, before, tile0, n); described = true; }
-        steps.advance(a, 1);
-        which ^= 1;
-        if (steps.left > 0) begin(cur);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            if (i * 8 >= nr) break;
-            if (i) __syncthreads();
-#pragma unroll
-            for (int k = 0; k < 2 * NK; ++k)
-                *reinterpret_cast<float2 *>(meet + (warp * 8 + g) * DP + k * 8 + tq * 2) = make_float2(o[k][2 * i], o[k][2 * i + 1]);
-            __syncthreads();
-            constexpr int N = 4, TPR = DP / N;              // threads a row
-            for (int x = (int)threadIdx.x; x < 8 * TPR; x += FEW_WARPS * 32) {
-                const int r = x / TPR, col = x % TPR * N;
-                const int2 w = rows[now][i * 8 + r];
-                if (col < a.D && (w.x >= 0 || !whole)) {
-                    float M = -INFINITY, L = 0.f, v[N] = {}, u[FEW_WARPS][N];
-                    float2 ml[FEW_WARPS];
-#pragma unroll
-                    for (int k = 0; k < FEW_WARPS; ++k) {
-                        ml[k] = meet_ml[k * FEW_ROWS + i * 8 + r];
-                        attn_load(meet + (k * 8 + r) * DP + col, u[k]);
-                    }
-                    attn_add_all(M, L, v, ml, u, FEW_WARPS);
-                    if (whole) attn_finish<T>(a, w.x, w.y, col, M, L, v);
-                    else {
-                        if (col == 0) a.ml[slot * FEW_ROWS + i * 8 + r] = make_float2(M, L);
-                        *reinterpret_cast<float4 *>(a.po + (slot * FEW_ROWS + i * 8 + r) * a.D + col) = make_float4(v[0], v[1], v[2], v[3]);
-                    }
-                }
-            }
-        }
-        __syncthreads();                                    // (all have read)
-        tile0 = cur.tile;
-        before = deal.count(c) - steps.left;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) { m[i] = -INFINITY; l[i] = 0.f; }
-#pragma unroll
-        for (int k = 0; k < 2 * NK; ++k)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[k][e] = 0.f;
+        over = cur.tile + 1 == cur.t.nt || steps.left == 1;
+        if (!over) steps.advance(a, 1);
     }
     if (threadIdx.x == 0 && !a.common && !described) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
     if (!ok) {                              // copies that are still under way end before the block does (a millisecond at most each)
@@ -429,6 +426,19 @@ __global__ void __launch_bounds__(JOIN_WARPS * 32) ubp_attention_join_kernel(con
     }
 }
 
+// Queries off 16 bytes -> rows that lie on them.
+__global__ void __launch_bounds__(256) ubp_attention_copy_queries_kernel(const uint16_t *q, int64_t ts, int64_t hs, int64_t rows, int Hq, int D, uint4 *to)
+{
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int per = D / 8;
+    for (int64_t x = (int64_t)blockIdx.x * 256 + threadIdx.x; x < rows * per; x += (int64_t)gridDim.x * 256) {
+        const int64_t row = x / per, t = row / Hq;
+        const uint16_t *h = q + t * ts + (row - t * Hq) * hs + (x - row * per) * 8;
+        to[x] = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16);
+    }
+}
+
 template <typename T> int launch_few_t(const CUtensorMap &k, const CUtensorMap &v, const AttnArgs &a, int grid, void *stream)
 {
     static std::atomic<bool> done[5][64] = {};
@@ -450,6 +460,14 @@ int launch_attn_few(const AttnArgs &a, int dtype, int grid, void *stream)
     if (const int rc = attn_encode_cache(&k, a, a.k, dtype, few_keys(a.D <= 64 ? 64 : 128))) return rc;
     if (const int rc = attn_encode_cache(&v, a, a.v, dtype, few_keys(a.D <= 64 ? 64 : 128))) return rc;
     return dtype == UBP_BF16 ? launch_few_t<__nv_bfloat16>(k, v, a, grid, stream) : launch_few_t<__half>(k, v, a, grid, stream);
+}
+
+int launch_attn_copy_queries(const void *q, int64_t ts, int64_t hs, int64_t T, int Hq, int D, void *to, void *stream)
+{
+    static std::atomic<bool> done[64] = {};
+    const int64_t blocks = (T * Hq * (D / 8) + 255) / 256, most = 8 * device_sms();
+    return attn_launch(ubp_attention_copy_queries_kernel, done, dim3((unsigned)(blocks < most ? blocks : most)), 256, 0, stream, static_cast<const uint16_t *>(q), ts, hs,
+                       T * (int64_t)Hq, Hq, D, static_cast<uint4 *>(to));
 }
 
 int launch_attn_join(const AttnArgs &a, int dtype, int grid, void *stream)

@@ -244,37 +244,19 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                 const int kvh = sg.s.c.hu / a.chunks;
                                 // the item's queries, as soon as the products of the one before it have read theirs: the rows of a tile are the
                                 // group's heads of consecutive tokens, one box (rows past the sequence's end, whatever they hold, are not stored)
-                                for (int i = 0; ok && i < (sg.two(a) ? 2 : 1); ++i) {
-                                    if (queries[i]++) ok = attn_wait(smem_u32(&bars.q_empty[i]), (uint32_t)queries[i] & 1u, &abort_flag);
-                                    if (!ok) break;
-                                    const int per = a.tpt / 2, g0 = (sg.s.c.hu - kvh * a.chunks) * a.gc;
-                                    const uint32_t dst = s_q + (uint32_t)i * PART, bar = smem_u32(&bars.q_full[i]);
-                                    if (a.q_direct) {
-                                        if (lane == 0) {
-                                            mbar_expect_tx(bar, (uint32_t)(DP / 64 * a.gc * per) * 128u);
-                #pragma unroll
-                                            for (int p = 0; p < DP / 64; ++p)
-                                                tma_load_3d(dst + (uint32_t)p * AT_PANEL, &tmQ, p * 64, kvh * a.G + g0, sg.s.c.q.s + sg.s.c.rt * a.tpt + i * per, bar);
-                                        }
-                                    } else {
-                                        for (int r = lane; r < a.gc * per; r += 32) {
-                                            const int2 at = attn_row_at(a, sg.s.c.q.s + sg.s.c.rt * a.tpt, sg.s.c.q.n - sg.s.c.rt * a.tpt, sg.s.c.hu, i * AT_TILE + r);
-                                            const uint16_t *q = static_cast<const uint16_t *>(a.q) + (at.x < 0 ? 0 : at.x * a.q_ts + at.y * a.q_hs);
-                #pragma unroll 1
-                                            for (int c = 0; c < 2 * NK; ++c) {
-                                                uint4 v = make_uint4(0, 0, 0, 0);
-                                                if (at.x >= 0 && c * 8 < a.D) {
-                                                    const uint16_t *h = q + c * 8;
-                                                    v = make_uint4(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16, h[4] | (uint32_t)h[5] << 16, h[6] | (uint32_t)h[7] << 16);
-                                                }
-                                                *reinterpret_cast<uint4 *>(smem + (uint32_t)i * PART + (uint32_t)(c / 8) * AT_PANEL + (uint32_t)r * 128u + (uint32_t)(((c & 7) ^ (r & 7)) << 4)) = v;
-                                            }
-                                        }
-                                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                                        __syncwarp();
-                                        if (lane == 0) mbar_arrive(bar);
-                                    }
-                                }
+                for (int i = 0; ok && i < (sg.two(a) ? 2 : 1); ++i) {
+                    if (queries[i]++) ok = attn_wait(smem_u32(&bars.q_empty[i]), (uint32_t)queries[i] & 1u, &abort_flag);
+                    if (!ok) break;
+                    const int per = a.tpt / 2, g0 = (sg.s.c.hu - kvh * a.chunks) * a.gc;
+                    const uint32_t dst = s_q + (uint32_t)i * PART, bar = smem_u32(&bars.q_full[i]);
+                    if (lane == 0) {
+                        mbar_expect_tx(bar, (uint32_t)(DP / 64 * a.gc * per) * 128u);
+#pragma unroll
+                        for (int p = 0; p < DP / 64; ++p)
+                            tma_load_3d(dst + (uint32_t)p * AT_PANEL, &tmQ, p * 64, kvh * a.G + g0, sg.s.c.q.s + sg.s.c.rt * a.tpt + i * per, bar);
+                    }
+                    __syncwarp();
+                }
             }
         } else if (warp == AT_MMA_WARP) {
         constexpr uint32_t fmt = std::is_same_v<T, __nv_bfloat16> ? 1 : 0;
@@ -614,12 +596,8 @@ int launch_attn_tc(const AttnArgs &a, int dtype, int grid, void *stream)
     CUtensorMap k, v, q;
     if (const int rc = attn_encode_cache(&k, a, a.k, dtype, AT_BN)) return rc;
     if (const int rc = attn_encode_cache(&v, a, a.v, dtype, AT_BN)) return rc;
-    AttnArgs b = a;
-    b.q_direct = (reinterpret_cast<uintptr_t>(a.q) & 15) == 0 && (a.T == 1 || a.q_ts % 8 == 0) && (a.Hq == 1 || a.q_hs % 8 == 0);
-    if (b.q_direct) {
-        if (const int rc = encode_queries(&q, a, dtype)) return rc;
-    } else q = k;
-    return dtype == UBP_BF16 ? launch_tc_t<__nv_bfloat16>(k, v, q, b, grid, stream) : launch_tc_t<__half>(k, v, q, b, grid, stream);
+    if (const int rc = encode_queries(&q, a, dtype)) return rc;
+    return dtype == UBP_BF16 ? launch_tc_t<__nv_bfloat16>(k, v, q, a, grid, stream) : launch_tc_t<__half>(k, v, q, a, grid, stream);
 }
 
 }  // namespace ubp
