@@ -523,7 +523,7 @@ int ubp_rotate_append(const ubp_cache_t *cache, const void *qkv, int64_t ld, int
  * sequences; they are read once, through row 0 of the table, for all of them together (the result is that of prefix == 0 up to
  * rounding). max_new: most new tokens of a sequence, if the caller knows (else T); only the choice of kernel depends on it.
  * scale > 0. Strides of q and out are between tokens and heads, in elements; heads are contiguous; no alignment beyond the
- * type's. out must not overlap q or the cache.
+ * type's (queries off 16 bytes are copied to the workspace first). out must not overlap q or the cache.
  * Scores, sums and outputs are fp32 until the end; the weights w_j are rounded to the cache's type for the product with v.
  * Sums run in an order fixed by the lengths: results are bitwise reproducible. What the cache holds outside the tokens that some
  * query of a sequence sees does not reach its outputs, infinities and NaNs included. An infinity or NaN in a value that some new
@@ -534,8 +534,8 @@ int ubp_rotate_append(const ubp_cache_t *cache, const void *qkv, int64_t ld, int
  * blocks of 16 rows (tokens times heads of a group), bound by reading the cache, 1 = blocks of 256 rows on the tensor cores.
  * ubp_attention_check synchronises `stream` and returns UBP_E_DEVICE if an attention kernel on the current device has reported a
  * bounded wait that ran out (its call's outputs are then incomplete); ubp_attention_clear_status takes the report back. */
-size_t ubp_attention_workspace_size(const ubp_cache_t *cache, int64_t T, int q_heads, int window, int sinks, int64_t prefix,
-                                    int64_t max_new);
+size_t ubp_attention_workspace_size(const ubp_cache_t *cache, const void *q, int64_t q_token_stride, int64_t q_head_stride,
+                                    int64_t T, int q_heads, int window, int sinks, int64_t prefix, int64_t max_new);
 int ubp_attention(const ubp_cache_t *cache, const void *q, int64_t q_token_stride, int64_t q_head_stride, int64_t T, int q_heads,
                   float scale, int window, int sinks, int64_t prefix, int64_t max_new, void *out, int64_t out_token_stride,
                   int64_t out_head_stride, void *workspace, size_t workspace_bytes, void *stream);

@@ -108,7 +108,7 @@ def load():
     L.ubp_linear.argtypes = [vp, vp, i64, vp, i64, vp, i32, vp, i64, vp, i64, i32, vp, sz, vp]
     L.ubp_rotate_append.argtypes = [C.POINTER(_Cache), vp, i64, i64, i32, vp, vp, C.c_float, vp, i64, i64, i32, i32, vp, i64, i64, vp]
     L.ubp_attention.argtypes = [C.POINTER(_Cache), vp, i64, i64, i64, i32, C.c_float, i32, i32, i64, i64, vp, i64, i64, vp, sz, vp]
-    L.ubp_attention_workspace_size.argtypes = [C.POINTER(_Cache), i64, i32, i32, i32, i64, i64]
+    L.ubp_attention_workspace_size.argtypes = [C.POINTER(_Cache), vp, i64, i64, i64, i32, i32, i32, i64, i64]
     L.ubp_attention_workspace_size.restype = sz
     L.ubp_attention_choice.argtypes = [C.POINTER(_Cache), i64, i32, i64, i64, C.POINTER(i32), C.POINTER(i32)]
     L.ubp_attention_check.argtypes = [vp]

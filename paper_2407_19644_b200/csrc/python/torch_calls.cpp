@@ -395,7 +395,7 @@ PyObject *attention(PyObject *, PyObject *const *a, Py_ssize_t n)
         if (!out) y = make(T, Hq, c.head_dim, type, dev);
         void *pw = ws ? ws->data_ptr() : nullptr;
         size_t nws = ws ? ws->numel() * ws->element_size() : 0;
-        if (!ws && (nws = p_attention_workspace(&c, T, (int)Hq, (int)window, (int)sinks, prefix, most)) != 0) {
+        if (!ws && (nws = p_attention_workspace(&c, q->data_ptr(), qts, qhs, T, (int)Hq, (int)window, (int)sinks, prefix, most)) != 0) {
             room = make((int64_t)nws, at::kByte, dev);
             pw = room.data_ptr();
         }

@@ -92,7 +92,7 @@ UBP_HD AttnTiles attn_tiles(const AttnArgs &a, int p0, int p1)
     AttnTiles t;
     const int up = (1 << a.bsh) - 1;
     t.end = imin(p1 + 1, a.kv1);
-    t.w0 = a.window > 0 && !a.common ? imax(a.kv0, p0 - a.window + 1) : a.kv0;
+    t.w0 = a.window > 0 && !a.common ? imax(a.kv0, imax(p0, 0) - a.window + 1) : a.kv0;
     t.s0 = a.kv0 >> a.bsh;
     t.lo = t.w0 >> a.bsh;
     t.ns = 0;

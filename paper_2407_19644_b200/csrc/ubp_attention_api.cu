@@ -74,10 +74,10 @@ struct AttnCall {
     bool own_tc = false, common_tc = false;
     int own_grid = 0, common_grid = 0;
     AttnSpace own_space{}, common_space{}, row_space{};
-    size_t q_bytes = 0, bytes = 0;
+    size_t q_bytes = 0, bytes = 0;      // queries off 16 bytes are copied first
 };
 
-int attn_plan(const ubp_cache_t *c, int64_t T, int q_heads, float scale, int window, int sinks, int64_t prefix, int64_t max_new, AttnCall &p)
+int attn_plan(const ubp_cache_t *c, const void *q, int64_t q_ts, int64_t q_hs, int64_t T, int q_heads, float scale, int window, int sinks, int64_t prefix, int64_t max_new, AttnCall &p)
 {
     const int sms = device_sms();
     AttnArgs a{};
@@ -102,7 +102,7 @@ int attn_plan(const ubp_cache_t *c, int64_t T, int q_heads, float scale, int win
     if (items / a.HU > INT32_MAX / tiles || ((a.cap >> a.bsh) + 2) > INT32_MAX / a.HU || items * tiles / sms >= INT32_MAX) return UBP_E_UNSUPPORTED;
     p.own_grid = (int)std::min<int64_t>(sms, items * tiles);
     p.own_space = attn_space(p.own_grid, 2 * (int64_t)p.own_grid, a.rows, a.D);
-    p.q_bytes = ((size_t)T * q_heads * a.D * 2 + 255) / 256 * 256;      // (queries off 16 bytes are copied first)
+    if (!on(q, 16) || (T > 1 && q_ts % 8) || (q_heads > 1 && q_hs % 8)) p.q_bytes = ((size_t)T * q_heads * a.D * 2 + 255) / 256 * 256;
     p.bytes = p.own_space.total + p.q_bytes;
     if (prefix > 0) {
         AttnArgs b = a;
@@ -136,11 +136,12 @@ int check_attention(const ubp_cache_t *c, int64_t T, int q_heads, float scale, i
 }  // namespace
 }  // namespace ubp
 
-extern "C" size_t ubp_attention_workspace_size(const ubp_cache_t *cache, int64_t T, int q_heads, int window, int sinks, int64_t prefix, int64_t max_new)
+extern "C" size_t ubp_attention_workspace_size(const ubp_cache_t *cache, const void *q, int64_t q_token_stride, int64_t q_head_stride, int64_t T,
+                                               int q_heads, int window, int sinks, int64_t prefix, int64_t max_new)
 {
     if (ubp::check_attention(cache, T, q_heads, 1.f, window, sinks, prefix, max_new) || T == 0 || cache->batch == 0) return 0;
     ubp::AttnCall p;
-    return ubp::attn_plan(cache, T, q_heads, 1.f, window, sinks, prefix, max_new, p) ? 0 : p.bytes;
+    return ubp::attn_plan(cache, q, q_token_stride, q_head_stride, T, q_heads, 1.f, window, sinks, prefix, max_new, p) ? 0 : p.bytes;
 }
 
 extern "C" int ubp_attention_choice(const ubp_cache_t *cache, int64_t T, int q_heads, int64_t prefix, int64_t max_new, int *kernel, int *prefix_kernel)
@@ -149,7 +150,8 @@ extern "C" int ubp_attention_choice(const ubp_cache_t *cache, int64_t T, int q_h
     if (const int rc = check_attention(cache, T, q_heads, 1.f, 0, 0, prefix, max_new)) return rc;
     if (!kernel || !prefix_kernel) return UBP_E_ARG;
     AttnCall p;
-    if (const int rc = attn_plan(cache, T, q_heads, 1.f, 0, 0, prefix, max_new, p)) return rc;
+    if (T == 0 || cache->batch == 0) { *kernel = 0; *prefix_kernel = -1; return UBP_OK; }
+    if (const int rc = attn_plan(cache, nullptr, 0, 0, T, q_heads, 1.f, 0, 0, prefix, max_new, p)) return rc;
     *kernel = p.own_tc;
     *prefix_kernel = prefix > 0 ? (int)p.common_tc : -1;
     return UBP_OK;
@@ -166,7 +168,7 @@ extern "C" int ubp_attention(const ubp_cache_t *cache, const void *q, int64_t q_
     const int D = cache->head_dim;
     if ((q_heads > 1 && (q_head_stride < D || out_head_stride < D)) || (T > 1 && (q_token_stride < D || out_token_stride < D))) return UBP_E_ARG;
     AttnCall p;
-    if (const int rc = attn_plan(cache, T, q_heads, scale, window, sinks, prefix, max_new, p)) return rc;
+    if (const int rc = attn_plan(cache, q, q_token_stride, q_head_stride, T, q_heads, scale, window, sinks, prefix, max_new, p)) return rc;
     if (!workspace || !on(workspace, 256)) return UBP_E_ARG;
     if (workspace_bytes < p.bytes) return UBP_E_SPACE;
     int *status = nullptr;
@@ -181,7 +183,7 @@ extern "C" int ubp_attention(const ubp_cache_t *cache, const void *q, int64_t q_
         a.po = reinterpret_cast<float *>(w + s.po);
         w += s.total;
     };
-    if (!on(q, 16) || (T > 1 && q_token_stride % 8) || (q_heads > 1 && q_head_stride % 8)) {
+    if (p.q_bytes) {
         if (const int rc = launch_attn_copy_queries(q, q_token_stride, q_head_stride, T, q_heads, D, w, stream)) return rc;
         q = w;
         q_head_stride = D;

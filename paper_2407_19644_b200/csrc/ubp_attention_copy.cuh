@@ -19,17 +19,20 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap *tm,
         ::"r"(dst), "l"(tm), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar) : "memory");
 }
 
-// Bounded wait of a whole warp: false if it ran out (`tries` of a millisecond) or another one of the block had. The hardware
-// suspends the warp for up to the hinted time: without the hint it comes back after a microsecond or so, and twenty warps that ask
-// again and again took the issue slots of those at work; a look at the global timer on the way cost thousands of cycles.
-__device__ __forceinline__ bool attn_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag, int tries = 1000)
+// Bounded wait of a whole warp: false if it ran out (two seconds of cycles: a warp may wait for as long as an item takes) or another
+// one of the block had. The hardware suspends the warp for up to the hinted millisecond: without the hint it comes back after a
+// microsecond or so, and twenty warps that ask again and again took the issue slots of those at work; a look at the global timer on
+// the way cost thousands of cycles.
+__device__ __forceinline__ bool attn_wait(uint32_t bar, uint32_t parity, volatile int *abort_flag, long long limit = 4000000000ll)
 {
-    for (int i = 0;; ++i) {
+    long long t0 = 0;
+    for (bool again = false;; again = true) {
         uint32_t done;
         asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                      : "=r"(done) : "r"(bar), "r"(parity), "r"(1000000u) : "memory");
         if (__all_sync(0xffffffffu, done)) return true;
-        if (i >= tries || *abort_flag) break;
+        if (!again) t0 = clock64();
+        else if (*abort_flag || clock64() - t0 > limit) break;
     }
     *abort_flag = 1;
     return false;

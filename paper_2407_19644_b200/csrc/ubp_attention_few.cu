@@ -330,7 +330,7 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     if (!ok) {                              // copies that are still under way end before the block does (a millisecond at most each)
         int gave_up = 0;
         for (int i = 0; i < ST; ++i)
-            for (uint32_t ph = 0; ph < 2; ++ph) attn_wait(smem_u32(&bar_full[warp][i]), ph, &gave_up, 1);
+            for (uint32_t ph = 0; ph < 2; ++ph) attn_wait(smem_u32(&bar_full[warp][i]), ph, &gave_up, 2000000);
         if (lane == 0) atomicExch(a.status, 1);
     }
 }

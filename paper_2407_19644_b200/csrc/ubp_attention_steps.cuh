@@ -187,7 +187,7 @@ __device__ __forceinline__ AttnRow attn_row(const AttnArgs &a, const AttnSeq &q,
         pos = imin(imax(a.lengths[b], 0), a.cap) - (e - s) + (t - s);
     }
     w.hi = imin(pos + 1, a.kv1);
-    w.lo = a.window > 0 ? imax(pos - a.window + 1, 0) : 0;
+    w.lo = a.window > 0 ? imax(imax(pos, 0) - a.window + 1, 0) : 0;
     return w;
 }
 __device__ __forceinline__ bool attn_sees(const AttnArgs &a, const AttnRow &w, int j)

@@ -506,17 +506,17 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
         // a block whose waits ran out leaves no copy and no product under way (a millisecond at most each)
         int gave_up = 0;
         if (warp == AT_Q_WARP) {
-            for (int f = 0; f < 4; ++f) attn_wait(smem_u32(&bars.q_full[f >> 1]), (uint32_t)f & 1u, &gave_up, 1);
+            for (int f = 0; f < 4; ++f) attn_wait(smem_u32(&bars.q_full[f >> 1]), (uint32_t)f & 1u, &gave_up, 2000000);
         }
         if (warp == AT_K_WARP || warp == AT_V_WARP) {
             for (int f = filled > ST ? filled - ST : 0; f <= filled; ++f) {
-                attn_wait(smem_u32(warp == AT_V_WARP ? &bars.v_full[f % ST] : &bars.k_full[f % ST]), (uint32_t)(f / ST) & 1u, &gave_up, 1);
-                if (warp == AT_V_WARP) attn_wait(smem_u32(&bars.patch), (uint32_t)(f & 1), &gave_up, 1);
+                attn_wait(smem_u32(warp == AT_V_WARP ? &bars.v_full[f % ST] : &bars.k_full[f % ST]), (uint32_t)(f / ST) & 1u, &gave_up, 2000000);
+                if (warp == AT_V_WARP) attn_wait(smem_u32(&bars.patch), (uint32_t)(f & 1), &gave_up, 2000000);
             }
         }
         if (warp == AT_MMA_WARP) {
             commit_one(smem_u32(&bars.drain));
-            attn_wait(smem_u32(&bars.drain), 0, &gave_up, 1);
+            attn_wait(smem_u32(&bars.drain), 0, &gave_up, 2000000);
         }
         __syncthreads();
     }

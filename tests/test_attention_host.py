@@ -34,7 +34,7 @@ def test_bad_caches(change, code):
     L, c = ubp.load(), cache(**change)
     assert L.ubp_rotate_append(ctypes.byref(c), *APPEND[1:]) == code
     assert L.ubp_attention(ctypes.byref(c), *ATTEND[1:]) == code
-    assert L.ubp_attention_workspace_size(ctypes.byref(c), 3, 4, 0, 0, 0, 1) == 0
+    assert L.ubp_attention_workspace_size(ctypes.byref(c), P, 4 * 64, 64, 3, 4, 0, 0, 0, 1) == 0
 
 
 def refused(fn, base, changes):
@@ -47,12 +47,11 @@ def refused(fn, base, changes):
 
 
 def test_append_refusals():
-    nan, inf = float("nan"), float("inf")
+    nan = float("nan")
     refused(ubp.load().ubp_rotate_append, APPEND,
             [(0, None, -1), (1, None, -1), (1, P + 1, -1), (2, 8 * 64 - 1, -1), (3, -1, -1), (4, 0, -1), (4, 3, -1), (5, P + 1, -1), (6, P + 1, -1), (7, -1.0, -1),
              (7, nan, -1), (8, P + 2, -1), (9, 63, -1), (10, 0, -1), (11, 0, -1), (11, 63, -1), (11, 66, -1), (13, None, -1), (13, P + 1, -1), (14, 63, -1),
              (15, 63, -1), (3, 1 << 31, -1)])
-    assert inf > 0
 
 
 def test_attention_refusals():
@@ -70,4 +69,4 @@ def test_no_tokens_is_a_no_op():
     a = list(APPEND)
     a[0], a[1], a[3] = ctypes.byref(c), None, 0
     assert L.ubp_rotate_append(*a) == 0
-    assert L.ubp_attention_workspace_size(ctypes.byref(c), 0, 4, 0, 0, 0, 1) == 0
+    assert L.ubp_attention_workspace_size(ctypes.byref(c), None, 4 * 64, 64, 0, 4, 0, 0, 0, 1) == 0

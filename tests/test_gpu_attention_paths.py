@@ -1,0 +1,164 @@
+"""Attention over a paged cache: which kernel runs, workspaces, long items, captures in a fresh process, extreme arguments."""
+import ctypes
+import os
+import subprocess
+import sys
+
+import pytest
+import torch
+
+from attention_ref import BF16, F16, Batch, check
+
+pytestmark = pytest.mark.gpu
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def ubp():
+    import paper_2407_19644_b200 as m
+    m.load()
+    return m
+
+
+def described(b, T=None):
+    from paper_2407_19644_b200.binding import _Cache
+    s = b.k.stride()
+    return _Cache(b.k.data_ptr(), b.v.data_ptr(), s[0], s[1], s[2], b.k.shape[0], b.page, b.Hkv, b.D, 2 if b.dtype == BF16 else 1, b.table.data_ptr(),
+                  b.table.stride(0), b.table.shape[1], b.B, b.len_t.data_ptr(), None if b.starts is None else b.starts.data_ptr())
+
+
+@pytest.mark.parametrize("new,G,max_new,prefix,kernels", [
+    ([1, 1], 8, 1, 0, (0, -1)), ([1, 1], 16, 1, 0, (0, -1)), ([1, 1], 17, 1, 0, (1, -1)), ([2, 1], 8, 2, 0, (0, -1)), ([3, 1], 8, 3, 0, (1, -1)),
+    ([2, 1], 8, 100, 0, (1, -1)), ([1, 1], 8, 1, 32, (0, 0)), ([1] * 3, 8, 1, 32, (0, 1)), ([1] * 3, 20, 1, 32, (1, 1))])
+def test_kernel_choice_and_results(ubp, new, G, max_new, prefix, kernels):
+    b = Batch(new, [n + 40 for n in new], G, 1, 64, F16, 16, prefix=prefix)
+    c, k, p = described(b), ctypes.c_int(), ctypes.c_int()
+    assert ubp.load().ubp_attention_choice(ctypes.byref(c), b.T, G, prefix, max_new, ctypes.byref(k), ctypes.byref(p)) == 0
+    assert (k.value, p.value) == kernels
+    q = b.queries()
+    want, tol = b.exact(q)
+    if prefix:
+        out = ubp.ubp_prefix_attention(q, *b.args(), prefix, starts=b.starts, max_new=max_new)
+    else:
+        out = ubp.ubp_attention(q, *b.args(), starts=b.starts, max_new=max_new)
+    check(out, want, tol, b.T)
+
+
+@pytest.mark.parametrize("new", [1, 60])
+@pytest.mark.parametrize("pad,lead", [(0, 0), (2, 0), (3, 1), (4, 2)])
+@pytest.mark.parametrize("prefix", [0, 33])
+def test_workspace_of_the_size_asked_for(ubp, new, pad, lead, prefix):
+    """A workspace of exactly that many bytes, between guards; one byte less is refused."""
+    b = Batch([new, 1], [new + 200, 120], 4, 2, 72, BF16, 16, prefix=prefix)
+    q = b.queries(pad=pad, lead=lead)
+    want, tol = b.exact(q)
+    c = described(b)
+    n = ubp.load().ubp_attention_workspace_size(ctypes.byref(c), q.data_ptr(), q.stride(0), q.stride(1), b.T, 4, 0, 0, prefix, max(new, 1))
+    room = torch.full((n + 512,), 77, dtype=torch.uint8, device="cuda")
+    fn = ubp.ubp_prefix_attention if prefix else ubp.ubp_attention
+    args = (q, *b.args(), prefix) if prefix else (q, *b.args())
+    check(fn(*args, starts=b.starts, max_new=new, workspace=room[256:256 + n]), want, tol, b.T)
+    assert (room[:256] == 77).all() and (room[256 + n:] == 77).all()
+    with pytest.raises(ubp.UbpError) as e:
+        fn(*args, starts=b.starts, max_new=new, workspace=room[256:256 + n - 1])
+    assert e.value.code == -3
+    with pytest.raises(ubp.UbpError) as e:
+        fn(*args, starts=b.starts, max_new=new, workspace=room[255:])
+    assert e.value.code == -1
+
+
+def test_items_that_take_milliseconds(ubp):
+    """A block may wait for as long as an item takes: eight thousand queries on a million tokens, checked on some rows."""
+    n, new, Hq, D, page = 1 << 20, 8192, 4, 64, 128
+    g = torch.Generator(device="cuda").manual_seed(3)
+    k, v = (torch.randn(n // page, 1, page, D, device="cuda", generator=g).to(F16) for _ in range(2))
+    table = torch.arange(n // page, dtype=torch.int32, device="cuda")[None]
+    lengths = torch.tensor([n], dtype=torch.int32, device="cuda")
+    starts = torch.tensor([0, new], dtype=torch.int32, device="cuda")
+    q = (4 * torch.randn(new, Hq, D, device="cuda", generator=g)).to(F16)
+    out = ubp.ubp_attention(q, k, v, table, lengths, starts=starts)
+    ubp.attention_check()
+    K, V = k.view(n, D).double(), v.view(n, D).double()
+    for t in (0, 1, 63, 64, 4095, 8190, 8191):
+        p = n - new + t + 1
+        s = (q[t].double() @ K[:p].t()) / 8
+        w = torch.softmax(s, 1)
+        want, size = w @ V[:p], w @ V[:p].abs()
+        # weights rounded to 2^-11 each and errors of the scores (62 exact products, sizes up to 4 * 64 * 4 / 8) as in the other tests
+        big = float((q[t].double().abs() @ K[:p].abs().t()).max() / 8)
+        tol = size * (2.0 ** -11 + 2 * ((D + 4) * 2.0 ** -23 * big + (big + 16) * 2.0 ** -21)) + 2.0 ** -11 * want.abs() + 2.0 ** -24
+        # sums of a million weights, a few of which matter: the partial sums' roundings add to at most 2^-23 of the sum for each of
+        # a tile's 128 and of the 8192 tiles that a row is rescaled or added over
+        tol += size * 2 * (128 + 8192) * 2.0 ** -23 + 2.0 ** -25 * float(V.abs().mean()) * p * float(w.max())
+        assert ((out[t].double() - want).abs() <= tol).all()
+
+
+def test_first_call_of_a_process_is_captured():
+    code = """
+import torch, paper_2407_19644_b200 as ubp
+q = torch.randn(2, 4, 64, device='cuda').bfloat16()
+k, v = (torch.randn(8, 2, 16, 64, device='cuda').bfloat16() for _ in range(2))
+t = torch.arange(8, dtype=torch.int32, device='cuda').view(2, 4)
+n = torch.tensor([60, 33], dtype=torch.int32, device='cuda')
+o, p = torch.zeros(2, 4, 64, device='cuda').bfloat16(), torch.zeros(2, 4, 64, device='cuda').bfloat16()
+s = torch.tensor([0, 1, 2], dtype=torch.int32, device='cuda')
+g = torch.cuda.CUDAGraph()
+with torch.cuda.graph(g):
+    ubp.ubp_attention(q, k, v, t, n, out=o)
+    ubp.ubp_attention(q, k, v, t, n, out=p, starts=s, max_new=50)
+    ubp.ubp_prefix_attention(q, k, v, t, n, 16)
+    ubp.ubp_rotate_append(torch.zeros(2, 8 * 64, device='cuda').bfloat16(), 4, k.clone(), v.clone(), t, n)
+g.replay()
+torch.cuda.synchronize()
+a = ubp.ubp_attention(q, k, v, t, n)
+assert torch.equal(o, a) and (p.float() - a.float()).abs().max() < 0.05, (o - a).abs().max()
+print('captured ok')
+"""
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and "captured ok" in r.stdout, r.stdout[-1000:] + r.stderr[-2000:]
+
+
+@pytest.mark.parametrize("max_new", [1, 60])
+def test_extreme_windows(ubp, max_new):
+    most = (1 << 31) - 1
+    b = Batch([1, 2], [300, 1], 4, 2, 64, BF16, 16)          # (the second has more new tokens than it is long)
+    b.K[1], b.V[1] = b.K[1][:1], b.V[1][:1]
+    q = b.queries()
+    out = ubp.ubp_attention(q, *b.args(), starts=b.starts, max_new=max_new)
+    for window, sinks in ((most, 0), (most, most), (5, most), (300, 300)):
+        got = ubp.ubp_attention(q, *b.args(), starts=b.starts, window=window, sinks=sinks, max_new=max_new)
+        assert torch.isfinite(got).all() and ((got.float() - out.float()).abs() <= 2.0 ** -7 * out.float().abs() + 2.0 ** -7).all()
+    got = ubp.ubp_attention(q, *b.args(), starts=b.starts, window=1, max_new=max_new)     # itself only: its own value
+    assert torch.equal(got[0], b.V[0][299].repeat_interleave(2, 0)) and (got[1] == 0).all() and torch.equal(got[2], b.V[1][0].repeat_interleave(2, 0))
+
+
+@pytest.mark.parametrize("max_new", [1, 60])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
+def test_unseen_tokens_do_not_matter(ubp, max_new, value):
+    """Keys and values that no new token sees -- behind the lengths, outside windows, before a page's first seen token -- may be
+    anything; so may unused pages."""
+    for window, sinks in ((0, 0), (100, 5), (37, 130)):
+        b = Batch([1, 1, 1], [437, 128, 1], 4, 2, 128, BF16, 64, seed=window)
+        q = b.queries()
+        want, tol = b.exact(q, window, sinks)
+        hidden = [torch.arange(n, device="cuda") for n in b.lengths]
+        for s, n in enumerate(b.lengths):
+            j = hidden[s]
+            gone = (j <= n - 1 - window) & (j >= sinks) if window else j < 0
+            page, slot = b.table[s].long()[j[gone] // 64], j[gone] % 64
+            b.k[page, :, slot] = value
+            b.v[page, :, slot] = value
+        check(ubp.ubp_attention(q, *b.args(), starts=b.starts, window=window, sinks=sinks, max_new=max_new), want, tol, 3)
+
+
+def test_results_do_not_depend_on_neighbours(ubp):
+    """A sequence's result is the same to its rounding alone and in a batch."""
+    b = Batch([3, 70, 1, 200], [90, 700, 1300, 200], 6, 2, 96, BF16, 32)
+    q = b.queries()
+    want, tol = b.exact(q)
+    for s in range(4):
+        rows = slice(b.first[s], b.first[s + 1])
+        alone = torch.tensor([0, b.new[s]], dtype=torch.int32, device="cuda")
+        out = ubp.ubp_attention(q[rows], b.k, b.v, b.table[s:s + 1], b.len_t[s:s + 1], starts=alone)
+        check(out, want[rows], tol[rows], b.new[s])
