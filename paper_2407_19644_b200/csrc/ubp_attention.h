@@ -49,6 +49,7 @@ struct AttnArgs {
     float sc;                       // scale * log2(e)
     int window, sinks;
     int kv0, kv1;                   // keys outside [kv0, kv1) are left out (a shared prefix is a call of its own)
+    int shared;                     // keys below it lie in the pages of table row 0 (boxes of a copy that lie below it as a whole)
     int common;                     // 1: the rows are all tokens of all sequences, the pages those of table row 0
     // partial results: rows x {reference maximum, sum} and rows x D of a slot
     float2 *ml;
@@ -194,6 +195,7 @@ inline AttnSpace attn_space(int64_t grid, int64_t slots, int rows, int D)
 
 // ---- launches; both kernels follow the same scheme and leave the same partial results
 int launch_attn_few(const AttnArgs &a, int dtype, int grid, void *stream);       // 16 rows an item (ubp_attention_few.cu)
+int launch_attn_cluster(const AttnArgs &a, int dtype, int size, void *stream);    // the same, a cluster of blocks a sequence and unit head
 int launch_attn_tc(const AttnArgs &a, int dtype, int grid, void *stream);        // 256 rows an item (ubp_attention_tc.cu)
 int launch_attn_copy_queries(const void *q, int64_t ts, int64_t hs, int64_t T, int Hq, int D, void *to, void *stream);      // -> [T][Hq][D]
 int launch_attn_join(const AttnArgs &a, int dtype, int grid, void *stream);       // `grid`: the kernel's before it

@@ -68,10 +68,22 @@ void set_rows(AttnArgs &a, int rows, int tiles)
     a.extra = tiles == 2 ? 2 : 3;
 }
 
+// Bytes of a shared prefix that are read again for the other sequences (mostly from L2) in the time that a call of its own for the
+// prefix and the join of its sums take. bf16, read again / a call of its own, us: 8 MB 17.0 / 21.8, 25 MB 11.7 / 24.3, 57 MB 18.0 /
+// 27.5, 66 MB 24.9 / 28.3, 123 MB 27.8 / 28.4, 131 MB 32.9 / 27.7, 197 MB 41.0 / 29.8, 254 MB 46.8 / 33.4, 516 MB 84 / 45.
+constexpr double ATTN_PREFIX_BYTES = 120e6;
+// Clusters of blocks of 16 rows: as many blocks as run at once (15 clusters of eight; 16 of them took 11.5 us instead of 6.3), and
+// tiles a block, by the longest that the table or the window allows. One token on 8 key heads of 128 values, cluster / steps dealt,
+// us: 500 keys 7.0 / 8.6, 2000 8.1 / 10.5, 4000 10.3 / 11.6, 8000 (eight tiles a block) 15.1 / 14.2; four sequences of 500 7.2 / 9.9, of
+// 4000 (eight tiles) 16.9 / 16.8; twelve of 500 (one block each) 9.8 / 12.9; 100 of 700 keys on one head of 64 values 7.9 / 11.9.
+constexpr int64_t ATTN_CLUSTER_BLOCKS = 120, ATTN_CLUSTER_TILES = 6;
+
 // A call's kernels, grids and the layout of its workspace; the same for the size query and the call.
 struct AttnCall {
     AttnArgs own, common;
     bool own_tc = false, common_tc = false;
+    int cluster = 0;                    // blocks of a cluster that share a sequence and unit head; 0: steps are dealt
+    bool has_common = false;
     int own_grid = 0, common_grid = 0;
     AttnSpace own_space{}, common_space{}, row_space{};
     size_t q_bytes = 0, bytes = 0;      // queries off 16 bytes are copied first
@@ -104,7 +116,18 @@ int attn_plan(const ubp_cache_t *c, const void *q, int64_t q_ts, int64_t q_hs, i
     p.own_space = attn_space(p.own_grid, 2 * (int64_t)p.own_grid, a.rows, a.D);
     if (!on(q, 16) || (T > 1 && q_ts % 8) || (q_heads > 1 && q_hs % 8)) p.q_bytes = ((size_t)T * q_heads * a.D * 2 + 255) / 256 * 256;
     p.bytes = p.own_space.total + p.q_bytes;
-    if (prefix > 0) {
+    // A shared prefix is read for all sequences at once only where reading it again for each takes longer than that saves.
+    const bool again = prefix > 0 && (double)(a.B - 1) * prefix * a.Hkv * a.D * 4.0 < ATTN_PREFIX_BYTES;
+    if (again) { a.kv0 = 0; a.shared = (int)prefix; }
+    // Few sequences and short work: a cluster of up to eight blocks for each sequence and unit head.
+    if (!p.own_tc && (prefix == 0 || again)) {
+        const int64_t units = (int64_t)a.B * a.HU, reach = (seen >> a.bsh) + 2;
+        int size = 8;
+        while (size > 1 && units * size > ATTN_CLUSTER_BLOCKS) size /= 2;
+        if (units * size <= ATTN_CLUSTER_BLOCKS && reach <= (int64_t)ATTN_CLUSTER_TILES * size) p.cluster = size;
+    }
+    if (p.cluster) { p.own_space = AttnSpace{}; p.bytes = p.q_bytes; }
+    if (prefix > 0 && !again) {
         AttnArgs b = a;
         b.common = 1;
         b.kv0 = 0; b.kv1 = (int)prefix;
@@ -120,6 +143,7 @@ int attn_plan(const ubp_cache_t *c, const void *q, int64_t q_ts, int64_t q_hs, i
         p.bytes += p.common_space.total + p.row_space.total;
         p.common = b;
     }
+    p.has_common = prefix > 0 && !again;
     p.own = a;
     return UBP_OK;
 }
@@ -152,8 +176,8 @@ extern "C" int ubp_attention_choice(const ubp_cache_t *cache, int64_t T, int q_h
     AttnCall p;
     if (T == 0 || cache->batch == 0) { *kernel = 0; *prefix_kernel = -1; return UBP_OK; }
     if (const int rc = attn_plan(cache, nullptr, 0, 0, T, q_heads, 1.f, 0, 0, prefix, max_new, p)) return rc;
-    *kernel = p.own_tc;
-    *prefix_kernel = prefix > 0 ? (int)p.common_tc : -1;
+    *kernel = p.own_tc ? 1 : p.cluster ? 2 : 0;
+    *prefix_kernel = p.has_common ? (int)p.common_tc : -1;
     return UBP_OK;
 }
 
@@ -169,7 +193,7 @@ extern "C" int ubp_attention(const ubp_cache_t *cache, const void *q, int64_t q_
     if ((q_heads > 1 && (q_head_stride < D || out_head_stride < D)) || (T > 1 && (q_token_stride < D || out_token_stride < D))) return UBP_E_ARG;
     AttnCall p;
     if (const int rc = attn_plan(cache, q, q_token_stride, q_head_stride, T, q_heads, scale, window, sinks, prefix, max_new, p)) return rc;
-    if (!workspace || !on(workspace, 256)) return UBP_E_ARG;
+    if (p.bytes && (!workspace || !on(workspace, 256))) return UBP_E_ARG;
     if (workspace_bytes < p.bytes) return UBP_E_SPACE;
     int *status = nullptr;
     if (const int rc = status_word(&status)) return rc;
@@ -191,7 +215,8 @@ extern "C" int ubp_attention(const ubp_cache_t *cache, const void *q, int64_t q_
     }
     w += p.q_bytes;
     finish(p.own, p.own_space);
-    if (prefix > 0) {
+    if (p.cluster) return launch_attn_cluster(p.own, cache->dtype, p.cluster, stream);
+    if (p.has_common) {
         finish(p.common, p.common_space);
         p.own.pml = p.common.pml = reinterpret_cast<float2 *>(w + p.row_space.ml);
         p.own.ppo = p.common.ppo = reinterpret_cast<float *>(w + p.row_space.po);

@@ -40,10 +40,10 @@ __device__ __forceinline__ bool attn_wait(uint32_t bar, uint32_t parity, volatil
 
 // Page of the box of `box` keys from j on, which lie in one page: out of the cache's range (its copy brings zeros) where no row of
 // the item sees a key of it, or where the table names none.
-__device__ __forceinline__ int attn_box_page(const AttnArgs &a, const AttnTiles &t, const int32_t *row, int j, int box)
+__device__ __forceinline__ int attn_box_page(const AttnArgs &a, const AttnTiles &t, int b, int j, int box)
 {
     if (j >= t.end || j + box <= a.kv0 || (j + box <= t.w0 && j >= a.sinks)) return a.pages;
-    const int p = row[j >> a.pshift];
+    const int p = a.table[(a.common || j + box <= a.shared ? 0 : (int64_t)b * a.ldt) + (j >> a.pshift)];
     return (uint32_t)p < (uint32_t)a.pages ? p : a.pages;
 }
 
@@ -52,8 +52,9 @@ __device__ __forceinline__ int attn_box_page(const AttnArgs &a, const AttnTiles 
 int attn_encode_cache(CUtensorMap *tm, const AttnArgs &a, const void *base, int dtype, int keys);
 
 // A launch that may begin before the kernel in front of it has ended; dynamic shared memory is allowed once a device and kernel.
+// cluster: blocks of a cluster (1: none).
 template <typename K, typename... A>
-int attn_launch(K kern, std::atomic<bool> (&done)[64], dim3 grid, int threads, size_t smem, void *stream, const A &...args)
+int attn_launch(K kern, std::atomic<bool> (&done)[64], dim3 grid, int threads, size_t smem, int cluster, void *stream, const A &...args)
 {
     cudaError_t e = cudaSuccess;
     if (smem > 48 * 1024) {
@@ -69,11 +70,15 @@ int attn_launch(K kern, std::atomic<bool> (&done)[64], dim3 grid, int threads, s
     cfg.blockDim = dim3((unsigned)threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = static_cast<cudaStream_t>(stream);
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     if (e == cudaSuccess) e = cudaLaunchKernelEx(&cfg, kern, args...);
     if (e == cudaSuccess) e = cudaGetLastError();
     if (e != cudaSuccess) { set_last_cuda_error((int)e); return UBP_E_CUDA; }

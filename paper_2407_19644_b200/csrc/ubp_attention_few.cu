@@ -53,18 +53,31 @@ template <typename T> __device__ __forceinline__ void mma16(float (&c)[4], const
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// from the same place in the shared memory of another block of the cluster
+__device__ __forceinline__ uint32_t rank_at(const void *p, uint32_t rank)
+{
+    uint32_t a;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_u32(p)), "r"(rank));
+    return a;
+}
+__device__ __forceinline__ float2 ld_rank2(const float2 *p, uint32_t rank)
+{
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(rank_at(p, rank)) : "memory");
+    return v;
+}
+__device__ __forceinline__ void ld_rank4(const float *p, uint32_t rank, float (&v)[4])
+{
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(rank_at(p, rank)) : "memory");
+}
+
 // The copies of a warp's steps: a cursor that runs ahead, with the pages of the next step already loaded.
 // Everything is the same in all lanes; lane 0 issues.
 template <int DP> struct FewCopies {
     AttnSteps s;
     int page[few_keys(DP) / 8], j0, kvh;
-    const int32_t *row;
 
-    __device__ __forceinline__ void item(const AttnArgs &a)
-    {
-        kvh = (int)((uint32_t)s.c.hu / (uint32_t)a.chunks);
-        row = a.table + (a.common ? 0 : (int64_t)s.c.b * a.ldt);
-    }
+    __device__ __forceinline__ void item(const AttnArgs &a) { kvh = (int)((uint32_t)s.c.hu / (uint32_t)a.chunks); }
     __device__ __forceinline__ void peek(const AttnArgs &a, int warp)
     {
         constexpr int KEYS = few_keys(DP);
@@ -72,7 +85,7 @@ template <int DP> struct FewCopies {
         const int box = imin(1 << a.pshift, KEYS);
 #pragma unroll
         for (int b = 0; b < KEYS / 8; ++b)
-            if (b * box < KEYS) page[b] = attn_box_page(a, s.c.t, row, j0 + b * box, box);
+            if (b * box < KEYS) page[b] = attn_box_page(a, s.c.t, s.c.b, j0 + b * box, box);
     }
     __device__ __forceinline__ void issue(const AttnArgs &a, const CUtensorMap *tmK, const CUtensorMap *tmV, uint32_t stage, uint32_t bar, int warp, int lane)
     {
@@ -102,7 +115,9 @@ template <int DP> struct FewCopies {
 };
 
 // NK: head size in steps of 16 (the copies bring zeros past it)
-template <typename T, int NK>
+// CLUSTER: a cluster of blocks takes a sequence and unit head, a share of its tiles each; their sums meet in distributed shared
+// memory, rank r finishes rows r, r + size, .. (short work of few sequences: no dealing of steps, no partial results, no second kernel)
+template <typename T, int NK, bool CLUSTER>
 __global__ void __launch_bounds__(FEW_WARPS * 32, 1)
 ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV, const AttnArgs a)
 {
@@ -117,6 +132,8 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     float *const meet = reinterpret_cast<float *>(smem + FEW_WARPS * FEW_RING);                      // [warp][8 rows][DP]
     float2 *const meet_ml = reinterpret_cast<float2 *>(meet + FEW_WARPS * 8 * DP);                    // [warp][row]
     const uint32_t ring = smem_u32(smem) + (uint32_t)warp * FEW_RING;
+    float *const part = reinterpret_cast<float *>(smem);               // CLUSTER: [row][DP] and [row] of the block's sums
+    float2 *const part_ml = reinterpret_cast<float2 *>(part + FEW_ROWS * DP);
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (lane == 0) {
         if (warp == 0) { prefetch_tensormap(&tmK); prefetch_tensormap(&tmV); abort_flag = 0; }
@@ -129,8 +146,18 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
 
     AttnDeal deal;
     AttnSteps steps;
+    int size = 1, rank = 0, tiles = 0;      // of the cluster; tiles of the item
     static_assert(sizeof(AttnPlace<FEW_WARPS * 32>) <= FEW_WARPS * 8 * 64 * 4, "lies where the warps' sums meet");
-    if (!attn_locate<FEW_WARPS * 32>(a, *reinterpret_cast<AttnPlace<FEW_WARPS * 32> *>(meet), deal, steps)) {
+    if constexpr (CLUSTER) {
+        asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(size));
+        rank = (int)cluster_rank();
+        const int u = (int)blockIdx.x / size, b = u / a.HU;
+        steps.c.set(a, b, u - b * a.HU, 0, 0);
+        if (steps.c.q.n == 0) return;       // (all of the cluster)
+        tiles = steps.c.t.nt;
+        steps.c.tile = tiles * rank / size;
+        steps.left = tiles * (rank + 1) / size - steps.c.tile;
+    } else if (!attn_locate<FEW_WARPS * 32>(a, *reinterpret_cast<AttnPlace<FEW_WARPS * 32> *>(meet), deal, steps)) {
         if (threadIdx.x == 0 && !a.common) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
         return;
     }
@@ -155,11 +182,19 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
         }
     };
     FewCopies<DP> copies;
-    copies.s = steps;
-    copies.item(a);
-    if (steps.left > 0) copies.peek(a, warp);
+    int st = 0;                             // stage of the next step
+    uint32_t phase = 0;
+    auto start = [&] {                      // the first copies of a share
+        copies.s = steps;
+        copies.item(a);
+        if (steps.left > 0) copies.peek(a, warp);
 #pragma unroll 1
-    for (int s = 0; s < ST - 1; ++s) copies.issue(a, &tmK, &tmV, ring + (uint32_t)s * 2 * PART, smem_u32(&bar_full[warp][s]), warp, lane);
+        for (int s = 0; s < ST - 1; ++s) {
+            const int to = st + s < ST ? st + s : st + s - ST;
+            copies.issue(a, &tmK, &tmV, ring + (uint32_t)to * 2 * PART, smem_u32(&bar_full[warp][to]), warp, lane);
+        }
+    };
+    if constexpr (!CLUSTER) start();
 
     // where the lane's rows of matrix instructions' operands lie in a part: piece (2 k + h) of 16 bytes at k * 32 (within 128 bytes)
     // xor h and the row; the same for keys (rows = keys) and values (transposed)
@@ -168,20 +203,20 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
     const uint32_t at_v = PART + (uint32_t)(rv * 128), xv = (uint32_t)(((lane >> 4) ^ (rv & 7)) << 4);
 
     float o[2 * NK][4], m[2], l[2];
-    int tile0 = 0, before = 0, st = 0;             // of the segment: its first tile, the share's steps before it
-    uint32_t phase = 0;
+    int tile0 = 0, before = 0;              // of the segment: its first tile, the share's steps before it
     bool ok = true, described = false, over = true, any = false;      // over: a segment has ended (or the first one begins); any: there was one
     while (true) {
         if (over) {
             // The segment before has ended: its warps' sums meet, rows 0 .. 7, then 8 .. 15 where the item has them. Before that, the
             // next item's queries are sent for. (Once in the code: a call of a few steps is bound by fetching instructions.)
+            if (CLUSTER && !any) start();
             const int c = (int)blockIdx.x, nr = any ? imin(imin(a.tpt, cur.q.n - cur.rt * a.tpt) * a.gc, FEW_ROWS) : 0, n = cur.tile + 1 - tile0, now = which;
             const bool whole = n == cur.t.nt && !a.common;
             int64_t slot = 2 * (int64_t)c + (before > 0 ? 1 : 0);
             if (a.common) slot = (int64_t)cur.hu * attn_row_blocks(a, cur.q) + cur.rt + c;
             if (any) {
-                if (threadIdx.x == 0 && !a.common && tile0 == 0 && !whole) { attn_describe(a, cur, deal, c, before, tile0, n); described = true; }
-                steps.advance(a, 1);
+                if (!CLUSTER && threadIdx.x == 0 && !a.common && tile0 == 0 && !whole) { attn_describe(a, cur, deal, c, before, tile0, n); described = true; }
+                if (!CLUSTER || steps.left > 0) steps.advance(a, 1);
                 which ^= 1;
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
@@ -190,7 +225,7 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
                     if (tq == 0) meet_ml[warp * FEW_ROWS + g + 8 * i] = make_float2(m[i], l[i]);
                 }
             }
-            if (steps.left > 0) begin(cur);
+            if (CLUSTER ? !any : steps.left > 0) begin(cur);
 #pragma unroll 1
             for (int i = 0; i * 8 < nr; ++i) {
                 if (i) __syncthreads();
@@ -202,7 +237,7 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
                 const int r = (int)threadIdx.x / TPR, col = (int)threadIdx.x % TPR * N;
                 if (r < 8) {
                     const int2 w = rows[now][i * 8 + r];
-                    if (col < a.D && (w.x >= 0 || !whole)) {
+                    if (col < a.D && (CLUSTER || w.x >= 0 || !whole)) {
                         float M = -INFINITY, L = 0.f, v[N] = {}, u[FEW_WARPS][N];
                         float2 ml[FEW_WARPS];
 #pragma unroll
@@ -211,7 +246,10 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
                             attn_load(meet + (k * 8 + r) * DP + col, u[k]);
                         }
                         attn_add_all(M, L, v, ml, u, FEW_WARPS);
-                        if (whole) attn_finish<T>(a, w.x, w.y, col, M, L, v);
+                        if constexpr (CLUSTER) {            // (over the ring: this share's copies have all been read)
+                            if (col == 0) part_ml[i * 8 + r] = make_float2(M, L);
+                            *reinterpret_cast<float4 *>(part + (i * 8 + r) * DP + col) = make_float4(v[0], v[1], v[2], v[3]);
+                        } else if (whole) attn_finish<T>(a, w.x, w.y, col, M, L, v);
                         else {
                             if (col == 0) a.ml[slot * FEW_ROWS + i * 8 + r] = make_float2(M, L);
                             *reinterpret_cast<float4 *>(a.po + (slot * FEW_ROWS + i * 8 + r) * a.D + col) = make_float4(v[0], v[1], v[2], v[3]);
@@ -219,18 +257,53 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
                     }
                 }
             }
-            if (steps.left <= 0) break;
-            if (any) __syncthreads();                       // (all have read)
+            if constexpr (CLUSTER) {
+                if (any) {
+                    cluster_sync();
+                    constexpr int N = 4;
+                    const int per = a.D / N;
+                    for (int x = (int)threadIdx.x; x < (nr - rank + size - 1) / size * per; x += FEW_WARPS * 32) {
+                        const int r = rank + x / per * size, col = x % per * N;
+                        const int2 w = rows[now][r];
+                        float M = -INFINITY, L = 0.f, v[N] = {}, u[8][N];
+                        float2 ml[8];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k)
+                            if (k < size) {
+                                ml[k] = ld_rank2(part_ml + r, (uint32_t)k);
+                                ld_rank4(part + r * DP + col, (uint32_t)k, u[k]);
+                            }
+                        attn_add_all(M, L, v, ml, u, size);
+                        if (w.x >= 0 && ok) attn_finish<T>(a, w.x, w.y, col, M, L, v);
+                    }
+                    cluster_sync();                         // (nobody leaves or goes on while its sums are being read)
+                    const int rt = cur.rt + 1;
+                    if (rt * a.tpt >= cur.q.n) break;
+                    // (more new tokens than the caller said: the next row block)
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    steps.c.set(a, cur.b, cur.hu, rt, 0);
+                    steps.c.tile = steps.c.t.nt * rank / size;
+                    steps.left = steps.c.t.nt * (rank + 1) / size - steps.c.tile;
+                    __syncthreads();
+                    any = false;
+                    continue;
+                }
+                over = steps.left <= 0;                     // (a share without tiles meets the others all the same)
+            } else {
+                if (steps.left <= 0) break;
+                if (any) __syncthreads();                   // (all have read)
+                over = false;
+            }
             any = true;
-            over = false;
             tile0 = cur.tile;
-            before = deal.count(c) - steps.left;
+            if constexpr (!CLUSTER) before = deal.count(c) - steps.left;
 #pragma unroll
             for (int i = 0; i < 2; ++i) { m[i] = -INFINITY; l[i] = 0.f; }
 #pragma unroll
             for (int k = 0; k < 2 * NK; ++k)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[k][e] = 0.f;
+            if (CLUSTER && over) continue;
         }
         __syncwarp();                       // (all lanes have read the stage that is copied to now)
         const int nx = st == 0 ? ST - 1 : st - 1;
@@ -326,7 +399,7 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
         over = cur.tile + 1 == cur.t.nt || steps.left == 1;
         if (!over) steps.advance(a, 1);
     }
-    if (threadIdx.x == 0 && !a.common && !described) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
+    if (!CLUSTER && threadIdx.x == 0 && !a.common && !described) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
     if (!ok) {                              // copies that are still under way end before the block does (a millisecond at most each)
         int gave_up = 0;
         for (int i = 0; i < ST; ++i)
@@ -439,16 +512,22 @@ __global__ void __launch_bounds__(256) ubp_attention_copy_queries_kernel(const u
     }
 }
 
-template <typename T> int launch_few_t(const CUtensorMap &k, const CUtensorMap &v, const AttnArgs &a, int grid, void *stream)
+// cluster: its size, 0: steps dealt to `grid` blocks
+template <typename T, bool CLUSTER> int launch_few_t(const AttnArgs &a, int dtype, int grid, int cluster, void *stream)
 {
     static std::atomic<bool> done[5][64] = {};
+    CUtensorMap k, v;
+    const int keys = few_keys(a.D <= 64 ? 64 : 128);
+    if (const int rc = attn_encode_cache(&k, a, a.k, dtype, keys)) return rc;
+    if (const int rc = attn_encode_cache(&v, a, a.v, dtype, keys)) return rc;
     const dim3 g((unsigned)grid);
+    constexpr int t = FEW_WARPS * 32;
     switch (a.D <= 64 ? 4 : (a.D + 15) / 16) {
-        case 4: return attn_launch(ubp_attention_few_kernel<T, 4>, done[0], g, FEW_WARPS * 32, few_smem(64), stream, k, v, a);
-        case 5: return attn_launch(ubp_attention_few_kernel<T, 5>, done[1], g, FEW_WARPS * 32, few_smem(128), stream, k, v, a);
-        case 6: return attn_launch(ubp_attention_few_kernel<T, 6>, done[2], g, FEW_WARPS * 32, few_smem(128), stream, k, v, a);
-        case 7: return attn_launch(ubp_attention_few_kernel<T, 7>, done[3], g, FEW_WARPS * 32, few_smem(128), stream, k, v, a);
-        default: return attn_launch(ubp_attention_few_kernel<T, 8>, done[4], g, FEW_WARPS * 32, few_smem(128), stream, k, v, a);
+        case 4: return attn_launch(ubp_attention_few_kernel<T, 4, CLUSTER>, done[0], g, t, few_smem(64), cluster, stream, k, v, a);
+        case 5: return attn_launch(ubp_attention_few_kernel<T, 5, CLUSTER>, done[1], g, t, few_smem(128), cluster, stream, k, v, a);
+        case 6: return attn_launch(ubp_attention_few_kernel<T, 6, CLUSTER>, done[2], g, t, few_smem(128), cluster, stream, k, v, a);
+        case 7: return attn_launch(ubp_attention_few_kernel<T, 7, CLUSTER>, done[3], g, t, few_smem(128), cluster, stream, k, v, a);
+        default: return attn_launch(ubp_attention_few_kernel<T, 8, CLUSTER>, done[4], g, t, few_smem(128), cluster, stream, k, v, a);
     }
 }
 
@@ -456,17 +535,20 @@ template <typename T> int launch_few_t(const CUtensorMap &k, const CUtensorMap &
 
 int launch_attn_few(const AttnArgs &a, int dtype, int grid, void *stream)
 {
-    CUtensorMap k, v;
-    if (const int rc = attn_encode_cache(&k, a, a.k, dtype, few_keys(a.D <= 64 ? 64 : 128))) return rc;
-    if (const int rc = attn_encode_cache(&v, a, a.v, dtype, few_keys(a.D <= 64 ? 64 : 128))) return rc;
-    return dtype == UBP_BF16 ? launch_few_t<__nv_bfloat16>(k, v, a, grid, stream) : launch_few_t<__half>(k, v, a, grid, stream);
+    return dtype == UBP_BF16 ? launch_few_t<__nv_bfloat16, false>(a, dtype, grid, 1, stream) : launch_few_t<__half, false>(a, dtype, grid, 1, stream);
+}
+
+int launch_attn_cluster(const AttnArgs &a, int dtype, int size, void *stream)
+{
+    const int grid = a.B * a.HU * size;
+    return dtype == UBP_BF16 ? launch_few_t<__nv_bfloat16, true>(a, dtype, grid, size, stream) : launch_few_t<__half, true>(a, dtype, grid, size, stream);
 }
 
 int launch_attn_copy_queries(const void *q, int64_t ts, int64_t hs, int64_t T, int Hq, int D, void *to, void *stream)
 {
     static std::atomic<bool> done[64] = {};
     const int64_t blocks = (T * Hq * (D / 8) + 255) / 256, most = 8 * device_sms();
-    return attn_launch(ubp_attention_copy_queries_kernel, done, dim3((unsigned)(blocks < most ? blocks : most)), 256, 0, stream, static_cast<const uint16_t *>(q), ts, hs,
+    return attn_launch(ubp_attention_copy_queries_kernel, done, dim3((unsigned)(blocks < most ? blocks : most)), 256, 0, 1, stream, static_cast<const uint16_t *>(q), ts, hs,
                        T * (int64_t)Hq, Hq, D, static_cast<uint4 *>(to));
 }
 
@@ -474,7 +556,7 @@ int launch_attn_join(const AttnArgs &a, int dtype, int grid, void *stream)
 {
     static std::atomic<bool> done[64] = {};       // (no dynamic shared memory: not looked at)
     auto go = [&](auto kern, int64_t x, int rows) {
-        return attn_launch(kern, done, dim3((unsigned)x, (unsigned)((a.rows + rows - 1) / rows)), JOIN_WARPS * 32, 0, stream, a, grid);
+        return attn_launch(kern, done, dim3((unsigned)x, (unsigned)((a.rows + rows - 1) / rows)), JOIN_WARPS * 32, 0, 1, stream, a, grid);
     };
     if (a.common) return go(ubp_attention_join_kernel<__half, true, 8>, (int64_t)((a.T + a.tpt - 1) / a.tpt) * a.HU, 8);
     if (a.rows == FEW_ROWS)

@@ -199,9 +199,8 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
             int patches = 0;
             for (; ok && sg.get(); sg.done(a)) {
                 const int kvh = sg.s.c.hu / a.chunks;
-                const int32_t *row = a.table + (a.common ? 0 : (int64_t)sg.s.c.b * a.ldt);
                 const AttnTiles &t = sg.s.c.t;
-                auto page_of = [&](int i) { return lane < nbox ? attn_box_page(a, t, row, attn_tile_at(t, sg.s.c.tile + i) * AT_BN + lane * box, box) : a.pages; };      // (a lane a box)
+                auto page_of = [&](int i) { return lane < nbox ? attn_box_page(a, t, sg.s.c.b, attn_tile_at(t, sg.s.c.tile + i) * AT_BN + lane * box, box) : a.pages; };      // (a lane a box)
                 int page = page_of(0);
                 for (int i = 0; i < sg.n; ++i, ++filled) {
                     const int st = filled % ST, j0 = attn_tile_at(t, sg.s.c.tile + i) * AT_BN, ahead = i + 1 < sg.n ? page_of(i + 1) : 0;
@@ -444,7 +443,8 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                     for (int e = 3; e < 31; e += 2) mx[c] = max3(mx[c], __uint_as_float(s[c][e]), __uint_as_float(s[c][e + 1]));
                     mx[c] = fmaxf(mx[c], __uint_as_float(s[c][31]));
                 }
-                const float top = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * a.sc;
+                // (a row that does not exist holds whatever was there: it has no say in when the others' sums are rescaled)
+                const float top = row.token >= 0 ? fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * a.sc : -INFINITY;
                 if (__any_sync(0xffffffffu, top > m + 8.f)) {
                     const float to = fmaxf(m, top), f = m == -INFINITY ? 0.f : attn_exp2(m - to);
                     m = to;
@@ -581,11 +581,11 @@ template <typename T> int launch_tc_t(const CUtensorMap &k, const CUtensorMap &v
     static std::atomic<bool> done[5][64] = {};
     const dim3 g((unsigned)grid);
     switch (a.D <= 64 ? 4 : (a.D + 15) / 16) {
-        case 4: return attn_launch(ubp_attention_tc_kernel<T, 4>, done[0], g, AT_THREADS, at_smem(64), stream, k, v, q, a);
-        case 5: return attn_launch(ubp_attention_tc_kernel<T, 5>, done[1], g, AT_THREADS, at_smem(128), stream, k, v, q, a);
-        case 6: return attn_launch(ubp_attention_tc_kernel<T, 6>, done[2], g, AT_THREADS, at_smem(128), stream, k, v, q, a);
-        case 7: return attn_launch(ubp_attention_tc_kernel<T, 7>, done[3], g, AT_THREADS, at_smem(128), stream, k, v, q, a);
-        default: return attn_launch(ubp_attention_tc_kernel<T, 8>, done[4], g, AT_THREADS, at_smem(128), stream, k, v, q, a);
+        case 4: return attn_launch(ubp_attention_tc_kernel<T, 4>, done[0], g, AT_THREADS, at_smem(64), 1, stream, k, v, q, a);
+        case 5: return attn_launch(ubp_attention_tc_kernel<T, 5>, done[1], g, AT_THREADS, at_smem(128), 1, stream, k, v, q, a);
+        case 6: return attn_launch(ubp_attention_tc_kernel<T, 6>, done[2], g, AT_THREADS, at_smem(128), 1, stream, k, v, q, a);
+        case 7: return attn_launch(ubp_attention_tc_kernel<T, 7>, done[3], g, AT_THREADS, at_smem(128), 1, stream, k, v, q, a);
+        default: return attn_launch(ubp_attention_tc_kernel<T, 8>, done[4], g, AT_THREADS, at_smem(128), 1, stream, k, v, q, a);
     }
 }
 

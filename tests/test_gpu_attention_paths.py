@@ -28,13 +28,17 @@ def described(b, T=None):
                   b.table.stride(0), b.table.shape[1], b.B, b.len_t.data_ptr(), None if b.starts is None else b.starts.data_ptr())
 
 
-@pytest.mark.parametrize("new,G,max_new,prefix,kernels", [
-    ([1, 1], 8, 1, 0, (0, -1)), ([1, 1], 16, 1, 0, (0, -1)), ([1, 1], 17, 1, 0, (1, -1)), ([2, 1], 8, 2, 0, (0, -1)), ([3, 1], 8, 3, 0, (1, -1)),
-    ([2, 1], 8, 100, 0, (1, -1)), ([1, 1], 8, 1, 32, (0, 0)), ([1] * 3, 8, 1, 32, (0, 1)), ([1] * 3, 20, 1, 32, (1, 1))])
-def test_kernel_choice_and_results(ubp, new, G, max_new, prefix, kernels):
-    b = Batch(new, [n + 40 for n in new], G, 1, 64, F16, 16, prefix=prefix)
+# kernel: 0 = 16 rows an item, steps dealt; 1 = 256 rows; 2 = 16 rows, a cluster an item; and that of the shared prefix (-1: read again)
+@pytest.mark.parametrize("new,lengths,Hq,Hkv,max_new,prefix,kernels", [
+    ([1, 1], [41, 90], 8, 1, 1, 0, (2, -1)), ([1, 1], [41, 90], 16, 1, 1, 0, (2, -1)), ([1, 1], [41, 90], 17, 1, 1, 0, (1, -1)),
+    ([2, 1], [41, 90], 8, 1, 2, 0, (2, -1)), ([3, 1], [41, 90], 8, 1, 3, 0, (1, -1)), ([2, 1], [41, 90], 8, 1, 100, 0, (1, -1)),
+    ([1, 1], [70000, 90], 8, 1, 1, 0, (0, -1)), ([1] * 40, [100] * 40, 16, 4, 1, 0, (0, -1)), ([1] * 3, [80, 70, 90], 8, 1, 1, 64, (2, -1)),
+    ([5, 1, 1], [80, 70, 90], 8, 1, 5, 64, (1, -1)), ([1] * 3, [150000, 150010, 150020], 8, 2, 1, 150000, (0, 0)),
+    ([1] * 40, [9000 + n for n in range(40)], 8, 2, 1, 9000, (0, 1)), ([9] * 30, [9000 + n for n in range(30)], 8, 4, 9, 8960, (1, 1))])
+def test_kernel_choice_and_results(ubp, new, lengths, Hq, Hkv, max_new, prefix, kernels):
+    b = Batch(new, lengths, Hq, Hkv, 64, F16, 16, prefix=prefix)
     c, k, p = described(b), ctypes.c_int(), ctypes.c_int()
-    assert ubp.load().ubp_attention_choice(ctypes.byref(c), b.T, G, prefix, max_new, ctypes.byref(k), ctypes.byref(p)) == 0
+    assert ubp.load().ubp_attention_choice(ctypes.byref(c), b.T, Hq, prefix, max_new, ctypes.byref(k), ctypes.byref(p)) == 0
     assert (k.value, p.value) == kernels
     q = b.queries()
     want, tol = b.exact(q)
@@ -43,14 +47,31 @@ def test_kernel_choice_and_results(ubp, new, G, max_new, prefix, kernels):
     else:
         out = ubp.ubp_attention(q, *b.args(), starts=b.starts, max_new=max_new)
     check(out, want, tol, b.T)
+    if max_new > 1 or prefix:
+        return
+    # more new tokens than the caller says: another kernel would be better, the result is the same
+    b = Batch([21, 3, 0, 40], [lengths[0] + 20, 33, 7, 40], Hq, Hkv, 64, F16, 16, behind=1)
+    q = b.queries()
+    want, tol = b.exact(q, 30, 2)
+    check(ubp.ubp_attention(q, *b.args(), starts=b.starts, max_new=1, window=30, sinks=2), want, tol, b.first[-1])
+
+
+def test_prefix_pages_in_the_first_row_only(ubp):
+    """Pages that lie below the prefix as a whole are read through row 0, whichever way the call takes."""
+    for lengths, prefix in (([100, 90, 97], 80), ([9000 + n for n in range(40)], 8992)):
+        b = Batch([1] * len(lengths), lengths, 8, 2, 64, BF16, 16, prefix=prefix)
+        q = b.queries()
+        want, tol = b.exact(q)
+        b.table[1:, :prefix // 16] = -3
+        check(ubp.ubp_prefix_attention(q, *b.args(), prefix, max_new=1), want, tol, b.T)
 
 
 @pytest.mark.parametrize("new", [1, 60])
 @pytest.mark.parametrize("pad,lead", [(0, 0), (2, 0), (3, 1), (4, 2)])
-@pytest.mark.parametrize("prefix", [0, 33])
+@pytest.mark.parametrize("prefix", [0, 75000])
 def test_workspace_of_the_size_asked_for(ubp, new, pad, lead, prefix):
     """A workspace of exactly that many bytes, between guards; one byte less is refused."""
-    b = Batch([new, 1], [new + 200, 120], 4, 2, 72, BF16, 16, prefix=prefix)
+    b = Batch([new, 1, 1, 1], [new + prefix + 200, prefix + 120, prefix + 1, prefix + 5], 4, 2, 72, BF16, 16, prefix=prefix, wide=600)
     q = b.queries(pad=pad, lead=lead)
     want, tol = b.exact(q)
     c = described(b)
@@ -59,7 +80,7 @@ def test_workspace_of_the_size_asked_for(ubp, new, pad, lead, prefix):
     fn = ubp.ubp_prefix_attention if prefix else ubp.ubp_attention
     args = (q, *b.args(), prefix) if prefix else (q, *b.args())
     check(fn(*args, starts=b.starts, max_new=new, workspace=room[256:256 + n]), want, tol, b.T)
-    assert (room[:256] == 77).all() and (room[256 + n:] == 77).all()
+    assert n > 0 and (room[:256] == 77).all() and (room[256 + n:] == 77).all()
     with pytest.raises(ubp.UbpError) as e:
         fn(*args, starts=b.starts, max_new=new, workspace=room[256:256 + n - 1])
     assert e.value.code == -3
@@ -162,3 +183,38 @@ def test_results_do_not_depend_on_neighbours(ubp):
         alone = torch.tensor([0, b.new[s]], dtype=torch.int32, device="cuda")
         out = ubp.ubp_attention(q[rows], b.k, b.v, b.table[s:s + 1], b.len_t[s:s + 1], starts=alone)
         check(out, want[rows], tol[rows], b.new[s])
+
+
+@pytest.mark.parametrize("D,G,Hkv,new,dtype", [
+    (64, 1, 2, [1] * 9, F16), (128, 4, 1, [1] * 9, BF16), (80, 16, 2, [1, 3, 0, 1, 40, 1, 1, 1, 2], F16), (72, 40, 2, [1] * 9, BF16),
+    (128, 1, 1, [1] * 9, BF16), (96, 3, 3, [30, 2, 70, 1, 1, 0, 200, 1, 1], BF16)])
+def test_prefix_read_once(ubp, D, G, Hkv, new, dtype):
+    """A prefix long enough for a call of its own, ending inside a page, queries inside it among others."""
+    prefix = 120 * 10 ** 6 // (8 * Hkv * D * 4) + 13
+    lengths = [prefix + [40, 3, 0, 1, 200, 700, 129, 64, 2][s] for s in range(9)]
+    b = Batch(new, lengths, Hkv * G, Hkv, D, dtype, 64, prefix=prefix, behind=2, seed=D)
+    q = b.queries(pad=G % 2)
+    c, k, p = described(b), ctypes.c_int(), ctypes.c_int()
+    assert ubp.load().ubp_attention_choice(ctypes.byref(c), b.T, Hkv * G, prefix, max(new), ctypes.byref(k), ctypes.byref(p)) == 0 and p.value >= 0
+    for window, sinks in ((0, 0), (500, 5)):
+        want, tol = b.exact(q, window, sinks)
+        out = torch.full((b.T, Hkv * G, D), -77.0, dtype=dtype, device="cuda")
+        got = ubp.ubp_prefix_attention(q, *b.args(), prefix, starts=b.starts, max_new=max(new), window=window, sinks=sinks, out=out)
+        check(got, want, tol, b.first[-1])
+        assert (out[b.first[-1]:] == -77.0).all()
+        again = ubp.ubp_prefix_attention(q, *b.args(), prefix, starts=b.starts, max_new=max(new), window=window, sinks=sinks, out=torch.empty_like(out))
+        assert torch.equal(again[:b.first[-1]], out[:b.first[-1]])
+
+
+@pytest.mark.parametrize("G", [3, 5, 48, 127])
+def test_unused_rows_have_no_say(ubp, G):
+    """Groups that do not fill a tile of 128 rows: what its other rows hold does not move a bit of the result."""
+    b = Batch([90, 33], [700, 1500], G, 1, 64, BF16, 16)
+    q = b.queries(3.0)
+    first = ubp.ubp_attention(q, *b.args(), starts=b.starts)
+    want, tol = b.exact(q)
+    check(first, want, tol, b.T)
+    other = Batch([300], [300], 8, 1, 128, BF16, 16, seed=3)
+    for scale in (1e-3, 1.0, 100.0):
+        ubp.ubp_attention(other.queries(scale), *other.args(), starts=other.starts)       # leaves its queries in the SMs' memory
+        assert torch.equal(ubp.ubp_attention(q, *b.args(), starts=b.starts), first)
