@@ -520,18 +520,20 @@ int ubp_rotate_append(const ubp_cache_t *cache, const void *qkv, int64_t ld, int
 /* ubp_attention: for the query at position p of its sequence
  *     o = sum_j w_j v_j / sum_j w_j,  w_j = exp(scale q.k_j),  over j <= p with window == 0 or j > p - window or j < sinks
  * A query that sees no key (p < 0) gives 0. prefix > 0: the caller states that the first `prefix` tokens are the same for all
- * sequences; they are read once, through row 0 of the table, for all of them together (the result is that of prefix == 0 up to
- * rounding). max_new: most new tokens of a sequence, if the caller knows (else T); only the choice of kernel depends on it.
+ * sequences (the result is that of prefix == 0 up to rounding). Pages that they fill are read through row 0 of the table, what they
+ * fill of a last page through row 0 or the sequence's own; they are read once for all sequences together where that is faster
+ * than again for each, and then count as seen by all of them. max_new: most new tokens of a sequence, if the caller knows (else T); only the choice of kernel depends on it.
  * scale > 0. Strides of q and out are between tokens and heads, in elements; heads are contiguous; no alignment beyond the
  * type's (queries off 16 bytes are copied to the workspace first). out must not overlap q or the cache.
  * Scores, sums and outputs are fp32 until the end; the weights w_j are rounded to the cache's type for the product with v.
  * Sums run in an order fixed by the lengths: results are bitwise reproducible. What the cache holds outside the tokens that some
  * query of a sequence sees does not reach its outputs, infinities and NaNs included. An infinity or NaN in a value that some new
  * tokens of a sequence see and others do not may make these NaN too.
- * workspace: device, 256-byte aligned, ubp_attention_workspace_size bytes (same arguments); its contents need not be set and
- * belong to one call at a time. */
+ * workspace: device, 256-byte aligned, ubp_attention_workspace_size bytes (same arguments; NULL if that is 0); its contents need
+ * not be set and belong to one call at a time. */
 /* ubp_attention_choice: which kernel a call takes for the sequences' own tokens, and for the shared prefix (-1 without one): 0 =
- * blocks of 16 rows (tokens times heads of a group), bound by reading the cache, 1 = blocks of 256 rows on the tensor cores.
+ * blocks of 16 rows (tokens times heads of a group), bound by reading the cache, 2 = the same for few sequences of short work, each
+ * head's by a cluster of blocks, 1 = blocks of 256 rows on the tensor cores. (Without a window, and with all rows aligned.)
  * ubp_attention_check synchronises `stream` and returns UBP_E_DEVICE if an attention kernel on the current device has reported a
  * bounded wait that ran out (its call's outputs are then incomplete); ubp_attention_clear_status takes the report back. */
 size_t ubp_attention_workspace_size(const ubp_cache_t *cache, const void *q, int64_t q_token_stride, int64_t q_head_stride,

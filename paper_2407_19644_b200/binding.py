@@ -776,9 +776,9 @@ def ubp_attention(q, k_cache, v_cache, page_table, lengths, starts=None, window:
 
 def ubp_prefix_attention(q, k_cache, v_cache, page_table, lengths, prefix: int, starts=None, window: int = 0, sinks: int = 0,
                          scale: Optional[float] = None, max_new: Optional[int] = None, out=None, stream=None, workspace=None):
-    """ubp_attention for sequences whose first `prefix` tokens are the same: these are read once, through the table's first row, for all
-    sequences together; then each sequence's own tokens. The result is ubp_attention's up to rounding. prefix need not fill its
-    last page (every sequence's own page then starts with copies of the prefix's last tokens)."""
+    """ubp_attention for sequences whose first `prefix` tokens are the same: their pages are those of the table's first row, and are
+    read once for all sequences together where that is faster than again for each. The result is ubp_attention's up to rounding.
+    prefix need not fill its last page (every sequence's own page then starts with copies of the prefix's last tokens)."""
     r = (_calls or _native()).attention(q, k_cache, v_cache, page_table, lengths, starts, prefix, window, sinks, scale, max_new, out,
                                         None if stream is None else stream.cuda_stream, workspace)
     if type(r) is int:

@@ -4,8 +4,8 @@
 
 --debug builds libubp_b200_debug.so instead: the same library with -DUBP_DEBUG, in which the kernels that work on a plan
 compare the indices they take from it or compute for shared / global memory with their extents, report a failure through the
-plan's status word and skip the access (nothing traps). The row operators have no plan and no status word: they are the same in
-both builds. Load it by setting UBP_B200_LIBRARY to its path before the package is imported.
+plan's status word and skip the access (nothing traps). The row operators and those of the paged cache have no plan (the
+attention kernels a status word of their own): they are the same in both builds. Load it by setting UBP_B200_LIBRARY to its path before the package is imported.
 """
 from __future__ import annotations
 

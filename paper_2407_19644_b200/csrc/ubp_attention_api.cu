@@ -116,8 +116,10 @@ int attn_plan(const ubp_cache_t *c, const void *q, int64_t q_ts, int64_t q_hs, i
     p.own_space = attn_space(p.own_grid, 2 * (int64_t)p.own_grid, a.rows, a.D);
     if (!on(q, 16) || (T > 1 && q_ts % 8) || (q_heads > 1 && q_hs % 8)) p.q_bytes = ((size_t)T * q_heads * a.D * 2 + 255) / 256 * 256;
     p.bytes = p.own_space.total + p.q_bytes;
-    // A shared prefix is read for all sequences at once only where reading it again for each takes longer than that saves.
-    const bool again = prefix > 0 && (double)(a.B - 1) * prefix * a.Hkv * a.D * 4.0 < ATTN_PREFIX_BYTES;
+    // A shared prefix is read for all sequences at once only where reading it again for each -- what a window leaves of it -- takes
+    // longer than that saves.
+    const double each = window > 0 ? std::min<double>((double)prefix, (double)window + sinks) : (double)prefix;
+    const bool again = prefix > 0 && (a.B * each - (double)prefix) * a.Hkv * a.D * 4.0 < ATTN_PREFIX_BYTES;
     if (again) { a.kv0 = 0; a.shared = (int)prefix; }
     // Few sequences and short work: a cluster of up to eight blocks for each sequence and unit head.
     if (!p.own_tc && (prefix == 0 || again)) {

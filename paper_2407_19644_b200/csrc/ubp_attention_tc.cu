@@ -241,8 +241,8 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
             int queries[2] = {0, 0};
             for (; ok && sg.get(); sg.done(a)) {
                 const int kvh = sg.s.c.hu / a.chunks;
-                                // the item's queries, as soon as the products of the one before it have read theirs: the rows of a tile are the
-                                // group's heads of consecutive tokens, one box (rows past the sequence's end, whatever they hold, are not stored)
+                // the item's queries, as soon as the products of the one before it have read theirs: the rows of a tile are the
+                // group's heads of consecutive tokens, one box (rows past the sequence's end, whatever they hold, are not stored)
                 for (int i = 0; ok && i < (sg.two(a) ? 2 : 1); ++i) {
                     if (queries[i]++) ok = attn_wait(smem_u32(&bars.q_empty[i]), (uint32_t)queries[i] & 1u, &abort_flag);
                     if (!ok) break;
@@ -258,72 +258,72 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                 }
             }
         } else if (warp == AT_MMA_WARP) {
-        constexpr uint32_t fmt = std::is_same_v<T, __nv_bfloat16> ? 1 : 0;
-        const uint32_t id_s = at_idesc(AT_BN, fmt, 0), id_o = at_idesc(NK * 16, fmt, 1);
-        const uint64_t q0 = make_desc(s_q, 16, 1024, AT_SWZ), k0 = make_desc(s_k, 16, 1024, AT_SWZ), v0 = make_desc(s_v, AT_PANEL, 1024, AT_SWZ);
-        uint32_t q_phase[2] = {0, 0}, p_phase[2] = {0, 0}, k_phase = 0, v_phase = 0;
-        int ks = 0, vs = 0;                                  // stages of the next keys and values
-        auto scores = [&](int i) {                            // S_i = Q_i K^T
-            const uint64_t q = q0 + (uint64_t)((uint32_t)i * (PART >> 4)), k = k0 + (uint64_t)((uint32_t)ks * (PART >> 4));
-            const uint32_t d = tmem + (uint32_t)i * 128u;
-            mma_ss4(d, q, k, id_s, 0);
-            if constexpr (NK == 8) mma_ss4(d, q + (AT_PANEL >> 4), k + (AT_PANEL >> 4), id_s, 1);
-            else {
+            constexpr uint32_t fmt = std::is_same_v<T, __nv_bfloat16> ? 1 : 0;
+            const uint32_t id_s = at_idesc(AT_BN, fmt, 0), id_o = at_idesc(NK * 16, fmt, 1);
+            const uint64_t q0 = make_desc(s_q, 16, 1024, AT_SWZ), k0 = make_desc(s_k, 16, 1024, AT_SWZ), v0 = make_desc(s_v, AT_PANEL, 1024, AT_SWZ);
+            uint32_t q_phase[2] = {0, 0}, p_phase[2] = {0, 0}, k_phase = 0, v_phase = 0;
+            int ks = 0, vs = 0;                                  // stages of the next keys and values
+            auto scores = [&](int i) {                            // S_i = Q_i K^T
+                const uint64_t q = q0 + (uint64_t)((uint32_t)i * (PART >> 4)), k = k0 + (uint64_t)((uint32_t)ks * (PART >> 4));
+                const uint32_t d = tmem + (uint32_t)i * 128u;
+                mma_ss4(d, q, k, id_s, 0);
+                if constexpr (NK == 8) mma_ss4(d, q + (AT_PANEL >> 4), k + (AT_PANEL >> 4), id_s, 1);
+                else {
 #pragma unroll
-                for (int n = 4; n < NK; ++n) mma_ss1(d, q + (AT_PANEL >> 4) + (uint64_t)((n - 4) * 2), k + (AT_PANEL >> 4) + (uint64_t)((n - 4) * 2), id_s, 1);
-            }
-            commit_one(smem_u32(&bars.s_full[i]));
-        };
-        auto wait = [&](uint64_t &bar, uint32_t phase) { ok = attn_wait(smem_u32(&bar), phase, &abort_flag); };
-        auto next_keys = [&] {
-            commit_one(smem_u32(&bars.k_empty[ks]));
-            if (++ks == ST) { ks = 0; k_phase ^= 1u; }
-        };
-        for (; ok && sg.get(); sg.done(a)) {
-            const int nt = sg.two(a) ? 2 : 1;
-            wait(bars.k_full[ks], k_phase);
-            for (int i = 0; ok && i < nt; ++i) {
-                wait(bars.q_full[i], q_phase[i]);
-                if (!ok) break;
-                q_phase[i] ^= 1u;
-                tmem_after();
-                scores(i);
-                if (sg.n == 1) commit_one(smem_u32(&bars.q_empty[i]));
-            }
-            if (!ok) break;
-            next_keys();
-            for (int j = 0; ok && j < sg.n; ++j) {
-                const bool more = j + 1 < sg.n;
-                wait(bars.v_full[vs], v_phase);
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    if (!ok || i >= nt) break;
-                    wait(bars.p_half[i], p_phase[i]);
+                    for (int n = 4; n < NK; ++n) mma_ss1(d, q + (AT_PANEL >> 4) + (uint64_t)((n - 4) * 2), k + (AT_PANEL >> 4) + (uint64_t)((n - 4) * 2), id_s, 1);
+                }
+                commit_one(smem_u32(&bars.s_full[i]));
+            };
+            auto wait = [&](uint64_t &bar, uint32_t phase) { ok = attn_wait(smem_u32(&bar), phase, &abort_flag); };
+            auto next_keys = [&] {
+                commit_one(smem_u32(&bars.k_empty[ks]));
+                if (++ks == ST) { ks = 0; k_phase ^= 1u; }
+            };
+            for (; ok && sg.get(); sg.done(a)) {
+                const int nt = sg.two(a) ? 2 : 1;
+                wait(bars.k_full[ks], k_phase);
+                for (int i = 0; ok && i < nt; ++i) {
+                    wait(bars.q_full[i], q_phase[i]);
                     if (!ok) break;
+                    q_phase[i] ^= 1u;
                     tmem_after();
-                    const uint64_t v = v0 + (uint64_t)((uint32_t)vs * (PART >> 4));
-                    const uint32_t d = tmem + 256u + (uint32_t)i * 128u, p = tmem + (uint32_t)i * 128u;
-                    mma_ts4(d, p, v, id_o, j > 0);
-                    wait(bars.p_full[i], p_phase[i]);
-                    if (!ok) break;
-                    p_phase[i] ^= 1u;
-                    tmem_after();
-                    mma_ts4(d, p + 32u, v + 512, id_o, 1);
-                    if (!more) commit_one(smem_u32(&bars.o_full[i]));
-                    else {
-                        if (i == 0) wait(bars.k_full[ks], k_phase);
-                        if (!ok) break;
-                        scores(i);
-                        if (j + 2 == sg.n) commit_one(smem_u32(&bars.q_empty[i]));
-                    }
+                    scores(i);
+                    if (sg.n == 1) commit_one(smem_u32(&bars.q_empty[i]));
                 }
                 if (!ok) break;
-                commit_one(smem_u32(&bars.v_empty[vs]));
-                if (++vs == ST) { vs = 0; v_phase ^= 1u; }
-                if (more) next_keys();
+                next_keys();
+                for (int j = 0; ok && j < sg.n; ++j) {
+                    const bool more = j + 1 < sg.n;
+                    wait(bars.v_full[vs], v_phase);
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        if (!ok || i >= nt) break;
+                        wait(bars.p_half[i], p_phase[i]);
+                        if (!ok) break;
+                        tmem_after();
+                        const uint64_t v = v0 + (uint64_t)((uint32_t)vs * (PART >> 4));
+                        const uint32_t d = tmem + 256u + (uint32_t)i * 128u, p = tmem + (uint32_t)i * 128u;
+                        mma_ts4(d, p, v, id_o, j > 0);
+                        wait(bars.p_full[i], p_phase[i]);
+                        if (!ok) break;
+                        p_phase[i] ^= 1u;
+                        tmem_after();
+                        mma_ts4(d, p + 32u, v + 512, id_o, 1);
+                        if (!more) commit_one(smem_u32(&bars.o_full[i]));
+                        else {
+                            if (i == 0) wait(bars.k_full[ks], k_phase);
+                            if (!ok) break;
+                            scores(i);
+                            if (j + 2 == sg.n) commit_one(smem_u32(&bars.q_empty[i]));
+                        }
+                    }
+                    if (!ok) break;
+                    commit_one(smem_u32(&bars.v_empty[vs]));
+                    if (++vs == ST) { vs = 0; v_phase ^= 1u; }
+                    if (more) next_keys();
+                }
             }
-        }
-        __syncwarp();
+            __syncwarp();
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");

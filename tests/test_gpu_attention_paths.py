@@ -218,3 +218,17 @@ def test_unused_rows_have_no_say(ubp, G):
     for scale in (1e-3, 1.0, 100.0):
         ubp.ubp_attention(other.queries(scale), *other.args(), starts=other.starts)       # leaves its queries in the SMs' memory
         assert torch.equal(ubp.ubp_attention(q, *b.args(), starts=b.starts), first)
+
+
+@pytest.mark.parametrize("D,G,Hkv,new", [(128, 4, 1, [1] * 9), (64, 3, 2, [1, 3, 0, 1, 200, 1, 1, 1, 2])])
+def test_prefix_under_a_window(ubp, D, G, Hkv, new):
+    """Windows that leave enough of a prefix for a call of its own, and shorter ones, under which each sequence reads its own part."""
+    prefix = 120 * 10 ** 6 // (8 * Hkv * D * 4) + 2000
+    lengths = [prefix + [40, 3, 0, 1, 200, 700, 129, 64, 2][s] for s in range(9)]
+    b = Batch(new, lengths, Hkv * G, Hkv, D, BF16, 64, prefix=prefix, seed=D)
+    q, c = b.queries(), described(b)
+    size = lambda window: ubp.load().ubp_attention_workspace_size(ctypes.byref(c), q.data_ptr(), q.stride(0), q.stride(1), b.T, Hkv * G, window, 0, prefix, max(new))
+    assert size(prefix - 100) > b.T * Hkv * G * D * 4 + size(100)        # (a call of its own leaves a row of sums for each query)
+    for window, sinks in ((prefix - 100, 3), (prefix + 50, 0), (prefix // 2, 70), (100, 70)):
+        want, tol = b.exact(q, window, sinks)
+        check(ubp.ubp_prefix_attention(q, *b.args(), prefix, starts=b.starts, max_new=max(new), window=window, sinks=sinks), want, tol, b.T)
