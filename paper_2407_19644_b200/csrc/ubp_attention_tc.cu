@@ -9,6 +9,12 @@
 // through shared memory. (Two threads a row, eight warps a tile: 5 % slower, the halves wait for one another in every step.)
 // One warp issues the products, three the copies: a page of the cache is a TMA box (64 values x tokens), in the 128-byte swizzle, so
 // that K is the K-major and V the MN-major operand as they lie in the cache.
+// Measured on a prompt of 8192 (3100 to 3600 cycles a step; the products are 2048 of them): a tile's softmax takes 2000 -- 370 to
+// bring the scores, 290 for the maximum, 1360 for the weights, with the special function unit busy for 1024 for each of the two
+// tiles -- and then its next scores are 1100 away: the end of its product with V, and its product with K, behind the other tile's.
+// In long runs the card reports its power limit. Tried: scores in two halves of 64 keys that are ready ahead (a product of 64
+// columns takes 48 cycles, not 32: 9 to 20 % slower); the maximum beside weights by the old reference, repeated if that will not
+// do (no difference); a part of the exponentials as polynomials (no difference, more of them slower).
 // O is rescaled only when a score lies more than 2^8 above the row's reference (weights stay below 2^8, sums far from overflow);
 // the sum over the weights takes them before they are rounded to 16 bits.
 // Steps are dealt to the blocks as in ubp_attention.h: one block an SM, the same number of key tiles for each.
@@ -44,7 +50,9 @@ static_assert(sizeof(AttnPlace<AT_THREADS>) <= 8 * AT_TURN, "lies there until th
 
 // N steps of 16 along the reduction: D (tensor memory) (+)= A B, A from shared memory, or the 16-bit values of tensor memory from
 // column `a` on. The whole warp calls with equal arguments, one elected lane issues: from a branch of a single lane the operands
-// had to be made uniform one by one, 120 cycles a product instead of the 64 that it takes.
+// had to be made uniform one by one, 120 cycles a product instead of the 64 that it takes. Few products wait in the tensor cores'
+// queue, so what the issuing warp does between them is time lost: see `uniform`. (Two issuing warps, one a tile: their products
+// interleave, both tiles wait for both: 12 to 25 % slower.)
 #define AT_MMA_BEGIN "{\n\t.reg .pred pe, pa, pt;\n\t.reg .b64 x, y;\n\t.reg .b32 z;\n\telect.sync _|pe, 0xffffffff;\n\tsetp.ne.b32 pa, %4, 0;\n\tsetp.eq.b32 pt, 0, 0;\n\t"
 #define AT_MMA_SS(X, Y, P) "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], " X ", " Y ", %3, " P ";\n\t"
 #define AT_MMA_TS(X, Y, P) "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [" X "], " Y ", %3, " P ";\n\t"
@@ -118,6 +126,11 @@ struct AtBars {
     uint64_t k_full[4], k_empty[4], v_full[4], v_empty[4], patch, drain;
 };
 
+// A value that all lanes of a warp have, so that the compiler knows: the issuing warp's loops, addresses and descriptors are then
+// computed once a warp and not once a lane, and need no exchange before each product (in turn on one card: a prompt of 16384 under a
+// window 986 -> 938 us, continuations 276 -> 268, ragged prompts 39.9 -> 37.6).
+__device__ __forceinline__ int uniform(int x) { return __shfl_sync(0xffffffffu, x, 0); }
+
 // Segments of a block's steps: consecutive tiles of one item.
 struct AtSegments {
     AttnSteps s;
@@ -144,7 +157,7 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
     __shared__ __align__(8) AtBars bars;
     __shared__ uint32_t tmem_slot;
     __shared__ int abort_flag;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = uniform((int)threadIdx.x >> 5), lane = threadIdx.x & 31;
 
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (threadIdx.x == 0) {
@@ -177,7 +190,7 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
     tmem_before();
     __syncthreads();
     tmem_after();
-    const uint32_t tmem = tmem_slot;
+    const uint32_t tmem = (uint32_t)uniform((int)tmem_slot);
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
     constexpr uint32_t TURN = (2 + 2 * ST) * PART;
@@ -279,8 +292,8 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                 commit_one(smem_u32(&bars.k_empty[ks]));
                 if (++ks == ST) { ks = 0; k_phase ^= 1u; }
             };
-            for (; ok && sg.get(); sg.done(a)) {
-                const int nt = sg.two(a) ? 2 : 1;
+            for (; ok && uniform(sg.get()); sg.done(a)) {
+                const int nt = uniform(sg.two(a) ? 2 : 1), steps = uniform(sg.n);
                 wait(bars.k_full[ks], k_phase);
                 for (int i = 0; ok && i < nt; ++i) {
                     wait(bars.q_full[i], q_phase[i]);
@@ -288,12 +301,12 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                     q_phase[i] ^= 1u;
                     tmem_after();
                     scores(i);
-                    if (sg.n == 1) commit_one(smem_u32(&bars.q_empty[i]));
+                    if (steps == 1) commit_one(smem_u32(&bars.q_empty[i]));
                 }
                 if (!ok) break;
                 next_keys();
-                for (int j = 0; ok && j < sg.n; ++j) {
-                    const bool more = j + 1 < sg.n;
+                for (int j = 0; ok && j < steps; ++j) {
+                    const bool more = j + 1 < steps;
                     wait(bars.v_full[vs], v_phase);
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
@@ -314,7 +327,7 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                             if (i == 0) wait(bars.k_full[ks], k_phase);
                             if (!ok) break;
                             scores(i);
-                            if (j + 2 == sg.n) commit_one(smem_u32(&bars.q_empty[i]));
+                            if (j + 2 == steps) commit_one(smem_u32(&bars.q_empty[i]));
                         }
                     }
                     if (!ok) break;
