@@ -12,7 +12,8 @@
 // An item counts for `extra` steps more than its tiles: what its beginning and end take. Without them, blocks that got many short
 // items (the first rows of a prompt, short sequences of a batch) took twice as long as the others. (With the heads inside the row
 // blocks, prompts of eight key heads ran at 757 TFLOP/s instead of 1197: the blocks at work then read eight times as many
-// different keys at a time.) For few sequences and short work a cluster of blocks takes all of an item instead.
+// different keys at a time.) For few sequences and short work a cluster of blocks takes all of an item instead; items of 256 rows with few
+// tiles are left whole.
 #ifndef UBP_ATTENTION_H_
 #define UBP_ATTENTION_H_
 
@@ -47,6 +48,7 @@ struct AttnArgs {
     int tpt;                        // tokens a row block takes
     int bsh;                        // keys a step takes: 1 << bsh
     int extra;                      // steps that an item counts for beside its tiles
+    int whole;                      // 1: items are not cut; a block takes those that begin in its share
     float sc;                       // scale * log2(e)
     int window, sinks;
     int kv0, kv1;                   // keys outside [kv0, kv1) are left out (a shared prefix is a call of its own)
@@ -139,18 +141,22 @@ struct AttnCursor {
     }
 };
 
-// The steps of a block that are left: a cursor at the next tile, and how many steps its share still holds (extras included).
+// The steps of a block that are left: a cursor at the next tile, and how many steps its share still holds (extras included; if
+// items are not cut, all tiles of the last item that begins in it).
 struct AttnSteps {
     AttnCursor c;
     int left;
     UBP_HD void seek(const AttnArgs &a)             // a share may begin in an item's extras
     {
-        if (left > 0 && c.tile >= c.t.nt) skip(a);
+        if (left > 0 && (c.tile >= c.t.nt || (a.whole && c.tile > 0))) skip(a);
+        else if (a.whole) left = imax(left, left > 0 ? c.t.nt : 0);
     }
     UBP_HD void skip(const AttnArgs &a)             // the rest of the item's steps
     {
         left -= c.t.nt + a.extra - c.tile;
-        if (left > 0) c.next_item(a);
+        if (left <= 0) return;
+        c.next_item(a);
+        if (a.whole) left = imax(left, c.t.nt);
     }
     UBP_HD int tiles() const { return imin(c.t.nt - c.tile, left); }      // of the item, in this share
     UBP_HD void advance(const AttnArgs &a, int n)   // past n tiles

@@ -78,6 +78,15 @@ constexpr double ATTN_PREFIX_BYTES = 120e6;
 // 4000 (eight tiles) 16.9 / 16.8; twelve of 500 (one block each) 9.8 / 12.9; 100 of 700 keys on one head of 64 values 7.9 / 11.9.
 constexpr int64_t ATTN_CLUSTER_BLOCKS = 120, ATTN_CLUSTER_TILES = 6;
 
+// Items of at most this many tiles (of 256 rows, of 16 rows), by the longest that the table or the window allows, are not cut: the most
+// that a block then has to do more than the others is one item, and cuts cost about as much (segments' ends, partial results, the
+// join). Left whole / cut, us, 32 heads on 8 of 128 values unless said: 256 rows: 7 prompts of 1 .. 901 on 12 / 4 heads, window 300
+// (7 tiles) 27.7 / 37.7, one of 512 (6) 17.5 / 23.1, one of 16384 with a window of 512 (8) 239 / 282, 4096 with 1024 (12) 100.6 / 100.1,
+// 1400 (13) 36.7 / 42.4, 20 of 100 on up to 1600 (14) 65.7 / 75.6, 8 of them 43.8 / 43.1, 2000 and 1500 on 16 / 4 heads (17) 54.0 /
+// 51.1, 8192 (66) 562 / 511. 16 rows: 64 tokens on up to 400 keys (5) 24.1 / 25.8, 17 on 500 (6) 10.3 / 13.9, 32 with a window of 512 (8)
+// 22.2 / 24.6, 64 on 900 (9) 37.3 / 36.8, 32 on 1500 (13) 34.1 / 26.3.
+constexpr int64_t ATTN_WHOLE_TILES = 14, ATTN_WHOLE_FEW = 8;
+
 // A call's kernels, grids and the layout of its workspace; the same for the size query and the call.
 struct AttnCall {
     AttnArgs own, common;
@@ -113,9 +122,8 @@ int attn_plan(const ubp_cache_t *c, const void *q, int64_t q_ts, int64_t q_hs, i
     // (the kernels count the steps of a unit head, and a block's, in 32 bits)
     if (items / a.HU > INT32_MAX / tiles || ((a.cap >> a.bsh) + 2) > INT32_MAX / a.HU || items * tiles / sms >= INT32_MAX) return UBP_E_UNSUPPORTED;
     p.own_grid = (int)std::min<int64_t>(sms, items * tiles);
-    p.own_space = attn_space(p.own_grid, 2 * (int64_t)p.own_grid, a.rows, a.D);
     if (!on(q, 16) || (T > 1 && q_ts % 8) || (q_heads > 1 && q_hs % 8)) p.q_bytes = ((size_t)T * q_heads * a.D * 2 + 255) / 256 * 256;
-    p.bytes = p.own_space.total + p.q_bytes;
+    p.bytes = p.q_bytes;
     // A shared prefix is read for all sequences at once only where reading it again for each -- what a window leaves of it -- takes
     // longer than that saves.
     const double each = window > 0 ? std::min<double>((double)prefix, (double)window + sinks) : (double)prefix;
@@ -128,7 +136,12 @@ int attn_plan(const ubp_cache_t *c, const void *q, int64_t q_ts, int64_t q_hs, i
         while (size > 1 && units * size > ATTN_CLUSTER_BLOCKS) size /= 2;
         if (units * size <= ATTN_CLUSTER_BLOCKS && reach <= (int64_t)ATTN_CLUSTER_TILES * size) p.cluster = size;
     }
-    if (p.cluster) { p.own_space = AttnSpace{}; p.bytes = p.q_bytes; }
+    const int64_t reach = ((prefix > 0 && !again ? std::min(seen, a.cap - prefix) : seen) >> a.bsh) + 2;
+    const bool whole = reach <= (p.own_tc ? ATTN_WHOLE_TILES : ATTN_WHOLE_FEW);
+    if (!p.cluster && !whole) {
+        p.own_space = attn_space(p.own_grid, 2 * (int64_t)p.own_grid, a.rows, a.D);
+        p.bytes += p.own_space.total;
+    }
     if (prefix > 0 && !again) {
         AttnArgs b = a;
         b.common = 1;
@@ -147,6 +160,7 @@ int attn_plan(const ubp_cache_t *c, const void *q, int64_t q_ts, int64_t q_hs, i
     }
     p.has_common = prefix > 0 && !again;
     p.own = a;
+    p.own.whole = whole;
     return UBP_OK;
 }
 
@@ -226,7 +240,7 @@ extern "C" int ubp_attention(const ubp_cache_t *cache, const void *q, int64_t q_
         if (const int rc = launch_attn_join(p.common, cache->dtype, p.common_grid, stream)) return rc;
     }
     if (const int rc = (p.own_tc ? launch_attn_tc : launch_attn_few)(p.own, cache->dtype, p.own_grid, stream)) return rc;
-    return launch_attn_join(p.own, cache->dtype, p.own_grid, stream);
+    return p.own.whole ? UBP_OK : launch_attn_join(p.own, cache->dtype, p.own_grid, stream);
 }
 
 extern "C" int ubp_attention_check(void *stream)

@@ -158,7 +158,7 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
         steps.c.tile = tiles * rank / size;
         steps.left = tiles * (rank + 1) / size - steps.c.tile;
     } else if (!attn_locate<FEW_WARPS * 32>(a, *reinterpret_cast<AttnPlace<FEW_WARPS * 32> *>(meet), deal, steps)) {
-        if (threadIdx.x == 0 && !a.common) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
+        if (threadIdx.x == 0 && !a.common && !a.whole) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
         return;
     }
     const AttnCursor &cur = steps.c;
@@ -399,7 +399,7 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
         over = cur.tile + 1 == cur.t.nt || steps.left == 1;
         if (!over) steps.advance(a, 1);
     }
-    if (!CLUSTER && threadIdx.x == 0 && !a.common && !described) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
+    if (!CLUSTER && threadIdx.x == 0 && !a.common && !a.whole && !described) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
     if (!ok) {                              // copies that are still under way end before the block does (a millisecond at most each)
         int gave_up = 0;
         for (int i = 0; i < ST; ++i)

@@ -510,7 +510,7 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
             if (warp == AT_SOFT_WARP && lane == 0 && !a.common && sg.s.c.tile == 0 && !complete) { attn_describe(a, sg.s.c, deal, c, x, 0, sg.n); described = true; }
             sg.done(a);
         }
-        if (warp == AT_SOFT_WARP && lane == 0 && !a.common && !described) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
+        if (warp == AT_SOFT_WARP && lane == 0 && !a.common && !a.whole && !described) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
     }
     if (!ok && lane == 0) atomicExch(a.status, 1);
     tmem_before();

@@ -257,11 +257,12 @@ def test_refusals(ubp):
     q256 = torch.zeros(2, 4, 136, device="cuda", dtype=BF16)
     k256, v256 = (torch.zeros(3, 2, 16, 136, device="cuda", dtype=BF16) for _ in range(2))
     small = torch.zeros(256, dtype=torch.uint8, device="cuda")
+    off = torch.zeros(2 * 4 * 64 + 1, dtype=BF16, device="cuda")[1:].view(2, 4, 64)      # (copied to the workspace first)
     for f, code in ((lambda: ubp.ubp_attention(q, k, v, t, n, scale=0.0), -1), (lambda: ubp.ubp_attention(q, k, v, t, n, scale=float("nan")), -1),
                     (lambda: ubp.ubp_attention(q, k, v, t, n, max_new=0), -1), (lambda: ubp.ubp_attention(q, k7, v7, t, n), -6),
                     (lambda: ubp.ubp_attention(q9, k9, v9, t, n), -6), (lambda: ubp.ubp_attention(q256, k256, v256, t, n), -6),
                     (lambda: ubp.ubp_attention(q, ko, vo, t, n), -1), (lambda: ubp.ubp_prefix_attention(q, k, v, t, n, -1), -1),
-                    (lambda: ubp.ubp_prefix_attention(q, k, v, t, n, 16 * t.shape[1] + 1), -1), (lambda: ubp.ubp_attention(q.repeat(20, 1, 1), k, v, t, n, starts=torch.tensor([0, 20, 40], dtype=torch.int32, device="cuda"), workspace=small), -3)):
+                    (lambda: ubp.ubp_prefix_attention(q, k, v, t, n, 16 * t.shape[1] + 1), -1), (lambda: ubp.ubp_attention(off, k, v, t, n, workspace=small), -3)):
         with pytest.raises(ubp.UbpError) as e:
             f()
         assert e.value.code == code

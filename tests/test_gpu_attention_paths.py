@@ -232,3 +232,27 @@ def test_prefix_under_a_window(ubp, D, G, Hkv, new):
     for window, sinks in ((prefix - 100, 3), (prefix + 50, 0), (prefix // 2, 70), (100, 70)):
         want, tol = b.exact(q, window, sinks)
         check(ubp.ubp_prefix_attention(q, *b.args(), prefix, starts=b.starts, max_new=max(new), window=window, sinks=sinks), want, tol, b.T)
+
+
+@pytest.mark.parametrize("new,old,window,prefix,whole", [
+    ([1, 5, 0, 300, 90, 2] * 4, [0, 700, 30, 400, 1, 90] * 4, 0, 0, True), ([200, 31, 600], [1000, 1500, 936], 0, 0, True),
+    ([200, 31, 600], [1000, 1700, 936], 0, 0, False), ([1500, 1, 0, 700], [0, 9000, 3, 20], 1000, 0, True), ([3] * 7, [1, 9, 300, 0, 2, 30, 31], 0, 70000, True),
+    ([1] * 150, [n * 17 % 600 for n in range(150)], 0, 0, True), ([1] * 400, [n * 13 % 700 for n in range(400)], 0, 0, True),
+    ([1] * 60, [1900] * 60, 0, 0, False), ([1] * 70, [n * 170 for n in range(70)], 300, 0, True), ([1] * 40, [n * 9 for n in range(40)], 0, 20000, True)])
+def test_short_items_are_not_cut(ubp, new, old, window, prefix, whole):
+    """Calls of short items need no partial results: their blocks take whole items, wherever the lengths put the shares' ends."""
+    b = Batch(new, [prefix + n + o for n, o in zip(new, old)], 8, 2, 128, BF16, 32, seed=len(new), prefix=prefix, behind=0 if max(new) == 1 else 2, single=max(new) == 1)
+    q = b.queries()
+    c = described(b)
+    size = lambda sinks, w: ubp.load().ubp_attention_workspace_size(ctypes.byref(c), q.data_ptr(), q.stride(0), q.stride(1), b.T, 8, w, sinks, prefix, max(new))
+    if not prefix:
+        assert (size(0, window) == 0) == whole
+    for sinks in (0, 3) if window else (0,):
+        want, tol = b.exact(q, window, sinks)
+        fn, args = (ubp.ubp_prefix_attention, b.args() + (prefix,)) if prefix else (ubp.ubp_attention, b.args())
+        out = torch.full((b.T, 8, 128), -77.0, dtype=BF16, device="cuda")
+        fn(q, *args, starts=b.starts, window=window, sinks=sinks, max_new=max(new), out=out)
+        check(out, want, tol, b.first[-1])
+        assert (out[b.first[-1]:] == -77.0).all()
+        again = fn(q, *args, starts=b.starts, window=window, sinks=sinks, max_new=max(new), out=torch.full_like(out, -77.0))
+        assert torch.equal(again, out)
