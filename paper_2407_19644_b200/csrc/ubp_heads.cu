@@ -8,7 +8,7 @@
 // all its heads. A thread holds two 16-byte pieces of a head that are rotated into one another, so that no pair needs another
 // thread; D / 16 threads share a head, and their part of the rotation stays in registers from head to head. Statistics, rotation
 // and products are fp32, each value is rounded once.
-// Measured: 16384 tokens of 48 heads of 128 values with norms 73 us, 5.6 TB/s; 1531 tokens of 20 heads of 80 in rows off 16 bytes 7.6
+// Measured: 16384 tokens of 48 heads of 128 values with norms 73 us, 5.6 TB/s; 1531 tokens of 20 heads of 80 in rows off 16 bytes 6.6
 // us; one token of 48 heads 2.3.
 #include <cuda_runtime.h>
 
@@ -100,7 +100,9 @@ template <typename T> __device__ __forceinline__ uint4 packed(const uint64_t (&v
 constexpr int HEADS_BLOCKS = 6;         // an SM holds
 // TPH: threads a head (a power of two, D / 16 of them at work). A block takes consecutive tokens, whose sequence and position
 // follow from one another, and its groups of TPH threads a token's heads in turns, AHEAD of a group's together.
-// STAGED: rows of qkv off 16 bytes come through shared memory, element by element, so that everything behind is the same.
+// STAGED: rows of qkv off 16 bytes come through shared memory, whole 16-byte lines of memory (all of a turn's under way together)
+// and single elements at the ends, so that everything behind is the same (all elements singly: 7.6 us where it takes 6.6; with three
+// heads of a group together, whose lines do not fit the registers, 9.4).
 template <typename T, int TPH, bool INTER, bool STAGED, int AHEAD>
 __global__ void __launch_bounds__(128, HEADS_BLOCKS) ubp_heads_kernel(const HeadArgs a, const int per)
 {
@@ -120,9 +122,26 @@ __global__ void __launch_bounds__(128, HEADS_BLOCKS) ubp_heads_kernel(const Head
         const T *row = static_cast<const T *>(a.qkv) + t * a.ld;
         if constexpr (STAGED) {
             const int first = h0 * a.D, n = imin(AHEAD * GROUPS, H - h0) * a.D;
+            const T *const src = row + first;
+            const int head = imin(n, (int)((16 - (reinterpret_cast<uintptr_t>(src) & 15)) & 15) / 2), body = (n - head) / 8, rest = n - head - 8 * body;
+            constexpr int V = (AHEAD * GROUPS * TPH * 16 / 8 + 127) / 128;
+            uint4 w[V];
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if ((int)threadIdx.x + i * 128 < body) w[i] = reinterpret_cast<const uint4 *>(src + head)[threadIdx.x + i * 128];
+            const int edge = (int)threadIdx.x < head ? (int)threadIdx.x : head + 8 * body + (int)threadIdx.x - head;
+            uint16_t x = 0;
+            if ((int)threadIdx.x < head + rest) x = reinterpret_cast<const uint16_t *>(src)[edge];
             __syncthreads();
-#pragma unroll 8
-            for (int i = (int)threadIdx.x; i < n; i += 128) stage[i] = row[first + i];
+#pragma unroll
+            for (int i = 0; i < V; ++i)
+                if ((int)threadIdx.x + i * 128 < body) {
+                    uint16_t *const to = reinterpret_cast<uint16_t *>(stage) + head + 8 * ((int)threadIdx.x + i * 128);
+                    const uint32_t u[4] = {w[i].x, w[i].y, w[i].z, w[i].w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) { to[2 * k] = (uint16_t)u[k]; to[2 * k + 1] = (uint16_t)(u[k] >> 16); }
+                }
+            if ((int)threadIdx.x < head + rest) reinterpret_cast<uint16_t *>(stage)[edge] = x;
             __syncthreads();
         }
 #pragma unroll
@@ -323,7 +342,7 @@ template <typename T> int launch_heads(const HeadArgs &a, int kind, void *stream
         }
         const int per = (a.T + HEADS_BLOCKS * sms - 1) / (HEADS_BLOCKS * sms);
         const dim3 g((unsigned)((a.T + per - 1) / per));
-        return kind == 2 ? launch(ubp_heads_kernel<T, P, I, false, 3>, g, stream, a, per) : launch(ubp_heads_kernel<T, P, I, true, 3>, g, stream, a, per);
+        return kind == 2 ? launch(ubp_heads_kernel<T, P, I, false, 3>, g, stream, a, per) : launch(ubp_heads_kernel<T, P, I, true, 2>, g, stream, a, per);
     };
     auto by_size = [&](auto inter) { return a.D <= 64 ? by(std::integral_constant<int, 4>{}, inter) : by(std::integral_constant<int, 8>{}, inter); };
     return a.interleaved ? by_size(std::true_type{}) : by_size(std::false_type{});
