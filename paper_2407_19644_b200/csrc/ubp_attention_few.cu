@@ -13,7 +13,7 @@
 // values, 1.14 GB, take 182 us with the join, 6.3 TB/s; three tokens on 100000 keys of two heads of 64 values, 0.15 GB, 34 us.
 // Pages that no row of the item sees, or that the cache does not have, are out of range for the copy and come as zeros; values of
 // unseen keys within a page are overwritten with zeros, so that nothing an unused slot holds reaches a result. The weights are
-// rounded to 16 bits for the second product (relative 2^-9 / 2^-12 each, the sum of weights is of the unrounded ones); scores,
+// rounded to 16 bits for the second product (relative 2^-8 / 2^-11 each, the sum of weights is of the unrounded ones); scores,
 // references, sums and outputs are fp32 until the end.
 #include <cuda.h>
 #include <cuda_runtime.h>
@@ -364,11 +364,12 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
                 mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 1));
                 mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 2)) * a.sc;
             }
-            // The reference only moves when a score lies more than 2^8 above it: weights stay below 2^8, sums far from overflow.
-            if (__any_sync(0xffffffffu, mx[0] > m[0] + 8.f || mx[1] > m[1] + 8.f)) {
+            // (the reference: see AttnRef)
+            constexpr float LIFT = AttnRef<T>::lift, LAG = AttnRef<T>::lag;
+            if (__any_sync(0xffffffffu, mx[0] > m[0] + (LIFT + LAG) || mx[1] > m[1] + (LIFT + LAG))) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const float to = fmaxf(m[i], mx[i]), f = m[i] == -INFINITY ? 0.f : attn_exp2(m[i] - to);
+                    const float to = fmaxf(m[i], mx[i] - LIFT), f = m[i] == -INFINITY ? 0.f : attn_exp2(m[i] - to);
                     m[i] = to;
                     l[i] *= f;
 #pragma unroll

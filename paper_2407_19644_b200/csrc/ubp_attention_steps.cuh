@@ -14,6 +14,16 @@ __device__ __forceinline__ float attn_exp2(float x)
     return y;
 }
 
+// A row's reference m lies `lift` below a score that was its largest at some time (in powers of two), and only moves when a score is
+// more than `lag` above that one, so that sums are rarely rescaled: weights 2^(s - m) stay below 2^(lift + lag), and the largest is
+// 2^lift or more. In bf16 a weight has the same relative error wherever it lies. f16 has 2^-24 as its smallest step, and the sum of
+// weights takes them unrounded: with the reference at the largest score, a first token far above the rest whose value is near 0
+// (8192 keys, scores N(0, 1), the first one 14 / 16 / 18 above 0) left relative errors of 0.008 / 0.05 / 0.3; 2^7 higher, 0.0004 /
+// 0.0006 / 0.0044, where unrounded weights give 0.0002 / 0.0006 / 0.0040 (the outputs' rounding). 2^12 leaves f16 a factor of 2^4 below its
+// overflow for the rounding of very large scores (one unit of theirs where they are 2^24).
+template <typename T> struct AttnRef { static constexpr float lift = 0.f, lag = 8.f; };
+template <> struct AttnRef<__half> { static constexpr float lift = 7.f, lag = 5.f; };
+
 // Shared memory of attn_locate, for blocks of NT threads.
 template <int NT> struct AttnPlace { int warp[2][32]; int pre[NT + 1]; int b, rt, before, from, to; };
 

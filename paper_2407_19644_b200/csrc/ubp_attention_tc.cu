@@ -15,8 +15,8 @@
 // In long runs the card reports its power limit. Tried: scores in two halves of 64 keys that are ready ahead (a product of 64
 // columns takes 48 cycles, not 32: 9 to 20 % slower); the maximum beside weights by the old reference, repeated if that will not
 // do (no difference); a part of the exponentials as polynomials (no difference, more of them slower).
-// O is rescaled only when a score lies more than 2^8 above the row's reference (weights stay below 2^8, sums far from overflow);
-// the sum over the weights takes them before they are rounded to 16 bits.
+// O is rescaled only when a score lies far enough above the row's reference (AttnRef: weights stay below 2^8, 2^12 in f16, sums far from
+// overflow); the sum over the weights takes them before they are rounded to 16 bits.
 // Steps are dealt to the blocks as in ubp_attention.h: one block an SM, the same number of key tiles for each.
 #include <cuda.h>
 #include <cuda_runtime.h>
@@ -458,8 +458,9 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                 }
                 // (a row that does not exist holds whatever was there: it has no say in when the others' sums are rescaled)
                 const float top = row.token >= 0 ? fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * a.sc : -INFINITY;
-                if (__any_sync(0xffffffffu, top > m + 8.f)) {
-                    const float to = fmaxf(m, top), f = m == -INFINITY ? 0.f : attn_exp2(m - to);
+                constexpr float LIFT = AttnRef<T>::lift, LAG = AttnRef<T>::lag;
+                if (__any_sync(0xffffffffu, top > m + (LIFT + LAG))) {
+                    const float to = fmaxf(m, top - LIFT), f = m == -INFINITY ? 0.f : attn_exp2(m - to);
                     m = to;
                     l *= f;
                     if (j > 0) {
