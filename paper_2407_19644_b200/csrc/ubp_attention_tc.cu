@@ -402,7 +402,7 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                     };
                     uint32_t o[2][32], w[32];
                     if (complete) {
-                        const float scale = l == 0.f ? 0.f : 1.f / l;
+                        const float scale = attn_scale(l);
 #pragma unroll 1
                         for (int d = 0; d < a.D; d += 64) {
                             tmem_ld32(t_o + (uint32_t)d, o[0]);
@@ -410,7 +410,8 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                             tmem_wait_ld();
 #pragma unroll
                             for (int e = 0; e < 32; ++e)
-                                w[e] = pack2<T>(__uint_as_float(o[e / 16][2 * e & 31]) * scale, __uint_as_float(o[e / 16][(2 * e & 31) + 1]) * scale);
+                                w[e] = pack2<T>(attn_scaled(__uint_as_float(o[e / 16][2 * e & 31]), scale),
+                                                attn_scaled(__uint_as_float(o[e / 16][(2 * e & 31) + 1]), scale));
                             store(w, d * 2, (a.D - d) * 2);
                         }
                     } else {
