@@ -509,7 +509,8 @@ typedef struct {
  *     (u_i, u_j) -> (u_i c_i - u_j s_i, u_j c_i + u_i s_i)        query and key heads, i < rotated / 2
  * with j = i + rotated / 2, or pairs (2 i, 2 i + 1) if interleaved; values from `rotated` on pass. c and s are row p of `rotation`
  * (device fp32, `positions` rows of rotated / 2 cosines and rotated / 2 sines; NULL: no rotation), p the token's position in its
- * sequence. The queries go to q (any strides; may be the queries' own place in qkv), keys and values to their places in the cache.
+ * sequence. The queries go to q (any strides), keys and values to their places in the cache. q may be the queries' own place in qkv
+ * (same start and strides); otherwise it must not overlap qkv (UBP_E_ARG; so does a q among qkv's rows with another stride).
  * gammas have the cache's type. Arithmetic is fp32, each value is rounded once; eps as in ubp_rmsnorm. A token whose position is
  * negative or has no row in the rotation is not appended and its queries are 0; one behind the table's end is not appended. Two
  * tokens with one place (a page given to two sequences) leave either's values. */

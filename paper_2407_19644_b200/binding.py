@@ -746,7 +746,7 @@ def ubp_rotate_append(qkv, q_heads: int, k_cache, v_cache, page_table, lengths, 
                       q_gamma=None, k_gamma=None, eps: float = 1e-6, out=None, stream=None):
     """Rows of a query, key and value projection, qkv [T][(q_heads + 2 kv heads) * head size], into queries and a paged cache: norm of
     each query and key head (where a gamma [head size] is given), position rotation, append. Returns the queries [T][q_heads][head
-    size]; `out` may be their own place in qkv.
+    size]; `out` may be their own place in qkv, and must not overlap it otherwise.
     k_cache, v_cache: bfloat16 or float16 [pages][kv heads][page size][head size], with equal strides. page_table: int32
     [sequences][pages of a sequence]; lengths: int32 [sequences], the new tokens among them; starts: int32 [sequences + 1], the rows
     of sequence b are starts[b] .. starts[b + 1] - 1 and hold its last tokens (None: one new token a sequence). Rows from

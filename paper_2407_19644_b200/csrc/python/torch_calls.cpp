@@ -356,6 +356,8 @@ PyObject *rotate_append(PyObject *, PyObject *const *a, Py_ssize_t n)
                    ", an even number of them up to the head size");
         int64_t ts = Hq * D, hs = D;
         if (out) heads(*out, "out", T, Hq, D, type, dev, ts, hs);
+        if (out && T > 0 && out->data_ptr() == qkv->data_ptr() && ((T > 1 && ts != ld) || (Hq > 1 && hs != D)))
+            refuse("out starts at qkv's place but is not the queries' own place in it");
         On on(dev, a[13]);
         at::Tensor q;
         if (!out) q = make(T, Hq, D, type, dev);

@@ -200,6 +200,39 @@ inline AttnSpace attn_space(int64_t grid, int64_t slots, int rows, int D)
     return s;
 }
 
+// ---- places of operands. Heads of T tokens: n pieces of w 16-bit elements a token, hs apart, tokens ts apart (a stride that is never
+// used may be anything).
+struct HeadPlaces {
+    const void *p;
+    int64_t ts, hs, n, w;
+    HeadPlaces(const void *p_, int64_t ts_, int64_t hs_, int64_t n_, int64_t w_) : p(p_), ts(ts_), hs(hs_), n(n_), w(w_)
+    {
+        if (hs == w) { w *= n; n = 1; }
+    }
+    int64_t end(int64_t T) const { return (T > 1 ? (T - 1) * ts : 0) + (n > 1 ? (n - 1) * hs : 0) + w; }
+};
+// whether pieces of w and v elements, the first x behind the second, meet for some two of T tokens
+inline bool pieces_meet(int64_t x, int64_t w, int64_t v, int64_t ts, int64_t T)
+{
+    if (T == 1) return x > -w && x < v;
+    const int64_t y = -w - x;                                      // the first i with x + i ts > -w, of -(T - 1) .. T - 1
+    int64_t i = (y >= 0 ? y / ts : -((-y + ts - 1) / ts)) + 1;
+    if (i < 1 - T) i = 1 - T;
+    return i < T && x + i * ts < v;
+}
+// Whether an element of a is one of b, of any two tokens. Where they lie among one another with different strides between tokens, that
+// counts as if it were so.
+inline bool places_meet(const HeadPlaces &a, const HeadPlaces &b, int64_t T)
+{
+    const int64_t d = (static_cast<const char *>(a.p) - static_cast<const char *>(b.p)) / 2;
+    if (d >= b.end(T) || -d >= a.end(T)) return false;
+    if (T > 1 && a.ts != b.ts) return true;
+    for (int64_t h = 0; h < a.n; ++h)
+        for (int64_t g = 0; g < b.n; ++g)
+            if (pieces_meet(d + h * a.hs - g * b.hs, a.w, b.w, a.ts, T)) return true;
+    return false;
+}
+
 // ---- launches; both kernels follow the same scheme and leave the same partial results
 int launch_attn_few(const AttnArgs &a, int dtype, int grid, void *stream);       // 16 rows an item (ubp_attention_few.cu)
 int launch_attn_cluster(const AttnArgs &a, int dtype, int size, void *stream);    // the same, a cluster of blocks a sequence and unit head

@@ -1,0 +1,24 @@
+"""The C entry points of the attention operators refuse outputs over inputs, without a GPU."""
+import ctypes
+
+import pytest
+
+import paper_2407_19644_b200 as ubp
+from test_attention_host import APPEND, P, cache
+
+D, ROW = 64, 8 * 64          # a row of 4 query heads, 2 key heads and 2 value heads
+
+
+def call(fn, base, c=None, **at):
+    a = list(base)
+    a[0] = ctypes.byref(c or cache())
+    for i, v in at.items():
+        a[int(i[1:])] = v
+    return fn(*a)
+
+
+# place of the queries behind qkv, in elements, and their strides
+@pytest.mark.parametrize("place,ts,hs", [(0, 4 * D, D), (0, ROW, 2 * D), (D, ROW, D), (4 * D, ROW, D), (7 * D, ROW, D), (ROW, ROW, D), (-D, ROW, D), (-ROW, ROW, D),
+                                         (2 * ROW, 4 * D, D), (8, 4 * D, D)])
+def test_queries_over_rows(place, ts, hs):
+    assert call(ubp.load().ubp_rotate_append, APPEND, _13=P + 2 * place, _14=ts, _15=hs) == -1

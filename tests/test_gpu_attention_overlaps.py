@@ -1,0 +1,65 @@
+"""Outputs that lie over inputs: refused where rows would be read after they were written, allowed otherwise."""
+import pytest
+import torch
+
+from attention_ref import BF16, Batch
+
+pytestmark = pytest.mark.gpu
+
+HQ, HKV, D = 4, 2, 64
+
+
+@pytest.fixture(scope="module")
+def ubp():
+    import paper_2407_19644_b200 as m
+    m.load()
+    return m
+
+
+def buffer(b, cols):
+    return torch.randn(b.T, cols, generator=b.g, device="cuda").to(b.dtype)
+
+
+def code_of(ubp, f):
+    with pytest.raises((ubp.UbpError, ValueError)) as e:
+        f()
+    return e.value.code if isinstance(e.value, ubp.UbpError) else -1
+
+
+@pytest.mark.parametrize("pad", [0, 3])
+def test_append_refuses_queries_over_rows(ubp, pad):
+    b = Batch([70, 30], [70, 40], HQ, HKV, D, BF16, 16)
+    width = (HQ + 2 * HKV) * D
+    whole = buffer(b, width + pad)
+    qkv = whole[:, :width]
+    heads = lambda start, ts, hs: whole.view(-1)[start:].as_strided((b.T, HQ, D), (ts, hs, 1))
+    keep = whole.clone(), b.k.clone().view(torch.int16)
+    for out in (heads(0, HQ * D, D), heads(0, width + pad, 2 * D), heads(D, width + pad, D), heads(HQ * D, width + pad, D), heads(HQ * D, HQ * D, D)):
+        assert code_of(ubp, lambda: ubp.ubp_rotate_append(qkv, HQ, *b.args(), starts=b.starts, out=out)) == -1
+    less = torch.tensor([0, 70, 99], dtype=torch.int32, device="cuda")
+    up = whole[1:, :HQ * D].unflatten(1, (HQ, D))              # the queries' places of the rows behind
+    assert code_of(ubp, lambda: ubp.ubp_rotate_append(qkv[:-1], HQ, *b.args(), starts=less, out=up)) == -1
+    assert torch.equal(whole, keep[0]) and torch.equal(b.k.view(torch.int16), keep[1])
+    with pytest.raises(ValueError):
+        ubp.ubp_rotate_append(qkv, HQ, *b.args(), starts=b.starts, out=heads(0, HQ * D, D))
+    one = Batch([1], [5], HQ, HKV, D, BF16, 16)                # a single token: heads over other heads
+    row = buffer(one, width)
+    assert code_of(ubp, lambda: ubp.ubp_rotate_append(row, HQ, *one.args(), out=row.view(-1).as_strided((1, HQ, D), (width, 2 * D, 1)))) == -1
+
+
+def test_append_allows_what_lies_apart(ubp):
+    b = Batch([70, 30], [70, 40], HQ, HKV, D, BF16, 16)
+    width, rot = (HQ + 2 * HKV) * D, ubp.rotation_table(100, D)
+    whole = buffer(b, width + HQ * D)
+    run = lambda qkv, out=None: ubp.ubp_rotate_append(qkv, HQ, *b.args(), starts=b.starts, rotation=rot, out=out)
+    want = run(whole[:, :width].clone())
+    beside = whole.clone()                                     # in columns of the same rows, before and behind
+    assert torch.equal(run(beside[:, :width], beside[:, width:].unflatten(1, (HQ, D))), want) and torch.equal(beside[:, :width], whole[:, :width])
+    front = torch.cat([whole[:, width:], whole[:, :width]], 1)
+    assert torch.equal(run(front[:, HQ * D:], front[:, :HQ * D].unflatten(1, (HQ, D))), want)
+    own = whole.clone()                                        # in the queries' own place
+    assert torch.equal(run(own[:, :width], own[:, :HQ * D].unflatten(1, (HQ, D))), want)
+    flat = torch.cat([whole[:, :width].reshape(-1), whole.new_zeros(b.T * HQ * D)])      # one behind the other
+    assert torch.equal(run(flat[:b.T * width].view(b.T, width), flat[b.T * width:].view(b.T, HQ, D)), want)
+    outside = torch.empty(HQ, b.T, D, dtype=BF16, device="cuda")                          # heads outside tokens
+    assert torch.equal(run(whole[:, :width].clone(), outside.transpose(0, 1)), want)
