@@ -525,7 +525,8 @@ int ubp_rotate_append(const ubp_cache_t *cache, const void *qkv, int64_t ld, int
  * fill of a last page through row 0 or the sequence's own; they are read once for all sequences together where that is faster
  * than again for each, and then count as seen by all of them. max_new: most new tokens of a sequence, if the caller knows (else T); only the choice of kernel depends on it.
  * scale > 0. Strides of q and out are between tokens and heads, in elements; heads are contiguous; no alignment beyond the
- * type's (queries off 16 bytes are copied to the workspace first). out must not overlap q or the cache.
+ * type's (queries off 16 bytes are copied to the workspace first). out must not overlap q (UBP_E_ARG; so does an out among q's rows
+ * with another stride between tokens) or the cache.
  * Scores, sums and outputs are fp32 until the end; the weights w_j are rounded to the cache's type for the product with v (f16: those
  * below 2^-21 of the row's largest to steps of 2^-31 of it or finer).
  * Sums run in an order fixed by the lengths: results are bitwise reproducible. What the cache holds outside the tokens that some

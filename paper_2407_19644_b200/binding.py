@@ -765,8 +765,8 @@ def ubp_attention(q, k_cache, v_cache, page_table, lengths, starts=None, window:
     as in ubp_rotate_append, which appends the new tokens first). The query at position p sees the keys j <= p; with a window only
     j > p - window, and the first `sinks` tokens. scale: of the scores, 1 / sqrt(head size) unless given. max_new: the most new
     tokens a sequence has, where the caller knows (a kernel for few rows is taken then; the result does not depend on it).
-    Returns [T][heads][head size]; rows of no sequence are left as they were in `out`. workspace: a CUDA tensor (allocated here when
-    not given). No gradient is recorded."""
+    Returns [T][heads][head size]; rows of no sequence are left as they were in `out`, which must not overlap q or the cache.
+    workspace: a CUDA tensor (allocated here when not given). No gradient is recorded."""
     r = (_calls or _native()).attention(q, k_cache, v_cache, page_table, lengths, starts, 0, window, sinks, scale, max_new, out,
                                         None if stream is None else stream.cuda_stream, workspace)
     if type(r) is int:

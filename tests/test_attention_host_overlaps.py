@@ -4,7 +4,7 @@ import ctypes
 import pytest
 
 import paper_2407_19644_b200 as ubp
-from test_attention_host import APPEND, P, cache
+from test_attention_host import APPEND, ATTEND, P, cache
 
 D, ROW = 64, 8 * 64          # a row of 4 query heads, 2 key heads and 2 value heads
 
@@ -22,3 +22,9 @@ def call(fn, base, c=None, **at):
                                          (2 * ROW, 4 * D, D), (8, 4 * D, D)])
 def test_queries_over_rows(place, ts, hs):
     assert call(ubp.load().ubp_rotate_append, APPEND, _13=P + 2 * place, _14=ts, _15=hs) == -1
+
+
+# place of the outputs behind q, in elements
+@pytest.mark.parametrize("place,ts,hs", [(0, 4 * D, D), (0, ROW, D), (8, 4 * D, D), (D, 4 * D, D), (-4 * D, 4 * D, D), (8 * D, 4 * D, D), (8 * D, 100 * D, D), (3 * D, 4 * D, 2 * D)])
+def test_outputs_over_queries(place, ts, hs):
+    assert call(ubp.load().ubp_attention, ATTEND, _11=P + 2 * place, _12=ts, _13=hs) == -1

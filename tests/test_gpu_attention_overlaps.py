@@ -1,8 +1,11 @@
 """Outputs that lie over inputs: refused where rows would be read after they were written, allowed otherwise."""
+import ctypes
+
 import pytest
 import torch
 
 from attention_ref import BF16, Batch
+from test_gpu_attention_paths import described
 
 pytestmark = pytest.mark.gpu
 
@@ -63,3 +66,40 @@ def test_append_allows_what_lies_apart(ubp):
     assert torch.equal(run(flat[:b.T * width].view(b.T, width), flat[b.T * width:].view(b.T, HQ, D)), want)
     outside = torch.empty(HQ, b.T, D, dtype=BF16, device="cuda")                          # heads outside tokens
     assert torch.equal(run(whole[:, :width].clone(), outside.transpose(0, 1)), want)
+
+
+def c_attention(ubp, b, q, out, room):
+    c = described(b)
+    ptr = lambda t: ctypes.c_void_p(t.data_ptr())
+    stride = lambda t: (t.stride(0), t.stride(1))
+    return ubp.load().ubp_attention(ctypes.byref(c), ptr(q), *stride(q), b.T, HQ, 0.125, 0, 0, 0, b.T, ptr(out), *stride(out), ptr(room), room.numel(),
+                                    ctypes.c_void_p(torch.cuda.current_stream().cuda_stream))
+
+
+def test_attention_refuses_outputs_over_queries(ubp):
+    b = Batch([70, 30], [170, 40], HQ, HKV, D, BF16, 16)
+    whole = buffer(b, 2 * HQ * D)
+    room = torch.empty(1 << 24, dtype=torch.uint8, device="cuda")
+    heads = lambda start, ts, hs: whole.view(-1)[start:].as_strided((b.T, HQ, D), (ts, hs, 1))
+    q, keep = heads(0, 2 * HQ * D, D), whole.clone()
+    for out in (q, heads(8, 2 * HQ * D, D), heads(D, 2 * HQ * D, D), heads(0, HQ * D, D), heads(0, 2 * HQ * D, 2 * D), heads(D, 2 * HQ * D, 2 * D),
+                heads(D // 2, 2 * HQ * D, 2 * D)):
+        assert c_attention(ubp, b, q, out, room) == -1
+        assert code_of(ubp, lambda: ubp.ubp_attention(q, *b.args(), starts=b.starts, out=out)) == -1
+    assert torch.equal(whole, keep)
+
+
+def test_attention_allows_outputs_beside_queries(ubp):
+    b = Batch([70, 30], [170, 40], HQ, HKV, D, BF16, 16)
+    whole = buffer(b, 2 * HQ * D)
+    pairs = lambda x: (x[:, :HQ * D].unflatten(1, (HQ, D)), x[:, HQ * D:].unflatten(1, (HQ, D)))            # side by side, either first
+    turns = lambda x: x.view(b.T, HQ, 2, D).unbind(2)                                                        # head by head
+    outer = lambda x: x.view(2 * HQ, b.T, D).transpose(0, 1).split(HQ, 1)                                    # heads outside tokens
+    behind = lambda x: x.view(2 * b.T, HQ, D).split(b.T)
+    for layout in (pairs, turns, outer, behind):
+        for first in (0, 1):
+            x = whole.clone()
+            q, out = layout(x)[first], layout(x)[1 - first]
+            want = ubp.ubp_attention(q.clone(memory_format=torch.contiguous_format), *b.args(), starts=b.starts)
+            before = q.clone()
+            assert torch.equal(ubp.ubp_attention(q, *b.args(), starts=b.starts, out=out), want) and torch.equal(q, before)
