@@ -232,6 +232,16 @@ inline bool places_meet(const HeadPlaces &a, const HeadPlaces &b, int64_t T)
             if (pieces_meet(d + h * a.hs - g * b.hs, a.w, b.w, a.ts, T)) return true;
     return false;
 }
+// whether heads of different tokens share elements
+inline bool places_repeat(const HeadPlaces &a, int64_t T)
+{
+    if (T == 1) return false;
+    if (a.n == 1) return a.ts < a.w;
+    if (a.ts >= (a.n - 1) * a.hs + a.w || a.hs >= (T - 1) * a.ts + a.w) return false;
+    for (int64_t h = 1; h < a.n; ++h)
+        if (pieces_meet(h * a.hs, a.w, a.w, a.ts, T)) return true;
+    return false;
+}
 
 // ---- launches; both kernels follow the same scheme and leave the same partial results
 int launch_attn_few(const AttnArgs &a, int dtype, int grid, void *stream);       // 16 rows an item (ubp_attention_few.cu)

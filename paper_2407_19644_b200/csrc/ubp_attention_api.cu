@@ -208,7 +208,8 @@ extern "C" int ubp_attention(const ubp_cache_t *cache, const void *q, int64_t q_
     const int D = cache->head_dim;
     if ((q_heads > 1 && (q_head_stride < D || out_head_stride < D)) || (T > 1 && (q_token_stride < D || out_token_stride < D))) return UBP_E_ARG;
     // (blocks read whole groups' queries, of other tokens and heads than they have written)
-    if (places_meet(HeadPlaces(out, out_token_stride, out_head_stride, q_heads, D), HeadPlaces(q, q_token_stride, q_head_stride, q_heads, D), T)) return UBP_E_ARG;
+    const HeadPlaces to(out, out_token_stride, out_head_stride, q_heads, D);
+    if (places_repeat(to, T) || places_meet(to, HeadPlaces(q, q_token_stride, q_head_stride, q_heads, D), T)) return UBP_E_ARG;
     AttnCall p;
     if (const int rc = attn_plan(cache, q, q_token_stride, q_head_stride, T, q_heads, scale, window, sinks, prefix, max_new, p)) return rc;
     if (p.bytes && (!workspace || !on(workspace, 256))) return UBP_E_ARG;

@@ -369,8 +369,9 @@ extern "C" int ubp_rotate_append(const ubp_cache_t *cache, const void *qkv, int6
     if ((T > 1 && (ld < width || q_token_stride < D)) || (q_heads > 1 && q_head_stride < D)) return UBP_E_ARG;
     // (blocks read rows that others may have written already: the queries' own place in qkv, where a head is read and written by the same
     // threads, or a place apart)
+    const HeadPlaces to(q, q_token_stride, q_head_stride, q_heads, D);
     const bool own = q == qkv && (T == 1 || q_token_stride == ld) && (q_heads == 1 || q_head_stride == D);
-    if (!own && places_meet(HeadPlaces(q, q_token_stride, q_head_stride, q_heads, D), HeadPlaces(qkv, ld, 0, 1, width), T)) return UBP_E_ARG;
+    if (places_repeat(to, T) || (!own && places_meet(to, HeadPlaces(qkv, ld, 0, 1, width), T))) return UBP_E_ARG;
     HeadArgs a{};
     a.qkv = qkv; a.ld = ld; a.q_gamma = q_gamma; a.k_gamma = k_gamma; a.eps = eps;
     a.rot = rotation; a.ldrot = rotation_stride; a.positions = (int)std::min<int64_t>(positions, INT32_MAX); a.r = rotation ? rotated : 0;

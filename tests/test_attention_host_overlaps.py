@@ -1,4 +1,4 @@
-"""The C entry points of the attention operators refuse outputs over inputs, without a GPU."""
+"""The C entry points of the attention operators refuse outputs over inputs and over themselves, without a GPU."""
 import ctypes
 
 import pytest
@@ -28,3 +28,10 @@ def test_queries_over_rows(place, ts, hs):
 @pytest.mark.parametrize("place,ts,hs", [(0, 4 * D, D), (0, ROW, D), (8, 4 * D, D), (D, 4 * D, D), (-4 * D, 4 * D, D), (8 * D, 4 * D, D), (8 * D, 100 * D, D), (3 * D, 4 * D, 2 * D)])
 def test_outputs_over_queries(place, ts, hs):
     assert call(ubp.load().ubp_attention, ATTEND, _11=P + 2 * place, _12=ts, _13=hs) == -1
+
+
+@pytest.mark.parametrize("ts,hs", [(D, D), (2 * D, D), (3 * D, D), (D, 2 * D), (4 * D - 8, D), (3 * D, 2 * D)])
+def test_outputs_over_themselves(ts, hs):
+    far = 1 << 30
+    assert call(ubp.load().ubp_rotate_append, APPEND, _13=far, _14=ts, _15=hs) == -1
+    assert call(ubp.load().ubp_attention, ATTEND, _11=far, _12=ts, _13=hs) == -1

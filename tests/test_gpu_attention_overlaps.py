@@ -1,4 +1,4 @@
-"""Outputs that lie over inputs: refused where rows would be read after they were written, allowed otherwise."""
+"""Outputs that lie over inputs, or over themselves: refused where rows would be read after they were written, allowed otherwise."""
 import ctypes
 
 import pytest
@@ -103,3 +103,18 @@ def test_attention_allows_outputs_beside_queries(ubp):
             want = ubp.ubp_attention(q.clone(memory_format=torch.contiguous_format), *b.args(), starts=b.starts)
             before = q.clone()
             assert torch.equal(ubp.ubp_attention(q, *b.args(), starts=b.starts, out=out), want) and torch.equal(q, before)
+
+
+def test_outputs_over_themselves(ubp):
+    """Heads that share places with the heads of other tokens."""
+    b = Batch([70, 30], [170, 40], HQ, HKV, D, BF16, 16)
+    qkv, q = buffer(b, (HQ + 2 * HKV) * D), b.queries()
+    buf = torch.full((1 << 17,), 5.0, dtype=BF16, device="cuda")
+    for ts, hs in ((D, D), (2 * D, D), (3 * D, D), (D, 2 * D), (3 * D, 2 * D), (4 * D - 8, D), (D, 99 * D), (8 * D, 4 * D + 8)):
+        out = buf.as_strided((b.T, HQ, D), (ts, hs, 1))
+        assert code_of(ubp, lambda: ubp.ubp_rotate_append(qkv, HQ, *b.args(), starts=b.starts, out=out)) == -1
+        assert code_of(ubp, lambda: ubp.ubp_attention(q, *b.args(), starts=b.starts, out=out)) == -1
+    assert (buf == 5.0).all()
+    want = ubp.ubp_attention(q, *b.args(), starts=b.starts)
+    for ts, hs in ((4 * D, D), (D, 100 * D), (9 * D, 2 * D), (2 * D, 201 * D), (8 * D, 4 * D + 32)):
+        assert torch.equal(ubp.ubp_attention(q, *b.args(), starts=b.starts, out=buf.as_strided((b.T, HQ, D), (ts, hs, 1))), want)
