@@ -183,6 +183,7 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
         }
     };
     FewCopies<DP> copies;
+    bool ok = true;                         // no wait has run out: a stage whose copy has not come is not copied to again
     int st = 0;                             // stage of the next step
     uint32_t phase = 0;
     auto start = [&] {                      // the first copies of a share
@@ -192,7 +193,7 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
 #pragma unroll 1
         for (int s = 0; s < ST - 1; ++s) {
             const int to = st + s < ST ? st + s : st + s - ST;
-            copies.issue(a, &tmK, &tmV, ring + (uint32_t)to * 2 * PART, smem_u32(&bar_full[warp][to]), warp, lane);
+            if (ok) copies.issue(a, &tmK, &tmV, ring + (uint32_t)to * 2 * PART, smem_u32(&bar_full[warp][to]), warp, lane);
         }
     };
     if constexpr (!CLUSTER) start();
@@ -205,7 +206,7 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
 
     float o[2 * NK][4], m[2], l[2];
     int tile0 = 0, before = 0;              // of the segment: its first tile, the share's steps before it
-    bool ok = true, described = false, over = true, any = false;      // over: a segment has ended (or the first one begins); any: there was one
+    bool described = false, over = true, any = false;      // over: a segment has ended (or the first one begins); any: there was one
     while (true) {
         if (over) {
             // The segment before has ended: its warps' sums meet, rows 0 .. 7, then 8 .. 15 where the item has them. Before that, the
@@ -308,8 +309,10 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
         }
         __syncwarp();                       // (all lanes have read the stage that is copied to now)
         const int nx = st == 0 ? ST - 1 : st - 1;
-        copies.issue(a, &tmK, &tmV, ring + (uint32_t)nx * 2 * PART, smem_u32(&bar_full[warp][nx]), warp, lane);
-        if (ok) ok = attn_wait(smem_u32(&bar_full[warp][st]), phase, &abort_flag);
+        if (ok) {
+            copies.issue(a, &tmK, &tmV, ring + (uint32_t)nx * 2 * PART, smem_u32(&bar_full[warp][nx]), warp, lane);
+            ok = attn_wait(smem_u32(&bar_full[warp][st]), phase, &abort_flag);
+        }
         const int j0 = attn_tile_at(cur.t, cur.tile) * (FEW_WARPS * KEYS) + warp * KEYS;
         const uint32_t base = ring + (uint32_t)st * 2 * PART;
         if (ok && j0 < cur.t.end && j0 + KEYS > a.kv0 && (j0 + KEYS > cur.t.w0 || j0 < a.sinks)) {
