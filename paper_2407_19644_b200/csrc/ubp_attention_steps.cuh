@@ -255,10 +255,8 @@ template <typename T, int N> __device__ __forceinline__ void attn_store(T *p, co
         for (int i = 0; i < N; ++i) p[i] = from_f32<T>(v[i]);
     }
 }
-// What a finished row's sums are multiplied with, and the product: 0 where nothing was seen (the sums may hold 0 times infinity then).
-__device__ __forceinline__ float attn_scale(float L) { return L == 0.f ? 0.f : 1.f / L; }
-__device__ __forceinline__ float attn_scaled(float o, float scale) { return scale == 0.f ? 0.f : o * scale; }
-// Finished sums of a row, from column col on, to the output.
+// Finished sums of a row, from column col on, to the output: o / L, 0 where nothing was seen. (A single part's sums of such a row may hold
+// 0 times infinity; attn_add and attn_add_all leave them out.)
 template <typename T, int N> __device__ __forceinline__ void attn_finish(const AttnArgs &a, int token, int head, int col, float M, float L, float (&o)[N])
 {
     if (a.pml) {
@@ -268,9 +266,9 @@ template <typename T, int N> __device__ __forceinline__ void attn_finish(const A
         attn_load(a.ppo + at * a.D + col, v);
         attn_add(M, L, o, ml.x, ml.y, v);
     }
-    const float r = attn_scale(L);
+    const float r = L == 0.f ? 0.f : 1.f / L;
 #pragma unroll
-    for (int i = 0; i < N; ++i) o[i] = attn_scaled(o[i], r);
+    for (int i = 0; i < N; ++i) o[i] *= r;
     attn_store(static_cast<T *>(a.out) + token * a.o_ts + head * a.o_hs + col, o);
 }
 

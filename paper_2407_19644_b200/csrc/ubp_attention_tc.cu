@@ -371,7 +371,7 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                         tmem_wait_ld();
                         float v[8], M = m, L = l;
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(o[e]);
+                        for (int e = 0; e < 8; ++e) v[e] = l == 0.f ? 0.f : __uint_as_float(o[e]);
                         if (token >= 0) attn_finish<T>(a, token, head, d, M, L, v);
                     }
                 } else {
@@ -402,7 +402,9 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                     };
                     uint32_t o[2][32], w[32];
                     if (complete) {
-                        const float scale = attn_scale(l);
+                        // (a row that saw nothing gives 0, whatever 0 times the values of others' keys is)
+                        const float scale = l == 0.f ? 0.f : 1.f / l;
+                        auto scaled = [&](uint32_t x) { return l == 0.f ? 0.f : __uint_as_float(x) * scale; };
 #pragma unroll 1
                         for (int d = 0; d < a.D; d += 64) {
                             tmem_ld32(t_o + (uint32_t)d, o[0]);
@@ -410,8 +412,7 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                             tmem_wait_ld();
 #pragma unroll
                             for (int e = 0; e < 32; ++e)
-                                w[e] = pack2<T>(attn_scaled(__uint_as_float(o[e / 16][2 * e & 31]), scale),
-                                                attn_scaled(__uint_as_float(o[e / 16][(2 * e & 31) + 1]), scale));
+                                w[e] = pack2<T>(scaled(o[e / 16][2 * e & 31]), scaled(o[e / 16][(2 * e & 31) + 1]));
                             store(w, d * 2, (a.D - d) * 2);
                         }
                     } else {
