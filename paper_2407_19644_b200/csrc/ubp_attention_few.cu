@@ -183,17 +183,18 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
         }
     };
     FewCopies<DP> copies;
-    bool ok = true;                         // no wait has run out: a stage whose copy has not come is not copied to again
+    bool ok = true;                         // no wait has run out
     int st = 0;                             // stage of the next step
     uint32_t phase = 0;
     auto start = [&] {                      // the first copies of a share
         copies.s = steps;
+        if (!ok) copies.s.left = 0;
         copies.item(a);
-        if (steps.left > 0) copies.peek(a, warp);
+        if (copies.s.left > 0) copies.peek(a, warp);
 #pragma unroll 1
         for (int s = 0; s < ST - 1; ++s) {
             const int to = st + s < ST ? st + s : st + s - ST;
-            if (ok) copies.issue(a, &tmK, &tmV, ring + (uint32_t)to * 2 * PART, smem_u32(&bar_full[warp][to]), warp, lane);
+            copies.issue(a, &tmK, &tmV, ring + (uint32_t)to * 2 * PART, smem_u32(&bar_full[warp][to]), warp, lane);
         }
     };
     if constexpr (!CLUSTER) start();
@@ -309,9 +310,10 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
         }
         __syncwarp();                       // (all lanes have read the stage that is copied to now)
         const int nx = st == 0 ? ST - 1 : st - 1;
-        if (ok) {
-            copies.issue(a, &tmK, &tmV, ring + (uint32_t)nx * 2 * PART, smem_u32(&bar_full[warp][nx]), warp, lane);
-            ok = attn_wait(smem_u32(&bar_full[warp][st]), phase, &abort_flag);
+        copies.issue(a, &tmK, &tmV, ring + (uint32_t)nx * 2 * PART, smem_u32(&bar_full[warp][nx]), warp, lane);
+        if (ok && !attn_wait(smem_u32(&bar_full[warp][st]), phase, &abort_flag)) {
+            ok = false;
+            copies.s.left = 0;              // (a stage whose copy has not come is not copied to again)
         }
         const int j0 = attn_tile_at(cur.t, cur.tile) * (FEW_WARPS * KEYS) + warp * KEYS;
         const uint32_t base = ring + (uint32_t)st * 2 * PART;
