@@ -489,7 +489,8 @@ int ubp_linear(const ubp_linear_plan_t *plan, const void *x, int64_t ldx, const 
  * key head h / (q_heads / kv_heads).
  * Errors of both calls: UBP_E_ARG (null, sizes, strides, alignment, q_heads not a multiple of kv_heads, batch != T without
  * starts, types, rows to be written of q or out that share elements), UBP_E_UNSUPPORTED (head_dim not a multiple of 8 or above
- * 128, page_size not a power of two or below 8), UBP_E_SPACE, UBP_E_CUDA. T == 0 is a no-op. */
+ * 128, page_size not a power of two or below 8, more than 2^31 - 4097 tokens or sequences), UBP_E_SPACE, UBP_E_CUDA. T == 0 is a
+ * no-op. */
 typedef struct {
     void *k, *v;                                    /* device */
     int64_t page_stride, head_stride, token_stride; /* elements */

@@ -42,7 +42,9 @@ int check_cache(const ubp_cache_t *c, int64_t T, int q_heads)
     if (q_heads % c->kv_heads) return UBP_E_ARG;
     if (!c->starts && c->batch != T) return UBP_E_ARG;
     if (c->head_dim % 8 || c->head_dim > 128 || c->page_size < 8 || (c->page_size & (c->page_size - 1))) return UBP_E_UNSUPPORTED;
-    if (T > INT32_MAX || c->batch >= INT32_MAX || c->pages > INT32_MAX) return UBP_E_UNSUPPORTED;
+    // (the kernels count tokens and sequences in 32 bits, up to a block's or a warp's share past the last one)
+    constexpr int64_t most = INT32_MAX - 4096;
+    if (T > most || c->batch > most || c->pages > INT32_MAX) return UBP_E_UNSUPPORTED;
     if (T == 0 || c->batch == 0) return UBP_OK;
     if (!c->k || !c->v || !c->table || !c->lengths) return UBP_E_ARG;
     if (!on(c->k, 16) || !on(c->v, 16) || !on(c->table, 4) || !on(c->lengths, 4) || !on(c->starts, 4)) return UBP_E_ARG;

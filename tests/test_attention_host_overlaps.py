@@ -1,4 +1,4 @@
-"""The C entry points of the attention operators refuse outputs over inputs and over themselves, without a GPU."""
+"""The C entry points of the attention operators refuse outputs over inputs and over themselves, and sizes near 2^31, without a GPU."""
 import ctypes
 
 import pytest
@@ -35,3 +35,11 @@ def test_outputs_over_themselves(ts, hs):
     far = 1 << 30
     assert call(ubp.load().ubp_rotate_append, APPEND, _13=far, _14=ts, _15=hs) == -1
     assert call(ubp.load().ubp_attention, ATTEND, _11=far, _12=ts, _13=hs) == -1
+
+
+@pytest.mark.parametrize("n", [(1 << 31) - 4096, (1 << 31) - 100, (1 << 31) - 2])
+def test_counts_near_the_end_of_32_bits(n):
+    L, many, long = ubp.load(), cache(batch=n, starts=P), cache(starts=P)
+    far = 1 << 60
+    assert call(L.ubp_rotate_append, APPEND, many, _13=far) == -6 and call(L.ubp_rotate_append, APPEND, long, _3=n, _13=far) == -6
+    assert call(L.ubp_attention, ATTEND, many, _11=far) == -6 and call(L.ubp_attention, ATTEND, long, _4=n, _11=far) == -6
