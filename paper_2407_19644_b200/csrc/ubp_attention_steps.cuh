@@ -28,7 +28,7 @@ template <> struct AttnRef<__half> { static constexpr float lift = 7.f, lag = 5.
 template <int NT> struct AttnPlace { int warp[2][32]; int pre[NT + 1]; int b, rt, before, from, to; };
 
 // The block's share of the steps, from its first one on. Called by all threads of the block, NT of them (a
-// multiple of 32); false, to all of them, if there is nothing to do. Row blocks (of all sequences, a thread each) are counted and
+// multiple of 32); false, to all of them, if there is nothing to do (or the steps of a unit head pass 32 bits). Row blocks (of all sequences, a thread each) are counted and
 // summed in parallel, for one unit head: all of a sequence's have equal steps, so that step x lies in the sequence that x / HU lies in.
 template <int NT>
 __device__ __forceinline__ bool attn_locate(const AttnArgs &a, AttnPlace<NT> &sh, AttnDeal &deal, AttnSteps &steps)
@@ -46,6 +46,7 @@ __device__ __forceinline__ bool attn_locate(const AttnArgs &a, AttnPlace<NT> &sh
         return x;
     };
     auto begin = [&](int64_t total) {
+        if (total > INT_MAX) return false;      // (only starts that do not ascend get there: see the host's limit)
         deal = AttnDeal(total * a.HU, (int)gridDim.x);
         if (c >= deal.grid) return false;
         first = deal.first(c);
