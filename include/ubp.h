@@ -484,9 +484,12 @@ int ubp_linear(const ubp_linear_plan_t *plan, const void *x, int64_t ldx, const 
  * a call's T rows are the tokens at positions lengths[b] - n .. lengths[b] - 1, n = starts[b + 1] - starts[b]; without starts
  * every sequence has one new token (batch == T). lengths, starts and table are device memory, read when the work runs: a captured
  * call follows them. Rows from starts[batch] on belong to no sequence: their outputs are left as they were.
- * Numbers on the device that make no sense do no harm: starts are cut to 0 .. T, lengths to 0 .. table_width * page_size; a page
- * outside 0 .. pages - 1 reads as zeros and is not written; with starts that do not ascend, rows that several sequences claim have
- * the result for one of them, or are left as they were. kv_heads divides the number of query heads; query head h goes with
+ * Numbers on the device that make no sense do no harm: starts are cut to 0 .. T; a page outside 0 .. pages - 1 reads as zeros and
+ * is not written; with starts that do not ascend, rows that several sequences claim have the result for one of them, or are left
+ * as they were; negative lengths count as 0. A sequence that has outgrown its table (lengths[b] > table_width * page_size) loses
+ * none of its cache: ubp_rotate_append takes its tokens' positions as they are and appends those that the table has a place for.
+ * ubp_attention cuts the length to the table, which gives the new tokens other positions than they were rotated for: its outputs
+ * for them are numbers, but not attention's. kv_heads divides the number of query heads; query head h goes with
  * key head h / (q_heads / kv_heads).
  * Errors of both calls: UBP_E_ARG (null, sizes, strides, alignment, q_heads not a multiple of kv_heads, batch != T without
  * starts, types, rows to be written of q or out that share elements), UBP_E_UNSUPPORTED (head_dim not a multiple of 8 or above

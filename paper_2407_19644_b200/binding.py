@@ -748,7 +748,8 @@ def ubp_rotate_append(qkv, q_heads: int, k_cache, v_cache, page_table, lengths, 
     each query and key head (where a gamma [head size] is given), position rotation, append. Returns the queries [T][q_heads][head
     size]; `out` may be their own place in qkv, and must not overlap it otherwise.
     k_cache, v_cache: bfloat16 or float16 [pages][kv heads][page size][head size], with equal strides. page_table: int32
-    [sequences][pages of a sequence]; lengths: int32 [sequences], the new tokens among them; starts: int32 [sequences + 1], the rows
+    [sequences][pages of a sequence]; lengths: int32 [sequences], the new tokens among them (no more than the table's row holds: what
+    lies behind it is not appended, and attention sees the row's tokens only); starts: int32 [sequences + 1], the rows
     of sequence b are starts[b] .. starts[b + 1] - 1 and hold its last tokens (None: one new token a sequence). Rows from
     starts[-1] on are left alone. rotation: float32 [positions][rotated], cosines and sines (rotation_table); interleaved: pairs
     (2 i, 2 i + 1) instead of (i, i + rotated / 2). No gradient is recorded."""

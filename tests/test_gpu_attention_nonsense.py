@@ -40,3 +40,24 @@ def test_starts_that_do_not_ascend(ubp):
     q = b.queries()
     want, tol = b.exact(q)
     check(ubp.ubp_attention(q, *b.args(), starts=b.starts), want, tol, b.T)
+
+
+@pytest.mark.parametrize("pad", [0, 3])
+def test_a_sequence_that_has_outgrown_its_table(ubp, pad):
+    """Its tokens keep their positions, those behind the table's end are not appended, and none takes an earlier one's place."""
+    b = Batch([3, 2], [50, 20], 2, 1, 64, BF16, 16)            # (64 places each)
+    b.len_t[0] = 66                                             # positions 63, 64, 65
+    buf = torch.randn(5, 4 * 64 + pad, generator=b.g, device="cuda").to(BF16)
+    qkv, rot = buf[:, :4 * 64], ubp.rotation_table(80, 64)
+    b.table[0] = torch.tensor([0, 1, 2, 3], dtype=torch.int32)
+    b.table[1, 0:2] = torch.tensor([4, 5], dtype=torch.int32)
+    b.table[1, 2:] = -1
+    b.k.zero_()
+    q = ubp.ubp_rotate_append(qkv, 2, *b.args(), starts=b.starts, rotation=rot)
+    changed = (b.k != 0).any(3)[:, 0]
+    assert changed.nonzero().tolist() == [[3, 15], [5, 2], [5, 3]]
+    wide = torch.cat([b.table, torch.full((2, 1), -1, dtype=torch.int32, device="cuda")], 1)
+    assert torch.equal(ubp.ubp_rotate_append(qkv, 2, b.k, b.v, wide, b.len_t, starts=b.starts, rotation=rot), q)
+    for max_new in (None, 1):
+        out = ubp.ubp_attention(b.queries(), b.k, b.k, b.table, b.len_t, starts=b.starts, max_new=max_new)
+        assert torch.isfinite(out).all()
