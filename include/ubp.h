@@ -528,7 +528,8 @@ int ubp_rotate_append(const ubp_cache_t *cache, const void *qkv, int64_t ld, int
  * A query that sees no key (p < 0) gives 0. prefix > 0: the caller states that the first `prefix` tokens are the same for all
  * sequences (the result is that of prefix == 0 up to rounding). Pages that they fill are read through row 0 of the table, what they
  * fill of a last page through row 0 or the sequence's own; they are read once for all sequences together where that is faster
- * than again for each, and then count as seen by all of them. max_new: most new tokens of a sequence, if the caller knows (else T); only the choice of kernel depends on it.
+ * than again for each, and then count as seen by all of them. max_new: most new tokens of a sequence, if the caller knows (else T);
+ * only the choice of kernel depends on it.
  * scale > 0. Strides of q and out are between tokens and heads, in elements; heads are contiguous; no alignment beyond the
  * type's (queries off 16 bytes are copied to the workspace first). out must not overlap q (UBP_E_ARG; so does an out among q's rows
  * with another stride between tokens) or the cache.
@@ -536,7 +537,7 @@ int ubp_rotate_append(const ubp_cache_t *cache, const void *qkv, int64_t ld, int
  * below 2^-21 of the row's largest to steps of 2^-31 of it or finer).
  * Sums run in an order fixed by the lengths: results are bitwise reproducible. What the cache holds outside the tokens that some
  * query of a sequence sees does not reach its outputs, infinities and NaNs included. An infinity or NaN in a value that some new
- * tokens of a sequence see and others do not may make these NaN too.
+ * tokens of a sequence see and others do not may make these NaN too (not those that see no key: they give 0).
  * workspace: device, 256-byte aligned, ubp_attention_workspace_size bytes (same arguments; NULL if that is 0); its contents need
  * not be set and belong to one call at a time. */
 /* ubp_attention_choice: which kernel a call takes for the sequences' own tokens, and for the shared prefix (-1 without one): 0 =

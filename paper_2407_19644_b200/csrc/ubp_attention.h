@@ -11,9 +11,9 @@
 // which only the device knows. An item that ends up with several blocks is joined by a second kernel from their partial results.
 // An item counts for `extra` steps more than its tiles: what its beginning and end take. Without them, blocks that got many short
 // items (the first rows of a prompt, short sequences of a batch) took twice as long as the others. (With the heads inside the row
-// blocks, prompts of eight key heads ran at 757 TFLOP/s instead of 1197: the blocks at work then read eight times as many
-// different keys at a time.) For few sequences and short work a cluster of blocks takes all of an item instead; items of 256 rows with few
-// tiles are left whole.
+// blocks, a long prompt of eight key heads took 1.58 times as long, in an early form of the kernel: the blocks at work then read
+// eight times as many different keys at a time.) For few sequences and short work a cluster of blocks takes all of an item instead;
+// items of few tiles are left whole.
 #ifndef UBP_ATTENTION_H_
 #define UBP_ATTENTION_H_
 

@@ -38,7 +38,8 @@ int check_cache(const ubp_cache_t *c, int64_t T, int q_heads)
 {
     if (!c) return UBP_E_ARG;
     if (c->dtype != UBP_BF16 && c->dtype != UBP_F16) return UBP_E_ARG;
-    if (c->batch < 0 || T < 0 || c->kv_heads < 1 || q_heads < 1 || c->head_dim < 1 || c->page_size < 1 || c->pages < 1 || c->table_width < 1) return UBP_E_ARG;
+    if (c->batch < 0 || T < 0 || c->kv_heads < 1 || q_heads < 1 || c->head_dim < 1) return UBP_E_ARG;
+    if (c->page_size < 1 || c->pages < 1 || c->table_width < 1) return UBP_E_ARG;
     if (q_heads % c->kv_heads) return UBP_E_ARG;
     if (!c->starts && c->batch != T) return UBP_E_ARG;
     if (c->head_dim % 8 || c->head_dim > 128 || c->page_size < 8 || (c->page_size & (c->page_size - 1))) return UBP_E_UNSUPPORTED;
@@ -100,7 +101,8 @@ struct AttnCall {
     size_t q_bytes = 0, bytes = 0;      // queries off 16 bytes are copied first
 };
 
-int attn_plan(const ubp_cache_t *c, const void *q, int64_t q_ts, int64_t q_hs, int64_t T, int q_heads, float scale, int window, int sinks, int64_t prefix, int64_t max_new, AttnCall &p)
+int attn_plan(const ubp_cache_t *c, const void *q, int64_t q_ts, int64_t q_hs, int64_t T, int q_heads, float scale, int window, int sinks,
+              int64_t prefix, int64_t max_new, AttnCall &p)
 {
     const int sms = device_sms();
     AttnArgs a{};
@@ -122,7 +124,8 @@ int attn_plan(const ubp_cache_t *c, const void *q, int64_t q_ts, int64_t q_hs, i
     const int64_t items = (a.T / a.tpt + (int64_t)a.B) * a.HU;
     const int64_t tiles = (seen >> a.bsh) + 2 + a.extra;
     // (the kernels count the steps of a unit head, and a block's, in 32 bits)
-    if (items / a.HU > INT32_MAX / tiles || ((a.cap >> a.bsh) + 2) > INT32_MAX / a.HU || items * tiles / sms >= INT32_MAX) return UBP_E_UNSUPPORTED;
+    if (items / a.HU > INT32_MAX / tiles || ((a.cap >> a.bsh) + 2) > INT32_MAX / a.HU || items * tiles / sms >= INT32_MAX)
+        return UBP_E_UNSUPPORTED;
     p.own_grid = (int)std::min<int64_t>(sms, items * tiles);
     if (!on(q, 16) || (T > 1 && q_ts % 8) || (q_heads > 1 && q_hs % 8)) p.q_bytes = ((size_t)T * q_heads * a.D * 2 + 255) / 256 * 256;
     p.bytes = p.q_bytes;
@@ -186,7 +189,8 @@ extern "C" size_t ubp_attention_workspace_size(const ubp_cache_t *cache, const v
     return ubp::attn_plan(cache, q, q_token_stride, q_head_stride, T, q_heads, 1.f, window, sinks, prefix, max_new, p) ? 0 : p.bytes;
 }
 
-extern "C" int ubp_attention_choice(const ubp_cache_t *cache, int64_t T, int q_heads, int64_t prefix, int64_t max_new, int *kernel, int *prefix_kernel)
+extern "C" int ubp_attention_choice(const ubp_cache_t *cache, int64_t T, int q_heads, int64_t prefix, int64_t max_new, int *kernel,
+                                    int *prefix_kernel)
 {
     using namespace ubp;
     if (const int rc = check_attention(cache, T, q_heads, 1.f, 0, 0, prefix, max_new)) return rc;

@@ -213,12 +213,16 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
             // The segment before has ended: its warps' sums meet, rows 0 .. 7, then 8 .. 15 where the item has them. Before that, the
             // next item's queries are sent for. (Once in the code: a call of a few steps is bound by fetching instructions.)
             if (CLUSTER && !any) start();
-            const int c = (int)blockIdx.x, nr = any ? imin(imin(a.tpt, cur.q.n - cur.rt * a.tpt) * a.gc, FEW_ROWS) : 0, n = cur.tile + 1 - tile0, now = which;
+            const int c = (int)blockIdx.x, n = cur.tile + 1 - tile0, now = which;
+            const int nr = any ? imin(imin(a.tpt, cur.q.n - cur.rt * a.tpt) * a.gc, FEW_ROWS) : 0;
             const bool whole = n == cur.t.nt && !a.common;
             int64_t slot = 2 * (int64_t)c + (before > 0 ? 1 : 0);
             if (a.common) slot = (int64_t)cur.hu * attn_row_blocks(a, cur.q) + cur.rt + c;
             if (any) {
-                if (!CLUSTER && threadIdx.x == 0 && !a.common && tile0 == 0 && !whole) { attn_describe(a, cur, deal, c, before, tile0, n); described = true; }
+                if (!CLUSTER && threadIdx.x == 0 && !a.common && tile0 == 0 && !whole) {
+                    attn_describe(a, cur, deal, c, before, tile0, n);
+                    described = true;
+                }
                 if (!CLUSTER || steps.left > 0) steps.advance(a, 1);
                 which ^= 1;
 #pragma unroll
@@ -234,7 +238,8 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
                 if (i) __syncthreads();
 #pragma unroll
                 for (int k = 0; k < 2 * NK; ++k)
-                    *reinterpret_cast<float2 *>(meet + (warp * 8 + g) * DP + k * 8 + tq * 2) = i ? make_float2(o[k][2], o[k][3]) : make_float2(o[k][0], o[k][1]);
+                    *reinterpret_cast<float2 *>(meet + (warp * 8 + g) * DP + k * 8 + tq * 2) =
+                        i ? make_float2(o[k][2], o[k][3]) : make_float2(o[k][0], o[k][1]);
                 __syncthreads();
                 constexpr int N = 4, TPR = DP / N;          // threads a row
                 const int r = (int)threadIdx.x / TPR, col = (int)threadIdx.x % TPR * N;
@@ -355,7 +360,8 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
                 for (int x = lane; x < KEYS * DP / 8; x += 32) {
                     const int r = x / (DP / 8), ch = x % (DP / 8), j = j0 + r;
                     if (!(j >= a.kv0 && j < cur.t.end && (j >= cur.t.w0 || j < a.sinks)))
-                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(base + PART + (uint32_t)(ch / 8) * PANEL + (uint32_t)(r * 128 + ch % 8 * 16)), "r"(0) : "memory");
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};"
+                                     ::"r"(base + PART + (uint32_t)(ch / 8) * PANEL + (uint32_t)(r * 128 + ch % 8 * 16)), "r"(0) : "memory");
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");      // (before the next copy to these places)
                 __syncwarp();

@@ -27,9 +27,9 @@ template <> struct AttnRef<__half> { static constexpr float lift = 7.f, lag = 5.
 // Shared memory of attn_locate, for blocks of NT threads.
 template <int NT> struct AttnPlace { int warp[2][32]; int pre[NT + 1]; int b, rt, before, from, to; };
 
-// The block's share of the steps, from its first one on. Called by all threads of the block, NT of them (a
-// multiple of 32); false, to all of them, if there is nothing to do (or the steps of a unit head pass 32 bits). Row blocks (of all sequences, a thread each) are counted and
-// summed in parallel, for one unit head: all of a sequence's have equal steps, so that step x lies in the sequence that x / HU lies in.
+// The block's share of the steps, from its first one on. Called by all threads of the block, NT of them (a multiple of 32); false, to all
+// of them, if there is nothing to do (or the steps of a unit head pass 32 bits). Row blocks (of all sequences, a thread each) are counted
+// and summed in parallel, for one unit head: all of a sequence's have equal steps, so that step x lies in the sequence that x / HU lies in.
 template <int NT>
 __device__ __forceinline__ bool attn_locate(const AttnArgs &a, AttnPlace<NT> &sh, AttnDeal &deal, AttnSteps &steps)
 {

@@ -213,14 +213,19 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
             for (; ok && sg.get(); sg.done(a)) {
                 const int kvh = sg.s.c.hu / a.chunks;
                 const AttnTiles &t = sg.s.c.t;
-                auto page_of = [&](int i) { return lane < nbox ? attn_box_page(a, t, sg.s.c.b, attn_tile_at(t, sg.s.c.tile + i) * AT_BN + lane * box, box) : a.pages; };      // (a lane a box)
+                auto page_of = [&](int i) {     // (a lane a box)
+                    return lane < nbox ? attn_box_page(a, t, sg.s.c.b, attn_tile_at(t, sg.s.c.tile + i) * AT_BN + lane * box, box) : a.pages;
+                };
                 int page = page_of(0);
                 for (int i = 0; i < sg.n; ++i, ++filled) {
                     const int st = filled % ST, j0 = attn_tile_at(t, sg.s.c.tile + i) * AT_BN, ahead = i + 1 < sg.n ? page_of(i + 1) : 0;
                     // Places of a page whose keys no row sees: whatever they hold, a weight of 0 times it has to be 0, so the values
                     // there are overwritten with zeros before the product reads them.
-                    const bool patch = values && ((j0 + AT_BN > t.end && (t.end & (box - 1))) || (j0 < a.kv0 && j0 + AT_BN > a.kv0 && (a.kv0 & (box - 1))) ||
-                                                  (j0 < t.w0 && j0 + AT_BN > t.w0) || (j0 < a.sinks && j0 + AT_BN > a.sinks && j0 < t.w0));
+                    const int j1 = j0 + AT_BN;
+                    const bool patch = values && ((j1 > t.end && (t.end & (box - 1))) ||                  // the last key
+                                                  (j0 < a.kv0 && j1 > a.kv0 && (a.kv0 & (box - 1))) ||    // the first one of this call
+                                                  (j0 < t.w0 && j1 > t.w0) ||                             // the window
+                                                  (j0 < a.sinks && j1 > a.sinks && j0 < t.w0));           // the first tokens
                     const uint32_t full = smem_u32(&bar_full[st]), dst = ring + (uint32_t)st * PART, bar = patch ? smem_u32(&bars.patch) : full;
                     if (filled >= ST) ok = attn_wait(smem_u32(&bar_empty[st]), (uint32_t)(filled / ST - 1) & 1u, &abort_flag);
                     if (!ok) break;
@@ -241,7 +246,8 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                         for (int x = lane; x < AT_BN * DP / 8; x += 32) {
                             const int r = x / (DP / 8), c = x % (DP / 8), j = j0 + r;
                             if (!(j >= a.kv0 && j < t.end && (j >= t.w0 || j < a.sinks)))
-                                *reinterpret_cast<uint4 *>(smem + (dst - s_q) + (uint32_t)(c / 8) * AT_PANEL + (uint32_t)r * 128u + (uint32_t)(c % 8) * 16u) = make_uint4(0, 0, 0, 0);
+                                *reinterpret_cast<uint4 *>(smem + (dst - s_q) + (uint32_t)(c / 8) * AT_PANEL + (uint32_t)(r * 128 + c % 8 * 16)) =
+                                    make_uint4(0, 0, 0, 0);
                         }
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         __syncwarp();
@@ -427,7 +433,8 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
             }
             if (!live) break;
             // keys that all (existing) rows of the warp see need no comparison
-            const int all_hi = __reduce_min_sync(0xffffffffu, row.token >= 0 ? row.hi : INT_MAX), all_lo = __reduce_max_sync(0xffffffffu, row.token >= 0 ? row.lo : 0);
+            const int all_hi = __reduce_min_sync(0xffffffffu, row.token >= 0 ? row.hi : INT_MAX);
+            const int all_lo = __reduce_max_sync(0xffffffffu, row.token >= 0 ? row.lo : 0);
             m = -INFINITY; l = 0.f;
             for (int j = 0; j < sg.n; ++j) {
                 const int j0 = attn_tile_at(sg.s.c.t, sg.s.c.tile + j) * AT_BN;
@@ -444,7 +451,8 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                     const int first = imax(row.lo, a.kv0) - j0, last = row.hi - j0, early = imin(a.sinks, row.hi) - j0, least = a.kv0 - j0;
 #pragma unroll
                     for (int c = 0; c < 4; ++c) {
-                        const uint32_t seen = (bits_below(last - c * 32) & ~bits_below(first - c * 32)) | (bits_below(early - c * 32) & ~bits_below(least - c * 32));
+                        const uint32_t seen = (bits_below(last - c * 32) & ~bits_below(first - c * 32)) |
+                                              (bits_below(early - c * 32) & ~bits_below(least - c * 32));
 #pragma unroll
                         for (int e = 0; e < 32; ++e)
                             if (!(seen & (1u << e))) s[c][e] = 0xff800000u;
@@ -510,7 +518,10 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
             before = true;
             complete = sg.n == sg.s.c.t.nt && !a.common;
             slot = a.common ? ((int64_t)sg.s.c.hu * attn_row_blocks(a, sg.s.c.q) + sg.s.c.rt) + c : 2 * (int64_t)c + (x > 0 ? 1 : 0);
-            if (warp == AT_SOFT_WARP && lane == 0 && !a.common && sg.s.c.tile == 0 && !complete) { attn_describe(a, sg.s.c, deal, c, x, 0, sg.n); described = true; }
+            if (warp == AT_SOFT_WARP && lane == 0 && !a.common && sg.s.c.tile == 0 && !complete) {
+                attn_describe(a, sg.s.c, deal, c, x, 0, sg.n);
+                described = true;
+            }
             sg.done(a);
         }
         if (warp == AT_SOFT_WARP && lane == 0 && !a.common && !a.whole && !described) a.desc[blockIdx.x] = make_int4(0, 0, 0, 0);
