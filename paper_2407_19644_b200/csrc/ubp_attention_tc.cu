@@ -221,11 +221,10 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                     const int st = filled % ST, j0 = attn_tile_at(t, sg.s.c.tile + i) * AT_BN, ahead = i + 1 < sg.n ? page_of(i + 1) : 0;
                     // Places of a page whose keys no row sees: whatever they hold, a weight of 0 times it has to be 0, so the values
                     // there are overwritten with zeros before the product reads them.
-                    const int j1 = j0 + AT_BN;
-                    const bool patch = values && ((j1 > t.end && (t.end & (box - 1))) ||                  // the last key
-                                                  (j0 < a.kv0 && j1 > a.kv0 && (a.kv0 & (box - 1))) ||    // the first one of this call
-                                                  (j0 < t.w0 && j1 > t.w0) ||                             // the window
-                                                  (j0 < a.sinks && j1 > a.sinks && j0 < t.w0));           // the first tokens
+                    const bool patch = values && ((j0 + AT_BN > t.end && (t.end & (box - 1))) ||                              // the last key
+                                                  (j0 < a.kv0 && j0 + AT_BN > a.kv0 && (a.kv0 & (box - 1))) ||                // the call's first
+                                                  (j0 < t.w0 && j0 + AT_BN > t.w0) ||                                         // the window
+                                                  (j0 < a.sinks && j0 + AT_BN > a.sinks && j0 < t.w0));                       // first tokens
                     const uint32_t full = smem_u32(&bar_full[st]), dst = ring + (uint32_t)st * PART, bar = patch ? smem_u32(&bars.patch) : full;
                     if (filled >= ST) ok = attn_wait(smem_u32(&bar_empty[st]), (uint32_t)(filled / ST - 1) & 1u, &abort_flag);
                     if (!ok) break;
@@ -246,8 +245,8 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                         for (int x = lane; x < AT_BN * DP / 8; x += 32) {
                             const int r = x / (DP / 8), c = x % (DP / 8), j = j0 + r;
                             if (!(j >= a.kv0 && j < t.end && (j >= t.w0 || j < a.sinks)))
-                                *reinterpret_cast<uint4 *>(smem + (dst - s_q) + (uint32_t)(c / 8) * AT_PANEL + (uint32_t)(r * 128 + c % 8 * 16)) =
-                                    make_uint4(0, 0, 0, 0);
+                                *reinterpret_cast<uint4 *>(smem + (dst - s_q) + (uint32_t)(c / 8) * AT_PANEL + (uint32_t)r * 128u +
+                                                           (uint32_t)(c % 8) * 16u) = make_uint4(0, 0, 0, 0);
                         }
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         __syncwarp();
