@@ -534,7 +534,8 @@ int ubp_rotate_append(const ubp_cache_t *cache, const void *qkv, int64_t ld, int
  * type's (queries off 16 bytes are copied to the workspace first). out must not overlap q (UBP_E_ARG; so does an out among q's rows
  * with another stride between tokens) or the cache.
  * Scores, sums and outputs are fp32 until the end; the weights w_j are rounded to the cache's type for the product with v (f16: those
- * below 2^-21 of the row's largest to steps of 2^-31 of it or finer).
+ * below 2^-21 of the row's largest to steps of 2^-31 of it or finer). Scores of 2^27 (f16) or 2^30 (bf16) and more may give NaN: one
+ * unit of theirs is then more than the weights' range.
  * Sums run in an order fixed by the lengths: results are bitwise reproducible. What the cache holds outside the tokens that some
  * query of a sequence sees does not reach its outputs, infinities and NaNs included. An infinity or NaN in a value that some new
  * tokens of a sequence see and others do not may make these NaN too (not those that see no key: they give 0).

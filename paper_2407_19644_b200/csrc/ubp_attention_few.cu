@@ -373,14 +373,14 @@ ubp_attention_few_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_c
 #pragma unroll
                 for (int n = 1; n < NB; ++n) mx[i] = fmaxf(mx[i], fmaxf(s[n][2 * i], s[n][2 * i + 1]));
                 mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 1));
-                mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 2)) * a.sc;
+                mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 2));
             }
             // (the reference: see AttnRef)
             constexpr float LIFT = AttnRef<T>::lift, LAG = AttnRef<T>::lag;
-            if (__any_sync(0xffffffffu, mx[0] > m[0] + (LIFT + LAG) || mx[1] > m[1] + (LIFT + LAG))) {
+            if (__any_sync(0xffffffffu, fmaf(mx[0], a.sc, -m[0]) > LIFT + LAG || fmaf(mx[1], a.sc, -m[1]) > LIFT + LAG)) {
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    const float to = fmaxf(m[i], mx[i] - LIFT), f = m[i] == -INFINITY ? 0.f : attn_exp2(m[i] - to);
+                    const float to = fmaxf(m[i], fmaf(mx[i], a.sc, -LIFT)), f = m[i] == -INFINITY ? 0.f : attn_exp2(m[i] - to);
                     m[i] = to;
                     l[i] *= f;
 #pragma unroll

@@ -19,8 +19,9 @@ __device__ __forceinline__ float attn_exp2(float x)
 // 2^lift or more. In bf16 a weight has the same relative error wherever it lies. f16 has 2^-24 as its smallest step, and the sum of
 // weights takes them unrounded: with the reference at the largest score, a first token far above the rest whose value is near 0
 // (8192 keys, scores N(0, 1), the first one 14 / 16 / 18 above 0) left relative errors of 0.008 / 0.05 / 0.3; 2^7 higher, 0.0004 /
-// 0.0006 / 0.0044, where unrounded weights give 0.0002 / 0.0006 / 0.0040 (the outputs' rounding). 2^12 leaves f16 a factor of 2^4 below its
-// overflow for the rounding of very large scores (one unit of theirs where they are 2^24).
+// 0.0006 / 0.0044, where unrounded weights give 0.0002 / 0.0006 / 0.0040 (the outputs' rounding). What is compared with `lag` is the
+// exponent as it is computed, by one fused product and difference, so that only the reference's own rounding, half a unit of the
+// scores, can lift a weight: with scores (of base 2) below 2^28 f16's stay below their overflow, below 2^31 bf16's.
 template <typename T> struct AttnRef { static constexpr float lift = 0.f, lag = 8.f; };
 template <> struct AttnRef<__half> { static constexpr float lift = 7.f, lag = 5.f; };
 

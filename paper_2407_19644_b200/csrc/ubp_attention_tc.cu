@@ -466,10 +466,10 @@ ubp_attention_tc_kernel(const __grid_constant__ CUtensorMap tmK, const __grid_co
                     mx[c] = fmaxf(mx[c], __uint_as_float(s[c][31]));
                 }
                 // (a row that does not exist holds whatever was there: it has no say in when the others' sums are rescaled)
-                const float top = row.token >= 0 ? fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * a.sc : -INFINITY;
+                const float top = row.token >= 0 ? fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) : -INFINITY;
                 constexpr float LIFT = AttnRef<T>::lift, LAG = AttnRef<T>::lag;
-                if (__any_sync(0xffffffffu, top > m + (LIFT + LAG))) {
-                    const float to = fmaxf(m, top - LIFT), f = m == -INFINITY ? 0.f : attn_exp2(m - to);
+                if (__any_sync(0xffffffffu, fmaf(top, a.sc, -m) > LIFT + LAG)) {
+                    const float to = fmaxf(m, fmaf(top, a.sc, -LIFT)), f = m == -INFINITY ? 0.f : attn_exp2(m - to);
                     m = to;
                     l *= f;
                     if (j > 0) {
